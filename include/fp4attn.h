@@ -48,13 +48,17 @@ enum {
   FP4ATTN_ERR_CUDA = 6,               /* a CUDA runtime / driver call failed                   */
   FP4ATTN_ERR_TIMEOUT = 7,            /* written to *device_status by a kernel whose bounded
                                          wait ran out; never returned synchronously            */
-  FP4ATTN_ERR_RANGE = 8               /* written to *device_status by a kernel running with a
+  FP4ATTN_ERR_RANGE = 8,              /* written to *device_status by a kernel running with a
                                          fixed row reference when a block exponent or a whole row
                                          fell outside the E8M0 range around it; never returned
                                          synchronously                                          */
+  FP4ATTN_ERR_PAGE = 9                /* written to *device_status by a kernel that was to use a token without a page: a
+                                         position outside the block table, or an entry that names no page of the
+                                         cache; never returned synchronously                    */
 };
 
-enum { FP4ATTN_FMT_MXFP4 = 0, FP4ATTN_FMT_NVFP4 = 1 };
+enum { FP4ATTN_FMT_MXFP4 = 0, FP4ATTN_FMT_NVFP4 = 1,
+       FP4ATTN_FMT_E4M3 = 2 };        /* of a cache only (fp4attn_cache), no format of fp4attn_quantize                 */
 enum { FP4ATTN_REFERENCE_RUNNING = 0, FP4ATTN_REFERENCE_FIXED = 1 };
 enum { FP4ATTN_ROLE_Q = 0, FP4ATTN_ROLE_K = 1, FP4ATTN_ROLE_V = 2 };
 /* how a normalised score x = y - E_B + log2 6 becomes an E2M1 probability code */
@@ -404,6 +408,104 @@ int fp4attn_softmax_arith_probe(int p_map, int exact_pairs, int iters, unsigned 
  * returns normally; the context stays usable.
  */
 int fp4attn_selftest_bounded_wait(long long limit_cycles, int* device_status, fp4attn_stream_t stream);
+
+/* ------------------------------------------------------------------ serving: positions, cache, attention over it
+ * (no counterpart in the paper, whose operators take whole sequences)
+ */
+enum { FP4ATTN_TYPE_BF16 = 0, FP4ATTN_TYPE_FP16 = 1, FP4ATTN_TYPE_FP32 = 2 };
+
+/* A tensor [B, heads, N, d] whose last axis is contiguous; the other strides are in elements and free (0 for an input that is
+ * broadcast).  16-byte accesses where the address and the strides allow them, single elements otherwise. */
+typedef struct {
+  void* data;
+  long long stride_b, stride_h, stride_n;
+} fp4attn_view;
+
+/*
+ * Rotary positions on Q and K in one launch (kv_heads = 0: on Q alone, k and k_out may be NULL).
+ *
+ * The first 2 * pairs elements of a head are rotated, the rest are carried over.  Pair i is elements (i, i + pairs), or (2i, 2i + 1)
+ * if interleaved.  With theta = positions[b, n] * inv_freq[i] (product and reduction in 64 bits: positions of a million lose
+ * nothing), c = fl32(factor * cos theta), s = fl32(factor * sin theta):
+ *     y1 = fl32(x1 c) - fl32(x2 s),  y2 = fl32(x2 c) + fl32(x1 s), each difference and sum rounded to fp32 and then to the type.
+ * transposed: s is negated - the gradient of the inputs from the gradient of the outputs (and, at factor 1, the inverse).
+ * Scaled positions (longer contexts than trained on) are a matter of inv_freq and factor.
+ *
+ * type: FP4ATTN_TYPE_BF16, _FP16 or _FP32, of all four tensors.  positions int32 [B, N], inv_freq fp32 [pairs] (device).
+ * d up to 256, 2 * pairs <= d.  An output may be its own input (the same view), not overlap it in another way.
+ */
+int fp4attn_rotary(const fp4attn_view* q, const fp4attn_view* k, const fp4attn_view* q_out, const fp4attn_view* k_out, int type,
+                   int B, int H, int kv_heads, int N, int d, const int* positions, const float* inv_freq, int pairs,
+                   int interleaved, int transposed, float factor, fp4attn_stream_t stream);
+
+/*
+ * A paged cache of quantized K and V: pages u8 [num_pages, kv_heads, record], record = fp4attn_cache_record_bytes(), 16-byte
+ * aligned; k_G, v_G fp32 [kv_heads] (device), positive and finite, fixed before the first write (2688 / max|x| of calibration
+ * data for NVFP4, 448 / max|x| for E4M3: larger values saturate).  page_size 16, 32, 64 or 128 tokens; d 64 or 128.
+ *
+ * A (page, head) record of P tokens is K codes, K scales, V codes, V scales:
+ *   NVFP4  K codes [d/32][P][16]: byte j of chunk c of token t = elements 32c + 2j (bits 0-3) and 32c + 2j + 1; K scales [P][d/16];
+ *          V codes [P/16][d/2][16]: byte (g, i, t) = elements 2i (bits 0-3) and 2i + 1 of token 16g + t;
+ *          V scales [d/16][P], the tokens of each aligned eight in the order 0 4 1 5 2 6 3 7.
+ *          Blocks of 16 elements of a token: S = E4M3(fl32(fl32(max|x| G) / 6)), codes E2M1(fl32(x fl32(G / S))) (0 where S is 0),
+ *          as fp4attn_quantize; a value is code * S / G.
+ *   E4M3   K [d/16][P][16]: byte j of chunk c = element 16c + j; V [P/16][d][16]: byte (g, i, t) = element i of token 16g + t;
+ *          no scales.  Byte E4M3(fl32(x G)), saturating at 448; a value is byte / G.
+ * NaN is written as 0, infinities saturate: a cache holds finite values only.
+ *
+ * A sequence's tokens stand at positions 0, 1, ...: position p of batch entry b in page block_table[b, p / page_size]
+ * (int32 [B, max_pages], device).  A position without a page is skipped and reported (FP4ATTN_ERR_PAGE in *device_status, which may
+ * be NULL and which the caller clears).  MXFP4 is no format of a cache: attention keeps K and V as 16-bit floats in the tensor core,
+ * which E8M0 scales leave.
+ */
+typedef struct {
+  void* pages;
+  const float* k_G;
+  const float* v_G;
+  int fmt;                            /* FP4ATTN_FMT_NVFP4 or FP4ATTN_FMT_E4M3                                            */
+  int page_size, num_pages, kv_heads, d;
+} fp4attn_cache;
+
+/* Bytes of a (page, head) record; 0 for what is not supported. */
+size_t fp4attn_cache_record_bytes(int fmt, int page_size, int d);
+
+/*
+ * Quantizes K and V [B, kv_heads, N, d] (type FP4ATTN_TYPE_BF16 or _FP16) into the pages: token n of batch entry b at position
+ * start[b] + n, for n < count[b] (int32 [B]; NULL: all N).  Nothing else of the pages is written.  No two tokens of a call
+ * may stand at one place (pages shared between sequences are not written).
+ * With pairs > 0, K is rotated first as by fp4attn_rotary at positions[b, n] (NULL: at start[b] + n) and rounded to its type,
+ * which gives the same bytes as the two calls.
+ */
+int fp4attn_cache_write(const fp4attn_cache* cache, const fp4attn_view* k, const fp4attn_view* v, int type, int B, int N,
+                        const int* block_table, int max_pages, const int* start, const int* count, const int* positions,
+                        const float* inv_freq, int pairs, int interleaved, float factor, int* device_status, fp4attn_stream_t stream);
+
+/* The values of positions start[b] .. start[b] + count[b] - 1 (count NULL: N of them) as K and V [B, kv_heads, N, d]; rows behind
+ * them are left as they were, rows without a page are zero.  A value is fl32(code * S * fl32(1 / G)), rounded to the type. */
+int fp4attn_cache_read(const fp4attn_cache* cache, const fp4attn_view* k_out, const fp4attn_view* v_out, int type, int B, int N,
+                       const int* block_table, int max_pages, const int* start, const int* count, int* device_status,
+                       fp4attn_stream_t stream);
+
+/*
+ * Attention of T query tokens of every sequence over its cache: q [B, H, T, d] (bf16 or fp16), O [B, H, T, d] of that type,
+ * contiguous, LSE fp32 [B, H, T] (may be NULL), natural logarithm.  Head h reads KV head h / (H / kv_heads).
+ *
+ * The sequence's first context[b] tokens are seen by every row.  The T tokens themselves stand in the cache behind them, at
+ * positions context[b] + j, and row t sees those whose bit j of tree_mask[b, t] is set (u64 [B, T]: a tree of drafted tokens;
+ * NULL: j <= t).  T = 1 is the step of one token.  count (int32 [B], NULL: T): rows t >= count[b] are not written.
+ * A row that sees nothing is O = 0, LSE = -infinity.  Positions without a page are seen by no row, and reported.  Bytes of
+ * positions that no row sees may hold anything.
+ *
+ * Scores, row maxima and sums are fp32; K, V and Q enter the products exactly (as f16, Q scaled by a power of two per row),
+ * probabilities rounded to f16.  softmax_scale 0: 1 / sqrt(d).  T up to 64.  workspace: device memory of the queried size,
+ * 16-byte aligned, for this call alone until it has run.
+ */
+enum { FP4ATTN_MOST_TREE_TOKENS = 64 };
+size_t fp4attn_tree_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d);
+int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, const int* block_table,
+                           int max_pages, const int* context, const int* count, const unsigned long long* tree_mask,
+                           float softmax_scale, void* O, float* LSE, int* device_status, void* workspace, size_t workspace_bytes,
+                           fp4attn_stream_t stream);
 
 #ifdef __cplusplus
 }

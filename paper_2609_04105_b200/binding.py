@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import importlib.machinery
 import importlib.util
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional, Tuple
@@ -30,7 +31,7 @@ SCHEDULE_ONE_QUERY, SCHEDULE_TWO_QUERY, SCHEDULE_AUTO = 0, 1, 2
 PV_MXFP4, PV_E4M3 = 0, 1
 QSCALE_CEIL, QSCALE_THR16, QSCALE_FLOOR, QSCALE_MSE = 0, 1, 2, 3
 (OK, ERR_INVALID_ARG, ERR_UNSUPPORTED_SHAPE, ERR_UNSUPPORTED_ARCH, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA,
- ERR_TIMEOUT, ERR_RANGE) = range(9)
+ ERR_TIMEOUT, ERR_RANGE, ERR_PAGE) = range(10)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfp4attn.so")
@@ -43,6 +44,8 @@ EXPORTS = [
     "fp4attn_quantize_nvfp4_noalloc", "fp4attn_selftest_bounded_wait", "fp4attn_quantize_mxfp4_rule",
     "fp4attn_quantize_nvfp4_per_head_workspace_bytes", "fp4attn_quantize_nvfp4_per_head", "fp4attn_release",
     "fp4attn_quantize_v_e4m3_workspace_bytes", "fp4attn_quantize_v_e4m3",
+    "fp4attn_rotary", "fp4attn_cache_record_bytes", "fp4attn_cache_write", "fp4attn_cache_read",
+    "fp4attn_tree_attention_workspace_bytes", "fp4attn_tree_attention",
 ]
 
 
@@ -99,6 +102,8 @@ def _load() -> ctypes.CDLL:
     lib.fp4attn_quantize_nvfp4_per_head_workspace_bytes.argtypes = [i, i, i, i]
     lib.fp4attn_quantize_nvfp4_per_head.restype = i
     lib.fp4attn_quantize_nvfp4_per_head.argtypes = [vp, i, i, i, i, i, vp, vp, vp, vp, sz, vp]
+    lib.fp4attn_cache_record_bytes.restype = sz
+    lib.fp4attn_cache_record_bytes.argtypes = [i, i, i]
     lib.fp4attn_selftest_bounded_wait.restype = i
     lib.fp4attn_selftest_bounded_wait.argtypes = [ctypes.c_longlong, vp, vp]
     lib.fp4attn_mma_peak_probe.restype = i
@@ -112,7 +117,8 @@ def _load() -> ctypes.CDLL:
 _NATIVE_CALLS = ["fp4attn_status_string", "fp4attn_packed_bytes", "fp4attn_scale_bytes", "fp4attn_quantize_workspace_bytes",
                  "fp4attn_quantize", "fp4attn_quantize_mxfp4_rule", "fp4attn_quantize_nvfp4_per_head_workspace_bytes",
                  "fp4attn_quantize_nvfp4_per_head", "fp4attn_quantize_v_e4m3_workspace_bytes", "fp4attn_quantize_v_e4m3",
-                 "fp4attn_fwd"]
+                 "fp4attn_fwd", "fp4attn_rotary", "fp4attn_cache_record_bytes", "fp4attn_cache_write", "fp4attn_cache_read",
+                 "fp4attn_tree_attention_workspace_bytes", "fp4attn_tree_attention"]
 
 
 def _load_native(lib_: ctypes.CDLL):
@@ -197,7 +203,7 @@ def fp4attn_quantize_nvfp4_noalloc(x: torch.Tensor, role: int, packed: torch.Ten
     return QuantizedOperand(packed, scales, G, FMT_NVFP4, role, (B, H, N, d))
 
 
-FMT_E4M3 = 2          # QuantizedOperand.fmt of an E4M3 V (fp4attn_quantize_v_e4m3); not a format of the C quantize calls
+FMT_E4M3 = 2          # of an E4M3 V (fp4attn_quantize_v_e4m3) and of a cache; not a format of the C quantize calls
 
 
 def fp4attn_quantize_v_e4m3(x: torch.Tensor) -> QuantizedOperand:
@@ -219,6 +225,110 @@ def fp4attn_fwd(q: QuantizedOperand, k: QuantizedOperand, v: QuantizedOperand, s
     fixed_reference: None - running row reference; an integer - that constant row reference (the shiftless path)."""
     return (_native_module or _native()).fwd(q, k, v, softmax_scale, out, lse, status, p_map, affine_a, affine_b, p_scale_rule, causal,
                                              exact_pairs, schedule, seq_len, fixed_reference)
+
+
+def fp4attn_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                               trained_length: int = 0, fast_turns: float = 32.0, slow_turns: float = 1.0,
+                               device="cuda") -> torch.Tensor:
+    """inv_freq, fp32 [rot_dim / 2]: base^(-2i / rot_dim), for contexts `factor` times as long as trained on scaled by
+      "linear"    every frequency / factor
+      "base"      base * factor^(rot_dim / (rot_dim - 2)): the slowest pair slows down by `factor`, the fastest not at all
+      "by_parts"  pairs that turn at least `fast_turns` times over trained_length keep their frequency, those that turn at most
+                  `slow_turns` times are divided by `factor`, in between by the share of the way (in turns)."""
+    if rot_dim < 2 or rot_dim % 2 or not factor > 0.0 or not base > 0.0:
+        raise ValueError("rot_dim must be even and positive, base and factor positive")
+    if scaling == "base":
+        if rot_dim == 2:
+            raise ValueError('scaling "base" needs two pairs or more')
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    f = base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "by_parts":
+        if trained_length <= 0 or not fast_turns > slow_turns:
+            raise ValueError('scaling "by_parts" needs trained_length, and fast_turns above slow_turns')
+        turns = trained_length * f / (2.0 * math.pi)
+        kept = ((turns - slow_turns) / (fast_turns - slow_turns)).clamp(0.0, 1.0)
+        f = f * kept + f / factor * (1.0 - kept)
+    elif scaling not in (None, "base"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return f.float().to(device)
+
+
+def fp4attn_rotary(q: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, k: Optional[torch.Tensor] = None,
+                   interleaved: bool = False, attention_factor: float = 1.0, q_out: Optional[torch.Tensor] = None,
+                   k_out: Optional[torch.Tensor] = None):
+    """Rotary positions on q [B,H,N,d], and on k [B,Hkv,N,d] in the same launch -> q_out, or (q_out, k_out).
+    bf16, fp16 or fp32, any strides but the last axis'; positions CUDA int32 [B,N]; inv_freq CUDA fp32 [pairs], for the first
+    2 * pairs elements of a head, in halves or (interleaved) as neighbours; cos and sin are multiplied by attention_factor.
+    An output may be its own input."""
+    return (_native_module or _native()).rotary(q, k, positions, inv_freq, interleaved, False, attention_factor, q_out, k_out)
+
+
+def fp4attn_rotary_backward(dq: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, k: Optional[torch.Tensor] = None,
+                            interleaved: bool = False, attention_factor: float = 1.0, q_out: Optional[torch.Tensor] = None,
+                            k_out: Optional[torch.Tensor] = None):
+    """The gradients of fp4attn_rotary's inputs from those of its outputs, dq and (as k) dk: the transposed rotation."""
+    return (_native_module or _native()).rotary(dq, k, positions, inv_freq, interleaved, True, attention_factor, q_out, k_out)
+
+
+@dataclass
+class QuantizedCache:
+    """A paged cache of quantized K and V (layout: include/fp4attn.h).  The factors are fixed before the first write."""
+    pages: torch.Tensor               # uint8 [pages, KV heads, bytes of a record]
+    k_G: torch.Tensor                 # fp32 [KV heads]: 2688 (NVFP4) or 448 (E4M3) / the largest magnitude expected
+    v_G: torch.Tensor
+    fmt: int                          # FMT_NVFP4 or FMT_E4M3
+    page_size: int                    # tokens: 16, 32, 64 or 128
+    d: int
+
+
+def fp4attn_cache_record_bytes(fmt: int, page_size: int, d: int) -> int:
+    """Bytes that a page takes per KV head; 0 for what is not supported."""
+    return lib().fp4attn_cache_record_bytes(fmt, page_size, d)
+
+
+def fp4attn_cache_create(num_pages: int, page_size: int, d: int, fmt: int, k_G: torch.Tensor, v_G: torch.Tensor) -> QuantizedCache:
+    """An empty cache of num_pages pages on the factors' device, one KV head per factor."""
+    record = fp4attn_cache_record_bytes(fmt, page_size, d)
+    if not record:
+        raise Fp4AttnError("fp4attn_cache_create: a cache is NVFP4 or E4M3, d 64 or 128, pages of 16, 32, 64 or 128 tokens")
+    pages = torch.zeros((num_pages, k_G.numel(), record), dtype=torch.uint8, device=k_G.device)
+    return QuantizedCache(pages, k_G, v_G, fmt, page_size, d)
+
+
+def fp4attn_cache_write(cache: QuantizedCache, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor, start: torch.Tensor,
+                        count: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+                        positions: Optional[torch.Tensor] = None, interleaved: bool = False, attention_factor: float = 1.0,
+                        status: Optional[torch.Tensor] = None) -> None:
+    """Quantizes k, v [B,Hkv,N,d] (bf16 or fp16, any strides but the last axis') into the pages of block_table (int32 [B, pages of a
+    sequence]): token n of entry b at position start[b] + n, for n < count[b] (int32 [B]; None: all).  With inv_freq, k is rotated
+    first, at positions [B,N] or (None) at the tokens' places.  `status` (int32 [1], cleared by the caller) receives ERR_PAGE if a
+    token had no page; such a token is skipped."""
+    (_native_module or _native()).cache_write(cache, k, v, block_table, start, count, positions, inv_freq, interleaved,
+                                              attention_factor, status)
+
+
+def fp4attn_cache_read(cache: QuantizedCache, block_table: torch.Tensor, start: torch.Tensor, N: int,
+                       count: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                       k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The values of N tokens of every sequence from position start[b] on -> (K, V) [B,Hkv,N,d], bf16 or fp16.  Rows n >= count[b] are
+    left as they were (zero in a tensor that this call made)."""
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise AssertionError("dtype must be torch.bfloat16 or torch.float16")
+    return (_native_module or _native()).cache_read(cache, block_table, start, N, count, dtype == torch.float16, k_out, v_out, status)
+
+
+def fp4attn_tree_attention(q: torch.Tensor, cache: QuantizedCache, block_table: torch.Tensor, context: torch.Tensor,
+                           tree_mask: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                           softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                           status: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of T <= 64 tokens of every sequence over the cache: q [B,H,T,d] (bf16 or fp16) -> (O of q's type [B,H,T,d], LSE fp32
+    [B,H,T]).  The T tokens are in the cache, behind the first context[b] (int32 [B]); every row sees those, and of the T tokens those
+    whose bit of tree_mask (int64 [B,T]) is set - None: its own and the ones before it.  A row that sees nothing is 0, its LSE
+    -infinity.  Rows t >= count[b] are left as they were (0 and -infinity in tensors that this call made)."""
+    return (_native_module or _native()).tree_attention(q, cache, block_table, context, tree_mask, count, softmax_scale, out, lse, status)
 
 
 def fp4attn_attention_host_workspace_bytes(qk_fmt: int, B: int, H: int, N: int, d: int) -> int:

@@ -24,18 +24,19 @@ extern "C" const char* fp4attn_status_string(int status) {
   switch (status) {
     case FP4ATTN_OK: return "ok";
     case FP4ATTN_ERR_INVALID_ARG: return "invalid argument";
-    case FP4ATTN_ERR_UNSUPPORTED_SHAPE: return "unsupported shape (d in {64,128}, N a multiple of 128)";
+    case FP4ATTN_ERR_UNSUPPORTED_SHAPE: return "unsupported shape (d in {64,128}, N a multiple of 128; caches: pages of 16, 32, 64 or 128 tokens, up to 64 query tokens)";
     case FP4ATTN_ERR_UNSUPPORTED_ARCH: return "device is not compute capability 10.0";
     case FP4ATTN_ERR_ALIGNMENT: return "pointer alignment";
     case FP4ATTN_ERR_WORKSPACE: return "workspace missing or too small";
     case FP4ATTN_ERR_CUDA: return "CUDA call failed";
     case FP4ATTN_ERR_TIMEOUT: return "bounded in-kernel wait ran out";
     case FP4ATTN_ERR_RANGE: return "logits outside the range of the fixed row reference";
+    case FP4ATTN_ERR_PAGE: return "a token without a page (outside the block table, or an entry outside the cache)";
     default: return "unknown status";
   }
 }
 
-extern "C" int fp4attn_version(void) { return 300; }
+extern "C" int fp4attn_version(void) { return 400; }
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 

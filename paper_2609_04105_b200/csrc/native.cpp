@@ -14,6 +14,8 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <limits>
+
 #include "../../include/fp4attn.h"
 
 namespace {
@@ -30,10 +32,18 @@ struct Api {
   decltype(&fp4attn_quantize_v_e4m3_workspace_bytes) e4m3_workspace_bytes;
   decltype(&fp4attn_quantize_v_e4m3) e4m3;
   decltype(&fp4attn_fwd) fwd;
+  decltype(&fp4attn_rotary) rotary;
+  decltype(&fp4attn_cache_record_bytes) cache_record_bytes;
+  decltype(&fp4attn_cache_write) cache_write;
+  decltype(&fp4attn_cache_read) cache_read;
+  decltype(&fp4attn_tree_attention_workspace_bytes) tree_workspace_bytes;
+  decltype(&fp4attn_tree_attention) tree_attention;
 };
 Api g_api;
 PyObject* g_error = nullptr;                            // Fp4AttnError
 enum { A_PACKED, A_SCALES, A_G, A_FMT, A_ROLE, A_SHAPE, A_PER_HEAD, A_COUNT };
+enum { C_PAGES, C_K_G, C_V_G, C_FMT, C_PAGE_SIZE, C_D, C_COUNT };
+PyObject* g_cache_names[C_COUNT];
 PyObject* g_names[A_COUNT];
 constexpr int kFmtE4m3 = 2;                             // QuantizedOperand.fmt of an E4M3 V
 
@@ -395,7 +405,284 @@ PyObject* py_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
   FP4_CATCH
 }
 
-// init(error class, status_string, packed_bytes, ..., fwd): addresses of the library's functions, in Api's order
+// ---------------------------------------------------------------- serving: positions, cache, attention over it
+
+// A tensor [B, heads, N, d] on a CUDA device, the last axis contiguous
+struct Strided {
+  const at::Tensor* t = nullptr;
+  int B = 0, H = 0, N = 0, d = 0, type = -1;
+  fp4attn_view view{};
+  bool take(PyObject* o, bool fp32) {
+    if (!THPVariable_Check(o)) return false;
+    t = &THPVariable_Unpack(o);
+    if (!t->is_cuda() || t->dim() != 4) return false;
+    type = t->scalar_type() == at::kBFloat16 ? FP4ATTN_TYPE_BF16 : t->scalar_type() == at::kHalf ? FP4ATTN_TYPE_FP16
+         : t->scalar_type() == at::kFloat && fp32 ? FP4ATTN_TYPE_FP32 : -1;
+    const auto s = t->sizes(), st = t->strides();
+    for (int i = 0; i < 4; ++i)
+      if (s[i] > INT32_MAX || s[i] < 1) return false;
+    B = (int)s[0]; H = (int)s[1]; N = (int)s[2]; d = (int)s[3];
+    // an axis of one index may have any stride: it is never taken, and must not spoil the alignment
+    view = {t->data_ptr(), B > 1 ? st[0] : 0, H > 1 ? st[1] : 0, N > 1 ? st[2] : 0};
+    return type >= 0 && (d == 1 || st[3] == 1);
+  }
+  bool like(const Strided& o) const { return B == o.B && N == o.N && d == o.d && type == o.type && t->device() == o.t->device(); }
+  // no two elements at one address (what is written must not be a broadcast)
+  bool distinct() const { return t->is_non_overlapping_and_dense() || spread(); }
+
+ private:
+  bool spread() const {
+    // strides sorted: each at least as long as what the smaller ones span
+    int64_t size[3] = {B, H, N}, stride[3] = {view.stride_b, view.stride_h, view.stride_n}, span = d;
+    for (int k = 0; k < 3; ++k) {
+      int at = -1;
+      for (int i = 0; i < 3; ++i)
+        if (size[i] > 1 && (at < 0 || stride[i] < stride[at])) at = i;
+      if (at < 0) break;
+      if (stride[at] < span) return false;
+      span = stride[at] * (size[at] - 1) + span;
+      size[at] = 1;
+    }
+    return true;
+  }
+};
+// a contiguous tensor of `n` values of `type` on `device`, or None where that is allowed
+bool plain(PyObject* o, at::ScalarType type, int64_t n, c10::Device device, bool optional, void** ptr) {
+  *ptr = nullptr;
+  if (o == Py_None) return optional;
+  if (!THPVariable_Check(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || t.scalar_type() != type || t.numel() != n || !t.is_contiguous() || t.device() != device) return false;
+  *ptr = t.data_ptr();
+  return true;
+}
+
+struct Cache {
+  fp4attn_cache c{};
+  c10::Device device{c10::kCPU};
+  const char* take(PyObject* o) {                        // null, or what is wrong ("": an exception is set)
+    PyObject* v[C_COUNT] = {};
+    const char* wrong = nullptr;
+    for (int i = 0; i < C_COUNT && !wrong; ++i)
+      if (!(v[i] = PyObject_GetAttr(o, g_cache_names[i]))) wrong = "";
+    if (!wrong) wrong = read(v);
+    for (int i = 0; i < C_COUNT; ++i) Py_XDECREF(v[i]);
+    return wrong;
+  }
+
+ private:
+  const char* read(PyObject** v) {
+    if (!THPVariable_Check(v[C_PAGES])) return "cache.pages must be a contiguous CUDA uint8 tensor [pages, KV heads, bytes of a record]";
+    const at::Tensor& t = THPVariable_Unpack(v[C_PAGES]);
+    if (!t.is_cuda() || t.scalar_type() != at::kByte || t.dim() != 3 || !t.is_contiguous() || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX)
+      return "cache.pages must be a contiguous CUDA uint8 tensor [pages, KV heads, bytes of a record]";
+    int a[3];
+    if (!ints(v + C_FMT, 3, a)) return "";
+    c.pages = t.data_ptr();
+    device = t.device();
+    c.num_pages = (int)t.size(0); c.kv_heads = (int)t.size(1);
+    c.fmt = a[0]; c.page_size = a[1]; c.d = a[2];
+    const size_t record = g_api.cache_record_bytes(c.fmt, c.page_size, c.d);
+    if (record && (size_t)t.size(2) != record) return "cache.pages must have fp4attn_cache_record_bytes(fmt, page_size, d) bytes a record";
+    void *kg, *vg;
+    if (!plain(v[C_K_G], at::kFloat, c.kv_heads, device, false, &kg) || !plain(v[C_V_G], at::kFloat, c.kv_heads, device, false, &vg))
+      return "cache.k_G and cache.v_G must be contiguous CUDA float32 tensors with one factor per KV head";
+    c.k_G = (const float*)kg; c.v_G = (const float*)vg;
+    return nullptr;
+  }
+};
+// what the calls over a cache share: table, counts
+struct Batch {
+  const int *table = nullptr, *start = nullptr, *count = nullptr;
+  int max_pages = 0;
+  int* status = nullptr;
+  const char* take(int B, c10::Device device, PyObject* table_o, PyObject* start_o, PyObject* count_o, PyObject* status_o) {
+    if (!THPVariable_Check(table_o)) return "block_table must be a contiguous CUDA int32 tensor [B, pages of a sequence]";
+    const at::Tensor& t = THPVariable_Unpack(table_o);
+    if (!t.is_cuda() || t.scalar_type() != at::kInt || t.dim() != 2 || !t.is_contiguous() || t.size(0) != B || t.size(1) < 1 ||
+        t.size(1) > INT32_MAX || t.device() != device)
+      return "block_table must be a contiguous CUDA int32 tensor [B, pages of a sequence] on the cache's device";
+    table = t.data_ptr<int>();
+    max_pages = (int)t.size(1);
+    void *s, *c, *st;
+    if (!plain(start_o, at::kInt, B, device, false, &s)) return "start / context must be a contiguous CUDA int32 tensor of B positions on the cache's device";
+    if (!plain(count_o, at::kInt, B, device, true, &c)) return "count must be a contiguous CUDA int32 tensor of B counts on the cache's device";
+    if (!plain(status_o, at::kInt, 1, device, true, &st)) return "status must be a CUDA int32 tensor of one element on the cache's device";
+    start = (const int*)s; count = (const int*)c; status = (int*)st;
+    return nullptr;
+  }
+};
+at::Tensor like_view(const Strided& s, c10::Device device) { return device_empty({s.B, s.H, s.N, s.d}, s.t->scalar_type(), device); }
+// an output tensor: what the caller gave, checked, or a new one
+bool output(PyObject* o, const Strided& like, Strided* out, at::Tensor* own) {
+  if (o == Py_None) {
+    *own = like_view(like, like.t->device());
+    out->t = own;
+    out->B = like.B; out->H = like.H; out->N = like.N; out->d = like.d; out->type = like.type;
+    out->view = {own->data_ptr(), own->stride(0), own->stride(1), own->stride(2)};
+    return true;
+  }
+  return out->take(o, true) && out->like(like) && out->H == like.H && out->distinct();
+}
+PyObject* given_or(PyObject* o, const at::Tensor& own) { return o == Py_None ? THPVariable_Wrap(own) : Py_NewRef(o); }
+
+// rotary(q, k, positions, inv_freq, interleaved, transposed, factor, q_out, k_out) -> q_out, or (q_out, k_out)
+PyObject* py_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  FP4_TRY
+  if (n != 9) return assertion("rotary takes 9 arguments");
+  Strided x[2], y[2];
+  at::Tensor own[2];
+  const bool two = args[1] != Py_None;
+  if (!x[0].take(args[0], true) || (two && !(x[1].take(args[1], true) && x[1].like(x[0]))))
+    return assertion("q (and k) must be CUDA tensors [B, heads, N, d], bfloat16, float16 or float32, the last axis contiguous; k of q's B, N, d, type and device");
+  if (!two && args[8] != Py_None) return assertion("k_out is given but k is not");
+  const c10::Device device = x[0].t->device();
+  void *positions, *freq = nullptr;
+  if (!plain(args[2], at::kInt, (int64_t)x[0].B * x[0].N, device, false, &positions))
+    return assertion("positions must be a contiguous CUDA int32 tensor [B, N] on q's device");
+  const int64_t pairs = THPVariable_Check(args[3]) ? THPVariable_Unpack(args[3]).numel() : 0;
+  if (pairs < 1 || pairs > INT32_MAX / 2 || !plain(args[3], at::kFloat, pairs, device, false, &freq))
+    return assertion("inv_freq must be a contiguous CUDA float32 tensor with one frequency per pair on q's device");
+  float factor;
+  const int interleaved = PyObject_IsTrue(args[4]), transposed = PyObject_IsTrue(args[5]);
+  if (interleaved < 0 || transposed < 0 || !number(args[6], &factor)) return nullptr;
+  const c10::cuda::OptionalCUDAGuard guard(device);
+  for (int i = 0; i <= (int)two; ++i)
+    if (!output(args[7 + i], x[i], &y[i], &own[i]))
+      return assertion("an output must be a CUDA tensor of its input's shape, type and device, the last axis contiguous, no element twice");
+  const int rc = unlocked([&] {
+    return g_api.rotary(&x[0].view, two ? &x[1].view : nullptr, &y[0].view, two ? &y[1].view : nullptr, x[0].type, x[0].B, x[0].H, x[1].H,
+                        x[0].N, x[0].d, (const int*)positions, (const float*)freq, (int)pairs, interleaved, transposed, factor, stream());
+  });
+  if (rc) return fail(rc, "fp4attn_rotary");
+  if (!two) return given_or(args[7], own[0]);
+  return Py_BuildValue("(NN)", given_or(args[7], own[0]), given_or(args[8], own[1]));
+  FP4_CATCH
+}
+
+// cache_write(cache, k, v, block_table, start, count, positions, inv_freq, interleaved, factor, status)
+PyObject* py_cache_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  FP4_TRY
+  if (n != 11) return assertion("cache_write takes 11 arguments");
+  Cache cache;
+  if (const char* wrong = cache.take(args[0])) return *wrong ? assertion(wrong) : nullptr;
+  Strided k, v;
+  if (!k.take(args[1], false) || !v.take(args[2], false) || !v.like(k) || v.H != k.H || k.H != cache.c.kv_heads || k.d != cache.c.d ||
+      k.t->device() != cache.device)
+    return assertion("k and v must be CUDA tensors [B, KV heads, N, d] of the cache's heads, d and device, bfloat16 or float16, the last axis contiguous");
+  Batch batch;
+  if (const char* wrong = batch.take(k.B, cache.device, args[3], args[4], args[5], args[10])) return assertion(wrong);
+  void *positions, *freq = nullptr;
+  if (!plain(args[6], at::kInt, (int64_t)k.B * k.N, cache.device, true, &positions))
+    return assertion("positions must be a contiguous CUDA int32 tensor [B, N] on the cache's device");
+  int64_t pairs = 0;
+  if (args[7] != Py_None) {
+    pairs = THPVariable_Check(args[7]) ? THPVariable_Unpack(args[7]).numel() : 0;
+    if (pairs < 1 || pairs > INT32_MAX / 2 || !plain(args[7], at::kFloat, pairs, cache.device, false, &freq))
+      return assertion("inv_freq must be a contiguous CUDA float32 tensor with one frequency per pair on the cache's device");
+  } else if (positions) {
+    return assertion("positions are given but inv_freq is not");
+  }
+  float factor;
+  const int interleaved = PyObject_IsTrue(args[8]);
+  if (interleaved < 0 || !number(args[9], &factor)) return nullptr;
+  const c10::cuda::OptionalCUDAGuard guard(cache.device);
+  const int rc = unlocked([&] {
+    return g_api.cache_write(&cache.c, &k.view, &v.view, k.type, k.B, k.N, batch.table, batch.max_pages, batch.start, batch.count,
+                             (const int*)positions, (const float*)freq, (int)pairs, interleaved, factor, batch.status, stream());
+  });
+  if (rc) return fail(rc, "fp4attn_cache_write");
+  Py_RETURN_NONE;
+  FP4_CATCH
+}
+
+// cache_read(cache, block_table, start, N, count, is float16, k_out, v_out, status) -> (k_out, v_out)
+PyObject* py_cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  FP4_TRY
+  if (n != 9) return assertion("cache_read takes 9 arguments");
+  Cache cache;
+  if (const char* wrong = cache.take(args[0])) return *wrong ? assertion(wrong) : nullptr;
+  if (!THPVariable_Check(args[1]) || THPVariable_Unpack(args[1]).dim() != 2)
+    return assertion("block_table must be a contiguous CUDA int32 tensor [B, pages of a sequence]");
+  const int64_t B = THPVariable_Unpack(args[1]).size(0);
+  int N;
+  if (!ints(args + 3, 1, &N)) return nullptr;
+  const int half = PyObject_IsTrue(args[5]);
+  if (half < 0) return nullptr;
+  if (B < 1 || B > INT32_MAX || N < 1) return assertion("cache_read needs at least one sequence and one token");
+  Batch batch;
+  if (const char* wrong = batch.take((int)B, cache.device, args[1], args[2], args[4], args[8])) return assertion(wrong);
+  const c10::cuda::OptionalCUDAGuard guard(cache.device);
+  const at::ScalarType type = half ? at::kHalf : at::kBFloat16;
+  Strided out[2];
+  at::Tensor own[2];
+  for (int i = 0; i < 2; ++i) {
+    if (args[6 + i] == Py_None) {
+      own[i] = device_empty({B, cache.c.kv_heads, N, cache.c.d}, type, cache.device);
+      if (batch.count) own[i].zero_();                   // rows behind the counts are not written
+      out[i].view = {own[i].data_ptr(), own[i].stride(0), own[i].stride(1), own[i].stride(2)};
+    } else if (!out[i].take(args[6 + i], false) || out[i].t->scalar_type() != type || out[i].B != B || out[i].H != cache.c.kv_heads ||
+               out[i].N != N || out[i].d != cache.c.d || out[i].t->device() != cache.device || !out[i].distinct()) {
+      return assertion("k_out and v_out must be CUDA tensors [B, KV heads, N, d] of the cache's heads, d and device and of dtype, the last axis contiguous, no element twice");
+    }
+  }
+  const int rc = unlocked([&] {
+    return g_api.cache_read(&cache.c, &out[0].view, &out[1].view, half ? FP4ATTN_TYPE_FP16 : FP4ATTN_TYPE_BF16, (int)B, N, batch.table,
+                            batch.max_pages, batch.start, batch.count, batch.status, stream());
+  });
+  if (rc) return fail(rc, "fp4attn_cache_read");
+  return Py_BuildValue("(NN)", given_or(args[6], own[0]), given_or(args[7], own[1]));
+  FP4_CATCH
+}
+
+// tree_attention(q, cache, block_table, context, tree_mask, count, softmax_scale, out, lse, status) -> (out, lse)
+PyObject* py_tree_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  FP4_TRY
+  if (n != 10) return assertion("tree_attention takes 10 arguments");
+  Cache cache;
+  if (const char* wrong = cache.take(args[1])) return *wrong ? assertion(wrong) : nullptr;
+  Strided q;
+  if (!q.take(args[0], false) || q.d != cache.c.d || q.t->device() != cache.device || cache.c.kv_heads < 1 || q.H % cache.c.kv_heads != 0)
+    return assertion("q must be a CUDA tensor [B, H, T, d] of the cache's d and device, bfloat16 or float16, the last axis contiguous; H a multiple of the KV heads");
+  Batch batch;
+  if (const char* wrong = batch.take(q.B, cache.device, args[2], args[3], args[5], args[9])) return assertion(wrong);
+  void *mask, *out_ptr, *lse_ptr;
+  if (!plain(args[4], at::kLong, (int64_t)q.B * q.N, cache.device, true, &mask))
+    return assertion("tree_mask must be a contiguous CUDA int64 tensor [B, T] on the cache's device");
+  float scale;
+  if (!number(args[6], &scale)) return nullptr;
+  const int64_t rows = (int64_t)q.B * q.H * q.N;
+  if (!plain(args[7], q.t->scalar_type(), rows * q.d, cache.device, true, &out_ptr) || !plain(args[8], at::kFloat, rows, cache.device, true, &lse_ptr))
+    return assertion("out [B, H, T, d] of q's type and lse [B, H, T] float32 must be contiguous CUDA tensors on the cache's device");
+  const c10::cuda::OptionalCUDAGuard guard(cache.device);
+  const size_t nw = g_api.tree_workspace_bytes(q.B, q.H, cache.c.kv_heads, q.N, q.d);
+  THPObjectPtr out(Py_NewRef(args[7])), lse(Py_NewRef(args[8]));
+  Results r;
+  at::Tensor none, &o = out_ptr ? none : r.add({q.B, q.H, q.N, q.d}, q.t->scalar_type()), &l = lse_ptr ? none : r.add({q.B, q.H, q.N}, at::kFloat);
+  at::Tensor& ws = nw ? r.add({(int64_t)nw}, at::kByte) : none;
+  r.allocate(cache.device);
+  if (o.defined()) {
+    if (batch.count) o.zero_();                          // rows behind the counts are not written
+    out_ptr = o.data_ptr();
+    out = THPVariable_Wrap(o);
+  }
+  if (l.defined()) {
+    if (batch.count) l.fill_(-std::numeric_limits<float>::infinity());
+    lse_ptr = l.data_ptr();
+    lse = THPVariable_Wrap(l);
+  }
+  if (!out || !lse) return nullptr;
+  const int rc = unlocked([&] {
+    return g_api.tree_attention(&q.view, q.type, &cache.c, q.B, q.H, q.N, batch.table, batch.max_pages, batch.start, batch.count,
+                                (const unsigned long long*)mask, scale, out_ptr, (float*)lse_ptr, batch.status,
+                                nw ? ws.data_ptr() : nullptr, nw, stream());
+  });
+  if (rc) return fail(rc, "fp4attn_tree_attention");
+  return Py_BuildValue("(NN)", out.release(), lse.release());
+  FP4_CATCH
+}
+
+// init(error class, status_string, packed_bytes, ..., tree_attention): addresses of the library's functions, in Api's order
 PyObject* py_init(PyObject*, PyObject* const* args, Py_ssize_t n) {
   constexpr Py_ssize_t kFunctions = sizeof(Api) / sizeof(void*);
   if (n != 1 + kFunctions) return assertion("init takes the error class and one address per function");
@@ -412,7 +699,8 @@ PyObject* py_init(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define FP4_METHOD(NAME, FN) {NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(FN)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FP4_METHOD("init", py_init), FP4_METHOD("quantize", py_quantize), FP4_METHOD("quantize_mxfp4_rule", py_rule),
                          FP4_METHOD("quantize_nvfp4_per_head", py_per_head), FP4_METHOD("quantize_v_e4m3", py_e4m3),
-                         FP4_METHOD("fwd", py_fwd), {nullptr, nullptr, 0, nullptr}};
+                         FP4_METHOD("fwd", py_fwd), FP4_METHOD("rotary", py_rotary), FP4_METHOD("cache_write", py_cache_write),
+                         FP4_METHOD("cache_read", py_cache_read), FP4_METHOD("tree_attention", py_tree_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fp4attn_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -421,5 +709,8 @@ extern "C" __attribute__((visibility("default"))) PyObject* PyInit__fp4attn_nati
   const char* names[A_COUNT] = {"packed", "scales", "G", "fmt", "role", "shape", "per_head"};
   for (int i = 0; i < A_COUNT; ++i)
     if (!(g_names[i] = PyUnicode_InternFromString(names[i]))) return nullptr;
+  const char* cache_names[C_COUNT] = {"pages", "k_G", "v_G", "fmt", "page_size", "d"};
+  for (int i = 0; i < C_COUNT; ++i)
+    if (!(g_cache_names[i] = PyUnicode_InternFromString(cache_names[i]))) return nullptr;
   return PyModule_Create(&module);
 }
