@@ -1,96 +1,797 @@
 // Attention of one token, or of a tree of drafted tokens, of every sequence over its pages of a quantized cache.
 //
 // Row (b, h, t) sees the first context[b] tokens of the sequence, and of the T drafted tokens at positions context[b] ..
-// context[b] + T - 1 those whose bit of its mask is set.  One warp takes a row and walks its keys with a running maximum and sum.
+// context[b] + T - 1 those whose bit of its mask is set.
+//
+// The rows that read one KV head are few (1 to some hundreds), its keys are many, so keys and head dimension take the wide side of the
+// tensor core and rows the narrow one:  S^T = K Q^T (128 keys x R rows),  O^T += V^T P^T (d x R rows), R = 16, 32 or 64.  Their A operands,
+// K and V^T, live in tensor memory: a lane is a key of K, a head-dimension index of V^T, and the thread that turns a lane's
+// codes into f16 writes them there without a word of shared memory.  Only Q and P, the narrow operands, are read from shared memory.
+//
+// One CTA per SM.  The 128-key tiles of all (batch entry, KV head, row tile) items stand in one list, of which every CTA takes an equal
+// run, so that sequences of unlike lengths and few long ones fill the card alike.  An item whose tiles fall to several CTAs is left as
+// partial (maximum, sum, O) in the workspace and joined by a second kernel in the order of its keys.
+//
+//   warps 0-3    K: codes of a key -> f16 -> tensor memory; Q of an item, scaled by a power of two per row, -> f16 -> shared memory
+//   warps 4-7    V: codes of an index, 128 tokens -> f16 -> tensor memory
+//   warps 8-     softmax, a thread per key and 32 (16) rows: maxima, exp2, P^T -> shared memory; rescale of O, end of an item
+//   then         one warp brings the pages in (one bulk copy per page: a (page, head) record is one run of bytes), one issues the products
+//
+// The reference of a row, its maximum at some time, moves only when a score exceeds it by more than 2^8: probabilities up to 256 fit f16 as
+// well, and neither a reduction over keys (they are in lanes) nor a pass over O is then part of an ordinary tile.
 #include "kv_cache.cuh"
+#include "ptx.cuh"
+
+#include <limits.h>
+
+#include <algorithm>
 
 namespace fp4attn {
 
 int check_cache(const fp4attn_cache* c, int B, const int* block_table, int max_pages, const int* start, const int* count, CacheRef* ref);
 
 namespace {
+using namespace ptx;
+
+constexpr int kTile = 128;                 // keys of a tile
+constexpr int kMostCtas = 160;             // partial results: two per CTA
+constexpr float kLag = 8.f;                // octaves by which a score may exceed its row's reference
+constexpr float kShift = 7.f;              // a probability of 1 is 2^7: with the lag just inside f16, whose subnormals then begin at 2^-21
 
 struct TreeParams {
   const void* q;
   long long q_sb, q_sh, q_sn;
   CacheRef cache;
   const int *context, *count;
-  const unsigned long long* mask;    // [B, T] or null: token t sees 0 .. t
-  void* out;                         // [B, H, T, d]
-  float* lse;                        // [B, H, T]
+  const unsigned long long* mask;          // [B, T] or null: token t sees 0 .. t
+  void* out;                               // [B, H, T, d]
+  float* lse;                              // [B, H, T]
   int* status;
-  int B, H, T, group;
+  float* part;                             // [2 * kMostCtas][R][D]
+  float2* part_ml;                         // [2 * kMostCtas][R]: reference, sum
+  int2* split;                             // [items]: first and last CTA of an item in parts; first = -1: whole
+  int B, H, T, group, rows, row_tiles;     // rows = group * T of a KV head
   float scale;
+  bool half, q_vector;
 };
 
-template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(128) tree_row_kernel(const TreeParams p) {
-  using L = RecordLayout<FMT, D>;
-  launch_dependents();
-  wait_prior_grids();
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (row >= (long long)p.B * p.H * p.T) return;
-  const int t = (int)(row % p.T), h = (int)(row / p.T % p.H), b = (int)(row / p.T / p.H), kvh = h / p.group;
-  if (p.count && t >= __ldg(p.count + b)) return;
-  constexpr int E = D / 32;
-  const int P = 1 << p.cache.log_page;
-  const T* q = static_cast<const T*>(p.q) + b * p.q_sb + h * p.q_sh + t * p.q_sn;
-  float qv[E], o[E];
-  for (int i = 0; i < E; ++i) {
-    qv[i] = to_float(q[2 * lane + 64 * (i >> 1) + (i & 1)]);
-    o[i] = 0.f;
-  }
-  const float c = p.scale * 1.4426950408889634f / __ldg(p.cache.k_G + kvh);
-  const unsigned long long bits = p.mask ? __ldg(p.mask + (size_t)b * p.T + t) : (2ull << t) - 1;
-  const int ctx = max(0, __ldg(p.context + b));
-  float m = -INFINITY, l = 0.f;
-  const long long held = (long long)p.cache.max_pages << p.cache.log_page, end = min((long long)ctx + p.T, held);
-  if ((long long)ctx + p.T > held && p.status) *p.status = FP4ATTN_ERR_PAGE;
-  for (long long k = 0; k < end; ++k) {
-    if (k >= ctx && !(bits >> (k - ctx) & 1)) continue;
-    const int page = p.cache.page_of(b, k);
-    if (page < 0) {
-      if (p.status) *p.status = FP4ATTN_ERR_PAGE;
-      continue;
-    }
-    const uint8_t* const rec = p.cache.rec(page, kvh);
-    const int at = (int)(k & (P - 1));
-    float s = 0.f, v[E];
-    for (int i = 0; i < E; ++i) {
-      const int e = 2 * lane + 64 * (i >> 1) + (i & 1);
-      float kv, vv;
-      if (L::kFp4) {
-        const float2 kp = half2_of(cvt_f16x2_e2m1x2<0>(rec[(e / 32 * P + at) * 16 + e % 32 / 2]));
-        const float2 vp = half2_of(cvt_f16x2_e2m1x2<0>(rec[L::v_codes(P) + (at / 16 * L::kRow + e / 2) * 16 + at % 16]));
-        kv = (e & 1 ? kp.y : kp.x) * e4m3_value(rec[L::k_scales(P) + at * L::kScales + e / 16]);
-        vv = (e & 1 ? vp.y : vp.x) * e4m3_value(rec[L::v_scales(P) + e / 16 * P + v_scale_place(at)]);
-      } else {
-        kv = e4m3_value(rec[(e / 16 * P + at) * 16 + e % 16]);
-        vv = e4m3_value(rec[L::v_codes(P) + (at / 16 * L::kRow + e) * 16 + at % 16]);
-      }
-      s += qv[i] * kv;
-      v[i] = vv;
-    }
-    for (int x = 16; x; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-    s *= c;
-    const float m2 = fmaxf(m, s);
-    const float old = m == -INFINITY ? 0.f : exp2f(m - m2), w = exp2f(s - m2);
-    l = l * old + w;
-    for (int i = 0; i < E; ++i) o[i] = o[i] * old + w * v[i];
-    m = m2;
-  }
-  const float r = l > 0.f ? 1.f / (l * __ldg(p.cache.v_G + kvh)) : l;     // a NaN stays one
-  T* const y = static_cast<T*>(p.out) + row * D;
-  for (int i = 0; i < E; ++i) y[2 * lane + 64 * (i >> 1) + (i & 1)] = from_float<T>(l == 0.f ? 0.f : o[i] * r);
-  if (lane == 0 && p.lse) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+// ---- what a CTA walks: tiles of items, in order
+struct Walk {
+  int b, u, kt, nt;                        // batch entry, (KV head, row tile), tile of the item, tiles of the item
+  int ctx, len;                            // context, keys (context and drafted tokens) that the table has room for
+};
+__device__ __forceinline__ void load_entry(Walk& w, const TreeParams& p) {
+  const long long room = (long long)p.cache.max_pages << p.cache.log_page;
+  const int c = max(0, __ldg(p.context + w.b));
+  w.ctx = (int)min((long long)c, room);
+  w.len = (int)min((long long)c + p.T, room);
+  w.nt = (w.len + kTile - 1) / kTile;
+}
+__device__ __forceinline__ void advance(Walk& w, const TreeParams& p, int units) {
+  if (++w.kt < w.nt) return;
+  w.kt = 0;
+  if (++w.u < units) return;
+  w.u = 0;
+  if (++w.b < p.B) load_entry(w, p);
+}
+// drafted tokens that entry b has
+__device__ __forceinline__ int drafted(const TreeParams& p, int b) { return p.count ? max(0, min(__ldg(p.count + b), p.T)) : p.T; }
+__device__ __forceinline__ unsigned long long row_mask(const TreeParams& p, int b, int t, int n) {
+  if (t >= n) return 0ull;
+  return p.mask ? __ldg(p.mask + (size_t)b * p.T + t) : (2ull << t) - 1;
 }
 
-template <typename T, int FMT, int D>
+template <int FMT, int D, int R>
+struct TreeCfg {
+  using L = RecordLayout<FMT, D>;
+  static constexpr int kSoftmaxGroups = R > 32 ? R / 32 : 1;
+  static constexpr int kCols = R / kSoftmaxGroups;                 // rows of a softmax thread
+  static constexpr int kFirstSoftmax = 8;                          // warps
+  static constexpr int kProducer = kFirstSoftmax + 4 * kSoftmaxGroups, kIssuer = kProducer + 1;
+  static constexpr int kThreads = 32 * (kIssuer + 1);
+  static constexpr int kStage = kTile * 2 * L::kToken;
+  static constexpr int kStages = kStage >= 32768 ? 4 : kStage > 16384 ? 6 : 8;
+  static constexpr int kQ = R * D * 2, kP = kTile * R * 2;
+  static constexpr int kRing = 16;                                 // tiles whose page validity is remembered
+  // shared memory
+  static constexpr int kOffStage = 0;
+  static constexpr int kOffQ = kOffStage + kStages * kStage;
+  static constexpr int kOffP = kOffQ + 2 * kQ;
+  static constexpr int kOffCM = kOffP + 2 * kP;                    // float2 [R]: score constant, minus the reference
+  // float [4][R]: score constants of the last items.  Four: Q of tile i is made when the products of tile i - 2 are done, so the
+  // softmax warps, which have then taken the scores of tile i - 4, may be three items behind
+  static constexpr int kOffC = kOffCM + 8 * R;
+  static constexpr int kOffBits = kOffC + 16 * R;                  // u64 [R]
+  static constexpr int kOffWarp = kOffBits + 8 * R;                // float [4][R]: maxima or sums of the four warps
+  static constexpr int kOffScale = kOffWarp + 16 * R;              // float [R]: factors on O
+  static constexpr int kOffValid = kOffScale + 4 * R;              // u32 [kRing]
+  static constexpr int kOffScan = kOffValid + 4 * kRing;           // i64 [32]
+  static constexpr int kOffFind = kOffScan + 256;                  // i64 [2]
+  static constexpr int kOffBar = kOffFind + 64;
+  static constexpr int kSmem = kOffBar + 512 + 1024;
+  // barriers
+  enum { KA_FULL = 0, KA_FREE = 2, VA_FULL = 4, S_FULL = 6, S_FREE = 8, P_FULL = 10, PV_DONE = 12, Q_FULL = 14, DRAIN = 16, RING = 18 };
+  static constexpr int kBars = RING + 2 * kStages;
+  static_assert(kBars * 8 + 16 <= 512, "barriers");
+  // tensor memory columns
+  static constexpr int kKA = 0, kVA = D, kS = kVA + kTile, kO = kS + 2 * R;
+  static_assert(kO + R <= 512, "tensor memory");
+};
+
+template <bool HALF>
+__device__ __forceinline__ float2 unpack16(uint32_t w) { return HALF ? unpack2<__half>(w) : unpack2<__nv_bfloat16>(w); }
+
+// 16 tokens of which bit t of `valid` says which count -> byte masks of the sixteen bytes in the order V (or its scales) keeps them
+template <bool PERMUTED>
+__device__ __forceinline__ uint4 byte_masks(uint32_t valid) {
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int t = 0; t < 16; ++t) {
+    const int at = PERMUTED ? v_scale_place(t) : t;
+    if (valid >> t & 1) w[at >> 2] |= 0xFFu << (8 * (at & 3));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint32_t splat_half(uint32_t h2, int hi) { return __byte_perm(h2, 0, hi ? 0x3232 : 0x1010); }
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void tmem_ld_x(uint32_t addr, uint32_t (&r)[16]) { tmem_ld_32x32b_x16(addr, r); }
+__device__ __forceinline__ void tmem_ld_x(uint32_t addr, uint32_t (&r)[32]) { tmem_ld_32x32b_x32(addr, r); }
+
+// sum over the warp of each of N values: lane i ends with the total of value i (N = 16: lanes i and i + 16)
+template <int N>
+__device__ __forceinline__ float warp_sums(float (&v)[N], int lane) {
+  int n = N;
+#pragma unroll
+  for (int step = N / 2; step; step >>= 1) {
+    const bool up = lane & step;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      if (i < step) {
+        const float give = up ? v[i] : v[i + step], keep = up ? v[i + step] : v[i];
+        v[i] = keep + __shfl_xor_sync(0xffffffffu, give, step);
+      }
+    }
+  }
+  (void)n;
+  return N == 16 ? v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16) : v[0];
+}
+
+template <int FMT, int D, int R>
+__global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(const TreeParams p) {
+  using C = TreeCfg<FMT, D, R>;
+  using L = typename C::L;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* const sgen = smem_raw + (sbase - smem_u32(smem_raw));
+  const uint32_t abort_at = sbase + C::kOffBar + 8 * C::kBars, tslot = abort_at + 4;
+  volatile uint32_t* const abort_word = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars);
+  auto bar = [&](int i) { return sbase + C::kOffBar + 8u * i; };
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int units = p.cache.kv_heads * p.row_tiles;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(C::KA_FULL + i), 4);
+      mbar_init(bar(C::KA_FREE + i), 1);
+      mbar_init(bar(C::VA_FULL + i), 4);
+      mbar_init(bar(C::S_FULL + i), 1);
+      mbar_init(bar(C::S_FREE + i), 4 * C::kSoftmaxGroups);
+      mbar_init(bar(C::P_FULL + i), 4 * C::kSoftmaxGroups);
+      mbar_init(bar(C::PV_DONE + i), 1);
+      mbar_init(bar(C::Q_FULL + i), 4);
+      mbar_init(bar(C::DRAIN + i), 1);
+    }
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(bar(C::RING + s), 1);
+      mbar_init(bar(C::RING + C::kStages + s), 8);
+    }
+    *abort_word = 0;
+    fence_barrier_init();
+  }
+  if (warp == C::kIssuer) { tmem_alloc(tslot, 512); tmem_relinquish(); }
+  wait_prior_grids();
+
+  // ---- this CTA's run of tiles
+  Walk w0;
+  long long t0, t1, total;
+  {
+    const int per = (p.B + C::kThreads - 1) / C::kThreads, b0 = threadIdx.x * per, b1 = min(p.B, b0 + per);
+    long long mine = 0;
+    Walk w;
+    for (w.b = b0; w.b < b1; ++w.b) { load_entry(w, p); mine += (long long)w.nt * units; }
+    long long incl = mine;
+    for (int s = 1; s < 32; s <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, incl, s);
+      if (lane >= s) incl += o;
+    }
+    long long* const scan = reinterpret_cast<long long*>(sgen + C::kOffScan);
+    long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
+    if (lane == 31) scan[warp] = incl;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    long long before = 0;
+    total = 0;
+    for (int i = 0; i < C::kThreads / 32; ++i) {
+      if (i < warp) before += scan[i];
+      total += scan[i];
+    }
+    before += incl - mine;
+    const long long ctas = min((long long)gridDim.x, total);
+    t0 = blockIdx.x < ctas ? blockIdx.x * total / ctas : total;
+    t1 = blockIdx.x < ctas ? (blockIdx.x + 1) * total / ctas : total;
+    if (t0 < t1 && before <= t0 && t0 < before + mine) {            // one thread
+      for (w.b = b0;; ++w.b) {
+        load_entry(w, p);
+        if (t0 < before + (long long)w.nt * units) break;
+        before += (long long)w.nt * units;
+      }
+      find[0] = w.b;
+      find[1] = t0 - before;
+    }
+    __syncthreads();
+    w0.b = t0 < t1 ? (int)find[0] : 0;
+    load_entry(w0, p);
+    const long long r = t0 < t1 ? find[1] : 0;
+    w0.u = (int)(r / w0.nt);
+    w0.kt = (int)(r - (long long)w0.u * w0.nt);
+  }
+  const int n_tiles = (int)min(t1 - t0, (long long)INT_MAX);
+  const long long ctas = min((long long)gridDim.x, total);
+  auto cta_of = [&](long long tile) { return (int)(((tile + 1) * ctas - 1) / total); };
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
+  uint32_t* const valid_ring = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
+  const int P = 1 << p.cache.log_page;
+  bool ok = true;
+
+  if (warp == C::kProducer) {
+    // ===================================================================== pages -> shared memory
+    Walk w = w0;
+    const int slots = kTile >> p.cache.log_page;                    // pages of a tile: 1 to 8
+    int s = 0, ph = 0;
+    bool lost = false;
+    for (int i = 0; i < n_tiles; ++i, advance(w, p, units)) {
+      const int kvh = w.u / p.row_tiles, first = w.kt * kTile;
+      int page = -1;
+      if (lane < slots && first + lane * P < w.len) {
+        page = p.cache.page_of(w.b, first + lane * P);
+        lost |= page < 0;
+      }
+      lost |= w.kt == 0 && (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len;
+      const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
+      if (ok) ok = mbar_wait(bar(C::RING + C::kStages + s), ph ^ 1, abort_at);
+      if (!ok) break;
+      if (lane == 0) {
+        valid_ring[i % C::kRing] = held;
+        mbar_arrive_expect_tx(bar(C::RING + s), __popc(held) * p.cache.record);
+      }
+      __syncwarp();
+      if (page >= 0)
+        bulk_load_1d(sbase + C::kOffStage + s * C::kStage + lane * p.cache.record, p.cache.rec(page, kvh), p.cache.record, bar(C::RING + s));
+      if (++s == C::kStages) { s = 0; ph ^= 1; }
+    }
+    if (__any_sync(0xffffffffu, lost) && lane == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
+    if (!ok) {                                                      // given up: the copies in flight end before shared memory does
+      for (int k = 0; k < C::kStages; ++k)
+        for (int spin = 0; spin < (1 << 12) && !mbar_try_wait(bar(C::RING + k), k < s ? ph : ph ^ 1); ++spin) {}
+    }
+  } else if (warp == C::kIssuer) {
+    // ===================================================================== products
+    // Q: K-major, core matrices of 8 rows x 16 bytes, those along d neighbours; P: row-major (MN), core matrices of 8 keys x 16 bytes (8 rows),
+    // those along rows neighbours
+    constexpr uint32_t kIdescS = make_idesc_f16(128, R, false), kIdescO = make_idesc_f16(128, R, true);
+    Walk w = w0;
+    int item = 0;
+    auto products_o = [&](int i, bool fresh) {                      // O^T (+)= V^T P^T of tile i
+      const int buf = i & 1, ph = (i >> 1) & 1;
+      if (ok) ok = mbar_wait(bar(C::VA_FULL + buf), ph, abort_at);
+      if (ok) ok = mbar_wait(bar(C::P_FULL + buf), ph, abort_at);
+      if (!ok) return;
+      tc_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          tc_mma_f16_ta(tmem + C::kO, tmem + C::kVA + 64 * buf + 8 * k,
+                        make_smem_desc(sbase + C::kOffP + buf * C::kP + k * 2 * (R / 8) * 128, (R / 8) * 128, 128, kSwzNone), kIdescO,
+                        !(fresh && k == 0));
+        tc_commit(bar(C::PV_DONE + buf));
+      }
+      __syncwarp();
+    };
+    bool fresh = true, fresh_before = true;                         // is the tile (the one before) the first of its item here?
+    for (int i = 0; i < n_tiles; ++i) {
+      const int buf = i & 1, ph = (i >> 1) & 1;
+      if (fresh && ok) ok = mbar_wait(bar(C::Q_FULL + (item & 1)), (item >> 1) & 1, abort_at);
+      if (ok) ok = mbar_wait(bar(C::KA_FULL + buf), ph, abort_at);
+      if (ok) ok = mbar_wait(bar(C::S_FREE + buf), ph ^ 1, abort_at);
+      if (!ok) break;
+      tc_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          tc_mma_f16_ta(tmem + C::kS + R * buf, tmem + C::kKA + (D / 2) * buf + 8 * k,
+                        make_smem_desc(sbase + C::kOffQ + (item & 1) * C::kQ + k * 256, 128, (D / 8) * 128, kSwzNone), kIdescS, k > 0);
+        tc_commit(bar(C::S_FULL + buf));
+        tc_commit(bar(C::KA_FREE + buf));
+      }
+      __syncwarp();
+      if (i > 0) products_o(i - 1, fresh_before);                   // one tile behind: S of the next is under way while P is made
+      if (!ok) break;
+      fresh_before = fresh;
+      fresh = w.kt + 1 == w.nt;
+      item += fresh;
+      advance(w, p, units);
+    }
+    if (ok && n_tiles > 0) products_o(n_tiles - 1, fresh_before);
+    if (!ok && elect_one()) tc_commit(bar(C::DRAIN));
+  } else if (warp < 4) {
+    // ===================================================================== Q and K
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const int key = threadIdx.x, slot = key >> p.cache.log_page, t = key & (P - 1);
+    const float c0 = p.scale * 1.4426950408889634f;
+    Walk w = w0;
+    int s = 0, sph = 0, item = 0;
+    bool fresh = true;
+    for (int i = 0; i < n_tiles; ++i) {
+      const int buf = i & 1, ph = (i >> 1) & 1;
+      if (ok) ok = mbar_wait(bar(C::KA_FREE + buf), ph ^ 1, abort_at);
+      if (ok && fresh) {
+        // Rows scaled by a power of two into f16's range (the largest element to [2^14, 2^15)): exact for 8-bit significands, and a row's
+        // scores are scaled back by its constant.  The buffer is free: tile i - 2 or an earlier one was the last that read it.
+        const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R;
+        const float c = __fdiv_rn(c0, __ldg(p.cache.k_G + kvh));
+        constexpr int kParts = D / 16;                              // threads of a row
+#pragma unroll
+        for (int j = threadIdx.x; j < R * kParts; j += 128) {
+          const int r = j / kParts, e = (j % kParts) * 16, row = row0 + r;
+          float v[16];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) v[x] = 0.f;
+          if (row < p.rows) {
+            const int hl = row / p.T, tok = row - hl * p.T;
+            const uint16_t* q = static_cast<const uint16_t*>(p.q) + w.b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
+            uint32_t raw[8];
+            if (p.q_vector) {
+              *reinterpret_cast<uint4*>(raw) = __ldg(reinterpret_cast<const uint4*>(q));
+              *reinterpret_cast<uint4*>(raw + 4) = __ldg(reinterpret_cast<const uint4*>(q) + 1);
+            } else {
+#pragma unroll
+              for (int x = 0; x < 8; ++x) raw[x] = (uint32_t)__ldg(q + 2 * x) | (uint32_t)__ldg(q + 2 * x + 1) << 16;
+            }
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              const float2 f = p.half ? unpack16<true>(raw[x]) : unpack16<false>(raw[x]);
+              v[2 * x] = f.x;
+              v[2 * x + 1] = f.y;
+            }
+          }
+          float a = 0.f;
+#pragma unroll
+          for (int x = 0; x < 16; ++x) a = fmaxf(a, fabsf(v[x]));
+#pragma unroll
+          for (int x = 1; x < kParts; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
+          // 2^(14 - exponent), at most 2^100: rows below 2^-86 lose bits of scores that are nothing beside the others
+          const uint32_t up = a == 0.f ? 127u : min(268u - (__float_as_uint(a) >> 23), 227u);
+          const float f = __uint_as_float(up << 23);
+          uint32_t h[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(v[2 * x] * f, v[2 * x + 1] * f);
+          uint8_t* const dst = sgen + C::kOffQ + (item & 1) * C::kQ + ((r >> 3) * (D / 8) + (e >> 3)) * 128 + (r & 7) * 16;
+          *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(dst + 128) = make_uint4(h[4], h[5], h[6], h[7]);
+          if (e == 0) reinterpret_cast<float*>(sgen + C::kOffC)[(item & 3) * R + r] = c * __uint_as_float((254u - up) << 23);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::Q_FULL + (item & 1)));
+      }
+      if (ok) ok = mbar_wait(bar(C::RING + s), sph, abort_at);
+      if (ok) {
+        tc_fence_after();
+        const uint8_t* const rec = sgen + C::kOffStage + s * C::kStage + slot * p.cache.record;
+        const uint32_t dst = tmem + lanes + C::kKA + (D / 2) * buf;
+        if (L::kFp4) {
+          uint32_t sw[2];
+          if (D == 128) *reinterpret_cast<uint2*>(sw) = *reinterpret_cast<const uint2*>(rec + L::k_scales(P) + t * L::kScales);
+          else sw[0] = *reinterpret_cast<const uint32_t*>(rec + L::k_scales(P) + t * L::kScales);
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            const uint4 raw = *reinterpret_cast<const uint4*>(rec + (c * P + t) * 16);
+            const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+            const uint32_t two = cvt_f16x2_e4m3x2(sw[c >> 1] >> (16 * (c & 1)) & 0xFFFFu);
+            uint32_t h[16];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t f = splat_half(two, x >> 1);
+              h[4 * x] = mul_half2(cvt_f16x2_e2m1x2<0>(words[x]), f);
+              h[4 * x + 1] = mul_half2(cvt_f16x2_e2m1x2<1>(words[x]), f);
+              h[4 * x + 2] = mul_half2(cvt_f16x2_e2m1x2<2>(words[x]), f);
+              h[4 * x + 3] = mul_half2(cvt_f16x2_e2m1x2<3>(words[x]), f);
+            }
+            tmem_st_32x32b_x16(dst + 16 * c, h);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t h[16];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const uint4 raw = *reinterpret_cast<const uint4*>(rec + ((2 * c + y) * P + t) * 16);
+              const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+              for (int x = 0; x < 8; ++x) h[8 * y + x] = cvt_f16x2_e4m3x2(words[x >> 1] >> (16 * (x & 1)) & 0xFFFFu);
+            }
+            tmem_st_32x32b_x16(dst + 16 * c, h);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::RING + C::kStages + s));   // (the loads are done: their values have been used)
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::KA_FULL + buf));
+      }
+      if (++s == C::kStages) { s = 0; sph ^= 1; }
+      fresh = w.kt + 1 == w.nt;
+      item += fresh;
+      advance(w, p, units);
+    }
+  } else if (warp < 8) {
+    // ===================================================================== V
+    const uint32_t lanes = (uint32_t)((warp - 4) * 32) << 16;
+    const int e = threadIdx.x - 128;                                // index of the head dimension
+    Walk w = w0;
+    int s = 0, sph = 0, b_of = -1;
+    unsigned long long seen = 0;                                    // drafted tokens that some row sees
+    for (int i = 0; i < n_tiles; ++i, advance(w, p, units)) {
+      const int buf = i & 1, ph = (i >> 1) & 1;
+      if (w.b != b_of) {
+        b_of = w.b;
+        const int n = drafted(p, w.b);
+        seen = row_mask(p, w.b, lane, n) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n) : 0ull);
+        seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
+      }
+      if (ok) ok = mbar_wait(bar(C::PV_DONE + buf), ph ^ 1, abort_at);
+      if (ok) ok = mbar_wait(bar(C::RING + s), sph, abort_at);
+      if (ok) {
+        tc_fence_after();
+        const uint32_t held = valid_ring[i % C::kRing];
+        const int first = w.kt * kTile;
+        // what no row sees counts as zero: it may be any bytes, and a probability of 0 times a NaN would be one
+        const bool all = first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
+        const uint8_t* const stage = sgen + C::kOffStage + s * C::kStage;
+        const uint32_t dst = tmem + lanes + C::kVA + 64 * buf, shift = 4 * (e & 1);
+        if (e < D) {
+#pragma unroll
+          for (int j2 = 0; j2 < kTile / 32; ++j2) {
+            uint32_t h[16];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const int at = 32 * j2 + 16 * y, slot = at >> p.cache.log_page, t = at & (P - 1);
+              const uint8_t* const rec = stage + slot * p.cache.record;
+              uint32_t ok16 = 0xFFFFu;
+              if (!all) {
+                const int in = w.ctx - (first + at);                // tokens of these that belong to the context
+                const unsigned long long dr = in >= 0 ? (in < 16 ? seen << in : 0ull) : (-in < 64 ? seen >> -in : 0ull);
+                ok16 = (uint32_t)dr & 0xFFFFu;
+                if (in > 0) ok16 |= in >= 16 ? 0xFFFFu : (1u << in) - 1;
+                if (!(held >> slot & 1)) ok16 = 0;
+                const int left = w.len - (first + at);              // tokens that the table has room for
+                if (left < 16) ok16 &= left > 0 ? (1u << left) - 1 : 0u;
+              }
+              uint4 raw = *reinterpret_cast<const uint4*>(rec + L::v_codes(P) + ((t >> 4) * L::kRow + (L::kFp4 ? e >> 1 : e)) * 16);
+              if (L::kFp4) {
+                uint4 sc = *reinterpret_cast<const uint4*>(rec + L::v_scales(P) + (e >> 4) * P + t);
+                if (!all) {
+                  const uint4 m = byte_masks<true>(ok16);
+                  sc.x &= m.x; sc.y &= m.y; sc.z &= m.z; sc.w &= m.w;
+                }
+                const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w}, scw[4] = {sc.x, sc.y, sc.z, sc.w};
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {                       // eight tokens: i and i + 4 in a byte
+                  const uint32_t n = (cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u);
+                  h[8 * y + 4 * x] = mul_half2(cvt_f16x2_e2m1x2<0>(n), cvt_f16x2_e4m3x2(scw[2 * x] & 0xFFFFu));
+                  h[8 * y + 4 * x + 1] = mul_half2(cvt_f16x2_e2m1x2<1>(n), cvt_f16x2_e4m3x2(scw[2 * x] >> 16));
+                  h[8 * y + 4 * x + 2] = mul_half2(cvt_f16x2_e2m1x2<2>(n), cvt_f16x2_e4m3x2(scw[2 * x + 1] & 0xFFFFu));
+                  h[8 * y + 4 * x + 3] = mul_half2(cvt_f16x2_e2m1x2<3>(n), cvt_f16x2_e4m3x2(scw[2 * x + 1] >> 16));
+                }
+              } else {
+                if (!all) {
+                  const uint4 m = byte_masks<false>(ok16);
+                  raw.x &= m.x; raw.y &= m.y; raw.z &= m.z; raw.w &= m.w;
+                }
+                const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int x = 0; x < 8; ++x) h[8 * y + x] = cvt_f16x2_e4m3x2(cw[x >> 1] >> (16 * (x & 1)) & 0xFFFFu);
+              }
+            }
+            tmem_st_32x32b_x16(dst + 16 * j2, h);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::RING + C::kStages + s));
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::VA_FULL + buf));
+      }
+      if (++s == C::kStages) { s = 0; sph ^= 1; }
+    }
+  } else {
+    // ===================================================================== softmax
+    constexpr int N = C::kCols;
+    const int group = (warp - C::kFirstSoftmax) >> 2, quarter = warp & 3, key = quarter * 32 + lane, c0 = group * N;
+    const int id = 1 + group;                                       // named barrier of the group's 128 threads
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    float2* const cm = reinterpret_cast<float2*>(sgen + C::kOffCM) + c0;
+    unsigned long long* const bits = reinterpret_cast<unsigned long long*>(sgen + C::kOffBits) + c0;
+    float* const of_warp = reinterpret_cast<float*>(sgen + C::kOffWarp) + quarter * R + c0;
+    const float* const warps = reinterpret_cast<const float*>(sgen + C::kOffWarp) + c0;
+    float* const factor = reinterpret_cast<float*>(sgen + C::kOffScale) + c0;
+    // where this key's probabilities stand among the keys of P: as V's tokens do in tensor memory
+    const int place = L::kFp4 ? v_scale_place(key) : key;
+    Walk w = w0;
+    int item = 0, kt_first = w0.kt;
+    bool fresh = true;
+    float l[N];
+    for (int i = 0; i < n_tiles; ++i) {
+      const int buf = i & 1, ph = (i >> 1) & 1;
+      const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R + c0;
+      if (fresh) {
+        kt_first = w.kt;
+        if (key < N) {
+          const int row = row0 + key;
+          bits[key] = row < p.rows ? row_mask(p, w.b, row % p.T, drafted(p, w.b)) : 0ull;
+        }
+#pragma unroll
+        for (int r = 0; r < N; ++r) l[r] = 0.f;
+      }
+      if (ok) ok = mbar_wait(bar(C::S_FULL + buf), ph, abort_at);
+      if (fresh) {                                                  // (Q's constants were there before its products were issued)
+        if (key < N) cm[key] = make_float2(reinterpret_cast<const float*>(sgen + C::kOffC)[(item & 3) * R + c0 + key], INFINITY);
+        bar_sync(id, 128);
+      }
+      tc_fence_after();
+      const uint32_t scores = tmem + lanes + C::kS + R * buf + c0;
+      uint32_t raw[N];
+      tmem_ld_x(scores, raw);
+      tmem_wait_ld();
+      const int pos = w.kt * kTile + key;
+      const uint32_t held = valid_ring[i % C::kRing];
+      const bool context = pos < w.ctx && (held >> (key >> p.cache.log_page) & 1);
+      const bool draft = !context && pos >= w.ctx && pos < w.len && (held >> (key >> p.cache.log_page) & 1);
+      // scores in octaves above the rows' references (+ kShift); those that are not seen go to -infinity
+      float x[N], top = -INFINITY;
+      const bool plain = __all_sync(0xffffffffu, context);
+      auto relative = [&](bool references) {
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+          const float2 k = cm[r];
+          x[r] = fmaf(__uint_as_float(raw[r]), k.x, references ? k.y : 0.f);
+        }
+        if (!plain) {
+#pragma unroll
+          for (int r = 0; r < N; ++r)
+            if (!(context || (draft && (bits[r] >> (pos - w.ctx) & 1)))) x[r] = -INFINITY;
+        }
+      };
+      relative(true);
+#pragma unroll
+      for (int r = 0; r < N; ++r) top = fmaxf(top, x[r]);
+      if (bar_any(id, 128, fresh || top > kLag + kShift)) {
+        // the references move: to the largest score seen so far (the scores are read again: kept, they would cost as many registers)
+        tmem_ld_x(scores, raw);
+        tmem_wait_ld();
+        relative(false);
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+          const float m = warp_max(x[r]);
+          if (lane == 0) of_warp[r] = m;
+        }
+        bar_sync(id, 128);
+        if (key < N) {
+          const float old = kShift - cm[key].y;                     // -infinity: none yet
+          const float m = fmaxf(fmaxf(fmaxf(warps[key], warps[R + key]), fmaxf(warps[2 * R + key], warps[3 * R + key])), old);
+          factor[key] = m == -INFINITY ? 1.f : exp2_approx(old - m);
+          cm[key].y = kShift - m;
+        }
+        bar_sync(id, 128);
+        tmem_ld_x(scores, raw);
+        tmem_wait_ld();
+        relative(true);
+#pragma unroll
+        for (int r = 0; r < N; ++r) l[r] *= factor[r];
+        if (!fresh) {
+          // O of the tiles before
+          if (ok) ok = mbar_wait(bar(C::PV_DONE + (buf ^ 1)), ((i - 1) >> 1) & 1, abort_at);
+          tc_fence_after();
+          uint32_t o[N];
+          tmem_ld_x(tmem + lanes + C::kO + c0, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int r = 0; r < N; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * factor[r]);
+#pragma unroll
+          for (int r = 0; r < N; r += 16) tmem_st_32x32b_x16(tmem + lanes + C::kO + c0 + r, o + r);
+          tmem_wait_st();
+          tc_fence_before();
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(bar(C::S_FREE + buf));
+      if (ok) ok = mbar_wait(bar(C::PV_DONE + buf), ph ^ 1, abort_at);   // P of tile i - 2 has been read
+      uint8_t* const dst = sgen + C::kOffP + buf * C::kP + (place >> 3) * (R / 8) * 128 + (c0 >> 3) * 128 + (place & 7) * 16;
+#pragma unroll
+      for (int r = 0; r < N; r += 8) {
+        uint32_t h[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float a = exp2_approx(x[r + 2 * y]), b = exp2_approx(x[r + 2 * y + 1]);
+          l[r + 2 * y] += a;
+          l[r + 2 * y + 1] += b;
+          h[y] = pack_pair<__half>(a, b);
+        }
+        *reinterpret_cast<uint4*>(dst + (r >> 3) * 128) = make_uint4(h[0], h[1], h[2], h[3]);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(bar(C::P_FULL + buf));
+      fresh = false;
+      if (w.kt + 1 == w.nt || i + 1 == n_tiles) {
+        // ---- end of the item, or of this CTA's part of it
+        const bool whole = kt_first == 0 && w.kt + 1 == w.nt;
+        const float sum = warp_sums<N>(l, lane);
+        if (lane < N) of_warp[lane] = sum;
+        if (ok) ok = mbar_wait(bar(C::PV_DONE + buf), ph, abort_at);
+        bar_sync(id, 128);
+        const int n = drafted(p, w.b);
+        const long long out0 = ((long long)w.b * p.H + (long long)kvh * p.group) * p.T;
+        const int slot = 2 * (int)blockIdx.x + (kt_first == 0);
+        if (key < N) {
+          const float total_l = warps[key] + warps[R + key] + warps[2 * R + key] + warps[3 * R + key], m = kShift - cm[key].y;
+          const int row = row0 + key;
+          if (whole) {
+            // nothing seen: 0, not 0 / 0
+            factor[key] = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + kvh));
+            if (ok && p.lse && row < p.rows && row % p.T < n)
+              p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (m - kShift + log2f(total_l)) * 0.6931471805599453f;
+          } else if (ok) {
+            p.part_ml[(size_t)slot * R + c0 + key] = make_float2(m, total_l);
+          }
+        }
+        if (group == 0 && key == 0 && kt_first == 0 && ok) {
+          const long long item_first = t0 + i - w.kt;               // tile of the list that is the item's first
+          p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(item_first + w.nt - 1));
+        }
+        bar_sync(id, 128);
+        tc_fence_after();
+        uint32_t o[N];
+        tmem_ld_x(tmem + lanes + C::kO + c0, o);
+        tmem_wait_ld();
+        tc_fence_before();
+        const uint32_t keep = __ballot_sync(0xffffffffu, lane < N && row0 + lane < p.rows && (row0 + lane) % p.T < n);
+        if (ok && key < D) {
+          if (whole) {
+            uint16_t* const dst = static_cast<uint16_t*>(p.out) + (size_t)(out0 + row0) * D + key;
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+              const float y = __uint_as_float(o[r]) * factor[r];
+              const uint16_t h = p.half ? __half_as_ushort(__float2half_rn(y)) : __bfloat16_as_ushort(__float2bfloat16_rn(y));
+              if (keep >> r & 1) dst[r * D] = h;
+            }
+          } else {
+#pragma unroll
+            for (int r = 0; r < N; ++r) p.part[((size_t)slot * R + c0 + r) * D + key] = __uint_as_float(o[r]);
+          }
+        }
+        fresh = true;
+        ++item;
+      }
+      advance(w, p, units);
+    }
+  }
+  launch_dependents();
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_word && threadIdx.x == 0 && p.status) *p.status = FP4ATTN_ERR_TIMEOUT;
+  if (warp == C::kIssuer) {
+    if (*abort_word && !ok && lane == 0)                            // given up: the products in flight end before tensor memory does
+      for (int spin = 0; spin < (1 << 14) && !mbar_try_wait(bar(C::DRAIN), 0); ++spin) {}
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Joins the parts of the items that fell to several CTAs, in the order of their keys; a warp per row.
+template <int D, int R>
+__global__ void __launch_bounds__(128) tree_join_kernel(const TreeParams p) {
+  wait_prior_grids();
+  const int units = p.cache.kv_heads * p.row_tiles;
+  const int item = blockIdx.x, b = item / units, u = item - b * units, kvh = u / p.row_tiles, lane = threadIdx.x & 31;
+  const int r = blockIdx.y * 4 + (threadIdx.x >> 5), row = (u - kvh * p.row_tiles) * R + r;
+  if (r >= R || row >= p.rows || row % p.T >= drafted(p, b)) return;
+  const int2 ctas = p.split[item];
+  if (ctas.x < 0 || ctas.y < ctas.x || ctas.y >= kMostCtas) return;   // whole (or a kernel that gave up)
+  const int n = ctas.y - ctas.x + 1;
+  auto slot = [&](int i) { return (size_t)(i ? 2 * (ctas.x + i) : 2 * ctas.x + 1); };
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, p.part_ml[slot(i) * R + r].x);
+  m = warp_max(m);
+  constexpr int E = D / 32;
+  float o[E] = {}, l = 0.f;
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    const int i = i0 + lane;
+    const float2 ml = i < n ? p.part_ml[slot(i) * R + r] : make_float2(-INFINITY, 0.f);
+    const float mine = m == -INFINITY ? 0.f : exp2_approx(ml.x - m);
+    const float weighted = ml.x == -INFINITY ? ml.y : mine * ml.y;
+    for (int k = 0; k < min(32, n - i0); ++k) {
+      const float f = __shfl_sync(0xffffffffu, mine, k);
+      l += __shfl_sync(0xffffffffu, weighted, k);
+      const float* const src = p.part + (slot(i0 + k) * R + r) * D + lane * E;
+#pragma unroll
+      for (int x = 0; x < E; ++x) o[x] = fmaf(f, src[x], o[x]);
+    }
+  }
+  const float f = l == 0.f ? 0.f : __fdiv_rn(1.f, l * __ldg(p.cache.v_G + kvh));
+  const size_t at = ((size_t)b * p.H + (size_t)kvh * p.group) * p.T + row;
+#pragma unroll
+  for (int x = 0; x < E; x += 2) {
+    const uint32_t two = p.half ? pack_pair<__half>(o[x] * f, o[x + 1] * f) : pack_pair<__nv_bfloat16>(o[x] * f, o[x + 1] * f);
+    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at * D + lane * E + x) = two;
+  }
+  if (lane == 0 && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (m - kShift + log2f(l)) * 0.6931471805599453f;
+}
+
+// ---- workspace: partial O, their references and sums, what is split
+int rows_of_tile(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+struct TreePlan {
+  int R, row_tiles;
+  size_t ml, split, total;
+};
+TreePlan plan(int B, int H, int kv_heads, int T, int d) {
+  TreePlan t;
+  const int rows = H / kv_heads * T;
+  t.R = rows_of_tile(rows);
+  t.row_tiles = (rows + t.R - 1) / t.R;
+  const size_t part = (size_t)2 * kMostCtas * t.R * d * 4;
+  t.ml = part;
+  t.split = t.ml + (size_t)2 * kMostCtas * t.R * 8;
+  t.total = t.split + (((size_t)B * kv_heads * t.row_tiles * 8 + 15) & ~(size_t)15);
+  return t;
+}
+
+template <int FMT, int D, int R>
 int launch_tree(const TreeParams& p, cudaStream_t st) {
-  const long long rows = (long long)p.B * p.H * p.T;
-  const cudaError_t e = launch_overlapped(tree_row_kernel<T, FMT, D>, dim3((unsigned)((rows + 3) / 4)), 128u, 0, st, p);
+  using C = TreeCfg<FMT, D, R>;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FP4ATTN_ERR_CUDA;
+  static std::atomic<bool> attr_set[kMaxDevices];
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(tree_kernel<FMT, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
+    attr_set[dev].store(true, std::memory_order_release);
+  }
+  const int sms = device_sms();
+  if (!sms) return FP4ATTN_ERR_CUDA;
+  const int units = p.cache.kv_heads * p.row_tiles;
+  const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * units;
+  const unsigned grid = (unsigned)std::min<long long>(std::min(sms, kMostCtas), most_tiles);
+  cudaError_t e = launch_overlapped(tree_kernel<FMT, D, R>, dim3(grid), C::kThreads, C::kSmem, st, p);
+  if (e == cudaSuccess)
+    e = launch_overlapped(tree_join_kernel<D, R>, dim3((unsigned)(p.B * units), (unsigned)(std::min(R, p.rows) + 3) / 4), 128u, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
+}
+template <int FMT, int D>
+int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
+  return R == 16 ? launch_tree<FMT, D, 16>(p, st) : R == 32 ? launch_tree<FMT, D, 32>(p, st) : launch_tree<FMT, D, 64>(p, st);
 }
 
 }  // namespace
@@ -99,8 +800,9 @@ int launch_tree(const TreeParams& p, cudaStream_t st) {
 using namespace fp4attn;
 
 extern "C" size_t fp4attn_tree_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d) {
-  (void)B; (void)H; (void)kv_heads; (void)T; (void)d;
-  return 0;
+  if (B <= 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || T <= 0 || T > FP4ATTN_MOST_TREE_TOKENS || (d != 64 && d != 128)) return 0;
+  if ((long long)B * H * T >= (1ll << 31)) return 0;
+  return plan(B, H, kv_heads, T, d).total;
 }
 
 extern "C" int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, const int* block_table,
@@ -116,21 +818,26 @@ extern "C" int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4
   if (T > FP4ATTN_MOST_TREE_TOKENS || (long long)B * H * T >= (1ll << 31)) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;
   if (((uintptr_t)q->data & 1) || ((uintptr_t)O & 15) || ((uintptr_t)tree_mask & 7) || ((uintptr_t)LSE | (uintptr_t)device_status) & 3)
     return FP4ATTN_ERR_ALIGNMENT;
+  const TreePlan t = plan(B, H, cache->kv_heads, T, cache->d);
+  if (!workspace || workspace_bytes < t.total) return FP4ATTN_ERR_WORKSPACE;
+  if ((uintptr_t)workspace & 15) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
-  (void)workspace; (void)workspace_bytes;
   TreeParams p = {};
   p.q = q->data; p.q_sb = q->stride_b; p.q_sh = q->stride_h; p.q_sn = q->stride_n;
+  p.q_vector = view_vectors(*q, 2);
+  p.half = type == FP4ATTN_TYPE_FP16;
   p.cache = ref;
   p.context = context; p.count = count; p.mask = tree_mask;
   p.out = O; p.lse = LSE; p.status = device_status;
   p.B = B; p.H = H; p.T = T; p.group = H / cache->kv_heads;
+  p.rows = p.group * T;
+  p.row_tiles = t.row_tiles;
   p.scale = softmax_scale > 0.f ? softmax_scale : (float)(1.0 / sqrt((double)cache->d));
+  p.part = (float*)workspace;
+  p.part_ml = (float2*)((char*)workspace + t.ml);
+  p.split = (int2*)((char*)workspace + t.split);
   cudaStream_t st = (cudaStream_t)stream;
-#define FP4ATTN_TREE(T_)                                                                                                              \
-  if (cache->fmt == FP4ATTN_FMT_NVFP4)                                                                                                \
-    return cache->d == 64 ? launch_tree<T_, FP4ATTN_FMT_NVFP4, 64>(p, st) : launch_tree<T_, FP4ATTN_FMT_NVFP4, 128>(p, st);           \
-  return cache->d == 64 ? launch_tree<T_, FP4ATTN_FMT_E4M3, 64>(p, st) : launch_tree<T_, FP4ATTN_FMT_E4M3, 128>(p, st);
-  if (type == FP4ATTN_TYPE_BF16) { FP4ATTN_TREE(__nv_bfloat16) }
-  FP4ATTN_TREE(__half)
-#undef FP4ATTN_TREE
+  if (cache->fmt == FP4ATTN_FMT_NVFP4)
+    return cache->d == 64 ? launch_rows<FP4ATTN_FMT_NVFP4, 64>(p, t.R, st) : launch_rows<FP4ATTN_FMT_NVFP4, 128>(p, t.R, st);
+  return cache->d == 64 ? launch_rows<FP4ATTN_FMT_E4M3, 64>(p, t.R, st) : launch_rows<FP4ATTN_FMT_E4M3, 128>(p, t.R, st);
 }

@@ -278,8 +278,8 @@ def test_cache_tokens_without_a_page():
 def _check_attention(got, q, cache, table, context, bits, counts=None, scale=None, unseen=()):
     """With size = the largest sum of |q k| scale over a row's keys: a score is off by d sums in fp32 and a few roundings of its
     constant, ds = (d + 8) u size; exp2 by 2^-21 and the rounding of its argument, 2 u |z| <= 2 u size; a probability by the f16
-    rounding, 2^-11, or half a step of f16's subnormals; a sum of n terms in fp32, in any order, by (n - 1) u of the sum of their
-    magnitudes.  These enter numerator and sum, so O is off by 2 (ds + 2^-20 + n u) + 2^-11 of sum p |v| and 2^-24 a key of max |v|, then
+    rounding, 2^-11, or half a step of f16's subnormals, 2^-25 of at least 2^-7 of the largest; a sum of n terms in fp32, in any order, by (n - 1) u of the sum of their
+    magnitudes.  These enter numerator and sum, so O is off by 2 (ds + 2^-20 + n u) + 2^-11 of sum p |v| and 2^-32 a key of max |v|, then
     by its type's rounding; LSE by ds + 2^-20 + n u and fp32's rounding."""
     out, lse = (_np(x) for x in got)
     B, H, T, d = q.shape
@@ -298,7 +298,7 @@ def _check_attention(got, q, cache, table, context, bits, counts=None, scale=Non
             for hq in range(h * (H // kv), (h + 1) * (H // kv)):
                 o, l, pv, size = S.attend(_np(q[b, hq]), k, v, mask, scale)
                 ds = (d + 10) * U * size[:, None]
-                bound = HALF[q.dtype] * np.abs(o) + (2 * (ds + 2.0 ** -20 + len(held) * U) + 2.0 ** -11) * pv + 2.0 ** -24 * np.abs(v).max(initial=0.0) + 2.0 ** -40
+                bound = HALF[q.dtype] * np.abs(o) + (2 * (ds + 2.0 ** -20 + len(held) * U) + 2.0 ** -11) * pv + len(held) * 2.0 ** -32 * np.abs(v).max(initial=0.0) + 2.0 ** -40
                 err = np.abs(out[b, hq] - o)
                 assert (err[:n] <= bound[:n] * (1 + 2.0 ** -8)).all(), (b, hq, np.max(err[:n] - bound[:n]))
                 a = l[:n]
