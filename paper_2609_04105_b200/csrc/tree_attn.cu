@@ -124,13 +124,14 @@ __device__ __forceinline__ float2 unpack16(uint32_t w) { return HALF ? unpack2<_
 // 16 tokens of which bit t of `valid` says which count -> byte masks of the sixteen bytes in the order V (or its scales) keeps them
 template <bool PERMUTED>
 __device__ __forceinline__ uint4 byte_masks(uint32_t valid) {
-  uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-  for (int t = 0; t < 16; ++t) {
-    const int at = PERMUTED ? v_scale_place(t) : t;
-    if (valid >> t & 1) w[at >> 2] |= 0xFFu << (8 * (at & 3));
+  if (PERMUTED) {                                                  // each eight: 0 4 1 5 2 6 3 7
+    uint32_t lo = valid & 0x0F0Fu, hi = valid >> 4 & 0x0F0Fu;
+    lo = (lo | lo << 2) & 0x3333u; lo = (lo | lo << 1) & 0x5555u;
+    hi = (hi | hi << 2) & 0x3333u; hi = (hi | hi << 1) & 0x5555u;
+    valid = lo | hi << 1;
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  auto four = [](uint32_t bits) { return ((bits & 15u) * 0x00204081u & 0x01010101u) * 0xFFu; };
+  return make_uint4(four(valid), four(valid >> 4), four(valid >> 8), four(valid >> 12));
 }
 __device__ __forceinline__ uint32_t splat_half(uint32_t h2, int hi) { return __byte_perm(h2, 0, hi ? 0x3232 : 0x1010); }
 __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
@@ -398,39 +399,38 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         tc_fence_after();
         const uint8_t* const rec = sgen + C::kOffStage + s * C::kStage + slot * p.cache.record;
         const uint32_t dst = tmem + lanes + C::kKA + (D / 2) * buf;
-        if (L::kFp4) {
-          uint32_t sw[2];
-          if (D == 128) *reinterpret_cast<uint2*>(sw) = *reinterpret_cast<const uint2*>(rec + L::k_scales(P) + t * L::kScales);
-          else sw[0] = *reinterpret_cast<const uint32_t*>(rec + L::k_scales(P) + t * L::kScales);
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            const uint4 raw = *reinterpret_cast<const uint4*>(rec + (c * P + t) * 16);
-            const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
-            const uint32_t two = cvt_f16x2_e4m3x2(sw[c >> 1] >> (16 * (c & 1)) & 0xFFFFu);
-            uint32_t h[16];
+        // (rolled loops: what the four roles of a scheduler run in turn has to stay in its instruction cache)
+        const uint8_t* codes = rec + t * 16;
+        uint2 sw = make_uint2(0u, 0u);
+        if (L::kFp4 && D == 128) sw = *reinterpret_cast<const uint2*>(rec + L::k_scales(P) + t * L::kScales);
+        if (L::kFp4 && D == 64) sw.x = *reinterpret_cast<const uint32_t*>(rec + L::k_scales(P) + t * L::kScales);
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t h[16];
+          if (L::kFp4) {
+            const uint4 raw = *reinterpret_cast<const uint4*>(codes);
+            codes += P * 16;
+            const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w}, two = cvt_f16x2_e4m3x2(sw.x & 0xFFFFu);
+            sw.x = __funnelshift_r(sw.x, sw.y, 16);
+            sw.y >>= 16;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const uint32_t f = splat_half(two, x >> 1);
-              h[4 * x] = mul_half2(cvt_f16x2_e2m1x2<0>(words[x]), f);
-              h[4 * x + 1] = mul_half2(cvt_f16x2_e2m1x2<1>(words[x]), f);
-              h[4 * x + 2] = mul_half2(cvt_f16x2_e2m1x2<2>(words[x]), f);
-              h[4 * x + 3] = mul_half2(cvt_f16x2_e2m1x2<3>(words[x]), f);
-            }
-            tmem_st_32x32b_x16(dst + 16 * c, h);
-          }
-        } else {
+              cvt_f16x2_e2m1x8(words[x], h + 4 * x);
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t h[16];
+              for (int y = 0; y < 4; ++y) h[4 * x + y] = mul_half2(h[4 * x + y], f);
+            }
+          } else {
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const uint4 raw = *reinterpret_cast<const uint4*>(rec + ((2 * c + y) * P + t) * 16);
+              const uint4 raw = *reinterpret_cast<const uint4*>(codes);
+              codes += P * 16;
               const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-              for (int x = 0; x < 8; ++x) h[8 * y + x] = cvt_f16x2_e4m3x2(words[x >> 1] >> (16 * (x & 1)) & 0xFFFFu);
+              for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(words[x], h + 8 * y + 2 * x);
             }
-            tmem_st_32x32b_x16(dst + 16 * c, h);
           }
+          tmem_st_32x32b_x16(dst + 16 * c, h);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::RING + C::kStages + s));   // (the loads are done: their values have been used)
@@ -470,50 +470,43 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         const uint8_t* const stage = sgen + C::kOffStage + s * C::kStage;
         const uint32_t dst = tmem + lanes + C::kVA + 64 * buf, shift = 4 * (e & 1);
         if (e < D) {
-#pragma unroll
-          for (int j2 = 0; j2 < kTile / 32; ++j2) {
-            uint32_t h[16];
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const int at = 32 * j2 + 16 * y, slot = at >> p.cache.log_page, t = at & (P - 1);
-              const uint8_t* const rec = stage + slot * p.cache.record;
-              uint32_t ok16 = 0xFFFFu;
-              if (!all) {
-                const int in = w.ctx - (first + at);                // tokens of these that belong to the context
-                const unsigned long long dr = in >= 0 ? (in < 16 ? seen << in : 0ull) : (-in < 64 ? seen >> -in : 0ull);
-                ok16 = (uint32_t)dr & 0xFFFFu;
-                if (in > 0) ok16 |= in >= 16 ? 0xFFFFu : (1u << in) - 1;
-                if (!(held >> slot & 1)) ok16 = 0;
-                const int left = w.len - (first + at);              // tokens that the table has room for
-                if (left < 16) ok16 &= left > 0 ? (1u << left) - 1 : 0u;
-              }
-              uint4 raw = *reinterpret_cast<const uint4*>(rec + L::v_codes(P) + ((t >> 4) * L::kRow + (L::kFp4 ? e >> 1 : e)) * 16);
-              if (L::kFp4) {
-                uint4 sc = *reinterpret_cast<const uint4*>(rec + L::v_scales(P) + (e >> 4) * P + t);
-                if (!all) {
-                  const uint4 m = byte_masks<true>(ok16);
-                  sc.x &= m.x; sc.y &= m.y; sc.z &= m.z; sc.w &= m.w;
-                }
-                const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w}, scw[4] = {sc.x, sc.y, sc.z, sc.w};
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {                       // eight tokens: i and i + 4 in a byte
-                  const uint32_t n = (cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u);
-                  h[8 * y + 4 * x] = mul_half2(cvt_f16x2_e2m1x2<0>(n), cvt_f16x2_e4m3x2(scw[2 * x] & 0xFFFFu));
-                  h[8 * y + 4 * x + 1] = mul_half2(cvt_f16x2_e2m1x2<1>(n), cvt_f16x2_e4m3x2(scw[2 * x] >> 16));
-                  h[8 * y + 4 * x + 2] = mul_half2(cvt_f16x2_e2m1x2<2>(n), cvt_f16x2_e4m3x2(scw[2 * x + 1] & 0xFFFFu));
-                  h[8 * y + 4 * x + 3] = mul_half2(cvt_f16x2_e2m1x2<3>(n), cvt_f16x2_e4m3x2(scw[2 * x + 1] >> 16));
-                }
-              } else {
-                if (!all) {
-                  const uint4 m = byte_masks<false>(ok16);
-                  raw.x &= m.x; raw.y &= m.y; raw.z &= m.z; raw.w &= m.w;
-                }
-                const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-                for (int x = 0; x < 8; ++x) h[8 * y + x] = cvt_f16x2_e4m3x2(cw[x >> 1] >> (16 * (x & 1)) & 0xFFFFu);
-              }
+#pragma unroll 1
+          for (int at = 0; at < kTile; at += 16) {                  // sixteen tokens
+            const int slot = at >> p.cache.log_page, t = at & (P - 1);
+            const uint8_t* const rec = stage + slot * p.cache.record + L::v_codes(P);
+            uint4 raw = *reinterpret_cast<const uint4*>(rec + t * L::kRow + (L::kFp4 ? e >> 1 : e) * 16);
+            uint4 sc = make_uint4(0u, 0u, 0u, 0u);
+            if (L::kFp4) sc = *reinterpret_cast<const uint4*>(rec + P * L::kRow + (e >> 4) * P + t);
+            if (!all) {
+              const int in = w.ctx - (first + at);                  // tokens of these that belong to the context
+              const unsigned long long dr = in >= 0 ? (in < 16 ? seen << in : 0ull) : (-in < 64 ? seen >> -in : 0ull);
+              uint32_t valid = (uint32_t)dr & 0xFFFFu;
+              if (in > 0) valid |= in >= 16 ? 0xFFFFu : (1u << in) - 1;
+              const int left = w.len - (first + at);                // tokens that the table has room for
+              if (left < 16) valid &= left > 0 ? (1u << left) - 1 : 0u;
+              if (!(held >> slot & 1)) valid = 0;
+              const uint4 m = byte_masks<L::kFp4>(valid);
+              uint4& x = L::kFp4 ? sc : raw;
+              x.x &= m.x; x.y &= m.y; x.z &= m.z; x.w &= m.w;
             }
-            tmem_st_32x32b_x16(dst + 16 * j2, h);
+            const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w}, scw[4] = {sc.x, sc.y, sc.z, sc.w};
+            uint32_t h[8];
+            if (L::kFp4) {
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {                         // eight tokens: i and i + 4 in a byte
+                const uint32_t n = (cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u);
+                uint32_t f[4];
+                cvt_f16x2_e2m1x8(n, h + 4 * x);
+                cvt_f16x2_e4m3x4(scw[2 * x], f);
+                cvt_f16x2_e4m3x4(scw[2 * x + 1], f + 2);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) h[4 * x + y] = mul_half2(h[4 * x + y], f[y]);
+              }
+            } else {
+#pragma unroll
+              for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(cw[x], h + 2 * x);
+            }
+            tmem_st_32x32b_x8(dst + (at >> 1), h);
           }
         }
         __syncwarp();
