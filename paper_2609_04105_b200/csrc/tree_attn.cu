@@ -13,8 +13,9 @@
 // partial (maximum, sum, O) in the workspace and joined by a second kernel in the order of its keys.
 //
 //   warps 0-3    K: codes of a key -> f16 -> tensor memory; Q of an item, scaled by a power of two per row, -> f16 -> shared memory
-//   warps 4-7    V: codes of an index, 128 tokens -> f16 -> tensor memory
-//   warps 8-     softmax, a thread per key and 32 (16) rows: maxima, exp2, P^T -> shared memory; rescale of O, end of an item
+//   warps 4-11   V: codes of an index, 64 tokens -> f16 -> tensor memory
+//   warps 12-    softmax, groups of four, a thread per key and 16 rows: exp2, P^T -> shared memory; rescale of O, end of an item.  Up to 32
+//                rows, tiles alternate between two sets of groups, each with references, sums and an O of its own
 //   then         one warp brings the pages in (one bulk copy per page: a (page, head) record is one run of bytes), one issues the products
 //
 // The reference of a row, its maximum at some time, moves only when a score exceeds it by more than 2^8: probabilities up to 256 fit f16 as
@@ -84,10 +85,11 @@ __device__ __forceinline__ unsigned long long row_mask(const TreeParams& p, int 
 template <int FMT, int D, int R>
 struct TreeCfg {
   using L = RecordLayout<FMT, D>;
-  static constexpr int kSoftmaxGroups = R > 32 ? R / 32 : 1;
-  static constexpr int kCols = R / kSoftmaxGroups;                 // rows of a softmax thread
-  static constexpr int kFirstSoftmax = 8;                          // warps
-  static constexpr int kProducer = kFirstSoftmax + 4 * kSoftmaxGroups, kIssuer = kProducer + 1;
+  static constexpr int kN = 16;                                    // rows of a softmax thread
+  static constexpr int kColGroups = R / kN;
+  static constexpr int kSets = R <= 32 ? 2 : 1;                    // sets of softmax groups that tiles alternate between
+  static constexpr int kFirstV = 4, kFirstSoftmax = 12;            // warps
+  static constexpr int kProducer = kFirstSoftmax + 4 * kColGroups * kSets, kIssuer = kProducer + 1;
   static constexpr int kThreads = 32 * (kIssuer + 1);
   static constexpr int kStage = kTile * 2 * L::kToken;
   static constexpr int kStages = kStage >= 32768 ? 4 : kStage > 16384 ? 6 : 8;
@@ -97,41 +99,40 @@ struct TreeCfg {
   static constexpr int kOffStage = 0;
   static constexpr int kOffQ = kOffStage + kStages * kStage;
   static constexpr int kOffP = kOffQ + 2 * kQ;
-  static constexpr int kOffCM = kOffP + 2 * kP;                    // float2 [R]: score constant, minus the reference
+  static constexpr int kOffVScale = kOffP + 2 * kP;                // f16 [8 warps][2 blocks][64 tokens]
+  static constexpr int kOffCM = kOffVScale + 2048;                 // float2 [kSets][R]: score constant, kShift minus the reference
   // float [4][R]: score constants of the last items.  Four: Q of tile i is made when the products of tile i - 2 are done, so the
   // softmax warps, which have then taken the scores of tile i - 4, may be three items behind
-  static constexpr int kOffC = kOffCM + 8 * R;
-  static constexpr int kOffBits = kOffC + 16 * R;                  // u64 [R]
-  static constexpr int kOffWarp = kOffBits + 8 * R;                // float [4][R]: maxima or sums of the four warps
-  static constexpr int kOffScale = kOffWarp + 16 * R;              // float [R]: factors on O
-  static constexpr int kOffValid = kOffScale + 4 * R;              // u32 [kRing]
+  static constexpr int kOffC = kOffCM + 8 * R * kSets;
+  static constexpr int kOffBits = kOffC + 16 * R;                  // u64 [kSets][R]
+  static constexpr int kOffWarp = kOffBits + 8 * R * kSets;        // float [kSets][4][R]: maxima or sums of the four warps
+  static constexpr int kOffScale = kOffWarp + 16 * R * kSets;      // float [kSets][R]: factors on O
+  static constexpr int kOffValid = kOffScale + 4 * R * kSets;      // u32 [kRing]
   static constexpr int kOffScan = kOffValid + 4 * kRing;           // i64 [32]
   static constexpr int kOffFind = kOffScan + 256;                  // i64 [2]
   static constexpr int kOffBar = kOffFind + 64;
   static constexpr int kSmem = kOffBar + 512 + 1024;
+  static_assert(kSmem <= 227 * 1024, "shared memory");
   // barriers
   enum { KA_FULL = 0, KA_FREE = 2, VA_FULL = 4, S_FULL = 6, S_FREE = 8, P_FULL = 10, PV_DONE = 12, Q_FULL = 14, DRAIN = 16, RING = 18 };
   static constexpr int kBars = RING + 2 * kStages;
   static_assert(kBars * 8 + 16 <= 512, "barriers");
   // tensor memory columns
   static constexpr int kKA = 0, kVA = D, kS = kVA + kTile, kO = kS + 2 * R;
-  static_assert(kO + R <= 512, "tensor memory");
+  static_assert(kO + R * kSets <= 512, "tensor memory");
 };
 
 template <bool HALF>
 __device__ __forceinline__ float2 unpack16(uint32_t w) { return HALF ? unpack2<__half>(w) : unpack2<__nv_bfloat16>(w); }
 
-// 16 tokens of which bit t of `valid` says which count -> byte masks of the sixteen bytes in the order V (or its scales) keeps them
-template <bool PERMUTED>
-__device__ __forceinline__ uint4 byte_masks(uint32_t valid) {
-  if (PERMUTED) {                                                  // each eight: 0 4 1 5 2 6 3 7
-    uint32_t lo = valid & 0x0F0Fu, hi = valid >> 4 & 0x0F0Fu;
-    lo = (lo | lo << 2) & 0x3333u; lo = (lo | lo << 1) & 0x5555u;
-    hi = (hi | hi << 2) & 0x3333u; hi = (hi | hi << 1) & 0x5555u;
-    valid = lo | hi << 1;
-  }
-  auto four = [](uint32_t bits) { return ((bits & 15u) * 0x00204081u & 0x01010101u) * 0xFFu; };
-  return make_uint4(four(valid), four(valid >> 4), four(valid >> 8), four(valid >> 12));
+// four bits -> byte masks of a word
+__device__ __forceinline__ uint32_t byte_mask(uint32_t bits) { return ((bits & 15u) * 0x00204081u & 0x01010101u) * 0xFFu; }
+// eight bits in the order V scales are kept in: 0 4 1 5 2 6 3 7
+__device__ __forceinline__ uint32_t permute_eight(uint32_t v) {
+  uint32_t lo = v & 15u, hi = v >> 4 & 15u;
+  lo = (lo | lo << 2) & 0x33u; lo = (lo | lo << 1) & 0x55u;
+  hi = (hi | hi << 2) & 0x33u; hi = (hi | hi << 1) & 0x55u;
+  return lo | hi << 1;
 }
 __device__ __forceinline__ uint32_t splat_half(uint32_t h2, int hi) { return __byte_perm(h2, 0, hi ? 0x3232 : 0x1010); }
 __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
@@ -143,26 +144,27 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ void tmem_ld_x(uint32_t addr, uint32_t (&r)[16]) { tmem_ld_32x32b_x16(addr, r); }
-__device__ __forceinline__ void tmem_ld_x(uint32_t addr, uint32_t (&r)[32]) { tmem_ld_32x32b_x32(addr, r); }
-
-// sum over the warp of each of N values: lane i ends with the total of value i (N = 16: lanes i and i + 16)
-template <int N>
-__device__ __forceinline__ float warp_sums(float (&v)[N], int lane) {
-  int n = N;
+// sum over the warp of each of 16 values: lanes i and i + 16 end with the total of value i
+__device__ __forceinline__ float warp_sums(float (&v)[16], int lane) {
 #pragma unroll
-  for (int step = N / 2; step; step >>= 1) {
+  for (int step = 8; step; step >>= 1) {
     const bool up = lane & step;
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
+    for (int i = 0; i < 8; ++i) {
       if (i < step) {
         const float give = up ? v[i] : v[i + step], keep = up ? v[i + step] : v[i];
         v[i] = keep + __shfl_xor_sync(0xffffffffu, give, step);
       }
     }
   }
-  (void)n;
-  return N == 16 ? v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16) : v[0];
+  return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
+}
+// of the eight tokens from position `pos` on, those that count (bit t: token t): the context, and the drafted tokens that some row sees
+__device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long long seen, int pos) {
+  const int in = w.ctx - pos, left = w.len - pos;                  // tokens of these in the context; that the table has room for
+  uint32_t v = in >= 8 ? 0xFFu : in >= 0 ? (uint32_t)(seen << in) & 0xFFu : -in < 64 ? (uint32_t)(seen >> -in) & 0xFFu : 0u;
+  if (in > 0 && in < 8) v |= (1u << in) - 1;
+  return left >= 8 ? v : left > 0 ? v & ((1u << left) - 1) : 0u;
 }
 
 template <int FMT, int D, int R>
@@ -182,17 +184,17 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(C::KA_FULL + i), 4);
       mbar_init(bar(C::KA_FREE + i), 1);
-      mbar_init(bar(C::VA_FULL + i), 4);
+      mbar_init(bar(C::VA_FULL + i), 8);
       mbar_init(bar(C::S_FULL + i), 1);
-      mbar_init(bar(C::S_FREE + i), 4 * C::kSoftmaxGroups);
-      mbar_init(bar(C::P_FULL + i), 4 * C::kSoftmaxGroups);
+      mbar_init(bar(C::S_FREE + i), 4 * C::kColGroups);
+      mbar_init(bar(C::P_FULL + i), 4 * C::kColGroups);
       mbar_init(bar(C::PV_DONE + i), 1);
       mbar_init(bar(C::Q_FULL + i), 4);
       mbar_init(bar(C::DRAIN + i), 1);
     }
     for (int s = 0; s < C::kStages; ++s) {
       mbar_init(bar(C::RING + s), 1);
-      mbar_init(bar(C::RING + C::kStages + s), 8);
+      mbar_init(bar(C::RING + C::kStages + s), 12);
     }
     *abort_word = 0;
     fence_barrier_init();
@@ -202,8 +204,10 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
 
   // ---- this CTA's run of tiles
   Walk w0;
-  long long t0, t1, total;
+  int n_tiles;
+  long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);   // entry and place of the first tile; its number; all tiles; CTAs
   {
+    long long t0, t1, total;
     const int per = (p.B + C::kThreads - 1) / C::kThreads, b0 = threadIdx.x * per, b1 = min(p.B, b0 + per);
     long long mine = 0;
     Walk w;
@@ -214,7 +218,6 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
       if (lane >= s) incl += o;
     }
     long long* const scan = reinterpret_cast<long long*>(sgen + C::kOffScan);
-    long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
     if (lane == 31) scan[warp] = incl;
     tc_fence_before();
     __syncthreads();
@@ -238,6 +241,12 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
       find[0] = w.b;
       find[1] = t0 - before;
     }
+    if (threadIdx.x == 0) {
+      find[2] = t0;
+      find[3] = total;
+      find[4] = ctas;
+    }
+    n_tiles = (int)min(t1 - t0, (long long)INT_MAX);
     __syncthreads();
     w0.b = t0 < t1 ? (int)find[0] : 0;
     load_entry(w0, p);
@@ -245,9 +254,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
     w0.u = (int)(r / w0.nt);
     w0.kt = (int)(r - (long long)w0.u * w0.nt);
   }
-  const int n_tiles = (int)min(t1 - t0, (long long)INT_MAX);
-  const long long ctas = min((long long)gridDim.x, total);
-  auto cta_of = [&](long long tile) { return (int)(((tile + 1) * ctas - 1) / total); };
+  auto cta_of = [&](long long tile) { return (int)(((tile + 1) * find[4] - 1) / find[3]); };
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
   uint32_t* const valid_ring = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
   const int P = 1 << p.cache.log_page;
@@ -300,14 +307,16 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
-          tc_mma_f16_ta(tmem + C::kO, tmem + C::kVA + 64 * buf + 8 * k,
+          tc_mma_f16_ta(tmem + C::kO + (C::kSets == 2 ? R * buf : 0), tmem + C::kVA + 64 * buf + 8 * k,
                         make_smem_desc(sbase + C::kOffP + buf * C::kP + k * 2 * (R / 8) * 128, (R / 8) * 128, 128, kSwzNone), kIdescO,
                         !(fresh && k == 0));
         tc_commit(bar(C::PV_DONE + buf));
       }
       __syncwarp();
     };
-    bool fresh = true, fresh_before = true;                         // is the tile (the one before) the first of its item here?
+    // is the tile the first of its item here; the one before, the first of its item for its set of softmax groups?
+    bool fresh = true, first_before = true;
+    int of_item = 0;                                                // tiles of the item so far
     for (int i = 0; i < n_tiles; ++i) {
       const int buf = i & 1, ph = (i >> 1) & 1;
       if (fresh && ok) ok = mbar_wait(bar(C::Q_FULL + (item & 1)), (item >> 1) & 1, abort_at);
@@ -324,14 +333,15 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         tc_commit(bar(C::KA_FREE + buf));
       }
       __syncwarp();
-      if (i > 0) products_o(i - 1, fresh_before);                   // one tile behind: S of the next is under way while P is made
+      if (i > 0) products_o(i - 1, first_before);                   // one tile behind: S of the next is under way while P is made
       if (!ok) break;
-      fresh_before = fresh;
+      first_before = of_item < C::kSets;
       fresh = w.kt + 1 == w.nt;
+      of_item = fresh ? 0 : of_item + 1;
       item += fresh;
       advance(w, p, units);
     }
-    if (ok && n_tiles > 0) products_o(n_tiles - 1, fresh_before);
+    if (ok && n_tiles > 0) products_o(n_tiles - 1, first_before);
     if (!ok && elect_one()) tc_commit(bar(C::DRAIN));
   } else if (warp < 4) {
     // ===================================================================== Q and K
@@ -404,7 +414,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         uint2 sw = make_uint2(0u, 0u);
         if (L::kFp4 && D == 128) sw = *reinterpret_cast<const uint2*>(rec + L::k_scales(P) + t * L::kScales);
         if (L::kFp4 && D == 64) sw.x = *reinterpret_cast<const uint32_t*>(rec + L::k_scales(P) + t * L::kScales);
-#pragma unroll 1
+#pragma unroll 2
         for (int c = 0; c < D / 32; ++c) {
           uint32_t h[16];
           if (L::kFp4) {
@@ -444,10 +454,11 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
       item += fresh;
       advance(w, p, units);
     }
-  } else if (warp < 8) {
+  } else if (warp < C::kFirstSoftmax) {
     // ===================================================================== V
-    const uint32_t lanes = (uint32_t)((warp - 4) * 32) << 16;
-    const int e = threadIdx.x - 128;                                // index of the head dimension
+    const int quarter = warp & 3, half = (warp - C::kFirstV) >> 2, e = quarter * 32 + lane;      // index of the head dimension
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    uint8_t* const scales = sgen + C::kOffVScale + (warp - C::kFirstV) * 256;
     Walk w = w0;
     int s = 0, sph = 0, b_of = -1;
     unsigned long long seen = 0;                                    // drafted tokens that some row sees
@@ -467,46 +478,50 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         const int first = w.kt * kTile;
         // what no row sees counts as zero: it may be any bytes, and a probability of 0 times a NaN would be one
         const bool all = first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
-        const uint8_t* const stage = sgen + C::kOffStage + s * C::kStage;
-        const uint32_t dst = tmem + lanes + C::kVA + 64 * buf, shift = 4 * (e & 1);
-        if (e < D) {
-#pragma unroll 1
-          for (int at = 0; at < kTile; at += 16) {                  // sixteen tokens
-            const int slot = at >> p.cache.log_page, t = at & (P - 1);
-            const uint8_t* const rec = stage + slot * p.cache.record + L::v_codes(P);
-            uint4 raw = *reinterpret_cast<const uint4*>(rec + t * L::kRow + (L::kFp4 ? e >> 1 : e) * 16);
-            uint4 sc = make_uint4(0u, 0u, 0u, 0u);
-            if (L::kFp4) sc = *reinterpret_cast<const uint4*>(rec + P * L::kRow + (e >> 4) * P + t);
+        const uint8_t* const stage = sgen + C::kOffStage + s * C::kStage + L::v_codes(P);
+        const uint32_t dst = tmem + lanes + C::kVA + 64 * buf + 32 * half, shift = 4 * (e & 1);
+        if (quarter * 32 < D) {
+          if (L::kFp4) {
+            // the scales of this warp's two blocks and 64 tokens, once for all sixteen lanes that need them
+            const int at = 64 * half + 4 * (lane & 15), slot = at >> p.cache.log_page;
+            uint32_t sc = *reinterpret_cast<const uint32_t*>(stage + slot * p.cache.record + P * L::kRow + (e >> 4) * P + (at & (P - 1)));
             if (!all) {
-              const int in = w.ctx - (first + at);                  // tokens of these that belong to the context
-              const unsigned long long dr = in >= 0 ? (in < 16 ? seen << in : 0ull) : (-in < 64 ? seen >> -in : 0ull);
-              uint32_t valid = (uint32_t)dr & 0xFFFFu;
-              if (in > 0) valid |= in >= 16 ? 0xFFFFu : (1u << in) - 1;
-              const int left = w.len - (first + at);                // tokens that the table has room for
-              if (left < 16) valid &= left > 0 ? (1u << left) - 1 : 0u;
-              if (!(held >> slot & 1)) valid = 0;
-              const uint4 m = byte_masks<L::kFp4>(valid);
-              uint4& x = L::kFp4 ? sc : raw;
-              x.x &= m.x; x.y &= m.y; x.z &= m.z; x.w &= m.w;
+              const uint32_t v = held >> slot & 1 ? permute_eight(valid_eight(w, seen, first + (at & ~7))) : 0u;
+              sc &= byte_mask(at & 4 ? v >> 4 : v);
             }
-            const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w}, scw[4] = {sc.x, sc.y, sc.z, sc.w};
+            uint32_t f[2];
+            cvt_f16x2_e4m3x4(sc, f);
+            *reinterpret_cast<uint2*>(scales + lane * 8) = make_uint2(f[0], f[1]);
+            __syncwarp();
+          }
+#pragma unroll 2
+          for (int j = 0; j < 64; j += 16) {                        // sixteen tokens
+            const int at = 64 * half + j, slot = at >> p.cache.log_page, t = at & (P - 1);
+            const uint8_t* const rec = stage + slot * p.cache.record;
+            uint4 raw = *reinterpret_cast<const uint4*>(rec + t * L::kRow + (L::kFp4 ? e >> 1 : e) * 16);
             uint32_t h[8];
             if (L::kFp4) {
+              const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
               for (int x = 0; x < 2; ++x) {                         // eight tokens: i and i + 4 in a byte
-                const uint32_t n = (cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u);
-                uint32_t f[4];
-                cvt_f16x2_e2m1x8(n, h + 4 * x);
-                cvt_f16x2_e4m3x4(scw[2 * x], f);
-                cvt_f16x2_e4m3x4(scw[2 * x + 1], f + 2);
-#pragma unroll
-                for (int y = 0; y < 4; ++y) h[4 * x + y] = mul_half2(h[4 * x + y], f[y]);
+                const uint4 f = *reinterpret_cast<const uint4*>(scales + (lane >> 4) * 128 + j * 2 + 16 * x);
+                cvt_f16x2_e2m1x8((cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u), h + 4 * x);
+                h[4 * x] = mul_half2(h[4 * x], f.x);
+                h[4 * x + 1] = mul_half2(h[4 * x + 1], f.y);
+                h[4 * x + 2] = mul_half2(h[4 * x + 2], f.z);
+                h[4 * x + 3] = mul_half2(h[4 * x + 3], f.w);
               }
             } else {
+              if (!all) {
+                const uint32_t lo = held >> slot & 1 ? valid_eight(w, seen, first + at) : 0u;
+                const uint32_t hi = held >> slot & 1 ? valid_eight(w, seen, first + at + 8) : 0u;
+                raw.x &= byte_mask(lo); raw.y &= byte_mask(lo >> 4); raw.z &= byte_mask(hi); raw.w &= byte_mask(hi >> 4);
+              }
+              const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
               for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(cw[x], h + 2 * x);
             }
-            tmem_st_32x32b_x8(dst + (at >> 1), h);
+            tmem_st_32x32b_x8(dst + (j >> 1), h);
           }
         }
         __syncwarp();
@@ -520,20 +535,25 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
     }
   } else {
     // ===================================================================== softmax
-    constexpr int N = C::kCols;
-    const int group = (warp - C::kFirstSoftmax) >> 2, quarter = warp & 3, key = quarter * 32 + lane, c0 = group * N;
-    const int id = 1 + group;                                       // named barrier of the group's 128 threads
+    constexpr int N = C::kN;
+    const int group = (warp - C::kFirstSoftmax) >> 2, set = group / C::kColGroups, cols = group % C::kColGroups, c0 = cols * N;
+    const int quarter = warp & 3, key = quarter * 32 + lane;
+    const int id = 1 + group, id_all = 5 + cols;                    // named barriers: this group's 128 threads; the sets of these rows
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    float2* const cm = reinterpret_cast<float2*>(sgen + C::kOffCM) + c0;
-    unsigned long long* const bits = reinterpret_cast<unsigned long long*>(sgen + C::kOffBits) + c0;
-    float* const of_warp = reinterpret_cast<float*>(sgen + C::kOffWarp) + quarter * R + c0;
-    const float* const warps = reinterpret_cast<const float*>(sgen + C::kOffWarp) + c0;
-    float* const factor = reinterpret_cast<float*>(sgen + C::kOffScale) + c0;
+    float2* const cm_all = reinterpret_cast<float2*>(sgen + C::kOffCM) + c0;                     // [kSets] R apart
+    float2* const cm = cm_all + set * R;
+    unsigned long long* const bits = reinterpret_cast<unsigned long long*>(sgen + C::kOffBits) + set * R + c0;
+    float* const warps_all = reinterpret_cast<float*>(sgen + C::kOffWarp) + c0;                  // [kSets][4] R apart
+    float* const warps = warps_all + set * 4 * R;
+    float* const factor_all = reinterpret_cast<float*>(sgen + C::kOffScale) + c0;
+    float* const factor = factor_all + set * R;
     // where this key's probabilities stand among the keys of P: as V's tokens do in tensor memory
     const int place = L::kFp4 ? v_scale_place(key) : key;
+    const uint32_t p_row = (uint32_t)((place >> 3) * (R / 8) * 128 + (c0 >> 3) * 128 + (place & 7) * 16);
+    const uint32_t o_mine = tmem + lanes + C::kO + set * R + c0;
     Walk w = w0;
-    int item = 0, kt_first = w0.kt;
-    bool fresh = true;
+    int item = 0, kt_first = w0.kt, last = 0;
+    bool fresh = true, started = false;                             // of the item; has this set had a tile of it?
     float l[N];
     for (int i = 0; i < n_tiles; ++i) {
       const int buf = i & 1, ph = (i >> 1) & 1;
@@ -546,143 +566,184 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         }
 #pragma unroll
         for (int r = 0; r < N; ++r) l[r] = 0.f;
+        fresh = started = false;
       }
-      if (ok) ok = mbar_wait(bar(C::S_FULL + buf), ph, abort_at);
-      if (fresh) {                                                  // (Q's constants were there before its products were issued)
-        if (key < N) cm[key] = make_float2(reinterpret_cast<const float*>(sgen + C::kOffC)[(item & 3) * R + c0 + key], INFINITY);
-        bar_sync(id, 128);
-      }
-      tc_fence_after();
-      const uint32_t scores = tmem + lanes + C::kS + R * buf + c0;
-      uint32_t raw[N];
-      tmem_ld_x(scores, raw);
-      tmem_wait_ld();
-      const int pos = w.kt * kTile + key;
-      const uint32_t held = valid_ring[i % C::kRing];
-      const bool context = pos < w.ctx && (held >> (key >> p.cache.log_page) & 1);
-      const bool draft = !context && pos >= w.ctx && pos < w.len && (held >> (key >> p.cache.log_page) & 1);
-      // scores in octaves above the rows' references (+ kShift); those that are not seen go to -infinity
-      float x[N], top = -INFINITY;
-      const bool plain = __all_sync(0xffffffffu, context);
-      auto relative = [&](bool references) {
-#pragma unroll
-        for (int r = 0; r < N; ++r) {
-          const float2 k = cm[r];
-          x[r] = fmaf(__uint_as_float(raw[r]), k.x, references ? k.y : 0.f);
+      if (C::kSets == 1 || buf == set) {
+        if (ok) ok = mbar_wait(bar(C::S_FULL + buf), ph, abort_at);
+        if (!started) {                                             // (Q's constants were there before its products were issued)
+          if (key < N) cm[key] = make_float2(reinterpret_cast<const float*>(sgen + C::kOffC)[(item & 3) * R + c0 + key], INFINITY);
+          bar_sync(id, 128);
         }
-        if (!plain) {
-#pragma unroll
-          for (int r = 0; r < N; ++r)
-            if (!(context || (draft && (bits[r] >> (pos - w.ctx) & 1)))) x[r] = -INFINITY;
-        }
-      };
-      relative(true);
-#pragma unroll
-      for (int r = 0; r < N; ++r) top = fmaxf(top, x[r]);
-      if (bar_any(id, 128, fresh || top > kLag + kShift)) {
-        // the references move: to the largest score seen so far (the scores are read again: kept, they would cost as many registers)
-        tmem_ld_x(scores, raw);
+        tc_fence_after();
+        const uint32_t scores = tmem + lanes + C::kS + R * buf + c0;
+        uint32_t raw[N];
+        tmem_ld_32x32b_x16(scores, raw);
         tmem_wait_ld();
-        relative(false);
+        const int pos = w.kt * kTile + key;
+        const bool held = valid_ring[i % C::kRing] >> (key >> p.cache.log_page) & 1;
+        const bool context = pos < w.ctx && held, draft = !context && pos >= w.ctx && pos < w.len && held;
+        // scores in octaves above the rows' references (+ kShift); those that are not seen go to -infinity
+        float x[N], top = -INFINITY;
+        uint32_t rows_seeing = context ? 0xFFFFu : 0u;
+        if (draft) {                                                // (a loop: unrolled, its loads and shifts ran in every tile)
+#pragma unroll 1
+          for (int r = 0; r < N; ++r) rows_seeing |= (uint32_t)(bits[r] >> (pos - w.ctx) & 1ull) << r;
+        }
+        const bool plain = __all_sync(0xffffffffu, context);
+        auto relative = [&](bool references) {
 #pragma unroll
-        for (int r = 0; r < N; ++r) {
-          const float m = warp_max(x[r]);
-          if (lane == 0) of_warp[r] = m;
-        }
-        bar_sync(id, 128);
-        if (key < N) {
-          const float old = kShift - cm[key].y;                     // -infinity: none yet
-          const float m = fmaxf(fmaxf(fmaxf(warps[key], warps[R + key]), fmaxf(warps[2 * R + key], warps[3 * R + key])), old);
-          factor[key] = m == -INFINITY ? 1.f : exp2_approx(old - m);
-          cm[key].y = kShift - m;
-        }
-        bar_sync(id, 128);
-        tmem_ld_x(scores, raw);
-        tmem_wait_ld();
+          for (int r = 0; r < N; r += 2) {
+            const float4 k = *reinterpret_cast<const float4*>(cm + r);
+            x[r] = fmaf(__uint_as_float(raw[r]), k.x, references ? k.y : 0.f);
+            x[r + 1] = fmaf(__uint_as_float(raw[r + 1]), k.z, references ? k.w : 0.f);
+          }
+          if (!plain) {
+#pragma unroll
+            for (int r = 0; r < N; ++r)
+              if (!(rows_seeing >> r & 1)) x[r] = -INFINITY;
+          }
+        };
         relative(true);
 #pragma unroll
-        for (int r = 0; r < N; ++r) l[r] *= factor[r];
-        if (!fresh) {
-          // O of the tiles before
-          if (ok) ok = mbar_wait(bar(C::PV_DONE + (buf ^ 1)), ((i - 1) >> 1) & 1, abort_at);
-          tc_fence_after();
-          uint32_t o[N];
-          tmem_ld_x(tmem + lanes + C::kO + c0, o);
+        for (int r = 0; r < N; ++r) top = fmaxf(top, x[r]);
+        if (bar_any(id, 128, !started || top > kLag + kShift)) {
+          // the references move: to the largest score seen so far (the scores are read again: kept, they would cost as many registers)
+          tmem_ld_32x32b_x16(scores, raw);
           tmem_wait_ld();
+          relative(false);
 #pragma unroll
-          for (int r = 0; r < N; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * factor[r]);
+          for (int r = 0; r < N; ++r) {
+            const float m = warp_max(x[r]);
+            if (lane == 0) warps[quarter * R + r] = m;
+          }
+          bar_sync(id, 128);
+          if (key < N) {
+            const float old = kShift - cm[key].y;                   // -infinity: none yet
+            const float m = fmaxf(fmaxf(fmaxf(warps[key], warps[R + key]), fmaxf(warps[2 * R + key], warps[3 * R + key])), old);
+            factor[key] = m == -INFINITY ? 1.f : exp2_approx(old - m);
+            cm[key].y = kShift - m;
+          }
+          bar_sync(id, 128);
+          tmem_ld_32x32b_x16(scores, raw);
+          tmem_wait_ld();
+          relative(true);
 #pragma unroll
-          for (int r = 0; r < N; r += 16) tmem_st_32x32b_x16(tmem + lanes + C::kO + c0 + r, o + r);
-          tmem_wait_st();
-          tc_fence_before();
+          for (int r = 0; r < N; ++r) l[r] *= factor[r];
+          if (started) {                                            // O of this set's tiles before
+            if (ok) ok = mbar_wait(bar(C::PV_DONE + (last & 1)), (last >> 1) & 1, abort_at);
+            tc_fence_after();
+            uint32_t o[N];
+            tmem_ld_32x32b_x16(o_mine, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int r = 0; r < N; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * factor[r]);
+            tmem_st_32x32b_x16(o_mine, o);
+            tmem_wait_st();
+          }
         }
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (ok && lane == 0) mbar_arrive(bar(C::S_FREE + buf));
-      if (ok) ok = mbar_wait(bar(C::PV_DONE + buf), ph ^ 1, abort_at);   // P of tile i - 2 has been read
-      uint8_t* const dst = sgen + C::kOffP + buf * C::kP + (place >> 3) * (R / 8) * 128 + (c0 >> 3) * 128 + (place & 7) * 16;
+        tc_fence_before();
+        __syncwarp();
+        if (ok && lane == 0) mbar_arrive(bar(C::S_FREE + buf));
+        if (ok) ok = mbar_wait(bar(C::PV_DONE + buf), ph ^ 1, abort_at);   // P of tile i - 2 has been read
+        uint8_t* const dst = sgen + C::kOffP + buf * C::kP + p_row;
 #pragma unroll
-      for (int r = 0; r < N; r += 8) {
-        uint32_t h[4];
+        for (int r = 0; r < N; r += 8) {
+          uint32_t h[4];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const float a = exp2_approx(x[r + 2 * y]), b = exp2_approx(x[r + 2 * y + 1]);
-          l[r + 2 * y] += a;
-          l[r + 2 * y + 1] += b;
-          h[y] = pack_pair<__half>(a, b);
+          for (int y = 0; y < 4; ++y) {
+            const float a = exp2_approx(x[r + 2 * y]), b = exp2_approx(x[r + 2 * y + 1]);
+            l[r + 2 * y] += a;
+            l[r + 2 * y + 1] += b;
+            h[y] = pack_pair<__half>(a, b);
+          }
+          *reinterpret_cast<uint4*>(dst + (r >> 3) * 128) = make_uint4(h[0], h[1], h[2], h[3]);
         }
-        *reinterpret_cast<uint4*>(dst + (r >> 3) * 128) = make_uint4(h[0], h[1], h[2], h[3]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (ok && lane == 0) mbar_arrive(bar(C::P_FULL + buf));
+        started = true;
+        last = i;
       }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (ok && lane == 0) mbar_arrive(bar(C::P_FULL + buf));
-      fresh = false;
       if (w.kt + 1 == w.nt || i + 1 == n_tiles) {
-        // ---- end of the item, or of this CTA's part of it
+        // ---- end of the item, or of this CTA's part of it: the sets of these rows together
         const bool whole = kt_first == 0 && w.kt + 1 == w.nt;
-        const float sum = warp_sums<N>(l, lane);
-        if (lane < N) of_warp[lane] = sum;
-        if (ok) ok = mbar_wait(bar(C::PV_DONE + buf), ph, abort_at);
-        bar_sync(id, 128);
+        const float sum = warp_sums(l, lane);
+        if (lane < N) warps[quarter * R + lane] = sum;
+        if (!started && key < N) cm[key].y = INFINITY;
+        if (ok && started) ok = mbar_wait(bar(C::PV_DONE + (last & 1)), (last >> 1) & 1, abort_at);
+        bar_sync(id_all, 128 * C::kSets);
         const int n = drafted(p, w.b);
         const long long out0 = ((long long)w.b * p.H + (long long)kvh * p.group) * p.T;
         const int slot = 2 * (int)blockIdx.x + (kt_first == 0);
-        if (key < N) {
-          const float total_l = warps[key] + warps[R + key] + warps[2 * R + key] + warps[3 * R + key], m = kShift - cm[key].y;
-          const int row = row0 + key;
-          if (whole) {
-            // nothing seen: 0, not 0 / 0
-            factor[key] = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + kvh));
-            if (ok && p.lse && row < p.rows && row % p.T < n)
-              p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (m - kShift + log2f(total_l)) * 0.6931471805599453f;
-          } else if (ok) {
-            p.part_ml[(size_t)slot * R + c0 + key] = make_float2(m, total_l);
+        if (set == 0 && key < N) {
+          float m[C::kSets], part[C::kSets], f[C::kSets], top = -INFINITY, total_l = 0.f;
+#pragma unroll
+          for (int k = 0; k < C::kSets; ++k) {
+            const float* const wk = warps_all + k * 4 * R + key;
+            part[k] = wk[0] + wk[R] + wk[2 * R] + wk[3 * R];
+            m[k] = kShift - cm_all[k * R + key].y;
+            top = fmaxf(top, m[k]);
           }
+#pragma unroll
+          for (int k = 0; k < C::kSets; ++k) {
+            f[k] = m[k] == top ? 1.f : exp2_approx(m[k] - top);     // (both -infinity: nothing seen)
+            if (m[k] == -INFINITY && part[k] == 0.f) f[k] = 0.f;    // no tile, or nothing seen in them: what its O holds does not count
+            total_l += f[k] * part[k];
+          }
+          const int row = row0 + key;
+          float inv = 1.f;
+          if (whole) {
+            inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + kvh));     // nothing seen: 0, not 0 / 0
+            if (ok && p.lse && row < p.rows && row % p.T < n)
+              p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (top - kShift + log2f(total_l)) * 0.6931471805599453f;
+          } else if (ok) {
+            p.part_ml[(size_t)slot * R + c0 + key] = make_float2(top, total_l);
+          }
+#pragma unroll
+          for (int k = 0; k < C::kSets; ++k) factor_all[k * R + key] = f[k] * inv;
         }
         if (group == 0 && key == 0 && kt_first == 0 && ok) {
-          const long long item_first = t0 + i - w.kt;               // tile of the list that is the item's first
+          const long long item_first = find[2] + i - w.kt;               // tile of the list that is the item's first
           p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(item_first + w.nt - 1));
         }
-        bar_sync(id, 128);
+        bar_sync(id_all, 128 * C::kSets);
         tc_fence_after();
-        uint32_t o[N];
-        tmem_ld_x(tmem + lanes + C::kO + c0, o);
+        // a set takes its share of the rows
+        constexpr int M = N / C::kSets;
+        const int r0 = set * M;
+        float o[M];
+        uint32_t v[C::kSets][M];
+#pragma unroll
+        for (int k = 0; k < C::kSets; ++k) {
+          const uint32_t from = tmem + lanes + C::kO + k * R + c0 + r0;
+          if constexpr (M == 8) tmem_ld_32x32b_x8(from, v[k]);
+          else tmem_ld_32x32b_x16(from, v[k]);
+        }
         tmem_wait_ld();
+#pragma unroll
+        for (int r = 0; r < M; ++r) {
+          o[r] = 0.f;
+#pragma unroll
+          for (int k = 0; k < C::kSets; ++k) {
+            const float f = factor_all[k * R + r0 + r];
+            o[r] += f == 0.f ? 0.f : __uint_as_float(v[k][r]) * f;
+          }
+        }
         tc_fence_before();
-        const uint32_t keep = __ballot_sync(0xffffffffu, lane < N && row0 + lane < p.rows && (row0 + lane) % p.T < n);
+        if (C::kSets > 1) bar_sync(id_all, 128 * C::kSets);         // the next item's products may overwrite either O
+        const uint32_t keep = __ballot_sync(0xffffffffu, lane < M && row0 + r0 + lane < p.rows && (row0 + r0 + lane) % p.T < n);
         if (ok && key < D) {
           if (whole) {
-            uint16_t* const dst = static_cast<uint16_t*>(p.out) + (size_t)(out0 + row0) * D + key;
+            uint16_t* const dst = static_cast<uint16_t*>(p.out) + (size_t)(out0 + row0 + r0) * D + key;
 #pragma unroll
-            for (int r = 0; r < N; ++r) {
-              const float y = __uint_as_float(o[r]) * factor[r];
-              const uint16_t h = p.half ? __half_as_ushort(__float2half_rn(y)) : __bfloat16_as_ushort(__float2bfloat16_rn(y));
+            for (int r = 0; r < M; ++r) {
+              const uint16_t h = p.half ? __half_as_ushort(__float2half_rn(o[r])) : __bfloat16_as_ushort(__float2bfloat16_rn(o[r]));
               if (keep >> r & 1) dst[r * D] = h;
             }
           } else {
+            float* const dst = p.part + ((size_t)slot * R + c0 + r0) * D + key;
 #pragma unroll
-            for (int r = 0; r < N; ++r) p.part[((size_t)slot * R + c0 + r) * D + key] = __uint_as_float(o[r]);
+            for (int r = 0; r < M; ++r) dst[r * D] = o[r];
           }
         }
         fresh = true;
