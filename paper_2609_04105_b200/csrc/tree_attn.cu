@@ -16,7 +16,7 @@
 //   warps 4-11   V: codes of an index, 64 tokens -> f16 -> tensor memory
 //   warps 12-    softmax, groups of four, a thread per key and 16 rows: exp2, P^T -> shared memory; rescale of O, end of an item.  Up to 32
 //                rows, tiles alternate between two sets of groups, each with references, sums and an O of its own
-//   then         one warp brings the pages in (one bulk copy per page: a (page, head) record is one run of bytes), one issues the products
+//   then         one warp brings the pages in (one bulk copy per page: a (page, head) record is one run of bytes), two issue the products
 //
 // The reference of a row, its maximum at some time, moves only when a score exceeds it by more than 2^8: probabilities up to 256 fit f16 as
 // well, and neither a reduction over keys (they are in lanes) nor a pass over O is then part of an ordinary tile.
@@ -82,15 +82,16 @@ __device__ __forceinline__ unsigned long long row_mask(const TreeParams& p, int 
   return p.mask ? __ldg(p.mask + (size_t)b * p.T + t) : (2ull << t) - 1;
 }
 
-template <int FMT, int D, int R>
+// R: rows of a tile; N: rows of a softmax thread (8 only where the item has no more: the other columns of R = 16 are zero)
+template <int FMT, int D, int R, int N>
 struct TreeCfg {
   using L = RecordLayout<FMT, D>;
-  static constexpr int kN = 16;                                    // rows of a softmax thread
-  static constexpr int kColGroups = R / kN;
+  static constexpr int kN = N;
+  static constexpr int kColGroups = R > 16 ? R / N : 1;
   static constexpr int kSets = R <= 32 ? 2 : 1;                    // sets of softmax groups that tiles alternate between
   static constexpr int kFirstV = 4, kFirstSoftmax = 12;            // warps
-  static constexpr int kProducer = kFirstSoftmax + 4 * kColGroups * kSets, kIssuer = kProducer + 1;
-  static constexpr int kThreads = 32 * (kIssuer + 1);
+  static constexpr int kProducer = kFirstSoftmax + 4 * kColGroups * kSets, kIssuerS = kProducer + 1, kIssuerO = kProducer + 2;
+  static constexpr int kThreads = 32 * (kIssuerO + 1);
   static constexpr int kStage = kTile * 2 * L::kToken;
   static constexpr int kStages = kStage >= 32768 ? 4 : kStage > 16384 ? 6 : 8;
   static constexpr int kQ = R * D * 2, kP = kTile * R * 2;
@@ -144,20 +145,30 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// sum over the warp of each of 16 values: lanes i and i + 16 end with the total of value i
-__device__ __forceinline__ float warp_sums(float (&v)[16], int lane) {
+// sum over the warp of each of N values: lane i ends with the total of value i % N
+template <int N>
+__device__ __forceinline__ float warp_sums(float (&v)[N], int lane) {
 #pragma unroll
-  for (int step = 8; step; step >>= 1) {
+  for (int step = N / 2; step; step >>= 1) {
     const bool up = lane & step;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N / 2; ++i) {
       if (i < step) {
         const float give = up ? v[i] : v[i + step], keep = up ? v[i + step] : v[i];
         v[i] = keep + __shfl_xor_sync(0xffffffffu, give, step);
       }
     }
   }
-  return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
+  float s = v[0];
+#pragma unroll
+  for (int step = N; step < 32; step <<= 1) s += __shfl_xor_sync(0xffffffffu, s, step);
+  return s;
+}
+template <int N>
+__device__ __forceinline__ void tmem_ld_cols(uint32_t addr, uint32_t (&r)[N]) {
+  if constexpr (N == 16) tmem_ld_32x32b_x16(addr, r);
+  else if constexpr (N == 8) tmem_ld_32x32b_x8(addr, r);
+  else tmem_ld_32x32b_x4(addr, r);
 }
 // of the eight tokens from position `pos` on, those that count (bit t: token t): the context, and the drafted tokens that some row sees
 __device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long long seen, int pos) {
@@ -167,9 +178,9 @@ __device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long lon
   return left >= 8 ? v : left > 0 ? v & ((1u << left) - 1) : 0u;
 }
 
-template <int FMT, int D, int R>
-__global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(const TreeParams p) {
-  using C = TreeCfg<FMT, D, R>;
+template <int FMT, int D, int R, int N_>
+__global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kernel(const TreeParams p) {
+  using C = TreeCfg<FMT, D, R, N_>;
   using L = typename C::L;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -199,7 +210,11 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
     *abort_word = 0;
     fence_barrier_init();
   }
-  if (warp == C::kIssuer) { tmem_alloc(tslot, 512); tmem_relinquish(); }
+  if (warp == C::kIssuerS) { tmem_alloc(tslot, 512); tmem_relinquish(); }
+  if (C::kN < 16) {                                                 // probabilities of the rows that are none
+    for (int i = threadIdx.x; i < 2 * C::kP / 16; i += C::kThreads) *reinterpret_cast<uint4*>(sgen + C::kOffP + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+  }
   wait_prior_grids();
 
   // ---- this CTA's run of tiles
@@ -291,58 +306,61 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
       for (int k = 0; k < C::kStages; ++k)
         for (int spin = 0; spin < (1 << 12) && !mbar_try_wait(bar(C::RING + k), k < s ? ph : ph ^ 1); ++spin) {}
     }
-  } else if (warp == C::kIssuer) {
-    // ===================================================================== products
-    // Q: K-major, core matrices of 8 rows x 16 bytes, those along d neighbours; P: row-major (MN), core matrices of 8 keys x 16 bytes (8 rows),
-    // those along rows neighbours
-    constexpr uint32_t kIdescS = make_idesc_f16(128, R, false), kIdescO = make_idesc_f16(128, R, true);
+  } else if (warp == C::kIssuerS) {
+    // ===================================================================== S^T = K Q^T
+    // Q: K-major, core matrices of 8 rows x 16 bytes, those along d neighbours.  A product takes 45 clocks or more whatever its N up to 64,
+    // and its issue waits for the one before: two warps issue, so that the waits of one lie under the products of the other.
+    constexpr uint32_t kIdesc = make_idesc_f16(128, R, false);
     Walk w = w0;
     int item = 0;
-    auto products_o = [&](int i, bool fresh) {                      // O^T (+)= V^T P^T of tile i
-      const int buf = i & 1, ph = (i >> 1) & 1;
-      if (ok) ok = mbar_wait(bar(C::VA_FULL + buf), ph, abort_at);
-      if (ok) ok = mbar_wait(bar(C::P_FULL + buf), ph, abort_at);
-      if (!ok) return;
-      tc_fence_after();
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          tc_mma_f16_ta(tmem + C::kO + (C::kSets == 2 ? R * buf : 0), tmem + C::kVA + 64 * buf + 8 * k,
-                        make_smem_desc(sbase + C::kOffP + buf * C::kP + k * 2 * (R / 8) * 128, (R / 8) * 128, 128, kSwzNone), kIdescO,
-                        !(fresh && k == 0));
-        tc_commit(bar(C::PV_DONE + buf));
-      }
-      __syncwarp();
-    };
-    // is the tile the first of its item here; the one before, the first of its item for its set of softmax groups?
-    bool fresh = true, first_before = true;
-    int of_item = 0;                                                // tiles of the item so far
+    bool fresh = true;
     for (int i = 0; i < n_tiles; ++i) {
       const int buf = i & 1, ph = (i >> 1) & 1;
       if (fresh && ok) ok = mbar_wait(bar(C::Q_FULL + (item & 1)), (item >> 1) & 1, abort_at);
-      if (ok) ok = mbar_wait(bar(C::KA_FULL + buf), ph, abort_at);
       if (ok) ok = mbar_wait(bar(C::S_FREE + buf), ph ^ 1, abort_at);
+      if (ok) ok = mbar_wait(bar(C::KA_FULL + buf), ph, abort_at);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
           tc_mma_f16_ta(tmem + C::kS + R * buf, tmem + C::kKA + (D / 2) * buf + 8 * k,
-                        make_smem_desc(sbase + C::kOffQ + (item & 1) * C::kQ + k * 256, 128, (D / 8) * 128, kSwzNone), kIdescS, k > 0);
+                        make_smem_desc(sbase + C::kOffQ + (item & 1) * C::kQ + k * 256, 128, (D / 8) * 128, kSwzNone), kIdesc, k > 0);
         tc_commit(bar(C::S_FULL + buf));
         tc_commit(bar(C::KA_FREE + buf));
       }
       __syncwarp();
-      if (i > 0) products_o(i - 1, first_before);                   // one tile behind: S of the next is under way while P is made
-      if (!ok) break;
-      first_before = of_item < C::kSets;
       fresh = w.kt + 1 == w.nt;
-      of_item = fresh ? 0 : of_item + 1;
       item += fresh;
       advance(w, p, units);
     }
-    if (ok && n_tiles > 0) products_o(n_tiles - 1, first_before);
     if (!ok && elect_one()) tc_commit(bar(C::DRAIN));
+  } else if (warp == C::kIssuerO) {
+    // ===================================================================== O^T += V^T P^T
+    // P: rows are contiguous (MN-major), core matrices of 8 keys x 16 bytes (8 rows), those along rows neighbours
+    constexpr uint32_t kIdesc = make_idesc_f16(128, R, true);
+    Walk w = w0;
+    int of_item = 0;                                                // tiles of the item so far
+    for (int i = 0; i < n_tiles; ++i) {
+      const int buf = i & 1, ph = (i >> 1) & 1;
+      if (ok) ok = mbar_wait(bar(C::VA_FULL + buf), ph, abort_at);
+      if (ok) ok = mbar_wait(bar(C::P_FULL + buf), ph, abort_at);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t more = of_item >= C::kSets;                    // not the first tile of the item that this O gets
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          tc_mma_f16_ta(tmem + C::kO + (C::kSets == 2 ? R * buf : 0), tmem + C::kVA + 64 * buf + 8 * k,
+                        make_smem_desc(sbase + C::kOffP + buf * C::kP + k * 2 * (R / 8) * 128, (R / 8) * 128, 128, kSwzNone), kIdesc,
+                        k > 0 ? 1u : more);
+        tc_commit(bar(C::PV_DONE + buf));
+      }
+      __syncwarp();
+      of_item = w.kt + 1 == w.nt ? 0 : of_item + 1;
+      advance(w, p, units);
+    }
+    if (!ok && elect_one()) tc_commit(bar(C::DRAIN + 1));
   } else if (warp < 4) {
     // ===================================================================== Q and K
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
@@ -459,6 +477,13 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
     const int quarter = warp & 3, half = (warp - C::kFirstV) >> 2, e = quarter * 32 + lane;      // index of the head dimension
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     uint8_t* const scales = sgen + C::kOffVScale + (warp - C::kFirstV) * 256;
+    // this lane's codes of its 64 tokens in a stage: four chunks of sixteen tokens, inside a page or at the same place of the next
+    const int at0 = 64 * half, log_page = p.cache.log_page, record = p.cache.record;
+    const uint32_t codes0 = (uint32_t)((at0 >> log_page) * record + L::v_codes(P) + (at0 & (P - 1)) * L::kRow + (L::kFp4 ? e >> 1 : e) * 16);
+    const uint32_t step1 = P == 16 ? (uint32_t)record : 16 * L::kRow;
+    const uint32_t step2 = P <= 32 ? (uint32_t)((32 >> log_page) * record) : 32 * L::kRow;
+    const int at_sc = at0 + 4 * (lane & 15);
+    const uint32_t scale0 = (uint32_t)((at_sc >> log_page) * record + L::v_scales(P) + (e >> 4) * P + (at_sc & (P - 1)));
     Walk w = w0;
     int s = 0, sph = 0, b_of = -1;
     unsigned long long seen = 0;                                    // drafted tokens that some row sees
@@ -478,33 +503,33 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         const int first = w.kt * kTile;
         // what no row sees counts as zero: it may be any bytes, and a probability of 0 times a NaN would be one
         const bool all = first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
-        const uint8_t* const stage = sgen + C::kOffStage + s * C::kStage + L::v_codes(P);
+        const uint8_t* const stage = sgen + C::kOffStage + s * C::kStage;
         const uint32_t dst = tmem + lanes + C::kVA + 64 * buf + 32 * half, shift = 4 * (e & 1);
         if (quarter * 32 < D) {
           if (L::kFp4) {
             // the scales of this warp's two blocks and 64 tokens, once for all sixteen lanes that need them
-            const int at = 64 * half + 4 * (lane & 15), slot = at >> p.cache.log_page;
-            uint32_t sc = *reinterpret_cast<const uint32_t*>(stage + slot * p.cache.record + P * L::kRow + (e >> 4) * P + (at & (P - 1)));
+            uint32_t sc = *reinterpret_cast<const uint32_t*>(stage + scale0);
             if (!all) {
-              const uint32_t v = held >> slot & 1 ? permute_eight(valid_eight(w, seen, first + (at & ~7))) : 0u;
-              sc &= byte_mask(at & 4 ? v >> 4 : v);
+              const uint32_t v = held >> (at_sc >> log_page) & 1 ? permute_eight(valid_eight(w, seen, first + (at_sc & ~7))) : 0u;
+              sc &= byte_mask(at_sc & 4 ? v >> 4 : v);
             }
             uint32_t f[2];
             cvt_f16x2_e4m3x4(sc, f);
             *reinterpret_cast<uint2*>(scales + lane * 8) = make_uint2(f[0], f[1]);
             __syncwarp();
           }
+          const uint8_t* codes = stage + codes0;
+          const uint8_t* factors = scales + (lane >> 4) * 128;
 #pragma unroll 2
           for (int j = 0; j < 64; j += 16) {                        // sixteen tokens
-            const int at = 64 * half + j, slot = at >> p.cache.log_page, t = at & (P - 1);
-            const uint8_t* const rec = stage + slot * p.cache.record;
-            uint4 raw = *reinterpret_cast<const uint4*>(rec + t * L::kRow + (L::kFp4 ? e >> 1 : e) * 16);
+            uint4 raw = *reinterpret_cast<const uint4*>(j & 16 ? codes + step1 : codes);
+            if (j & 16) codes += step2;
             uint32_t h[8];
             if (L::kFp4) {
               const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
               for (int x = 0; x < 2; ++x) {                         // eight tokens: i and i + 4 in a byte
-                const uint4 f = *reinterpret_cast<const uint4*>(scales + (lane >> 4) * 128 + j * 2 + 16 * x);
+                const uint4 f = *reinterpret_cast<const uint4*>(factors + 2 * j + 16 * x);
                 cvt_f16x2_e2m1x8((cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u), h + 4 * x);
                 h[4 * x] = mul_half2(h[4 * x], f.x);
                 h[4 * x + 1] = mul_half2(h[4 * x + 1], f.y);
@@ -513,8 +538,9 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
               }
             } else {
               if (!all) {
-                const uint32_t lo = held >> slot & 1 ? valid_eight(w, seen, first + at) : 0u;
-                const uint32_t hi = held >> slot & 1 ? valid_eight(w, seen, first + at + 8) : 0u;
+                const bool here = held >> ((at0 + j) >> log_page) & 1;
+                const uint32_t lo = here ? valid_eight(w, seen, first + at0 + j) : 0u;
+                const uint32_t hi = here ? valid_eight(w, seen, first + at0 + j + 8) : 0u;
                 raw.x &= byte_mask(lo); raw.y &= byte_mask(lo >> 4); raw.z &= byte_mask(hi); raw.w &= byte_mask(hi >> 4);
               }
               const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -577,7 +603,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         tc_fence_after();
         const uint32_t scores = tmem + lanes + C::kS + R * buf + c0;
         uint32_t raw[N];
-        tmem_ld_32x32b_x16(scores, raw);
+        tmem_ld_cols(scores, raw);
         tmem_wait_ld();
         const int pos = w.kt * kTile + key;
         const bool held = valid_ring[i % C::kRing] >> (key >> p.cache.log_page) & 1;
@@ -608,7 +634,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         for (int r = 0; r < N; ++r) top = fmaxf(top, x[r]);
         if (bar_any(id, 128, !started || top > kLag + kShift)) {
           // the references move: to the largest score seen so far (the scores are read again: kept, they would cost as many registers)
-          tmem_ld_32x32b_x16(scores, raw);
+          tmem_ld_cols(scores, raw);
           tmem_wait_ld();
           relative(false);
 #pragma unroll
@@ -624,7 +650,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
             cm[key].y = kShift - m;
           }
           bar_sync(id, 128);
-          tmem_ld_32x32b_x16(scores, raw);
+          tmem_ld_cols(scores, raw);
           tmem_wait_ld();
           relative(true);
 #pragma unroll
@@ -633,11 +659,12 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
             if (ok) ok = mbar_wait(bar(C::PV_DONE + (last & 1)), (last >> 1) & 1, abort_at);
             tc_fence_after();
             uint32_t o[N];
-            tmem_ld_32x32b_x16(o_mine, o);
+            tmem_ld_cols(o_mine, o);
             tmem_wait_ld();
 #pragma unroll
             for (int r = 0; r < N; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * factor[r]);
-            tmem_st_32x32b_x16(o_mine, o);
+            if constexpr (N == 16) tmem_st_32x32b_x16(o_mine, o);
+            else tmem_st_32x32b_x8(o_mine, o);
             tmem_wait_st();
           }
         }
@@ -716,8 +743,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
 #pragma unroll
         for (int k = 0; k < C::kSets; ++k) {
           const uint32_t from = tmem + lanes + C::kO + k * R + c0 + r0;
-          if constexpr (M == 8) tmem_ld_32x32b_x8(from, v[k]);
-          else tmem_ld_32x32b_x16(from, v[k]);
+          tmem_ld_cols(from, v[k]);
         }
         tmem_wait_ld();
 #pragma unroll
@@ -756,9 +782,10 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
   tc_fence_before();
   __syncthreads();
   if (*abort_word && threadIdx.x == 0 && p.status) *p.status = FP4ATTN_ERR_TIMEOUT;
-  if (warp == C::kIssuer) {
-    if (*abort_word && !ok && lane == 0)                            // given up: the products in flight end before tensor memory does
-      for (int spin = 0; spin < (1 << 14) && !mbar_try_wait(bar(C::DRAIN), 0); ++spin) {}
+  if (warp == C::kIssuerS) {
+    if (*abort_word && lane == 0)                                   // given up: the products in flight end before tensor memory does
+      for (int k = 0; k < 2; ++k)
+        for (int spin = 0; spin < (1 << 14) && !mbar_try_wait(bar(C::DRAIN + k), 0); ++spin) {}
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, 512);
@@ -823,14 +850,14 @@ TreePlan plan(int B, int H, int kv_heads, int T, int d) {
   return t;
 }
 
-template <int FMT, int D, int R>
+template <int FMT, int D, int R, int N>
 int launch_tree(const TreeParams& p, cudaStream_t st) {
-  using C = TreeCfg<FMT, D, R>;
+  using C = TreeCfg<FMT, D, R, N>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FP4ATTN_ERR_CUDA;
   static std::atomic<bool> attr_set[kMaxDevices];
   if (!attr_set[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(tree_kernel<FMT, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
+    if (cudaFuncSetAttribute(tree_kernel<FMT, D, R, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
     attr_set[dev].store(true, std::memory_order_release);
   }
   const int sms = device_sms();
@@ -838,14 +865,15 @@ int launch_tree(const TreeParams& p, cudaStream_t st) {
   const int units = p.cache.kv_heads * p.row_tiles;
   const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * units;
   const unsigned grid = (unsigned)std::min<long long>(std::min(sms, kMostCtas), most_tiles);
-  cudaError_t e = launch_overlapped(tree_kernel<FMT, D, R>, dim3(grid), C::kThreads, C::kSmem, st, p);
+  cudaError_t e = launch_overlapped(tree_kernel<FMT, D, R, N>, dim3(grid), C::kThreads, C::kSmem, st, p);
   if (e == cudaSuccess)
     e = launch_overlapped(tree_join_kernel<D, R>, dim3((unsigned)(p.B * units), (unsigned)(std::min(R, p.rows) + 3) / 4), 128u, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
 template <int FMT, int D>
 int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
-  return R == 16 ? launch_tree<FMT, D, 16>(p, st) : R == 32 ? launch_tree<FMT, D, 32>(p, st) : launch_tree<FMT, D, 64>(p, st);
+  if (p.rows <= 8) return launch_tree<FMT, D, 16, 8>(p, st);
+  return R == 16 ? launch_tree<FMT, D, 16, 16>(p, st) : R == 32 ? launch_tree<FMT, D, 32, 16>(p, st) : launch_tree<FMT, D, 64, 16>(p, st);
 }
 
 }  // namespace
