@@ -56,24 +56,35 @@ struct TreeParams {
   bool half, q_vector;
 };
 
-// ---- what a CTA walks: tiles of items, in order
+// ---- what a CTA walks: tiles of items, in order.  The roles of a scheduler run in turn and each is one chain of instructions, so a tile
+// costs what its loops execute besides the work: what changes with an item only is kept out of them (here: two instructions a tile).
 struct Walk {
-  int b, u, kt, nt;                        // batch entry, (KV head, row tile), tile of the item, tiles of the item
+  int b, u;                                // batch entry, (KV head, row tile)
+  int first, left;                         // first key of the tile, tiles of the item from here on
   int ctx, len;                            // context, keys (context and drafted tokens) that the table has room for
 };
-__device__ __forceinline__ void load_entry(Walk& w, const TreeParams& p) {
+__device__ __forceinline__ int load_entry(Walk& w, const TreeParams& p) {   // tiles of an item
   const long long room = (long long)p.cache.max_pages << p.cache.log_page;
   const int c = max(0, __ldg(p.context + w.b));
   w.ctx = (int)min((long long)c, room);
   w.len = (int)min((long long)c + p.T, room);
-  w.nt = (w.len + kTile - 1) / kTile;
+  return (w.len + kTile - 1) / kTile;
 }
-__device__ __forceinline__ void advance(Walk& w, const TreeParams& p, int units) {
-  if (++w.kt < w.nt) return;
-  w.kt = 0;
-  if (++w.u < units) return;
-  w.u = 0;
-  if (++w.b < p.B) load_entry(w, p);
+__device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
+__device__ __forceinline__ void next_item(Walk& w, const TreeParams& p, int units) {
+  w.first = 0;
+  if (++w.u == units) {
+    w.u = 0;
+    ++w.b;
+  }
+  if (w.b < p.B) w.left = load_entry(w, p);
+}
+// to the next tile; was this one the last of its item?
+__device__ __forceinline__ bool advance(Walk& w, const TreeParams& p, int units) {
+  w.first += kTile;
+  if (!rare(--w.left == 0)) return false;
+  next_item(w, p, units);
+  return true;
 }
 // drafted tokens that entry b has
 __device__ __forceinline__ int drafted(const TreeParams& p, int b) { return p.count ? max(0, min(__ldg(p.count + b), p.T)) : p.T; }
@@ -226,7 +237,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     const int per = (p.B + C::kThreads - 1) / C::kThreads, b0 = threadIdx.x * per, b1 = min(p.B, b0 + per);
     long long mine = 0;
     Walk w;
-    for (w.b = b0; w.b < b1; ++w.b) { load_entry(w, p); mine += (long long)w.nt * units; }
+    for (w.b = b0; w.b < b1; ++w.b) mine += (long long)load_entry(w, p) * units;
     long long incl = mine;
     for (int s = 1; s < 32; s <<= 1) {
       const long long o = __shfl_up_sync(0xffffffffu, incl, s);
@@ -249,9 +260,9 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     t1 = blockIdx.x < ctas ? (blockIdx.x + 1) * total / ctas : total;
     if (t0 < t1 && before <= t0 && t0 < before + mine) {            // one thread
       for (w.b = b0;; ++w.b) {
-        load_entry(w, p);
-        if (t0 < before + (long long)w.nt * units) break;
-        before += (long long)w.nt * units;
+        const long long here = (long long)load_entry(w, p) * units;
+        if (t0 < before + here) break;
+        before += here;
       }
       find[0] = w.b;
       find[1] = t0 - before;
@@ -264,10 +275,12 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     n_tiles = (int)min(t1 - t0, (long long)INT_MAX);
     __syncthreads();
     w0.b = t0 < t1 ? (int)find[0] : 0;
-    load_entry(w0, p);
+    const int nt = load_entry(w0, p);
     const long long r = t0 < t1 ? find[1] : 0;
-    w0.u = (int)(r / w0.nt);
-    w0.kt = (int)(r - (long long)w0.u * w0.nt);
+    w0.u = (int)(r / nt);
+    const int kt = (int)(r - (long long)w0.u * nt);
+    w0.first = kt * kTile;
+    w0.left = nt - kt;
   }
   auto cta_of = [&](long long tile) { return (int)(((tile + 1) * find[4] - 1) / find[3]); };
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
@@ -281,17 +294,17 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     const int slots = kTile >> p.cache.log_page;                    // pages of a tile: 1 to 8
     int s = 0, ph = 0;
     bool lost = false;
-    for (int i = 0; i < n_tiles; ++i, advance(w, p, units)) {
-      const int kvh = w.u / p.row_tiles, first = w.kt * kTile;
-      int page = -1;
-      if (lane < slots && first + lane * P < w.len) {
-        page = p.cache.page_of(w.b, first + lane * P);
-        lost |= page < 0;
-      }
-      lost |= w.kt == 0 && (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len;
+    auto page_of = [&](const Walk& at) {                            // of this lane, of the tile
+      if (lane >= slots || at.first + lane * P >= at.len) return -1;
+      const int page = p.cache.page_of(at.b, at.first + lane * P);
+      lost |= page < 0;
+      return page;
+    };
+    int page = n_tiles ? page_of(w) : -1, kvh = w.u / p.row_tiles;
+    if (n_tiles && (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len) lost = true;
+    for (int i = 0; i < n_tiles; ++i) {
       const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
-      if (ok) ok = mbar_wait(bar(C::RING + C::kStages + s), ph ^ 1, abort_at);
-      if (!ok) break;
+      if (!(ok = mbar_wait(bar(C::RING + C::kStages + s), ph ^ 1, abort_at))) break;
       if (lane == 0) {
         valid_ring[i % C::kRing] = held;
         mbar_arrive_expect_tx(bar(C::RING + s), __popc(held) * p.cache.record);
@@ -300,6 +313,11 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
       if (page >= 0)
         bulk_load_1d(sbase + C::kOffStage + s * C::kStage + lane * p.cache.record, p.cache.rec(page, kvh), p.cache.record, bar(C::RING + s));
       if (++s == C::kStages) { s = 0; ph ^= 1; }
+      if (rare(advance(w, p, units)) && i + 1 < n_tiles) {
+        kvh = w.u / p.row_tiles;
+        if ((long long)max(0, __ldg(p.context + w.b)) + p.T > w.len) lost = true;
+      }
+      if (i + 1 < n_tiles) page = page_of(w);                       // the table's entries come while this tile's stage is waited for
     }
     if (__any_sync(0xffffffffu, lost) && lane == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
     if (!ok) {                                                      // given up: the copies in flight end before shared memory does
@@ -316,10 +334,9 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     bool fresh = true;
     for (int i = 0; i < n_tiles; ++i) {
       const int buf = i & 1, ph = (i >> 1) & 1;
-      if (fresh && ok) ok = mbar_wait(bar(C::Q_FULL + (item & 1)), (item >> 1) & 1, abort_at);
-      if (ok) ok = mbar_wait(bar(C::S_FREE + buf), ph ^ 1, abort_at);
-      if (ok) ok = mbar_wait(bar(C::KA_FULL + buf), ph, abort_at);
-      if (!ok) break;
+      if (rare(fresh) && !(ok = mbar_wait(bar(C::Q_FULL + (item & 1)), (item >> 1) & 1, abort_at))) break;
+      if (!(ok = mbar_wait(bar(C::S_FREE + buf), ph ^ 1, abort_at))) break;
+      if (!(ok = mbar_wait(bar(C::KA_FULL + buf), ph, abort_at))) break;
       tc_fence_after();
       if (elect_one()) {
 #pragma unroll
@@ -330,9 +347,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         tc_commit(bar(C::KA_FREE + buf));
       }
       __syncwarp();
-      fresh = w.kt + 1 == w.nt;
+      fresh = advance(w, p, units);
       item += fresh;
-      advance(w, p, units);
     }
     if (!ok && elect_one()) tc_commit(bar(C::DRAIN));
   } else if (warp == C::kIssuerO) {
@@ -343,9 +359,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     int of_item = 0;                                                // tiles of the item so far
     for (int i = 0; i < n_tiles; ++i) {
       const int buf = i & 1, ph = (i >> 1) & 1;
-      if (ok) ok = mbar_wait(bar(C::VA_FULL + buf), ph, abort_at);
-      if (ok) ok = mbar_wait(bar(C::P_FULL + buf), ph, abort_at);
-      if (!ok) break;
+      if (!(ok = mbar_wait(bar(C::VA_FULL + buf), ph, abort_at))) break;
+      if (!(ok = mbar_wait(bar(C::P_FULL + buf), ph, abort_at))) break;
       tc_fence_after();
       const uint32_t more = of_item >= C::kSets;                    // not the first tile of the item that this O gets
       if (elect_one()) {
@@ -357,8 +372,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         tc_commit(bar(C::PV_DONE + buf));
       }
       __syncwarp();
-      of_item = w.kt + 1 == w.nt ? 0 : of_item + 1;
-      advance(w, p, units);
+      of_item = advance(w, p, units) ? 0 : of_item + 1;
     }
     if (!ok && elect_one()) tc_commit(bar(C::DRAIN + 1));
   } else if (warp < 4) {
@@ -371,8 +385,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     bool fresh = true;
     for (int i = 0; i < n_tiles; ++i) {
       const int buf = i & 1, ph = (i >> 1) & 1;
-      if (ok) ok = mbar_wait(bar(C::KA_FREE + buf), ph ^ 1, abort_at);
-      if (ok && fresh) {
+      if (!(ok = mbar_wait(bar(C::KA_FREE + buf), ph ^ 1, abort_at))) break;
+      if (rare(fresh)) {
         // Rows scaled by a power of two into f16's range (the largest element to [2^14, 2^15)): exact for 8-bit significands, and a row's
         // scores are scaled back by its constant.  The buffer is free: tile i - 2 or an earlier one was the last that read it.
         const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R;
@@ -422,8 +436,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::Q_FULL + (item & 1)));
       }
-      if (ok) ok = mbar_wait(bar(C::RING + s), sph, abort_at);
-      if (ok) {
+      if (!(ok = mbar_wait(bar(C::RING + s), sph, abort_at))) break;
+      {
         tc_fence_after();
         const uint8_t* const rec = sgen + C::kOffStage + s * C::kStage + slot * p.cache.record;
         const uint32_t dst = tmem + lanes + C::kKA + (D / 2) * buf;
@@ -468,9 +482,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         if (lane == 0) mbar_arrive(bar(C::KA_FULL + buf));
       }
       if (++s == C::kStages) { s = 0; sph ^= 1; }
-      fresh = w.kt + 1 == w.nt;
+      fresh = advance(w, p, units);
       item += fresh;
-      advance(w, p, units);
     }
   } else if (warp < C::kFirstSoftmax) {
     // ===================================================================== V
@@ -489,18 +502,18 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     unsigned long long seen = 0;                                    // drafted tokens that some row sees
     for (int i = 0; i < n_tiles; ++i, advance(w, p, units)) {
       const int buf = i & 1, ph = (i >> 1) & 1;
-      if (w.b != b_of) {
+      if (rare(w.b != b_of)) {
         b_of = w.b;
         const int n = drafted(p, w.b);
         seen = row_mask(p, w.b, lane, n) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n) : 0ull);
         seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
       }
-      if (ok) ok = mbar_wait(bar(C::PV_DONE + buf), ph ^ 1, abort_at);
-      if (ok) ok = mbar_wait(bar(C::RING + s), sph, abort_at);
-      if (ok) {
+      if (!(ok = mbar_wait(bar(C::PV_DONE + buf), ph ^ 1, abort_at))) break;
+      if (!(ok = mbar_wait(bar(C::RING + s), sph, abort_at))) break;
+      {
         tc_fence_after();
         const uint32_t held = valid_ring[i % C::kRing];
-        const int first = w.kt * kTile;
+        const int first = w.first;
         // what no row sees counts as zero: it may be any bytes, and a probability of 0 times a NaN would be one
         const bool all = first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
         const uint8_t* const stage = sgen + C::kOffStage + s * C::kStage;
@@ -509,7 +522,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           if (L::kFp4) {
             // the scales of this warp's two blocks and 64 tokens, once for all sixteen lanes that need them
             uint32_t sc = *reinterpret_cast<const uint32_t*>(stage + scale0);
-            if (!all) {
+            if (rare(!all)) {
               const uint32_t v = held >> (at_sc >> log_page) & 1 ? permute_eight(valid_eight(w, seen, first + (at_sc & ~7))) : 0u;
               sc &= byte_mask(at_sc & 4 ? v >> 4 : v);
             }
@@ -537,7 +550,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
                 h[4 * x + 3] = mul_half2(h[4 * x + 3], f.w);
               }
             } else {
-              if (!all) {
+              if (rare(!all)) {
                 const bool here = held >> ((at0 + j) >> log_page) & 1;
                 const uint32_t lo = here ? valid_eight(w, seen, first + at0 + j) : 0u;
                 const uint32_t hi = here ? valid_eight(w, seen, first + at0 + j + 8) : 0u;
@@ -578,16 +591,15 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     const uint32_t p_row = (uint32_t)((place >> 3) * (R / 8) * 128 + (c0 >> 3) * 128 + (place & 7) * 16);
     const uint32_t o_mine = tmem + lanes + C::kO + set * R + c0;
     Walk w = w0;
-    int item = 0, kt_first = w0.kt, last = 0;
+    int item = 0, part_first = 0, last = 0;                         // part_first: first key of the item that this CTA takes
     bool fresh = true, started = false;                             // of the item; has this set had a tile of it?
     float l[N];
     for (int i = 0; i < n_tiles; ++i) {
       const int buf = i & 1, ph = (i >> 1) & 1;
-      const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R + c0;
-      if (fresh) {
-        kt_first = w.kt;
+      if (rare(fresh)) {
+        part_first = w.first;
         if (key < N) {
-          const int row = row0 + key;
+          const int row = w.u % p.row_tiles * R + c0 + key;
           bits[key] = row < p.rows ? row_mask(p, w.b, row % p.T, drafted(p, w.b)) : 0ull;
         }
 #pragma unroll
@@ -596,7 +608,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
       }
       if (C::kSets == 1 || buf == set) {
         if (ok) ok = mbar_wait(bar(C::S_FULL + buf), ph, abort_at);
-        if (!started) {                                             // (Q's constants were there before its products were issued)
+        if (rare(!started)) {                                       // (Q's constants were there before its products were issued)
           if (key < N) cm[key] = make_float2(reinterpret_cast<const float*>(sgen + C::kOffC)[(item & 3) * R + c0 + key], INFINITY);
           bar_sync(id, 128);
         }
@@ -605,17 +617,22 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         uint32_t raw[N];
         tmem_ld_cols(scores, raw);
         tmem_wait_ld();
-        const int pos = w.kt * kTile + key;
-        const bool held = valid_ring[i % C::kRing] >> (key >> p.cache.log_page) & 1;
-        const bool context = pos < w.ctx && held, draft = !context && pos >= w.ctx && pos < w.len && held;
+        const uint32_t held = valid_ring[i % C::kRing];
         // scores in octaves above the rows' references (+ kShift); those that are not seen go to -infinity
         float x[N], top = -INFINITY;
-        uint32_t rows_seeing = context ? 0xFFFFu : 0u;
-        if (draft) {                                                // (a loop: unrolled, its loads and shifts ran in every tile)
+        uint32_t rows_seeing = 0xFFFFu;                             // rows of this thread that see its key
+        const bool plain = w.first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
+        if (rare(!plain)) {
+          const int pos = w.first + key;
+          const bool here = held >> (key >> p.cache.log_page) & 1;
+          if (!(here && pos < w.ctx)) {
+            rows_seeing = 0;
+            if (here && pos < w.len) {
 #pragma unroll 1
-          for (int r = 0; r < N; ++r) rows_seeing |= (uint32_t)(bits[r] >> (pos - w.ctx) & 1ull) << r;
+              for (int r = 0; r < N; ++r) rows_seeing |= (uint32_t)(bits[r] >> (pos - w.ctx) & 1ull) << r;
+            }
+          }
         }
-        const bool plain = __all_sync(0xffffffffu, context);
         auto relative = [&](bool references) {
 #pragma unroll
           for (int r = 0; r < N; r += 2) {
@@ -623,7 +640,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
             x[r] = fmaf(__uint_as_float(raw[r]), k.x, references ? k.y : 0.f);
             x[r + 1] = fmaf(__uint_as_float(raw[r + 1]), k.z, references ? k.w : 0.f);
           }
-          if (!plain) {
+          if (rare(!plain)) {
 #pragma unroll
             for (int r = 0; r < N; ++r)
               if (!(rows_seeing >> r & 1)) x[r] = -INFINITY;
@@ -632,7 +649,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         relative(true);
 #pragma unroll
         for (int r = 0; r < N; ++r) top = fmaxf(top, x[r]);
-        if (bar_any(id, 128, !started || top > kLag + kShift)) {
+        if (rare(bar_any(id, 128, !started || top > kLag + kShift))) {
           // the references move: to the largest score seen so far (the scores are read again: kept, they would cost as many registers)
           tmem_ld_cols(scores, raw);
           tmem_wait_ld();
@@ -691,9 +708,10 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         started = true;
         last = i;
       }
-      if (w.kt + 1 == w.nt || i + 1 == n_tiles) {
+      if (rare(w.left == 1 || i + 1 == n_tiles)) {
         // ---- end of the item, or of this CTA's part of it: the sets of these rows together
-        const bool whole = kt_first == 0 && w.kt + 1 == w.nt;
+        const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R + c0;
+        const bool whole = part_first == 0 && w.left == 1;
         const float sum = warp_sums(l, lane);
         if (lane < N) warps[quarter * R + lane] = sum;
         if (!started && key < N) cm[key].y = INFINITY;
@@ -701,7 +719,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         bar_sync(id_all, 128 * C::kSets);
         const int n = drafted(p, w.b);
         const long long out0 = ((long long)w.b * p.H + (long long)kvh * p.group) * p.T;
-        const int slot = 2 * (int)blockIdx.x + (kt_first == 0);
+        const int slot = 2 * (int)blockIdx.x + (part_first == 0);
         if (set == 0 && key < N) {
           float m[C::kSets], part[C::kSets], f[C::kSets], top = -INFINITY, total_l = 0.f;
 #pragma unroll
@@ -729,10 +747,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
 #pragma unroll
           for (int k = 0; k < C::kSets; ++k) factor_all[k * R + key] = f[k] * inv;
         }
-        if (group == 0 && key == 0 && kt_first == 0 && ok) {
-          const long long item_first = find[2] + i - w.kt;               // tile of the list that is the item's first
-          p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(item_first + w.nt - 1));
-        }
+        if (group == 0 && key == 0 && part_first == 0 && ok)
+          p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find[2] + i + w.left - 1));
         bar_sync(id_all, 128 * C::kSets);
         tc_fence_after();
         // a set takes its share of the rows
