@@ -12,10 +12,12 @@
 // run, so that sequences of unlike lengths and few long ones fill the card alike.  An item whose tiles fall to several CTAs is left as
 // partial (maximum, sum, O) in the workspace and joined by a second kernel in the order of its keys.
 //
-//   warps 0-3    K: codes of a key -> f16 -> tensor memory; Q of an item, scaled by a power of two per row, -> f16 -> shared memory
-//   warps 4-11   V: codes of an index, 64 tokens -> f16 -> tensor memory
-//   warps 12-    softmax, groups of four, a thread per key and 16 rows: exp2, P^T -> shared memory; rescale of O, end of an item.  Up to 32
-//                rows, tiles alternate between two sets of groups, each with references, sums and an O of its own
+//   K            codes of a key -> f16 -> tensor memory; Q of an item, scaled by a power of two per row, -> f16 -> shared memory
+//   V            codes of an index -> f16 -> tensor memory
+//   softmax      a thread per key and 8 or 16 rows: exp2, P^T -> shared memory; rescale of O, end of an item
+//   each in groups of four warps that tiles alternate between, where there are enough warps: a tile is one long chain of instructions for
+//   a warp, so the time of a tile is that of the slowest role's chain over its groups.  Up to 32 rows, the two sets of softmax groups have
+//   references, sums and an O each.
 //   then         one warp brings the pages in (one bulk copy per page: a (page, head) record is one run of bytes), two issue the products
 //
 // The reference of a row, its maximum at some time, moves only when a score exceeds it by more than 2^8: probabilities up to 256 fit f16 as
@@ -86,6 +88,15 @@ __device__ __forceinline__ bool advance(Walk& w, const TreeParams& p, int units)
   next_item(w, p, units);
   return true;
 }
+// n tiles on; how many items ended on the way, and whether the tile is the first of its item
+__device__ __forceinline__ int advance_by(Walk& w, const TreeParams& p, int units, int n, bool* fresh) {
+  int ended = 0;
+  for (int k = 0; k < n; ++k) {
+    *fresh = advance(w, p, units);
+    ended += *fresh;
+  }
+  return ended;
+}
 // drafted tokens that entry b has
 __device__ __forceinline__ int drafted(const TreeParams& p, int b) { return p.count ? max(0, min(__ldg(p.count + b), p.T)) : p.T; }
 __device__ __forceinline__ unsigned long long row_mask(const TreeParams& p, int b, int t, int n) {
@@ -100,23 +111,30 @@ struct TreeCfg {
   static constexpr int kN = N;
   static constexpr int kColGroups = R > 16 ? R / N : 1;
   static constexpr int kSets = R <= 32 ? 2 : 1;                    // sets of softmax groups that tiles alternate between
-  static constexpr int kFirstV = 4, kFirstSoftmax = 12;            // warps
+  static constexpr int kKGroups = R == 16 ? 2 : 1, kVGroups = 2;   // groups of four warps that tiles alternate between
+  static constexpr int kFirstV = 4 * kKGroups, kFirstSoftmax = kFirstV + 4 * kVGroups;         // warps
   static constexpr int kProducer = kFirstSoftmax + 4 * kColGroups * kSets, kIssuerS = kProducer + 1, kIssuerO = kProducer + 2;
   static constexpr int kThreads = 32 * (kIssuerO + 1);
+  static_assert(kThreads <= 1024, "warps");
   static constexpr int kStage = kTile * 2 * L::kToken;
   static constexpr int kStages = kStage >= 32768 ? 4 : kStage > 16384 ? 6 : 8;
+  // Buffers between the roles: deep enough that the hand-overs (some 200 clocks each) of one tile lie under the work on others
+  static constexpr int kSB = kSets == 2 ? 4 : 2, kVB = 3;          // scores; V^T in tensor memory and P
+  static constexpr int kKB = D == 64 ? 4 : R == 16 ? 3 : 2;        // K in tensor memory
+  static constexpr int kQB = kKB;                                  // Q: see the K warps
   static constexpr int kQ = R * D * 2, kP = kTile * R * 2;
-  static constexpr int kRing = 16;                                 // tiles whose page validity is remembered
+  // The softmax warps may be kKB + kSB tiles behind the K warps, and those kStages behind the producer: what they take from either
+  // past the barriers is kept for as many items and tiles.
+  static constexpr int kRingC = 8, kRing = 32;
+  static_assert(kKB + kSB <= kRingC && kStages + kKB + kSB <= kRing, "rings");
   // shared memory
   static constexpr int kOffStage = 0;
   static constexpr int kOffQ = kOffStage + kStages * kStage;
-  static constexpr int kOffP = kOffQ + 2 * kQ;
-  static constexpr int kOffVScale = kOffP + 2 * kP;                // f16 [8 warps][2 blocks][64 tokens]
-  static constexpr int kOffCM = kOffVScale + 2048;                 // float2 [kSets][R]: score constant, kShift minus the reference
-  // float [4][R]: score constants of the last items.  Four: Q of tile i is made when the products of tile i - 2 are done, so the
-  // softmax warps, which have then taken the scores of tile i - 4, may be three items behind
-  static constexpr int kOffC = kOffCM + 8 * R * kSets;
-  static constexpr int kOffBits = kOffC + 16 * R;                  // u64 [kSets][R]
+  static constexpr int kOffP = kOffQ + kQB * kQ;
+  static constexpr int kOffVScale = kOffP + kVB * kP;                // f16 [V warps][2 blocks][128 tokens]
+  static constexpr int kOffCM = kOffVScale + 4 * kVGroups * 512;                 // float [kSets][2][R]: kShift minus the reference; score constant
+  static constexpr int kOffC = kOffCM + 8 * R * kSets;             // float [kRingC][R]: score constants of the last items
+  static constexpr int kOffBits = kOffC + 4 * R * kRingC;                  // u64 [kSets][R]
   static constexpr int kOffWarp = kOffBits + 8 * R * kSets;        // float [kSets][4][R]: maxima or sums of the four warps
   static constexpr int kOffScale = kOffWarp + 16 * R * kSets;      // float [kSets][R]: factors on O
   static constexpr int kOffValid = kOffScale + 4 * R * kSets;      // u32 [kRing]
@@ -126,12 +144,47 @@ struct TreeCfg {
   static constexpr int kSmem = kOffBar + 512 + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
   // barriers
-  enum { KA_FULL = 0, KA_FREE = 2, VA_FULL = 4, S_FULL = 6, S_FREE = 8, P_FULL = 10, PV_DONE = 12, Q_FULL = 14, DRAIN = 16, RING = 18 };
-  static constexpr int kBars = RING + 2 * kStages;
+  enum { KA_FULL = 0, KA_FREE = KA_FULL + kKB, VA_FULL = KA_FREE + kKB, P_FULL = VA_FULL + kVB, PV_DONE = P_FULL + kVB, S_FULL = PV_DONE + kVB,
+         S_FREE = S_FULL + kSB, Q_FULL = S_FREE + kSB, DRAIN = Q_FULL + kQB, RING_FULL = DRAIN + 2, RING_FREE = RING_FULL + kStages };
+  static constexpr int kBars = RING_FREE + kStages;
   static_assert(kBars * 8 + 16 <= 512, "barriers");
   // tensor memory columns
-  static constexpr int kKA = 0, kVA = D, kS = kVA + kTile, kO = kS + 2 * R;
+  static constexpr int kKA = 0, kVA = kKA + kKB * D / 2, kS = kVA + kVB * kTile / 2, kO = kS + kSB * R;
   static_assert(kO + R * kSets <= 512, "tensor memory");
+};
+
+// Waits for a barrier's phase; the whole warp goes on together.  A wait that runs out, or sees that another one did, sets the abort word
+// and returns as if the phase had come: what the roles then read and multiply means nothing, but stays in bounds, and every wait of
+// theirs ends at once, so that they run out of tiles.  The phase has come at the first look, or while that look was suspended, in nearly
+// every wait.  The loop behind it is a function of its own: inlined at each wait it took 12 % of the time, in instruction fetches.
+__device__ __noinline__ void wait_longer(uint32_t bar, uint32_t parity, uint32_t abort_at) {
+  uint32_t since = 0;
+  for (uint32_t n = 1;; ++n) {
+    uint32_t gone;
+    asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(gone) : "r"(abort_at) : "memory");
+    if (gone || mbar_try_wait(bar, parity)) return;
+    if (n % kPolls) continue;
+    uint32_t now;
+    asm volatile("mov.u32 %0, %%clock;" : "=r"(now));
+    if (n == kPolls) since = now;
+    if (now - since >= kWaitClocks) break;
+  }
+  asm volatile("st.volatile.shared.u32 [%0], 1;" ::"r"(abort_at) : "memory");
+}
+__device__ __forceinline__ void wait_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
+  if (rare(!mbar_try_wait(bar, parity))) wait_longer(bar, parity, abort_at);
+  __syncwarp();
+}
+// which of N buffers, and the phase of its barriers
+template <int N>
+struct Turn {
+  int at = 0, phase = 0;
+  __device__ __forceinline__ void next(int n = 1) {
+    if ((at += n) >= N) {
+      at -= N;
+      phase ^= 1;
+    }
+  }
 };
 
 template <bool HALF>
@@ -150,6 +203,21 @@ __device__ __forceinline__ uint32_t splat_half(uint32_t h2, int hi) { return __b
 __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
+}
+// x = a * b + c, l += a: two at a time
+__device__ __forceinline__ void fma_pair(float& x0, float& x1, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, uint32_t c0, uint32_t c1) {
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(x0), "=f"(x1) : "r"(a0), "r"(a1), "r"(b0), "r"(b1), "r"(c0), "r"(c1));
+}
+__device__ __forceinline__ void add_pair(float& l0, float& l1, float a0, float a1) {
+  asm("{\n\t.reg .b64 a, l;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 l, {%0, %1};\n\tadd.rn.f32x2 l, l, a;\n\tmov.b64 {%0, %1}, l;\n\t}"
+      : "+f"(l0), "+f"(l1) : "f"(a0), "f"(a1));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 __device__ __forceinline__ float exp2_approx(float x) {
   float r;
@@ -203,27 +271,31 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
   const int units = p.cache.kv_heads * p.row_tiles;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < C::kKB; ++i) {
       mbar_init(bar(C::KA_FULL + i), 4);
       mbar_init(bar(C::KA_FREE + i), 1);
-      mbar_init(bar(C::VA_FULL + i), 8);
-      mbar_init(bar(C::S_FULL + i), 1);
-      mbar_init(bar(C::S_FREE + i), 4 * C::kColGroups);
+    }
+    for (int i = 0; i < C::kVB; ++i) {
+      mbar_init(bar(C::VA_FULL + i), 4);
       mbar_init(bar(C::P_FULL + i), 4 * C::kColGroups);
       mbar_init(bar(C::PV_DONE + i), 1);
-      mbar_init(bar(C::Q_FULL + i), 4);
-      mbar_init(bar(C::DRAIN + i), 1);
     }
+    for (int i = 0; i < C::kSB; ++i) {
+      mbar_init(bar(C::S_FULL + i), 1);
+      mbar_init(bar(C::S_FREE + i), 4 * C::kColGroups);
+    }
+    for (int i = 0; i < C::kQB; ++i) mbar_init(bar(C::Q_FULL + i), 4);
+    for (int i = 0; i < 2; ++i) mbar_init(bar(C::DRAIN + i), 1);
     for (int s = 0; s < C::kStages; ++s) {
-      mbar_init(bar(C::RING + s), 1);
-      mbar_init(bar(C::RING + C::kStages + s), 12);
+      mbar_init(bar(C::RING_FULL + s), 1);
+      mbar_init(bar(C::RING_FREE + s), 8);
     }
     *abort_word = 0;
     fence_barrier_init();
   }
   if (warp == C::kIssuerS) { tmem_alloc(tslot, 512); tmem_relinquish(); }
   if (C::kN < 16) {                                                 // probabilities of the rows that are none
-    for (int i = threadIdx.x; i < 2 * C::kP / 16; i += C::kThreads) *reinterpret_cast<uint4*>(sgen + C::kOffP + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = threadIdx.x; i < C::kVB * C::kP / 16; i += C::kThreads) *reinterpret_cast<uint4*>(sgen + C::kOffP + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
   }
   wait_prior_grids();
@@ -286,13 +358,13 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
   uint32_t* const valid_ring = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
   const int P = 1 << p.cache.log_page;
-  bool ok = true;
+  auto wait = [&](int b, int phase) { wait_phase(bar(b), (uint32_t)phase, abort_at); };
 
   if (warp == C::kProducer) {
     // ===================================================================== pages -> shared memory
     Walk w = w0;
     const int slots = kTile >> p.cache.log_page;                    // pages of a tile: 1 to 8
-    int s = 0, ph = 0;
+    Turn<C::kStages> ring;
     bool lost = false;
     auto page_of = [&](const Walk& at) {                            // of this lane, of the tile
       if (lane >= slots || at.first + lane * P >= at.len) return -1;
@@ -304,15 +376,16 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     if (n_tiles && (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len) lost = true;
     for (int i = 0; i < n_tiles; ++i) {
       const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
-      if (!(ok = mbar_wait(bar(C::RING + C::kStages + s), ph ^ 1, abort_at))) break;
+      wait(C::RING_FREE + ring.at, ring.phase ^ 1);
       if (lane == 0) {
         valid_ring[i % C::kRing] = held;
-        mbar_arrive_expect_tx(bar(C::RING + s), __popc(held) * p.cache.record);
+        mbar_arrive_expect_tx(bar(C::RING_FULL + ring.at), __popc(held) * p.cache.record);
       }
       __syncwarp();
       if (page >= 0)
-        bulk_load_1d(sbase + C::kOffStage + s * C::kStage + lane * p.cache.record, p.cache.rec(page, kvh), p.cache.record, bar(C::RING + s));
-      if (++s == C::kStages) { s = 0; ph ^= 1; }
+        bulk_load_1d(sbase + C::kOffStage + ring.at * C::kStage + lane * p.cache.record, p.cache.rec(page, kvh), p.cache.record,
+                     bar(C::RING_FULL + ring.at));
+      ring.next();
       if (rare(advance(w, p, units)) && i + 1 < n_tiles) {
         kvh = w.u / p.row_tiles;
         if ((long long)max(0, __ldg(p.context + w.b)) + p.T > w.len) lost = true;
@@ -320,9 +393,10 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
       if (i + 1 < n_tiles) page = page_of(w);                       // the table's entries come while this tile's stage is waited for
     }
     if (__any_sync(0xffffffffu, lost) && lane == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
-    if (!ok) {                                                      // given up: the copies in flight end before shared memory does
-      for (int k = 0; k < C::kStages; ++k)
-        for (int spin = 0; spin < (1 << 12) && !mbar_try_wait(bar(C::RING + k), k < s ? ph : ph ^ 1); ++spin) {}
+    // the last copies end before this warp does (also where the others have given up on them)
+    for (int k = 0; k < C::kStages && k < n_tiles; ++k) {
+      ring.at = ring.at ? ring.at - 1 : (ring.phase ^= 1, C::kStages - 1);
+      wait(C::RING_FULL + ring.at, ring.phase);
     }
   } else if (warp == C::kIssuerS) {
     // ===================================================================== S^T = K Q^T
@@ -330,70 +404,84 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     // and its issue waits for the one before: two warps issue, so that the waits of one lie under the products of the other.
     constexpr uint32_t kIdesc = make_idesc_f16(128, R, false);
     Walk w = w0;
-    int item = 0;
+    Turn<C::kKB> kb;
+    Turn<C::kSB> sb;
+    Turn<C::kQB> qb;
     bool fresh = true;
     for (int i = 0; i < n_tiles; ++i) {
-      const int buf = i & 1, ph = (i >> 1) & 1;
-      if (rare(fresh) && !(ok = mbar_wait(bar(C::Q_FULL + (item & 1)), (item >> 1) & 1, abort_at))) break;
-      if (!(ok = mbar_wait(bar(C::S_FREE + buf), ph ^ 1, abort_at))) break;
-      if (!(ok = mbar_wait(bar(C::KA_FULL + buf), ph, abort_at))) break;
+      if (rare(fresh)) wait(C::Q_FULL + qb.at, qb.phase);
+      wait(C::S_FREE + sb.at, sb.phase ^ 1);
+      wait(C::KA_FULL + kb.at, kb.phase);
       tc_fence_after();
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          tc_mma_f16_ta(tmem + C::kS + R * buf, tmem + C::kKA + (D / 2) * buf + 8 * k,
-                        make_smem_desc(sbase + C::kOffQ + (item & 1) * C::kQ + k * 256, 128, (D / 8) * 128, kSwzNone), kIdesc, k > 0);
-        tc_commit(bar(C::S_FULL + buf));
-        tc_commit(bar(C::KA_FREE + buf));
+          tc_mma_f16_ta(tmem + C::kS + R * sb.at, tmem + C::kKA + (D / 2) * kb.at + 8 * k,
+                        make_smem_desc(sbase + C::kOffQ + qb.at * C::kQ + k * 256, 128, (D / 8) * 128, kSwzNone), kIdesc, k > 0);
+        tc_commit(bar(C::S_FULL + sb.at));
+        tc_commit(bar(C::KA_FREE + kb.at));
       }
       __syncwarp();
+      kb.next();
+      sb.next();
       fresh = advance(w, p, units);
-      item += fresh;
+      if (rare(fresh)) qb.next();
     }
-    if (!ok && elect_one()) tc_commit(bar(C::DRAIN));
+    if (elect_one()) tc_commit(bar(C::DRAIN));
+    __syncwarp();
   } else if (warp == C::kIssuerO) {
     // ===================================================================== O^T += V^T P^T
     // P: rows are contiguous (MN-major), core matrices of 8 keys x 16 bytes (8 rows), those along rows neighbours
     constexpr uint32_t kIdesc = make_idesc_f16(128, R, true);
     Walk w = w0;
     int of_item = 0;                                                // tiles of the item so far
+    Turn<C::kVB> vb;
     for (int i = 0; i < n_tiles; ++i) {
-      const int buf = i & 1, ph = (i >> 1) & 1;
-      if (!(ok = mbar_wait(bar(C::VA_FULL + buf), ph, abort_at))) break;
-      if (!(ok = mbar_wait(bar(C::P_FULL + buf), ph, abort_at))) break;
+      wait(C::VA_FULL + vb.at, vb.phase);
+      wait(C::P_FULL + vb.at, vb.phase);
       tc_fence_after();
       const uint32_t more = of_item >= C::kSets;                    // not the first tile of the item that this O gets
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
-          tc_mma_f16_ta(tmem + C::kO + (C::kSets == 2 ? R * buf : 0), tmem + C::kVA + 64 * buf + 8 * k,
-                        make_smem_desc(sbase + C::kOffP + buf * C::kP + k * 2 * (R / 8) * 128, (R / 8) * 128, 128, kSwzNone), kIdesc,
+          tc_mma_f16_ta(tmem + C::kO + (C::kSets == 2 ? R * (i & 1) : 0), tmem + C::kVA + 64 * vb.at + 8 * k,
+                        make_smem_desc(sbase + C::kOffP + vb.at * C::kP + k * 2 * (R / 8) * 128, (R / 8) * 128, 128, kSwzNone), kIdesc,
                         k > 0 ? 1u : more);
-        tc_commit(bar(C::PV_DONE + buf));
+        tc_commit(bar(C::PV_DONE + vb.at));
       }
       __syncwarp();
+      vb.next();
       of_item = advance(w, p, units) ? 0 : of_item + 1;
     }
-    if (!ok && elect_one()) tc_commit(bar(C::DRAIN + 1));
-  } else if (warp < 4) {
+    if (elect_one()) tc_commit(bar(C::DRAIN + 1));
+    __syncwarp();
+  } else if (warp < C::kFirstV) {
     // ===================================================================== Q and K
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-    const int key = threadIdx.x, slot = key >> p.cache.log_page, t = key & (P - 1);
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const int group = warp >> 2, quarter = warp & 3;
+    const int key = quarter * 32 + lane, slot = key >> p.cache.log_page, t = key & (P - 1);
     const float c0 = p.scale * 1.4426950408889634f;
     Walk w = w0;
-    int s = 0, sph = 0, item = 0;
+    Turn<C::kStages> ring;
+    Turn<C::kKB> kb;
+    int item = 0;
     bool fresh = true;
-    for (int i = 0; i < n_tiles; ++i) {
-      const int buf = i & 1, ph = (i >> 1) & 1;
-      if (!(ok = mbar_wait(bar(C::KA_FREE + buf), ph ^ 1, abort_at))) break;
+    if (group && n_tiles > 0) {
+      item = advance_by(w, p, units, group, &fresh);
+      ring.next(group);
+      kb.next(group);
+    }
+    for (int i = group; i < n_tiles; i += C::kKGroups) {
+      wait(C::KA_FREE + kb.at, kb.phase ^ 1);
       if (rare(fresh)) {
         // Rows scaled by a power of two into f16's range (the largest element to [2^14, 2^15)): exact for 8-bit significands, and a row's
-        // scores are scaled back by its constant.  The buffer is free: tile i - 2 or an earlier one was the last that read it.
-        const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R;
+        // scores are scaled back by its constant.  The buffer is free: as many items back, the last tile that read it was tile i - kKB or
+        // an earlier one, whose product is done.
+        const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R, qb = item % C::kQB;
         const float c = __fdiv_rn(c0, __ldg(p.cache.k_G + kvh));
         constexpr int kParts = D / 16;                              // threads of a row
 #pragma unroll
-        for (int j = threadIdx.x; j < R * kParts; j += 128) {
+        for (int j = key; j < R * kParts; j += 128) {
           const int r = j / kParts, e = (j % kParts) * 16, row = row0 + r;
           float v[16];
 #pragma unroll
@@ -427,20 +515,20 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           uint32_t h[8];
 #pragma unroll
           for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(v[2 * x] * f, v[2 * x + 1] * f);
-          uint8_t* const dst = sgen + C::kOffQ + (item & 1) * C::kQ + ((r >> 3) * (D / 8) + (e >> 3)) * 128 + (r & 7) * 16;
+          uint8_t* const dst = sgen + C::kOffQ + qb * C::kQ + ((r >> 3) * (D / 8) + (e >> 3)) * 128 + (r & 7) * 16;
           *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
           *reinterpret_cast<uint4*>(dst + 128) = make_uint4(h[4], h[5], h[6], h[7]);
-          if (e == 0) reinterpret_cast<float*>(sgen + C::kOffC)[(item & 3) * R + r] = c * __uint_as_float((254u - up) << 23);
+          if (e == 0) reinterpret_cast<float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * R + r] = c * __uint_as_float((254u - up) << 23);
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::Q_FULL + (item & 1)));
+        if (lane == 0) mbar_arrive(bar(C::Q_FULL + qb));
       }
-      if (!(ok = mbar_wait(bar(C::RING + s), sph, abort_at))) break;
+      wait(C::RING_FULL + ring.at, ring.phase);
       {
         tc_fence_after();
-        const uint8_t* const rec = sgen + C::kOffStage + s * C::kStage + slot * p.cache.record;
-        const uint32_t dst = tmem + lanes + C::kKA + (D / 2) * buf;
+        const uint8_t* const rec = sgen + C::kOffStage + ring.at * C::kStage + slot * p.cache.record;
+        const uint32_t dst = tmem + lanes + C::kKA + (D / 2) * kb.at;
         // (rolled loops: what the four roles of a scheduler run in turn has to stay in its instruction cache)
         const uint8_t* codes = rec + t * 16;
         uint2 sw = make_uint2(0u, 0u);
@@ -475,68 +563,78 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           tmem_st_32x32b_x16(dst + 16 * c, h);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::RING + C::kStages + s));   // (the loads are done: their values have been used)
+        if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));   // (the loads are done: their values have been used)
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::KA_FULL + buf));
+        if (lane == 0) mbar_arrive(bar(C::KA_FULL + kb.at));
       }
-      if (++s == C::kStages) { s = 0; sph ^= 1; }
-      fresh = advance(w, p, units);
-      item += fresh;
+      ring.next(C::kKGroups);
+      kb.next(C::kKGroups);
+      item += advance_by(w, p, units, C::kKGroups, &fresh);
     }
   } else if (warp < C::kFirstSoftmax) {
     // ===================================================================== V
-    const int quarter = warp & 3, half = (warp - C::kFirstV) >> 2, e = quarter * 32 + lane;      // index of the head dimension
+    const int quarter = warp & 3, group = (warp - C::kFirstV) >> 2, e = quarter * 32 + lane;      // index of the head dimension
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    uint8_t* const scales = sgen + C::kOffVScale + (warp - C::kFirstV) * 256;
-    // this lane's codes of its 64 tokens in a stage: four chunks of sixteen tokens, inside a page or at the same place of the next
-    const int at0 = 64 * half, log_page = p.cache.log_page, record = p.cache.record;
-    const uint32_t codes0 = (uint32_t)((at0 >> log_page) * record + L::v_codes(P) + (at0 & (P - 1)) * L::kRow + (L::kFp4 ? e >> 1 : e) * 16);
-    const uint32_t step1 = P == 16 ? (uint32_t)record : 16 * L::kRow;
-    const uint32_t step2 = P <= 32 ? (uint32_t)((32 >> log_page) * record) : 32 * L::kRow;
-    const int at_sc = at0 + 4 * (lane & 15);
+    uint8_t* const scales = sgen + C::kOffVScale + (warp - C::kFirstV) * 512;
+    // this lane's codes in a stage: chunks of sixteen tokens, further in the page or at the same place of the next
+    const int log_page = p.cache.log_page, record = p.cache.record;
+    const uint32_t codes0 = (uint32_t)(L::v_codes(P) + (L::kFp4 ? e >> 1 : e) * 16);
+    const uint32_t step16 = P == 16 ? (uint32_t)record : 16 * L::kRow;
+    const uint32_t step32 = P <= 32 ? (uint32_t)((32 >> log_page) * record) : 32 * L::kRow;
+    const uint32_t step64 = P <= 64 ? (uint32_t)((64 >> log_page) * record) : 64 * L::kRow;
+    const int at_sc = 8 * (lane & 15);                              // eight tokens whose scales of block e / 16 this lane converts
     const uint32_t scale0 = (uint32_t)((at_sc >> log_page) * record + L::v_scales(P) + (e >> 4) * P + (at_sc & (P - 1)));
     Walk w = w0;
-    int s = 0, sph = 0, b_of = -1;
+    Turn<C::kStages> ring;
+    Turn<C::kVB> vb;
+    int b_of = -1;
     unsigned long long seen = 0;                                    // drafted tokens that some row sees
-    for (int i = 0; i < n_tiles; ++i, advance(w, p, units)) {
-      const int buf = i & 1, ph = (i >> 1) & 1;
+    bool fresh;
+    if (group && n_tiles > 0) {
+      advance_by(w, p, units, group, &fresh);
+      ring.next(group);
+      vb.next(group);
+    }
+    for (int i = group; i < n_tiles; i += C::kVGroups) {
       if (rare(w.b != b_of)) {
         b_of = w.b;
         const int n = drafted(p, w.b);
         seen = row_mask(p, w.b, lane, n) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n) : 0ull);
         seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
       }
-      if (!(ok = mbar_wait(bar(C::PV_DONE + buf), ph ^ 1, abort_at))) break;
-      if (!(ok = mbar_wait(bar(C::RING + s), sph, abort_at))) break;
+      wait(C::PV_DONE + vb.at, vb.phase ^ 1);
+      wait(C::RING_FULL + ring.at, ring.phase);
       {
         tc_fence_after();
         const uint32_t held = valid_ring[i % C::kRing];
         const int first = w.first;
         // what no row sees counts as zero: it may be any bytes, and a probability of 0 times a NaN would be one
         const bool all = first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
-        const uint8_t* const stage = sgen + C::kOffStage + s * C::kStage;
-        const uint32_t dst = tmem + lanes + C::kVA + 64 * buf + 32 * half, shift = 4 * (e & 1);
+        const uint8_t* const stage = sgen + C::kOffStage + ring.at * C::kStage;
+        const uint32_t dst = tmem + lanes + C::kVA + 64 * vb.at, shift = 4 * (e & 1);
         if (quarter * 32 < D) {
           if (L::kFp4) {
-            // the scales of this warp's two blocks and 64 tokens, once for all sixteen lanes that need them
-            uint32_t sc = *reinterpret_cast<const uint32_t*>(stage + scale0);
+            // the scales of this warp's two blocks, once for all sixteen lanes that need them
+            uint2 sc = *reinterpret_cast<const uint2*>(stage + scale0);
             if (rare(!all)) {
-              const uint32_t v = held >> (at_sc >> log_page) & 1 ? permute_eight(valid_eight(w, seen, first + (at_sc & ~7))) : 0u;
-              sc &= byte_mask(at_sc & 4 ? v >> 4 : v);
+              const uint32_t v = held >> (at_sc >> log_page) & 1 ? permute_eight(valid_eight(w, seen, first + at_sc)) : 0u;
+              sc.x &= byte_mask(v);
+              sc.y &= byte_mask(v >> 4);
             }
-            uint32_t f[2];
-            cvt_f16x2_e4m3x4(sc, f);
-            *reinterpret_cast<uint2*>(scales + lane * 8) = make_uint2(f[0], f[1]);
+            uint32_t f[4];
+            cvt_f16x2_e4m3x4(sc.x, f);
+            cvt_f16x2_e4m3x4(sc.y, f + 2);
+            *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(f[0], f[1], f[2], f[3]);
             __syncwarp();
           }
           const uint8_t* codes = stage + codes0;
-          const uint8_t* factors = scales + (lane >> 4) * 128;
+          const uint8_t* factors = scales + (lane >> 4) * 256;
 #pragma unroll 2
-          for (int j = 0; j < 64; j += 16) {                        // sixteen tokens
-            uint4 raw = *reinterpret_cast<const uint4*>(j & 16 ? codes + step1 : codes);
-            if (j & 16) codes += step2;
+          for (int j = 0; j < kTile; j += 16) {                     // sixteen tokens
+            uint4 raw = *reinterpret_cast<const uint4*>(j & 16 ? codes + step16 : codes);
+            if (j & 16) codes = j & 32 ? stage + codes0 + step64 : codes + step32;
             uint32_t h[8];
             if (L::kFp4) {
               const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -551,9 +649,9 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
               }
             } else {
               if (rare(!all)) {
-                const bool here = held >> ((at0 + j) >> log_page) & 1;
-                const uint32_t lo = here ? valid_eight(w, seen, first + at0 + j) : 0u;
-                const uint32_t hi = here ? valid_eight(w, seen, first + at0 + j + 8) : 0u;
+                const bool here = held >> (j >> log_page) & 1;
+                const uint32_t lo = here ? valid_eight(w, seen, first + j) : 0u;
+                const uint32_t hi = here ? valid_eight(w, seen, first + j + 8) : 0u;
                 raw.x &= byte_mask(lo); raw.y &= byte_mask(lo >> 4); raw.z &= byte_mask(hi); raw.w &= byte_mask(hi >> 4);
               }
               const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -564,13 +662,15 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::RING + C::kStages + s));
+        if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::VA_FULL + buf));
+        if (lane == 0) mbar_arrive(bar(C::VA_FULL + vb.at));
       }
-      if (++s == C::kStages) { s = 0; sph ^= 1; }
+      ring.next(C::kVGroups);
+      vb.next(C::kVGroups);
+      advance_by(w, p, units, C::kVGroups, &fresh);
     }
   } else {
     // ===================================================================== softmax
@@ -579,8 +679,9 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     const int quarter = warp & 3, key = quarter * 32 + lane;
     const int id = 1 + group, id_all = 5 + cols;                    // named barriers: this group's 128 threads; the sets of these rows
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    float2* const cm_all = reinterpret_cast<float2*>(sgen + C::kOffCM) + c0;                     // [kSets] R apart
-    float2* const cm = cm_all + set * R;
+    float* const ref_all = reinterpret_cast<float*>(sgen + C::kOffCM) + c0;                      // [kSets][2] R apart: kShift - reference
+    float* const ref = ref_all + set * 2 * R;
+    float* const con = ref + R;                                                                  // score constants
     unsigned long long* const bits = reinterpret_cast<unsigned long long*>(sgen + C::kOffBits) + set * R + c0;
     float* const warps_all = reinterpret_cast<float*>(sgen + C::kOffWarp) + c0;                  // [kSets][4] R apart
     float* const warps = warps_all + set * 4 * R;
@@ -591,11 +692,13 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     const uint32_t p_row = (uint32_t)((place >> 3) * (R / 8) * 128 + (c0 >> 3) * 128 + (place & 7) * 16);
     const uint32_t o_mine = tmem + lanes + C::kO + set * R + c0;
     Walk w = w0;
-    int item = 0, part_first = 0, last = 0;                         // part_first: first key of the item that this CTA takes
+    Turn<C::kSB> sb;
+    Turn<C::kVB> vb;
+    int item = 0, part_first = 0, last = 0, last_phase = 0;   // last: this set's last tile, its buffer of P
+    //                       // part_first: first key of the item that this CTA takes
     bool fresh = true, started = false;                             // of the item; has this set had a tile of it?
     float l[N];
     for (int i = 0; i < n_tiles; ++i) {
-      const int buf = i & 1, ph = (i >> 1) & 1;
       if (rare(fresh)) {
         part_first = w.first;
         if (key < N) {
@@ -606,14 +709,17 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         for (int r = 0; r < N; ++r) l[r] = 0.f;
         fresh = started = false;
       }
-      if (C::kSets == 1 || buf == set) {
-        if (ok) ok = mbar_wait(bar(C::S_FULL + buf), ph, abort_at);
+      if (C::kSets == 1 || (i & 1) == set) {
+        wait(C::S_FULL + sb.at, sb.phase);
         if (rare(!started)) {                                       // (Q's constants were there before its products were issued)
-          if (key < N) cm[key] = make_float2(reinterpret_cast<const float*>(sgen + C::kOffC)[(item & 3) * R + c0 + key], INFINITY);
+          if (key < N) {
+            con[key] = reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * R + c0 + key];
+            ref[key] = INFINITY;
+          }
           bar_sync(id, 128);
         }
         tc_fence_after();
-        const uint32_t scores = tmem + lanes + C::kS + R * buf + c0;
+        const uint32_t scores = tmem + lanes + C::kS + R * sb.at + c0;
         uint32_t raw[N];
         tmem_ld_cols(scores, raw);
         tmem_wait_ld();
@@ -635,10 +741,12 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         }
         auto relative = [&](bool references) {
 #pragma unroll
-          for (int r = 0; r < N; r += 2) {
-            const float4 k = *reinterpret_cast<const float4*>(cm + r);
-            x[r] = fmaf(__uint_as_float(raw[r]), k.x, references ? k.y : 0.f);
-            x[r + 1] = fmaf(__uint_as_float(raw[r + 1]), k.z, references ? k.w : 0.f);
+          for (int r = 0; r < N; r += 4) {
+            const uint4 c = *reinterpret_cast<const uint4*>(con + r);
+            uint4 k = *reinterpret_cast<const uint4*>(ref + r);
+            if (!references) k = make_uint4(0u, 0u, 0u, 0u);
+            fma_pair(x[r], x[r + 1], raw[r], raw[r + 1], c.x, c.y, k.x, k.y);
+            fma_pair(x[r + 2], x[r + 3], raw[r + 2], raw[r + 3], c.z, c.w, k.z, k.w);
           }
           if (rare(!plain)) {
 #pragma unroll
@@ -648,7 +756,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         };
         relative(true);
 #pragma unroll
-        for (int r = 0; r < N; ++r) top = fmaxf(top, x[r]);
+        for (int r = 0; r < N; r += 2) top = max3(top, x[r], x[r + 1]);
         if (rare(bar_any(id, 128, !started || top > kLag + kShift))) {
           // the references move: to the largest score seen so far (the scores are read again: kept, they would cost as many registers)
           tmem_ld_cols(scores, raw);
@@ -661,10 +769,10 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           }
           bar_sync(id, 128);
           if (key < N) {
-            const float old = kShift - cm[key].y;                   // -infinity: none yet
+            const float old = kShift - ref[key];                   // -infinity: none yet
             const float m = fmaxf(fmaxf(fmaxf(warps[key], warps[R + key]), fmaxf(warps[2 * R + key], warps[3 * R + key])), old);
             factor[key] = m == -INFINITY ? 1.f : exp2_approx(old - m);
-            cm[key].y = kShift - m;
+            ref[key] = kShift - m;
           }
           bar_sync(id, 128);
           tmem_ld_cols(scores, raw);
@@ -673,7 +781,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
 #pragma unroll
           for (int r = 0; r < N; ++r) l[r] *= factor[r];
           if (started) {                                            // O of this set's tiles before
-            if (ok) ok = mbar_wait(bar(C::PV_DONE + (last & 1)), (last >> 1) & 1, abort_at);
+            wait(C::PV_DONE + last, last_phase);
             tc_fence_after();
             uint32_t o[N];
             tmem_ld_cols(o_mine, o);
@@ -687,35 +795,37 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         }
         tc_fence_before();
         __syncwarp();
-        if (ok && lane == 0) mbar_arrive(bar(C::S_FREE + buf));
-        if (ok) ok = mbar_wait(bar(C::PV_DONE + buf), ph ^ 1, abort_at);   // P of tile i - 2 has been read
-        uint8_t* const dst = sgen + C::kOffP + buf * C::kP + p_row;
+        if (lane == 0) mbar_arrive(bar(C::S_FREE + sb.at));
+        wait(C::PV_DONE + vb.at, vb.phase ^ 1);                     // what stood in this P has been read
+        uint8_t* const dst = sgen + C::kOffP + vb.at * C::kP + p_row;
 #pragma unroll
         for (int r = 0; r < N; r += 8) {
           uint32_t h[4];
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const float a = exp2_approx(x[r + 2 * y]), b = exp2_approx(x[r + 2 * y + 1]);
-            l[r + 2 * y] += a;
-            l[r + 2 * y + 1] += b;
+            add_pair(l[r + 2 * y], l[r + 2 * y + 1], a, b);
             h[y] = pack_pair<__half>(a, b);
           }
           *reinterpret_cast<uint4*>(dst + (r >> 3) * 128) = make_uint4(h[0], h[1], h[2], h[3]);
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (ok && lane == 0) mbar_arrive(bar(C::P_FULL + buf));
+        if (lane == 0) mbar_arrive(bar(C::P_FULL + vb.at));
         started = true;
-        last = i;
+        last = vb.at;
+        last_phase = vb.phase;
       }
+      sb.next();
+      vb.next();
       if (rare(w.left == 1 || i + 1 == n_tiles)) {
         // ---- end of the item, or of this CTA's part of it: the sets of these rows together
         const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R + c0;
         const bool whole = part_first == 0 && w.left == 1;
         const float sum = warp_sums(l, lane);
         if (lane < N) warps[quarter * R + lane] = sum;
-        if (!started && key < N) cm[key].y = INFINITY;
-        if (ok && started) ok = mbar_wait(bar(C::PV_DONE + (last & 1)), (last >> 1) & 1, abort_at);
+        if (!started && key < N) ref[key] = INFINITY;
+        if (started) wait(C::PV_DONE + last, last_phase);
         bar_sync(id_all, 128 * C::kSets);
         const int n = drafted(p, w.b);
         const long long out0 = ((long long)w.b * p.H + (long long)kvh * p.group) * p.T;
@@ -726,7 +836,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           for (int k = 0; k < C::kSets; ++k) {
             const float* const wk = warps_all + k * 4 * R + key;
             part[k] = wk[0] + wk[R] + wk[2 * R] + wk[3 * R];
-            m[k] = kShift - cm_all[k * R + key].y;
+            m[k] = kShift - ref_all[k * 2 * R + key];
             top = fmaxf(top, m[k]);
           }
 #pragma unroll
@@ -739,15 +849,15 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           float inv = 1.f;
           if (whole) {
             inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + kvh));     // nothing seen: 0, not 0 / 0
-            if (ok && p.lse && row < p.rows && row % p.T < n)
+            if (p.lse && row < p.rows && row % p.T < n)
               p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (top - kShift + log2f(total_l)) * 0.6931471805599453f;
-          } else if (ok) {
+          } else {
             p.part_ml[(size_t)slot * R + c0 + key] = make_float2(top, total_l);
           }
 #pragma unroll
           for (int k = 0; k < C::kSets; ++k) factor_all[k * R + key] = f[k] * inv;
         }
-        if (group == 0 && key == 0 && part_first == 0 && ok)
+        if (group == 0 && key == 0 && part_first == 0)
           p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find[2] + i + w.left - 1));
         bar_sync(id_all, 128 * C::kSets);
         tc_fence_after();
@@ -774,7 +884,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         tc_fence_before();
         if (C::kSets > 1) bar_sync(id_all, 128 * C::kSets);         // the next item's products may overwrite either O
         const uint32_t keep = __ballot_sync(0xffffffffu, lane < M && row0 + r0 + lane < p.rows && (row0 + r0 + lane) % p.T < n);
-        if (ok && key < D) {
+        if (key < D) {
           if (whole) {
             uint16_t* const dst = static_cast<uint16_t*>(p.out) + (size_t)(out0 + row0 + r0) * D + key;
 #pragma unroll
