@@ -37,7 +37,7 @@ namespace {
 using namespace ptx;
 
 constexpr int kTile = 128;                 // keys of a tile
-constexpr int kMostCtas = 160;             // partial results: two per CTA
+constexpr int kMostCtas = 320;             // partial results: two per CTA
 constexpr float kLag = 8.f;                // octaves by which a score may exceed its row's reference
 constexpr float kShift = 7.f;              // a probability of 1 is 2^7: with the lag just inside f16, whose subnormals then begin at 2^-21
 
@@ -224,6 +224,10 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// Biased exponent of the factor of a row of Q whose largest magnitude is a: 2^(14 - exponent of a), at most 2^100 (rows below 2^-86 lose
+// bits of scores that are nothing beside any others)
+__device__ __forceinline__ uint32_t row_exponent(float a) { return a == 0.f ? 127u : min(268u - (__float_as_uint(a) >> 23), 227u); }
+
 // sum over the warp of each of N values: lane i ends with the total of value i % N
 template <int N>
 __device__ __forceinline__ float warp_sums(float (&v)[N], int lane) {
@@ -256,6 +260,98 @@ __device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long lon
   if (in > 0 && in < 8) v |= (1u << in) - 1;
   return left >= 8 ? v : left > 0 ? v & ((1u << left) - 1) : 0u;
 }
+
+// This CTA's run of tiles: how many, and where it starts.  find: entry and place of the first tile, its number in the list, all tiles,
+// CTAs.  Two barriers of the block; everything that the block wrote to shared memory before is visible after it.
+template <int THREADS>
+__device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0, long long* scan, long long* find) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int per = (p.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, b1 = min(p.B, b0 + per);
+  long long mine = 0;
+  Walk w;
+#pragma unroll 1
+  for (w.b = b0; w.b < b1; ++w.b) mine += (long long)load_entry(w, p) * units;
+  long long incl = mine;
+#pragma unroll 1
+  for (int s = 1; s < 32; s <<= 1) {
+    const long long o = __shfl_up_sync(0xffffffffu, incl, s);
+    if (lane >= s) incl += o;
+  }
+  if (lane == 31) scan[warp] = incl;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll 1
+  for (int i = 0; i < THREADS / 32; ++i) {
+    if (i < warp) before += scan[i];
+    total += scan[i];
+  }
+  before += incl - mine;
+  const long long ctas = min((long long)gridDim.x, total);
+  const long long t0 = blockIdx.x < ctas ? blockIdx.x * total / ctas : total, t1 = blockIdx.x < ctas ? (blockIdx.x + 1) * total / ctas : total;
+  if (t0 < t1 && before <= t0 && t0 < before + mine) {              // one thread
+    for (w.b = b0;; ++w.b) {
+      const long long here = (long long)load_entry(w, p) * units;
+      if (t0 < before + here) break;
+      before += here;
+    }
+    find[0] = w.b;
+    find[1] = t0 - before;
+  }
+  if (threadIdx.x == 0) {
+    find[2] = t0;
+    find[3] = total;
+    find[4] = ctas;
+  }
+  __syncthreads();
+  w0.b = t0 < t1 ? (int)find[0] : 0;
+  const int nt = load_entry(w0, p);
+  const long long r = t0 < t1 ? find[1] : 0;
+  w0.u = (int)(r / nt);
+  const int kt = (int)(r - (long long)w0.u * nt);
+  w0.first = kt * kTile;
+  w0.left = nt - kt;
+  return (int)min(t1 - t0, (long long)INT_MAX);
+}
+
+// Brings the pages of tiles into a ring of stages, one bulk copy each; a whole warp.  RING: tiles for which `valid` remembers which of their
+// pages exist.
+template <int STAGES, int STAGE, int RING>
+struct Pages {
+  Walk w;
+  Turn<STAGES> ring;
+  int i = 0;                                                        // tile
+  bool lost = false;
+  __device__ __forceinline__ void bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
+    const int lane = threadIdx.x & 31, P = 1 << p.cache.log_page, slots = kTile >> p.cache.log_page;       // pages of a tile: 1 to 8
+    int page = -1;
+    if (lane < slots && w.first + lane * P < w.len) {
+      page = p.cache.page_of(w.b, w.first + lane * P);
+      lost |= page < 0;
+    }
+    const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
+    wait_phase(free + 8 * ring.at, ring.phase ^ 1, abort_at);
+    if (lane == 0) {
+      valid[i % RING] = held;
+      mbar_arrive_expect_tx(full + 8 * ring.at, __popc(held) * p.cache.record);
+    }
+    __syncwarp();
+    if (page >= 0)
+      bulk_load_1d(stages + ring.at * STAGE + lane * p.cache.record, p.cache.rec(page, w.u / p.row_tiles), p.cache.record, full + 8 * ring.at);
+  }
+  __device__ __forceinline__ void skip(const TreeParams& p, int units, int n) {
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+      advance(w, p, units);
+      ring.next();
+    }
+    i += n;
+  }
+  // does the table have room for the entry's tokens?
+  __device__ __forceinline__ void look(const TreeParams& p) { lost |= w.b < p.B && (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len; }
+  __device__ __forceinline__ void tell(const TreeParams& p) const {
+    if (__any_sync(0xffffffffu, lost) && (threadIdx.x & 31) == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
+  }
+};
 
 template <int FMT, int D, int R, int N_>
 __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kernel(const TreeParams p) {
@@ -298,62 +394,12 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     for (int i = threadIdx.x; i < C::kVB * C::kP / 16; i += C::kThreads) *reinterpret_cast<uint4*>(sgen + C::kOffP + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
   }
+  tc_fence_before();
   wait_prior_grids();
-
-  // ---- this CTA's run of tiles
   Walk w0;
-  int n_tiles;
-  long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);   // entry and place of the first tile; its number; all tiles; CTAs
-  {
-    long long t0, t1, total;
-    const int per = (p.B + C::kThreads - 1) / C::kThreads, b0 = threadIdx.x * per, b1 = min(p.B, b0 + per);
-    long long mine = 0;
-    Walk w;
-    for (w.b = b0; w.b < b1; ++w.b) mine += (long long)load_entry(w, p) * units;
-    long long incl = mine;
-    for (int s = 1; s < 32; s <<= 1) {
-      const long long o = __shfl_up_sync(0xffffffffu, incl, s);
-      if (lane >= s) incl += o;
-    }
-    long long* const scan = reinterpret_cast<long long*>(sgen + C::kOffScan);
-    if (lane == 31) scan[warp] = incl;
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    long long before = 0;
-    total = 0;
-    for (int i = 0; i < C::kThreads / 32; ++i) {
-      if (i < warp) before += scan[i];
-      total += scan[i];
-    }
-    before += incl - mine;
-    const long long ctas = min((long long)gridDim.x, total);
-    t0 = blockIdx.x < ctas ? blockIdx.x * total / ctas : total;
-    t1 = blockIdx.x < ctas ? (blockIdx.x + 1) * total / ctas : total;
-    if (t0 < t1 && before <= t0 && t0 < before + mine) {            // one thread
-      for (w.b = b0;; ++w.b) {
-        const long long here = (long long)load_entry(w, p) * units;
-        if (t0 < before + here) break;
-        before += here;
-      }
-      find[0] = w.b;
-      find[1] = t0 - before;
-    }
-    if (threadIdx.x == 0) {
-      find[2] = t0;
-      find[3] = total;
-      find[4] = ctas;
-    }
-    n_tiles = (int)min(t1 - t0, (long long)INT_MAX);
-    __syncthreads();
-    w0.b = t0 < t1 ? (int)find[0] : 0;
-    const int nt = load_entry(w0, p);
-    const long long r = t0 < t1 ? find[1] : 0;
-    w0.u = (int)(r / nt);
-    const int kt = (int)(r - (long long)w0.u * nt);
-    w0.first = kt * kTile;
-    w0.left = nt - kt;
-  }
+  long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
+  const int n_tiles = find_run<C::kThreads>(p, units, w0, reinterpret_cast<long long*>(sgen + C::kOffScan), find);
+  tc_fence_after();
   auto cta_of = [&](long long tile) { return (int)(((tile + 1) * find[4] - 1) / find[3]); };
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
   uint32_t* const valid_ring = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
@@ -362,41 +408,18 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
 
   if (warp == C::kProducer) {
     // ===================================================================== pages -> shared memory
-    Walk w = w0;
-    const int slots = kTile >> p.cache.log_page;                    // pages of a tile: 1 to 8
-    Turn<C::kStages> ring;
-    bool lost = false;
-    auto page_of = [&](const Walk& at) {                            // of this lane, of the tile
-      if (lane >= slots || at.first + lane * P >= at.len) return -1;
-      const int page = p.cache.page_of(at.b, at.first + lane * P);
-      lost |= page < 0;
-      return page;
-    };
-    int page = n_tiles ? page_of(w) : -1, kvh = w.u / p.row_tiles;
-    if (n_tiles && (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len) lost = true;
-    for (int i = 0; i < n_tiles; ++i) {
-      const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
-      wait(C::RING_FREE + ring.at, ring.phase ^ 1);
-      if (lane == 0) {
-        valid_ring[i % C::kRing] = held;
-        mbar_arrive_expect_tx(bar(C::RING_FULL + ring.at), __popc(held) * p.cache.record);
-      }
-      __syncwarp();
-      if (page >= 0)
-        bulk_load_1d(sbase + C::kOffStage + ring.at * C::kStage + lane * p.cache.record, p.cache.rec(page, kvh), p.cache.record,
-                     bar(C::RING_FULL + ring.at));
-      ring.next();
-      if (rare(advance(w, p, units)) && i + 1 < n_tiles) {
-        kvh = w.u / p.row_tiles;
-        if ((long long)max(0, __ldg(p.context + w.b)) + p.T > w.len) lost = true;
-      }
-      if (i + 1 < n_tiles) page = page_of(w);                       // the table's entries come while this tile's stage is waited for
+    Pages<C::kStages, C::kStage, C::kRing> pages;
+    pages.w = w0;
+    while (pages.i < n_tiles) {
+      if (rare(pages.i == 0 || pages.w.first == 0)) pages.look(p);
+      pages.bring(p, sbase + C::kOffStage, bar(C::RING_FULL), bar(C::RING_FREE), abort_at, valid_ring);
+      pages.skip(p, units, 1);
     }
-    if (__any_sync(0xffffffffu, lost) && lane == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
+    pages.tell(p);
     // the last copies end before this warp does (also where the others have given up on them)
     for (int k = 0; k < C::kStages && k < n_tiles; ++k) {
-      ring.at = ring.at ? ring.at - 1 : (ring.phase ^= 1, C::kStages - 1);
-      wait(C::RING_FULL + ring.at, ring.phase);
+      pages.ring.at = pages.ring.at ? pages.ring.at - 1 : (pages.ring.phase ^= 1, C::kStages - 1);
+      wait(C::RING_FULL + pages.ring.at, pages.ring.phase);
     }
   } else if (warp == C::kIssuerS) {
     // ===================================================================== S^T = K Q^T
@@ -509,8 +532,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           for (int x = 0; x < 16; ++x) a = fmaxf(a, fabsf(v[x]));
 #pragma unroll
           for (int x = 1; x < kParts; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
-          // 2^(14 - exponent), at most 2^100: rows below 2^-86 lose bits of scores that are nothing beside the others
-          const uint32_t up = a == 0.f ? 127u : min(268u - (__float_as_uint(a) >> 23), 227u);
+          const uint32_t up = row_exponent(a);
           const float f = __uint_as_float(up << 23);
           uint32_t h[8];
 #pragma unroll
@@ -918,6 +940,400 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
   }
 }
 
+// ---------------------------------------------------------------- sixteen rows or fewer: a warp by itself
+// What bounds few rows is the reading; the kernel above spends more instructions per tile on handing it from role to role than on its keys
+// (4100 a tile of 128 keys, d = 128, half of them hand-overs; 32 sequences of up to 32768 tokens, 4 rows: 200 us, whose reading takes 94).  Here nothing
+// is handed over: a warp takes 16 keys of every tile from their codes to its own maximum, sum and O, all in registers, and the warps of
+// a CTA meet at the end of an item.
+//
+// The operands of the 16 x 8 x 16 products stay where they are loaded, because the orders of keys and of d are free:
+//   S^T = K Q^T   A: keys x d.  Lane (r, c) = (lane / 4, lane % 4) has keys r and r + 8: it takes D / 4 elements of either from d = c D / 4 on, in
+//                 one piece; step j of the product over d is elements 4j .. 4j + 3 of each lane's piece.  Row r stands for token 4 (r / 2) + r % 2 of the
+//                 sixteen, row r + 8 for the token two further.
+//   O^T += V^T P^T  A: d x keys.  Lane (r, c) has tokens 4c .. 4c + 3, a word of a chunk of V; rows r and r + 8 of product t are elements 16t + 2r
+//                 and 16t + 2r + 1, the two nibbles of a byte (sixteen elements are one block of scales).
+//                 B: P^T, which S^T leaves as keys x rows: two 8 x 8 transposes.
+template <int FMT, int D, int NT>
+struct WarpCfg {
+  using L = RecordLayout<FMT, D>;
+  static constexpr int kWarps = 8, kThreads = 32 * kWarps;
+  static constexpr int R = 8 * NT;
+  static constexpr int kStage = kTile * 2 * L::kToken;
+  static constexpr int kStages = kStage > 18432 ? 2 : kStage > 16384 ? 4 : kStage > 9216 ? 4 : 6;
+  static constexpr int kRow = D + 4;                               // floats of a row of O in shared memory
+  static constexpr int kOffO = kStages * kStage;                   // float [8 warps][8 rows][kRow]
+  static constexpr int kOffML = kOffO + kWarps * 8 * kRow * 4;     // float2 [8 warps][8 rows]
+  static constexpr int kOffScale = kOffML + kWarps * 8 * 8;        // f16 [8 warps][D / 16][16 tokens]
+  static constexpr int kOffValid = kOffScale + kWarps * (D / 16) * 32;
+  static constexpr int kOffScan = kOffValid + 4 * 8;
+  static constexpr int kOffFind = kOffScan + 128;
+  static constexpr int kOffBar = kOffFind + 64;
+  static constexpr int kSmem = kOffBar + 2 * 8 * kStages + 16 + 128;
+  static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs an SM");
+};
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
+template <int FMT, int D, int NT>
+__global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, 2) tree_warp_kernel(const TreeParams p) {
+  using C = WarpCfg<FMT, D, NT>;
+  using L = typename C::L;
+  constexpr int R = C::R, kSteps = D / 16;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (smem_u32(smem_raw) + 127u) & ~127u;
+  uint8_t* const sgen = smem_raw + (sbase - smem_u32(smem_raw));
+  const uint32_t full = sbase + C::kOffBar, free = full + 8 * C::kStages, abort_at = free + 8 * C::kStages;
+  volatile uint32_t* const abort_word = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 16 * C::kStages);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int units = p.cache.kv_heads;                              // one row tile
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(free + 8 * s, C::kWarps);
+    }
+    *abort_word = 0;
+    fence_barrier_init();
+  }
+  wait_prior_grids();
+  Walk w0;
+  long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
+  const int n_tiles = find_run<C::kThreads>(p, units, w0, reinterpret_cast<long long*>(sgen + C::kOffScan), find);
+  uint32_t* const valid = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
+  const int P = 1 << p.cache.log_page;
+
+  // The pages of the first tiles; then the warps take turns, each bringing those of the tile that follows the ones on their way
+  Pages<C::kStages, C::kStage, C::kStages> pages;
+  pages.w = w0;
+  constexpr int kAhead = C::kStages - 1;
+  if (warp == 0 && n_tiles > 0) {
+    pages.look(p);
+    while (pages.i < kAhead && pages.i < n_tiles) {
+      pages.bring(p, sbase, full, free, abort_at, valid);
+      pages.skip(p, units, 1);
+    }
+  } else {
+    pages.skip(p, units, kAhead + warp);
+  }
+  {
+    const int r = lane >> 2, c = lane & 3;
+    // places in a stage: this warp's sixteen tokens, and what the lane takes of them
+    const int tok0 = 16 * warp, slot = tok0 >> p.cache.log_page, t_page = tok0 & (P - 1);
+    const int tok_a = 4 * (r >> 1) + (r & 1);                       // token of row r; row r + 8: two further
+    constexpr int kPiece = L::kRow / 4;                             // code bytes of a lane's piece of a key: 8, 16 or 32
+    const uint32_t rec0 = (uint32_t)(slot * p.cache.record);
+    const uint32_t k_at = rec0 + (uint32_t)((c * kPiece / 16 * P + t_page + tok_a) * 16 + c * kPiece % 16);
+    const uint32_t ks_at = rec0 + (uint32_t)(L::k_scales(P) + (t_page + tok_a) * L::kScales + c * (D / 64));
+    const uint32_t v_at = rec0 + (uint32_t)(L::v_codes(P) + t_page * L::kRow + (L::kFp4 ? r : 2 * r) * 16 + 4 * c);
+    uint8_t* const scales = sgen + C::kOffScale + warp * (D / 16) * 32;
+    // scales of V that this lane converts: four tokens (as they lie) of block lane / 4
+    const uint32_t vs_at = rec0 + (uint32_t)(L::v_scales(P) + (lane >> 2) * P + t_page + 4 * c);
+    const int sc_eight = 8 * (c >> 1), sc_first = 2 * (c & 1);      // they are tokens sc_eight + sc_first + {0, 4, 1, 5}
+    float* const o_smem = reinterpret_cast<float*>(sgen + C::kOffO);
+    float2* const ml_smem = reinterpret_cast<float2*>(sgen + C::kOffML);
+
+    Walk w = w0;
+    Turn<C::kStages> ring;
+    bool fresh = true;
+    int part_first = 0, b_of = -1, n_drafted = 0;
+    unsigned long long seen = 0;
+    uint32_t qf[NT][kSteps][2];                                     // Q^T: rows 8n + lane / 4
+    float con[NT][2], ref[NT][2], l[NT][2];                         // of rows 8n + 2c, + 1: score constant, kShift minus the reference, sum
+    float o[kSteps][NT][4];
+#pragma unroll 1
+    for (int i = 0; i < n_tiles; ++i) {
+      if (rare(fresh)) {
+        fresh = false;
+        part_first = w.first;
+        if (w.b != b_of) {
+          b_of = w.b;
+          n_drafted = drafted(p, w.b);
+          seen = row_mask(p, w.b, lane, n_drafted) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n_drafted) : 0ull);
+          seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
+        }
+        const float c0 = __fdiv_rn(p.scale * 1.4426950408889634f, __ldg(p.cache.k_G + w.u));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          // Q scaled by a power of two per row, as above
+          const int row = 8 * n + r;
+          float v[D / 4];
+          if (row < p.rows) {
+            const int hl = row / p.T, tok = row - hl * p.T;
+            const uint16_t* q = static_cast<const uint16_t*>(p.q) + w.b * p.q_sb + (long long)(w.u * p.group + hl) * p.q_sh + tok * p.q_sn + c * (D / 4);
+#pragma unroll
+            for (int x = 0; x < D / 4; x += 8) {
+              uint32_t raw[4];
+              if (p.q_vector) {
+                *reinterpret_cast<uint4*>(raw) = __ldg(reinterpret_cast<const uint4*>(q + x));
+              } else {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) raw[y] = (uint32_t)__ldg(q + x + 2 * y) | (uint32_t)__ldg(q + x + 2 * y + 1) << 16;
+              }
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                const float2 f = p.half ? unpack16<true>(raw[y]) : unpack16<false>(raw[y]);
+                v[x + 2 * y] = f.x;
+                v[x + 2 * y + 1] = f.y;
+              }
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < D / 4; ++x) v[x] = 0.f;
+          }
+          float a = 0.f;
+#pragma unroll
+          for (int x = 0; x < D / 4; ++x) a = fmaxf(a, fabsf(v[x]));
+          a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+          a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+          const uint32_t up = row_exponent(a);
+          const float f = __uint_as_float(up << 23), mine = c0 * __uint_as_float((254u - up) << 23);
+#pragma unroll
+          for (int x = 0; x < kSteps; ++x) {
+            qf[n][x][0] = pack_pair<__half>(v[4 * x] * f, v[4 * x + 1] * f);
+            qf[n][x][1] = pack_pair<__half>(v[4 * x + 2] * f, v[4 * x + 3] * f);
+          }
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            con[n][y] = __shfl_sync(0xffffffffu, mine, (2 * c + y) * 4);
+            ref[n][y] = INFINITY;
+            l[n][y] = 0.f;
+          }
+#pragma unroll
+          for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) o[x][n][y] = 0.f;
+        }
+      }
+      wait_phase(full + 8 * ring.at, ring.phase, abort_at);
+      const uint8_t* const stage = sgen + ring.at * C::kStage;
+      const uint32_t held = valid[ring.at];
+      const bool plain = w.first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
+      const bool here = held >> slot & 1;
+      // ---- scales of V: f16, by block and token
+      if (L::kFp4 && lane < D / 4) {
+        uint32_t sc = *reinterpret_cast<const uint32_t*>(stage + vs_at);
+        if (rare(!plain)) {
+          const uint32_t v = here ? permute_eight(valid_eight(w, seen, w.first + tok0 + sc_eight)) : 0u;
+          sc &= byte_mask(c & 1 ? v >> 4 : v);
+        }
+        uint32_t f[2];
+        cvt_f16x2_e4m3x4(sc, f);                                    // tokens (x, x + 4), (x + 1, x + 5): kept as (x, x + 1), (x + 4, x + 5)
+        uint8_t* const to = scales + (lane >> 2) * 32 + (sc_eight + sc_first) * 2;
+        *reinterpret_cast<uint32_t*>(to) = __byte_perm(f[0], f[1], 0x5410);
+        *reinterpret_cast<uint32_t*>(to + 8) = __byte_perm(f[0], f[1], 0x7632);
+      }
+      // ---- scores
+      float s[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) s[n][y] = 0.f;
+      {
+        uint32_t h[2][2 * kSteps];                                  // f16 pairs of the two keys
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint8_t* const at = stage + k_at + 32 * k;
+          if (L::kFp4) {
+            uint32_t words[D / 32], f[2];
+            if (D == 128) *reinterpret_cast<uint4*>(words) = *reinterpret_cast<const uint4*>(at);
+            else *reinterpret_cast<uint2*>(words) = *reinterpret_cast<const uint2*>(at);
+            const uint8_t* const sat = stage + ks_at + 2 * L::kScales * k;
+            const uint32_t two = cvt_f16x2_e4m3x2(D == 128 ? *reinterpret_cast<const uint16_t*>(sat) : *sat);
+            f[0] = splat_half(two, 0);
+            f[1] = splat_half(two, 1);
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x) {
+              cvt_f16x2_e2m1x8(words[x], h[k] + 4 * x);
+#pragma unroll
+              for (int y = 0; y < 4; ++y) h[k][4 * x + y] = mul_half2(h[k][4 * x + y], f[D == 128 ? x >> 1 : 0]);
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < D / 64; ++x) {
+              const uint4 raw = *reinterpret_cast<const uint4*>(at + x * P * 16);
+              const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+              for (int y = 0; y < 4; ++y) cvt_f16x2_e4m3x4(words[y], h[k] + 8 * x + 2 * y);
+            }
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_16x8x16(s[n], h[0][2 * x], h[1][2 * x], h[0][2 * x + 1], h[1][2 * x + 1], qf[n][x][0], qf[n][x][1]);
+      }
+      // ---- probabilities: octaves above the rows' references (+ kShift); what is not seen goes to -infinity
+      float x[NT][4], top = -INFINITY;
+      uint32_t hidden = 0;                                          // bit 4n + y: s[n][y] is not seen
+      if (rare(!plain)) {
+#pragma unroll 1
+        for (int y = 0; y < 4; ++y) {
+          const int pos = w.first + tok0 + tok_a + 2 * (y >> 1);
+#pragma unroll 1
+          for (int n = 0; n < NT; ++n) {
+            const int row = 8 * n + 2 * c + (y & 1);
+            bool vis = here && pos < w.len;
+            if (pos >= w.ctx) vis = vis && row < p.rows && (row_mask(p, w.b, row % p.T, n_drafted) >> ((pos - w.ctx) & 63) & 1);
+            hidden |= (vis ? 0u : 1u) << (4 * n + y);
+          }
+        }
+      }
+      auto relative = [&] {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            x[n][y] = fmaf(s[n][y], con[n][y & 1], ref[n][y & 1]);
+            if (hidden >> (4 * n + y) & 1) x[n][y] = -INFINITY;
+          }
+      };
+      relative();
+#pragma unroll
+      for (int n = 0; n < NT; ++n) top = max3(max3(top, x[n][0], x[n][1]), x[n][2], x[n][3]);
+      if (rare(__any_sync(0xffffffffu, top > kLag + kShift))) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float m = -INFINITY;                                    // the largest seen; max leaves NaN out
+            if (!(hidden >> (4 * n + y) & 1)) m = fmaxf(m, s[n][y] * con[n][y]);
+            if (!(hidden >> (4 * n + y + 2) & 1)) m = fmaxf(m, s[n][y + 2] * con[n][y]);
+            for (int z = 4; z < 32; z <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, z));
+            const float old = kShift - ref[n][y];                   // -infinity: none yet
+            m = fmaxf(m, old);
+            const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
+            ref[n][y] = kShift - m;
+            l[n][y] *= f;
+#pragma unroll
+            for (int z = 0; z < kSteps; ++z) {
+              o[z][n][y] *= f;
+              o[z][n][y + 2] *= f;
+            }
+          }
+        relative();
+      }
+      uint32_t pb[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) x[n][y] = exp2_approx(x[n][y]);
+        l[n][0] += x[n][0] + x[n][2];
+        l[n][1] += x[n][1] + x[n][3];
+        pb[n][0] = transpose_8x8(pack_pair<__half>(x[n][0], x[n][1]));
+        pb[n][1] = transpose_8x8(pack_pair<__half>(x[n][2], x[n][3]));
+      }
+      __syncwarp();                                                 // V's scales are there
+      // ---- O
+      uint32_t keep_bytes = 0xFFFFFFFFu;                            // E4M3: tokens 4c .. that nobody sees count as zero
+      if (!L::kFp4 && rare(!plain)) {
+        const uint32_t v = here ? valid_eight(w, seen, w.first + tok0 + sc_eight) : 0u;
+        keep_bytes = byte_mask(c & 1 ? v >> 4 : v);
+      }
+#pragma unroll
+      for (int z = 0; z < kSteps; ++z) {
+        uint32_t a[4];
+        if (L::kFp4) {
+          const uint32_t raw = *reinterpret_cast<const uint32_t*>(stage + v_at + z * 128), s4 = raw >> 4, s8 = raw >> 8;
+          const uint2 f = *reinterpret_cast<const uint2*>(scales + z * 32 + 8 * c);
+          uint32_t even[4], odd[4];
+          cvt_f16x2_e2m1x8((raw & 0x0F0F0F0Fu) | (s4 & 0xF0F0F0F0u), even);     // bytes 0 and 2: tokens (0, 1), (2, 3)
+          cvt_f16x2_e2m1x8((s4 & 0x0F0F0F0Fu) | (s8 & 0xF0F0F0F0u), odd);
+          a[0] = mul_half2(even[0], f.x);
+          a[1] = mul_half2(odd[0], f.x);
+          a[2] = mul_half2(even[2], f.y);
+          a[3] = mul_half2(odd[2], f.y);
+        } else {
+          const uint32_t even = *reinterpret_cast<const uint32_t*>(stage + v_at + z * 256) & keep_bytes;
+          const uint32_t odd = *reinterpret_cast<const uint32_t*>(stage + v_at + z * 256 + 16) & keep_bytes;
+          uint32_t e2[2], o2[2];
+          cvt_f16x2_e4m3x4(even, e2);
+          cvt_f16x2_e4m3x4(odd, o2);
+          a[0] = e2[0]; a[1] = o2[0]; a[2] = e2[1]; a[3] = o2[1];
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_16x8x16(o[z][n], a[0], a[1], a[2], a[3], pb[n][0], pb[n][1]);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(free + 8 * ring.at);
+      ring.next();
+      if (pages.i == i + kAhead) {                                  // this warp's turn
+        if (pages.i < n_tiles) {
+          pages.look(p);
+          pages.bring(p, sbase, full, free, abort_at, valid);
+        }
+        pages.skip(p, units, C::kWarps);
+      }
+      // ---- end of the item, or of this CTA's part of it: the warps together
+      if (rare(w.left == 1 || i + 1 == n_tiles)) {
+        const bool whole = part_first == 0 && w.left == 1;
+        const long long out0 = ((long long)w.b * p.H + (long long)w.u * p.group) * p.T;
+        const int slot_of = 2 * (int)blockIdx.x + (part_first == 0);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {                              // eight rows at a time
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float sum = l[n][y];
+            for (int z = 4; z < 32; z <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, z);
+            const int row = 2 * c + y;
+            if (lane < 4) ml_smem[warp * 8 + row] = make_float2(kShift - ref[n][y], sum);
+            float* const dst = o_smem + (warp * 8 + row) * C::kRow + 2 * r;
+#pragma unroll
+            for (int z = 0; z < kSteps; ++z) *reinterpret_cast<float2*>(dst + 16 * z) = make_float2(o[z][n][y], o[z][n][y + 2]);
+          }
+          bar_sync(1, 32 * C::kWarps);
+          // a thread per row and four elements
+#pragma unroll 1
+          for (int j = threadIdx.x; j < min(8, p.rows - 8 * n) * (D / 4); j += 32 * C::kWarps) {
+            const int row8 = j / (D / 4), row = 8 * n + row8, e = j % (D / 4) * 4;
+            float top_m = -INFINITY, total_l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < C::kWarps; ++k) top_m = fmaxf(top_m, ml_smem[k * 8 + row8].x);
+            for (int k = 0; k < C::kWarps; ++k) {
+              const float2 ml = ml_smem[k * 8 + row8];
+              const float f = ml.x == top_m ? 1.f : exp2_approx(ml.x - top_m);
+              const float4 v = *reinterpret_cast<const float4*>(o_smem + (k * 8 + row8) * C::kRow + e);
+              total_l += f * ml.y;
+              y[0] = fmaf(f, v.x, y[0]); y[1] = fmaf(f, v.y, y[1]); y[2] = fmaf(f, v.z, y[2]); y[3] = fmaf(f, v.w, y[3]);
+            }
+            if (whole) {
+              if (row % p.T < n_drafted) {
+                const float inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + w.u));     // nothing seen: 0
+                const uint2 h = p.half ? make_uint2(pack_pair<__half>(y[0] * inv, y[1] * inv), pack_pair<__half>(y[2] * inv, y[3] * inv))
+                                       : make_uint2(pack_pair<__nv_bfloat16>(y[0] * inv, y[1] * inv), pack_pair<__nv_bfloat16>(y[2] * inv, y[3] * inv));
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + (size_t)(out0 + row) * D + e) = h;
+                if (e == 0 && p.lse) p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (top_m - kShift + log2f(total_l)) * 0.6931471805599453f;
+              }
+            } else {
+              *reinterpret_cast<float4*>(p.part + ((size_t)slot_of * R + row) * D + e) = make_float4(y[0], y[1], y[2], y[3]);
+              if (e == 0) p.part_ml[(size_t)slot_of * R + row] = make_float2(top_m, total_l);
+            }
+          }
+          bar_sync(1, 32 * C::kWarps);
+        }
+        if (threadIdx.x == 0 && part_first == 0)
+          p.split[(size_t)w.b * units + w.u] =
+              whole ? make_int2(-1, -1) : make_int2(blockIdx.x, (int)(((find[2] + i + w.left) * find[4] - 1) / find[3]));
+        fresh = true;
+      }
+      advance(w, p, units);
+    }
+    pages.tell(p);
+  }
+  launch_dependents();
+  __syncthreads();
+  if (rare(*abort_word != 0)) {                                     // given up: the copies in flight end before shared memory does
+    if (threadIdx.x == 0 && p.status) *p.status = FP4ATTN_ERR_TIMEOUT;
+    if (threadIdx.x < 2 * C::kStages)
+      for (int spin = 0; spin < (1 << 10) && !mbar_try_wait(full + 8 * (threadIdx.x >> 1), threadIdx.x & 1); ++spin) {}
+    __syncthreads();
+  }
+}
+
 // Joins the parts of the items that fell to several CTAs, in the order of their keys; a warp per row.
 template <int D, int R>
 __global__ void __launch_bounds__(128) tree_join_kernel(const TreeParams p) {
@@ -996,10 +1412,29 @@ int launch_tree(const TreeParams& p, cudaStream_t st) {
     e = launch_overlapped(tree_join_kernel<D, R>, dim3((unsigned)(p.B * units), (unsigned)(std::min(R, p.rows) + 3) / 4), 128u, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
+template <int FMT, int D, int NT>
+int launch_warps(const TreeParams& p, cudaStream_t st) {
+  using C = WarpCfg<FMT, D, NT>;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FP4ATTN_ERR_CUDA;
+  static std::atomic<bool> attr_set[kMaxDevices];
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(tree_warp_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
+    attr_set[dev].store(true, std::memory_order_release);
+  }
+  const int sms = device_sms();
+  if (!sms) return FP4ATTN_ERR_CUDA;
+  const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * p.cache.kv_heads;
+  const unsigned grid = (unsigned)std::min<long long>(std::min(2 * sms, kMostCtas), most_tiles);
+  cudaError_t e = launch_overlapped(tree_warp_kernel<FMT, D, NT>, dim3(grid), C::kThreads, C::kSmem, st, p);
+  if (e == cudaSuccess)
+    e = launch_overlapped(tree_join_kernel<D, C::R>, dim3((unsigned)(p.B * p.cache.kv_heads), (unsigned)(p.rows + 3) / 4), 128u, 0, st, p);
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
+}
 template <int FMT, int D>
 int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
-  if (p.rows <= 8) return launch_tree<FMT, D, 16, 8>(p, st);
-  return R == 16 ? launch_tree<FMT, D, 16, 16>(p, st) : R == 32 ? launch_tree<FMT, D, 32, 16>(p, st) : launch_tree<FMT, D, 64, 16>(p, st);
+  if (p.rows <= 8) return launch_warps<FMT, D, 1>(p, st);
+  return R == 16 ? launch_warps<FMT, D, 2>(p, st) : R == 32 ? launch_tree<FMT, D, 32, 16>(p, st) : launch_tree<FMT, D, 64, 16>(p, st);
 }
 
 }  // namespace
