@@ -37,7 +37,7 @@ namespace {
 using namespace ptx;
 
 constexpr int kTile = 128;                 // keys of a tile
-constexpr int kMostCtas = 320;             // partial results: two per CTA
+constexpr int kMostCtas = 640;             // partial results: two per CTA
 constexpr float kLag = 8.f;                // octaves by which a score may exceed its row's reference
 constexpr float kShift = 7.f;              // a probability of 1 is 2^7: with the lag just inside f16, whose subnormals then begin at 2^-21
 
@@ -321,13 +321,18 @@ struct Pages {
   Turn<STAGES> ring;
   int i = 0;                                                        // tile
   bool lost = false;
-  __device__ __forceinline__ void bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
+  int page = -1;                                                    // of this lane, of the tile
+  __device__ __forceinline__ void find(const TreeParams& p) {
     const int lane = threadIdx.x & 31, P = 1 << p.cache.log_page, slots = kTile >> p.cache.log_page;       // pages of a tile: 1 to 8
-    int page = -1;
+    page = -1;
     if (lane < slots && w.first + lane * P < w.len) {
       page = p.cache.page_of(w.b, w.first + lane * P);
       lost |= page < 0;
     }
+    lost |= (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len;                                       // the table has no room for the last tokens
+  }
+  __device__ __forceinline__ void bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
+    const int lane = threadIdx.x & 31;
     const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
     wait_phase(free + 8 * ring.at, ring.phase ^ 1, abort_at);
     if (lane == 0) {
@@ -346,8 +351,6 @@ struct Pages {
     }
     i += n;
   }
-  // does the table have room for the entry's tokens?
-  __device__ __forceinline__ void look(const TreeParams& p) { lost |= w.b < p.B && (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len; }
   __device__ __forceinline__ void tell(const TreeParams& p) const {
     if (__any_sync(0xffffffffu, lost) && (threadIdx.x & 31) == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
   }
@@ -410,10 +413,11 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     // ===================================================================== pages -> shared memory
     Pages<C::kStages, C::kStage, C::kRing> pages;
     pages.w = w0;
+    if (n_tiles > 0) pages.find(p);
     while (pages.i < n_tiles) {
-      if (rare(pages.i == 0 || pages.w.first == 0)) pages.look(p);
       pages.bring(p, sbase + C::kOffStage, bar(C::RING_FULL), bar(C::RING_FREE), abort_at, valid_ring);
       pages.skip(p, units, 1);
+      if (pages.i < n_tiles) pages.find(p);                         // the table's entries come while the stage is waited for
     }
     pages.tell(p);
     // the last copies end before this warp does (also where the others have given up on them)
@@ -943,35 +947,37 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
 // ---------------------------------------------------------------- sixteen rows or fewer: a warp by itself
 // What bounds few rows is the reading; the kernel above spends more instructions per tile on handing it from role to role than on its keys
 // (4100 a tile of 128 keys, d = 128, half of them hand-overs; 32 sequences of up to 32768 tokens, 4 rows: 200 us, whose reading takes 94).  Here nothing
-// is handed over: a warp takes 16 keys of every tile from their codes to its own maximum, sum and O, all in registers, and the warps of
+// is handed over: a warp takes 32 keys of a tile from their codes to its own maximum, sum and O, all in registers, and the four warps of
 // a CTA meet at the end of an item.
 //
 // The operands of the 16 x 8 x 16 products stay where they are loaded, because the orders of keys and of d are free:
-//   S^T = K Q^T   A: keys x d.  Lane (r, c) = (lane / 4, lane % 4) has keys r and r + 8: it takes D / 4 elements of either from d = c D / 4 on, in
-//                 one piece; step j of the product over d is elements 4j .. 4j + 3 of each lane's piece.  Row r stands for token 4 (r / 2) + r % 2 of the
-//                 sixteen, row r + 8 for the token two further.
-//   O^T += V^T P^T  A: d x keys.  Lane (r, c) has tokens 4c .. 4c + 3, a word of a chunk of V; rows r and r + 8 of product t are elements 16t + 2r
-//                 and 16t + 2r + 1, the two nibbles of a byte (sixteen elements are one block of scales).
-//                 B: P^T, which S^T leaves as keys x rows: two 8 x 8 transposes.
+//   S^T = K Q^T   A: keys x d, twice sixteen keys.  Lane (r, c) = (lane / 4, lane % 4) has keys r and r + 8: it takes D / 4 elements of either
+//                 from d = c D / 4 on, in one piece; step j of the product over d is elements 4j .. 4j + 3 of each lane's piece.
+//   O^T += V^T P^T  A: d x keys.  Lane (r, c) has tokens 8c .. 8c + 7, half a chunk of V; rows r and r + 8 of product t are elements 16t + 2r
+//                 and 16t + 2r + 1, the two nibbles of a byte (sixteen elements are one block of scales).  NVFP4: step q has tokens
+//                 8c + 2q + {0, 4 | 1, 5} (codes of tokens i and i + 4 meet in a byte, as their scales do), E4M3: 8c + 4q + {0, 1 | 2, 3}.
+//                 B: P^T, which S^T leaves as keys x rows: 8 x 8 transposes.  So rows r and r + 8 of the q-th sixteen keys of S^T are those
+//                 of the tokens that stand in columns r of the two halves of step q.
 template <int FMT, int D, int NT>
 struct WarpCfg {
   using L = RecordLayout<FMT, D>;
-  static constexpr int kWarps = 8, kThreads = 32 * kWarps;
+  static constexpr int kWarps = 4, kThreads = 32 * kWarps;
   static constexpr int R = 8 * NT;
   static constexpr int kStage = kTile * 2 * L::kToken;
-  static constexpr int kStages = kStage > 18432 ? 2 : kStage > 16384 ? 4 : kStage > 9216 ? 4 : 6;
+  static constexpr int kStages = kStage > 16384 ? 2 : kStage > 9216 ? 2 : 4;
+  static constexpr int kCtas = kStage > 18432 ? 2 : NT == 2 ? 3 : 4;           // of an SM
   static constexpr int kRow = D + 4;                               // floats of a row of O in shared memory
-  static constexpr int kOffO = kStages * kStage;                   // float [8 warps][8 rows][kRow]
-  static constexpr int kOffML = kOffO + kWarps * 8 * kRow * 4;     // float2 [8 warps][8 rows]
-  static constexpr int kOffScale = kOffML + kWarps * 8 * 8;        // f16 [8 warps][D / 16][16 tokens]
-  static constexpr int kOffValid = kOffScale + kWarps * (D / 16) * 32;
+  static constexpr int kOffO = kStages * kStage;                   // float [4 warps][8 rows][kRow]
+  static constexpr int kOffML = kOffO + kWarps * 8 * kRow * 4;     // float2 [4 warps][8 rows]
+  static constexpr int kOffScale = kOffML + kWarps * 8 * 8;        // f16 [4 warps][D / 16][32 tokens]
+  static constexpr int kOffValid = kOffScale + kWarps * (D / 16) * 64;
   static constexpr int kOffScan = kOffValid + 4 * 8;
   static constexpr int kOffFind = kOffScan + 128;
   static constexpr int kOffBar = kOffFind + 64;
   static constexpr int kSmem = kOffBar + 2 * 8 * kStages + 16 + 128;
-  static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs an SM");
+  static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "CTAs of an SM");
 };
-__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_16x8x16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -982,7 +988,7 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
 }
 
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, 2) tree_warp_kernel(const TreeParams p) {
+__global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D, NT>::kCtas) tree_warp_kernel(const TreeParams p) {
   using C = WarpCfg<FMT, D, NT>;
   using L = typename C::L;
   constexpr int R = C::R, kSteps = D / 16;
@@ -1008,33 +1014,39 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, 2) tree_warp_ke
   uint32_t* const valid = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
   const int P = 1 << p.cache.log_page;
 
-  // The pages of the first tiles; then the warps take turns, each bringing those of the tile that follows the ones on their way
+  // The pages of the first tiles; then the warps take turns, each bringing those of the tile that takes the place of the one they have just
+  // been through.  A warp that brings a tile has itself taken its part of the tile that stood in that stage before: the stage's
+  // barrier cannot be further back than a wait by parity can tell.
   Pages<C::kStages, C::kStage, C::kStages> pages;
   pages.w = w0;
-  constexpr int kAhead = C::kStages - 1;
-  if (warp == 0 && n_tiles > 0) {
-    pages.look(p);
-    while (pages.i < kAhead && pages.i < n_tiles) {
+  if (warp == 0) {
+    while (pages.i < C::kStages && pages.i < n_tiles) {
+      pages.find(p);
       pages.bring(p, sbase, full, free, abort_at, valid);
       pages.skip(p, units, 1);
     }
   } else {
-    pages.skip(p, units, kAhead + warp);
+    pages.skip(p, units, C::kStages + warp);
   }
+  if (pages.i < n_tiles) pages.find(p);
   {
     const int r = lane >> 2, c = lane & 3;
-    // places in a stage: this warp's sixteen tokens, and what the lane takes of them
-    const int tok0 = 16 * warp, slot = tok0 >> p.cache.log_page, t_page = tok0 & (P - 1);
-    const int tok_a = 4 * (r >> 1) + (r & 1);                       // token of row r; row r + 8: two further
+    const int tok0 = 32 * warp;                                     // this warp's tokens of a tile
+    // places in a stage of what the lane takes of them.  A sixteen of tokens is in one page, two may be in two.
+    auto base_of = [&](int sixteen) {
+      const int at = tok0 + 16 * sixteen;
+      return (uint32_t)((at >> p.cache.log_page) * p.cache.record);
+    };
+    auto in_page = [&](int tok) { return (tok0 + tok) & (P - 1); };
+    const int tok_k = 8 * (r >> 1) + (L::kFp4 ? 4 : 1) * (r & 1);   // token of row r of the first sixteen keys; row r + 8 and the second sixteen:
+    constexpr int kSecondRow = L::kFp4 ? 1 : 2, kSecondStep = L::kFp4 ? 2 : 4;                   // so many further
     constexpr int kPiece = L::kRow / 4;                             // code bytes of a lane's piece of a key: 8, 16 or 32
-    const uint32_t rec0 = (uint32_t)(slot * p.cache.record);
-    const uint32_t k_at = rec0 + (uint32_t)((c * kPiece / 16 * P + t_page + tok_a) * 16 + c * kPiece % 16);
-    const uint32_t ks_at = rec0 + (uint32_t)(L::k_scales(P) + (t_page + tok_a) * L::kScales + c * (D / 64));
-    const uint32_t v_at = rec0 + (uint32_t)(L::v_codes(P) + t_page * L::kRow + (L::kFp4 ? r : 2 * r) * 16 + 4 * c);
-    uint8_t* const scales = sgen + C::kOffScale + warp * (D / 16) * 32;
-    // scales of V that this lane converts: four tokens (as they lie) of block lane / 4
-    const uint32_t vs_at = rec0 + (uint32_t)(L::v_scales(P) + (lane >> 2) * P + t_page + 4 * c);
-    const int sc_eight = 8 * (c >> 1), sc_first = 2 * (c & 1);      // they are tokens sc_eight + sc_first + {0, 4, 1, 5}
+    const uint32_t k_at = base_of(r >> 2) + (uint32_t)((c * kPiece / 16 * P + in_page(tok_k)) * 16 + c * kPiece % 16);
+    const uint32_t ks_at = base_of(r >> 2) + (uint32_t)(L::k_scales(P) + in_page(tok_k) * L::kScales + c * (D / 64));
+    const uint32_t v_at = base_of(c >> 1) + (uint32_t)(L::v_codes(P) + in_page(16 * (c >> 1)) * L::kRow + (L::kFp4 ? r : 2 * r) * 16 + 8 * (c & 1));
+    uint8_t* const scales = sgen + C::kOffScale + warp * (D / 16) * 64;
+    // scales of V that this lane converts: the eight tokens 8c .. of block lane / 4
+    const uint32_t vs_at = base_of(c >> 1) + (uint32_t)(L::v_scales(P) + (lane >> 2) * P + in_page(8 * c));
     float* const o_smem = reinterpret_cast<float*>(sgen + C::kOffO);
     float2* const ml_smem = reinterpret_cast<float2*>(sgen + C::kOffML);
 
@@ -1110,165 +1122,178 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, 2) tree_warp_ke
             for (int y = 0; y < 4; ++y) o[x][n][y] = 0.f;
         }
       }
-      wait_phase(full + 8 * ring.at, ring.phase, abort_at);
-      const uint8_t* const stage = sgen + ring.at * C::kStage;
-      const uint32_t held = valid[ring.at];
-      const bool plain = w.first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
-      const bool here = held >> slot & 1;
-      // ---- scales of V: f16, by block and token
-      if (L::kFp4 && lane < D / 4) {
-        uint32_t sc = *reinterpret_cast<const uint32_t*>(stage + vs_at);
-        if (rare(!plain)) {
-          const uint32_t v = here ? permute_eight(valid_eight(w, seen, w.first + tok0 + sc_eight)) : 0u;
-          sc &= byte_mask(c & 1 ? v >> 4 : v);
-        }
-        uint32_t f[2];
-        cvt_f16x2_e4m3x4(sc, f);                                    // tokens (x, x + 4), (x + 1, x + 5): kept as (x, x + 1), (x + 4, x + 5)
-        uint8_t* const to = scales + (lane >> 2) * 32 + (sc_eight + sc_first) * 2;
-        *reinterpret_cast<uint32_t*>(to) = __byte_perm(f[0], f[1], 0x5410);
-        *reinterpret_cast<uint32_t*>(to + 8) = __byte_perm(f[0], f[1], 0x7632);
-      }
-      // ---- scores
-      float s[NT][4];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) s[n][y] = 0.f;
       {
-        uint32_t h[2][2 * kSteps];                                  // f16 pairs of the two keys
+        wait_phase(full + 8 * ring.at, ring.phase, abort_at);
+        const uint8_t* const stage = sgen + ring.at * C::kStage;
+        const uint32_t held = valid[ring.at];
+        const bool plain = w.first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
+        const bool v_here = held >> ((tok0 + 8 * c) >> p.cache.log_page) & 1;
+        uint32_t v_mask = 0xFFu;                                    // of tokens 8c .., those that count
+        if (rare(!plain)) v_mask = v_here ? valid_eight(w, seen, w.first + tok0 + 8 * c) : 0u;
+        // ---- scales of V: f16, by block and token
+        if (L::kFp4 && lane < D / 4) {
+          uint2 sc = *reinterpret_cast<const uint2*>(stage + vs_at);
+          if (rare(!plain)) {
+            const uint32_t v = permute_eight(v_mask);
+            sc.x &= byte_mask(v);
+            sc.y &= byte_mask(v >> 4);
+          }
+          uint32_t f[4];
+          cvt_f16x2_e4m3x4(sc.x, f);
+          cvt_f16x2_e4m3x4(sc.y, f + 2);
+          *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(f[0], f[1], f[2], f[3]);
+        }
+        // ---- scores
+        float s[NT][8];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint8_t* const at = stage + k_at + 32 * k;
-          if (L::kFp4) {
-            uint32_t words[D / 32], f[2];
-            if (D == 128) *reinterpret_cast<uint4*>(words) = *reinterpret_cast<const uint4*>(at);
-            else *reinterpret_cast<uint2*>(words) = *reinterpret_cast<const uint2*>(at);
-            const uint8_t* const sat = stage + ks_at + 2 * L::kScales * k;
-            const uint32_t two = cvt_f16x2_e4m3x2(D == 128 ? *reinterpret_cast<const uint16_t*>(sat) : *sat);
-            f[0] = splat_half(two, 0);
-            f[1] = splat_half(two, 1);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int x = 0; x < D / 32; ++x) {
-              cvt_f16x2_e2m1x8(words[x], h[k] + 4 * x);
+          for (int y = 0; y < 8; ++y) s[n][y] = 0.f;
 #pragma unroll
-              for (int y = 0; y < 4; ++y) h[k][4 * x + y] = mul_half2(h[k][4 * x + y], f[D == 128 ? x >> 1 : 0]);
+        for (int q = 0; q < 2; ++q) {
+          uint32_t h[2][2 * kSteps];                                // f16 pairs of the two keys
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int on = kSecondStep * q + kSecondRow * k;
+            const uint8_t* const at = stage + k_at + 16 * on;
+            if (L::kFp4) {
+              uint32_t words[D / 32], f[2];
+              if (D == 128) *reinterpret_cast<uint4*>(words) = *reinterpret_cast<const uint4*>(at);
+              else *reinterpret_cast<uint2*>(words) = *reinterpret_cast<const uint2*>(at);
+              const uint8_t* const sat = stage + ks_at + L::kScales * on;
+              const uint32_t two = cvt_f16x2_e4m3x2(D == 128 ? *reinterpret_cast<const uint16_t*>(sat) : *sat);
+              f[0] = splat_half(two, 0);
+              f[1] = splat_half(two, 1);
+#pragma unroll
+              for (int x = 0; x < D / 32; ++x) {
+                cvt_f16x2_e2m1x8(words[x], h[k] + 4 * x);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) h[k][4 * x + y] = mul_half2(h[k][4 * x + y], f[D == 128 ? x >> 1 : 0]);
+              }
+            } else {
+#pragma unroll
+              for (int x = 0; x < D / 64; ++x) {
+                const uint4 raw = *reinterpret_cast<const uint4*>(at + x * P * 16);
+                const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int y = 0; y < 4; ++y) cvt_f16x2_e4m3x4(words[y], h[k] + 8 * x + 2 * y);
+              }
             }
-          } else {
+          }
 #pragma unroll
-            for (int x = 0; x < D / 64; ++x) {
-              const uint4 raw = *reinterpret_cast<const uint4*>(at + x * P * 16);
-              const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+          for (int x = 0; x < kSteps; ++x)
 #pragma unroll
-              for (int y = 0; y < 4; ++y) cvt_f16x2_e4m3x4(words[y], h[k] + 8 * x + 2 * y);
+            for (int n = 0; n < NT; ++n)
+              mma_16x8x16(s[n] + 4 * q, h[0][2 * x], h[1][2 * x], h[0][2 * x + 1], h[1][2 * x + 1], qf[n][x][0], qf[n][x][1]);
+        }
+        // ---- probabilities: octaves above the rows' references (+ kShift); what is not seen goes to -infinity
+        float x[NT][8], top = -INFINITY;
+        uint32_t hidden = 0;                                        // bit 8n + y: s[n][y] is not seen
+        if (rare(!plain)) {
+#pragma unroll 1
+          for (int y = 0; y < 8; ++y) {
+            const int tok = tok_k + kSecondStep * (y >> 2) + kSecondRow * (y >> 1 & 1), pos = w.first + tok0 + tok;
+            const bool here = held >> ((tok0 + tok) >> p.cache.log_page) & 1;
+#pragma unroll 1
+            for (int n = 0; n < NT; ++n) {
+              const int row = 8 * n + 2 * c + (y & 1);
+              bool vis = here && pos < w.len;
+              if (pos >= w.ctx) vis = vis && row < p.rows && (row_mask(p, w.b, row % p.T, n_drafted) >> ((pos - w.ctx) & 63) & 1);
+              hidden |= (vis ? 0u : 1u) << (8 * n + y);
             }
           }
         }
+        auto relative = [&] {
 #pragma unroll
-        for (int x = 0; x < kSteps; ++x)
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_16x8x16(s[n], h[0][2 * x], h[1][2 * x], h[0][2 * x + 1], h[1][2 * x + 1], qf[n][x][0], qf[n][x][1]);
-      }
-      // ---- probabilities: octaves above the rows' references (+ kShift); what is not seen goes to -infinity
-      float x[NT][4], top = -INFINITY;
-      uint32_t hidden = 0;                                          // bit 4n + y: s[n][y] is not seen
-      if (rare(!plain)) {
-#pragma unroll 1
-        for (int y = 0; y < 4; ++y) {
-          const int pos = w.first + tok0 + tok_a + 2 * (y >> 1);
-#pragma unroll 1
-          for (int n = 0; n < NT; ++n) {
-            const int row = 8 * n + 2 * c + (y & 1);
-            bool vis = here && pos < w.len;
-            if (pos >= w.ctx) vis = vis && row < p.rows && (row_mask(p, w.b, row % p.T, n_drafted) >> ((pos - w.ctx) & 63) & 1);
-            hidden |= (vis ? 0u : 1u) << (4 * n + y);
+            for (int y = 0; y < 8; ++y) x[n][y] = fmaf(s[n][y], con[n][y & 1], ref[n][y & 1]);
+          if (rare(hidden != 0)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int y = 0; y < 8; ++y)
+                if (hidden >> (8 * n + y) & 1) x[n][y] = -INFINITY;
           }
+        };
+        relative();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int y = 0; y < 8; y += 2) top = max3(top, x[n][y], x[n][y + 1]);
+        if (rare(__any_sync(0xffffffffu, top > kLag + kShift))) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              float m = -INFINITY;                                  // the largest seen; max leaves NaN out
+#pragma unroll
+              for (int z = 0; z < 8; z += 2)
+                if (!(hidden >> (8 * n + y + z) & 1)) m = fmaxf(m, s[n][y + z] * con[n][y]);
+              for (int z = 4; z < 32; z <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, z));
+              const float old = kShift - ref[n][y];                 // -infinity: none yet
+              m = fmaxf(m, old);
+              const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
+              ref[n][y] = kShift - m;
+              l[n][y] *= f;
+#pragma unroll
+              for (int z = 0; z < kSteps; ++z) {
+                o[z][n][y] *= f;
+                o[z][n][y + 2] *= f;
+              }
+            }
+          relative();
         }
-      }
-      auto relative = [&] {
+        uint32_t pb[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            x[n][y] = fmaf(s[n][y], con[n][y & 1], ref[n][y & 1]);
-            if (hidden >> (4 * n + y) & 1) x[n][y] = -INFINITY;
+            const float a = exp2_approx(x[n][2 * y]), b = exp2_approx(x[n][2 * y + 1]);
+            add_pair(l[n][0], l[n][1], a, b);
+            pb[n][y] = transpose_8x8(pack_pair<__half>(a, b));
           }
-      };
-      relative();
+        __syncwarp();                                               // V's scales are there
+        // ---- O
 #pragma unroll
-      for (int n = 0; n < NT; ++n) top = max3(max3(top, x[n][0], x[n][1]), x[n][2], x[n][3]);
-      if (rare(__any_sync(0xffffffffu, top > kLag + kShift))) {
+        for (int z = 0; z < kSteps; ++z) {
+          uint32_t even[4], odd[4];                                 // elements 16z + 2r and 16z + 2r + 1, pairs of tokens
+          if (L::kFp4) {
+            const uint2 raw = *reinterpret_cast<const uint2*>(stage + v_at + z * 128);
+            const uint4 f = *reinterpret_cast<const uint4*>(scales + z * 64 + 16 * c);
+            cvt_f16x2_e2m1x8((raw.x & 0x0F0F0F0Fu) | (raw.y << 4 & 0xF0F0F0F0u), even);
+            cvt_f16x2_e2m1x8((raw.x >> 4 & 0x0F0F0F0Fu) | (raw.y & 0xF0F0F0F0u), odd);
+            const uint32_t g[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float m = -INFINITY;                                    // the largest seen; max leaves NaN out
-            if (!(hidden >> (4 * n + y) & 1)) m = fmaxf(m, s[n][y] * con[n][y]);
-            if (!(hidden >> (4 * n + y + 2) & 1)) m = fmaxf(m, s[n][y + 2] * con[n][y]);
-            for (int z = 4; z < 32; z <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, z));
-            const float old = kShift - ref[n][y];                   // -infinity: none yet
-            m = fmaxf(m, old);
-            const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
-            ref[n][y] = kShift - m;
-            l[n][y] *= f;
-#pragma unroll
-            for (int z = 0; z < kSteps; ++z) {
-              o[z][n][y] *= f;
-              o[z][n][y + 2] *= f;
+            for (int y = 0; y < 4; ++y) {
+              even[y] = mul_half2(even[y], g[y]);
+              odd[y] = mul_half2(odd[y], g[y]);
             }
+          } else {
+            uint2 e = *reinterpret_cast<const uint2*>(stage + v_at + z * 256), d = *reinterpret_cast<const uint2*>(stage + v_at + z * 256 + 16);
+            if (rare(!plain)) {
+              const uint32_t lo = byte_mask(v_mask), hi = byte_mask(v_mask >> 4);
+              e.x &= lo; e.y &= hi; d.x &= lo; d.y &= hi;
+            }
+            cvt_f16x2_e4m3x4(e.x, even);
+            cvt_f16x2_e4m3x4(e.y, even + 2);
+            cvt_f16x2_e4m3x4(d.x, odd);
+            cvt_f16x2_e4m3x4(d.y, odd + 2);
           }
-        relative();
-      }
-      uint32_t pb[NT][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+          for (int q = 0; q < 2; ++q)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) x[n][y] = exp2_approx(x[n][y]);
-        l[n][0] += x[n][0] + x[n][2];
-        l[n][1] += x[n][1] + x[n][3];
-        pb[n][0] = transpose_8x8(pack_pair<__half>(x[n][0], x[n][1]));
-        pb[n][1] = transpose_8x8(pack_pair<__half>(x[n][2], x[n][3]));
-      }
-      __syncwarp();                                                 // V's scales are there
-      // ---- O
-      uint32_t keep_bytes = 0xFFFFFFFFu;                            // E4M3: tokens 4c .. that nobody sees count as zero
-      if (!L::kFp4 && rare(!plain)) {
-        const uint32_t v = here ? valid_eight(w, seen, w.first + tok0 + sc_eight) : 0u;
-        keep_bytes = byte_mask(c & 1 ? v >> 4 : v);
-      }
-#pragma unroll
-      for (int z = 0; z < kSteps; ++z) {
-        uint32_t a[4];
-        if (L::kFp4) {
-          const uint32_t raw = *reinterpret_cast<const uint32_t*>(stage + v_at + z * 128), s4 = raw >> 4, s8 = raw >> 8;
-          const uint2 f = *reinterpret_cast<const uint2*>(scales + z * 32 + 8 * c);
-          uint32_t even[4], odd[4];
-          cvt_f16x2_e2m1x8((raw & 0x0F0F0F0Fu) | (s4 & 0xF0F0F0F0u), even);     // bytes 0 and 2: tokens (0, 1), (2, 3)
-          cvt_f16x2_e2m1x8((s4 & 0x0F0F0F0Fu) | (s8 & 0xF0F0F0F0u), odd);
-          a[0] = mul_half2(even[0], f.x);
-          a[1] = mul_half2(odd[0], f.x);
-          a[2] = mul_half2(even[2], f.y);
-          a[3] = mul_half2(odd[2], f.y);
-        } else {
-          const uint32_t even = *reinterpret_cast<const uint32_t*>(stage + v_at + z * 256) & keep_bytes;
-          const uint32_t odd = *reinterpret_cast<const uint32_t*>(stage + v_at + z * 256 + 16) & keep_bytes;
-          uint32_t e2[2], o2[2];
-          cvt_f16x2_e4m3x4(even, e2);
-          cvt_f16x2_e4m3x4(odd, o2);
-          a[0] = e2[0]; a[1] = o2[0]; a[2] = e2[1]; a[3] = o2[1];
+            for (int n = 0; n < NT; ++n) mma_16x8x16(o[z][n], even[2 * q], odd[2 * q], even[2 * q + 1], odd[2 * q + 1], pb[n][2 * q], pb[n][2 * q + 1]);
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma_16x8x16(o[z][n], a[0], a[1], a[2], a[3], pb[n][0], pb[n][1]);
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(free + 8 * ring.at);
-      ring.next();
-      if (pages.i == i + kAhead) {                                  // this warp's turn
-        if (pages.i < n_tiles) {
-          pages.look(p);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(free + 8 * ring.at);
+        if (pages.i == i + C::kStages && pages.i < n_tiles) {        // this warp's turn
           pages.bring(p, sbase, full, free, abort_at, valid);
+          pages.skip(p, units, C::kWarps);
+          if (pages.i < n_tiles) pages.find(p);                     // (the entries come until its next turn)
         }
-        pages.skip(p, units, C::kWarps);
       }
+      ring.next();
       // ---- end of the item, or of this CTA's part of it: the warps together
       if (rare(w.left == 1 || i + 1 == n_tiles)) {
         const bool whole = part_first == 0 && w.left == 1;
@@ -1425,7 +1450,7 @@ int launch_warps(const TreeParams& p, cudaStream_t st) {
   const int sms = device_sms();
   if (!sms) return FP4ATTN_ERR_CUDA;
   const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * p.cache.kv_heads;
-  const unsigned grid = (unsigned)std::min<long long>(std::min(2 * sms, kMostCtas), most_tiles);
+  const unsigned grid = (unsigned)std::min<long long>(std::min(C::kCtas * sms, kMostCtas), most_tiles);
   cudaError_t e = launch_overlapped(tree_warp_kernel<FMT, D, NT>, dim3(grid), C::kThreads, C::kSmem, st, p);
   if (e == cudaSuccess)
     e = launch_overlapped(tree_join_kernel<D, C::R>, dim3((unsigned)(p.B * p.cache.kv_heads), (unsigned)(p.rows + 3) / 4), 128u, 0, st, p);
