@@ -313,13 +313,13 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
   return (int)min(t1 - t0, (long long)INT_MAX);
 }
 
-// Brings the pages of tiles into a ring of stages, one bulk copy each; a whole warp.  RING: tiles for which `valid` remembers which of their
-// pages exist.
-template <int STAGES, int STAGE, int RING>
+// Brings the pages of tiles into a ring of stages, one bulk copy each; a whole warp.  RING: stages for which `valid` remembers which of the
+// pages exist.  PARTS = 2: K and V by themselves, each in a stage of its own.
+template <int STAGES, int STAGE, int RING, int PARTS = 1>
 struct Pages {
   Walk w;
   Turn<STAGES> ring;
-  int i = 0;                                                        // tile
+  int i = 0;                                                        // part
   bool lost = false;
   int page = -1;                                                    // of this lane, of the tile
   __device__ __forceinline__ void find(const TreeParams& p) {
@@ -335,21 +335,23 @@ struct Pages {
     const int lane = threadIdx.x & 31;
     const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
     wait_phase(free + 8 * ring.at, ring.phase ^ 1, abort_at);
+    const int bytes = p.cache.record / PARTS;
     if (lane == 0) {
       valid[i % RING] = held;
-      mbar_arrive_expect_tx(full + 8 * ring.at, __popc(held) * p.cache.record);
+      mbar_arrive_expect_tx(full + 8 * ring.at, __popc(held) * bytes);
     }
     __syncwarp();
     if (page >= 0)
-      bulk_load_1d(stages + ring.at * STAGE + lane * p.cache.record, p.cache.rec(page, w.u / p.row_tiles), p.cache.record, full + 8 * ring.at);
+      bulk_load_1d(stages + ring.at * STAGE + lane * bytes, p.cache.rec(page, w.u / p.row_tiles) + (PARTS == 2 ? (i & 1) * bytes : 0), bytes,
+                   full + 8 * ring.at);
   }
   __device__ __forceinline__ void skip(const TreeParams& p, int units, int n) {
 #pragma unroll 1
     for (int k = 0; k < n; ++k) {
-      advance(w, p, units);
+      if (PARTS == 1 || (i & 1)) advance(w, p, units);
       ring.next();
+      ++i;
     }
-    i += n;
   }
   __device__ __forceinline__ void tell(const TreeParams& p) const {
     if (__any_sync(0xffffffffu, lost) && (threadIdx.x & 31) == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
@@ -963,15 +965,16 @@ struct WarpCfg {
   using L = RecordLayout<FMT, D>;
   static constexpr int kWarps = 4, kThreads = 32 * kWarps;
   static constexpr int R = 8 * NT;
-  static constexpr int kStage = kTile * 2 * L::kToken;
-  static constexpr int kStages = kStage > 16384 ? 2 : kStage > 9216 ? 2 : 4;
-  static constexpr int kCtas = kStage > 18432 ? 2 : NT == 2 ? 3 : 4;           // of an SM
-  static constexpr int kRow = D + 4;                               // floats of a row of O in shared memory
+  static constexpr int kStage = kTile * L::kToken;                 // K or V of a tile
+  static constexpr int kCtas = kStage > 9216 ? 2 : NT == 2 ? 3 : 4;            // of an SM
+  static constexpr int kStages = kStage > 9216 ? 6 : kStage > 8192 ? (kCtas == 3 ? 7 : 5) : 6;
+  static constexpr int kRow = D / 2;                               // floats of a row of half an O in shared memory (unpadded: it is full)
   static constexpr int kOffO = kStages * kStage;                   // float [4 warps][8 rows][kRow]
   static constexpr int kOffML = kOffO + kWarps * 8 * kRow * 4;     // float2 [4 warps][8 rows]
   static constexpr int kOffScale = kOffML + kWarps * 8 * 8;        // f16 [4 warps][D / 16][32 tokens]
   static constexpr int kOffValid = kOffScale + kWarps * (D / 16) * 64;
-  static constexpr int kOffScan = kOffValid + 4 * 8;
+  static constexpr int kOffScan = kOffValid + 4 * 8;               // (room for kStages words)
+  static_assert(kStages <= 8, "valid");
   static constexpr int kOffFind = kOffScan + 128;
   static constexpr int kOffBar = kOffFind + 64;
   static constexpr int kSmem = kOffBar + 2 * 8 * kStages + 16 + 128;
@@ -1014,13 +1017,14 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
   uint32_t* const valid = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
   const int P = 1 << p.cache.log_page;
 
-  // The pages of the first tiles; then the warps take turns, each bringing those of the tile that takes the place of the one they have just
-  // been through.  A warp that brings a tile has itself taken its part of the tile that stood in that stage before: the stage's
-  // barrier cannot be further back than a wait by parity can tell.
-  Pages<C::kStages, C::kStage, C::kStages> pages;
+  // K and V of the first tiles; then the warps take turns, each bringing what takes the place of the K or V before the one they have just
+  // been through (of that one the other warps may not be through yet).  A warp that fills a stage has itself been through what stood there before: the stage's barrier cannot be further back
+  // than a wait by parity can tell.
+  Pages<C::kStages, C::kStage, C::kStages, 2> pages;
   pages.w = w0;
+  const int n_parts = n_tiles > INT_MAX / 2 ? INT_MAX : 2 * n_tiles;
   if (warp == 0) {
-    while (pages.i < C::kStages && pages.i < n_tiles) {
+    while (pages.i < C::kStages && pages.i < n_parts) {
       pages.find(p);
       pages.bring(p, sbase, full, free, abort_at, valid);
       pages.skip(p, units, 1);
@@ -1028,14 +1032,21 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
   } else {
     pages.skip(p, units, C::kStages + warp);
   }
-  if (pages.i < n_tiles) pages.find(p);
+  if (pages.i < n_parts) pages.find(p);
+  auto next_pages = [&](int part) {                                 // this warp's turn?
+    if (pages.i == part - 1 + C::kStages && pages.i < n_parts) {
+      pages.bring(p, sbase, full, free, abort_at, valid);
+      pages.skip(p, units, C::kWarps);
+      if (pages.i < n_parts) pages.find(p);                         // (the entries come until its next turn)
+    }
+  };
   {
     const int r = lane >> 2, c = lane & 3;
     const int tok0 = 32 * warp;                                     // this warp's tokens of a tile
     // places in a stage of what the lane takes of them.  A sixteen of tokens is in one page, two may be in two.
     auto base_of = [&](int sixteen) {
       const int at = tok0 + 16 * sixteen;
-      return (uint32_t)((at >> p.cache.log_page) * p.cache.record);
+      return (uint32_t)((at >> p.cache.log_page) * (p.cache.record / 2));
     };
     auto in_page = [&](int tok) { return (tok0 + tok) & (P - 1); };
     const int tok_k = 8 * (r >> 1) + (L::kFp4 ? 4 : 1) * (r & 1);   // token of row r of the first sixteen keys; row r + 8 and the second sixteen:
@@ -1043,10 +1054,10 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
     constexpr int kPiece = L::kRow / 4;                             // code bytes of a lane's piece of a key: 8, 16 or 32
     const uint32_t k_at = base_of(r >> 2) + (uint32_t)((c * kPiece / 16 * P + in_page(tok_k)) * 16 + c * kPiece % 16);
     const uint32_t ks_at = base_of(r >> 2) + (uint32_t)(L::k_scales(P) + in_page(tok_k) * L::kScales + c * (D / 64));
-    const uint32_t v_at = base_of(c >> 1) + (uint32_t)(L::v_codes(P) + in_page(16 * (c >> 1)) * L::kRow + (L::kFp4 ? r : 2 * r) * 16 + 8 * (c & 1));
+    const uint32_t v_at = base_of(c >> 1) + (uint32_t)(in_page(16 * (c >> 1)) * L::kRow + (L::kFp4 ? r : 2 * r) * 16 + 8 * (c & 1));
     uint8_t* const scales = sgen + C::kOffScale + warp * (D / 16) * 64;
     // scales of V that this lane converts: the eight tokens 8c .. of block lane / 4
-    const uint32_t vs_at = base_of(c >> 1) + (uint32_t)(L::v_scales(P) + (lane >> 2) * P + in_page(8 * c));
+    const uint32_t vs_at = base_of(c >> 1) + (uint32_t)(P * L::kRow + (lane >> 2) * P + in_page(8 * c));
     float* const o_smem = reinterpret_cast<float*>(sgen + C::kOffO);
     float2* const ml_smem = reinterpret_cast<float2*>(sgen + C::kOffML);
 
@@ -1124,25 +1135,12 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
       }
       {
         wait_phase(full + 8 * ring.at, ring.phase, abort_at);
-        const uint8_t* const stage = sgen + ring.at * C::kStage;
+        const uint8_t* stage = sgen + ring.at * C::kStage;
         const uint32_t held = valid[ring.at];
         const bool plain = w.first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
         const bool v_here = held >> ((tok0 + 8 * c) >> p.cache.log_page) & 1;
         uint32_t v_mask = 0xFFu;                                    // of tokens 8c .., those that count
         if (rare(!plain)) v_mask = v_here ? valid_eight(w, seen, w.first + tok0 + 8 * c) : 0u;
-        // ---- scales of V: f16, by block and token
-        if (L::kFp4 && lane < D / 4) {
-          uint2 sc = *reinterpret_cast<const uint2*>(stage + vs_at);
-          if (rare(!plain)) {
-            const uint32_t v = permute_eight(v_mask);
-            sc.x &= byte_mask(v);
-            sc.y &= byte_mask(v >> 4);
-          }
-          uint32_t f[4];
-          cvt_f16x2_e4m3x4(sc.x, f);
-          cvt_f16x2_e4m3x4(sc.y, f + 2);
-          *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(f[0], f[1], f[2], f[3]);
-        }
         // ---- scores
         float s[NT][8];
 #pragma unroll
@@ -1186,6 +1184,10 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             for (int n = 0; n < NT; ++n)
               mma_16x8x16(s[n] + 4 * q, h[0][2 * x], h[1][2 * x], h[0][2 * x + 1], h[1][2 * x + 1], qf[n][x][0], qf[n][x][1]);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(free + 8 * ring.at);
+        ring.next();
+        next_pages(2 * i);
         // ---- probabilities: octaves above the rows' references (+ kShift); what is not seen goes to -infinity
         float x[NT][8], top = -INFINITY;
         uint32_t hidden = 0;                                        // bit 8n + y: s[n][y] is not seen
@@ -1253,7 +1255,22 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             add_pair(l[n][0], l[n][1], a, b);
             pb[n][y] = transpose_8x8(pack_pair<__half>(a, b));
           }
-        __syncwarp();                                               // V's scales are there
+        wait_phase(full + 8 * ring.at, ring.phase, abort_at);
+        stage = sgen + ring.at * C::kStage;
+        // ---- scales of V: f16, by block and token
+        if (L::kFp4 && lane < D / 4) {
+          uint2 sc = *reinterpret_cast<const uint2*>(stage + vs_at);
+          if (rare(!plain)) {
+            const uint32_t v = permute_eight(v_mask);
+            sc.x &= byte_mask(v);
+            sc.y &= byte_mask(v >> 4);
+          }
+          uint32_t f[4];
+          cvt_f16x2_e4m3x4(sc.x, f);
+          cvt_f16x2_e4m3x4(sc.y, f + 2);
+          *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(f[0], f[1], f[2], f[3]);
+        }
+        __syncwarp();
         // ---- O
 #pragma unroll
         for (int z = 0; z < kSteps; ++z) {
@@ -1287,59 +1304,59 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(free + 8 * ring.at);
-        if (pages.i == i + C::kStages && pages.i < n_tiles) {        // this warp's turn
-          pages.bring(p, sbase, full, free, abort_at, valid);
-          pages.skip(p, units, C::kWarps);
-          if (pages.i < n_tiles) pages.find(p);                     // (the entries come until its next turn)
-        }
+        ring.next();
+        next_pages(2 * i + 1);
       }
-      ring.next();
       // ---- end of the item, or of this CTA's part of it: the warps together
       if (rare(w.left == 1 || i + 1 == n_tiles)) {
         const bool whole = part_first == 0 && w.left == 1;
         const long long out0 = ((long long)w.b * p.H + (long long)w.u * p.group) * p.T;
         const int slot_of = 2 * (int)blockIdx.x + (part_first == 0);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {                              // eight rows at a time
+        for (int n = 0; n < NT; ++n)                                // eight rows and half the elements at a time
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float sum = l[n][y];
-            for (int z = 4; z < 32; z <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, z);
-            const int row = 2 * c + y;
-            if (lane < 4) ml_smem[warp * 8 + row] = make_float2(kShift - ref[n][y], sum);
-            float* const dst = o_smem + (warp * 8 + row) * C::kRow + 2 * r;
+          for (int z0 = 0; z0 < kSteps; z0 += kSteps / 2) {
 #pragma unroll
-            for (int z = 0; z < kSteps; ++z) *reinterpret_cast<float2*>(dst + 16 * z) = make_float2(o[z][n][y], o[z][n][y + 2]);
-          }
-          bar_sync(1, 32 * C::kWarps);
-          // a thread per row and four elements
-#pragma unroll 1
-          for (int j = threadIdx.x; j < min(8, p.rows - 8 * n) * (D / 4); j += 32 * C::kWarps) {
-            const int row8 = j / (D / 4), row = 8 * n + row8, e = j % (D / 4) * 4;
-            float top_m = -INFINITY, total_l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int k = 0; k < C::kWarps; ++k) top_m = fmaxf(top_m, ml_smem[k * 8 + row8].x);
-            for (int k = 0; k < C::kWarps; ++k) {
-              const float2 ml = ml_smem[k * 8 + row8];
-              const float f = ml.x == top_m ? 1.f : exp2_approx(ml.x - top_m);
-              const float4 v = *reinterpret_cast<const float4*>(o_smem + (k * 8 + row8) * C::kRow + e);
-              total_l += f * ml.y;
-              y[0] = fmaf(f, v.x, y[0]); y[1] = fmaf(f, v.y, y[1]); y[2] = fmaf(f, v.z, y[2]); y[3] = fmaf(f, v.w, y[3]);
-            }
-            if (whole) {
-              if (row % p.T < n_drafted) {
-                const float inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + w.u));     // nothing seen: 0
-                const uint2 h = p.half ? make_uint2(pack_pair<__half>(y[0] * inv, y[1] * inv), pack_pair<__half>(y[2] * inv, y[3] * inv))
-                                       : make_uint2(pack_pair<__nv_bfloat16>(y[0] * inv, y[1] * inv), pack_pair<__nv_bfloat16>(y[2] * inv, y[3] * inv));
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + (size_t)(out0 + row) * D + e) = h;
-                if (e == 0 && p.lse) p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (top_m - kShift + log2f(total_l)) * 0.6931471805599453f;
+            for (int y = 0; y < 2; ++y) {
+              const int row = 2 * c + y;
+              if (z0 == 0) {
+                float sum = l[n][y];
+                for (int z = 4; z < 32; z <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, z);
+                if (lane < 4) ml_smem[warp * 8 + row] = make_float2(kShift - ref[n][y], sum);
               }
-            } else {
-              *reinterpret_cast<float4*>(p.part + ((size_t)slot_of * R + row) * D + e) = make_float4(y[0], y[1], y[2], y[3]);
-              if (e == 0) p.part_ml[(size_t)slot_of * R + row] = make_float2(top_m, total_l);
+              float* const dst = o_smem + (warp * 8 + row) * C::kRow + 2 * r;
+#pragma unroll
+              for (int z = 0; z < kSteps / 2; ++z) *reinterpret_cast<float2*>(dst + 16 * z) = make_float2(o[z0 + z][n][y], o[z0 + z][n][y + 2]);
             }
+            __syncthreads();
+            // a thread per row and four elements
+#pragma unroll 1
+            for (int j = threadIdx.x; j < min(8, p.rows - 8 * n) * (D / 8); j += C::kThreads) {
+              const int row8 = j / (D / 8), row = 8 * n + row8, e8 = j % (D / 8) * 4, e = 16 * z0 + e8;
+              float top_m = -INFINITY, total_l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+              for (int k = 0; k < C::kWarps; ++k) top_m = fmaxf(top_m, ml_smem[k * 8 + row8].x);
+              for (int k = 0; k < C::kWarps; ++k) {
+                const float2 ml = ml_smem[k * 8 + row8];
+                const float f = ml.x == top_m ? 1.f : exp2_approx(ml.x - top_m);
+                const float4 v = *reinterpret_cast<const float4*>(o_smem + (k * 8 + row8) * C::kRow + e8);
+                total_l += f * ml.y;
+                y[0] = fmaf(f, v.x, y[0]); y[1] = fmaf(f, v.y, y[1]); y[2] = fmaf(f, v.z, y[2]); y[3] = fmaf(f, v.w, y[3]);
+              }
+              if (whole) {
+                if (row % p.T < n_drafted) {
+                  const float inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + w.u));     // nothing seen: 0
+                  const uint2 h = p.half ? make_uint2(pack_pair<__half>(y[0] * inv, y[1] * inv), pack_pair<__half>(y[2] * inv, y[3] * inv))
+                                         : make_uint2(pack_pair<__nv_bfloat16>(y[0] * inv, y[1] * inv), pack_pair<__nv_bfloat16>(y[2] * inv, y[3] * inv));
+                  *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + (size_t)(out0 + row) * D + e) = h;
+                  if (e == 0 && p.lse) p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (top_m - kShift + log2f(total_l)) * 0.6931471805599453f;
+                }
+              } else {
+                *reinterpret_cast<float4*>(p.part + ((size_t)slot_of * R + row) * D + e) = make_float4(y[0], y[1], y[2], y[3]);
+                if (e == 0) p.part_ml[(size_t)slot_of * R + row] = make_float2(top_m, total_l);
+              }
+            }
+            __syncthreads();
           }
-          bar_sync(1, 32 * C::kWarps);
-        }
         if (threadIdx.x == 0 && part_first == 0)
           p.split[(size_t)w.b * units + w.u] =
               whole ? make_int2(-1, -1) : make_int2(blockIdx.x, (int)(((find[2] + i + w.left) * find[4] - 1) / find[3]));
