@@ -1,17 +1,19 @@
 // Quantizing K and V into the pages of a cache, and reading them back.
 //
-// Both are bound by HBM: 2 bytes an element on the 16-bit side, 9/16 or 1 in the cache.  A block takes the tokens of one batch
-// entry that stand in an aligned sixteen of the sequence - the unit in which V is kept - for a range of heads; a thread takes
-// sixteen elements of one token, which is one NVFP4 block: 32 bytes in, no exchange with other threads for the block's
-// maximum.  The bytes of K and V of the sixteen tokens are put together in shared memory as they lie in the page and leave
-// in 16-byte stores.  Where the call's tokens do not fill a sixteen, V's bytes leave one by one: the others belong to
-// tokens that are there already.
+// Both are bound by HBM: 2 bytes an element on the 16-bit side, 9/16 or 1 in the cache.  A block takes some tokens of one KV head, half
+// of its threads K and half V, 128 elements a thread; nothing goes through shared memory and no thread waits for another block's work.
+//   K  is kept token by token: a thread takes sixteen elements of one token (an NVFP4 block) to write, eight to read.
+//   V  is kept in chunks of sixteen tokens at one pair of elements (E4M3: one element): a thread takes eight elements of the sixteen tokens of
+//      such chunks and turns bytes around in registers, so that both sides are accessed 16 bytes at a time, neighbouring lanes at
+//      neighbouring addresses.  Where a call's tokens do not fill a sixteen, V's bytes are written one by one: the others belong to tokens
+//      that are there already.
 #include "kv_cache.cuh"
 
 namespace fp4attn {
 namespace {
 
-constexpr int kTok = 16;                                          // tokens of a block
+constexpr int kThreads = 128, kHalf = 64;
+template <int D> constexpr int kBlockTokens = 8192 / D;           // 64 threads of 128 elements
 
 template <typename T>
 struct WriteParams {
@@ -20,27 +22,43 @@ struct WriteParams {
   const int *start, *count, *positions;
   const float* inv_freq;
   int* status;
-  int B, N, groups, heads_per_block, pairs;
+  int B, N, heads_per_block, pairs;
   float factor;
   bool vector, interleaved;
 };
 
-// sixteen elements from x[first] on
+// eight elements from x on, as four words
 template <typename T>
-__device__ __forceinline__ void load16(const T* x, bool vector, float* v) {
+__device__ __forceinline__ uint4 load8(const T* x, bool vector) {
+  if (vector) return __ldg(reinterpret_cast<const uint4*>(x));
+  const uint16_t* y = reinterpret_cast<const uint16_t*>(x);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__ldg(y + 2 * i) | (uint32_t)__ldg(y + 2 * i + 1) << 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* y, bool vector, uint4 raw) {
   if (vector) {
-    uint32_t w[8];
-    *reinterpret_cast<uint4*>(w) = __ldg(reinterpret_cast<const uint4*>(x));
-    *reinterpret_cast<uint4*>(w + 4) = __ldg(reinterpret_cast<const uint4*>(x) + 1);
+    *reinterpret_cast<uint4*>(y) = raw;
+    return;
+  }
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  uint16_t* z = reinterpret_cast<uint16_t*>(y);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 f = unpack2<T>(w[i]);
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
-    }
-  } else {
+  for (int i = 0; i < 4; ++i) {
+    z[2 * i] = (uint16_t)w[i];
+    z[2 * i + 1] = (uint16_t)(w[i] >> 16);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(uint4 raw, float* v) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = to_float(x[i]);
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = unpack2<T>(w[i]);
+    v[2 * i] = f.x;
+    v[2 * i + 1] = f.y;
   }
 }
 
@@ -57,7 +75,10 @@ __device__ __forceinline__ void rotate16(const T* row, int e0, bool vector, bool
     const bool whole = vector && pairs % 16 == 0;                 // the partners are sixteen neighbours too
     float w[16];
     const int other = e0 < pairs ? e0 + pairs : e0 - pairs;
-    if (whole && e0 < 2 * pairs) load16(row + other, true, w);
+    if (whole && e0 < 2 * pairs) {
+      unpack8<T>(load8(row + other, true), w);
+      unpack8<T>(load8(row + other + 8, true), w + 8);
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int e = e0 + i;
@@ -72,119 +93,190 @@ __device__ __forceinline__ void rotate16(const T* row, int e0, bool vector, bool
   for (int i = 0; i < 16; ++i) v[i] = to_float(from_float<T>(v[i]));
 }
 
-// NVFP4 block: eight bytes of codes; the scale byte.  NaN counts as 0 (the cache holds finite values only).
-__device__ __forceinline__ uint2 nvfp4_block(float* v, float G, uint32_t* scale) {
+// NaN counts as 0 (the cache holds finite values only)
+template <int N>
+__device__ __forceinline__ float clean_max(float* v) {
   float a = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < N; ++i) {
     v[i] = v[i] == v[i] ? v[i] : 0.f;
     a = fmaxf(a, fabsf(v[i]));
   }
-  const uint32_t byte = cvt_e4m3x2(__fdiv_rn(__fmul_rn(a, G), 6.f), 0.f) & 0xFFu;
-  const float S = e4m3_value(byte);
-  const float r = S > 0.f ? __fdiv_rn(G, S) : 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = __fmul_rn(v[i], r);
-  *scale = byte;
-  return make_uint2(cvt_e2m1x8(v), cvt_e2m1x8(v + 8));
+  return a;
 }
-// sixteen E4M3 bytes
-__device__ __forceinline__ uint4 e4m3_block(float* v, float G) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = v[i] == v[i] ? __fmul_rn(v[i], G) : 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = cvt_e4m3x2(v[4 * i], v[4 * i + 1]) | cvt_e4m3x2(v[4 * i + 2], v[4 * i + 3]) << 16;
-  return make_uint4(w[0], w[1], w[2], w[3]);
+// scale byte of an NVFP4 block of largest magnitude a, and the factor on its elements
+__device__ __forceinline__ float nvfp4_scale(float a, float G, uint32_t* byte) {
+  *byte = cvt_e4m3x2(__fdiv_rn(__fmul_rn(a, G), 6.f), 0.f) & 0xFFu;
+  const float S = e4m3_value(*byte);
+  return S > 0.f ? __fdiv_rn(G, S) : 0.f;
+}
+__device__ __forceinline__ uint32_t e4m3x4(const float* v, float G) {
+  return cvt_e4m3x2(__fmul_rn(v[0], G), __fmul_rn(v[1], G)) | cvt_e4m3x2(__fmul_rn(v[2], G), __fmul_rn(v[3], G)) << 16;
+}
+// byte j of word i <-> byte i of word j
+__device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4]) {
+  const uint32_t a = __byte_perm(w[0], w[1], 0x5140), b = __byte_perm(w[2], w[3], 0x5140);
+  const uint32_t c = __byte_perm(w[0], w[1], 0x7362), d = __byte_perm(w[2], w[3], 0x7362);
+  w[0] = __byte_perm(a, b, 0x5410);
+  w[1] = __byte_perm(a, b, 0x7632);
+  w[2] = __byte_perm(c, d, 0x5410);
+  w[3] = __byte_perm(c, d, 0x7632);
 }
 
-// Threads: token (of sixteen) fastest, then the head's sixteens of elements.  Grid: sixteens of the sequence, batch, head ranges.
-template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(D) cache_write_kernel(const WriteParams<T> p) {
+// the tokens of a block: `pos0` its first place in the sequence, a multiple of its tokens; first .. last - 1 those that the call has
+template <int D>
+struct Span {
+  long long pos0, first, last;
+  int start;
+  __device__ __forceinline__ Span(const int* starts, const int* counts, int N, int b) {
+    start = __ldg(starts + b);
+    const int n = counts ? max(0, min(__ldg(counts + b), N)) : N;
+    constexpr int kTokens = kBlockTokens<D>;
+    pos0 = ((long long)(start >= 0 ? start / kTokens : -((kTokens - 1 - (long long)start) / kTokens)) + blockIdx.x) * kTokens;
+    first = max((long long)start, pos0);
+    last = min((long long)start + n, pos0 + kTokens);
+  }
+  __device__ __forceinline__ bool has(int tok) const { return pos0 + tok >= first && pos0 + tok < last; }
+  __device__ __forceinline__ int index(int tok) const { return (int)(pos0 + tok - start); }
+};
+
+// Grid: blocks of the sequence, batch, head ranges.
+template <typename T, int FMT, int D, bool ROTARY>
+__global__ void __launch_bounds__(kThreads, ROTARY ? 4 : 5) cache_write_kernel(const WriteParams<T> p) {
   using L = RecordLayout<FMT, D>;
-  // one head's bytes as they lie in the page, K: codes by chunk of 16 bytes and token, scales by token; V: codes by index and token,
-  // scales by block and place
-  __shared__ alignas(16) uint8_t sk[kTok * L::kRow], sv[kTok * L::kRow], sks[kTok * (L::kScales + 1)], svs[kTok * (L::kScales + 1)];
-  extern __shared__ float2 table[];                               // [16][pairs]: cosines and sines of the tokens
+  extern __shared__ float2 table[];                               // [tokens][pairs]: cosines and sines
   launch_dependents();
   wait_prior_grids();
-  const int b = blockIdx.y, tid = threadIdx.x, tok = tid & 15, blk = tid >> 4;
-  const int start = __ldg(p.start + b), n = p.count ? max(0, min(__ldg(p.count + b), p.N)) : p.N;
-  // the sixteen that this block takes; a start below 0 counts from there (its tokens in front of 0 have no page)
-  const long long pos0 = ((long long)(start >> 4) + blockIdx.x) << 4;
-  const long long first = max((long long)start, pos0), last = min((long long)start + n, pos0 + kTok);
-  if (first >= last) return;
+  const int b = blockIdx.y, tid = threadIdx.x;
+  const Span<D> span(p.start, p.count, p.N, b);
+  if (span.first >= span.last) return;
   const int P = 1 << p.cache.log_page;
-  const long long pos = pos0 + tok;
-  const bool mine = pos >= first && pos < last;
-  const int page = p.cache.page_of(b, pos0);                      // a page holds whole sixteens
-  if (page < 0) {
-    if (tid == 0 && blockIdx.z == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
-    return;
-  }
-  const int t0 = (int)(pos0 & (P - 1)), i = (int)(pos - start);                 // place in the page; index in the call
-  if (p.pairs) {
-    for (int j = tid; j < kTok * p.pairs; j += D) {
-      const int t = j / p.pairs, f = j - t * p.pairs;
-      if (pos0 + t < first || pos0 + t >= last) continue;
-      const int at = p.positions ? __ldg(p.positions + (size_t)b * p.N + (pos0 + t - start)) : (int)(pos0 + t);
-      table[j] = cos_sin(at, __ldg(p.inv_freq + f), p.factor);
+  if (ROTARY) {
+    const int t_first = (int)(span.first - span.pos0), t_count = (int)(span.last - span.first);
+    for (int j = tid; j < t_count * p.pairs; j += kThreads) {
+      const int t = t_first + j / p.pairs, f = j % p.pairs;
+      const int at = p.positions ? __ldg(p.positions + (size_t)b * p.N + span.index(t)) : (int)(span.pos0 + t);
+      table[t * p.pairs + f] = cos_sin(at, __ldg(p.inv_freq + f), p.factor);
     }
     __syncthreads();
   }
-  const bool whole = last - first == kTok;
+  bool lost = false;
   const int h_end = min((int)(blockIdx.z + 1) * p.heads_per_block, p.cache.kv_heads);
   for (int h = blockIdx.z * p.heads_per_block; h < h_end; ++h) {
-    if (mine) {
-      const T* krow = p.k.row(b, h, i);
-      float x[16], y[16];
-      load16(krow + blk * 16, p.vector, x);
-      load16(p.v.row(b, h, i) + blk * 16, p.vector, y);
-      if (p.pairs) rotate16<T, D>(krow, blk * 16, p.vector, p.interleaved, p.pairs, table + tok * p.pairs, x);
-      const float kG = __ldg(p.cache.k_G + h), vG = __ldg(p.cache.v_G + h);
-      if (L::kFp4) {
-        uint32_t ks, vs;
-        const uint2 kc = nvfp4_block(x, kG, &ks), vc = nvfp4_block(y, vG, &vs);
-        *reinterpret_cast<uint2*>(sk + ((blk >> 1) * kTok + tok) * 16 + (blk & 1) * 8) = kc;
-        sks[tok * L::kScales + blk] = (uint8_t)ks;
-        svs[blk * kTok + v_scale_place(tok)] = (uint8_t)vs;
+    if (tid < kHalf) {
+      // ---- V: eight elements of sixteen tokens
+      constexpr int kLanes = D / 8, kRows = L::kFp4 ? 4 : 8;        // chunks of a thread
+      const int t0 = tid / kLanes * 16, e8 = tid % kLanes;
+      if (span.pos0 + t0 >= span.last || span.pos0 + t0 + 16 <= span.first) continue;
+      const int page = p.cache.page_of(b, span.pos0 + t0);          // a page holds whole sixteens
+      lost |= page < 0;
+      if (page < 0) continue;
+      const float G = __ldg(p.cache.v_G + h);
+      uint32_t rows[kRows][4], sc[4] = {0u, 0u, 0u, 0u};
+      uint32_t have = 0;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) sv[(blk * 8 + r) * kTok + tok] = (uint8_t)((r < 4 ? vc.x : vc.y) >> (8 * (r & 3)));
+      for (int q = 0; q < 4; ++q) {
+        uint4 raw[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int t = t0 + 4 * q + y;
+          raw[y] = make_uint4(0u, 0u, 0u, 0u);
+          if (span.has(t)) {
+            raw[y] = load8(p.v.row(b, h, span.index(t)) + 8 * e8, p.vector);
+            have |= 1u << (4 * q + y);
+          }
+        }
+        uint32_t lo[4], hi[4];                                      // codes of the four tokens; E4M3: of elements 0-3 and 4-7
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          float v[8];
+          unpack8<T>(raw[y], v);
+          float a = clean_max<8>(v);
+          if (L::kFp4) {
+            a = fmaxf(a, __shfl_xor_sync(3u << (tid & 30), a, 1));
+            uint32_t byte;
+            const float r = nvfp4_scale(a, G, &byte);
+#pragma unroll
+            for (int z = 0; z < 8; ++z) v[z] = __fmul_rn(v[z], r);
+            lo[y] = cvt_e2m1x8(v);
+            const int at = v_scale_place(4 * q + y);
+            sc[at >> 2] |= byte << (8 * (at & 3));
+          } else {
+            lo[y] = e4m3x4(v, G);
+            hi[y] = e4m3x4(v + 4, G);
+          }
+        }
+        transpose_bytes(lo);
+        if (!L::kFp4) transpose_bytes(hi);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          rows[y][q] = lo[y];
+          if (!L::kFp4) rows[kRows - 4 + y][q] = hi[y];
+        }
+      }
+      uint8_t* const rec = p.cache.rec(page, h);
+      const int in_page = (int)((span.pos0 + t0) & (P - 1));
+      uint8_t* const chunks = rec + L::v_codes(P) + in_page * L::kRow + kRows * e8 * 16;
+      uint8_t* const scales = rec + L::v_scales(P) + (e8 >> 1) * P + in_page;
+      if (have == 0xFFFFu) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) *reinterpret_cast<uint4*>(chunks + 16 * r) = make_uint4(rows[r][0], rows[r][1], rows[r][2], rows[r][3]);
+        if (L::kFp4 && !(e8 & 1)) *reinterpret_cast<uint4*>(scales) = make_uint4(sc[0], sc[1], sc[2], sc[3]);
       } else {
-        *reinterpret_cast<uint4*>(sk + (blk * kTok + tok) * 16) = e4m3_block(x, kG);
-        const uint4 vc = e4m3_block(y, vG);
-        const uint32_t w[4] = {vc.x, vc.y, vc.z, vc.w};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sv[(blk * 16 + r) * kTok + tok] = (uint8_t)(w[r >> 2] >> (8 * (r & 3)));
+        for (int t = 0; t < 16; ++t) {
+          if (!(have >> t & 1)) continue;
+#pragma unroll
+          for (int r = 0; r < kRows; ++r) chunks[16 * r + t] = (uint8_t)(rows[r][t >> 2] >> (8 * (t & 3)));
+          const int at = v_scale_place(t);
+          if (L::kFp4 && !(e8 & 1)) scales[at] = (uint8_t)(sc[at >> 2] >> (8 * (at & 3)));
+        }
       }
-    }
-    __syncthreads();
-    uint8_t* const rec = p.cache.rec(page, h);
-    // K: a token's 16-byte chunks
-    for (int j = tid; j < kTok * L::kRow / 16; j += D) {
-      const int c = j >> 4, t = j & 15;
-      if (whole || (pos0 + t >= first && pos0 + t < last))
-        *reinterpret_cast<uint4*>(rec + (c * P + t0 + t) * 16) = *reinterpret_cast<const uint4*>(sk + j * 16);
-    }
-    uint8_t* const vrec = rec + L::v_codes(P) + t0 * L::kRow;
-    if (whole) {
-      for (int j = tid; j < L::kRow; j += D) *reinterpret_cast<uint4*>(vrec + j * 16) = *reinterpret_cast<const uint4*>(sv + j * 16);
-      if (L::kFp4 && tid < L::kScales)                             // K: sixteen rows of scales in a run; V: a run of sixteen per block
-        *reinterpret_cast<uint4*>(rec + L::k_scales(P) + t0 * L::kScales + tid * 16) = *reinterpret_cast<const uint4*>(sks + tid * 16);
-      else if (L::kFp4 && tid < 2 * L::kScales)
-        *reinterpret_cast<uint4*>(rec + L::v_scales(P) + (tid - L::kScales) * P + t0) = *reinterpret_cast<const uint4*>(svs + (tid - L::kScales) * 16);
     } else {
-      for (int j = tid; j < kTok * L::kRow; j += D) {
-        const int t = j & 15;
-        if (pos0 + t >= first && pos0 + t < last) vrec[j] = sv[j];
-      }
-      if (L::kFp4 && mine) {
-        rec[L::k_scales(P) + (t0 + tok) * L::kScales + blk] = sks[tok * L::kScales + blk];
-        rec[L::v_scales(P) + blk * P + t0 + v_scale_place(tok)] = svs[blk * kTok + v_scale_place(tok)];
+      // ---- K: sixteen elements of a token at a time
+      constexpr int kParts = D / 16, kPieces = kBlockTokens<D> * kParts / kHalf, kAtOnce = ROTARY ? 2 : 4;
+      const float G = __ldg(p.cache.k_G + h);
+#pragma unroll 1
+      for (int q0 = 0; q0 < kPieces; q0 += kAtOnce) {
+        uint4 raw[kAtOnce][2];
+        int page[kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+          const int j = (q0 + q) * kHalf + tid - kHalf, t = j / kParts, part = j % kParts;
+          page[q] = -1;
+          if (!span.has(t)) continue;
+          const T* const x = p.k.row(b, h, span.index(t)) + 16 * part;
+          raw[q][0] = load8(x, p.vector);
+          raw[q][1] = load8(x + 8, p.vector);
+          page[q] = p.cache.page_of(b, span.pos0 + t);
+          lost |= page[q] < 0;
+        }
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+          if (page[q] < 0) continue;
+          const int j = (q0 + q) * kHalf + tid - kHalf, t = j / kParts, part = j % kParts;
+          float v[16];
+          unpack8<T>(raw[q][0], v);
+          unpack8<T>(raw[q][1], v + 8);
+          if (ROTARY) rotate16<T, D>(p.k.row(b, h, span.index(t)), 16 * part, p.vector, p.interleaved, p.pairs, table + t * p.pairs, v);
+          const float a = clean_max<16>(v);
+          uint8_t* const rec = p.cache.rec(page[q], h);
+          const int in_page = (int)((span.pos0 + t) & (P - 1));
+          if (L::kFp4) {
+            uint32_t byte;
+            const float r = nvfp4_scale(a, G, &byte);
+#pragma unroll
+            for (int z = 0; z < 16; ++z) v[z] = __fmul_rn(v[z], r);
+            *reinterpret_cast<uint2*>(rec + ((part >> 1) * P + in_page) * 16 + (part & 1) * 8) = make_uint2(cvt_e2m1x8(v), cvt_e2m1x8(v + 8));
+            rec[L::k_scales(P) + in_page * L::kScales + part] = (uint8_t)byte;
+          } else {
+            *reinterpret_cast<uint4*>(rec + (part * P + in_page) * 16) = make_uint4(e4m3x4(v, G), e4m3x4(v + 4, G), e4m3x4(v + 8, G), e4m3x4(v + 12, G));
+          }
+        }
       }
     }
-    __syncthreads();
   }
+  if (lost && p.status) *p.status = FP4ATTN_ERR_PAGE;
 }
 
 template <typename T>
@@ -193,127 +285,150 @@ struct ReadParams {
   CacheRef cache;
   const int *start, *count;
   int* status;
-  int B, N, groups, heads_per_block;
+  int B, N;
   bool vector;
 };
 
+// eight values, of eight E2M1 codes and their scale or of eight E4M3 bytes: code * scale is exact in f16
 template <typename T>
-__device__ __forceinline__ void store16(T* y, bool vector, const float* v) {
-  if (vector) {
-    uint32_t w[8];
+__device__ __forceinline__ uint4 values_e2m1(uint32_t codes, uint32_t scale_splat, float r) {
+  uint32_t h[4], w[4];
+  cvt_f16x2_e2m1x8(codes, h);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = pack_pair<T>(v[2 * i], v[2 * i + 1]);
-    *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
-    *(reinterpret_cast<uint4*>(y) + 1) = make_uint4(w[4], w[5], w[6], w[7]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] = from_float<T>(v[i]);
+  for (int i = 0; i < 4; ++i) {
+    const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&scale_splat));
+    const float2 f = __half22float2(x);
+    w[i] = pack_pair<T>(f.x * r, f.y * r);
   }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void e4m3x16_values(uint4 raw, float scale, float* v) {
-  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+template <typename T>
+__device__ __forceinline__ uint4 values_e4m3(uint32_t lo, uint32_t hi, float r) {
+  uint32_t h[4], w[4];
+  cvt_f16x2_e4m3x4(lo, h);
+  cvt_f16x2_e4m3x4(hi, h + 2);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float2 f = half2_of(cvt_f16x2_e4m3x2(w[i >> 1] >> (16 * (i & 1)) & 0xFFFFu));
-    v[2 * i] = f.x * scale;
-    v[2 * i + 1] = f.y * scale;
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = half2_of(h[i]);
+    w[i] = pack_pair<T>(f.x * r, f.y * r);
   }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ uint32_t e4m3_splat(uint32_t byte) { return cvt_f16x2_e4m3x2(byte * 0x0101u); }
 
 // As cache_write_kernel.  A value is code * scale (exact) * fl(1 / G), rounded once more to T: two units in the last place of
 // fp32 beside the quotient by G, which would take as long as reading the cache.
 template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(D) cache_read_kernel(const ReadParams<T> p) {
+__global__ void __launch_bounds__(kThreads, 8) cache_read_kernel(const ReadParams<T> p) {
   using L = RecordLayout<FMT, D>;
-  __shared__ alignas(16) uint8_t sv[kTok * L::kRow], svs[kTok * (L::kScales + 1)];
   launch_dependents();
   wait_prior_grids();
-  const int b = blockIdx.y, tid = threadIdx.x, tok = tid & 15, blk = tid >> 4;
-  const int start = __ldg(p.start + b), n = p.count ? max(0, min(__ldg(p.count + b), p.N)) : p.N;
-  const long long pos0 = ((long long)(start >> 4) + blockIdx.x) << 4;
-  const long long first = max((long long)start, pos0), last = min((long long)start + n, pos0 + kTok);
-  if (first >= last) return;
+  const int b = blockIdx.y, h = blockIdx.z, tid = threadIdx.x;
+  const Span<D> span(p.start, p.count, p.N, b);
+  if (span.first >= span.last) return;
   const int P = 1 << p.cache.log_page;
-  const long long pos = pos0 + tok;
-  const bool mine = pos >= first && pos < last;
-  const int page = p.cache.page_of(b, pos0);
-  if (page < 0 && tid == 0 && blockIdx.z == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
-  const int t0 = (int)(pos0 & (P - 1)), i = (int)(pos - start);
-  const int h_end = min((int)(blockIdx.z + 1) * p.heads_per_block, p.cache.kv_heads);
-  for (int h = blockIdx.z * p.heads_per_block; h < h_end; ++h) {
-    float x[16], y[16];
+  constexpr int kLanes = D / 8;
+  bool lost = false;
+  if (tid < kHalf) {
+    // ---- V: eight elements of sixteen tokens
+    constexpr int kRows = L::kFp4 ? 4 : 8;
+    const int t0 = tid / kLanes * 16, e8 = tid % kLanes;
+    if (span.pos0 + t0 < span.last && span.pos0 + t0 + 16 > span.first) {
+      const int page = p.cache.page_of(b, span.pos0 + t0);
+      lost |= page < 0;
+      uint32_t rows[kRows][4], sc[4] = {0u, 0u, 0u, 0u};
+      if (page >= 0) {
+        const uint8_t* const rec = p.cache.rec(page, h);
+        const int in_page = (int)((span.pos0 + t0) & (P - 1));
+        const uint4* const chunks = reinterpret_cast<const uint4*>(rec + L::v_codes(P) + in_page * L::kRow + kRows * e8 * 16);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = y[r] = 0.f;                // no page: zeros
-    if (page >= 0) {
-      const uint8_t* const rec = p.cache.rec(page, h);
-      const uint8_t* const vrec = rec + L::v_codes(P) + t0 * L::kRow;
-      const float kr = __fdiv_rn(1.f, __ldg(p.cache.k_G + h)), vr = __fdiv_rn(1.f, __ldg(p.cache.v_G + h));
-      __syncthreads();                                             // the head before is out of shared memory
-      for (int j = tid; j < L::kRow; j += D) *reinterpret_cast<uint4*>(sv + j * 16) = __ldg(reinterpret_cast<const uint4*>(vrec) + j);
-      if (L::kFp4 && tid < L::kScales)
-        *reinterpret_cast<uint4*>(svs + tid * 16) = __ldg(reinterpret_cast<const uint4*>(rec + L::v_scales(P) + tid * P + t0));
-      if (L::kFp4) {
-        const uint2 kc = __ldg(reinterpret_cast<const uint2*>(rec + ((blk >> 1) * P + t0 + tok) * 16 + (blk & 1) * 8));
-        const float ks = e4m3_value(__ldg(rec + L::k_scales(P) + (t0 + tok) * L::kScales + blk));
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const uint32_t c = w ? kc.y : kc.x;
-          const float2 f0 = half2_of(cvt_f16x2_e2m1x2<0>(c)), f1 = half2_of(cvt_f16x2_e2m1x2<1>(c));
-          const float2 f2 = half2_of(cvt_f16x2_e2m1x2<2>(c)), f3 = half2_of(cvt_f16x2_e2m1x2<3>(c));
-          const float e[8] = {f0.x, f0.y, f1.x, f1.y, f2.x, f2.y, f3.x, f3.y};
-#pragma unroll
-          for (int r = 0; r < 8; ++r) x[8 * w + r] = e[r] * ks * kr;
+        for (int r = 0; r < kRows; ++r) {
+          const uint4 w = __ldg(chunks + r);
+          rows[r][0] = w.x; rows[r][1] = w.y; rows[r][2] = w.z; rows[r][3] = w.w;
+        }
+        if (L::kFp4) {
+          const uint4 w = __ldg(reinterpret_cast<const uint4*>(rec + L::v_scales(P) + (e8 >> 1) * P + in_page));
+          sc[0] = w.x; sc[1] = w.y; sc[2] = w.z; sc[3] = w.w;
         }
       } else {
-        e4m3x16_values(__ldg(reinterpret_cast<const uint4*>(rec + (blk * P + t0 + tok) * 16)), kr, x);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) rows[r][0] = rows[r][1] = rows[r][2] = rows[r][3] = 0u;
       }
-      __syncthreads();
-      if (L::kFp4) {
-        const float vs = e4m3_value(svs[blk * kTok + v_scale_place(tok)]);
+      const float r = __fdiv_rn(1.f, __ldg(p.cache.v_G + h));
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const float2 f = half2_of(cvt_f16x2_e2m1x2<0>(sv[(blk * 8 + r) * kTok + tok]));
-          y[2 * r] = f.x * vs * vr;
-          y[2 * r + 1] = f.y * vs * vr;
+      for (int q = 0; q < 4; ++q) {
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          lo[y] = rows[y][q];
+          hi[y] = rows[kRows - 4 + y][q];
         }
-      } else {
+        transpose_bytes(lo);
+        if (!L::kFp4) transpose_bytes(hi);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) y[r] = e4m3_value(sv[(blk * 16 + r) * kTok + tok]) * vr;
+        for (int y = 0; y < 4; ++y) {
+          const int t = t0 + 4 * q + y, at = v_scale_place(4 * q + y);
+          if (!span.has(t)) continue;
+          const uint4 out = L::kFp4 ? values_e2m1<T>(lo[y], e4m3_splat(sc[at >> 2] >> (8 * (at & 3)) & 0xFFu), r) : values_e4m3<T>(lo[y], hi[y], r);
+          store8(p.v.row(b, h, span.index(t)) + 8 * e8, p.vector, out);
+        }
       }
     }
-    if (mine) {
-      store16(p.k.row(b, h, i) + blk * 16, p.vector, x);
-      store16(p.v.row(b, h, i) + blk * 16, p.vector, y);
+  } else {
+    // ---- K: eight elements of a token at a time
+    constexpr int kPieces = kBlockTokens<D> * kLanes / kHalf, kAtOnce = 8;
+    const float r = __fdiv_rn(1.f, __ldg(p.cache.k_G + h));
+#pragma unroll 1
+    for (int q0 = 0; q0 < kPieces; q0 += kAtOnce) {
+      uint2 raw[kAtOnce];                                           // NVFP4: codes and the scale's byte
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        const int j = (q0 + q) * kHalf + tid - kHalf, t = j / kLanes, e8 = j % kLanes;
+        raw[q] = make_uint2(0u, 0u);
+        if (!span.has(t)) continue;
+        const int page = p.cache.page_of(b, span.pos0 + t);
+        lost |= page < 0;
+        if (page < 0) continue;                                     // zeros
+        const uint8_t* const rec = p.cache.rec(page, h);
+        const int in_page = (int)((span.pos0 + t) & (P - 1));
+        if (L::kFp4) {
+          raw[q].x = __ldg(reinterpret_cast<const uint32_t*>(rec + ((e8 >> 2) * P + in_page) * 16 + (e8 & 3) * 4));
+          raw[q].y = __ldg(rec + L::k_scales(P) + in_page * L::kScales + (e8 >> 1));
+        } else {
+          raw[q] = __ldg(reinterpret_cast<const uint2*>(rec + ((e8 >> 1) * P + in_page) * 16 + (e8 & 1) * 8));
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        const int j = (q0 + q) * kHalf + tid - kHalf, t = j / kLanes, e8 = j % kLanes;
+        if (!span.has(t)) continue;
+        const uint4 out = L::kFp4 ? values_e2m1<T>(raw[q].x, e4m3_splat(raw[q].y), r) : values_e4m3<T>(raw[q].x, raw[q].y, r);
+        store8(p.k.row(b, h, span.index(t)) + 8 * e8, p.vector, out);
+      }
     }
   }
-}
-
-// grid of either kernel; false where the device does not tell its size
-bool cover(int B, int N, int kv_heads, dim3* grid, int* heads_per_block) {
-  const int sms = device_sms();
-  if (!sms) return false;
-  const int groups = (N + 14) / kTok + 1;                          // N tokens touch at most so many aligned sixteens
-  // heads of a block: as many as leave eight blocks an SM
-  long long per = (long long)groups * B * kv_heads / (8ll * sms);
-  if (per < 1) per = 1;
-  if (per > kv_heads) per = kv_heads;
-  *heads_per_block = (int)per;
-  *grid = dim3((unsigned)groups, (unsigned)B, (unsigned)((kv_heads + per - 1) / per));
-  return true;
+  if (lost && p.status) *p.status = FP4ATTN_ERR_PAGE;
 }
 
 template <typename T, int FMT, int D>
 int launch_write(WriteParams<T> p, cudaStream_t st) {
-  dim3 grid;
-  if (!cover(p.B, p.N, p.cache.kv_heads, &grid, &p.heads_per_block)) return FP4ATTN_ERR_CUDA;
-  const cudaError_t e = launch_overlapped(cache_write_kernel<T, FMT, D>, grid, D, sizeof(float2) * kTok * p.pairs, st, p);
+  const int sms = device_sms(), blocks = (int)(((long long)p.N + kBlockTokens<D> - 2) / kBlockTokens<D> + 1);    // N tokens touch at most so many
+  if (!sms) return FP4ATTN_ERR_CUDA;
+  // Heads of a block: one - its loads then wait for nothing but each other -, or where they share the cosines and sines of their tokens as
+  // many as leave four blocks an SM
+  long long per = p.pairs ? (long long)blocks * p.B * p.cache.kv_heads / (4ll * sms) : 1;
+  if (per < 1) per = 1;
+  if (per > p.cache.kv_heads) per = p.cache.kv_heads;
+  p.heads_per_block = (int)per;
+  const dim3 grid((unsigned)blocks, (unsigned)p.B, (unsigned)((p.cache.kv_heads + per - 1) / per));
+  const cudaError_t e = p.pairs ? launch_overlapped(cache_write_kernel<T, FMT, D, true>, grid, kThreads, sizeof(float2) * kBlockTokens<D> * p.pairs, st, p)
+                                : launch_overlapped(cache_write_kernel<T, FMT, D, false>, grid, kThreads, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
 template <typename T, int FMT, int D>
 int launch_read(ReadParams<T> p, cudaStream_t st) {
-  dim3 grid;
-  if (!cover(p.B, p.N, p.cache.kv_heads, &grid, &p.heads_per_block)) return FP4ATTN_ERR_CUDA;
-  const cudaError_t e = launch_overlapped(cache_read_kernel<T, FMT, D>, grid, D, 0, st, p);
+  const int blocks = (int)(((long long)p.N + kBlockTokens<D> - 2) / kBlockTokens<D> + 1);
+  const cudaError_t e = launch_overlapped(cache_read_kernel<T, FMT, D>, dim3((unsigned)blocks, (unsigned)p.B, (unsigned)p.cache.kv_heads), kThreads, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
 
