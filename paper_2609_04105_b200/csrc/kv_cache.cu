@@ -1,19 +1,19 @@
 // Quantizing K and V into the pages of a cache, and reading them back.
 //
 // Both are bound by HBM: 2 bytes an element on the 16-bit side, 9/16 or 1 in the cache.  A block takes some tokens of one KV head, half
-// of its threads K and half V, 128 elements a thread; nothing goes through shared memory and no thread waits for another block's work.
+// of its threads K and half V, 64 elements a thread (128: too few threads, 29 us for the write and 43 us for the read below); nothing goes through shared memory and no thread waits for another block's work.
 //   K  is kept token by token: a thread takes sixteen elements of one token (an NVFP4 block) to write, eight to read.
-//   V  is kept in chunks of sixteen tokens at one pair of elements (E4M3: one element): a thread takes eight elements of the sixteen tokens of
-//      such chunks and turns bytes around in registers, so that both sides are accessed 16 bytes at a time, neighbouring lanes at
-//      neighbouring addresses.  Where a call's tokens do not fill a sixteen, V's bytes are written one by one: the others belong to tokens
-//      that are there already.
+//   V  is kept in chunks of sixteen tokens at one pair of elements (E4M3: one element): a thread takes eight elements of eight tokens, half of
+//      such chunks, and turns bytes around in registers, so that the 16-bit side is accessed 16 bytes and the cache 8 bytes at a time, neighbouring
+//      lanes at neighbouring addresses.  Where a call's tokens do not fill an eight, V's bytes are written one by one: the others belong to
+//      tokens that are there already.
 #include "kv_cache.cuh"
 
 namespace fp4attn {
 namespace {
 
 constexpr int kThreads = 128, kHalf = 64;
-template <int D> constexpr int kBlockTokens = 8192 / D;           // 64 threads of 128 elements
+template <int D> constexpr int kBlockTokens = 4096 / D;           // 64 threads of 64 elements
 
 template <typename T>
 struct WriteParams {
@@ -140,9 +140,10 @@ struct Span {
   __device__ __forceinline__ int index(int tok) const { return (int)(pos0 + tok - start); }
 };
 
-// Grid: blocks of the sequence, batch, head ranges.
-template <typename T, int FMT, int D, bool ROTARY>
-__global__ void __launch_bounds__(kThreads, ROTARY ? 4 : 5) cache_write_kernel(const WriteParams<T> p) {
+// Grid: blocks of the sequence, batch, head ranges.  GENERAL: with rotary positions, or rows that take no 16-byte accesses (an instance of
+// its own: either costs the plain one registers that it does not have).
+template <typename T, int FMT, int D, bool GENERAL>
+__global__ void __launch_bounds__(kThreads, GENERAL ? 4 : 6) cache_write_kernel(const WriteParams<T> p) {
   using L = RecordLayout<FMT, D>;
   extern __shared__ float2 table[];                               // [tokens][pairs]: cosines and sines
   launch_dependents();
@@ -151,7 +152,8 @@ __global__ void __launch_bounds__(kThreads, ROTARY ? 4 : 5) cache_write_kernel(c
   const Span<D> span(p.start, p.count, p.N, b);
   if (span.first >= span.last) return;
   const int P = 1 << p.cache.log_page;
-  if (ROTARY) {
+  const bool vector = GENERAL ? p.vector : true;
+  if (GENERAL && p.pairs) {
     const int t_first = (int)(span.first - span.pos0), t_count = (int)(span.last - span.first);
     for (int j = tid; j < t_count * p.pairs; j += kThreads) {
       const int t = t_first + j / p.pairs, f = j % p.pairs;
@@ -164,25 +166,25 @@ __global__ void __launch_bounds__(kThreads, ROTARY ? 4 : 5) cache_write_kernel(c
   const int h_end = min((int)(blockIdx.z + 1) * p.heads_per_block, p.cache.kv_heads);
   for (int h = blockIdx.z * p.heads_per_block; h < h_end; ++h) {
     if (tid < kHalf) {
-      // ---- V: eight elements of sixteen tokens
-      constexpr int kLanes = D / 8, kRows = L::kFp4 ? 4 : 8;        // chunks of a thread
-      const int t0 = tid / kLanes * 16, e8 = tid % kLanes;
-      if (span.pos0 + t0 >= span.last || span.pos0 + t0 + 16 <= span.first) continue;
-      const int page = p.cache.page_of(b, span.pos0 + t0);          // a page holds whole sixteens
+      // ---- V: eight elements of eight tokens
+      constexpr int kLanes = D / 8, kRows = L::kFp4 ? 4 : 8;        // chunks of a thread, half of each
+      const int t0 = tid / kLanes * 8, e8 = tid % kLanes;
+      if (span.pos0 + t0 >= span.last || span.pos0 + t0 + 8 <= span.first) continue;
+      const int page = p.cache.page_of(b, span.pos0 + t0);          // a page holds whole eights
       lost |= page < 0;
       if (page < 0) continue;
       const float G = __ldg(p.cache.v_G + h);
-      uint32_t rows[kRows][4], sc[4] = {0u, 0u, 0u, 0u};
+      uint32_t rows[kRows][2], sc[2] = {0u, 0u};
       uint32_t have = 0;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < 2; ++q) {
         uint4 raw[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const int t = t0 + 4 * q + y;
           raw[y] = make_uint4(0u, 0u, 0u, 0u);
           if (span.has(t)) {
-            raw[y] = load8(p.v.row(b, h, span.index(t)) + 8 * e8, p.vector);
+            raw[y] = load8(p.v.row(b, h, span.index(t)) + 8 * e8, vector);
             have |= 1u << (4 * q + y);
           }
         }
@@ -216,15 +218,15 @@ __global__ void __launch_bounds__(kThreads, ROTARY ? 4 : 5) cache_write_kernel(c
       }
       uint8_t* const rec = p.cache.rec(page, h);
       const int in_page = (int)((span.pos0 + t0) & (P - 1));
-      uint8_t* const chunks = rec + L::v_codes(P) + in_page * L::kRow + kRows * e8 * 16;
+      uint8_t* const chunks = rec + L::v_codes(P) + (in_page & ~15) * L::kRow + kRows * e8 * 16 + (in_page & 8);
       uint8_t* const scales = rec + L::v_scales(P) + (e8 >> 1) * P + in_page;
-      if (have == 0xFFFFu) {
+      if (have == 0xFFu) {
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) *reinterpret_cast<uint4*>(chunks + 16 * r) = make_uint4(rows[r][0], rows[r][1], rows[r][2], rows[r][3]);
-        if (L::kFp4 && !(e8 & 1)) *reinterpret_cast<uint4*>(scales) = make_uint4(sc[0], sc[1], sc[2], sc[3]);
+        for (int r = 0; r < kRows; ++r) *reinterpret_cast<uint2*>(chunks + 16 * r) = make_uint2(rows[r][0], rows[r][1]);
+        if (L::kFp4 && !(e8 & 1)) *reinterpret_cast<uint2*>(scales) = make_uint2(sc[0], sc[1]);
       } else {
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
+        for (int t = 0; t < 8; ++t) {
           if (!(have >> t & 1)) continue;
 #pragma unroll
           for (int r = 0; r < kRows; ++r) chunks[16 * r + t] = (uint8_t)(rows[r][t >> 2] >> (8 * (t & 3)));
@@ -234,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, ROTARY ? 4 : 5) cache_write_kernel(c
       }
     } else {
       // ---- K: sixteen elements of a token at a time
-      constexpr int kParts = D / 16, kPieces = kBlockTokens<D> * kParts / kHalf, kAtOnce = ROTARY ? 2 : 4;
+      constexpr int kParts = D / 16, kPieces = kBlockTokens<D> * kParts / kHalf, kAtOnce = 2;
       const float G = __ldg(p.cache.k_G + h);
 #pragma unroll 1
       for (int q0 = 0; q0 < kPieces; q0 += kAtOnce) {
@@ -246,8 +248,8 @@ __global__ void __launch_bounds__(kThreads, ROTARY ? 4 : 5) cache_write_kernel(c
           page[q] = -1;
           if (!span.has(t)) continue;
           const T* const x = p.k.row(b, h, span.index(t)) + 16 * part;
-          raw[q][0] = load8(x, p.vector);
-          raw[q][1] = load8(x + 8, p.vector);
+          raw[q][0] = load8(x, vector);
+          raw[q][1] = load8(x + 8, vector);
           page[q] = p.cache.page_of(b, span.pos0 + t);
           lost |= page[q] < 0;
         }
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, ROTARY ? 4 : 5) cache_write_kernel(c
           float v[16];
           unpack8<T>(raw[q][0], v);
           unpack8<T>(raw[q][1], v + 8);
-          if (ROTARY) rotate16<T, D>(p.k.row(b, h, span.index(t)), 16 * part, p.vector, p.interleaved, p.pairs, table + t * p.pairs, v);
+          if (GENERAL && p.pairs) rotate16<T, D>(p.k.row(b, h, span.index(t)), 16 * part, vector, p.interleaved, p.pairs, table + t * p.pairs, v);
           const float a = clean_max<16>(v);
           uint8_t* const rec = p.cache.rec(page[q], h);
           const int in_page = (int)((span.pos0 + t) & (P - 1));
@@ -330,38 +332,31 @@ __global__ void __launch_bounds__(kThreads, 8) cache_read_kernel(const ReadParam
   constexpr int kLanes = D / 8;
   bool lost = false;
   if (tid < kHalf) {
-    // ---- V: eight elements of sixteen tokens
+    // ---- V: eight elements of eight tokens
     constexpr int kRows = L::kFp4 ? 4 : 8;
-    const int t0 = tid / kLanes * 16, e8 = tid % kLanes;
-    if (span.pos0 + t0 < span.last && span.pos0 + t0 + 16 > span.first) {
+    const int t0 = tid / kLanes * 8, e8 = tid % kLanes;
+    if (span.pos0 + t0 < span.last && span.pos0 + t0 + 8 > span.first) {
       const int page = p.cache.page_of(b, span.pos0 + t0);
       lost |= page < 0;
-      uint32_t rows[kRows][4], sc[4] = {0u, 0u, 0u, 0u};
+      uint2 rows[kRows], sc = make_uint2(0u, 0u);
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) rows[r] = make_uint2(0u, 0u);
       if (page >= 0) {
         const uint8_t* const rec = p.cache.rec(page, h);
         const int in_page = (int)((span.pos0 + t0) & (P - 1));
-        const uint4* const chunks = reinterpret_cast<const uint4*>(rec + L::v_codes(P) + in_page * L::kRow + kRows * e8 * 16);
+        const uint8_t* const chunks = rec + L::v_codes(P) + (in_page & ~15) * L::kRow + kRows * e8 * 16 + (in_page & 8);
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          const uint4 w = __ldg(chunks + r);
-          rows[r][0] = w.x; rows[r][1] = w.y; rows[r][2] = w.z; rows[r][3] = w.w;
-        }
-        if (L::kFp4) {
-          const uint4 w = __ldg(reinterpret_cast<const uint4*>(rec + L::v_scales(P) + (e8 >> 1) * P + in_page));
-          sc[0] = w.x; sc[1] = w.y; sc[2] = w.z; sc[3] = w.w;
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) rows[r][0] = rows[r][1] = rows[r][2] = rows[r][3] = 0u;
+        for (int r = 0; r < kRows; ++r) rows[r] = __ldg(reinterpret_cast<const uint2*>(chunks + 16 * r));
+        if (L::kFp4) sc = __ldg(reinterpret_cast<const uint2*>(rec + L::v_scales(P) + (e8 >> 1) * P + in_page));
       }
       const float r = __fdiv_rn(1.f, __ldg(p.cache.v_G + h));
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < 2; ++q) {
         uint32_t lo[4], hi[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-          lo[y] = rows[y][q];
-          hi[y] = rows[kRows - 4 + y][q];
+          lo[y] = q ? rows[y].y : rows[y].x;
+          hi[y] = q ? rows[kRows - 4 + y].y : rows[kRows - 4 + y].x;
         }
         transpose_bytes(lo);
         if (!L::kFp4) transpose_bytes(hi);
@@ -369,7 +364,8 @@ __global__ void __launch_bounds__(kThreads, 8) cache_read_kernel(const ReadParam
         for (int y = 0; y < 4; ++y) {
           const int t = t0 + 4 * q + y, at = v_scale_place(4 * q + y);
           if (!span.has(t)) continue;
-          const uint4 out = L::kFp4 ? values_e2m1<T>(lo[y], e4m3_splat(sc[at >> 2] >> (8 * (at & 3)) & 0xFFu), r) : values_e4m3<T>(lo[y], hi[y], r);
+          const uint4 out = L::kFp4 ? values_e2m1<T>(lo[y], e4m3_splat((at & 4 ? sc.y : sc.x) >> (8 * (at & 3)) & 0xFFu), r)
+                                    : values_e4m3<T>(lo[y], hi[y], r);
           store8(p.v.row(b, h, span.index(t)) + 8 * e8, p.vector, out);
         }
       }
@@ -421,8 +417,9 @@ int launch_write(WriteParams<T> p, cudaStream_t st) {
   if (per > p.cache.kv_heads) per = p.cache.kv_heads;
   p.heads_per_block = (int)per;
   const dim3 grid((unsigned)blocks, (unsigned)p.B, (unsigned)((p.cache.kv_heads + per - 1) / per));
-  const cudaError_t e = p.pairs ? launch_overlapped(cache_write_kernel<T, FMT, D, true>, grid, kThreads, sizeof(float2) * kBlockTokens<D> * p.pairs, st, p)
-                                : launch_overlapped(cache_write_kernel<T, FMT, D, false>, grid, kThreads, 0, st, p);
+  const cudaError_t e = p.pairs || !p.vector
+                            ? launch_overlapped(cache_write_kernel<T, FMT, D, true>, grid, kThreads, sizeof(float2) * kBlockTokens<D> * p.pairs, st, p)
+                            : launch_overlapped(cache_write_kernel<T, FMT, D, false>, grid, kThreads, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
 template <typename T, int FMT, int D>

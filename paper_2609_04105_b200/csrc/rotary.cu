@@ -84,15 +84,27 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams<T> 
     table[i] = cs;
   }
   __syncthreads();
+  // A thread keeps its unit and steps through the rows (heads of a token, token by token): no division per unit, which took as long as the
+  // rest (2 x 4096 tokens of 40 heads, d = 128: 38.6 us with three).
   const int units = VECTOR ? (INTERLEAVED ? p.d / V : (p.d - p.pairs) / V) : p.d - p.pairs;
   const int h0 = blockIdx.y * p.heads_per_block;
   const int n_heads = min(p.heads_per_block, p.heads[0] + p.heads[1] - h0);
-  for (int i = threadIdx.x; i < n_tok * n_heads * units; i += kThreads) {
-    const int u = i % units, r = i / units, hh = r % n_heads, t = r / n_heads;
-    const long long tok = first + t;
-    const int b = (int)(tok / p.N), n = (int)(tok - (long long)b * p.N), h = h0 + hh;
-    const int w = h >= p.heads[0], head = w ? h - p.heads[0] : h;
+  const int at_once = kThreads / units, u = threadIdx.x % units;   // rows of a pass (units: at most d, 256)
+  int hh = threadIdx.x / units, t = 0;
+  if (hh >= at_once) return;
+  int b = (int)(first / p.N), n = (int)(first - (long long)b * p.N);
+  for (;;) {
+    while (hh >= n_heads) {
+      hh -= n_heads;
+      if (++t >= n_tok) return;
+      if (++n == p.N) {
+        n = 0;
+        ++b;
+      }
+    }
+    const int h = h0 + hh, w = h >= p.heads[0], head = w ? h - p.heads[0] : h;
     rotary_unit<T, INTERLEAVED, VECTOR>(p.in[w].row(b, head, n), p.out[w].row(b, head, n), u, p.pairs, table + t * p.pairs);
+    hh += at_once;
   }
 }
 
@@ -115,9 +127,9 @@ int launch(const fp4attn_view* x, const fp4attn_view* y, int Hq, int Hk, int B, 
   if (!sms) return FP4ATTN_ERR_CUDA;
   const long long tokens = (long long)B * N;
   const int heads = Hq + Hk;
-  // up to eight tokens a block while that leaves four blocks an SM; heads split while there are fewer
-  long long per = tokens / (4ll * sms);
-  p.tokens_per_block = (int)(per < 1 ? 1 : per > 8 ? 8 : per);
+  // up to four tokens a block while that leaves eight blocks an SM; heads split while there are fewer
+  long long per = tokens / (8ll * sms);
+  p.tokens_per_block = (int)(per < 1 ? 1 : per > 4 ? 4 : per);
   const long long blocks = (tokens + p.tokens_per_block - 1) / p.tokens_per_block;
   long long split = blocks < 2ll * sms ? (2ll * sms + blocks - 1) / blocks : 1;
   if (split > heads) split = heads;
