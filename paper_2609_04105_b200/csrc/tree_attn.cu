@@ -261,56 +261,97 @@ __device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long lon
   return left >= 8 ? v : left > 0 ? v & ((1u << left) - 1) : 0u;
 }
 
+// floor(a * b / c), floor((a + 1) * b / c), ... of tile numbers: in 32 bits where they are enough (64-bit divisions took 0.5 us of the
+// smallest calls)
+__device__ __forceinline__ long long mul_div(long long a, long long b, long long c) {
+  const long long ab = a * b;
+  return ab < (1ll << 31) ? (long long)((uint32_t)ab / (uint32_t)c) : ab / c;
+}
 // This CTA's run of tiles: how many, and where it starts.  find: entry and place of the first tile, its number in the list, all tiles,
-// CTAs.  Two barriers of the block; everything that the block wrote to shared memory before is visible after it.
+// CTAs.  A barrier of the block (two for a batch of more than 32): everything that the block wrote to shared memory before is visible after it.
 template <int THREADS>
 __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0, long long* scan, long long* find) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int per = (p.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, b1 = min(p.B, b0 + per);
-  long long mine = 0;
   Walk w;
-#pragma unroll 1
-  for (w.b = b0; w.b < b1; ++w.b) mine += (long long)load_entry(w, p) * units;
-  long long incl = mine;
-#pragma unroll 1
-  for (int s = 1; s < 32; s <<= 1) {
-    const long long o = __shfl_up_sync(0xffffffffu, incl, s);
-    if (lane >= s) incl += o;
-  }
-  if (lane == 31) scan[warp] = incl;
-  __syncthreads();
-  long long before = 0, total = 0;
-#pragma unroll 1
-  for (int i = 0; i < THREADS / 32; ++i) {
-    if (i < warp) before += scan[i];
-    total += scan[i];
-  }
-  before += incl - mine;
-  const long long ctas = min((long long)gridDim.x, total);
-  const long long t0 = blockIdx.x < ctas ? blockIdx.x * total / ctas : total, t1 = blockIdx.x < ctas ? (blockIdx.x + 1) * total / ctas : total;
-  if (t0 < t1 && before <= t0 && t0 < before + mine) {              // one thread
-    for (w.b = b0;; ++w.b) {
-      const long long here = (long long)load_entry(w, p) * units;
-      if (t0 < before + here) break;
-      before += here;
+  long long t0, t1, total;
+  auto run = [&] {
+    const long long ctas = min((long long)gridDim.x, total);
+    t0 = blockIdx.x < ctas ? mul_div(blockIdx.x, total, ctas) : total;
+    t1 = blockIdx.x < ctas ? mul_div(blockIdx.x + 1, total, ctas) : total;
+    if (threadIdx.x == 0) {
+      find[2] = t0;
+      find[3] = total;
+      find[4] = ctas;
     }
-    find[0] = w.b;
-    find[1] = t0 - before;
+  };
+  long long at;                                                     // of the first tile among its entry's
+  if (p.B <= 32) {                                                  // every warp for itself
+    w.b = lane;
+    const int nt = lane < p.B ? load_entry(w, p) : 0;
+    const long long mine = (long long)nt * units;
+    long long incl = mine;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, incl, s);
+      if (lane >= s) incl += o;
+    }
+    total = __shfl_sync(0xffffffffu, incl, 31);
+    run();
+    const uint32_t behind = __ballot_sync(0xffffffffu, incl > t0);  // entries that end behind the first tile
+    const int b = t0 < t1 ? __ffs(behind) - 1 : 0;
+    w0.b = b;
+    w0.ctx = __shfl_sync(0xffffffffu, w.ctx, b);
+    w0.len = __shfl_sync(0xffffffffu, w.len, b);
+    w0.left = __shfl_sync(0xffffffffu, nt, b);
+    at = t0 < t1 ? t0 - __shfl_sync(0xffffffffu, incl - mine, b) : 0;
+    __syncthreads();
+  } else {
+    const int per = (p.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, b1 = min(p.B, b0 + per);
+    long long mine = 0;
+#pragma unroll 1
+    for (w.b = b0; w.b < b1; ++w.b) mine += (long long)load_entry(w, p) * units;
+    long long incl = mine;
+#pragma unroll 1
+    for (int s = 1; s < 32; s <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, incl, s);
+      if (lane >= s) incl += o;
+    }
+    if (lane == 31) scan[warp] = incl;
+    __syncthreads();
+    long long before = 0;
+    total = 0;
+#pragma unroll 1
+    for (int i = 0; i < THREADS / 32; ++i) {
+      if (i < warp) before += scan[i];
+      total += scan[i];
+    }
+    before += incl - mine;
+    run();
+    if (t0 < t1 && before <= t0 && t0 < before + mine) {            // one thread
+      for (w.b = b0;; ++w.b) {
+        const long long here = (long long)load_entry(w, p) * units;
+        if (t0 < before + here) break;
+        before += here;
+      }
+      find[0] = w.b;
+      find[1] = t0 - before;
+    }
+    __syncthreads();
+    w0.b = t0 < t1 ? (int)find[0] : 0;
+    w0.left = load_entry(w0, p);
+    at = t0 < t1 ? find[1] : 0;
   }
-  if (threadIdx.x == 0) {
-    find[2] = t0;
-    find[3] = total;
-    find[4] = ctas;
-  }
-  __syncthreads();
-  w0.b = t0 < t1 ? (int)find[0] : 0;
-  const int nt = load_entry(w0, p);
-  const long long r = t0 < t1 ? find[1] : 0;
-  w0.u = (int)(r / nt);
-  const int kt = (int)(r - (long long)w0.u * nt);
+  w0.u = (int)mul_div(at, 1, w0.left);
+  const int kt = (int)(at - (long long)w0.u * w0.left);
   w0.first = kt * kTile;
-  w0.left = nt - kt;
+  w0.left -= kt;
   return (int)min(t1 - t0, (long long)INT_MAX);
+}
+
+// the CTA that has a tile of the list
+__device__ __forceinline__ int cta_of(const long long* find, long long tile) {
+  const long long a = (tile + 1) * find[4] - 1;
+  return (int)(a < (1ll << 31) ? (uint32_t)a / (uint32_t)find[3] : a / find[3]);
 }
 
 // Brings the pages of tiles into a ring of stages, one bulk copy each; a whole warp.  RING: stages for which `valid` remembers which of the
@@ -400,12 +441,12 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     fence_proxy_async_smem();
   }
   tc_fence_before();
+  launch_dependents();                                              // the joining kernel: its launch lies under this one
   wait_prior_grids();
   Walk w0;
   long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
   const int n_tiles = find_run<C::kThreads>(p, units, w0, reinterpret_cast<long long*>(sgen + C::kOffScan), find);
   tc_fence_after();
-  auto cta_of = [&](long long tile) { return (int)(((tile + 1) * find[4] - 1) / find[3]); };
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
   uint32_t* const valid_ring = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
   const int P = 1 << p.cache.log_page;
@@ -886,7 +927,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
           for (int k = 0; k < C::kSets; ++k) factor_all[k * R + key] = f[k] * inv;
         }
         if (group == 0 && key == 0 && part_first == 0)
-          p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find[2] + i + w.left - 1));
+          p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find, find[2] + i + w.left - 1));
         bar_sync(id_all, 128 * C::kSets);
         tc_fence_after();
         // a set takes its share of the rows
@@ -932,7 +973,6 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
       advance(w, p, units);
     }
   }
-  launch_dependents();
   tc_fence_before();
   __syncthreads();
   if (*abort_word && threadIdx.x == 0 && p.status) *p.status = FP4ATTN_ERR_TIMEOUT;
@@ -1001,7 +1041,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
   const uint32_t full = sbase + C::kOffBar, free = full + 8 * C::kStages, abort_at = free + 8 * C::kStages;
   volatile uint32_t* const abort_word = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 16 * C::kStages);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const int units = p.cache.kv_heads;                              // one row tile
+  const int units = p.cache.kv_heads * p.row_tiles;
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
       mbar_init(full + 8 * s, 1);
@@ -1010,6 +1050,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
     *abort_word = 0;
     fence_barrier_init();
   }
+  launch_dependents();                                              // the joining kernel: its launch lies under this one
   wait_prior_grids();
   Walk w0;
   long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
@@ -1064,7 +1105,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
     Walk w = w0;
     Turn<C::kStages> ring;
     bool fresh = true;
-    int part_first = 0, b_of = -1, n_drafted = 0;
+    int part_first = 0, b_of = -1, n_drafted = 0, kvh = 0, row0 = 0;
     unsigned long long seen = 0;
     uint32_t qf[NT][kSteps][2];                                     // Q^T: rows 8n + lane / 4
     float con[NT][2], ref[NT][2], l[NT][2];                         // of rows 8n + 2c, + 1: score constant, kShift minus the reference, sum
@@ -1080,15 +1121,17 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
           seen = row_mask(p, w.b, lane, n_drafted) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n_drafted) : 0ull);
           seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
         }
-        const float c0 = __fdiv_rn(p.scale * 1.4426950408889634f, __ldg(p.cache.k_G + w.u));
+        kvh = w.u / p.row_tiles;
+        row0 = (w.u - kvh * p.row_tiles) * R;
+        const float c0 = __fdiv_rn(p.scale * 1.4426950408889634f, __ldg(p.cache.k_G + kvh));
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           // Q scaled by a power of two per row, as above
-          const int row = 8 * n + r;
+          const int row = row0 + 8 * n + r;
           float v[D / 4];
           if (row < p.rows) {
             const int hl = row / p.T, tok = row - hl * p.T;
-            const uint16_t* q = static_cast<const uint16_t*>(p.q) + w.b * p.q_sb + (long long)(w.u * p.group + hl) * p.q_sh + tok * p.q_sn + c * (D / 4);
+            const uint16_t* q = static_cast<const uint16_t*>(p.q) + w.b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + c * (D / 4);
 #pragma unroll
             for (int x = 0; x < D / 4; x += 8) {
               uint32_t raw[4];
@@ -1198,7 +1241,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             const bool here = held >> ((tok0 + tok) >> p.cache.log_page) & 1;
 #pragma unroll 1
             for (int n = 0; n < NT; ++n) {
-              const int row = 8 * n + 2 * c + (y & 1);
+              const int row = row0 + 8 * n + 2 * c + (y & 1);
               bool vis = here && pos < w.len;
               if (pos >= w.ctx) vis = vis && row < p.rows && (row_mask(p, w.b, row % p.T, n_drafted) >> ((pos - w.ctx) & 63) & 1);
               hidden |= (vis ? 0u : 1u) << (8 * n + y);
@@ -1310,7 +1353,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
       // ---- end of the item, or of this CTA's part of it: the warps together
       if (rare(w.left == 1 || i + 1 == n_tiles)) {
         const bool whole = part_first == 0 && w.left == 1;
-        const long long out0 = ((long long)w.b * p.H + (long long)w.u * p.group) * p.T;
+        const long long out0 = ((long long)w.b * p.H + (long long)kvh * p.group) * p.T;
         const int slot_of = 2 * (int)blockIdx.x + (part_first == 0);
 #pragma unroll
         for (int n = 0; n < NT; ++n)                                // eight rows and half the elements at a time
@@ -1331,8 +1374,8 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             __syncthreads();
             // a thread per row and four elements
 #pragma unroll 1
-            for (int j = threadIdx.x; j < min(8, p.rows - 8 * n) * (D / 8); j += C::kThreads) {
-              const int row8 = j / (D / 8), row = 8 * n + row8, e8 = j % (D / 8) * 4, e = 16 * z0 + e8;
+            for (int j = threadIdx.x; j < min(8, p.rows - row0 - 8 * n) * (D / 8); j += C::kThreads) {
+              const int row8 = j / (D / 8), in_tile = 8 * n + row8, row = row0 + in_tile, e8 = j % (D / 8) * 4, e = 16 * z0 + e8;
               float top_m = -INFINITY, total_l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
               for (int k = 0; k < C::kWarps; ++k) top_m = fmaxf(top_m, ml_smem[k * 8 + row8].x);
               for (int k = 0; k < C::kWarps; ++k) {
@@ -1344,29 +1387,28 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
               }
               if (whole) {
                 if (row % p.T < n_drafted) {
-                  const float inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + w.u));     // nothing seen: 0
+                  const float inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + kvh));     // nothing seen: 0
                   const uint2 h = p.half ? make_uint2(pack_pair<__half>(y[0] * inv, y[1] * inv), pack_pair<__half>(y[2] * inv, y[3] * inv))
                                          : make_uint2(pack_pair<__nv_bfloat16>(y[0] * inv, y[1] * inv), pack_pair<__nv_bfloat16>(y[2] * inv, y[3] * inv));
                   *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + (size_t)(out0 + row) * D + e) = h;
                   if (e == 0 && p.lse) p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (top_m - kShift + log2f(total_l)) * 0.6931471805599453f;
                 }
               } else {
-                *reinterpret_cast<float4*>(p.part + ((size_t)slot_of * R + row) * D + e) = make_float4(y[0], y[1], y[2], y[3]);
-                if (e == 0) p.part_ml[(size_t)slot_of * R + row] = make_float2(top_m, total_l);
+                *reinterpret_cast<float4*>(p.part + ((size_t)slot_of * R + in_tile) * D + e) = make_float4(y[0], y[1], y[2], y[3]);
+                if (e == 0) p.part_ml[(size_t)slot_of * R + in_tile] = make_float2(top_m, total_l);
               }
             }
             __syncthreads();
           }
         if (threadIdx.x == 0 && part_first == 0)
           p.split[(size_t)w.b * units + w.u] =
-              whole ? make_int2(-1, -1) : make_int2(blockIdx.x, (int)(((find[2] + i + w.left) * find[4] - 1) / find[3]));
+              whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find, find[2] + i + w.left - 1));
         fresh = true;
       }
       advance(w, p, units);
     }
     pages.tell(p);
   }
-  launch_dependents();
   __syncthreads();
   if (rare(*abort_word != 0)) {                                     // given up: the copies in flight end before shared memory does
     if (threadIdx.x == 0 && p.status) *p.status = FP4ATTN_ERR_TIMEOUT;
@@ -1396,14 +1438,25 @@ __global__ void __launch_bounds__(128) tree_join_kernel(const TreeParams p) {
   for (int i0 = 0; i0 < n; i0 += 32) {
     const int i = i0 + lane;
     const float2 ml = i < n ? p.part_ml[slot(i) * R + r] : make_float2(-INFINITY, 0.f);
-    const float mine = m == -INFINITY ? 0.f : exp2_approx(ml.x - m);
+    const float mine = m == -INFINITY || i >= n ? 0.f : exp2_approx(ml.x - m);
     const float weighted = ml.x == -INFINITY ? ml.y : mine * ml.y;
-    for (int k = 0; k < min(32, n - i0); ++k) {
-      const float f = __shfl_sync(0xffffffffu, mine, k);
-      l += __shfl_sync(0xffffffffu, weighted, k);
-      const float* const src = p.part + (slot(i0 + k) * R + r) * D + lane * E;
+    constexpr int kAtOnce = 8;                                      // loads on their way together
+    for (int k0 = 0; k0 < min(32, n - i0); k0 += kAtOnce) {
+      float part[kAtOnce][E];
 #pragma unroll
-      for (int x = 0; x < E; ++x) o[x] = fmaf(f, src[x], o[x]);
+      for (int k = 0; k < kAtOnce; ++k) {
+        const bool is = i0 + k0 + k < n;
+        const float* const src = p.part + (slot(is ? i0 + k0 + k : 0) * R + r) * D + lane * E;
+        if constexpr (E == 4) *reinterpret_cast<float4*>(part[k]) = is ? *reinterpret_cast<const float4*>(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+        else *reinterpret_cast<float2*>(part[k]) = is ? *reinterpret_cast<const float2*>(src) : make_float2(0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {                           // (behind the last part: weights and parts of 0)
+        const float f = __shfl_sync(0xffffffffu, mine, k0 + k);
+        l += __shfl_sync(0xffffffffu, weighted, k0 + k);
+#pragma unroll
+        for (int x = 0; x < E; ++x) o[x] = fmaf(f, part[k][x], o[x]);
+      }
     }
   }
   const float f = l == 0.f ? 0.f : __fdiv_rn(1.f, l * __ldg(p.cache.v_G + kvh));
@@ -1466,17 +1519,19 @@ int launch_warps(const TreeParams& p, cudaStream_t st) {
   }
   const int sms = device_sms();
   if (!sms) return FP4ATTN_ERR_CUDA;
-  const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * p.cache.kv_heads;
+  const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * p.cache.kv_heads * p.row_tiles;
   const unsigned grid = (unsigned)std::min<long long>(std::min(C::kCtas * sms, kMostCtas), most_tiles);
   cudaError_t e = launch_overlapped(tree_warp_kernel<FMT, D, NT>, dim3(grid), C::kThreads, C::kSmem, st, p);
   if (e == cudaSuccess)
-    e = launch_overlapped(tree_join_kernel<D, C::R>, dim3((unsigned)(p.B * p.cache.kv_heads), (unsigned)(p.rows + 3) / 4), 128u, 0, st, p);
+    e = launch_overlapped(tree_join_kernel<D, C::R>, dim3((unsigned)(p.B * p.cache.kv_heads * p.row_tiles), (unsigned)(std::min(p.rows, C::R) + 3) / 4), 128u, 0,
+                          st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
 template <int FMT, int D>
 int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
   if (p.rows <= 8) return launch_warps<FMT, D, 1>(p, st);
-  return R == 16 ? launch_warps<FMT, D, 2>(p, st) : R == 32 ? launch_tree<FMT, D, 32, 16>(p, st) : launch_tree<FMT, D, 64, 16>(p, st);
+  if (R == 16) return launch_warps<FMT, D, 2>(p, st);
+  return R == 32 ? launch_tree<FMT, D, 32, 16>(p, st) : launch_tree<FMT, D, 64, 16>(p, st);
 }
 
 }  // namespace
