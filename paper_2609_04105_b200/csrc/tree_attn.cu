@@ -1070,15 +1070,21 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
       pages.bring(p, sbase, full, free, abort_at, valid);
       pages.skip(p, units, 1);
     }
-  } else {
+  } else if (C::kStages + warp < n_parts) {
     pages.skip(p, units, C::kStages + warp);
+  } else {
+    pages.i = n_parts;                                              // no turn
   }
   if (pages.i < n_parts) pages.find(p);
   auto next_pages = [&](int part) {                                 // this warp's turn?
     if (pages.i == part - 1 + C::kStages && pages.i < n_parts) {
       pages.bring(p, sbase, full, free, abort_at, valid);
-      pages.skip(p, units, C::kWarps);
-      if (pages.i < n_parts) pages.find(p);                         // (the entries come until its next turn)
+      if (pages.i >= n_parts - C::kWarps) {
+        pages.i = n_parts;
+      } else {
+        pages.skip(p, units, C::kWarps);
+        pages.find(p);                                              // (the entries come until its next turn)
+      }
     }
   };
   {
@@ -1236,15 +1242,19 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
         uint32_t hidden = 0;                                        // bit 8n + y: s[n][y] is not seen
         if (rare(!plain)) {
 #pragma unroll 1
-          for (int y = 0; y < 8; ++y) {
-            const int tok = tok_k + kSecondStep * (y >> 2) + kSecondRow * (y >> 1 & 1), pos = w.first + tok0 + tok;
-            const bool here = held >> ((tok0 + tok) >> p.cache.log_page) & 1;
-#pragma unroll 1
-            for (int n = 0; n < NT; ++n) {
-              const int row = row0 + 8 * n + 2 * c + (y & 1);
-              bool vis = here && pos < w.len;
-              if (pos >= w.ctx) vis = vis && row < p.rows && (row_mask(p, w.b, row % p.T, n_drafted) >> ((pos - w.ctx) & 63) & 1);
-              hidden |= (vis ? 0u : 1u) << (8 * n + y);
+          for (int n = 0; n < NT; ++n) {
+            unsigned long long mask[2];                             // drafted tokens that the rows see
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const int row = row0 + 8 * n + 2 * c + y;
+              mask[y] = row < p.rows ? row_mask(p, w.b, row % p.T, n_drafted) : 0ull;
+            }
+#pragma unroll
+            for (int y = 0; y < 8; y += 2) {
+              const int tok = tok_k + kSecondStep * (y >> 2) + kSecondRow * (y >> 1 & 1), pos = w.first + tok0 + tok, in = pos - w.ctx;
+              const bool here = (held >> ((tok0 + tok) >> p.cache.log_page) & 1) && pos < w.len;
+              const uint32_t m0 = in < 0 ? 1u : (uint32_t)(mask[0] >> (in & 63)) & 1u, m1 = in < 0 ? 1u : (uint32_t)(mask[1] >> (in & 63)) & 1u;
+              hidden |= (here ? (m0 | m1 << 1) ^ 3u : 3u) << (8 * n + y);
             }
           }
         }
