@@ -104,23 +104,27 @@ __device__ __forceinline__ unsigned long long row_mask(const TreeParams& p, int 
   return p.mask ? __ldg(p.mask + (size_t)b * p.T + t) : (2ull << t) - 1;
 }
 
-// R: rows of a tile; N: rows of a softmax thread (8 only where the item has no more: the other columns of R = 16 are zero)
-template <int FMT, int D, int R, int N>
+// R: rows of a tile, 32 or 64
+template <int FMT, int D, int R>
 struct TreeCfg {
   using L = RecordLayout<FMT, D>;
-  static constexpr int kN = N;
-  static constexpr int kColGroups = R > 16 ? R / N : 1;
+  static constexpr int kN = 32;                                    // rows of a softmax thread
+  static constexpr int kColGroups = R / kN;
   static constexpr int kSets = R <= 32 ? 2 : 1;                    // sets of softmax groups that tiles alternate between
-  static constexpr int kKGroups = R == 16 ? 2 : 1, kVGroups = 2;   // groups of four warps that tiles alternate between
+  static constexpr int kKGroups = 1, kVGroups = 2;                 // groups of four warps that tiles alternate between
   static constexpr int kFirstV = 4 * kKGroups, kFirstSoftmax = kFirstV + 4 * kVGroups;         // warps
   static constexpr int kProducer = kFirstSoftmax + 4 * kColGroups * kSets, kIssuerS = kProducer + 1, kIssuerO = kProducer + 2;
-  static constexpr int kThreads = 32 * (kIssuerO + 1);
-  static_assert(kThreads <= 1024, "warps");
+  static constexpr int kThreads = 32 * (kProducer + 4);            // the last warp only makes up a warpgroup
+  // Registers: 80 a thread at launch.  A softmax thread needs 128 for its 32 rows (with 16 rows a thread and 64 registers a third of
+  // its scores and sums were in local memory: 3850 clocks a tile of 64 rows); the other roles give up what it takes.
+  static constexpr int kRegsLaunch = 80, kRegsAux = 32, kRegsKV = 64, kRegsSoftmax = 128;
+  static_assert(kThreads * kRegsLaunch <= 65536 &&
+                kRegsAux + (kKGroups + kVGroups) * kRegsKV + kColGroups * kSets * kRegsSoftmax <= kThreads / 128 * kRegsLaunch, "register shares");
   static constexpr int kStage = kTile * 2 * L::kToken;
   static constexpr int kStages = kStage >= 32768 ? 4 : kStage > 16384 ? 6 : 8;
   // Buffers between the roles: deep enough that the hand-overs (some 200 clocks each) of one tile lie under the work on others
   static constexpr int kSB = kSets == 2 ? 4 : 2, kVB = 3;          // scores; V^T in tensor memory and P
-  static constexpr int kKB = D == 64 ? 4 : R == 16 ? 3 : 2;        // K in tensor memory
+  static constexpr int kKB = D == 64 ? 4 : 2;                      // K in tensor memory
   static constexpr int kQB = kKB;                                  // Q: see the K warps
   static constexpr int kQ = R * D * 2, kP = kTile * R * 2;
   // The softmax warps may be kKB + kSB tiles behind the K warps, and those kStages behind the producer: what they take from either
@@ -156,8 +160,9 @@ struct TreeCfg {
 // Waits for a barrier's phase; the whole warp goes on together.  A wait that runs out, or sees that another one did, sets the abort word
 // and returns as if the phase had come: what the roles then read and multiply means nothing, but stays in bounds, and every wait of
 // theirs ends at once, so that they run out of tiles.  The phase has come at the first look, or while that look was suspended, in nearly
-// every wait.  The loop behind it is a function of its own: inlined at each wait it took 12 % of the time, in instruction fetches.
-__device__ __noinline__ void wait_longer(uint32_t bar, uint32_t parity, uint32_t abort_at) {
+// every wait.  CALL: the loop behind it is a function of its own: inlined at each wait it took up to 12 % of the time, in instruction
+// fetches.  (Code that shares out registers by setmaxnreg may not call.)
+__device__ __forceinline__ void poll_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
   uint32_t since = 0;
   for (uint32_t n = 1;; ++n) {
     uint32_t gone;
@@ -171,8 +176,13 @@ __device__ __noinline__ void wait_longer(uint32_t bar, uint32_t parity, uint32_t
   }
   asm volatile("st.volatile.shared.u32 [%0], 1;" ::"r"(abort_at) : "memory");
 }
+__device__ __noinline__ void wait_longer(uint32_t bar, uint32_t parity, uint32_t abort_at) { poll_phase(bar, parity, abort_at); }
+template <bool CALL>
 __device__ __forceinline__ void wait_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
-  if (rare(!mbar_try_wait(bar, parity))) wait_longer(bar, parity, abort_at);
+  if (rare(!mbar_try_wait(bar, parity))) {
+    if (CALL) wait_longer(bar, parity, abort_at);
+    else poll_phase(bar, parity, abort_at);
+  }
   __syncwarp();
 }
 // which of N buffers, and the phase of its barriers
@@ -249,9 +259,8 @@ __device__ __forceinline__ float warp_sums(float (&v)[N], int lane) {
 }
 template <int N>
 __device__ __forceinline__ void tmem_ld_cols(uint32_t addr, uint32_t (&r)[N]) {
-  if constexpr (N == 16) tmem_ld_32x32b_x16(addr, r);
-  else if constexpr (N == 8) tmem_ld_32x32b_x8(addr, r);
-  else tmem_ld_32x32b_x4(addr, r);
+  if constexpr (N == 32) tmem_ld_32x32b_x32(addr, r);
+  else tmem_ld_32x32b_x16(addr, r);
 }
 // of the eight tokens from position `pos` on, those that count (bit t: token t): the context, and the drafted tokens that some row sees
 __device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long long seen, int pos) {
@@ -356,7 +365,7 @@ __device__ __forceinline__ int cta_of(const long long* find, long long tile) {
 
 // Brings the pages of tiles into a ring of stages, one bulk copy each; a whole warp.  RING: stages for which `valid` remembers which of the
 // pages exist.  PARTS = 2: K and V by themselves, each in a stage of its own.
-template <int STAGES, int STAGE, int RING, int PARTS = 1>
+template <int STAGES, int STAGE, int RING, int PARTS, bool CALL>
 struct Pages {
   Walk w;
   Turn<STAGES> ring;
@@ -375,7 +384,7 @@ struct Pages {
   __device__ __forceinline__ void bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
     const int lane = threadIdx.x & 31;
     const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
-    wait_phase(free + 8 * ring.at, ring.phase ^ 1, abort_at);
+    wait_phase<CALL>(free + 8 * ring.at, ring.phase ^ 1, abort_at);
     const int bytes = p.cache.record / PARTS;
     if (lane == 0) {
       valid[i % RING] = held;
@@ -399,9 +408,9 @@ struct Pages {
   }
 };
 
-template <int FMT, int D, int R, int N_>
-__global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kernel(const TreeParams p) {
-  using C = TreeCfg<FMT, D, R, N_>;
+template <int FMT, int D, int R>
+__global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(const TreeParams p) {
+  using C = TreeCfg<FMT, D, R>;
   using L = typename C::L;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -436,10 +445,6 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     fence_barrier_init();
   }
   if (warp == C::kIssuerS) { tmem_alloc(tslot, 512); tmem_relinquish(); }
-  if (C::kN < 16) {                                                 // probabilities of the rows that are none
-    for (int i = threadIdx.x; i < C::kVB * C::kP / 16; i += C::kThreads) *reinterpret_cast<uint4*>(sgen + C::kOffP + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
-    fence_proxy_async_smem();
-  }
   tc_fence_before();
   launch_dependents();                                              // the joining kernel: its launch lies under this one
   wait_prior_grids();
@@ -450,11 +455,13 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
   uint32_t* const valid_ring = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
   const int P = 1 << p.cache.log_page;
-  auto wait = [&](int b, int phase) { wait_phase(bar(b), (uint32_t)phase, abort_at); };
+  auto wait = [&](int b, int phase) { wait_phase<false>(bar(b), (uint32_t)phase, abort_at); };
 
+  if (warp >= C::kProducer) {
+  registers_fewer<C::kRegsAux>();
   if (warp == C::kProducer) {
     // ===================================================================== pages -> shared memory
-    Pages<C::kStages, C::kStage, C::kRing> pages;
+    Pages<C::kStages, C::kStage, C::kRing, 1, false> pages;
     pages.w = w0;
     if (n_tiles > 0) pages.find(p);
     while (pages.i < n_tiles) {
@@ -525,7 +532,10 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
     }
     if (elect_one()) tc_commit(bar(C::DRAIN + 1));
     __syncwarp();
-  } else if (warp < C::kFirstV) {
+  }
+  } else if (warp < C::kFirstSoftmax) {
+  registers_fewer<C::kRegsKV>();
+  if (warp < C::kFirstV) {
     // ===================================================================== Q and K
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const int group = warp >> 2, quarter = warp & 3;
@@ -642,7 +652,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
       kb.next(C::kKGroups);
       item += advance_by(w, p, units, C::kKGroups, &fresh);
     }
-  } else if (warp < C::kFirstSoftmax) {
+  } else {
     // ===================================================================== V
     const int quarter = warp & 3, group = (warp - C::kFirstV) >> 2, e = quarter * 32 + lane;      // index of the head dimension
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
@@ -741,8 +751,10 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
       vb.next(C::kVGroups);
       advance_by(w, p, units, C::kVGroups, &fresh);
     }
+  }
   } else {
     // ===================================================================== softmax
+    registers_more<C::kRegsSoftmax>();
     constexpr int N = C::kN;
     const int group = (warp - C::kFirstSoftmax) >> 2, set = group / C::kColGroups, cols = group % C::kColGroups, c0 = cols * N;
     const int quarter = warp & 3, key = quarter * 32 + lane;
@@ -795,7 +807,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
         const uint32_t held = valid_ring[i % C::kRing];
         // scores in octaves above the rows' references (+ kShift); those that are not seen go to -infinity
         float x[N], top = -INFINITY;
-        uint32_t rows_seeing = 0xFFFFu;                             // rows of this thread that see its key
+        uint32_t rows_seeing = 0xFFFFFFFFu;                             // rows of this thread that see its key
         const bool plain = w.first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
         if (rare(!plain)) {
           const int pos = w.first + key;
@@ -857,8 +869,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R, N_>::kThreads, 1) tree_kern
             tmem_wait_ld();
 #pragma unroll
             for (int r = 0; r < N; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * factor[r]);
-            if constexpr (N == 16) tmem_st_32x32b_x16(o_mine, o);
-            else tmem_st_32x32b_x8(o_mine, o);
+            tmem_st_32x32b_x16(o_mine, o);
+            tmem_st_32x32b_x16(o_mine + 16, o + 16);
             tmem_wait_st();
           }
         }
@@ -1061,7 +1073,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
   // K and V of the first tiles; then the warps take turns, each bringing what takes the place of the K or V before the one they have just
   // been through (of that one the other warps may not be through yet).  A warp that fills a stage has itself been through what stood there before: the stage's barrier cannot be further back
   // than a wait by parity can tell.
-  Pages<C::kStages, C::kStage, C::kStages, 2> pages;
+  Pages<C::kStages, C::kStage, C::kStages, 2, true> pages;
   pages.w = w0;
   const int n_parts = n_tiles > INT_MAX / 2 ? INT_MAX : 2 * n_tiles;
   if (warp == 0) {
@@ -1183,7 +1195,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
         }
       }
       {
-        wait_phase(full + 8 * ring.at, ring.phase, abort_at);
+        wait_phase<true>(full + 8 * ring.at, ring.phase, abort_at);
         const uint8_t* stage = sgen + ring.at * C::kStage;
         const uint32_t held = valid[ring.at];
         const bool plain = w.first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
@@ -1308,7 +1320,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             add_pair(l[n][0], l[n][1], a, b);
             pb[n][y] = transpose_8x8(pack_pair<__half>(a, b));
           }
-        wait_phase(full + 8 * ring.at, ring.phase, abort_at);
+        wait_phase<true>(full + 8 * ring.at, ring.phase, abort_at);
         stage = sgen + ring.at * C::kStage;
         // ---- scales of V: f16, by block and token
         if (L::kFp4 && lane < D / 4) {
@@ -1497,14 +1509,14 @@ TreePlan plan(int B, int H, int kv_heads, int T, int d) {
   return t;
 }
 
-template <int FMT, int D, int R, int N>
+template <int FMT, int D, int R>
 int launch_tree(const TreeParams& p, cudaStream_t st) {
-  using C = TreeCfg<FMT, D, R, N>;
+  using C = TreeCfg<FMT, D, R>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FP4ATTN_ERR_CUDA;
   static std::atomic<bool> attr_set[kMaxDevices];
   if (!attr_set[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(tree_kernel<FMT, D, R, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
+    if (cudaFuncSetAttribute(tree_kernel<FMT, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
     attr_set[dev].store(true, std::memory_order_release);
   }
   const int sms = device_sms();
@@ -1512,7 +1524,7 @@ int launch_tree(const TreeParams& p, cudaStream_t st) {
   const int units = p.cache.kv_heads * p.row_tiles;
   const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * units;
   const unsigned grid = (unsigned)std::min<long long>(std::min(sms, kMostCtas), most_tiles);
-  cudaError_t e = launch_overlapped(tree_kernel<FMT, D, R, N>, dim3(grid), C::kThreads, C::kSmem, st, p);
+  cudaError_t e = launch_overlapped(tree_kernel<FMT, D, R>, dim3(grid), C::kThreads, C::kSmem, st, p);
   if (e == cudaSuccess)
     e = launch_overlapped(tree_join_kernel<D, R>, dim3((unsigned)(p.B * units), (unsigned)(std::min(R, p.rows) + 3) / 4), 128u, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
@@ -1541,7 +1553,7 @@ template <int FMT, int D>
 int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
   if (p.rows <= 8) return launch_warps<FMT, D, 1>(p, st);
   if (R == 16) return launch_warps<FMT, D, 2>(p, st);
-  return R == 32 ? launch_tree<FMT, D, 32, 16>(p, st) : launch_tree<FMT, D, 64, 16>(p, st);
+  return R == 32 ? launch_tree<FMT, D, 32>(p, st) : launch_tree<FMT, D, 64>(p, st);
 }
 
 }  // namespace
