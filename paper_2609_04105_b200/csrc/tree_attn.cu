@@ -138,8 +138,8 @@ struct TreeCfg {
   static constexpr int kOffVScale = kOffP + kVB * kP;                // f16 [V warps][2 blocks][128 tokens]
   static constexpr int kOffCM = kOffVScale + 4 * kVGroups * 512;                 // float [kSets][2][R]: kShift minus the reference; score constant
   static constexpr int kOffC = kOffCM + 8 * R * kSets;             // float [kRingC][R]: score constants of the last items
-  static constexpr int kOffBits = kOffC + 4 * R * kRingC;                  // u64 [kSets][R]
-  static constexpr int kOffWarp = kOffBits + 8 * R * kSets;        // float [kSets][4][R]: maxima or sums of the four warps
+  static constexpr int kOffBits = kOffC + 4 * R * kRingC;          // u32 [kSets][kColGroups][64]: rows that see a drafted token
+  static constexpr int kOffWarp = kOffBits + 256 * kColGroups * kSets;         // float [kSets][4][R]: maxima or sums of the four warps
   static constexpr int kOffScale = kOffWarp + 16 * R * kSets;      // float [kSets][R]: factors on O
   static constexpr int kOffValid = kOffScale + 4 * R * kSets;      // u32 [kRing]
   static constexpr int kOffScan = kOffValid + 4 * kRing;           // i64 [32]
@@ -763,7 +763,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
     float* const ref_all = reinterpret_cast<float*>(sgen + C::kOffCM) + c0;                      // [kSets][2] R apart: kShift - reference
     float* const ref = ref_all + set * 2 * R;
     float* const con = ref + R;                                                                  // score constants
-    unsigned long long* const bits = reinterpret_cast<unsigned long long*>(sgen + C::kOffBits) + set * R + c0;
+    uint32_t* const bits = reinterpret_cast<uint32_t*>(sgen + C::kOffBits) + 64 * group;
     float* const warps_all = reinterpret_cast<float*>(sgen + C::kOffWarp) + c0;                  // [kSets][4] R apart
     float* const warps = warps_all + set * 4 * R;
     float* const factor_all = reinterpret_cast<float*>(sgen + C::kOffScale) + c0;
@@ -782,9 +782,16 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
     for (int i = 0; i < n_tiles; ++i) {
       if (rare(fresh)) {
         part_first = w.first;
-        if (key < N) {
-          const int row = w.u % p.row_tiles * R + c0 + key;
-          bits[key] = row < p.rows ? row_mask(p, w.b, row % p.T, drafted(p, w.b)) : 0ull;
+        {
+          // a lane has a row's mask; a word per drafted token, sixteen a warp
+          const int row = w.u % p.row_tiles * R + c0 + lane;
+          const unsigned long long mask = row < p.rows ? row_mask(p, w.b, row % p.T, drafted(p, w.b)) : 0ull;
+          const uint32_t mine = (uint32_t)(mask >> (16 * quarter));
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const uint32_t word = __ballot_sync(0xffffffffu, mine >> j & 1);
+            if (lane == j) bits[16 * quarter + j] = word;
+          }
         }
 #pragma unroll
         for (int r = 0; r < N; ++r) l[r] = 0.f;
@@ -812,13 +819,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         if (rare(!plain)) {
           const int pos = w.first + key;
           const bool here = held >> (key >> p.cache.log_page) & 1;
-          if (!(here && pos < w.ctx)) {
-            rows_seeing = 0;
-            if (here && pos < w.len) {
-#pragma unroll 1
-              for (int r = 0; r < N; ++r) rows_seeing |= (uint32_t)(bits[r] >> (pos - w.ctx) & 1ull) << r;
-            }
-          }
+          rows_seeing = !here || pos >= w.len ? 0u : pos < w.ctx ? 0xFFFFFFFFu : bits[pos - w.ctx];
         }
         auto relative = [&](bool references) {
 #pragma unroll
