@@ -512,26 +512,29 @@ struct Batch {
     return nullptr;
   }
 };
-at::Tensor like_view(const Strided& s, c10::Device device) { return device_empty({s.B, s.H, s.N, s.d}, s.t->scalar_type(), device); }
-// an output tensor: what the caller gave, checked, or a new one
-bool output(PyObject* o, const Strided& like, Strided* out, at::Tensor* own) {
-  if (o == Py_None) {
-    *own = like_view(like, like.t->device());
-    out->t = own;
-    out->B = like.B; out->H = like.H; out->N = like.N; out->d = like.d; out->type = like.type;
-    out->view = {own->data_ptr(), own->stride(0), own->stride(1), own->stride(2)};
+// Output tensors: what the caller gave, checked, or pieces of one allocation
+struct Outputs {
+  Results r;
+  at::Tensor* own[2] = {nullptr, nullptr};
+  bool take(int i, PyObject* o, const Strided& like, Strided* out) {
+    if (o != Py_None) return out->take(o, true) && out->like(like) && out->H == like.H && out->distinct();
+    own[i] = &r.add({like.B, like.H, like.N, like.d}, like.t->scalar_type());
     return true;
   }
-  return out->take(o, true) && out->like(like) && out->H == like.H && out->distinct();
-}
-PyObject* given_or(PyObject* o, const at::Tensor& own) { return o == Py_None ? THPVariable_Wrap(own) : Py_NewRef(o); }
+  void allocate(c10::Device device, Strided* out) {
+    if (r.n) r.allocate(device);
+    for (int i = 0; i < 2; ++i)
+      if (own[i]) out[i].view = {own[i]->data_ptr(), own[i]->stride(0), own[i]->stride(1), own[i]->stride(2)};
+  }
+  PyObject* give(int i, PyObject* o) const { return own[i] ? THPVariable_Wrap(*own[i]) : Py_NewRef(o); }
+};
 
 // rotary(q, k, positions, inv_freq, interleaved, transposed, factor, q_out, k_out) -> q_out, or (q_out, k_out)
 PyObject* py_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
   FP4_TRY
   if (n != 9) return assertion("rotary takes 9 arguments");
   Strided x[2], y[2];
-  at::Tensor own[2];
+  Outputs outputs;
   const bool two = args[1] != Py_None;
   if (!x[0].take(args[0], true) || (two && !(x[1].take(args[1], true) && x[1].like(x[0]))))
     return assertion("q (and k) must be CUDA tensors [B, heads, N, d], bfloat16, float16 or float32, the last axis contiguous; k of q's B, N, d, type and device");
@@ -548,15 +551,16 @@ PyObject* py_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (interleaved < 0 || transposed < 0 || !number(args[6], &factor)) return nullptr;
   const c10::cuda::OptionalCUDAGuard guard(device);
   for (int i = 0; i <= (int)two; ++i)
-    if (!output(args[7 + i], x[i], &y[i], &own[i]))
+    if (!outputs.take(i, args[7 + i], x[i], &y[i]))
       return assertion("an output must be a CUDA tensor of its input's shape, type and device, the last axis contiguous, no element twice");
+  outputs.allocate(device, y);
   const int rc = unlocked([&] {
     return g_api.rotary(&x[0].view, two ? &x[1].view : nullptr, &y[0].view, two ? &y[1].view : nullptr, x[0].type, x[0].B, x[0].H, x[1].H,
                         x[0].N, x[0].d, (const int*)positions, (const float*)freq, (int)pairs, interleaved, transposed, factor, stream());
   });
   if (rc) return fail(rc, "fp4attn_rotary");
-  if (!two) return given_or(args[7], own[0]);
-  return Py_BuildValue("(NN)", given_or(args[7], own[0]), given_or(args[8], own[1]));
+  if (!two) return outputs.give(0, args[7]);
+  return Py_BuildValue("(NN)", outputs.give(0, args[7]), outputs.give(1, args[8]));
   FP4_CATCH
 }
 
@@ -615,23 +619,24 @@ PyObject* py_cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const c10::cuda::OptionalCUDAGuard guard(cache.device);
   const at::ScalarType type = half ? at::kHalf : at::kBFloat16;
   Strided out[2];
-  at::Tensor own[2];
+  Outputs outputs;
   for (int i = 0; i < 2; ++i) {
     if (args[6 + i] == Py_None) {
-      own[i] = device_empty({B, cache.c.kv_heads, N, cache.c.d}, type, cache.device);
-      if (batch.count) own[i].zero_();                   // rows behind the counts are not written
-      out[i].view = {own[i].data_ptr(), own[i].stride(0), own[i].stride(1), own[i].stride(2)};
+      outputs.own[i] = &outputs.r.add({B, cache.c.kv_heads, N, cache.c.d}, type);
     } else if (!out[i].take(args[6 + i], false) || out[i].t->scalar_type() != type || out[i].B != B || out[i].H != cache.c.kv_heads ||
                out[i].N != N || out[i].d != cache.c.d || out[i].t->device() != cache.device || !out[i].distinct()) {
       return assertion("k_out and v_out must be CUDA tensors [B, KV heads, N, d] of the cache's heads, d and device and of dtype, the last axis contiguous, no element twice");
     }
   }
+  outputs.allocate(cache.device, out);
+  for (at::Tensor* own : outputs.own)
+    if (own && batch.count) own->zero_();                // rows behind the counts are not written
   const int rc = unlocked([&] {
     return g_api.cache_read(&cache.c, &out[0].view, &out[1].view, half ? FP4ATTN_TYPE_FP16 : FP4ATTN_TYPE_BF16, (int)B, N, batch.table,
                             batch.max_pages, batch.start, batch.count, batch.status, stream());
   });
   if (rc) return fail(rc, "fp4attn_cache_read");
-  return Py_BuildValue("(NN)", given_or(args[6], own[0]), given_or(args[7], own[1]));
+  return Py_BuildValue("(NN)", outputs.give(0, args[6]), outputs.give(1, args[7]));
   FP4_CATCH
 }
 
@@ -659,8 +664,8 @@ PyObject* py_tree_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   THPObjectPtr out(Py_NewRef(args[7])), lse(Py_NewRef(args[8]));
   Results r;
   at::Tensor none, &o = out_ptr ? none : r.add({q.B, q.H, q.N, q.d}, q.t->scalar_type()), &l = lse_ptr ? none : r.add({q.B, q.H, q.N}, at::kFloat);
-  at::Tensor& ws = nw ? r.add({(int64_t)nw}, at::kByte) : none;
-  r.allocate(cache.device);
+  if (r.n) r.allocate(cache.device);
+  const at::Tensor ws = nw ? device_empty({(int64_t)nw}, at::kByte, cache.device) : none;
   if (o.defined()) {
     if (batch.count) o.zero_();                          // rows behind the counts are not written
     out_ptr = o.data_ptr();
