@@ -1578,7 +1578,7 @@ extern "C" int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4
   if (!q || !q->data || !O || H <= 0 || T <= 0 || !(softmax_scale >= 0.f)) return FP4ATTN_ERR_INVALID_ARG;
   if (type != FP4ATTN_TYPE_BF16 && type != FP4ATTN_TYPE_FP16) return FP4ATTN_ERR_INVALID_ARG;
   if (H % cache->kv_heads != 0) return FP4ATTN_ERR_INVALID_ARG;
-  if (T > FP4ATTN_MOST_TREE_TOKENS || (long long)B * H * T >= (1ll << 31)) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;
+  if (T > FP4ATTN_MOST_TREE_TOKENS || (long long)B * H * T >= (1ll << 31)) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;     // (items are no more)
   if (((uintptr_t)q->data & 1) || ((uintptr_t)O & 15) || ((uintptr_t)tree_mask & 7) || ((uintptr_t)LSE | (uintptr_t)device_status) & 3)
     return FP4ATTN_ERR_ALIGNMENT;
   const TreePlan t = plan(B, H, cache->kv_heads, T, cache->d);

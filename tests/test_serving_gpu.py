@@ -339,6 +339,13 @@ TREE = [  # B, H, kv, T, d, P, contexts
     (1, 3, 3, 64, 64, 16, [0]),
     (5, 2, 1, 2, 128, 16, [5, 2000, 0, 64, 700]),
     (1, 2, 1, 1, 128, 64, [20011]),
+    (2, 9, 1, 1, 128, 16, [333, 129]),
+    (1, 3, 1, 5, 64, 128, [1025]),
+    (2, 8, 1, 64, 64, 128, [200, 66]),
+    (1, 24, 2, 33, 128, 16, [127]),
+    (40, 2, 2, 1, 64, 16, [(37 * i) % 300 for i in range(40)]),
+    (35, 5, 1, 5, 128, 32, [(91 * i) % 200 for i in range(35)]),
+    (1030, 1, 1, 1, 64, 16, [i % 19 for i in range(1030)]),
 ]
 
 
@@ -394,6 +401,32 @@ def test_tree_attention_empty_rows_counts_and_what_nobody_sees(fmt):
         assert torch.equal(out[b, :, :n], want[0][b, :, :n]) and torch.equal(lse[b, :, :n], want[1][b, :, :n])
         assert (out[b, :, n:] == 9.0).all() and (lse[b, :, n:] == 9.0).all()
         assert not own[0][b, :, n:].any() and torch.isneginf(own[1][b, :, n:]).all()
+
+
+@pytest.mark.parametrize("H", [4, 40])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_tree_attention_drafted_tokens_that_were_not_written(fmt, H):
+    """Behind a count, and where no row's bit is set, the drafted tokens' bytes may be anything too: other rows are as without them."""
+    Bd, g = _bd(), _gen(26)
+    B, kv, T, d, P = 3, 2, 6, 64, 16
+    context, counts = [40, 0, 125], [3, 6, 1]
+    cache, table = _filled(Bd, g, fmt, B, kv, P, d, 140)
+    q = _randn(g, B, H, T, d)
+    bits = torch.tensor([[1, 3, 7, 15, 31, 63], [1, 3, 1, 1, 3, 1], [1, 3, 5, 9, 17, 33]], dtype=torch.int64, device="cuda")
+    for mask in (None, bits):
+        want = Bd.fp4attn_tree_attention(q, cache, table, _i32(context), tree_mask=mask, count=_i32(counts))
+        kept = cache.pages.clone()
+        kc, ks, vc, vs, _ = S.places(fmt, P, d)
+        for b in range(B):
+            unseen = [j for j in range(T) if j >= counts[b] or (mask is not None and not any(int(x) >> j & 1 for x in bits[b, :counts[b]]))]
+            for j in unseen:
+                pos = context[b] + j
+                for at in (kc, ks, vc, vs):
+                    if at is not None:
+                        cache.pages[int(table[b, pos // P]), :, torch.from_numpy(np.unique(at[pos % P])).cuda()] = 0xFF
+        got = Bd.fp4attn_tree_attention(q, cache, table, _i32(context), tree_mask=mask, count=_i32(counts))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        cache.pages.copy_(kept)
 
 
 def test_tree_attention_extreme_logits_and_queries():
