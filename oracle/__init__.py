@@ -33,4 +33,7 @@ Pinned by tests/test_oracle_*.py (run with -m "not gpu"):
                                                   ties, saturation; closed forms of the V factor; representable
                                                   probabilities against brute force; constant V, flushing, key
                                                   permutation, causal prefix; the accuracy level the paper reports
+  serving.py    rotary positions, paged cache, tree attention -> a rotation of complex numbers, products that go by the
+                                                  difference of positions; every byte of a record used once, round
+                                                  trips within the formats' steps; brute-force attention
 """

@@ -4,7 +4,8 @@
 // context[b] + T - 1 those whose bit of its mask is set.
 //
 // The rows that read one KV head are few (1 to some hundreds), its keys are many, so keys and head dimension take the wide side of the
-// tensor core and rows the narrow one:  S^T = K Q^T (128 keys x R rows),  O^T += V^T P^T (d x R rows), R = 16, 32 or 64.  Their A operands,
+// tensor core and rows the narrow one:  S^T = K Q^T (128 keys x R rows),  O^T += V^T P^T (d x R rows), R = 32 or 64.  (Sixteen rows or
+// fewer have a kernel of their own, further down.)  Their A operands,
 // K and V^T, live in tensor memory: a lane is a key of K, a head-dimension index of V^T, and the thread that turns a lane's
 // codes into f16 writes them there without a word of shared memory.  Only Q and P, the narrow operands, are read from shared memory.
 //
@@ -14,11 +15,14 @@
 //
 //   K            codes of a key -> f16 -> tensor memory; Q of an item, scaled by a power of two per row, -> f16 -> shared memory
 //   V            codes of an index -> f16 -> tensor memory
-//   softmax      a thread per key and 8 or 16 rows: exp2, P^T -> shared memory; rescale of O, end of an item
-//   each in groups of four warps that tiles alternate between, where there are enough warps: a tile is one long chain of instructions for
-//   a warp, so the time of a tile is that of the slowest role's chain over its groups.  Up to 32 rows, the two sets of softmax groups have
-//   references, sums and an O each.
+//   softmax      a thread per key and 32 rows: exp2, P^T -> shared memory; rescale of O, end of an item
+//   each in groups of four warps; tiles alternate between the two groups of V and, up to 32 rows, between two softmax groups with references,
+//   sums and an O each: a tile is one long chain of instructions for a warp, and the time of a tile is that of the slowest chain.
 //   then         one warp brings the pages in (one bulk copy per page: a (page, head) record is one run of bytes), two issue the products
+//
+// What bounds it: the softmax chain, 3400 clocks a tile of 64 rows (its products take 800, exp2 512, reading 800): 4 sequences of 8192 tokens, 64
+// drafted tokens of 32 heads over 8 KV heads, d = 128, NVFP4: 93 us, 285 TFLOP/s; 16 drafted tokens of 16 heads over 4, d = 64, E4M3, 8 sequences
+// of up to 4096: 26 us, of which starting, joining and the first tiles are more than half.
 //
 // The reference of a row, its maximum at some time, moves only when a score exceeds it by more than 2^8: probabilities up to 256 fit f16 as
 // well, and neither a reduction over keys (they are in lanes) nor a pass over O is then part of an ordinary tile.
@@ -1000,9 +1004,9 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
 }
 
 // ---------------------------------------------------------------- sixteen rows or fewer: a warp by itself
-// What bounds few rows is the reading; the kernel above spends more instructions per tile on handing it from role to role than on its keys
-// (4100 a tile of 128 keys, d = 128, half of them hand-overs; 32 sequences of up to 32768 tokens, 4 rows: 200 us, whose reading takes 94).  Here nothing
-// is handed over: a warp takes 32 keys of a tile from their codes to its own maximum, sum and O, all in registers, and the four warps of
+// What should bound few rows is the reading; with the roles of the kernel above a tile costs more instructions for handing it from role to
+// role than for its keys (4100 a tile of 128 keys, d = 128, half of them hand-overs; 32 sequences of up to 32768 tokens, 4 rows: 200 us, whose
+// reading takes 94).  Here nothing is handed over (2700 a tile, 149 us; one token over 1000 keys 9.7 us instead of 11.7): a warp takes 32 keys of a tile from their codes to its own maximum, sum and O, all in registers, and the four warps of
 // a CTA meet at the end of an item.
 //
 // The operands of the 16 x 8 x 16 products stay where they are loaded, because the orders of keys and of d are free:
@@ -1552,6 +1556,9 @@ int launch_warps(const TreeParams& p, cudaStream_t st) {
 }
 template <int FMT, int D>
 int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
+  // Few rows by warps, more by roles.  32 to 256 rows in tiles of sixteen by warps | by roles, us: 32 rows 8 x 4096 tokens d = 128 41 | 24, one
+  // sequence of 1000 tokens 18 | 13; 64 rows 81 | 42, 22 | 16; 256 rows 265 | 114, 39 | 26; E4M3 alike (d = 64: 1.1 to 1.3 times).  16 rows:
+  // 4 of them took 200 | 149 us by roles | by warps.
   if (p.rows <= 8) return launch_warps<FMT, D, 1>(p, st);
   if (R == 16) return launch_warps<FMT, D, 2>(p, st);
   return R == 32 ? launch_tree<FMT, D, 32>(p, st) : launch_tree<FMT, D, 64>(p, st);
