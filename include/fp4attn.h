@@ -493,9 +493,10 @@ int fp4attn_cache_read(const fp4attn_cache* cache, const fp4attn_view* k_out, co
  *
  * The sequence's first context[b] tokens are seen by every row.  The T tokens themselves stand in the cache behind them, at
  * positions context[b] + j, and row t sees those whose bit j of tree_mask[b, t] is set (u64 [B, T]: a tree of drafted tokens;
- * NULL: j <= t).  T = 1 is the step of one token.  count (int32 [B], NULL: T): rows t >= count[b] are not written.
- * A row that sees nothing is O = 0, LSE = -infinity.  Positions without a page are seen by no row, and reported.  Bytes of
- * positions that no row sees may hold anything.
+ * NULL: j <= t).  T = 1 is the step of one token.  count (int32 [B], NULL: T): rows t >= count[b] are not written; of an entry
+ * with count[b] <= 0 (a batch padded to its size) nothing is read.
+ * A row that sees nothing is O = 0, LSE = -infinity.  Positions without a page are seen by no row, and reported if they are below
+ * context[b] + count[b].  Bytes of positions that no row sees may hold anything.
  *
  * Scores, row maxima and sums are fp32; K, V and Q enter the products exactly (as f16, Q scaled by a power of two per row),
  * probabilities rounded to f16.  softmax_scale 0: 1 / sqrt(d).  T up to 64.  workspace: device memory of the queried size,

@@ -327,7 +327,8 @@ def fp4attn_tree_attention(q: torch.Tensor, cache: QuantizedCache, block_table: 
     """Attention of T <= 64 tokens of every sequence over the cache: q [B,H,T,d] (bf16 or fp16) -> (O of q's type [B,H,T,d], LSE fp32
     [B,H,T]).  The T tokens are in the cache, behind the first context[b] (int32 [B]); every row sees those, and of the T tokens those
     whose bit of tree_mask (int64 [B,T]) is set - None: its own and the ones before it.  A row that sees nothing is 0, its LSE
-    -infinity.  Rows t >= count[b] are left as they were (0 and -infinity in tensors that this call made)."""
+    -infinity.  Rows t >= count[b] are left as they were (0 and -infinity in tensors that this call made); a batch padded to its size
+    has entries with count 0, which need no pages."""
     return (_native_module or _native()).tree_attention(q, cache, block_table, context, tree_mask, count, softmax_scale, out, lse, status)
 
 

@@ -446,6 +446,8 @@ struct Strided {
     return true;
   }
 };
+// the shape `sizes`, or None
+bool shaped(PyObject* o, at::IntArrayRef sizes) { return o == Py_None || (THPVariable_Check(o) && THPVariable_Unpack(o).sizes() == sizes); }
 // a contiguous tensor of `n` values of `type` on `device`, or None where that is allowed
 bool plain(PyObject* o, at::ScalarType type, int64_t n, c10::Device device, bool optional, void** ptr) {
   *ptr = nullptr;
@@ -541,7 +543,7 @@ PyObject* py_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!two && args[8] != Py_None) return assertion("k_out is given but k is not");
   const c10::Device device = x[0].t->device();
   void *positions, *freq = nullptr;
-  if (!plain(args[2], at::kInt, (int64_t)x[0].B * x[0].N, device, false, &positions))
+  if (!plain(args[2], at::kInt, (int64_t)x[0].B * x[0].N, device, false, &positions) || !shaped(args[2], {x[0].B, x[0].N}))
     return assertion("positions must be a contiguous CUDA int32 tensor [B, N] on q's device");
   const int64_t pairs = THPVariable_Check(args[3]) ? THPVariable_Unpack(args[3]).numel() : 0;
   if (pairs < 1 || pairs > INT32_MAX / 2 || !plain(args[3], at::kFloat, pairs, device, false, &freq))
@@ -577,7 +579,7 @@ PyObject* py_cache_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Batch batch;
   if (const char* wrong = batch.take(k.B, cache.device, args[3], args[4], args[5], args[10])) return assertion(wrong);
   void *positions, *freq = nullptr;
-  if (!plain(args[6], at::kInt, (int64_t)k.B * k.N, cache.device, true, &positions))
+  if (!plain(args[6], at::kInt, (int64_t)k.B * k.N, cache.device, true, &positions) || !shaped(args[6], {k.B, k.N}))
     return assertion("positions must be a contiguous CUDA int32 tensor [B, N] on the cache's device");
   int64_t pairs = 0;
   if (args[7] != Py_None) {
@@ -652,12 +654,13 @@ PyObject* py_tree_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Batch batch;
   if (const char* wrong = batch.take(q.B, cache.device, args[2], args[3], args[5], args[9])) return assertion(wrong);
   void *mask, *out_ptr, *lse_ptr;
-  if (!plain(args[4], at::kLong, (int64_t)q.B * q.N, cache.device, true, &mask))
+  if (!plain(args[4], at::kLong, (int64_t)q.B * q.N, cache.device, true, &mask) || !shaped(args[4], {q.B, q.N}))
     return assertion("tree_mask must be a contiguous CUDA int64 tensor [B, T] on the cache's device");
   float scale;
   if (!number(args[6], &scale)) return nullptr;
   const int64_t rows = (int64_t)q.B * q.H * q.N;
-  if (!plain(args[7], q.t->scalar_type(), rows * q.d, cache.device, true, &out_ptr) || !plain(args[8], at::kFloat, rows, cache.device, true, &lse_ptr))
+  if (!plain(args[7], q.t->scalar_type(), rows * q.d, cache.device, true, &out_ptr) || !shaped(args[7], {q.B, q.H, q.N, q.d}) ||
+      !plain(args[8], at::kFloat, rows, cache.device, true, &lse_ptr) || !shaped(args[8], {q.B, q.H, q.N}))
     return assertion("out [B, H, T, d] of q's type and lse [B, H, T] float32 must be contiguous CUDA tensors on the cache's device");
   const c10::cuda::OptionalCUDAGuard guard(cache.device);
   const size_t nw = g_api.tree_workspace_bytes(q.B, q.H, cache.c.kv_heads, q.N, q.d);

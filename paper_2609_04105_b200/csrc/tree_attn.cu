@@ -68,13 +68,17 @@ struct Walk {
   int b, u;                                // batch entry, (KV head, row tile)
   int first, left;                         // first key of the tile, tiles of the item from here on
   int ctx, len;                            // context, keys (context and drafted tokens) that the table has room for
+  int need;                                // keys that are there: a page that the table does not have among them is reported
 };
-__device__ __forceinline__ int load_entry(Walk& w, const TreeParams& p) {   // tiles of an item
-  const long long room = (long long)p.cache.max_pages << p.cache.log_page;
-  const int c = max(0, __ldg(p.context + w.b));
-  w.ctx = (int)min((long long)c, room);
-  w.len = (int)min((long long)c + p.T, room);
-  return (w.len + kTile - 1) / kTile;
+// drafted tokens that entry b has
+__device__ __forceinline__ int drafted(const TreeParams& p, int b) { return p.count ? max(0, min(__ldg(p.count + b), p.T)) : p.T; }
+// tiles of an item: one at least, of no keys, where an entry has no rows
+__device__ __forceinline__ int load_entry(Walk& w, const TreeParams& p) {
+  const int room = p.cache.max_pages << p.cache.log_page, n = drafted(p, w.b), c = n ? max(0, __ldg(p.context + w.b)) : 0;
+  w.ctx = min(c, room);
+  w.need = (int)min((long long)c + n, (long long)INT_MAX);
+  w.len = n ? (int)min((long long)c + (p.mask ? p.T : n), (long long)room) : 0;        // (a mask may look behind the count)
+  return max(1, (w.len + kTile - 1) / kTile);
 }
 __device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
 __device__ __forceinline__ void next_item(Walk& w, const TreeParams& p, int units) {
@@ -101,8 +105,6 @@ __device__ __forceinline__ int advance_by(Walk& w, const TreeParams& p, int unit
   }
   return ended;
 }
-// drafted tokens that entry b has
-__device__ __forceinline__ int drafted(const TreeParams& p, int b) { return p.count ? max(0, min(__ldg(p.count + b), p.T)) : p.T; }
 __device__ __forceinline__ unsigned long long row_mask(const TreeParams& p, int b, int t, int n) {
   if (t >= n) return 0ull;
   return p.mask ? __ldg(p.mask + (size_t)b * p.T + t) : (2ull << t) - 1;
@@ -315,6 +317,7 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
     w0.b = b;
     w0.ctx = __shfl_sync(0xffffffffu, w.ctx, b);
     w0.len = __shfl_sync(0xffffffffu, w.len, b);
+    w0.need = __shfl_sync(0xffffffffu, w.need, b);
     w0.left = __shfl_sync(0xffffffffu, nt, b);
     at = t0 < t1 ? t0 - __shfl_sync(0xffffffffu, incl - mine, b) : 0;
     __syncthreads();
@@ -381,9 +384,9 @@ struct Pages {
     page = -1;
     if (lane < slots && w.first + lane * P < w.len) {
       page = p.cache.page_of(w.b, w.first + lane * P);
-      lost |= page < 0;
+      lost |= page < 0 && w.first + lane * P < w.need;
     }
-    lost |= (long long)max(0, __ldg(p.context + w.b)) + p.T > w.len;                                       // the table has no room for the last tokens
+    lost |= w.need > w.len;                                         // the table has no room for the last tokens
   }
   __device__ __forceinline__ void bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
     const int lane = threadIdx.x & 31;
@@ -779,8 +782,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
     Walk w = w0;
     Turn<C::kSB> sb;
     Turn<C::kVB> vb;
-    int item = 0, part_first = 0, last = 0, last_phase = 0;   // last: this set's last tile, its buffer of P
-    //                       // part_first: first key of the item that this CTA takes
+    int item = 0, part_first = 0;                                   // part_first: first key of the item that this CTA takes
+    int last = 0, last_phase = 0;                                   // of this set's last tile: its buffer of P
     bool fresh = true, started = false;                             // of the item; has this set had a tile of it?
     float l[N];
     for (int i = 0; i < n_tiles; ++i) {

@@ -429,6 +429,43 @@ def test_tree_attention_drafted_tokens_that_were_not_written(fmt, H):
         cache.pages.copy_(kept)
 
 
+@pytest.mark.parametrize("H", [4, 40])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_tree_attention_padded_batch(fmt, H):
+    """Entries without rows need no pages and no context of sense; pages behind a count need not exist.  Nothing of that is an error, and
+    the other entries are as without them; a page missing below a count is reported."""
+    Bd, g = _bd(), _gen(27)
+    B, kv, T, d, P = 4, 2, 6, 128, 16
+    context, counts = [46, 2 ** 31 - 1, 128, 31], [2, 0, 6, 1]
+    cache, table = _filled(Bd, g, fmt, B, kv, P, d, 144)
+    q = _randn(g, B, H, T, d)
+    bits = torch.tensor([[1, 3, 7, 15, 31, 63]] * B, dtype=torch.int64, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    few = table.clone()
+    few[0, 3:] = -1                                             # position 48: the third drafted token
+    few[1] = -1
+    few[3, 2:] = 1 << 30
+    for mask in (None, bits):
+        got = Bd.fp4attn_tree_attention(q, cache, few, _i32(context), tree_mask=mask, count=_i32(counts), status=status)
+        assert status.item() == 0
+        for b in (0, 2, 3):
+            alone = Bd.fp4attn_tree_attention(q[b:b + 1], cache, table[b:b + 1], _i32(context[b:b + 1]), tree_mask=None if mask is None else mask[b:b + 1],
+                                              count=_i32(counts[b:b + 1]))
+            for x, y in zip(got, alone):
+                # Other splits of the keys: other references, so other roundings of each probability, by 2^-11 of it on either side,
+                # 2^-10 of sum p |v| and of the sum together 2^-9 max |v| <= 2^-6 (|v| < 6 here); then bf16's on either side, 2^-7 of the value
+                assert torch.allclose(x[b].float(), y[0].float(), rtol=2.0 ** -7, atol=2.0 ** -6)
+        assert not got[0][1].any() and torch.isneginf(got[1][1]).all()
+        few[3, 1] = -1
+        Bd.fp4attn_tree_attention(q, cache, few, _i32(context), tree_mask=mask, count=_i32(counts), status=status)
+        assert status.item() == Bd.ERR_PAGE
+        status.zero_()
+        few[3, 1] = table[3, 1]
+    # nobody there at all
+    out, lse = Bd.fp4attn_tree_attention(q, cache, torch.full_like(table, -1), _i32([7] * B), count=_i32([0, -3, 0, 0]), status=status)
+    assert status.item() == 0 and not out.any() and torch.isneginf(lse).all()
+
+
 def test_tree_attention_extreme_logits_and_queries():
     """Logits of thousands (one key takes all), rows of unlike sizes side by side, tiny and zero queries, a scale of the caller's."""
     Bd, g = _bd(), _gen(22)
@@ -595,6 +632,22 @@ def test_step_repeats_captures_and_runs_beside_another():
     graphs[0].replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(outs[0], _step(Bd, states[0])))
+
+
+def test_binding_refuses_tensors_of_another_shape():
+    """As many elements in another order of the axes are another tensor."""
+    Bd, g = _bd(), _gen(52)
+    cache, table = _filled(Bd, g, "nvfp4", 2, 2, 16, 64, 20)
+    start, f = _i32([3, 4]), Bd.fp4attn_rotary_frequencies(64)
+    q, k, pos = _randn(g, 2, 4, 3, 64), _randn(g, 2, 2, 3, 64), _i32([[0, 1, 2]] * 2)
+    bits = torch.ones(2, 3, dtype=torch.int64, device="cuda")
+    for call in (lambda: Bd.fp4attn_tree_attention(q, cache, table, start, out=torch.empty_like(q.transpose(1, 2).contiguous())),
+                 lambda: Bd.fp4attn_tree_attention(q, cache, table, start, lse=torch.empty(2, 3, 4, device="cuda")),
+                 lambda: Bd.fp4attn_tree_attention(q, cache, table, start, tree_mask=bits.t().contiguous()),
+                 lambda: Bd.fp4attn_rotary(q, pos.t().contiguous(), f), lambda: Bd.fp4attn_rotary(q, pos.flatten(), f),
+                 lambda: Bd.fp4attn_cache_write(cache, k, k, table, start, inv_freq=f, positions=pos.t().contiguous())):
+        with pytest.raises(AssertionError):
+            call()
 
 
 def test_binding_refusals_on_the_device():
