@@ -465,300 +465,300 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
   auto wait = [&](int b, int phase) { wait_phase<false>(bar(b), (uint32_t)phase, abort_at); };
 
   if (warp >= C::kProducer) {
-  registers_fewer<C::kRegsAux>();
-  if (warp == C::kProducer) {
-    // ===================================================================== pages -> shared memory
-    Pages<C::kStages, C::kStage, C::kRing, 1, false> pages;
-    pages.w = w0;
-    if (n_tiles > 0) pages.find(p);
-    while (pages.i < n_tiles) {
-      pages.bring(p, sbase + C::kOffStage, bar(C::RING_FULL), bar(C::RING_FREE), abort_at, valid_ring);
-      pages.skip(p, units, 1);
-      if (pages.i < n_tiles) pages.find(p);                         // the table's entries come while the stage is waited for
-    }
-    pages.tell(p);
-    // the last copies end before this warp does (also where the others have given up on them)
-    for (int k = 0; k < C::kStages && k < n_tiles; ++k) {
-      pages.ring.at = pages.ring.at ? pages.ring.at - 1 : (pages.ring.phase ^= 1, C::kStages - 1);
-      wait(C::RING_FULL + pages.ring.at, pages.ring.phase);
-    }
-  } else if (warp == C::kIssuerS) {
-    // ===================================================================== S^T = K Q^T
-    // Q: K-major, core matrices of 8 rows x 16 bytes, those along d neighbours.  A product takes 45 clocks or more whatever its N up to 64,
-    // and its issue waits for the one before: two warps issue, so that the waits of one lie under the products of the other.
-    constexpr uint32_t kIdesc = make_idesc_f16(128, R, false);
-    Walk w = w0;
-    Turn<C::kKB> kb;
-    Turn<C::kSB> sb;
-    Turn<C::kQB> qb;
-    bool fresh = true;
-    for (int i = 0; i < n_tiles; ++i) {
-      if (rare(fresh)) wait(C::Q_FULL + qb.at, qb.phase);
-      wait(C::S_FREE + sb.at, sb.phase ^ 1);
-      wait(C::KA_FULL + kb.at, kb.phase);
-      tc_fence_after();
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-          tc_mma_f16_ta(tmem + C::kS + R * sb.at, tmem + C::kKA + (D / 2) * kb.at + 8 * k,
-                        make_smem_desc(sbase + C::kOffQ + qb.at * C::kQ + k * 256, 128, (D / 8) * 128, kSwzNone), kIdesc, k > 0);
-        tc_commit(bar(C::S_FULL + sb.at));
-        tc_commit(bar(C::KA_FREE + kb.at));
+    registers_fewer<C::kRegsAux>();
+    if (warp == C::kProducer) {
+      // ===================================================================== pages -> shared memory
+      Pages<C::kStages, C::kStage, C::kRing, 1, false> pages;
+      pages.w = w0;
+      if (n_tiles > 0) pages.find(p);
+      while (pages.i < n_tiles) {
+        pages.bring(p, sbase + C::kOffStage, bar(C::RING_FULL), bar(C::RING_FREE), abort_at, valid_ring);
+        pages.skip(p, units, 1);
+        if (pages.i < n_tiles) pages.find(p);                         // the table's entries come while the stage is waited for
       }
-      __syncwarp();
-      kb.next();
-      sb.next();
-      fresh = advance(w, p, units);
-      if (rare(fresh)) qb.next();
-    }
-    if (elect_one()) tc_commit(bar(C::DRAIN));
-    __syncwarp();
-  } else if (warp == C::kIssuerO) {
-    // ===================================================================== O^T += V^T P^T
-    // P: rows are contiguous (MN-major), core matrices of 8 keys x 16 bytes (8 rows), those along rows neighbours
-    constexpr uint32_t kIdesc = make_idesc_f16(128, R, true);
-    Walk w = w0;
-    int of_item = 0;                                                // tiles of the item so far
-    Turn<C::kVB> vb;
-    for (int i = 0; i < n_tiles; ++i) {
-      wait(C::VA_FULL + vb.at, vb.phase);
-      wait(C::P_FULL + vb.at, vb.phase);
-      tc_fence_after();
-      const uint32_t more = of_item >= C::kSets;                    // not the first tile of the item that this O gets
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          tc_mma_f16_ta(tmem + C::kO + (C::kSets == 2 ? R * (i & 1) : 0), tmem + C::kVA + 64 * vb.at + 8 * k,
-                        make_smem_desc(sbase + C::kOffP + vb.at * C::kP + k * 2 * (R / 8) * 128, (R / 8) * 128, 128, kSwzNone), kIdesc,
-                        k > 0 ? 1u : more);
-        tc_commit(bar(C::PV_DONE + vb.at));
+      pages.tell(p);
+      // the last copies end before this warp does (also where the others have given up on them)
+      for (int k = 0; k < C::kStages && k < n_tiles; ++k) {
+        pages.ring.at = pages.ring.at ? pages.ring.at - 1 : (pages.ring.phase ^= 1, C::kStages - 1);
+        wait(C::RING_FULL + pages.ring.at, pages.ring.phase);
       }
-      __syncwarp();
-      vb.next();
-      of_item = advance(w, p, units) ? 0 : of_item + 1;
-    }
-    if (elect_one()) tc_commit(bar(C::DRAIN + 1));
-    __syncwarp();
-  }
-  } else if (warp < C::kFirstSoftmax) {
-  registers_fewer<C::kRegsKV>();
-  if (warp < C::kFirstV) {
-    // ===================================================================== Q and K
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const int group = warp >> 2, quarter = warp & 3;
-    const int key = quarter * 32 + lane, slot = key >> p.cache.log_page, t = key & (P - 1);
-    const float c0 = p.scale * 1.4426950408889634f;
-    Walk w = w0;
-    Turn<C::kStages> ring;
-    Turn<C::kKB> kb;
-    int item = 0;
-    bool fresh = true;
-    if (group && n_tiles > 0) {
-      item = advance_by(w, p, units, group, &fresh);
-      ring.next(group);
-      kb.next(group);
-    }
-    for (int i = group; i < n_tiles; i += C::kKGroups) {
-      wait(C::KA_FREE + kb.at, kb.phase ^ 1);
-      if (rare(fresh)) {
-        // Rows scaled by a power of two into f16's range (the largest element to [2^14, 2^15)): exact for 8-bit significands, and a row's
-        // scores are scaled back by its constant.  The buffer is free: as many items back, the last tile that read it was tile i - kKB or
-        // an earlier one, whose product is done.
-        const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R, qb = item % C::kQB;
-        const float c = __fdiv_rn(c0, __ldg(p.cache.k_G + kvh));
-        constexpr int kParts = D / 16;                              // threads of a row
-#pragma unroll
-        for (int j = key; j < R * kParts; j += 128) {
-          const int r = j / kParts, e = (j % kParts) * 16, row = row0 + r;
-          float v[16];
-#pragma unroll
-          for (int x = 0; x < 16; ++x) v[x] = 0.f;
-          if (row < p.rows) {
-            const int hl = row / p.T, tok = row - hl * p.T;
-            const uint16_t* q = static_cast<const uint16_t*>(p.q) + w.b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
-            uint32_t raw[8];
-            if (p.q_vector) {
-              *reinterpret_cast<uint4*>(raw) = __ldg(reinterpret_cast<const uint4*>(q));
-              *reinterpret_cast<uint4*>(raw + 4) = __ldg(reinterpret_cast<const uint4*>(q) + 1);
-            } else {
-#pragma unroll
-              for (int x = 0; x < 8; ++x) raw[x] = (uint32_t)__ldg(q + 2 * x) | (uint32_t)__ldg(q + 2 * x + 1) << 16;
-            }
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              const float2 f = p.half ? unpack16<true>(raw[x]) : unpack16<false>(raw[x]);
-              v[2 * x] = f.x;
-              v[2 * x + 1] = f.y;
-            }
-          }
-          float a = 0.f;
-#pragma unroll
-          for (int x = 0; x < 16; ++x) a = fmaxf(a, fabsf(v[x]));
-#pragma unroll
-          for (int x = 1; x < kParts; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
-          const uint32_t up = row_exponent(a);
-          const float f = __uint_as_float(up << 23);
-          uint32_t h[8];
-#pragma unroll
-          for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(v[2 * x] * f, v[2 * x + 1] * f);
-          uint8_t* const dst = sgen + C::kOffQ + qb * C::kQ + ((r >> 3) * (D / 8) + (e >> 3)) * 128 + (r & 7) * 16;
-          *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(dst + 128) = make_uint4(h[4], h[5], h[6], h[7]);
-          if (e == 0) reinterpret_cast<float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * R + r] = c * __uint_as_float((254u - up) << 23);
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::Q_FULL + qb));
-      }
-      wait(C::RING_FULL + ring.at, ring.phase);
-      {
+    } else if (warp == C::kIssuerS) {
+      // ===================================================================== S^T = K Q^T
+      // Q: K-major, core matrices of 8 rows x 16 bytes, those along d neighbours.  A product takes 45 clocks or more whatever its N up to 64,
+      // and its issue waits for the one before: two warps issue, so that the waits of one lie under the products of the other.
+      constexpr uint32_t kIdesc = make_idesc_f16(128, R, false);
+      Walk w = w0;
+      Turn<C::kKB> kb;
+      Turn<C::kSB> sb;
+      Turn<C::kQB> qb;
+      bool fresh = true;
+      for (int i = 0; i < n_tiles; ++i) {
+        if (rare(fresh)) wait(C::Q_FULL + qb.at, qb.phase);
+        wait(C::S_FREE + sb.at, sb.phase ^ 1);
+        wait(C::KA_FULL + kb.at, kb.phase);
         tc_fence_after();
-        const uint8_t* const rec = sgen + C::kOffStage + ring.at * C::kStage + slot * p.cache.record;
-        const uint32_t dst = tmem + lanes + C::kKA + (D / 2) * kb.at;
-        // (rolled loops: what the four roles of a scheduler run in turn has to stay in its instruction cache)
-        const uint8_t* codes = rec + t * 16;
-        uint2 sw = make_uint2(0u, 0u);
-        if (L::kFp4 && D == 128) sw = *reinterpret_cast<const uint2*>(rec + L::k_scales(P) + t * L::kScales);
-        if (L::kFp4 && D == 64) sw.x = *reinterpret_cast<const uint32_t*>(rec + L::k_scales(P) + t * L::kScales);
-#pragma unroll 2
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t h[16];
-          if (L::kFp4) {
-            const uint4 raw = *reinterpret_cast<const uint4*>(codes);
-            codes += P * 16;
-            const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w}, two = cvt_f16x2_e4m3x2(sw.x & 0xFFFFu);
-            sw.x = __funnelshift_r(sw.x, sw.y, 16);
-            sw.y >>= 16;
+        if (elect_one()) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const uint32_t f = splat_half(two, x >> 1);
-              cvt_f16x2_e2m1x8(words[x], h + 4 * x);
+          for (int k = 0; k < D / 16; ++k)
+            tc_mma_f16_ta(tmem + C::kS + R * sb.at, tmem + C::kKA + (D / 2) * kb.at + 8 * k,
+                          make_smem_desc(sbase + C::kOffQ + qb.at * C::kQ + k * 256, 128, (D / 8) * 128, kSwzNone), kIdesc, k > 0);
+          tc_commit(bar(C::S_FULL + sb.at));
+          tc_commit(bar(C::KA_FREE + kb.at));
+        }
+        __syncwarp();
+        kb.next();
+        sb.next();
+        fresh = advance(w, p, units);
+        if (rare(fresh)) qb.next();
+      }
+      if (elect_one()) tc_commit(bar(C::DRAIN));
+      __syncwarp();
+    } else if (warp == C::kIssuerO) {
+      // ===================================================================== O^T += V^T P^T
+      // P: rows are contiguous (MN-major), core matrices of 8 keys x 16 bytes (8 rows), those along rows neighbours
+      constexpr uint32_t kIdesc = make_idesc_f16(128, R, true);
+      Walk w = w0;
+      int of_item = 0;                                                // tiles of the item so far
+      Turn<C::kVB> vb;
+      for (int i = 0; i < n_tiles; ++i) {
+        wait(C::VA_FULL + vb.at, vb.phase);
+        wait(C::P_FULL + vb.at, vb.phase);
+        tc_fence_after();
+        const uint32_t more = of_item >= C::kSets;                    // not the first tile of the item that this O gets
+        if (elect_one()) {
 #pragma unroll
-              for (int y = 0; y < 4; ++y) h[4 * x + y] = mul_half2(h[4 * x + y], f);
+          for (int k = 0; k < kTile / 16; ++k)
+            tc_mma_f16_ta(tmem + C::kO + (C::kSets == 2 ? R * (i & 1) : 0), tmem + C::kVA + 64 * vb.at + 8 * k,
+                          make_smem_desc(sbase + C::kOffP + vb.at * C::kP + k * 2 * (R / 8) * 128, (R / 8) * 128, 128, kSwzNone), kIdesc,
+                          k > 0 ? 1u : more);
+          tc_commit(bar(C::PV_DONE + vb.at));
+        }
+        __syncwarp();
+        vb.next();
+        of_item = advance(w, p, units) ? 0 : of_item + 1;
+      }
+      if (elect_one()) tc_commit(bar(C::DRAIN + 1));
+      __syncwarp();
+    }
+  } else if (warp < C::kFirstSoftmax) {
+    registers_fewer<C::kRegsKV>();
+    if (warp < C::kFirstV) {
+      // ===================================================================== Q and K
+      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+      const int group = warp >> 2, quarter = warp & 3;
+      const int key = quarter * 32 + lane, slot = key >> p.cache.log_page, t = key & (P - 1);
+      const float c0 = p.scale * 1.4426950408889634f;
+      Walk w = w0;
+      Turn<C::kStages> ring;
+      Turn<C::kKB> kb;
+      int item = 0;
+      bool fresh = true;
+      if (group && n_tiles > 0) {
+        item = advance_by(w, p, units, group, &fresh);
+        ring.next(group);
+        kb.next(group);
+      }
+      for (int i = group; i < n_tiles; i += C::kKGroups) {
+        wait(C::KA_FREE + kb.at, kb.phase ^ 1);
+        if (rare(fresh)) {
+          // Rows scaled by a power of two into f16's range (the largest element to [2^14, 2^15)): exact for 8-bit significands, and a row's
+          // scores are scaled back by its constant.  The buffer is free: as many items back, the last tile that read it was tile i - kKB or
+          // an earlier one, whose product is done.
+          const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R, qb = item % C::kQB;
+          const float c = __fdiv_rn(c0, __ldg(p.cache.k_G + kvh));
+          constexpr int kParts = D / 16;                              // threads of a row
+#pragma unroll
+          for (int j = key; j < R * kParts; j += 128) {
+            const int r = j / kParts, e = (j % kParts) * 16, row = row0 + r;
+            float v[16];
+#pragma unroll
+            for (int x = 0; x < 16; ++x) v[x] = 0.f;
+            if (row < p.rows) {
+              const int hl = row / p.T, tok = row - hl * p.T;
+              const uint16_t* q = static_cast<const uint16_t*>(p.q) + w.b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
+              uint32_t raw[8];
+              if (p.q_vector) {
+                *reinterpret_cast<uint4*>(raw) = __ldg(reinterpret_cast<const uint4*>(q));
+                *reinterpret_cast<uint4*>(raw + 4) = __ldg(reinterpret_cast<const uint4*>(q) + 1);
+              } else {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) raw[x] = (uint32_t)__ldg(q + 2 * x) | (uint32_t)__ldg(q + 2 * x + 1) << 16;
+              }
+#pragma unroll
+              for (int x = 0; x < 8; ++x) {
+                const float2 f = p.half ? unpack16<true>(raw[x]) : unpack16<false>(raw[x]);
+                v[2 * x] = f.x;
+                v[2 * x + 1] = f.y;
+              }
             }
-          } else {
+            float a = 0.f;
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
+            for (int x = 0; x < 16; ++x) a = fmaxf(a, fabsf(v[x]));
+#pragma unroll
+            for (int x = 1; x < kParts; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
+            const uint32_t up = row_exponent(a);
+            const float f = __uint_as_float(up << 23);
+            uint32_t h[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(v[2 * x] * f, v[2 * x + 1] * f);
+            uint8_t* const dst = sgen + C::kOffQ + qb * C::kQ + ((r >> 3) * (D / 8) + (e >> 3)) * 128 + (r & 7) * 16;
+            *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4*>(dst + 128) = make_uint4(h[4], h[5], h[6], h[7]);
+            if (e == 0) reinterpret_cast<float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * R + r] = c * __uint_as_float((254u - up) << 23);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::Q_FULL + qb));
+        }
+        wait(C::RING_FULL + ring.at, ring.phase);
+        {
+          tc_fence_after();
+          const uint8_t* const rec = sgen + C::kOffStage + ring.at * C::kStage + slot * p.cache.record;
+          const uint32_t dst = tmem + lanes + C::kKA + (D / 2) * kb.at;
+          // (rolled loops: what the four roles of a scheduler run in turn has to stay in its instruction cache)
+          const uint8_t* codes = rec + t * 16;
+          uint2 sw = make_uint2(0u, 0u);
+          if (L::kFp4 && D == 128) sw = *reinterpret_cast<const uint2*>(rec + L::k_scales(P) + t * L::kScales);
+          if (L::kFp4 && D == 64) sw.x = *reinterpret_cast<const uint32_t*>(rec + L::k_scales(P) + t * L::kScales);
+#pragma unroll 2
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t h[16];
+            if (L::kFp4) {
               const uint4 raw = *reinterpret_cast<const uint4*>(codes);
               codes += P * 16;
-              const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+              const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w}, two = cvt_f16x2_e4m3x2(sw.x & 0xFFFFu);
+              sw.x = __funnelshift_r(sw.x, sw.y, 16);
+              sw.y >>= 16;
 #pragma unroll
-              for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(words[x], h + 8 * y + 2 * x);
-            }
-          }
-          tmem_st_32x32b_x16(dst + 16 * c, h);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));   // (the loads are done: their values have been used)
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::KA_FULL + kb.at));
-      }
-      ring.next(C::kKGroups);
-      kb.next(C::kKGroups);
-      item += advance_by(w, p, units, C::kKGroups, &fresh);
-    }
-  } else {
-    // ===================================================================== V
-    const int quarter = warp & 3, group = (warp - C::kFirstV) >> 2, e = quarter * 32 + lane;      // index of the head dimension
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    uint8_t* const scales = sgen + C::kOffVScale + (warp - C::kFirstV) * 512;
-    // this lane's codes in a stage: chunks of sixteen tokens, further in the page or at the same place of the next
-    const int log_page = p.cache.log_page, record = p.cache.record;
-    const uint32_t codes0 = (uint32_t)(L::v_codes(P) + (L::kFp4 ? e >> 1 : e) * 16);
-    const uint32_t step16 = P == 16 ? (uint32_t)record : 16 * L::kRow;
-    const uint32_t step32 = P <= 32 ? (uint32_t)((32 >> log_page) * record) : 32 * L::kRow;
-    const uint32_t step64 = P <= 64 ? (uint32_t)((64 >> log_page) * record) : 64 * L::kRow;
-    const int at_sc = 8 * (lane & 15);                              // eight tokens whose scales of block e / 16 this lane converts
-    const uint32_t scale0 = (uint32_t)((at_sc >> log_page) * record + L::v_scales(P) + (e >> 4) * P + (at_sc & (P - 1)));
-    Walk w = w0;
-    Turn<C::kStages> ring;
-    Turn<C::kVB> vb;
-    int b_of = -1;
-    unsigned long long seen = 0;                                    // drafted tokens that some row sees
-    bool fresh;
-    if (group && n_tiles > 0) {
-      advance_by(w, p, units, group, &fresh);
-      ring.next(group);
-      vb.next(group);
-    }
-    for (int i = group; i < n_tiles; i += C::kVGroups) {
-      if (rare(w.b != b_of)) {
-        b_of = w.b;
-        const int n = drafted(p, w.b);
-        seen = row_mask(p, w.b, lane, n) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n) : 0ull);
-        seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
-      }
-      wait(C::PV_DONE + vb.at, vb.phase ^ 1);
-      wait(C::RING_FULL + ring.at, ring.phase);
-      {
-        tc_fence_after();
-        const uint32_t held = valid_ring[i % C::kRing];
-        const int first = w.first;
-        // what no row sees counts as zero: it may be any bytes, and a probability of 0 times a NaN would be one
-        const bool all = first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
-        const uint8_t* const stage = sgen + C::kOffStage + ring.at * C::kStage;
-        const uint32_t dst = tmem + lanes + C::kVA + 64 * vb.at, shift = 4 * (e & 1);
-        if (quarter * 32 < D) {
-          if (L::kFp4) {
-            // the scales of this warp's two blocks, once for all sixteen lanes that need them
-            uint2 sc = *reinterpret_cast<const uint2*>(stage + scale0);
-            if (rare(!all)) {
-              const uint32_t v = held >> (at_sc >> log_page) & 1 ? permute_eight(valid_eight(w, seen, first + at_sc)) : 0u;
-              sc.x &= byte_mask(v);
-              sc.y &= byte_mask(v >> 4);
-            }
-            uint32_t f[4];
-            cvt_f16x2_e4m3x4(sc.x, f);
-            cvt_f16x2_e4m3x4(sc.y, f + 2);
-            *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(f[0], f[1], f[2], f[3]);
-            __syncwarp();
-          }
-          const uint8_t* codes = stage + codes0;
-          const uint8_t* factors = scales + (lane >> 4) * 256;
-#pragma unroll 2
-          for (int j = 0; j < kTile; j += 16) {                     // sixteen tokens
-            uint4 raw = *reinterpret_cast<const uint4*>(j & 16 ? codes + step16 : codes);
-            if (j & 16) codes = j & 32 ? stage + codes0 + step64 : codes + step32;
-            uint32_t h[8];
-            if (L::kFp4) {
-              const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
+              for (int x = 0; x < 4; ++x) {
+                const uint32_t f = splat_half(two, x >> 1);
+                cvt_f16x2_e2m1x8(words[x], h + 4 * x);
 #pragma unroll
-              for (int x = 0; x < 2; ++x) {                         // eight tokens: i and i + 4 in a byte
-                const uint4 f = *reinterpret_cast<const uint4*>(factors + 2 * j + 16 * x);
-                cvt_f16x2_e2m1x8((cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u), h + 4 * x);
-                h[4 * x] = mul_half2(h[4 * x], f.x);
-                h[4 * x + 1] = mul_half2(h[4 * x + 1], f.y);
-                h[4 * x + 2] = mul_half2(h[4 * x + 2], f.z);
-                h[4 * x + 3] = mul_half2(h[4 * x + 3], f.w);
+                for (int y = 0; y < 4; ++y) h[4 * x + y] = mul_half2(h[4 * x + y], f);
               }
             } else {
-              if (rare(!all)) {
-                const bool here = held >> (j >> log_page) & 1;
-                const uint32_t lo = here ? valid_eight(w, seen, first + j) : 0u;
-                const uint32_t hi = here ? valid_eight(w, seen, first + j + 8) : 0u;
-                raw.x &= byte_mask(lo); raw.y &= byte_mask(lo >> 4); raw.z &= byte_mask(hi); raw.w &= byte_mask(hi >> 4);
-              }
-              const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-              for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(cw[x], h + 2 * x);
+              for (int y = 0; y < 2; ++y) {
+                const uint4 raw = *reinterpret_cast<const uint4*>(codes);
+                codes += P * 16;
+                const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(words[x], h + 8 * y + 2 * x);
+              }
             }
-            tmem_st_32x32b_x8(dst + (j >> 1), h);
+            tmem_st_32x32b_x16(dst + 16 * c, h);
           }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));   // (the loads are done: their values have been used)
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::KA_FULL + kb.at));
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::VA_FULL + vb.at));
+        ring.next(C::kKGroups);
+        kb.next(C::kKGroups);
+        item += advance_by(w, p, units, C::kKGroups, &fresh);
       }
-      ring.next(C::kVGroups);
-      vb.next(C::kVGroups);
-      advance_by(w, p, units, C::kVGroups, &fresh);
+    } else {
+      // ===================================================================== V
+      const int quarter = warp & 3, group = (warp - C::kFirstV) >> 2, e = quarter * 32 + lane;      // index of the head dimension
+      const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+      uint8_t* const scales = sgen + C::kOffVScale + (warp - C::kFirstV) * 512;
+      // this lane's codes in a stage: chunks of sixteen tokens, further in the page or at the same place of the next
+      const int log_page = p.cache.log_page, record = p.cache.record;
+      const uint32_t codes0 = (uint32_t)(L::v_codes(P) + (L::kFp4 ? e >> 1 : e) * 16);
+      const uint32_t step16 = P == 16 ? (uint32_t)record : 16 * L::kRow;
+      const uint32_t step32 = P <= 32 ? (uint32_t)((32 >> log_page) * record) : 32 * L::kRow;
+      const uint32_t step64 = P <= 64 ? (uint32_t)((64 >> log_page) * record) : 64 * L::kRow;
+      const int at_sc = 8 * (lane & 15);                              // eight tokens whose scales of block e / 16 this lane converts
+      const uint32_t scale0 = (uint32_t)((at_sc >> log_page) * record + L::v_scales(P) + (e >> 4) * P + (at_sc & (P - 1)));
+      Walk w = w0;
+      Turn<C::kStages> ring;
+      Turn<C::kVB> vb;
+      int b_of = -1;
+      unsigned long long seen = 0;                                    // drafted tokens that some row sees
+      bool fresh;
+      if (group && n_tiles > 0) {
+        advance_by(w, p, units, group, &fresh);
+        ring.next(group);
+        vb.next(group);
+      }
+      for (int i = group; i < n_tiles; i += C::kVGroups) {
+        if (rare(w.b != b_of)) {
+          b_of = w.b;
+          const int n = drafted(p, w.b);
+          seen = row_mask(p, w.b, lane, n) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n) : 0ull);
+          seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
+        }
+        wait(C::PV_DONE + vb.at, vb.phase ^ 1);
+        wait(C::RING_FULL + ring.at, ring.phase);
+        {
+          tc_fence_after();
+          const uint32_t held = valid_ring[i % C::kRing];
+          const int first = w.first;
+          // what no row sees counts as zero: it may be any bytes, and a probability of 0 times a NaN would be one
+          const bool all = first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
+          const uint8_t* const stage = sgen + C::kOffStage + ring.at * C::kStage;
+          const uint32_t dst = tmem + lanes + C::kVA + 64 * vb.at, shift = 4 * (e & 1);
+          if (quarter * 32 < D) {
+            if (L::kFp4) {
+              // the scales of this warp's two blocks, once for all sixteen lanes that need them
+              uint2 sc = *reinterpret_cast<const uint2*>(stage + scale0);
+              if (rare(!all)) {
+                const uint32_t v = held >> (at_sc >> log_page) & 1 ? permute_eight(valid_eight(w, seen, first + at_sc)) : 0u;
+                sc.x &= byte_mask(v);
+                sc.y &= byte_mask(v >> 4);
+              }
+              uint32_t f[4];
+              cvt_f16x2_e4m3x4(sc.x, f);
+              cvt_f16x2_e4m3x4(sc.y, f + 2);
+              *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(f[0], f[1], f[2], f[3]);
+              __syncwarp();
+            }
+            const uint8_t* codes = stage + codes0;
+            const uint8_t* factors = scales + (lane >> 4) * 256;
+#pragma unroll 2
+            for (int j = 0; j < kTile; j += 16) {                     // sixteen tokens
+              uint4 raw = *reinterpret_cast<const uint4*>(j & 16 ? codes + step16 : codes);
+              if (j & 16) codes = j & 32 ? stage + codes0 + step64 : codes + step32;
+              uint32_t h[8];
+              if (L::kFp4) {
+                const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {                         // eight tokens: i and i + 4 in a byte
+                  const uint4 f = *reinterpret_cast<const uint4*>(factors + 2 * j + 16 * x);
+                  cvt_f16x2_e2m1x8((cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u), h + 4 * x);
+                  h[4 * x] = mul_half2(h[4 * x], f.x);
+                  h[4 * x + 1] = mul_half2(h[4 * x + 1], f.y);
+                  h[4 * x + 2] = mul_half2(h[4 * x + 2], f.z);
+                  h[4 * x + 3] = mul_half2(h[4 * x + 3], f.w);
+                }
+              } else {
+                if (rare(!all)) {
+                  const bool here = held >> (j >> log_page) & 1;
+                  const uint32_t lo = here ? valid_eight(w, seen, first + j) : 0u;
+                  const uint32_t hi = here ? valid_eight(w, seen, first + j + 8) : 0u;
+                  raw.x &= byte_mask(lo); raw.y &= byte_mask(lo >> 4); raw.z &= byte_mask(hi); raw.w &= byte_mask(hi >> 4);
+                }
+                const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(cw[x], h + 2 * x);
+              }
+              tmem_st_32x32b_x8(dst + (j >> 1), h);
+            }
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::VA_FULL + vb.at));
+        }
+        ring.next(C::kVGroups);
+        vb.next(C::kVGroups);
+        advance_by(w, p, units, C::kVGroups, &fresh);
+      }
     }
-  }
   } else {
     // ===================================================================== softmax
     registers_more<C::kRegsSoftmax>();
@@ -1009,8 +1009,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
 // ---------------------------------------------------------------- sixteen rows or fewer: a warp by itself
 // What should bound few rows is the reading; with the roles of the kernel above a tile costs more instructions for handing it from role to
 // role than for its keys (4100 a tile of 128 keys, d = 128, half of them hand-overs; 32 sequences of up to 32768 tokens, 4 rows: 200 us, whose
-// reading takes 94).  Here nothing is handed over (2700 a tile, 149 us; one token over 1000 keys 9.7 us instead of 11.7): a warp takes 32 keys of a tile from their codes to its own maximum, sum and O, all in registers, and the four warps of
-// a CTA meet at the end of an item.
+// reading takes 94).  Here nothing is handed over (2700 a tile, 149 us; one token over 1000 keys 9.8 us instead of 11.7): a warp takes 32 keys
+// of a tile from their codes to its own maximum, sum and O, all in registers, and the four warps of a CTA meet at the end of an item.
 //
 // The operands of the 16 x 8 x 16 products stay where they are loaded, because the orders of keys and of d are free:
 //   S^T = K Q^T   A: keys x d, twice sixteen keys.  Lane (r, c) = (lane / 4, lane % 4) has keys r and r + 8: it takes D / 4 elements of either
@@ -1079,8 +1079,8 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
   const int P = 1 << p.cache.log_page;
 
   // K and V of the first tiles; then the warps take turns, each bringing what takes the place of the K or V before the one they have just
-  // been through (of that one the other warps may not be through yet).  A warp that fills a stage has itself been through what stood there before: the stage's barrier cannot be further back
-  // than a wait by parity can tell.
+  // been through (of that one the other warps may not be through yet).  A warp that fills a stage has itself been through what stood there
+  // before: the stage's barrier cannot be further back than a wait by parity can tell.
   Pages<C::kStages, C::kStage, C::kStages, 2, true> pages;
   pages.w = w0;
   const int n_parts = n_tiles > INT_MAX / 2 ? INT_MAX : 2 * n_tiles;
