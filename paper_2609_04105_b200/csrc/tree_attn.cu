@@ -21,7 +21,7 @@
 //   then         one warp brings the pages in (one bulk copy per page: a (page, head) record is one run of bytes), two issue the products
 //
 // What bounds it: the softmax chain, 3400 clocks a tile of 64 rows (its products take 800, exp2 512, reading 800): 4 sequences of 8192 tokens, 64
-// drafted tokens of 32 heads over 8 KV heads, d = 128, NVFP4: 93 us, 285 TFLOP/s; 16 drafted tokens of 16 heads over 4, d = 64, E4M3, 8 sequences
+// drafted tokens of 32 heads over 8 KV heads, d = 128, NVFP4: 97 us, 273 TFLOP/s; 16 drafted tokens of 16 heads over 4, d = 64, E4M3, 8 sequences
 // of up to 4096: 26 us, of which starting, joining and the first tiles are more than half.
 //
 // The reference of a row, its maximum at some time, moves only when a score exceeds it by more than 2^8: probabilities up to 256 fit f16 as
@@ -1009,7 +1009,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
 // ---------------------------------------------------------------- sixteen rows or fewer: a warp by itself
 // What should bound few rows is the reading; with the roles of the kernel above a tile costs more instructions for handing it from role to
 // role than for its keys (4100 a tile of 128 keys, d = 128, half of them hand-overs; 32 sequences of up to 32768 tokens, 4 rows: 200 us, whose
-// reading takes 94).  Here nothing is handed over (2700 a tile, 149 us; one token over 1000 keys 9.8 us instead of 11.7): a warp takes 32 keys
+// reading takes 94).  Here nothing is handed over (2700 a tile, 152 us; one token over 1000 keys 10 us instead of 11.7): a warp takes 32 keys
 // of a tile from their codes to its own maximum, sum and O, all in registers, and the four warps of a CTA meet at the end of an item.
 //
 // The operands of the 16 x 8 x 16 products stay where they are loaded, because the orders of keys and of d are free:
@@ -1560,8 +1560,8 @@ int launch_warps(const TreeParams& p, cudaStream_t st) {
 template <int FMT, int D>
 int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
   // Few rows by warps, more by roles.  32 to 256 rows in tiles of sixteen by warps | by roles, us: 32 rows 8 x 4096 tokens d = 128 41 | 24, one
-  // sequence of 1000 tokens 18 | 13; 64 rows 81 | 42, 22 | 16; 256 rows 265 | 114, 39 | 26; E4M3 alike (d = 64: 1.1 to 1.3 times).  16 rows:
-  // 4 of them took 200 | 149 us by roles | by warps.
+  // sequence of 1000 tokens 18 | 13; 64 rows 81 | 42, 22 | 16; 256 rows 265 | 114, 39 | 26; E4M3 alike (d = 64: 1.1 to 1.3 times).  Of
+  // sixteen or fewer, 4 rows, 32 x up to 32768 tokens: 152 us by warps, 200 by roles.
   if (p.rows <= 8) return launch_warps<FMT, D, 1>(p, st);
   if (R == 16) return launch_warps<FMT, D, 2>(p, st);
   return R == 32 ? launch_tree<FMT, D, 32>(p, st) : launch_tree<FMT, D, 64>(p, st);
