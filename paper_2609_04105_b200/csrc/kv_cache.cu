@@ -32,11 +32,11 @@ struct WriteParams {
 // eight elements from x on, as four words
 template <typename T>
 __device__ __forceinline__ uint4 load8(const T* x, bool vector) {
-  if (vector) return __ldg(reinterpret_cast<const uint4*>(x));
+  if (vector) return load(reinterpret_cast<const uint4*>(x));
   const uint16_t* y = reinterpret_cast<const uint16_t*>(x);
   uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__ldg(y + 2 * i) | (uint32_t)__ldg(y + 2 * i + 1) << 16;
+  for (int i = 0; i < 4; ++i) w[i] = (uint32_t)load(y + 2 * i) | (uint32_t)load(y + 2 * i + 1) << 16;
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <typename T>
@@ -131,8 +131,8 @@ struct Span {
   long long pos0, first, last;
   int start;
   __device__ __forceinline__ Span(const int* starts, const int* counts, int N, int b) {
-    start = __ldg(starts + b);
-    const int n = counts ? max(0, min(__ldg(counts + b), N)) : N;
+    start = load(starts + b);
+    const int n = counts ? max(0, min(load(counts + b), N)) : N;
     constexpr int kTokens = kBlockTokens<D>;
     pos0 = ((long long)(start >= 0 ? start / kTokens : -((kTokens - 1 - (long long)start) / kTokens)) + blockIdx.x) * kTokens;
     first = max((long long)start, pos0);
@@ -159,8 +159,8 @@ __global__ void __launch_bounds__(kThreads, GENERAL ? 4 : 6) cache_write_kernel(
     const int t_first = (int)(span.first - span.pos0), t_count = (int)(span.last - span.first);
     for (int j = tid; j < t_count * p.pairs; j += kThreads) {
       const int t = t_first + j / p.pairs, f = j % p.pairs;
-      const int at = p.positions ? __ldg(p.positions + (size_t)b * p.N + span.index(t)) : (int)(span.pos0 + t);
-      table[t * p.pairs + f] = cos_sin(at, __ldg(p.inv_freq + f), p.factor);
+      const int at = p.positions ? load(p.positions + (size_t)b * p.N + span.index(t)) : (int)(span.pos0 + t);
+      table[t * p.pairs + f] = cos_sin(at, load(p.inv_freq + f), p.factor);
     }
     __syncthreads();
   }
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, GENERAL ? 4 : 6) cache_write_kernel(
       const int page = p.cache.page_of(b, span.pos0 + t0);          // a page holds whole eights
       lost |= page < 0;
       if (page < 0) continue;
-      const float G = __ldg(p.cache.v_G + h);
+      const float G = load(p.cache.v_G + h);
       uint32_t rows[kRows][2], sc[2] = {0u, 0u};
       uint32_t have = 0;
 #pragma unroll
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, GENERAL ? 4 : 6) cache_write_kernel(
     } else {
       // ---- K: sixteen elements of a token at a time
       constexpr int kParts = D / 16, kPieces = kBlockTokens<D> * kParts / kHalf, kAtOnce = 2;
-      const float G = __ldg(p.cache.k_G + h);
+      const float G = load(p.cache.k_G + h);
 #pragma unroll 1
       for (int q0 = 0; q0 < kPieces; q0 += kAtOnce) {
         uint4 raw[kAtOnce][2];
@@ -348,10 +348,10 @@ __global__ void __launch_bounds__(kThreads, 8) cache_read_kernel(const ReadParam
         const int in_page = (int)((span.pos0 + t0) & (P - 1));
         const uint8_t* const chunks = rec + L::v_codes(P) + (in_page & ~15) * L::kRow + kRows * e8 * 16 + (in_page & 8);
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) rows[r] = __ldg(reinterpret_cast<const uint2*>(chunks + 16 * r));
-        if (L::kFp4) sc = __ldg(reinterpret_cast<const uint2*>(rec + L::v_scales(P) + (e8 >> 1) * P + in_page));
+        for (int r = 0; r < kRows; ++r) rows[r] = load(reinterpret_cast<const uint2*>(chunks + 16 * r));
+        if (L::kFp4) sc = load(reinterpret_cast<const uint2*>(rec + L::v_scales(P) + (e8 >> 1) * P + in_page));
       }
-      const float r = __fdiv_rn(1.f, __ldg(p.cache.v_G + h));
+      const float r = __fdiv_rn(1.f, load(p.cache.v_G + h));
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         uint32_t lo[4], hi[4];
@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_read_kernel(const ReadParam
   } else {
     // ---- K: eight elements of a token at a time
     constexpr int kPieces = kBlockTokens<D> * kLanes / kHalf, kAtOnce = 8;
-    const float r = __fdiv_rn(1.f, __ldg(p.cache.k_G + h));
+    const float r = __fdiv_rn(1.f, load(p.cache.k_G + h));
 #pragma unroll 1
     for (int q0 = 0; q0 < kPieces; q0 += kAtOnce) {
       uint2 raw[kAtOnce];                                           // NVFP4: codes and the scale's byte
@@ -390,10 +390,10 @@ __global__ void __launch_bounds__(kThreads, 8) cache_read_kernel(const ReadParam
         const uint8_t* const rec = p.cache.rec(page, h);
         const int in_page = (int)((span.pos0 + t) & (P - 1));
         if (L::kFp4) {
-          raw[q].x = __ldg(reinterpret_cast<const uint32_t*>(rec + ((e8 >> 2) * P + in_page) * 16 + (e8 & 3) * 4));
-          raw[q].y = __ldg(rec + L::k_scales(P) + in_page * L::kScales + (e8 >> 1));
+          raw[q].x = load(reinterpret_cast<const uint32_t*>(rec + ((e8 >> 2) * P + in_page) * 16 + (e8 & 3) * 4));
+          raw[q].y = load(rec + L::k_scales(P) + in_page * L::kScales + (e8 >> 1));
         } else {
-          raw[q] = __ldg(reinterpret_cast<const uint2*>(rec + ((e8 >> 1) * P + in_page) * 16 + (e8 & 1) * 8));
+          raw[q] = load(reinterpret_cast<const uint2*>(rec + ((e8 >> 1) * P + in_page) * 16 + (e8 & 1) * 8));
         }
       }
 #pragma unroll

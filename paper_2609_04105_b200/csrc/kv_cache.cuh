@@ -9,6 +9,12 @@
 
 namespace fp4attn {
 
+// Every load of a kernel of this path is a coherent one.  A kernel begins before its predecessor has ended, and what it reads (pages, rows,
+// tables, positions) may be what that one writes: the non-coherent path (__ldg, ld.global.nc) is defined only for memory that nobody writes
+// while the kernel lives.  wait_prior_grids makes what was written visible to ordinary loads.
+template <typename T>
+__device__ __forceinline__ T load(const T* p) { return *p; }
+
 struct CacheRef {
   uint8_t* pages;
   const float *k_G, *v_G;            // one factor per KV head
@@ -21,7 +27,7 @@ struct CacheRef {
   __device__ __forceinline__ int page_of(int b, long long pos) const {
     const long long i = pos >> log_page;
     if (pos < 0 || i >= max_pages) return -1;
-    const int id = __ldg(table + (size_t)b * max_pages + i);
+    const int id = load(table + (size_t)b * max_pages + i);
     return id >= 0 && id < num_pages ? id : -1;
   }
   __device__ __forceinline__ uint8_t* rec(int page, int head) const {

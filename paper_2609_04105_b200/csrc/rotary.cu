@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams<T> 
   const int n_tok = (int)min((long long)p.tokens_per_block, tokens - first);
   for (int i = threadIdx.x; i < n_tok * p.pairs; i += kThreads) {
     const int t = i / p.pairs, f = i - t * p.pairs;
-    float2 cs = cos_sin(__ldg(p.positions + first + t), __ldg(p.inv_freq + f), p.factor);
+    float2 cs = cos_sin(load(p.positions + first + t), load(p.inv_freq + f), p.factor);
     cs.y *= p.sign;
     table[i] = cs;
   }

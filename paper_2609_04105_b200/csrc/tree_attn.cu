@@ -71,10 +71,10 @@ struct Walk {
   int need;                                // keys that are there: a page that the table does not have among them is reported
 };
 // drafted tokens that entry b has
-__device__ __forceinline__ int drafted(const TreeParams& p, int b) { return p.count ? max(0, min(__ldg(p.count + b), p.T)) : p.T; }
+__device__ __forceinline__ int drafted(const TreeParams& p, int b) { return p.count ? max(0, min(load(p.count + b), p.T)) : p.T; }
 // tiles of an item: one at least, of no keys, where an entry has no rows
 __device__ __forceinline__ int load_entry(Walk& w, const TreeParams& p) {
-  const int room = p.cache.max_pages << p.cache.log_page, n = drafted(p, w.b), c = n ? max(0, __ldg(p.context + w.b)) : 0;
+  const int room = p.cache.max_pages << p.cache.log_page, n = drafted(p, w.b), c = n ? max(0, load(p.context + w.b)) : 0;
   w.ctx = min(c, room);
   w.need = (int)min((long long)c + n, (long long)INT_MAX);
   w.len = n ? (int)min((long long)c + (p.mask ? p.T : n), (long long)room) : 0;        // (a mask may look behind the count)
@@ -107,7 +107,7 @@ __device__ __forceinline__ int advance_by(Walk& w, const TreeParams& p, int unit
 }
 __device__ __forceinline__ unsigned long long row_mask(const TreeParams& p, int b, int t, int n) {
   if (t >= n) return 0ull;
-  return p.mask ? __ldg(p.mask + (size_t)b * p.T + t) : (2ull << t) - 1;
+  return p.mask ? load(p.mask + (size_t)b * p.T + t) : (2ull << t) - 1;
 }
 
 // R: rows of a tile, 32 or 64
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
           // scores are scaled back by its constant.  The buffer is free: as many items back, the last tile that read it was tile i - kKB or
           // an earlier one, whose product is done.
           const int kvh = w.u / p.row_tiles, row0 = (w.u - kvh * p.row_tiles) * R, qb = item % C::kQB;
-          const float c = __fdiv_rn(c0, __ldg(p.cache.k_G + kvh));
+          const float c = __fdiv_rn(c0, load(p.cache.k_G + kvh));
           constexpr int kParts = D / 16;                              // threads of a row
 #pragma unroll
           for (int j = key; j < R * kParts; j += 128) {
@@ -578,11 +578,11 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
               const uint16_t* q = static_cast<const uint16_t*>(p.q) + w.b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
               uint32_t raw[8];
               if (p.q_vector) {
-                *reinterpret_cast<uint4*>(raw) = __ldg(reinterpret_cast<const uint4*>(q));
-                *reinterpret_cast<uint4*>(raw + 4) = __ldg(reinterpret_cast<const uint4*>(q) + 1);
+                *reinterpret_cast<uint4*>(raw) = load(reinterpret_cast<const uint4*>(q));
+                *reinterpret_cast<uint4*>(raw + 4) = load(reinterpret_cast<const uint4*>(q) + 1);
               } else {
 #pragma unroll
-                for (int x = 0; x < 8; ++x) raw[x] = (uint32_t)__ldg(q + 2 * x) | (uint32_t)__ldg(q + 2 * x + 1) << 16;
+                for (int x = 0; x < 8; ++x) raw[x] = (uint32_t)load(q + 2 * x) | (uint32_t)load(q + 2 * x + 1) << 16;
               }
 #pragma unroll
               for (int x = 0; x < 8; ++x) {
@@ -937,7 +937,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
           const int row = row0 + key;
           float inv = 1.f;
           if (whole) {
-            inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + kvh));     // nothing seen: 0, not 0 / 0
+            inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * load(p.cache.v_G + kvh));     // nothing seen: 0, not 0 / 0
             if (p.lse && row < p.rows && row % p.T < n)
               p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (top - kShift + log2f(total_l)) * 0.6931471805599453f;
           } else {
@@ -1149,7 +1149,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
         }
         kvh = w.u / p.row_tiles;
         row0 = (w.u - kvh * p.row_tiles) * R;
-        const float c0 = __fdiv_rn(p.scale * 1.4426950408889634f, __ldg(p.cache.k_G + kvh));
+        const float c0 = __fdiv_rn(p.scale * 1.4426950408889634f, load(p.cache.k_G + kvh));
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           // Q scaled by a power of two per row, as above
@@ -1162,10 +1162,10 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             for (int x = 0; x < D / 4; x += 8) {
               uint32_t raw[4];
               if (p.q_vector) {
-                *reinterpret_cast<uint4*>(raw) = __ldg(reinterpret_cast<const uint4*>(q + x));
+                *reinterpret_cast<uint4*>(raw) = load(reinterpret_cast<const uint4*>(q + x));
               } else {
 #pragma unroll
-                for (int y = 0; y < 4; ++y) raw[y] = (uint32_t)__ldg(q + x + 2 * y) | (uint32_t)__ldg(q + x + 2 * y + 1) << 16;
+                for (int y = 0; y < 4; ++y) raw[y] = (uint32_t)load(q + x + 2 * y) | (uint32_t)load(q + x + 2 * y + 1) << 16;
               }
 #pragma unroll
               for (int y = 0; y < 4; ++y) {
@@ -1417,7 +1417,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
               }
               if (whole) {
                 if (row % p.T < n_drafted) {
-                  const float inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * __ldg(p.cache.v_G + kvh));     // nothing seen: 0
+                  const float inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * load(p.cache.v_G + kvh));     // nothing seen: 0
                   const uint2 h = p.half ? make_uint2(pack_pair<__half>(y[0] * inv, y[1] * inv), pack_pair<__half>(y[2] * inv, y[3] * inv))
                                          : make_uint2(pack_pair<__nv_bfloat16>(y[0] * inv, y[1] * inv), pack_pair<__nv_bfloat16>(y[2] * inv, y[3] * inv));
                   *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + (size_t)(out0 + row) * D + e) = h;
@@ -1489,7 +1489,7 @@ __global__ void __launch_bounds__(128) tree_join_kernel(const TreeParams p) {
       }
     }
   }
-  const float f = l == 0.f ? 0.f : __fdiv_rn(1.f, l * __ldg(p.cache.v_G + kvh));
+  const float f = l == 0.f ? 0.f : __fdiv_rn(1.f, l * load(p.cache.v_G + kvh));
   const size_t at = ((size_t)b * p.H + (size_t)kvh * p.group) * p.T + row;
 #pragma unroll
   for (int x = 0; x < E; x += 2) {
