@@ -11,9 +11,10 @@ namespace fp4attn {
 
 // Every load of a kernel of this path is a coherent one.  A kernel begins before its predecessor has ended, and what it reads (pages, rows,
 // tables, positions) may be what that one writes: the non-coherent path (__ldg, ld.global.nc) is defined only for memory that nobody writes
-// while the kernel lives.  wait_prior_grids makes what was written visible to ordinary loads.
+// while the kernel lives.  wait_prior_grids makes what was written visible to ordinary loads.  (As an explicit load, not `*p`: the compiler
+// moved the dereferences of the attention kernel's walk to other places, 320 instead of 252 bytes of spills and 102 instead of 98 us.)
 template <typename T>
-__device__ __forceinline__ T load(const T* p) { return *p; }
+__device__ __forceinline__ T load(const T* p) { return __ldca(p); }
 
 struct CacheRef {
   uint8_t* pages;
