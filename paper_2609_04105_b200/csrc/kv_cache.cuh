@@ -72,8 +72,9 @@ __device__ __forceinline__ uint32_t cvt_f16x2_e2m1x2(uint32_t word) {
   return r;
 }
 // The eight codes of a word, or the four E4M3 bytes, at once: the byte is then taken by the conversion itself (64 conversions a clock
-// and SM; 32 with a shift in front of each).  Only for whole words as they come out of memory: on a byte that the compiler knows to be
-// extended with zeros, this form gave wrong values.
+// and SM; 32 with a shift in front of each).  Right for every value of every byte, of words out of memory, permuted, masked, united or extended
+// with zeros alike.  (One byte alone so, the other three names unused, gave wrong values where the word was a byte extended with
+// zeros: cvt_f16x2_e2m1x2 shifts.)
 __device__ __forceinline__ void cvt_f16x2_e2m1x8(uint32_t word, uint32_t* h) {
   asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
       "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
