@@ -41,7 +41,9 @@ namespace {
 using namespace ptx;
 
 constexpr int kTile = 128;                 // keys of a tile
-constexpr int kMostCtas = 640;             // partial results: two per CTA
+// CTAs of a call, each of which may leave two partial results: four an SM by warps, one by roles
+constexpr int kMostWarpCtas = 640, kMostRoleCtas = 160;
+template <int R> constexpr int kMostCtas = R <= 16 ? kMostWarpCtas : kMostRoleCtas;
 constexpr float kLag = 8.f;                // octaves by which a score may exceed its row's reference
 constexpr float kShift = 7.f;              // a probability of 1 is 2^7: with the lag just inside f16, whose subnormals then begin at 2^-21
 
@@ -54,8 +56,8 @@ struct TreeParams {
   void* out;                               // [B, H, T, d]
   float* lse;                              // [B, H, T]
   int* status;
-  float* part;                             // [2 * kMostCtas][R][D]
-  float2* part_ml;                         // [2 * kMostCtas][R]: reference, sum
+  float* part;                             // [2 * kMostCtas<R>][R][D]
+  float2* part_ml;                         // [2 * kMostCtas<R>][R]: reference, sum
   int2* split;                             // [items]: first and last CTA of an item in parts; first = -1: whole
   int B, H, T, group, rows, row_tiles;     // rows = group * T of a KV head
   float scale;
@@ -1457,7 +1459,7 @@ __global__ void __launch_bounds__(128) tree_join_kernel(const TreeParams p) {
   const int r = blockIdx.y * 4 + (threadIdx.x >> 5), row = (u - kvh * p.row_tiles) * R + r;
   if (r >= R || row >= p.rows || row % p.T >= drafted(p, b)) return;
   const int2 ctas = p.split[item];
-  if (ctas.x < 0 || ctas.y < ctas.x || ctas.y >= kMostCtas) return;   // whole (or a kernel that gave up)
+  if (ctas.x < 0 || ctas.y < ctas.x || ctas.y >= kMostCtas<R>) return;   // whole (or a kernel that gave up)
   const int n = ctas.y - ctas.x + 1;
   auto slot = [&](int i) { return (size_t)(i ? 2 * (ctas.x + i) : 2 * ctas.x + 1); };
   float m = -INFINITY;
@@ -1500,7 +1502,7 @@ __global__ void __launch_bounds__(128) tree_join_kernel(const TreeParams p) {
 }
 
 // ---- workspace: partial O, their references and sums, what is split
-int rows_of_tile(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+int rows_of_tile(int rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
 struct TreePlan {
   int R, row_tiles;
   size_t ml, split, total;
@@ -1510,9 +1512,9 @@ TreePlan plan(int B, int H, int kv_heads, int T, int d) {
   const int rows = H / kv_heads * T;
   t.R = rows_of_tile(rows);
   t.row_tiles = (rows + t.R - 1) / t.R;
-  const size_t part = (size_t)2 * kMostCtas * t.R * d * 4;
-  t.ml = part;
-  t.split = t.ml + (size_t)2 * kMostCtas * t.R * 8;
+  const size_t slots = 2 * (t.R <= 16 ? kMostWarpCtas : kMostRoleCtas);        // of the kernel that will run (launch_rows)
+  t.ml = slots * t.R * d * 4;
+  t.split = t.ml + slots * t.R * 8;
   t.total = t.split + (((size_t)B * kv_heads * t.row_tiles * 8 + 15) & ~(size_t)15);
   return t;
 }
@@ -1531,7 +1533,7 @@ int launch_tree(const TreeParams& p, cudaStream_t st) {
   if (!sms) return FP4ATTN_ERR_CUDA;
   const int units = p.cache.kv_heads * p.row_tiles;
   const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * units;
-  const unsigned grid = (unsigned)std::min<long long>(std::min(sms, kMostCtas), most_tiles);
+  const unsigned grid = (unsigned)std::min<long long>(std::min(sms, kMostCtas<R>), most_tiles);
   cudaError_t e = launch_overlapped(tree_kernel<FMT, D, R>, dim3(grid), C::kThreads, C::kSmem, st, p);
   if (e == cudaSuccess)
     e = launch_overlapped(tree_join_kernel<D, R>, dim3((unsigned)(p.B * units), (unsigned)(std::min(R, p.rows) + 3) / 4), 128u, 0, st, p);
@@ -1550,7 +1552,7 @@ int launch_warps(const TreeParams& p, cudaStream_t st) {
   const int sms = device_sms();
   if (!sms) return FP4ATTN_ERR_CUDA;
   const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * p.cache.kv_heads * p.row_tiles;
-  const unsigned grid = (unsigned)std::min<long long>(std::min(C::kCtas * sms, kMostCtas), most_tiles);
+  const unsigned grid = (unsigned)std::min<long long>(std::min(C::kCtas * sms, kMostCtas<C::R>), most_tiles);
   cudaError_t e = launch_overlapped(tree_warp_kernel<FMT, D, NT>, dim3(grid), C::kThreads, C::kSmem, st, p);
   if (e == cudaSuccess)
     e = launch_overlapped(tree_join_kernel<D, C::R>, dim3((unsigned)(p.B * p.cache.kv_heads * p.row_tiles), (unsigned)(std::min(p.rows, C::R) + 3) / 4), 128u, 0,
@@ -1562,7 +1564,7 @@ int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
   // Few rows by warps, more by roles.  32 to 256 rows in tiles of sixteen by warps | by roles, us: 32 rows 8 x 4096 tokens d = 128 41 | 24, one
   // sequence of 1000 tokens 18 | 13; 64 rows 81 | 42, 22 | 16; 256 rows 265 | 114, 39 | 26; E4M3 alike (d = 64: 1.1 to 1.3 times).  Of
   // sixteen or fewer, 4 rows, 32 x up to 32768 tokens: 152 us by warps, 200 by roles.
-  if (p.rows <= 8) return launch_warps<FMT, D, 1>(p, st);
+  if (R == 8) return launch_warps<FMT, D, 1>(p, st);
   if (R == 16) return launch_warps<FMT, D, 2>(p, st);
   return R == 32 ? launch_tree<FMT, D, 32>(p, st) : launch_tree<FMT, D, 64>(p, st);
 }
