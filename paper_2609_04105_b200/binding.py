@@ -255,21 +255,57 @@ def fp4attn_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: Opt
     return f.float().to(device)
 
 
+def _rotary(q, k, positions, inv_freq, interleaved, transposed, factor, q_out, k_out):
+    out = (_native_module or _native()).rotary(q, k, positions, inv_freq, interleaved, transposed, factor, q_out, k_out)
+    return _Rotary.apply(q, k, positions, inv_freq, interleaved, transposed, factor) if out is NotImplemented else out
+
+
+class _Rotary(torch.autograd.Function):
+    """The rotation is linear: the gradient of its inputs is the transposed one of the gradient of its outputs, whose own gradient is the rotation
+    again."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, inv_freq, interleaved, transposed, factor):
+        ctx.save_for_backward(positions, inv_freq)
+        ctx.how = (interleaved, transposed, factor)
+        ctx.set_materialize_grads(False)
+        out = (_native_module or _native()).rotary(q, k, positions, inv_freq, interleaved, transposed, factor, None, None)
+        if k is not None:
+            ctx.mark_non_differentiable(*[y for y, needed in zip(out, ctx.needs_input_grad) if not needed])
+        return out
+
+    @staticmethod
+    def backward(ctx, dq, dk=None):
+        positions, inv_freq = ctx.saved_tensors
+        interleaved, transposed, factor = ctx.how
+        # (a gradient may come broadcast along the last axis, as that of a sum)
+        given = [i for i, g in enumerate((dq, dk)) if g is not None and ctx.needs_input_grad[i]]
+        grads = [g if g is None or g.stride(-1) == 1 else g.contiguous() for g in (dq, dk)]
+        dx = [None, None]
+        if given:
+            out = _rotary(grads[given[0]], grads[1] if len(given) == 2 else None, positions, inv_freq, interleaved, not transposed, factor, None, None)
+            for i, g in zip(given, out if len(given) == 2 else (out,)):
+                dx[i] = g
+        return dx[0], dx[1], None, None, None, None, None
+
+
 def fp4attn_rotary(q: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, k: Optional[torch.Tensor] = None,
                    interleaved: bool = False, attention_factor: float = 1.0, q_out: Optional[torch.Tensor] = None,
                    k_out: Optional[torch.Tensor] = None):
     """Rotary positions on q [B,H,N,d], and on k [B,Hkv,N,d] in the same launch -> q_out, or (q_out, k_out).
     bf16, fp16 or fp32, any strides but the last axis'; positions CUDA int32 [B,N]; inv_freq CUDA fp32 [pairs], for the first
     2 * pairs elements of a head, in halves or (interleaved) as neighbours; cos and sin are multiplied by attention_factor.
-    An output may be its own input."""
-    return (_native_module or _native()).rotary(q, k, positions, inv_freq, interleaved, False, attention_factor, q_out, k_out)
+    An output may be its own input.  Differentiable in q and k, to any order; a call with outputs of the caller's records nothing and is
+    refused where an input requires a gradient."""
+    return _rotary(q, k, positions, inv_freq, interleaved, False, attention_factor, q_out, k_out)
 
 
 def fp4attn_rotary_backward(dq: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, k: Optional[torch.Tensor] = None,
                             interleaved: bool = False, attention_factor: float = 1.0, q_out: Optional[torch.Tensor] = None,
                             k_out: Optional[torch.Tensor] = None):
-    """The gradients of fp4attn_rotary's inputs from those of its outputs, dq and (as k) dk: the transposed rotation."""
-    return (_native_module or _native()).rotary(dq, k, positions, inv_freq, interleaved, True, attention_factor, q_out, k_out)
+    """The gradients of fp4attn_rotary's inputs from those of its outputs, dq and (as k) dk: the transposed rotation.  For callers that go
+    backward by hand; differentiable as fp4attn_rotary is."""
+    return _rotary(dq, k, positions, inv_freq, interleaved, True, attention_factor, q_out, k_out)
 
 
 @dataclass

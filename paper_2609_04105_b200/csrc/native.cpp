@@ -10,6 +10,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -531,7 +532,8 @@ struct Outputs {
   PyObject* give(int i, PyObject* o) const { return own[i] ? THPVariable_Wrap(*own[i]) : Py_NewRef(o); }
 };
 
-// rotary(q, k, positions, inv_freq, interleaved, transposed, factor, q_out, k_out) -> q_out, or (q_out, k_out)
+// rotary(q, k, positions, inv_freq, interleaved, transposed, factor, q_out, k_out) -> q_out, or (q_out, k_out); NotImplemented, with nothing done,
+// where gradients are recorded and an input takes one: binding.py then makes the call inside an autograd function
 PyObject* py_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
   FP4_TRY
   if (n != 9) return assertion("rotary takes 9 arguments");
@@ -551,6 +553,14 @@ PyObject* py_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
   float factor;
   const int interleaved = PyObject_IsTrue(args[4]), transposed = PyObject_IsTrue(args[5]);
   if (interleaved < 0 || transposed < 0 || !number(args[6], &factor)) return nullptr;
+  if (c10::GradMode::is_enabled()) {
+    if (THPVariable_Unpack(args[3]).requires_grad()) return assertion("inv_freq takes no gradient");
+    if (x[0].t->requires_grad() || (two && x[1].t->requires_grad())) {
+      if (args[7] != Py_None || args[8] != Py_None)
+        return assertion("q_out and k_out carry no gradient, and an input requires one: leave them out, or call under torch.no_grad()");
+      Py_RETURN_NOTIMPLEMENTED;
+    }
+  }
   const c10::cuda::OptionalCUDAGuard guard(device);
   for (int i = 0; i <= (int)two; ++i)
     if (!outputs.take(i, args[7 + i], x[i], &y[i]))
