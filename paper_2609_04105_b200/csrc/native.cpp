@@ -412,6 +412,7 @@ PyObject* py_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
 struct Strided {
   const at::Tensor* t = nullptr;
   int B = 0, H = 0, N = 0, d = 0, type = -1;
+  bool empty = false;                                    // (then refused, for this reason)
   fp4attn_view view{};
   bool take(PyObject* o, bool fp32) {
     if (!THPVariable_Check(o)) return false;
@@ -420,6 +421,7 @@ struct Strided {
     type = t->scalar_type() == at::kBFloat16 ? FP4ATTN_TYPE_BF16 : t->scalar_type() == at::kHalf ? FP4ATTN_TYPE_FP16
          : t->scalar_type() == at::kFloat && fp32 ? FP4ATTN_TYPE_FP32 : -1;
     const auto s = t->sizes(), st = t->strides();
+    empty = type >= 0 && t->numel() == 0;
     for (int i = 0; i < 4; ++i)
       if (s[i] > INT32_MAX || s[i] < 1) return false;
     B = (int)s[0]; H = (int)s[1]; N = (int)s[2]; d = (int)s[3];
@@ -447,6 +449,7 @@ struct Strided {
     return true;
   }
 };
+const char* kNothing = "a call needs at least one sequence, head, token and element: leave out calls of an empty batch";
 // the shape `sizes`, or None
 bool shaped(PyObject* o, at::IntArrayRef sizes) { return o == Py_None || (THPVariable_Check(o) && THPVariable_Unpack(o).sizes() == sizes); }
 // a contiguous tensor of `n` values of `type` on `device`, or None where that is allowed
@@ -541,7 +544,7 @@ PyObject* py_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Outputs outputs;
   const bool two = args[1] != Py_None;
   if (!x[0].take(args[0], true) || (two && !(x[1].take(args[1], true) && x[1].like(x[0]))))
-    return assertion("q (and k) must be CUDA tensors [B, heads, N, d], bfloat16, float16 or float32, the last axis contiguous; k of q's B, N, d, type and device");
+    return assertion(x[0].empty || x[1].empty ? kNothing : "q (and k) must be CUDA tensors [B, heads, N, d], bfloat16, float16 or float32, the last axis contiguous; k of q's B, N, d, type and device");
   if (!two && args[8] != Py_None) return assertion("k_out is given but k is not");
   const c10::Device device = x[0].t->device();
   void *positions, *freq = nullptr;
@@ -585,7 +588,7 @@ PyObject* py_cache_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Strided k, v;
   if (!k.take(args[1], false) || !v.take(args[2], false) || !v.like(k) || v.H != k.H || k.H != cache.c.kv_heads || k.d != cache.c.d ||
       k.t->device() != cache.device)
-    return assertion("k and v must be CUDA tensors [B, KV heads, N, d] of the cache's heads, d and device, bfloat16 or float16, the last axis contiguous");
+    return assertion(k.empty || v.empty ? kNothing : "k and v must be CUDA tensors [B, KV heads, N, d] of the cache's heads, d and device, bfloat16 or float16, the last axis contiguous");
   Batch batch;
   if (const char* wrong = batch.take(k.B, cache.device, args[3], args[4], args[5], args[10])) return assertion(wrong);
   void *positions, *freq = nullptr;
@@ -625,7 +628,7 @@ PyObject* py_cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!ints(args + 3, 1, &N)) return nullptr;
   const int half = PyObject_IsTrue(args[5]);
   if (half < 0) return nullptr;
-  if (B < 1 || B > INT32_MAX || N < 1) return assertion("cache_read needs at least one sequence and one token");
+  if (B < 1 || B > INT32_MAX || N < 1) return assertion(kNothing);
   Batch batch;
   if (const char* wrong = batch.take((int)B, cache.device, args[1], args[2], args[4], args[8])) return assertion(wrong);
   const c10::cuda::OptionalCUDAGuard guard(cache.device);
@@ -660,7 +663,7 @@ PyObject* py_tree_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (const char* wrong = cache.take(args[1])) return *wrong ? assertion(wrong) : nullptr;
   Strided q;
   if (!q.take(args[0], false) || q.d != cache.c.d || q.t->device() != cache.device || cache.c.kv_heads < 1 || q.H % cache.c.kv_heads != 0)
-    return assertion("q must be a CUDA tensor [B, H, T, d] of the cache's d and device, bfloat16 or float16, the last axis contiguous; H a multiple of the KV heads");
+    return assertion(q.empty ? kNothing : "q must be a CUDA tensor [B, H, T, d] of the cache's d and device, bfloat16 or float16, the last axis contiguous; H a multiple of the KV heads");
   Batch batch;
   if (const char* wrong = batch.take(q.B, cache.device, args[2], args[3], args[5], args[9])) return assertion(wrong);
   void *mask, *out_ptr, *lse_ptr;
