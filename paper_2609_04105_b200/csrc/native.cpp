@@ -162,6 +162,10 @@ bool ints(PyObject* const* args, Py_ssize_t n, int* out, bool convert = false) {
     const long v = o ? PyLong_AsLong(o) : -1;
     Py_XDECREF(o);
     if (v == -1 && PyErr_Occurred()) return false;
+    if (v < INT32_MIN || v > INT32_MAX) {                // (cut to 32 bits it would be another number, and pass)
+      PyErr_SetString(PyExc_OverflowError, "int does not fit 32 bits");
+      return false;
+    }
     out[i] = (int)v;
   }
   return true;

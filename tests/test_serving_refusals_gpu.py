@@ -19,3 +19,20 @@ def test_empty_batches_are_named():
                      lambda: Bd.fp4attn_tree_attention(q, cache, table[:B], start[:B])):
             with pytest.raises(AssertionError, match="at least one sequence"):
                 call()
+
+
+def test_whole_numbers_beyond_32_bits():
+    """2^32 + n is not n."""
+    Bd, g = _bd(), _gen(2)
+    cache, table = _filled(Bd, g, "nvfp4", 2, 2, 16, 64, 20)
+    start = _i32([3, 4])
+    with pytest.raises(OverflowError):
+        Bd.fp4attn_cache_read(cache, table, start, (1 << 32) + 3)
+    q = _randn(g, 2, 4, 3, 64)
+    for fmt, page in ((cache.fmt + (1 << 32), 16), (cache.fmt, 16 - (1 << 32))):
+        wrong = Bd.QuantizedCache(cache.pages, cache.k_G, cache.v_G, fmt, page, 64)
+        with pytest.raises(OverflowError):
+            Bd.fp4attn_tree_attention(q, wrong, table, start)
+    x = _randn(g, 1, 1, 128, 64)
+    with pytest.raises(OverflowError):
+        Bd.fp4attn_quantize(x, Bd.FMT_NVFP4 + (1 << 32), 0)
