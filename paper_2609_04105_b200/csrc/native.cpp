@@ -434,6 +434,10 @@ struct Strided {
     return type >= 0 && (d == 1 || st[3] == 1);
   }
   bool like(const Strided& o) const { return B == o.B && N == o.N && d == o.d && type == o.type && t->device() == o.t->device(); }
+  bool begins_with(const Strided& o) const { return t && o.t && view.data == o.view.data; }
+  bool same_view(const Strided& o) const {
+    return begins_with(o) && H == o.H && view.stride_b == o.view.stride_b && view.stride_h == o.view.stride_h && view.stride_n == o.view.stride_n;
+  }
   // no two elements at one address (what is written must not be a broadcast)
   bool distinct() const { return t->is_non_overlapping_and_dense() || spread(); }
 
@@ -572,6 +576,10 @@ PyObject* py_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
   for (int i = 0; i <= (int)two; ++i)
     if (!outputs.take(i, args[7 + i], x[i], &y[i]))
       return assertion("an output must be a CUDA tensor of its input's shape, type and device, the last axis contiguous, no element twice");
+  // What is written in place is written by the thread that has read it; in another order, or over the other tensor, it is not
+  for (int i = 0; i <= (int)two; ++i)
+    if ((y[i].begins_with(x[i]) && !y[i].same_view(x[i])) || y[i].begins_with(x[1 - i]) || (i == 1 && y[1].begins_with(y[0])))
+      return assertion("an output may be its own input, the same view of it, and must not overlap any other tensor of the call");
   outputs.allocate(device, y);
   const int rc = unlocked([&] {
     return g_api.rotary(&x[0].view, two ? &x[1].view : nullptr, &y[0].view, two ? &y[1].view : nullptr, x[0].type, x[0].B, x[0].H, x[1].H,
@@ -647,6 +655,7 @@ PyObject* py_cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
       return assertion("k_out and v_out must be CUDA tensors [B, KV heads, N, d] of the cache's heads, d and device and of dtype, the last axis contiguous, no element twice");
     }
   }
+  if (out[1].begins_with(out[0])) return assertion("k_out and v_out must not overlap");
   outputs.allocate(cache.device, out);
   for (at::Tensor* own : outputs.own)
     if (own && batch.count) own->zero_();                // rows behind the counts are not written

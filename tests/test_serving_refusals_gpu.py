@@ -36,3 +36,23 @@ def test_whole_numbers_beyond_32_bits():
     x = _randn(g, 1, 1, 128, 64)
     with pytest.raises(OverflowError):
         Bd.fp4attn_quantize(x, Bd.FMT_NVFP4 + (1 << 32), 0)
+
+
+def test_outputs_over_one_another():
+    """The same memory for both outputs, an output over the other input, or over its own in another order: rows would be overwritten while
+    others are still read, or twice."""
+    Bd, g = _bd(), _gen(3)
+    cache, table = _filled(Bd, g, "nvfp4", 2, 2, 16, 64, 20)
+    f = Bd.fp4attn_rotary_frequencies(64)
+    q, k, pos = _randn(g, 2, 2, 2, 64), _randn(g, 2, 2, 2, 64), _i32([[0, 1]] * 2)
+    out, kept = torch.zeros_like(q), (q.clone(), k.clone())
+    for call in (lambda: Bd.fp4attn_rotary(q, pos, f, k=k, q_out=out, k_out=out), lambda: Bd.fp4attn_rotary(q, pos, f, k=k, q_out=k),
+                 lambda: Bd.fp4attn_rotary(q, pos, f, k=k, k_out=q), lambda: Bd.fp4attn_rotary(q, pos, f, k=k, q_out=k, k_out=q),
+                 lambda: Bd.fp4attn_rotary(q, pos, f, q_out=q.transpose(1, 2)), lambda: Bd.fp4attn_rotary(q, pos, f, k=k, q_out=q, k_out=q),
+                 lambda: Bd.fp4attn_cache_read(cache, table, _i32([3, 4]), 2, k_out=out, v_out=out)):
+        with pytest.raises(AssertionError, match="overlap"):
+            call()
+    assert not out.any() and torch.equal(q, kept[0]) and torch.equal(k, kept[1])
+    want = [x.clone() for x in Bd.fp4attn_rotary(q, pos, f, k=k)]
+    Bd.fp4attn_rotary(q, pos, f, k=k, q_out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
