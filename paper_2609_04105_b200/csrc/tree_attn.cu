@@ -151,7 +151,7 @@ struct TreeCfg {
   static constexpr int kOffScale = kOffWarp + 16 * R * kSets;      // float [kSets][R]: factors on O
   static constexpr int kOffValid = kOffScale + 4 * R * kSets;      // u32 [kRing]
   static constexpr int kOffScan = kOffValid + 4 * kRing;           // i64 [32]
-  static constexpr int kOffFind = kOffScan + 256;                  // i64 [2]
+  static constexpr int kOffFind = kOffScan + 256;                  // i64 [5] (room for eight)
   static constexpr int kOffBar = kOffFind + 64;
   static constexpr int kSmem = kOffBar + 512 + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -280,10 +280,10 @@ __device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long lon
 
 // floor(a * b / c), floor((a + 1) * b / c), ... of tile numbers: in 32 bits where they are enough (64-bit divisions took 0.5 us of the
 // smallest calls)
-__device__ __forceinline__ long long mul_div(long long a, long long b, long long c) {
-  const long long ab = a * b;
-  return ab < (1ll << 31) ? (long long)((uint32_t)ab / (uint32_t)c) : ab / c;
+__device__ __forceinline__ constexpr long long div_short(long long a, long long c) {
+  return (a | c) < (1ll << 31) ? (long long)((uint32_t)a / (uint32_t)c) : a / c;
 }
+__device__ __forceinline__ constexpr long long mul_div(long long a, long long b, long long c) { return div_short(a * b, c); }
 // This CTA's run of tiles: how many, and where it starts.  find: entry and place of the first tile, its number in the list, all tiles,
 // CTAs.  A barrier of the block (two for a batch of more than 32): everything that the block wrote to shared memory before is visible after it.
 template <int THREADS>
@@ -366,11 +366,13 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
   return (int)min(t1 - t0, (long long)INT_MAX);
 }
 
-// the CTA that has a tile of the list
-__device__ __forceinline__ int cta_of(const long long* find, long long tile) {
-  const long long a = (tile + 1) * find[4] - 1;
-  return (int)(a < (1ll << 31) ? (uint32_t)a / (uint32_t)find[3] : a / find[3]);
-}
+// the CTA that has a tile of the list, of `total` tiles in equal runs for `ctas`
+__device__ __forceinline__ constexpr int cta_of(long long tile, long long total, long long ctas) { return (int)div_short((tile + 1) * ctas - 1, total); }
+static_assert(cta_of(0, 5, 2) == 0 && cta_of(1, 5, 2) == 0 && cta_of(2, 5, 2) == 1 && cta_of(4, 5, 2) == 1, "runs 0-1, 2-4");
+static_assert(mul_div(1, 5, 2) == 2 && mul_div(2, 5, 2) == 5, "where they begin");
+static_assert(cta_of(7, (1ll << 32) + 1, 592) == 0 && cta_of((1ll << 32), (1ll << 32) + 1, 592) == 591 && mul_div(591, 1ll << 33, 592) < 1ll << 33 &&
+              cta_of(mul_div(591, 1ll << 33, 592), 1ll << 33, 592) == 591 && cta_of(mul_div(591, 1ll << 33, 592) - 1, 1ll << 33, 592) == 590,
+              "more tiles than 32 bits hold");
 
 // Brings the pages of tiles into a ring of stages, one bulk copy each; a whole warp.  RING: stages for which `valid` remembers which of the
 // pages exist.  PARTS = 2: K and V by themselves, each in a stage of its own.
@@ -949,7 +951,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
           for (int k = 0; k < C::kSets; ++k) factor_all[k * R + key] = f[k] * inv;
         }
         if (group == 0 && key == 0 && part_first == 0)
-          p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find, find[2] + i + w.left - 1));
+          p.split[(size_t)w.b * units + w.u] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find[2] + i + w.left - 1, find[3], find[4]));
         bar_sync(id_all, 128 * C::kSets);
         tc_fence_after();
         // a set takes its share of the rows
@@ -1434,7 +1436,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
           }
         if (threadIdx.x == 0 && part_first == 0)
           p.split[(size_t)w.b * units + w.u] =
-              whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find, find[2] + i + w.left - 1));
+              whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find[2] + i + w.left - 1, find[3], find[4]));
         fresh = true;
       }
       advance(w, p, units);
