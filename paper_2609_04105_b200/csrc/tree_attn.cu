@@ -4,8 +4,8 @@
 // context[b] + T - 1 those whose bit of its mask is set.
 //
 // The rows that read one KV head are few (1 to some hundreds), its keys are many, so keys and head dimension take the wide side of the
-// tensor core and rows the narrow one:  S^T = K Q^T (128 keys x R rows),  O^T += V^T P^T (d x R rows), R = 32 or 64.  (Sixteen rows or
-// fewer have a kernel of their own, further down.)  Their A operands,
+// tensor core and rows the narrow one:  S^T = K Q^T (128 keys x R rows),  O^T += V^T P^T (d x R rows), R = 32 or 64.  (Few rows - eight or
+// sixteen, see rows_of_tile - have a kernel of their own, further down.)  Their A operands,
 // K and V^T, live in tensor memory: a lane is a key of K, a head-dimension index of V^T, and the thread that turns a lane's
 // codes into f16 writes them there without a word of shared memory.  Only Q and P, the narrow operands, are read from shared memory.
 //
@@ -1010,7 +1010,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
   }
 }
 
-// ---------------------------------------------------------------- sixteen rows or fewer: a warp by itself
+// ---------------------------------------------------------------- few rows: a warp by itself
 // What should bound few rows is the reading; with the roles of the kernel above a tile costs more instructions for handing it from role to
 // role than for its keys (4100 a tile of 128 keys, d = 128, half of them hand-overs; 32 sequences of up to 32768 tokens, 4 rows: 200 us, whose
 // reading takes 94).  Here nothing is handed over (2700 a tile, 152 us; one token over 1000 keys 10 us instead of 11.7): a warp takes 32 keys
@@ -1031,7 +1031,7 @@ struct WarpCfg {
   static constexpr int R = 8 * NT;
   static constexpr int kStage = kTile * L::kToken;                 // K or V of a tile
   static constexpr int kCtas = kStage > 9216 ? 2 : NT == 2 ? 3 : 4;            // of an SM
-  static constexpr int kStages = kStage > 9216 ? 6 : kStage > 8192 ? (kCtas == 3 ? 7 : 5) : 6;
+  static constexpr int kStages = kStage > 9216 ? 6 : kStage > 8192 ? 5 : 6;
   static constexpr int kRow = D / 2;                               // floats of a row of half an O in shared memory (unpadded: it is full)
   static constexpr int kOffO = kStages * kStage;                   // float [4 warps][8 rows][kRow]
   static constexpr int kOffML = kOffO + kWarps * 8 * kRow * 4;     // float2 [4 warps][8 rows]
@@ -1504,15 +1504,27 @@ __global__ void __launch_bounds__(128) tree_join_kernel(const TreeParams p) {
 }
 
 // ---- workspace: partial O, their references and sums, what is split
-int rows_of_tile(int rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+// Few rows by warps (tiles of 8 or 16), more by roles (32 or 64).  By warps | by roles, us:
+//   4 rows, NVFP4, d = 128, 32 sequences x up to 32768 tokens: 152 | 200
+//   16 rows, 8 KV heads      1 x 1000      1 x 16000     8 x 4096      32 x 32000 (up to; 12 rows alike)
+//     NVFP4, d = 64       10.8 | 11.1   26.4 | 26.9   21.7 | 27.9    169 | 260
+//     E4M3, d = 64        11.0 | 11.1   26.5 | 26.1   21.4 | 29.3    158 | 273
+//     E4M3, d = 128       12.3 | 12.1   24.7 | 25.3   28.0 | 31.0    263 | 294
+//     NVFP4, d = 128      14.6 | 12.2   40.9 | 25.0   37.3 | 30.0    358 | 290    two groups of eight rows are more than its registers hold
+//   32 rows, d = 128: 1 x 1000 18 | 13, 8 x 4096 41 | 24; 64 rows 22 | 16, 81 | 42; 256 rows 39 | 26, 265 | 114; E4M3 alike (d = 64: 1.1 to 1.3 times)
+int rows_of_tile(int rows, int fmt, int d) {
+  if (rows <= 8) return 8;
+  if (rows <= 16 && !(fmt == FP4ATTN_FMT_NVFP4 && d == 128)) return 16;
+  return rows <= 32 ? 32 : 64;
+}
 struct TreePlan {
   int R, row_tiles;
   size_t ml, split, total;
 };
-TreePlan plan(int B, int H, int kv_heads, int T, int d) {
+TreePlan plan(int B, int H, int kv_heads, int T, int d, int fmt) {
   TreePlan t;
   const int rows = H / kv_heads * T;
-  t.R = rows_of_tile(rows);
+  t.R = rows_of_tile(rows, fmt, d);
   t.row_tiles = (rows + t.R - 1) / t.R;
   const size_t slots = 2 * (t.R <= 16 ? kMostWarpCtas : kMostRoleCtas);        // of the kernel that will run (launch_rows)
   t.ml = slots * t.R * d * 4;
@@ -1563,11 +1575,9 @@ int launch_warps(const TreeParams& p, cudaStream_t st) {
 }
 template <int FMT, int D>
 int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
-  // Few rows by warps, more by roles.  32 to 256 rows in tiles of sixteen by warps | by roles, us: 32 rows 8 x 4096 tokens d = 128 41 | 24, one
-  // sequence of 1000 tokens 18 | 13; 64 rows 81 | 42, 22 | 16; 256 rows 265 | 114, 39 | 26; E4M3 alike (d = 64: 1.1 to 1.3 times).  Of
-  // sixteen or fewer, 4 rows, 32 x up to 32768 tokens: 152 us by warps, 200 by roles.
   if (R == 8) return launch_warps<FMT, D, 1>(p, st);
-  if (R == 16) return launch_warps<FMT, D, 2>(p, st);
+  if constexpr (!(FMT == FP4ATTN_FMT_NVFP4 && D == 128))
+    if (R == 16) return launch_warps<FMT, D, 2>(p, st);
   return R == 32 ? launch_tree<FMT, D, 32>(p, st) : launch_tree<FMT, D, 64>(p, st);
 }
 
@@ -1579,7 +1589,7 @@ using namespace fp4attn;
 extern "C" size_t fp4attn_tree_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d) {
   if (B <= 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || T <= 0 || T > FP4ATTN_MOST_TREE_TOKENS || (d != 64 && d != 128)) return 0;
   if ((long long)B * H * T >= (1ll << 31)) return 0;
-  return plan(B, H, kv_heads, T, d).total;
+  return std::max(plan(B, H, kv_heads, T, d, FP4ATTN_FMT_NVFP4).total, plan(B, H, kv_heads, T, d, FP4ATTN_FMT_E4M3).total);
 }
 
 extern "C" int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, const int* block_table,
@@ -1595,8 +1605,8 @@ extern "C" int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4
   if (T > FP4ATTN_MOST_TREE_TOKENS || (long long)B * H * T >= (1ll << 31)) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;     // (items are no more)
   if (((uintptr_t)q->data & 1) || ((uintptr_t)O & 15) || ((uintptr_t)tree_mask & 7) || ((uintptr_t)LSE | (uintptr_t)device_status) & 3)
     return FP4ATTN_ERR_ALIGNMENT;
-  const TreePlan t = plan(B, H, cache->kv_heads, T, cache->d);
-  if (!workspace || workspace_bytes < t.total) return FP4ATTN_ERR_WORKSPACE;
+  const TreePlan t = plan(B, H, cache->kv_heads, T, cache->d, cache->fmt);
+  if (!workspace || workspace_bytes < fp4attn_tree_attention_workspace_bytes(B, H, cache->kv_heads, T, cache->d)) return FP4ATTN_ERR_WORKSPACE;
   if ((uintptr_t)workspace & 15) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   TreeParams p = {};
