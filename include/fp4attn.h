@@ -498,8 +498,10 @@ int fp4attn_cache_read(const fp4attn_cache* cache, const fp4attn_view* k_out, co
  * A row that sees nothing is O = 0, LSE = -infinity.  Positions without a page are seen by no row, and reported if they are below
  * context[b] + count[b].  Bytes of positions that no row sees may hold anything.
  *
- * Scores, row maxima and sums are fp32; K, V and Q enter the products exactly (as f16, Q scaled by a power of two per row),
- * probabilities rounded to f16.  softmax_scale 0: 1 / sqrt(d).  T up to 64.  workspace: device memory of the queried size,
+ * Scores, row maxima and sums are fp32; K and V enter the products exactly, as f16.  So does Q, scaled by a power of two per row, down to 2^-28
+ * of its row's largest element; what is smaller loses low bits, and below 2^-39 of it all.  Probabilities are rounded to f16 for the product with
+ * V (their sum, and so LSE, is not): beside the rounding of O to bf16 that does not show, O in fp16 has up to 1.3 times the root mean square
+ * error of that rounding alone.  softmax_scale 0: 1 / sqrt(d).  T up to 64.  workspace: device memory of the queried size,
  * 16-byte aligned, for this call alone until it has run.
  */
 enum { FP4ATTN_MOST_TREE_TOKENS = 64 };

@@ -8,7 +8,9 @@
 //      lanes at neighbouring addresses.  Where a call's tokens do not fill an eight, V's bytes are written one by one: the others belong to
 //      tokens that are there already.
 // NVFP4, d = 128, 8 KV heads: write of 4 x 4096 tokens 25 us (3.4 TB/s; through shared memory, a head after another, 50), read of 4 x 8192 39 us
-// (4.4 TB/s; 57).  What is left is arithmetic - two divisions a block, conversions, 40-50 % of the ALU - at the occupancy that registers allow.
+// (4.4 TB/s; 57).  What is left is instructions (ALU 54 %, issue 59 % of the write and 70 % of the read) at the occupancy that registers allow: two
+// divisions a block (for V in both lanes that share it), a page looked up for every piece of K.  With rotary positions the same write takes
+// 96 us: 122 to 128 registers, and ranges of heads that divide unevenly; rotary of K and a plain write after it take less than half.
 #include "kv_cache.cuh"
 
 namespace fp4attn {

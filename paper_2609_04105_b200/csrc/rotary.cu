@@ -1,8 +1,8 @@
 // Rotary positions of Q and K, and the transposed rotation for their gradients.
 //
 // Bound by HBM: every element is read once and written once, so a launch takes Q and K together and every access is 16 bytes
-// wide (2 x 4096 tokens of 32 + 8 heads, d = 128, bf16: 32 us, 5.3 TB/s; 4 x 4095 of 32, d = 64, half of each head turned in neighbouring
-// pairs: 37 us, 3.6 TB/s).  A block takes a few tokens and a range of heads.  The cosines and sines of its tokens are worked out once (in 64
+// wide (2 x 4096 tokens of 32 + 8 heads, d = 128, bf16: 33 us, 5.1 TB/s; fp32 57 us, 5.8 TB/s; 4 x 4095 of 32, d = 64, half of each head turned
+// in neighbouring pairs: 37 us, 3.6 TB/s).  A block takes a few tokens and a range of heads.  The cosines and sines of its tokens are worked out once (in 64
 // bits, see cos_sin) into shared memory and serve all of its heads.
 #include "kv_cache.cuh"
 

@@ -20,12 +20,16 @@
 //   sums and an O each: a tile is one long chain of instructions for a warp, and the time of a tile is that of the slowest chain.
 //   then         one warp brings the pages in (one bulk copy per page: a (page, head) record is one run of bytes), two issue the products
 //
-// What bounds it: the softmax chain, 3400 clocks a tile of 64 rows (its products take 800, exp2 512, reading 800): 4 sequences of 8192 tokens, 64
-// drafted tokens of 32 heads over 8 KV heads, d = 128, NVFP4: 97 us, 273 TFLOP/s; 16 drafted tokens of 16 heads over 4, d = 64, E4M3, 8 sequences
-// of up to 4096: 26 us, of which starting, joining and the first tiles are more than half.
+// What bounds it: the softmax chain, 3400 clocks a tile of 64 rows (its products take 800, exp2 512, reading 800), and that every row tile of a
+// KV head copies and converts the keys for itself: 4 sequences of 8192 tokens, 64 drafted tokens of 32 heads over 8 KV heads, d = 128,
+// NVFP4: 98 us, 271 TFLOP/s; 16 drafted tokens of 16 heads over 4, d = 64, E4M3, 8 sequences of up to 4096: 26 us, of which starting,
+// joining and the first tiles are more than half.
 //
 // The reference of a row, its maximum at some time, moves only when a score exceeds it by more than 2^8: probabilities up to 256 fit f16 as
-// well, and neither a reduction over keys (they are in lanes) nor a pass over O is then part of an ordinary tile.
+// well, and neither a reduction over keys (they are in lanes) nor a pass over O is then part of an ordinary tile.  Probabilities are f16 because V
+// is, exactly, and the product takes two operands of one type; each is off by at most 2^-11 of itself.  Beside bf16's rounding of O that is nothing
+// (root mean square error against 64 bits 1.005 of a 32-bit form's); fp16 outputs have up to 1.28 times a 32-bit form's error.  Sums are of the
+// values before they are rounded, for LSE's sake.
 #include "kv_cache.cuh"
 #include "ptx.cuh"
 
@@ -124,7 +128,8 @@ struct TreeCfg {
   static constexpr int kProducer = kFirstSoftmax + 4 * kColGroups * kSets, kIssuerS = kProducer + 1, kIssuerO = kProducer + 2;
   static constexpr int kThreads = 32 * (kProducer + 4);            // the last warp only makes up a warpgroup
   // Registers: 80 a thread at launch.  A softmax thread needs 128 for its 32 rows (with 16 rows a thread and 64 registers a third of
-  // its scores and sums were in local memory: 3850 clocks a tile of 64 rows); the other roles give up what it takes.
+  // its scores and sums were in local memory: 3850 clocks a tile of 64 rows); the other roles give up what it takes.  The compiler allots
+  // for 80 all the same: 81 loads and 47 stores of local memory a tile of 64 rows, all warps together, of 5250 instructions.
   static constexpr int kRegsLaunch = 80, kRegsAux = 32, kRegsKV = 64, kRegsSoftmax = 128;
   static_assert(kThreads * kRegsLaunch <= 65536 &&
                 kRegsAux + (kKGroups + kVGroups) * kRegsKV + kColGroups * kSets * kRegsSoftmax <= kThreads / 128 * kRegsLaunch, "register shares");
@@ -1014,7 +1019,8 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
 // What should bound few rows is the reading; with the roles of the kernel above a tile costs more instructions for handing it from role to
 // role than for its keys (4100 a tile of 128 keys, d = 128, half of them hand-overs; 32 sequences of up to 32768 tokens, 4 rows: 200 us, whose
 // reading takes 94).  Here nothing is handed over (2700 a tile, 152 us; one token over 1000 keys 10 us instead of 11.7): a warp takes 32 keys
-// of a tile from their codes to its own maximum, sum and O, all in registers, and the four warps of a CTA meet at the end of an item.
+// of a tile from their codes to its own maximum, sum and O, all in registers, and the four warps of a CTA meet at the end of an item.  What bounds
+// it is latency: four warps a scheduler do not cover the chain codes - convert - product - exp2 - transpose - product (issue 56 %, ALU 47 %, DRAM 41 %).
 //
 // The operands of the 16 x 8 x 16 products stay where they are loaded, because the orders of keys and of d are free:
 //   S^T = K Q^T   A: keys x d, twice sixteen keys.  Lane (r, c) = (lane / 4, lane % 4) has keys r and r + 8: it takes D / 4 elements of either
