@@ -224,3 +224,29 @@ def test_rotated_write_of_several_heads_a_block(B, kv, N, d, pairs, interleaved,
     Bd.fp4attn_cache_write(one, k, v, table, _i32(starts), inv_freq=f, positions=at if positions else None, interleaved=interleaved)
     Bd.fp4attn_cache_write(two, Bd.fp4attn_rotary(k, at, f, interleaved=interleaved), v, table, _i32(starts))
     assert one.pages.any() and torch.equal(one.pages, two.pages)
+
+
+@pytest.mark.parametrize("group,T", [(1, 5), (2, 8), (4, 8), (4, 16), (4, 40)])
+@pytest.mark.parametrize("fmt,d", [("nvfp4", 128), ("e4m3", 64)])
+def test_tree_attention_rows_that_are_not_finite(fmt, d, group, T):
+    """Queries with NaN and infinities: their own rows are NaN, the rows beside them right."""
+    Bd, g, rng = _bd(), _gen(5 * T + group), np.random.default_rng(T)
+    kv, P, rows = 2, 32, group * T
+    need = 3 * _sms() * (4 if rows <= 16 else 1)
+    B = -(-need // (5 * kv * -(-rows // 64)))
+    context = [5 * TILE - int(x) for x in rng.integers(0, 100, B)]
+    pool = -(-(5 * TILE + T) // P)
+    cache = _cache(Bd, fmt, pool, kv, P, d)
+    everything = torch.arange(pool, device="cuda", dtype=torch.int32)[None]
+    Bd.fp4attn_cache_write(cache, _randn(g, 1, kv, pool * P, d), _randn(g, 1, kv, pool * P, d), everything, _i32([0]))
+    table = everything.expand(B, -1).contiguous()
+    q = _randn(g, B, group * kv, T, d)
+    bad = q.clone()
+    bad[:, 0, 1, 3], bad[:, 0, 3, 5], bad[:, -1, 0, 7], bad[:, -1, 4] = math.nan, math.inf, -math.inf, math.nan
+    got = Bd.fp4attn_tree_attention(bad, cache, table, _i32(context))
+    clean = Bd.fp4attn_tree_attention(q, cache, table, _i32(context))
+    for h, t in ((0, 1), (0, 3), (group * kv - 1, 0), (group * kv - 1, 4)):
+        assert torch.isnan(got[0][:, h, t]).all() and torch.isnan(got[1][:, h, t]).all(), (h, t)
+        for x, y in zip(got, clean):
+            x[:, h, t] = y[:, h, t]
+    _check(got, q, cache, table, context, None, _pool_values(cache))
