@@ -511,6 +511,78 @@ int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4attn_cache*
                            float softmax_scale, void* O, float* LSE, int* device_status, void* workspace, size_t workspace_bytes,
                            fp4attn_stream_t stream);
 
+/*
+ * Attention of T query tokens of every sequence over its cache, T of any size: a step, a chunk of a prompt, a whole prompt.  q [B, H, T, d] (bf16
+ * or fp16), O [B, H, T, d] of that type, contiguous, LSE fp32 [B, H, T] (may be NULL), natural logarithm.  Head h reads KV head
+ * h / (H / kv_heads).
+ *
+ * The T tokens stand in the cache already, token t at position p = context[b] + t; of entry b there are n = count[b] (NULL: T), and rows
+ * t >= n are not written.  Row t sees positions j with first[b, t] <= j < last[b, t] and j < context[b] + n (int32 [B, T], device; first NULL: 0,
+ * last NULL: p + 1).  So a document's tokens see the document from first = its beginning on, a window of W is first = p + 1 - W, a prefix of L
+ * tokens that sees itself whole is last = max(p + 1, L).  With s = softmax_scale q.k (softmax_scale 0: 1 / sqrt(d)) a score is
+ *     x = soft_cap tanh(s / soft_cap) (soft_cap 0: s)  -  slopes[h] |p - j| (fp32 [H], device; NULL: 0)
+ * and O = softmax(x) V.  A row that sees nothing is O = 0, LSE = -infinity.  Bytes of positions that a row does not see may hold anything.
+ * Positions without a page are seen by no row; FP4ATTN_ERR_PAGE reports those that a row would see, and may report those that lie between
+ * positions that rows see.
+ *
+ * Precision as fp4attn_tree_attention (16-bit probabilities, fp32 scores, maxima, sums and O); a capped score is off by no more than 2^-20 of
+ * soft_cap, a bias by no more than 2^-21 of its slope times the largest distance.  workspace: device memory of the queried size, 16-byte aligned, for this call alone
+ * until it has run.  Two calls with the same arguments give the same bits.
+ */
+size_t fp4attn_paged_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d);
+int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, const int* block_table,
+                            int max_pages, const int* context, const int* count, const int* first, const int* last, float softmax_scale,
+                            float soft_cap, const float* slopes, void* O, float* LSE, int* device_status, void* workspace,
+                            size_t workspace_bytes, fp4attn_stream_t stream);
+
+/*
+ * The same for T <= 64 tokens of a batch whose sequences share prefixes, each read once for all of its sequences.  Entries
+ * group_start[g] .. group_start[g + 1] - 1 (int32 [groups + 1], device, not decreasing, clipped to 0 .. B) are those of group g; their first
+ * prefix_length[g] tokens (int32 [groups]) stand in the pages of prefix_table[g] (int32 [groups, prefix_pages]), the others as without a prefix:
+ * context[b] tokens, then the T of the call, in the pages of block_table[b].  Row t sees the prefix, the context, and of the T tokens those
+ * whose bit of tree_mask[b, t] is set (u64 [B, T]; NULL: j <= t), as in fp4attn_tree_attention (a mask may look behind the count).  An entry that
+ * is in no group has no prefix.  Distances of a bias count the prefix: p = prefix_length[g] + context[b] + t.
+ * The prefixes' last page may be partly filled; no page of a prefix needs to be a whole one.
+ */
+size_t fp4attn_shared_prefix_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d, int groups);
+int fp4attn_shared_prefix_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, int groups,
+                                    const int* prefix_table, int prefix_pages, const int* prefix_length, const int* group_start,
+                                    const int* block_table, int max_pages, const int* context, const int* count,
+                                    const unsigned long long* tree_mask, float softmax_scale, float soft_cap, const float* slopes, void* O,
+                                    float* LSE, int* device_status, void* workspace, size_t workspace_bytes, fp4attn_stream_t stream);
+
+/*
+ * Pages of a cache out of a stack of free ones: free[0 .. *count - 1] are the numbers of the free pages (int32 [num_pages], device; pages of
+ * the pool are numbered 0 .. num_pages - 1), *turn is 0 between calls (int32 [1], device).  Calls on one pool must not overlap on the GPU.
+ */
+typedef struct {
+  int* free;
+  int* count;
+  int* turn;
+  int num_pages, page_size;
+} fp4attn_page_pool;
+
+/*
+ * Pages for the next tokens of a batch, and where those go.  Entry b has start[b] tokens, so the first ceil(start[b] / page_size) of its pages
+ * are in its table; for count[b] more (int32 [B]; NULL: N) it gets those up to ceil((start[b] + count[b]) / page_size), taken from the top of
+ * the stack in the order of the entries and of their tables.  Where the stack has run out, -1 is written; that, and a table without room for an
+ * entry's pages, is reported (FP4ATTN_ERR_PAGE).  An entry with a negative start, or no tokens, gets nothing.
+ * slots (int64 [B, N], may be NULL): page * page_size + place in it of token n < count[b], -1 where it has no page and behind the count;
+ * positions (int32 [B, N], may be NULL): start[b] + n.  N = 0 (with count given): no slots, no positions.
+ */
+int fp4attn_pages_assign(const fp4attn_page_pool* pool, int B, int N, int* block_table, int max_pages, const int* start, const int* count,
+                         long long* slots, int* positions, int* device_status, fp4attn_stream_t stream);
+
+/*
+ * Pages back onto the stack: of entry b, whose length[b] tokens hold ceil(length[b] / page_size) pages, those behind the first keep[b] tokens'
+ * (int32 [B]; NULL: 0, all of them).  Their places in the table become -1; places that hold no page of the pool are passed over.  The last page of
+ * the last entry goes down first, so that a release of what one assign gave leaves the stack as it was.  More pages than the pool has (one
+ * released twice) are dropped and reported (FP4ATTN_ERR_PAGE).  workspace: device memory, 4-byte aligned.
+ */
+size_t fp4attn_pages_release_workspace_bytes(int B);
+int fp4attn_pages_release(const fp4attn_page_pool* pool, int B, int* block_table, int max_pages, const int* length, const int* keep,
+                          int* device_status, void* workspace, size_t workspace_bytes, fp4attn_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -129,3 +129,75 @@ def attend(q, k, v, mask, scale):
     p = p / np.where(any_seen, total, 1.0)[:, None]
     size = np.where(mask, (np.abs(q) @ np.abs(k).T) * scale, 0.0).max(1, initial=0.0)
     return p @ v, lse, p @ np.abs(v), size
+
+
+def attend_scores(q, k, v, mask, scale, cap=0.0, slope=0.0, distance=None):
+    """`attend` with scores capped by a tanh and a bias by distance [T,n]; also the largest |score| before the cap that a row sees."""
+    z = (q @ k.T) * scale
+    raw = np.where(mask, np.abs(z), 0.0).max(1, initial=0.0)
+    if cap:
+        z = cap * np.tanh(z / cap)
+    if distance is not None:
+        z = z - slope * distance
+    z = np.where(mask, z, -np.inf)
+    any_seen = mask.any(1)
+    top = np.where(any_seen, z.max(1, initial=-np.inf), 0.0)
+    p = np.exp(z - top[:, None])
+    total = p.sum(1)
+    with np.errstate(divide="ignore"):
+        lse = np.where(any_seen, top + np.log(total), -np.inf)
+    p = p / np.where(any_seen, total, 1.0)[:, None]
+    size = np.where(mask, (np.abs(q) @ np.abs(k).T) * scale, 0.0).max(1, initial=0.0)
+    return p @ v, lse, p @ np.abs(v), size, raw
+
+
+def between(context, T, n, first=None, last=None):
+    """Truth values [T, context + n]: what the rows of a sequence see, None as fp4attn_paged_attention takes it."""
+    ctx, n = max(0, int(context)), min(max(int(n), 0), T)
+    j = np.arange(ctx + n)[None]
+    lo = np.zeros((T, 1)) if first is None else np.asarray(first)[:, None]
+    hi = (ctx + np.arange(T) + 1)[:, None] if last is None else np.asarray(last)[:, None]
+    return (j >= lo) & (j < hi)
+
+
+def pages_assign(free, left, table, start, count, N, P):
+    """free int array, table int array [B,pages], both lists of lists or arrays, in place -> pages left, slots [B][N], positions, fine?"""
+    fine = True
+    B, room = len(table), len(table[0])
+    slots, positions = [[-1] * N for _ in range(B)], [[int(start[b]) + n for n in range(N)] for b in range(B)]
+    for b in range(B):
+        s, c = int(start[b]), max(0, int(count[b]) if count is not None else N)
+        if s >= 0:
+            for i in range(-(-s // P), -(-(s + c) // P) if c else 0):
+                if i >= room:
+                    fine = False
+                    break
+                if left > 0:
+                    left -= 1
+                    table[b][i] = free[left]
+                else:
+                    table[b][i] = -1
+                    fine = False
+        for n in range(min(N, c)):
+            pos = s + n
+            if s >= 0 and pos // P < room and 0 <= table[b][pos // P] < len(free):
+                slots[b][n] = int(table[b][pos // P]) * P + pos % P
+    return left, slots, positions, fine
+
+
+def pages_release(free, left, table, length, keep, P):
+    """In place -> pages on the stack, fine?"""
+    going = []
+    for b in range(len(table)):
+        for i in range(-(-max(0, int(keep[b]) if keep is not None else 0) // P), min(-(-max(0, int(length[b])) // P), len(table[0]))):
+            if 0 <= table[b][i] < len(free):
+                going.append(table[b][i])
+            table[b][i] = -1
+    fine = True
+    for page in reversed(going):
+        if left < len(free):
+            free[left] = page
+            left += 1
+        else:
+            fine = False
+    return left, fine

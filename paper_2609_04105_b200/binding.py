@@ -46,6 +46,9 @@ EXPORTS = [
     "fp4attn_quantize_v_e4m3_workspace_bytes", "fp4attn_quantize_v_e4m3",
     "fp4attn_rotary", "fp4attn_cache_record_bytes", "fp4attn_cache_write", "fp4attn_cache_read",
     "fp4attn_tree_attention_workspace_bytes", "fp4attn_tree_attention",
+    "fp4attn_paged_attention_workspace_bytes", "fp4attn_paged_attention",
+    "fp4attn_shared_prefix_attention_workspace_bytes", "fp4attn_shared_prefix_attention",
+    "fp4attn_pages_assign", "fp4attn_pages_release_workspace_bytes", "fp4attn_pages_release",
 ]
 
 
@@ -118,7 +121,9 @@ _NATIVE_CALLS = ["fp4attn_status_string", "fp4attn_packed_bytes", "fp4attn_scale
                  "fp4attn_quantize", "fp4attn_quantize_mxfp4_rule", "fp4attn_quantize_nvfp4_per_head_workspace_bytes",
                  "fp4attn_quantize_nvfp4_per_head", "fp4attn_quantize_v_e4m3_workspace_bytes", "fp4attn_quantize_v_e4m3",
                  "fp4attn_fwd", "fp4attn_rotary", "fp4attn_cache_record_bytes", "fp4attn_cache_write", "fp4attn_cache_read",
-                 "fp4attn_tree_attention_workspace_bytes", "fp4attn_tree_attention"]
+                 "fp4attn_tree_attention_workspace_bytes", "fp4attn_tree_attention",
+                 "fp4attn_paged_attention_workspace_bytes", "fp4attn_paged_attention", "fp4attn_shared_prefix_attention_workspace_bytes",
+                 "fp4attn_shared_prefix_attention", "fp4attn_pages_assign", "fp4attn_pages_release_workspace_bytes", "fp4attn_pages_release"]
 
 
 def _load_native(lib_: ctypes.CDLL):
@@ -366,6 +371,70 @@ def fp4attn_tree_attention(q: torch.Tensor, cache: QuantizedCache, block_table: 
     -infinity.  Rows t >= count[b] are left as they were (0 and -infinity in tensors that this call made); a batch padded to its size
     has entries with count 0, which need no pages."""
     return (_native_module or _native()).tree_attention(q, cache, block_table, context, tree_mask, count, softmax_scale, out, lse, status)
+
+
+def fp4attn_paged_attention(q: torch.Tensor, cache: QuantizedCache, block_table: torch.Tensor, context: torch.Tensor,
+                            count: Optional[torch.Tensor] = None, first: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None,
+                            softmax_scale: float = 0.0, soft_cap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                            out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                            status: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of T tokens of every sequence over the cache, T of any size (a step, a prompt's chunk, a prompt): q [B,H,T,d] (bf16 or
+    fp16) -> (O of q's type [B,H,T,d], LSE fp32 [B,H,T]).  The tokens are in the cache, token t at position p = context[b] + t (int32 [B]);
+    row t sees positions first[b,t] <= j < last[b,t] of those that are there (int32 [B,T]; None: from 0, up to p) - a document, a window, a prefix
+    that sees itself whole.  Scores are soft_cap * tanh(score / soft_cap) (0: as they are) - slopes[h] * |p - j| (fp32 [H]; None: no bias).  A row
+    that sees nothing is 0, its LSE -infinity.  Rows t >= count[b] are left as they were (0 and -infinity in tensors that this call made)."""
+    return (_native_module or _native()).paged_attention(q, cache, block_table, context, count, first, last, softmax_scale, soft_cap, slopes,
+                                                         out, lse, status)
+
+
+def fp4attn_shared_prefix_attention(q: torch.Tensor, cache: QuantizedCache, prefix_table: torch.Tensor, prefix_length: torch.Tensor,
+                                    group_start: torch.Tensor, block_table: torch.Tensor, context: torch.Tensor,
+                                    tree_mask: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                                    softmax_scale: float = 0.0, soft_cap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                                    status: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """fp4attn_tree_attention for a batch whose sequences share prefixes, each read once for all of its sequences.  Entries group_start[g] ..
+    group_start[g+1] - 1 (int32 [groups + 1], not decreasing) begin with the prefix_length[g] tokens (int32 [groups]) in the pages of
+    prefix_table[g] (int32 [groups, pages]); block_table and context say what a sequence has of its own behind it.  soft_cap and slopes as in
+    fp4attn_paged_attention; distances count the prefix."""
+    return (_native_module or _native()).shared_prefix_attention(q, cache, prefix_table, prefix_length, group_start, block_table, context, tree_mask,
+                                                                 count, softmax_scale, soft_cap, slopes, out, lse, status)
+
+
+@dataclass
+class PagePool:
+    """The free pages of a cache, on its device: a stack.  The pool's pages are numbered 0 .. free.numel() - 1."""
+    free: torch.Tensor                # int32 [pages]: free[:count] are the free pages
+    count: torch.Tensor               # int32 [1]
+    page_size: int
+    turn: Optional[torch.Tensor] = None        # int32 [1], 0 between calls
+
+    def __post_init__(self):
+        if self.turn is None:
+            self.turn = torch.zeros(1, dtype=torch.int32, device=self.free.device)
+
+
+def fp4attn_pages_create(num_pages: int, page_size: int, device="cuda") -> PagePool:
+    """A pool of num_pages free pages; page 0 is taken first."""
+    free = torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device)
+    return PagePool(free, torch.full((1,), num_pages, dtype=torch.int32, device=device), page_size)
+
+
+def fp4attn_pages_assign(pool: PagePool, block_table: torch.Tensor, start: torch.Tensor, count: Optional[torch.Tensor] = None, N: int = 0,
+                         status: Optional[torch.Tensor] = None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Pages for tokens start[b] .. start[b] + count[b] - 1 of every sequence (int32 [B]; count None: N tokens), written into block_table (int32
+    [B, pages of a sequence]) behind the ceil(start[b] / page_size) that are there -> (slots int64 [B,N]: page * page_size + place, -1 for what has
+    no page and behind the count; positions int32 [B,N]: start[b] + n); (None, None) with N = 0.  Where the pool or the table has no page
+    left, ERR_PAGE goes to `status` (int32 [1], cleared by the caller) and -1 into the table.  Nothing waits for the host; calls on one pool
+    must not overlap."""
+    return (_native_module or _native()).pages_assign(pool, block_table, start, count, N, status)
+
+
+def fp4attn_pages_release(pool: PagePool, block_table: torch.Tensor, length: torch.Tensor, keep: Optional[torch.Tensor] = None,
+                          status: Optional[torch.Tensor] = None) -> None:
+    """The pages of sequences of length[b] tokens (int32 [B]) back into the pool, but those of the first keep[b] tokens (int32 [B]; None: 0);
+    their places in block_table become -1.  Undoes an assign exactly: keep what there was before it."""
+    (_native_module or _native()).pages_release(pool, block_table, length, keep, status)
 
 
 def fp4attn_attention_host_workspace_bytes(qk_fmt: int, B: int, H: int, N: int, d: int) -> int:

@@ -39,12 +39,21 @@ struct Api {
   decltype(&fp4attn_cache_read) cache_read;
   decltype(&fp4attn_tree_attention_workspace_bytes) tree_workspace_bytes;
   decltype(&fp4attn_tree_attention) tree_attention;
+  decltype(&fp4attn_paged_attention_workspace_bytes) paged_workspace_bytes;
+  decltype(&fp4attn_paged_attention) paged_attention;
+  decltype(&fp4attn_shared_prefix_attention_workspace_bytes) shared_workspace_bytes;
+  decltype(&fp4attn_shared_prefix_attention) shared_prefix_attention;
+  decltype(&fp4attn_pages_assign) pages_assign;
+  decltype(&fp4attn_pages_release_workspace_bytes) release_workspace_bytes;
+  decltype(&fp4attn_pages_release) pages_release;
 };
 Api g_api;
 PyObject* g_error = nullptr;                            // Fp4AttnError
 enum { A_PACKED, A_SCALES, A_G, A_FMT, A_ROLE, A_SHAPE, A_PER_HEAD, A_COUNT };
 enum { C_PAGES, C_K_G, C_V_G, C_FMT, C_PAGE_SIZE, C_D, C_COUNT };
+enum { P_FREE, P_COUNT_OF, P_TURN, P_PAGE_SIZE, P_COUNT };
 PyObject* g_cache_names[C_COUNT];
+PyObject* g_pool_names[P_COUNT];
 PyObject* g_names[A_COUNT];
 constexpr int kFmtE4m3 = 2;                             // QuantizedOperand.fmt of an E4M3 V
 
@@ -716,7 +725,215 @@ PyObject* py_tree_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   FP4_CATCH
 }
 
-// init(error class, status_string, packed_bytes, ..., tree_attention): addresses of the library's functions, in Api's order
+// ---------------------------------------------------------------- prompts and shared prefixes over the cache
+
+// What attention over a cache takes besides its masks, and what it gives: checks, outputs, workspace
+struct Attention {
+  Cache cache;
+  Strided q;
+  Batch batch;
+  float scale = 0.f, cap = 0.f;
+  void *slopes = nullptr, *out_ptr = nullptr, *lse_ptr = nullptr;
+  THPObjectPtr out, lse;
+  at::Tensor ws;
+  size_t nw = 0;
+  // null, or what is wrong ("": an exception is set)
+  const char* take(PyObject* q_o, PyObject* cache_o, PyObject* table, PyObject* context, PyObject* count, PyObject* scale_o, PyObject* cap_o,
+                   PyObject* slopes_o, PyObject* out_o, PyObject* lse_o, PyObject* status) {
+    if (const char* wrong = cache.take(cache_o)) return wrong;
+    if (!q.take(q_o, false) || q.d != cache.c.d || q.t->device() != cache.device || cache.c.kv_heads < 1 || q.H % cache.c.kv_heads != 0)
+      return q.empty ? kNothing : "q must be a CUDA tensor [B, H, T, d] of the cache's d and device, bfloat16 or float16, the last axis contiguous; H a multiple of the KV heads";
+    if (const char* wrong = batch.take(q.B, cache.device, table, context, count, status)) return wrong;
+    if (!number(scale_o, &scale) || !number(cap_o, &cap)) return "";
+    if (!plain(slopes_o, at::kFloat, q.H, cache.device, true, &slopes)) return "slopes must be a contiguous CUDA float32 tensor [H] on the cache's device";
+    const int64_t rows = (int64_t)q.B * q.H * q.N;
+    if (!plain(out_o, q.t->scalar_type(), rows * q.d, cache.device, true, &out_ptr) || !shaped(out_o, {q.B, q.H, q.N, q.d}) ||
+        !plain(lse_o, at::kFloat, rows, cache.device, true, &lse_ptr) || !shaped(lse_o, {q.B, q.H, q.N}))
+      return "out [B, H, T, d] of q's type and lse [B, H, T] float32 must be contiguous CUDA tensors on the cache's device";
+    if (c10::GradMode::is_enabled() && (q.t->requires_grad() || (slopes && THPVariable_Unpack(slopes_o).requires_grad())))
+      return "attention over a quantized cache takes no gradient: detach the inputs, or call under torch.no_grad()";
+    return nullptr;
+  }
+  // false: an exception is set
+  bool allocate(PyObject* out_o, PyObject* lse_o, size_t bytes) {
+    nw = bytes;
+    out = THPObjectPtr(Py_NewRef(out_o));
+    lse = THPObjectPtr(Py_NewRef(lse_o));
+    Results r;
+    at::Tensor none, &o = out_ptr ? none : r.add({q.B, q.H, q.N, q.d}, q.t->scalar_type()), &l = lse_ptr ? none : r.add({q.B, q.H, q.N}, at::kFloat);
+    if (r.n) r.allocate(cache.device);
+    if (nw) ws = device_empty({(int64_t)nw}, at::kByte, cache.device);
+    if (o.defined()) {
+      if (batch.count) o.zero_();                        // rows behind the counts are not written
+      out_ptr = o.data_ptr();
+      out = THPVariable_Wrap(o);
+    }
+    if (l.defined()) {
+      if (batch.count) l.fill_(-std::numeric_limits<float>::infinity());
+      lse_ptr = l.data_ptr();
+      lse = THPVariable_Wrap(l);
+    }
+    return out && lse;
+  }
+  void* workspace() const { return nw ? ws.data_ptr() : nullptr; }
+  PyObject* give() { return Py_BuildValue("(NN)", out.release(), lse.release()); }
+};
+
+// paged_attention(q, cache, block_table, context, count, first, last, softmax_scale, soft_cap, slopes, out, lse, status) -> (out, lse)
+PyObject* py_paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  FP4_TRY
+  if (n != 13) return assertion("paged_attention takes 13 arguments");
+  Attention a;
+  if (const char* wrong = a.take(args[0], args[1], args[2], args[3], args[4], args[7], args[8], args[9], args[10], args[11], args[12]))
+    return *wrong ? assertion(wrong) : nullptr;
+  const Strided& q = a.q;
+  void *first, *last;
+  if (!plain(args[5], at::kInt, (int64_t)q.B * q.N, a.cache.device, true, &first) || !shaped(args[5], {q.B, q.N}) ||
+      !plain(args[6], at::kInt, (int64_t)q.B * q.N, a.cache.device, true, &last) || !shaped(args[6], {q.B, q.N}))
+    return assertion("first and last must be contiguous CUDA int32 tensors [B, T] on the cache's device");
+  const c10::cuda::OptionalCUDAGuard guard(a.cache.device);
+  if (!a.allocate(args[10], args[11], g_api.paged_workspace_bytes(q.B, q.H, a.cache.c.kv_heads, q.N, q.d))) return nullptr;
+  const int rc = unlocked([&] {
+    return g_api.paged_attention(&q.view, q.type, &a.cache.c, q.B, q.H, q.N, a.batch.table, a.batch.max_pages, a.batch.start, a.batch.count,
+                                 (const int*)first, (const int*)last, a.scale, a.cap, (const float*)a.slopes, a.out_ptr, (float*)a.lse_ptr,
+                                 a.batch.status, a.workspace(), a.nw, stream());
+  });
+  if (rc) return fail(rc, "fp4attn_paged_attention");
+  return a.give();
+  FP4_CATCH
+}
+
+// shared_prefix_attention(q, cache, prefix_table, prefix_length, group_start, block_table, context, tree_mask, count, softmax_scale, soft_cap,
+//                         slopes, out, lse, status) -> (out, lse)
+PyObject* py_shared_prefix_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  FP4_TRY
+  if (n != 15) return assertion("shared_prefix_attention takes 15 arguments");
+  Attention a;
+  if (const char* wrong = a.take(args[0], args[1], args[5], args[6], args[8], args[9], args[10], args[11], args[12], args[13], args[14]))
+    return *wrong ? assertion(wrong) : nullptr;
+  const Strided& q = a.q;
+  const char* const prefix_rule = "prefix_table must be a contiguous CUDA int32 tensor [groups, pages of a prefix] on the cache's device";
+  if (!THPVariable_Check(args[2]) || THPVariable_Unpack(args[2]).dim() != 2) return assertion(prefix_rule);
+  const int64_t groups = THPVariable_Unpack(args[2]).size(0), pages = THPVariable_Unpack(args[2]).size(1);
+  void *table, *length, *start, *mask;
+  if (groups < 1 || pages < 1 || groups > INT32_MAX || pages > INT32_MAX || !plain(args[2], at::kInt, groups * pages, a.cache.device, false, &table))
+    return assertion(prefix_rule);
+  if (!plain(args[3], at::kInt, groups, a.cache.device, false, &length)) return assertion("prefix_length must be a contiguous CUDA int32 tensor of one length per group on the cache's device");
+  if (!plain(args[4], at::kInt, groups + 1, a.cache.device, false, &start)) return assertion("group_start must be a contiguous CUDA int32 tensor of groups + 1 entries on the cache's device");
+  if (!plain(args[7], at::kLong, (int64_t)q.B * q.N, a.cache.device, true, &mask) || !shaped(args[7], {q.B, q.N}))
+    return assertion("tree_mask must be a contiguous CUDA int64 tensor [B, T] on the cache's device");
+  const c10::cuda::OptionalCUDAGuard guard(a.cache.device);
+  if (!a.allocate(args[12], args[13], g_api.shared_workspace_bytes(q.B, q.H, a.cache.c.kv_heads, q.N, q.d, (int)groups))) return nullptr;
+  const int rc = unlocked([&] {
+    return g_api.shared_prefix_attention(&q.view, q.type, &a.cache.c, q.B, q.H, q.N, (int)groups, (const int*)table, (int)pages, (const int*)length,
+                                         (const int*)start, a.batch.table, a.batch.max_pages, a.batch.start, a.batch.count,
+                                         (const unsigned long long*)mask, a.scale, a.cap, (const float*)a.slopes, a.out_ptr, (float*)a.lse_ptr,
+                                         a.batch.status, a.workspace(), a.nw, stream());
+  });
+  if (rc) return fail(rc, "fp4attn_shared_prefix_attention");
+  return a.give();
+  FP4_CATCH
+}
+
+// ---------------------------------------------------------------- pages out of a pool
+
+struct Pool {
+  fp4attn_page_pool c{};
+  c10::Device device{c10::kCPU};
+  const char* take(PyObject* o) {                        // null, or what is wrong ("": an exception is set)
+    PyObject* v[P_COUNT] = {};
+    const char* wrong = nullptr;
+    for (int i = 0; i < P_COUNT && !wrong; ++i)
+      if (!(v[i] = PyObject_GetAttr(o, g_pool_names[i]))) wrong = "";
+    if (!wrong) wrong = read(v);
+    for (int i = 0; i < P_COUNT; ++i) Py_XDECREF(v[i]);
+    return wrong;
+  }
+
+ private:
+  const char* read(PyObject** v) {
+    const char* const rule = "pool.free must be a contiguous CUDA int32 tensor of page numbers, pool.count and pool.turn int32 tensors of one element on its device";
+    if (!THPVariable_Check(v[P_FREE])) return rule;
+    const at::Tensor& t = THPVariable_Unpack(v[P_FREE]);
+    device = t.device();
+    void *free, *count, *turn;
+    if (t.numel() < 1 || t.numel() > INT32_MAX || !plain(v[P_FREE], at::kInt, t.numel(), device, false, &free) ||
+        !plain(v[P_COUNT_OF], at::kInt, 1, device, false, &count) || !plain(v[P_TURN], at::kInt, 1, device, false, &turn))
+      return rule;
+    if (!ints(v + P_PAGE_SIZE, 1, &c.page_size)) return "";
+    c.free = (int*)free; c.count = (int*)count; c.turn = (int*)turn;
+    c.num_pages = (int)t.numel();
+    return nullptr;
+  }
+};
+
+// block_table, which is written
+const char* take_table(PyObject* o, c10::Device device, int** table, int* B, int* max_pages) {
+  const char* const rule = "block_table must be a contiguous CUDA int32 tensor [B, pages of a sequence] on the pool's device";
+  if (!THPVariable_Check(o)) return rule;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.dim() != 2 || !t.is_cuda() || t.scalar_type() != at::kInt || !t.is_contiguous() || t.device() != device) return rule;
+  if (t.size(0) < 1 || t.size(0) > INT32_MAX) return kNothing;
+  if (t.size(1) < 1 || t.size(1) > INT32_MAX) return rule;
+  *table = t.data_ptr<int>();
+  *B = (int)t.size(0);
+  *max_pages = (int)t.size(1);
+  return nullptr;
+}
+
+// pages_assign(pool, block_table, start, count, N, status) -> (slots, positions), or (None, None) with N = 0
+PyObject* py_pages_assign(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  FP4_TRY
+  if (n != 6) return assertion("pages_assign takes 6 arguments");
+  Pool pool;
+  if (const char* wrong = pool.take(args[0])) return *wrong ? assertion(wrong) : nullptr;
+  int *table, B, max_pages, N;
+  if (const char* wrong = take_table(args[1], pool.device, &table, &B, &max_pages)) return assertion(wrong);
+  if (!ints(args + 4, 1, &N)) return nullptr;
+  if (N < 0 || (N == 0 && args[3] == Py_None)) return assertion("N must be a number of tokens; it may be 0 where count is given");
+  void *start, *count, *status;
+  if (!plain(args[2], at::kInt, B, pool.device, false, &start) || !plain(args[3], at::kInt, B, pool.device, true, &count))
+    return assertion("start and count must be contiguous CUDA int32 tensors of B values on the pool's device");
+  if (!plain(args[5], at::kInt, 1, pool.device, true, &status)) return assertion("status must be a CUDA int32 tensor of one element on the pool's device");
+  const c10::cuda::OptionalCUDAGuard guard(pool.device);
+  Results r;
+  at::Tensor none, &slots = N ? r.add({B, N}, at::kLong) : none, &positions = N ? r.add({B, N}, at::kInt) : none;
+  if (N) r.allocate(pool.device);
+  const int rc = unlocked([&] {
+    return g_api.pages_assign(&pool.c, B, N, table, max_pages, (const int*)start, (const int*)count, N ? (long long*)slots.data_ptr() : nullptr,
+                              N ? positions.data_ptr<int>() : nullptr, (int*)status, stream());
+  });
+  if (rc) return fail(rc, "fp4attn_pages_assign");
+  if (!N) return Py_BuildValue("(OO)", Py_None, Py_None);
+  return Py_BuildValue("(NN)", THPVariable_Wrap(slots), THPVariable_Wrap(positions));
+  FP4_CATCH
+}
+
+// pages_release(pool, block_table, length, keep, status)
+PyObject* py_pages_release(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  FP4_TRY
+  if (n != 5) return assertion("pages_release takes 5 arguments");
+  Pool pool;
+  if (const char* wrong = pool.take(args[0])) return *wrong ? assertion(wrong) : nullptr;
+  int *table, B, max_pages;
+  if (const char* wrong = take_table(args[1], pool.device, &table, &B, &max_pages)) return assertion(wrong);
+  void *length, *keep, *status;
+  if (!plain(args[2], at::kInt, B, pool.device, false, &length) || !plain(args[3], at::kInt, B, pool.device, true, &keep))
+    return assertion("length and keep must be contiguous CUDA int32 tensors of B values on the pool's device");
+  if (!plain(args[4], at::kInt, 1, pool.device, true, &status)) return assertion("status must be a CUDA int32 tensor of one element on the pool's device");
+  const c10::cuda::OptionalCUDAGuard guard(pool.device);
+  const size_t nw = g_api.release_workspace_bytes(B);
+  at::Tensor ws;
+  if (nw) ws = device_empty({(int64_t)nw}, at::kByte, pool.device);
+  const int rc = unlocked([&] {
+    return g_api.pages_release(&pool.c, B, table, max_pages, (const int*)length, (const int*)keep, (int*)status, nw ? ws.data_ptr() : nullptr, nw, stream());
+  });
+  if (rc) return fail(rc, "fp4attn_pages_release");
+  Py_RETURN_NONE;
+  FP4_CATCH
+}
+
+// init(error class, status_string, packed_bytes, ..., pages_release): addresses of the library's functions, in Api's order
 PyObject* py_init(PyObject*, PyObject* const* args, Py_ssize_t n) {
   constexpr Py_ssize_t kFunctions = sizeof(Api) / sizeof(void*);
   if (n != 1 + kFunctions) return assertion("init takes the error class and one address per function");
@@ -734,7 +951,9 @@ PyObject* py_init(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {FP4_METHOD("init", py_init), FP4_METHOD("quantize", py_quantize), FP4_METHOD("quantize_mxfp4_rule", py_rule),
                          FP4_METHOD("quantize_nvfp4_per_head", py_per_head), FP4_METHOD("quantize_v_e4m3", py_e4m3),
                          FP4_METHOD("fwd", py_fwd), FP4_METHOD("rotary", py_rotary), FP4_METHOD("cache_write", py_cache_write),
-                         FP4_METHOD("cache_read", py_cache_read), FP4_METHOD("tree_attention", py_tree_attention), {nullptr, nullptr, 0, nullptr}};
+                         FP4_METHOD("cache_read", py_cache_read), FP4_METHOD("tree_attention", py_tree_attention),
+                         FP4_METHOD("paged_attention", py_paged_attention), FP4_METHOD("shared_prefix_attention", py_shared_prefix_attention),
+                         FP4_METHOD("pages_assign", py_pages_assign), FP4_METHOD("pages_release", py_pages_release), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fp4attn_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -746,5 +965,8 @@ extern "C" __attribute__((visibility("default"))) PyObject* PyInit__fp4attn_nati
   const char* cache_names[C_COUNT] = {"pages", "k_G", "v_G", "fmt", "page_size", "d"};
   for (int i = 0; i < C_COUNT; ++i)
     if (!(g_cache_names[i] = PyUnicode_InternFromString(cache_names[i]))) return nullptr;
+  const char* pool_names[P_COUNT] = {"free", "count", "turn", "page_size"};
+  for (int i = 0; i < P_COUNT; ++i)
+    if (!(g_pool_names[i] = PyUnicode_InternFromString(pool_names[i]))) return nullptr;
   return PyModule_Create(&module);
 }

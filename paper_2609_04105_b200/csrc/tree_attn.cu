@@ -30,8 +30,7 @@
 // is, exactly, and the product takes two operands of one type; each is off by at most 2^-11 of itself.  Beside bf16's rounding of O that is nothing
 // (root mean square error against 64 bits 1.005 of a 32-bit form's); fp16 outputs have up to 1.28 times a 32-bit form's error.  Sums are of the
 // values before they are rounded, for LSE's sake.
-#include "kv_cache.cuh"
-#include "ptx.cuh"
+#include "cache_attn.cuh"
 
 #include <limits.h>
 
@@ -39,18 +38,12 @@
 
 namespace fp4attn {
 
-int check_cache(const fp4attn_cache* c, int B, const int* block_table, int max_pages, const int* start, const int* count, CacheRef* ref);
-
 namespace {
 using namespace ptx;
 
-constexpr int kTile = 128;                 // keys of a tile
 // CTAs of a call, each of which may leave two partial results: four an SM by warps, one by roles
 constexpr int kMostWarpCtas = 640, kMostRoleCtas = 160;
 template <int R> constexpr int kMostCtas = R <= 16 ? kMostWarpCtas : kMostRoleCtas;
-constexpr float kLag = 8.f;                // octaves by which a score may exceed its row's reference
-constexpr float kShift = 7.f;              // a probability of 1 is 2^7: with the lag just inside f16, whose subnormals then begin at 2^-21
-
 struct TreeParams {
   const void* q;
   long long q_sb, q_sh, q_sn;
@@ -86,7 +79,6 @@ __device__ __forceinline__ int load_entry(Walk& w, const TreeParams& p) {
   w.len = n ? (int)min((long long)c + (p.mask ? p.T : n), (long long)room) : 0;        // (a mask may look behind the count)
   return max(1, (w.len + kTile - 1) / kTile);
 }
-__device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
 __device__ __forceinline__ void next_item(Walk& w, const TreeParams& p, int units) {
   w.first = 0;
   if (++w.u == units) {
@@ -170,49 +162,6 @@ struct TreeCfg {
   static_assert(kO + R * kSets <= 512, "tensor memory");
 };
 
-// Waits for a barrier's phase; the whole warp goes on together.  A wait that runs out, or sees that another one did, sets the abort word
-// and returns as if the phase had come: what the roles then read and multiply means nothing, but stays in bounds, and every wait of
-// theirs ends at once, so that they run out of tiles.  The phase has come at the first look, or while that look was suspended, in nearly
-// every wait.  CALL: the loop behind it is a function of its own: inlined at each wait it took up to 12 % of the time, in instruction
-// fetches.  (Code that shares out registers by setmaxnreg may not call.)
-__device__ __forceinline__ void poll_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
-  uint32_t since = 0;
-  for (uint32_t n = 1;; ++n) {
-    uint32_t gone;
-    asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(gone) : "r"(abort_at) : "memory");
-    if (gone || mbar_try_wait(bar, parity)) return;
-    if (n % kPolls) continue;
-    uint32_t now;
-    asm volatile("mov.u32 %0, %%clock;" : "=r"(now));
-    if (n == kPolls) since = now;
-    if (now - since >= kWaitClocks) break;
-  }
-  asm volatile("st.volatile.shared.u32 [%0], 1;" ::"r"(abort_at) : "memory");
-}
-__device__ __noinline__ void wait_longer(uint32_t bar, uint32_t parity, uint32_t abort_at) { poll_phase(bar, parity, abort_at); }
-template <bool CALL>
-__device__ __forceinline__ void wait_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
-  if (rare(!mbar_try_wait(bar, parity))) {
-    if (CALL) wait_longer(bar, parity, abort_at);
-    else poll_phase(bar, parity, abort_at);
-  }
-  __syncwarp();
-}
-// which of N buffers, and the phase of its barriers
-template <int N>
-struct Turn {
-  int at = 0, phase = 0;
-  __device__ __forceinline__ void next(int n = 1) {
-    if ((at += n) >= N) {
-      at -= N;
-      phase ^= 1;
-    }
-  }
-};
-
-template <bool HALF>
-__device__ __forceinline__ float2 unpack16(uint32_t w) { return HALF ? unpack2<__half>(w) : unpack2<__nv_bfloat16>(w); }
-
 // four bits -> byte masks of a word
 __device__ __forceinline__ uint32_t byte_mask(uint32_t bits) { return ((bits & 15u) * 0x00204081u & 0x01010101u) * 0xFFu; }
 // eight bits in the order V scales are kept in: 0 4 1 5 2 6 3 7
@@ -222,35 +171,6 @@ __device__ __forceinline__ uint32_t permute_eight(uint32_t v) {
   hi = (hi | hi << 2) & 0x33u; hi = (hi | hi << 1) & 0x55u;
   return lo | hi << 1;
 }
-__device__ __forceinline__ uint32_t splat_half(uint32_t h2, int hi) { return __byte_perm(h2, 0, hi ? 0x3232 : 0x1010); }
-__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
-  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-// x = a * b + c, l += a: two at a time
-__device__ __forceinline__ void fma_pair(float& x0, float& x1, uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, uint32_t c0, uint32_t c1) {
-  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
-      "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
-      : "=f"(x0), "=f"(x1) : "r"(a0), "r"(a1), "r"(b0), "r"(b1), "r"(c0), "r"(c1));
-}
-__device__ __forceinline__ void add_pair(float& l0, float& l1, float a0, float a1) {
-  asm("{\n\t.reg .b64 a, l;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 l, {%0, %1};\n\tadd.rn.f32x2 l, l, a;\n\tmov.b64 {%0, %1}, l;\n\t}"
-      : "+f"(l0), "+f"(l1) : "f"(a0), "f"(a1));
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ float exp2_approx(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-// Biased exponent of the factor of a row of Q whose largest magnitude is a: 2^(14 - exponent of a), at most 2^100 (rows below 2^-86 lose
-// bits of scores that are nothing beside any others)
-__device__ __forceinline__ uint32_t row_exponent(float a) { return a == 0.f ? 127u : min(268u - (__float_as_uint(a) >> 23), 227u); }
-
 // sum over the warp of each of N values: lane i ends with the total of value i % N
 template <int N>
 __device__ __forceinline__ float warp_sums(float (&v)[N], int lane) {
@@ -283,12 +203,6 @@ __device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long lon
   return left >= 8 ? v : left > 0 ? v & ((1u << left) - 1) : 0u;
 }
 
-// floor(a * b / c), floor((a + 1) * b / c), ... of tile numbers: in 32 bits where they are enough (64-bit divisions took 0.5 us of the
-// smallest calls)
-__device__ __forceinline__ constexpr long long div_short(long long a, long long c) {
-  return (a | c) < (1ll << 31) ? (long long)((uint32_t)a / (uint32_t)c) : a / c;
-}
-__device__ __forceinline__ constexpr long long mul_div(long long a, long long b, long long c) { return div_short(a * b, c); }
 // This CTA's run of tiles: how many, and where it starts.  find: entry and place of the first tile, its number in the list, all tiles,
 // CTAs.  A barrier of the block (two for a batch of more than 32): everything that the block wrote to shared memory before is visible after it.
 template <int THREADS>
@@ -370,14 +284,6 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
   w0.left -= kt;
   return (int)min(t1 - t0, (long long)INT_MAX);
 }
-
-// the CTA that has a tile of the list, of `total` tiles in equal runs for `ctas`
-__device__ __forceinline__ constexpr int cta_of(long long tile, long long total, long long ctas) { return (int)div_short((tile + 1) * ctas - 1, total); }
-static_assert(cta_of(0, 5, 2) == 0 && cta_of(1, 5, 2) == 0 && cta_of(2, 5, 2) == 1 && cta_of(4, 5, 2) == 1, "runs 0-1, 2-4");
-static_assert(mul_div(1, 5, 2) == 2 && mul_div(2, 5, 2) == 5, "where they begin");
-static_assert(cta_of(7, (1ll << 32) + 1, 592) == 0 && cta_of((1ll << 32), (1ll << 32) + 1, 592) == 591 && mul_div(591, 1ll << 33, 592) < 1ll << 33 &&
-              cta_of(mul_div(591, 1ll << 33, 592), 1ll << 33, 592) == 591 && cta_of(mul_div(591, 1ll << 33, 592) - 1, 1ll << 33, 592) == 590,
-              "more tiles than 32 bits hold");
 
 // Brings the pages of tiles into a ring of stages, one bulk copy each; a whole warp.  RING: stages for which `valid` remembers which of the
 // pages exist.  PARTS = 2: K and V by themselves, each in a stage of its own.
