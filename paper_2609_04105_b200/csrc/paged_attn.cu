@@ -3,8 +3,26 @@
 // Row (b, h, t) at position p sees keys [first, last), clipped to the keys that are there.  With s the scaled product of q and a key,
 //     x = cap tanh(s / cap) (if capped) - slope_h |p - j|,   O = sum_j e^(x_j - m) v_j / sum_j e^(x_j - m),   LSE = m + ln sum_j e^(x_j - m).
 //
-// The simplest form: a warp per row, a key after another, everything in fp32.
-#include "kv_cache.cuh"
+// Rows are in lanes: S = Q K^T (128 rows x 128 keys), O += P V (128 rows x d), both on the fifth-generation tensor core with fp32 sums in tensor
+// memory.  The rows that read one KV head (tokens x heads of its group, tokens first) are an item's, 256 at a time or, where there are no more,
+// 128.  A row's maximum and sum then belong to one thread, and a key is converted once for all rows of the item:
+//
+//   producer   pages of a tile of 128 keys -> a ring of stages, K and V by themselves: one bulk copy a page
+//   K          codes -> f16 (exact) -> shared memory, a key a row; Q of an item, a power of two per row, -> f16 -> shared memory
+//   V          codes -> f16 (exact) -> shared memory, V^T: an index of the head dimension a row
+//   issuer     S of the next tile, O of this one, of two softmax groups in turn
+//   softmax    two groups of 128 threads, a thread a row: scores -> P, f16, over its own scores in tensor memory, where the product reads it
+//
+// Two groups because a tile is one long chain (scores - maximum - exp2 - P - product): while one waits for its products the other has the
+// exponential unit.  Items of more than 128 rows give each group half of the rows; those of fewer give the groups tiles in turn, with references,
+// sums and an O each, joined at the item's end.
+//
+// All tiles of all items stand in one list of which every CTA takes an equal run; what an item leaves in several CTAs (maximum, sum, O) is joined by a
+// second kernel in the order of its keys, so results repeat bit by bit.  With shared prefixes an item is a prefix's rows of all members of its group, or
+// a sequence's rows over its own tokens; every row is joined from both.
+//
+// References, f16 probabilities and the scale of Q are those of attention over drafted trees (tree_attn.cu).
+#include "cache_attn.cuh"
 
 #include <limits.h>
 #include <math.h>
@@ -13,118 +31,1108 @@
 
 namespace fp4attn {
 
-int check_cache(const fp4attn_cache* c, int B, const int* block_table, int max_pages, const int* start, const int* count, CacheRef* ref);
-
 namespace {
+
+constexpr int kMostCtas = 160;             // one an SM; each may leave two partial results
+
+// how a product becomes a score: scaled; scaled and capped; with a bias, and perhaps capped
+enum { kScaled, kCapped, kBiased };
 
 struct PagedParams {
   const void* q;
   long long q_sb, q_sh, q_sn;
   CacheRef cache;
   const int *context, *count, *first, *last;
+  const int2* ranges;                      // [B * row_tiles]: of the keys that a tile of rows sees, with first or last
   // shared prefixes: of each group, and where its entries begin
   const int *prefix_table, *prefix_length, *group_start;
   int groups, prefix_pages;
-  const unsigned long long* mask;
+  const unsigned long long* mask;          // [B, T] or null
   const float* slopes;
   void* out;
   float* lse;
   int* status;
-  int B, H, T, group;
+  float* part;                             // [2 * kMostCtas][rows of an item][D]
+  float2* part_ml;                         // [2 * kMostCtas][rows of an item]: reference, sum
+  int4* begun;                             // [kMostCtas]: the item that began in a CTA and went on in others: its x, its u, the last CTA; w: is there one
+  int2* split;                             // shared: of every item its first and last CTA; first = -1: whole
+  float* whole;                            // shared: [2][B, H, T][D] of whole items
+  float2* whole_ml;                        // [2][B, H, T]
+  int B, H, T, group, row_tiles;           // row_tiles: of a sequence's rows
   float scale, cap;
-  bool half;
+  bool half, q_vector;
 };
 
-template <int FMT, int D>
-__global__ void __launch_bounds__(128) row_kernel(const PagedParams p) {
+template <int FMT, int D, int RT>
+struct PagedCfg {
   using L = RecordLayout<FMT, D>;
-  constexpr int E = D / 32;
-  wait_prior_grids();
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31, P = 1 << p.cache.log_page;
-  if (row >= (long long)p.B * p.H * p.T) return;
-  const int t = (int)(row % p.T), h = (int)(row / p.T % p.H), b = (int)(row / ((long long)p.T * p.H)), kvh = h / p.group;
-  const int n = p.count ? max(0, min(load(p.count + b), p.T)) : p.T;
-  if (t >= n) return;
-  const int ctx = max(0, load(p.context + b));
-  float q[E];
-  for (int x = 0; x < E; ++x) {
-    const uint16_t w = load(static_cast<const uint16_t*>(p.q) + b * p.q_sb + h * p.q_sh + t * p.q_sn + lane * E + x);
-    q[x] = p.half ? __half2float(__ushort_as_half(w)) : __bfloat162float(__ushort_as_bfloat16(w));
-  }
-  const float c = __fdiv_rn(p.scale, load(p.cache.k_G + kvh)), slope = p.slopes ? load(p.slopes + h) : 0.f;
-  float m = -INFINITY, l = 0.f, o[E] = {};
-  bool lost = false;
-  auto run = [&](const int* table, int max_pages, long long lo, long long hi, long long reported, long long at, const unsigned long long* mask, int ctx) {
-    const long long room = (long long)max_pages << p.cache.log_page;
-    lost |= reported > room;                                        // the table has no room for the last tokens
-    for (long long j = lo; j < min(hi, room); ++j) {
-      if (mask && j >= ctx && !(*mask >> (j - ctx) & 1)) continue;
-      const long long i = j >> p.cache.log_page;
-      const int page = i < max_pages ? load(table + i) : -1;
-      if (page < 0 || page >= p.cache.num_pages) {
-        lost |= j < reported;
-        continue;
-      }
-      const uint8_t* const rec = p.cache.rec(page, kvh);
-      const int tok = (int)(j & (P - 1)), e = lane * E;
-      float k[E], v[E];
-      for (int x = 0; x < E; ++x) {
-        const int f = e + x;
-        if (L::kFp4) {
-          const uint32_t kb = load(rec + (f / 32 * P + tok) * 16 + f % 32 / 2) >> 4 * (f & 1) & 15u;
-          const uint32_t vb = load(rec + L::v_codes(P) + (tok / 16 * (D / 2) + f / 2) * 16 + tok % 16) >> 4 * (f & 1) & 15u;
-          k[x] = half2_of(cvt_f16x2_e2m1x2<0>(kb)).x * e4m3_value(load(rec + L::k_scales(P) + tok * L::kScales + f / 16));
-          v[x] = half2_of(cvt_f16x2_e2m1x2<0>(vb)).x * e4m3_value(load(rec + L::v_scales(P) + f / 16 * P + v_scale_place(tok)));
-        } else {
-          k[x] = e4m3_value(load(rec + (f / 16 * P + tok) * 16 + f % 16));
-          v[x] = e4m3_value(load(rec + L::v_codes(P) + (tok / 16 * D + f) * 16 + tok % 16));
-        }
-      }
-      float s = 0.f;
-      for (int x = 0; x < E; ++x) s = fmaf(q[x], k[x], s);
-      for (int y = 16; y; y >>= 1) s += __shfl_xor_sync(0xffffffffu, s, y);
-      s *= c;
-      if (p.cap > 0.f) s = p.cap * tanhf(s / p.cap);
-      s -= slope * fabsf((float)(at - j));
-      const float top = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - top), w = top == -INFINITY ? 0.f : expf(s - top);
-      m = top;
-      l = l * f + w;
-      for (int x = 0; x < E; ++x) o[x] = o[x] * f + w * v[x];
+  static constexpr int kRows = 128 * RT;                           // of an item
+  // warps
+  static constexpr int kFirstV = 4, kFirstSoftmax = 8, kProducer = 16, kIssuer = 17, kThreads = 32 * 18;
+  static constexpr int kStage = kTile * L::kToken;                 // K or V of a tile
+  static constexpr int kQ = kRows * D * 2, kOp = kTile * D * 2;    // an operand tile
+  static constexpr int kKB = 2, kVB = RT == 2 && D == 128 && !L::kFp4 ? 1 : 2;
+  static constexpr int kRing = 32, kRingC = 4;                     // tiles whose pages, items whose constants are remembered
+  static constexpr int kFixed = kQ + (kKB + kVB) * kOp + 2048 + 4 * kRows * kRingC + 2048 + 4 * kRing + 256 + 64 + 512 + 1024;
+  static constexpr int kStages = (227 * 1024 - kFixed) / kStage < 8 ? (227 * 1024 - kFixed) / kStage : 8;
+  static_assert(kStages >= 2, "shared memory");
+  static constexpr int kOffQ = 0, kOffK = kOffQ + kQ, kOffV = kOffK + kKB * kOp, kOffStage = kOffV + kVB * kOp;
+  static constexpr int kOffVScale = kOffStage + kStages * kStage;  // f16 [4 V warps][2 blocks][128 tokens]
+  static constexpr int kOffC = kOffVScale + 2048;                  // float [kRingC][kRows]: score constants of the last items
+  static constexpr int kOffML = kOffC + 4 * kRows * kRingC;        // float2 [2][128]
+  static constexpr int kOffValid = kOffML + 2048;                  // u32 [kRing]: pages of a tile that are there
+  static constexpr int kOffScan = kOffValid + 4 * kRing;           // i64 [18]
+  static constexpr int kOffFind = kOffScan + 256;                  // i64 [5]
+  static constexpr int kOffBar = kOffFind + 64;
+  static constexpr int kSmem = kOffBar + 512 + 1024;
+  static_assert(kSmem <= 227 * 1024 && kOffStage % 1024 == 0 && kStage % 16 == 0, "shared memory");
+  enum { K_FULL = 0, K_FREE = K_FULL + kKB, V_FULL = K_FREE + kKB, V_FREE = V_FULL + kVB, Q_FULL = V_FREE + kVB, Q_FREE, S_FULL, P_FULL = S_FULL + 2,
+         PV_DONE = P_FULL + 2, DRAIN = PV_DONE + 2, RING_FULL, RING_FREE = RING_FULL + kStages, kBars = RING_FREE + kStages };
+  static_assert(kBars * 8 + 16 <= 512, "barriers");
+  static constexpr int kS = 0, kO = 256;                           // tensor memory: scores (and P) of the two groups, their O
+};
+
+// tokens that entry b has
+__device__ __forceinline__ int tokens_of(const PagedParams& p, int b) { return p.count ? max(0, min(load(p.count + b), p.T)) : p.T; }
+
+// its context: what lies behind every table's room is all the same
+__device__ __forceinline__ int context_of(const PagedParams& p, int b) { return max(0, min(load(p.context + b), (1 << 30) - 1)); }
+
+// ---- items.  x: a tile of rows of a sequence (paged); a group's prefix, or a sequence by itself (shared).  All items of an x have as many tiles.
+struct Desc {
+  int nt;                                  // tiles of an item; 0: no item
+  int k0;                                  // its first tile of keys
+  int lo, hi, need;                        // keys of the item that may be seen; need: before they are clipped to the table
+  int row0, rows, rts;                     // first row (of x's only tile), rows of x, tiles of rows
+  int b;                                   // entry, or (prefix) the first of the group
+  int g;                                   // group of a prefix, -1
+  int ctx, n;                              // of the entry: context, tokens
+};
+template <int ROWS>
+__device__ __forceinline__ void describe(const PagedParams& p, int x, Desc& d) {
+  d.g = -1;
+  d.row0 = 0;
+  d.k0 = 0;
+  d.lo = 0;
+  long long need;
+  int room = p.cache.max_pages << p.cache.log_page;
+  if (!p.groups) {
+    d.b = x / p.row_tiles;
+    d.row0 = (x - d.b * p.row_tiles) * ROWS;
+    d.n = tokens_of(p, d.b);
+    d.ctx = context_of(p, d.b);
+    d.rows = d.n * p.group;
+    d.rts = 1;
+    d.nt = 0;
+    if (d.row0 >= d.rows) return;
+    if (p.ranges) {
+      const int2 r = load(p.ranges + x);
+      d.lo = r.x;
+      need = r.y;
+    } else {
+      need = (long long)d.ctx + (min(d.row0 + ROWS, d.rows) - 1) / p.group + 1;
     }
-  };
-  if (p.groups) {
-    int before = 0;
-    for (int g = 0; g < p.groups; ++g) {
-      if (b < load(p.group_start + g) || b >= load(p.group_start + g + 1)) continue;
-      before = max(0, load(p.prefix_length + g));
-      run(p.prefix_table + (size_t)g * p.prefix_pages, p.prefix_pages, 0, before, before, (long long)before + ctx + t, nullptr, 0);
-    }
-    const unsigned long long mask = p.mask ? load(p.mask + (size_t)b * p.T + t) : (2ull << t) - 1;
-    run(p.cache.table + (size_t)b * p.cache.max_pages, p.cache.max_pages, 0, (long long)ctx + n, (long long)ctx + n, (long long)ctx + t, &mask, ctx);
+  } else if (x < p.groups) {
+    const int b0 = max(0, min(load(p.group_start + x), p.B)), b1 = max(b0, min(load(p.group_start + x + 1), p.B));
+    d.g = x;
+    d.b = b0;
+    d.ctx = 0;
+    d.n = p.T;
+    d.rows = (b1 - b0) * p.T * p.group;
+    d.rts = (d.rows + ROWS - 1) / ROWS;
+    room = p.prefix_pages << p.cache.log_page;
+    need = max(0, load(p.prefix_length + x));
+    d.nt = 0;
+    if (!d.rows || !need) return;
   } else {
-    const long long there = (long long)ctx + n;
-    const long long lo = p.first ? max(0, load(p.first + (size_t)b * p.T + t)) : 0;
-    const long long hi = min(there, p.last ? (long long)load(p.last + (size_t)b * p.T + t) : (long long)ctx + t + 1);
-    run(p.cache.table + (size_t)b * p.cache.max_pages, p.cache.max_pages, lo, hi, hi, (long long)ctx + t, nullptr, 0);
+    d.b = x - p.groups;
+    d.n = tokens_of(p, d.b);
+    d.ctx = context_of(p, d.b);
+    d.rows = d.n * p.group;
+    d.rts = (d.rows + ROWS - 1) / ROWS;
+    d.nt = 0;
+    if (!d.rows) return;
+    need = (long long)d.ctx + d.n;
+    room = (int)min((long long)room, (long long)d.ctx + (p.mask ? p.T : d.n));       // (a mask may look behind the count)
   }
-  const float f = l == 0.f ? 0.f : __fdiv_rn(1.f, l * load(p.cache.v_G + kvh));
-  for (int x = 0; x < E; ++x) {
-    const float y = l == 0.f ? 0.f : o[x] * f;
-    static_cast<uint16_t*>(p.out)[row * D + lane * E + x] = p.half ? __half_as_ushort(__float2half_rn(y)) : __bfloat16_as_ushort(__float2bfloat16_rn(y));
+  d.need = (int)min(need, (long long)INT_MAX);
+  d.hi = p.groups && d.g < 0 ? room : min(d.need, room);
+  if (d.lo >= d.hi) {                      // rows that see nothing: one tile, all of it hidden
+    d.lo = d.hi = 0;
+    d.nt = 1;
+  } else {
+    d.k0 = d.lo / kTile;
+    d.nt = (d.hi + kTile - 1) / kTile - d.k0;
   }
-  if (lane == 0 && p.lse) p.lse[row] = l == 0.f ? -INFINITY : m + logf(l);
-  if (lost && lane == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
+}
+// of an item among the entries of p.split.  (Prefixes: those of a group begin behind as many whole tiles as the groups before it can fill.)
+template <int ROWS>
+__device__ __forceinline__ size_t split_place(const PagedParams& p, const Desc& d, int u) {
+  const int kvh = u / d.rts, rt = u - kvh * d.rts;
+  const long long rows = (long long)p.T * p.group;
+  const long long at = d.g >= 0 ? d.b * rows / ROWS + d.g + rt : p.B * rows / ROWS + p.groups + 1 + (long long)d.b * p.row_tiles + rt;
+  return (size_t)at * p.cache.kv_heads + kvh;
+}
+template <int ROWS>
+struct Walk {
+  Desc d;
+  int x, u;                                // item: u = KV head x row tiles + row tile
+  int tile;                                // of the item
+  int left;                                // of this CTA's run, this one included
+  bool fresh;                              // the item's first tile here
+  int row0;
+  __device__ __forceinline__ int kvh() const { return u / d.rts; }
+  __device__ __forceinline__ int first_key() const { return (d.k0 + tile) * kTile; }
+  __device__ __forceinline__ bool two() const { return ROWS > 128 && d.rows - row0 > 128; }
+  __device__ __forceinline__ bool ends() const { return tile + 1 == d.nt || left == 1; }        // the item here
+  __device__ __forceinline__ void set_rows() { row0 = d.row0 + u % d.rts * ROWS; }
+  __device__ __forceinline__ void next(const PagedParams& p) {
+    fresh = false;
+    --left;
+    if (!rare(++tile == d.nt) || left <= 0) return;
+    tile = 0;
+    fresh = true;
+    if (++u == d.rts * p.cache.kv_heads) {
+      u = 0;
+      do describe<ROWS>(p, ++x, d);
+      while (d.nt == 0);                   // (there is another item: the run goes on)
+    }
+    set_rows();
+  }
+};
+
+// This CTA's run of tiles.  find: its first tile's number, all tiles, CTAs.  Barriers of the block.
+template <int ROWS, int THREADS>
+__device__ __forceinline__ void find_run(const PagedParams& p, Walk<ROWS>& w, long long* scan, long long* find) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int X = p.groups ? p.groups + p.B : p.B * p.row_tiles;
+  const int per = (X + THREADS - 1) / THREADS, x0 = min(X, (int)threadIdx.x * per), x1 = min(X, x0 + per);
+  Desc d;
+  auto tiles = [&](int x) {
+    describe<ROWS>(p, x, d);
+    return d.nt ? (long long)d.nt * d.rts * p.cache.kv_heads : 0ll;
+  };
+  long long mine = 0;
+#pragma unroll 1
+  for (int x = x0; x < x1; ++x) mine += tiles(x);
+  long long incl = mine;
+#pragma unroll 1
+  for (int s = 1; s < 32; s <<= 1) {
+    const long long o = __shfl_up_sync(0xffffffffu, incl, s);
+    if (lane >= s) incl += o;
+  }
+  if (lane == 31) scan[warp] = incl;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll 1
+  for (int i = 0; i < THREADS / 32; ++i) {
+    if (i < warp) before += scan[i];
+    total += scan[i];
+  }
+  before += incl - mine;
+  const long long ctas = min((long long)gridDim.x, total);
+  const long long t0 = blockIdx.x < ctas ? mul_div(blockIdx.x, total, ctas) : total, t1 = blockIdx.x < ctas ? mul_div(blockIdx.x + 1, total, ctas) : total;
+  if (threadIdx.x == 0) {
+    find[2] = t0;
+    find[3] = total;
+    find[4] = ctas;
+  }
+  if (t0 < t1 && before <= t0 && t0 < before + mine) {              // one thread
+    int x = x0;
+    for (;; ++x) {
+      const long long here = tiles(x);
+      if (t0 < before + here) break;
+      before += here;
+    }
+    find[0] = x;
+    find[1] = t0 - before;
+  }
+  __syncthreads();
+  w.left = (int)min(t1 - t0, (long long)INT_MAX);
+  w.fresh = true;
+  w.x = w.u = w.tile = w.row0 = 0;
+  if (w.left <= 0) return;
+  w.x = (int)find[0];
+  describe<ROWS>(p, w.x, w.d);
+  w.u = (int)mul_div(find[1], 1, w.d.nt);
+  w.tile = (int)(find[1] - (long long)w.u * w.d.nt);
+  w.set_rows();
 }
 
-int launch(const PagedParams& p, int fmt, int d, cudaStream_t st) {
-  const dim3 grid((unsigned)(((long long)p.B * p.H * p.T + 3) / 4));
-  auto go = [&](auto* kernel) {
-    const cudaError_t e = launch_overlapped(kernel, grid, 128u, 0, st, p);
-    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
+// entry and token of row r of an item
+__device__ __forceinline__ void row_token(const PagedParams& p, const Desc& d, int r, int* b, int* t, int* h) {
+  const int v = r / p.group;
+  *h = r - v * p.group;
+  *b = d.b;
+  *t = v;
+  if (d.g >= 0) {
+    *b = d.b + v / p.T;
+    *t = v % p.T;
+  }
+}
+
+// bits [a, b) of a word, whatever a and b are
+__device__ __forceinline__ uint32_t bits_between(int a, int b) {
+  const uint32_t from = a <= 0 ? 0xFFFFFFFFu : a >= 32 ? 0u : 0xFFFFFFFFu << a, until = b >= 32 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << b) - 1;
+  return from & until;
+}
+// of 32 keys from place `c` x 32 of a tile on, those whose pages are there
+__device__ __forceinline__ uint32_t held_bits(uint32_t held, int c, int log_page) {
+  if (log_page >= 5) return held >> (32 * c >> log_page) & 1 ? 0xFFFFFFFFu : 0u;
+  return (held >> (2 * c) & 1 ? 0xFFFFu : 0u) | (held >> (2 * c + 1) & 1 ? 0xFFFF0000u : 0u);
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// f16 pairs: NaN and infinities of bytes that nobody wrote become numbers, everything that a cache holds stays (E4M3 ends at 448): a probability
+// of 0 times any of them is 0
+__device__ __forceinline__ uint32_t finite(uint32_t h2) {
+  const __half2 most = __float2half2_rn(448.f), r = __hmin2(*reinterpret_cast<const __half2*>(&h2), most);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// a score in octaves (of e^s), capped: cap tanh(s / cap) = cap - 2 cap / (1 + e^(2 s / cap)); in = 2 / cap, out = cap log2 e.  Off by no more than
+// 2^-21 of the cap: the exponential and the reciprocal by 2^-22 of themselves.  (The tanh of the special-function unit is off by 2^-11.)
+__device__ __forceinline__ float cap_score(float y, float in, float out) { return fmaf(-2.f * out, rcp_approx(1.f + exp2_approx(y * in)), out); }
+// place of 16-byte chunk c of a row of 128 bytes in a swizzled operand
+__device__ __forceinline__ uint32_t chunk_at(int row, int c) { return (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4)); }
+
+template <int FMT, int D, int RT, int SCORES>
+__global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kernel(const PagedParams p) {
+  using C = PagedCfg<FMT, D, RT>;
+  using L = typename C::L;
+  constexpr int ROWS = C::kRows;
+  constexpr bool CAP = SCORES == kCapped, ANY = SCORES == kBiased;     // ANY: a bias, and perhaps a cap
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* const sgen = smem_raw + (sbase - smem_u32(smem_raw));
+  const uint32_t abort_at = sbase + C::kOffBar + 8 * C::kBars, tslot = abort_at + 4;
+  volatile uint32_t* const abort_word = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars);
+  auto bar = [&](int i) { return sbase + C::kOffBar + 8u * i; };
+  auto wait = [&](int b, int phase) { wait_phase<true>(bar(b), (uint32_t)phase, abort_at); };
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kBars; ++i) {
+      const bool four = (i < C::K_FREE) || (i >= C::V_FULL && i < C::V_FREE) || i == C::Q_FULL || (i >= C::P_FULL && i < C::PV_DONE) || i >= C::RING_FREE;
+      mbar_init(bar(i), four ? 4 : 1);
+    }
+    *abort_word = 0;
+    fence_barrier_init();
+  }
+  if (warp == C::kIssuer) { tmem_alloc(tslot, 512); tmem_relinquish(); }
+  tc_fence_before();
+  launch_dependents();                                              // the joining kernel: its launch lies under this one
+  wait_prior_grids();
+  Walk<ROWS> w;
+  long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
+  if (threadIdx.x == 0 && p.begun) p.begun[blockIdx.x].w = 0;
+  find_run<ROWS, C::kThreads>(p, w, reinterpret_cast<long long*>(sgen + C::kOffScan), find);
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
+  uint32_t* const valid_ring = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
+  const int log_page = p.cache.log_page, P = 1 << log_page, half_record = p.cache.record / 2;
+  const uint32_t all_pages = (1u << (kTile >> log_page)) - 1;
+
+  if (warp == C::kProducer) {
+    // ===================================================================== pages -> shared memory
+    Turn<C::kStages> ring;
+    bool lost = false;
+    int parts = 0;
+#pragma unroll 1
+    for (int i = 0; w.left > 0; ++i) {
+      const int first = w.first_key(), pos = first + lane * P;
+      int page = -1;
+      if (lane < kTile >> log_page && pos < w.d.hi && pos + P > w.d.lo) {
+        if (w.d.g >= 0) {
+          const int id = load(p.prefix_table + (size_t)w.d.g * p.prefix_pages + (pos >> log_page));
+          page = id >= 0 && id < p.cache.num_pages ? id : -1;
+        } else {
+          page = p.cache.page_of(w.d.b, pos);
+        }
+        lost |= page < 0 && pos < w.d.need;
+      }
+      lost |= w.d.need > w.d.hi && w.d.nt - w.tile == 1 && (w.d.g >= 0 ? w.d.need > p.prefix_pages << log_page : w.d.need > p.cache.max_pages << log_page);
+      const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
+      const uint8_t* const rec = page >= 0 ? p.cache.rec(page, w.kvh()) : nullptr;
+#pragma unroll 1
+      for (int part = 0; part < 2; ++part) {
+        wait(C::RING_FREE + ring.at, ring.phase ^ 1);
+        if (lane == 0) {
+          if (part == 0) valid_ring[i % C::kRing] = held;
+          mbar_arrive_expect_tx(bar(C::RING_FULL + ring.at), __popc(held) * half_record);
+        }
+        __syncwarp();
+        if (page >= 0)
+          bulk_load_1d(sbase + C::kOffStage + ring.at * C::kStage + lane * half_record, rec + part * half_record, half_record, bar(C::RING_FULL + ring.at));
+        ring.next();
+        ++parts;
+      }
+      w.next(p);
+    }
+    if (__any_sync(0xffffffffu, lost) && lane == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
+    // the last copies end before this warp does (also where the others have given up on them)
+    for (int k = 0; k < C::kStages && k < parts; ++k) {
+      ring.at = ring.at ? ring.at - 1 : (ring.phase ^= 1, C::kStages - 1);
+      wait(C::RING_FULL + ring.at, ring.phase);
+    }
+  } else if (warp == C::kIssuer) {
+    // ===================================================================== products
+    // Jobs: a tile of 128 rows and a tile of keys.  Job j is of softmax group j & 1.  S of a group's next job is issued right behind its O: P stands
+    // where S did, and products run in the order of their issue.
+    constexpr uint32_t kIdescS = make_idesc_f16(128, kTile, false), kIdescO = make_idesc_f16(128, D, false);
+    Walk<ROWS> ws = w, wo = w;
+    Turn<C::kKB> kb;
+    Turn<C::kVB> vb;
+    int rs = 0, ro = 0, gs = 0, go = 0, q_phase = 0, jobs_in_item = 0;
+    int p_phase[2] = {0, 0};
+    auto issue_scores = [&] {
+      if (rare(ws.left <= 0)) return;
+      const bool two = ws.two();
+      if (rs == 0) {
+        if (rare(ws.fresh)) {
+          wait(C::Q_FULL, q_phase);
+          q_phase ^= 1;
+        }
+        wait(C::K_FULL + kb.at, kb.phase);
+      }
+      tc_fence_after();
+      const bool last = !two || rs == 1;
+      if (elect_one()) {
+        const uint32_t a = sbase + C::kOffQ + rs * (128 * D * 2), b = sbase + C::kOffK + kb.at * C::kOp;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t at = (k >> 2) * 16384 + (k & 3) * 32;
+          tc_mma_f16(tmem + C::kS + 128 * gs, make_smem_desc(a + at, 16, 1024, kSwz128), make_smem_desc(b + at, 16, 1024, kSwz128), kIdescS, k > 0);
+        }
+        tc_commit(bar(C::S_FULL + gs));
+        if (last) tc_commit(bar(C::K_FREE + kb.at));
+        if (last && ws.ends()) tc_commit(bar(C::Q_FREE));
+      }
+      __syncwarp();
+      gs ^= 1;
+      rs ^= 1;
+      if (last) {
+        rs = 0;
+        kb.next();
+        ws.next(p);
+      }
+    };
+    issue_scores();
+    issue_scores();
+#pragma unroll 1
+    while (wo.left > 0) {
+      const bool two = wo.two(), last = !two || ro == 1;
+      if (ro == 0) {
+        if (wo.fresh) jobs_in_item = 0;
+        wait(C::V_FULL + vb.at, vb.phase);
+      }
+      wait(C::P_FULL + go, p_phase[go]);
+      p_phase[go] ^= 1;
+      tc_fence_after();
+      const uint32_t more = jobs_in_item >= 2;                        // not the item's first of this group
+      if (elect_one()) {
+        const uint32_t b = sbase + C::kOffV + vb.at * C::kOp;
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          tc_mma_f16_ta(tmem + C::kO + D * go, tmem + C::kS + 128 * go + 8 * k, make_smem_desc(b + (k >> 2) * (D * 128) + (k & 3) * 32, 16, 1024, kSwz128), kIdescO,
+                        k > 0 ? 1u : more);
+        tc_commit(bar(C::PV_DONE + go));
+        if (last) tc_commit(bar(C::V_FREE + vb.at));
+      }
+      __syncwarp();
+      ++jobs_in_item;
+      go ^= 1;
+      ro ^= 1;
+      if (last) {
+        ro = 0;
+        vb.next();
+        wo.next(p);
+      }
+      issue_scores();
+    }
+    if (elect_one()) tc_commit(bar(C::DRAIN));
+    __syncwarp();
+  } else if (warp < C::kFirstV) {
+    // ===================================================================== K and Q
+    const int key = threadIdx.x, slot = key >> log_page, t = key & (P - 1);
+    const float c0 = p.scale * 1.4426950408889634f;
+    Turn<C::kStages> ring;
+    Turn<C::kKB> kb;
+    int item = 0, q_phase = 1;
+#pragma unroll 1
+    while (w.left > 0) {
+      wait(C::K_FREE + kb.at, kb.phase ^ 1);
+      wait(C::RING_FULL + ring.at, ring.phase);
+      {
+        const uint8_t* const rec = sgen + C::kOffStage + ring.at * C::kStage + slot * half_record;
+        const uint8_t* codes = rec + t * 16;
+        uint8_t* const dst = sgen + C::kOffK + kb.at * C::kOp;
+        uint2 sw = make_uint2(0u, 0u);
+        if (L::kFp4 && D == 128) sw = *reinterpret_cast<const uint2*>(rec + P * L::kRow + t * L::kScales);
+        if (L::kFp4 && D == 64) sw.x = *reinterpret_cast<const uint32_t*>(rec + P * L::kRow + t * L::kScales);
+#pragma unroll 2
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t h[16];
+          if (L::kFp4) {
+            const uint4 raw = *reinterpret_cast<const uint4*>(codes);
+            codes += P * 16;
+            const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w}, both = cvt_f16x2_e4m3x2(sw.x & 0xFFFFu);
+            sw.x = __funnelshift_r(sw.x, sw.y, 16);
+            sw.y >>= 16;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t f = splat_half(both, x >> 1);
+              cvt_f16x2_e2m1x8(words[x], h + 4 * x);
+#pragma unroll
+              for (int y = 0; y < 4; ++y) h[4 * x + y] = mul_half2(h[4 * x + y], f);
+            }
+          } else {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const uint4 raw = *reinterpret_cast<const uint4*>(codes);
+              codes += P * 16;
+              const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+              for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(words[x], h + 8 * y + 2 * x);
+            }
+          }
+          uint8_t* const panel = dst + (c >> 1) * 16384;
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            *reinterpret_cast<uint4*>(panel + chunk_at(key, 4 * (c & 1) + x)) = make_uint4(h[4 * x], h[4 * x + 1], h[4 * x + 2], h[4 * x + 3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::K_FULL + kb.at));
+      ring.next(2);
+      kb.next();
+      if (rare(w.fresh)) {
+        // Rows scaled by a power of two into f16's range (the largest element to [2^14, 2^15)): exact for 8-bit significands, and a row's scores are
+        // scaled back by its constant.  Rows up to the next 32 are written: a warp of softmax threads takes all of its 32 or none.
+        wait(C::Q_FREE, q_phase);
+        q_phase ^= 1;
+        const int kvh = w.kvh(), here = min(ROWS, w.d.rows - w.row0);
+        const float c = __fdiv_rn(c0, load(p.cache.k_G + kvh));
+        constexpr int kParts = D / 16;                              // threads of a row
+        float* const con = reinterpret_cast<float*>(sgen + C::kOffC) + (item & (C::kRingC - 1)) * ROWS;
+#pragma unroll 2
+        for (int j = key; j < ((here + 31) & ~31) * kParts; j += 128) {
+          const int r = j / kParts, e = (j % kParts) * 16;
+          float v[16];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) v[x] = 0.f;
+          if (r < here) {
+            int b, tok, hl;
+            row_token(p, w.d, w.row0 + r, &b, &tok, &hl);
+            const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
+            uint32_t raw[8];
+            if (p.q_vector) {
+              *reinterpret_cast<uint4*>(raw) = load(reinterpret_cast<const uint4*>(q));
+              *reinterpret_cast<uint4*>(raw + 4) = load(reinterpret_cast<const uint4*>(q) + 1);
+            } else {
+#pragma unroll
+              for (int x = 0; x < 8; ++x) raw[x] = (uint32_t)load(q + 2 * x) | (uint32_t)load(q + 2 * x + 1) << 16;
+            }
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              const float2 f = p.half ? unpack16<true>(raw[x]) : unpack16<false>(raw[x]);
+              v[2 * x] = f.x;
+              v[2 * x + 1] = f.y;
+            }
+          }
+          float a = 0.f;
+#pragma unroll
+          for (int x = 0; x < 16; ++x) a = fmaxf(a, fabsf(v[x]));
+#pragma unroll
+          for (int x = 1; x < kParts; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
+          const uint32_t up = row_exponent(a);
+          const float f = __uint_as_float(up << 23);
+          uint32_t h[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(v[2 * x] * f, v[2 * x + 1] * f);
+          uint8_t* const panel = sgen + C::kOffQ + (r >> 7) * (128 * D * 2) + (e >> 6) * 16384;
+          *reinterpret_cast<uint4*>(panel + chunk_at(r & 127, (e & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(panel + chunk_at(r & 127, ((e & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
+          if (e == 0) con[r] = c * __uint_as_float((254u - up) << 23);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::Q_FULL));
+        ++item;
+      }
+      w.next(p);
+    }
+  } else if (warp < C::kFirstSoftmax) {
+    // ===================================================================== V
+    // D = 128: a thread an index; D = 64: two threads, half of the tokens each
+    const int tid = threadIdx.x - 32 * C::kFirstV, e = D == 128 ? tid : tid & 63, tok0 = D == 128 ? 0 : tid & 64;
+    constexpr int kTokens = D == 128 ? 128 : 64;                      // of a thread
+    uint8_t* const scales = sgen + C::kOffVScale + (warp - C::kFirstV) * 512;
+    const uint32_t shift = 4 * (e & 1);
+    // eight tokens whose scales of a block of this warp's indices a lane converts
+    const int sc_tok = tok0 + 8 * (lane & (kTokens / 8 - 1)), sc_block = (e & ~31) / 16 + lane / (kTokens / 8);
+    const uint32_t scale0 = (uint32_t)((sc_tok >> log_page) * half_record + P * L::kRow + sc_block * P + (sc_tok & (P - 1)));
+    Turn<C::kStages> ring;
+    Turn<C::kVB> vb;
+    ring.next();
+#pragma unroll 1
+    for (int i = 0; w.left > 0; ++i) {
+      wait(C::V_FREE + vb.at, vb.phase ^ 1);
+      wait(C::RING_FULL + ring.at, ring.phase);
+      {
+        const int first = w.first_key();
+        // is every byte one that some row sees, hence one that was written?
+        const bool clean = valid_ring[i % C::kRing] == all_pages && !p.ranges && first >= w.d.lo && first + kTile <= (p.groups && w.d.g < 0 ? w.d.ctx : w.d.hi);
+        const uint8_t* const stage = sgen + C::kOffStage + ring.at * C::kStage;
+        uint8_t* const dst = sgen + C::kOffV + vb.at * C::kOp;
+        if (L::kFp4) {
+          if (lane < kTokens / 4) {
+            const uint2 sc = *reinterpret_cast<const uint2*>(stage + scale0);
+            uint32_t f[4];
+            cvt_f16x2_e4m3x4(sc.x, f);
+            cvt_f16x2_e4m3x4(sc.y, f + 2);
+            *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(finite(f[0]), finite(f[1]), finite(f[2]), finite(f[3]));
+          }
+          __syncwarp();
+        }
+        const uint8_t* const factors = scales + ((e >> 4) & 1) * (2 * kTokens);
+#pragma unroll 2
+        for (int j = 0; j < kTokens; j += 16) {                       // sixteen tokens
+          const int tok = tok0 + j;
+          const uint4 raw = *reinterpret_cast<const uint4*>(stage + (tok >> log_page) * half_record + ((tok & (P - 1)) >> 4) * (16 * L::kRow) + (L::kFp4 ? e >> 1 : e) * 16);
+          const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
+          uint32_t h[8];
+          if (L::kFp4) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {                             // eight tokens: i and i + 4 in a byte
+              const uint4 f = *reinterpret_cast<const uint4*>(factors + 2 * j + 16 * x);
+              cvt_f16x2_e2m1x8((cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u), h + 4 * x);
+              h[4 * x] = mul_half2(h[4 * x], f.x);
+              h[4 * x + 1] = mul_half2(h[4 * x + 1], f.y);
+              h[4 * x + 2] = mul_half2(h[4 * x + 2], f.z);
+              h[4 * x + 3] = mul_half2(h[4 * x + 3], f.w);
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(cw[x], h + 2 * x);
+            if (rare(!clean)) {
+#pragma unroll
+              for (int x = 0; x < 8; ++x) h[x] = finite(h[x]);
+            }
+          }
+          uint8_t* const panel = dst + (tok >> 6) * (D * 128);
+          *reinterpret_cast<uint4*>(panel + chunk_at(e, (tok & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(panel + chunk_at(e, ((tok & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::V_FULL + vb.at));
+      ring.next(2);
+      vb.next();
+      w.next(p);
+    }
+  } else {
+    // ===================================================================== softmax
+    const int group = (warp - C::kFirstSoftmax) >> 2, quarter = warp & 3, in_tile = quarter * 32 + lane;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t s_at = tmem + lanes + C::kS + 128 * group, o_at = tmem + lanes + C::kO + D * group;
+    float2* const ml = reinterpret_cast<float2*>(sgen + C::kOffML);
+    int par = 0, s_phase = 0, pv_phase = 1, item = 0, part_first = 0;
+    bool have = false, warp_live = false, live = false;               // a job of the item so far; a row of this warp, of this thread
+    int lo = 0, hi = 0, row = 0, ctx = 0, b = 0, t = 0, hl = 0;
+    long long done = 0;                                               // tiles of this CTA's run
+    float m = -INFINITY, l0 = 0.f, l1 = 0.f, con = 0.f, slope = 0.f;
+    int pos = 0;
+    unsigned long long mask = 0;
+    const float cap_in = p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f;
+#pragma unroll 1
+    while (w.left > 0) {
+      const bool two = w.two();
+      if (rare(w.fresh)) {
+        const int r = (two ? (group ^ par) * 128 : 0) + in_tile;
+        row = w.row0 + r;
+        live = row < w.d.rows;
+        part_first = w.tile;
+        m = -INFINITY;
+        l0 = l1 = 0.f;
+        have = false;
+        lo = hi = 0;
+        mask = 0;
+        ctx = w.d.ctx;
+        if (live) {
+          row_token(p, w.d, row, &b, &t, &hl);
+          if (ANY) {
+            slope = p.slopes ? load(p.slopes + w.kvh() * p.group + hl) * 1.4426950408889634f : 0.f;
+            pos = (int)((unsigned)(w.d.g >= 0 ? w.d.hi + context_of(p, b) : ctx) + (unsigned)t);
+          }
+          if (w.d.g >= 0) {
+            live = t < tokens_of(p, b);
+            hi = w.d.hi;
+          } else if (p.groups) {
+            if (p.mask) {
+              mask = load(p.mask + (size_t)b * p.T + t);
+              if (p.T < 64) mask &= (1ull << p.T) - 1;
+              hi = min(ctx, w.d.hi);
+            } else {
+              hi = min(ctx + t + 1, w.d.hi);
+            }
+          } else {
+            lo = p.first ? max(0, load(p.first + (size_t)b * p.T + t)) : 0;
+            hi = max(0, min(p.last ? load(p.last + (size_t)b * p.T + t) : ctx + t + 1, w.d.hi));
+          }
+        }
+        warp_live = __any_sync(0xffffffffu, live);
+        if (!live) hi = INT_MAX;                                      // (a row of zeros, or one that is not written: never the reason to look at masks)
+      }
+      if (two || par == group) {
+        wait(C::S_FULL + group, s_phase);
+        s_phase ^= 1;
+        tc_fence_after();
+        if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + (two ? (group ^ par) * 128 : 0) + in_tile] : 0.f;
+        if (warp_live) {
+          const int first = w.first_key();
+          const uint32_t held = valid_ring[done % C::kRing];
+          const bool plain = __all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + kTile);
+          float top = -INFINITY, c2 = con;
+          if (SCORES == kScaled && plain) {
+            uint32_t a[32], c[32];
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {
+              tmem_ld_32x32b_x32(s_at + 32 * k, a);
+              tmem_ld_32x32b_x32(s_at + 32 * k + 32, c);
+              tmem_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 32; x += 2) {
+                top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
+                top = max3(top, __uint_as_float(c[x]), __uint_as_float(c[x + 1]));
+              }
+            }
+            top *= con;
+          } else if (CAP && plain) {
+            uint32_t a[32];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              tmem_ld_32x32b_x32(s_at + 32 * k, a);
+              tmem_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 32; x += 2) top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
+            }
+            top = cap_score(top * con, cap_in, cap_out);
+          } else {
+            // the scores are changed, masked and put back
+            c2 = 1.f;
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+              uint32_t a[32];
+              tmem_ld_32x32b_x32(s_at + 32 * k, a);
+              const int at = first + 32 * k;
+              uint32_t seen = bits_between(lo - at, hi - at);
+              const int o = ctx - at;
+              if (p.mask && w.d.g < 0) seen |= o >= 32 || o <= -64 ? 0u : (uint32_t)(o >= 0 ? mask << o : mask >> -o);
+              seen &= held_bits(held, k, log_page);
+              const float far = (float)(pos - at);
+              tmem_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 32; ++x) {
+                float y = __uint_as_float(a[x]) * con;
+                if (CAP || (ANY && p.cap > 0.f)) y = cap_score(y, cap_in, cap_out);
+                if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
+                y = seen >> x & 1 ? y : -INFINITY;
+                top = fmaxf(top, y);
+                a[x] = __float_as_uint(y);
+              }
+              tmem_st_32x32b_x16(s_at + 32 * k, a);
+              tmem_st_32x32b_x16(s_at + 32 * k + 16, a + 16);
+            }
+            tmem_wait_st();
+          }
+          if (rare(__any_sync(0xffffffffu, top > m + kLag || m == -INFINITY))) {
+            // the reference moves: to the largest score seen so far
+            const float old = m;
+            m = fmaxf(m, top);
+            const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
+            l0 *= f;
+            l1 *= f;
+            if (have) {                                               // (S_FULL is behind the group's last product on O)
+#pragma unroll 1
+              for (int k = 0; k < D; k += 16) {
+                uint32_t o[16];
+                tmem_ld_32x32b_x16(o_at + k, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                tmem_st_32x32b_x16(o_at + k, o);
+              }
+              tmem_wait_st();
+            }
+          }
+          const float shift = m == -INFINITY ? 0.f : kShift - m;
+          uint32_t a[16], c[16];
+          auto work = [&](uint32_t* raw, int k) {                     // sixteen keys
+            uint32_t h[8];
+#pragma unroll
+            for (int y = 0; y < 16; y += 8) {
+              float z[8];
+#pragma unroll
+              for (int x = 0; x < 8; x += 2) {
+                if (CAP) {
+                  if (plain) {
+                    raw[y + x] = __float_as_uint(cap_score(__uint_as_float(raw[y + x]) * con, cap_in, cap_out));
+                    raw[y + x + 1] = __float_as_uint(cap_score(__uint_as_float(raw[y + x + 1]) * con, cap_in, cap_out));
+                  }
+                  z[x] = __uint_as_float(raw[y + x]) + shift;
+                  z[x + 1] = __uint_as_float(raw[y + x + 1]) + shift;
+                } else {
+                  const uint32_t cc = __float_as_uint(c2), ss = __float_as_uint(shift);
+                  fma_pair(z[x], z[x + 1], raw[y + x], raw[y + x + 1], cc, cc, ss, ss);
+                }
+                z[x] = exp2_approx(z[x]);
+                z[x + 1] = exp2_approx(z[x + 1]);
+                add_pair(l0, l1, z[x], z[x + 1]);
+              }
+              if (L::kFp4) {                                          // the order that V's tokens stand in: 0 4 1 5 2 6 3 7
+#pragma unroll
+                for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[x], z[x + 4]);
+              } else {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[2 * x], z[2 * x + 1]);
+              }
+            }
+            tmem_st_32x32b_x8(s_at + 8 * k, h);                       // (over scores that have been read)
+          };
+          tmem_ld_32x32b_x16(s_at, a);
+#pragma unroll
+          for (int k = 0; k < 8; k += 2) {
+            tmem_wait_ld();
+            tmem_ld_32x32b_x16(s_at + 16 * k + 16, c);
+            work(a, k);
+            tmem_wait_ld();
+            if (k < 6) tmem_ld_32x32b_x16(s_at + 16 * k + 32, a);
+            work(c, k + 1);
+          }
+          tmem_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::P_FULL + group));
+        have = true;
+        pv_phase ^= 1;
+      }
+      if (!two) par ^= 1;
+      if (rare(w.ends())) {
+        // ---- end of the item, or of this CTA's part of it
+        const bool whole = part_first == 0 && w.tile + 1 == w.d.nt;
+        const int kvh = w.kvh(), slot = 2 * (int)blockIdx.x + (part_first == 0);
+        if (have) wait(C::PV_DONE + group, pv_phase);
+        float f[2] = {1.f, 1.f}, top = m, sum = l0 + l1;
+        if (!two) {                                                   // both groups have had tiles of these rows
+          ml[group * 128 + in_tile] = make_float2(m, sum);
+          bar_sync(1, 256);
+          const float2 other = ml[(group ^ 1) * 128 + in_tile];
+          top = fmaxf(m, other.x);
+          const float mine = !have || m == -INFINITY && sum == 0.f ? 0.f : m == top ? 1.f : exp2_approx(m - top);
+          const float others = other.x == -INFINITY && other.y == 0.f ? 0.f : other.x == top ? 1.f : exp2_approx(other.x - top);
+          f[group] = mine;
+          f[group ^ 1] = others;
+          // (in one order, so that both groups have the same bits)
+          const float s0 = group == 0 ? mine * sum : others * other.y, s1 = group == 0 ? others * other.y : mine * sum;
+          sum = s0 + s1;
+        } else if (m == -INFINITY && sum == 0.f) {
+          f[group] = 0.f;
+        }
+        tc_fence_after();
+        const int r = row - w.row0;
+        const bool mine = live && row < w.d.rows;
+        long long at = 0;                                             // of the row among the outputs
+        if (mine) at = ((long long)b * p.H + kvh * p.group + hl) * p.T + t;
+        const bool out = whole && !p.groups;
+        float* dst = nullptr;
+        if (out) {
+          const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum * load(p.cache.v_G + kvh));          // nothing seen: 0, not 0 / 0
+          f[0] = f[0] == 0.f ? 0.f : f[0] * inv;
+          f[1] = f[1] == 0.f ? 0.f : f[1] * inv;
+          if (mine && p.lse && (two || group == 0)) p.lse[at] = sum == 0.f ? -INFINITY : (top - kShift + log2f(sum)) * 0.6931471805599453f;
+        } else if (mine) {
+          const bool own = w.d.g < 0;
+          dst = whole ? p.whole + (own ? (long long)p.B * p.H * p.T + at : at) * D : p.part + ((size_t)slot * ROWS + r) * D;
+          if (two || group == 0) *(whole ? p.whole_ml + (own ? (long long)p.B * p.H * p.T + at : at) : p.part_ml + (size_t)slot * ROWS + r) = make_float2(top, sum);
+        }
+        __syncwarp();
+        if (warp_live) {
+          const int d0 = two ? 0 : group * (D / 2), d1 = two ? D : d0 + D / 2;
+#pragma unroll 1
+          for (int e = d0; e < d1; e += 16) {
+            uint32_t v[16];
+            float o[16];
+            if (two) {
+              tmem_ld_32x32b_x16(o_at + e, v);
+              tmem_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 16; ++x) o[x] = f[group] == 0.f ? 0.f : __uint_as_float(v[x]) * f[group];
+            } else {
+              uint32_t v2[16];
+              tmem_ld_32x32b_x16(tmem + lanes + C::kO + e, v);
+              tmem_ld_32x32b_x16(tmem + lanes + C::kO + D + e, v2);
+              tmem_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 16; ++x)
+                o[x] = (f[0] == 0.f ? 0.f : __uint_as_float(v[x]) * f[0]) + (f[1] == 0.f ? 0.f : __uint_as_float(v2[x]) * f[1]);
+            }
+            if (mine && out) {
+              uint32_t h[8];
+#pragma unroll
+              for (int x = 0; x < 8; ++x) h[x] = p.half ? pack_pair<__half>(o[2 * x], o[2 * x + 1]) : pack_pair<__nv_bfloat16>(o[2 * x], o[2 * x + 1]);
+              uint4* const y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at * D + e);
+              y[0] = make_uint4(h[0], h[1], h[2], h[3]);
+              y[1] = make_uint4(h[4], h[5], h[6], h[7]);
+            } else if (mine) {
+#pragma unroll
+              for (int x = 0; x < 16; x += 4) *reinterpret_cast<float4*>(dst + e + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+            }
+            __syncwarp();
+          }
+        }
+        if (group == 0 && in_tile == 0) {
+          const int last_cta = cta_of(find[2] + done + (w.d.nt - 1 - w.tile), find[3], find[4]);
+          if (p.groups && part_first == 0) p.split[split_place<ROWS>(p, w.d, w.u)] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, last_cta);
+          if (!p.groups && part_first == 0 && !whole) p.begun[blockIdx.x] = make_int4(w.x, w.u, last_cta, 1);
+        }
+        tc_fence_before();
+        if (!two) bar_sync(1, 256);                                   // the next item's products may overwrite either O
+        ++item;
+      }
+      ++done;
+      w.next(p);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_word && threadIdx.x == 0 && p.status) *p.status = FP4ATTN_ERR_TIMEOUT;
+  if (warp == C::kIssuer) {
+    if (*abort_word && lane == 0)                                   // given up: the products in flight end before tensor memory does
+      for (int spin = 0; spin < (1 << 14) && !mbar_try_wait(bar(C::DRAIN), 0); ++spin) {}
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ---- joining: a warp a row, in the order of the keys
+template <int D>
+struct Sum {
+  static constexpr int E = D / 32;
+  float m = -INFINITY, l = 0.f, o[E] = {};
+  __device__ __forceinline__ void one(const float* src, float2 ml, int lane) {
+    m = ml.x;
+    l = ml.y;
+    fetch(src, lane, o);
+  }
+  static __device__ __forceinline__ void fetch(const float* src, int lane, float* y) {
+    if constexpr (E == 4) *reinterpret_cast<float4*>(y) = *reinterpret_cast<const float4*>(src + lane * E);
+    else *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(src + lane * E);
+  }
+  // row r of the parts that an item left in CTAs first .. last
+  __device__ __forceinline__ void parts(const PagedParams& p, int rows, int first, int last, int r, int lane) {
+    const int n = last - first + 1;
+    auto at = [&](int i) { return (size_t)(i ? 2 * (first + i) : 2 * first + 1) * rows + r; };
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, p.part_ml[at(i)].x);
+    m = warp_max(m);
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      const int i = i0 + lane;
+      const float2 ml = i < n ? p.part_ml[at(i)] : make_float2(-INFINITY, 0.f);
+      const float mine = m == -INFINITY || i >= n ? 0.f : exp2_approx(ml.x - m);
+      const float weighted = ml.x == -INFINITY ? ml.y : mine * ml.y;
+      constexpr int kAtOnce = 8;                                    // loads on their way together
+      for (int k0 = 0; k0 < min(32, n - i0); k0 += kAtOnce) {
+        float part[kAtOnce][E];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+#pragma unroll
+          for (int x = 0; x < E; ++x) part[k][x] = 0.f;
+          if (i0 + k0 + k < n) fetch(p.part + at(i0 + k0 + k) * D, lane, part[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {                         // (behind the last part: weights and parts of 0)
+          const float f = __shfl_sync(0xffffffffu, mine, k0 + k);
+          l += __shfl_sync(0xffffffffu, weighted, k0 + k);
+#pragma unroll
+          for (int x = 0; x < E; ++x) o[x] = fmaf(f, part[k][x], o[x]);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void add(const Sum& s) {
+    const float top = fmaxf(m, s.m), f = top == -INFINITY || m == top ? 1.f : exp2_approx(m - top), g = top == -INFINITY || s.m == top ? 1.f : exp2_approx(s.m - top);
+    m = top;
+    l = l * f + s.l * g;
+#pragma unroll
+    for (int x = 0; x < E; ++x) o[x] = o[x] * f + s.o[x] * g;
+  }
+  __device__ __forceinline__ void give(const PagedParams& p, size_t at, int kvh, int lane) const {
+    const float f = l == 0.f ? 0.f : __fdiv_rn(1.f, l * load(p.cache.v_G + kvh));
+#pragma unroll
+    for (int x = 0; x < E; x += 2) {
+      const uint32_t two = p.half ? pack_pair<__half>(o[x] * f, o[x + 1] * f) : pack_pair<__nv_bfloat16>(o[x] * f, o[x + 1] * f);
+      *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at * D + lane * E + x) = two;
+    }
+    if (lane == 0 && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (m - kShift + log2f(l)) * 0.6931471805599453f;
+  }
+};
+constexpr int kJoinThreads = 256;
+// the item that began in CTA blockIdx.x, if it went on in others
+template <int D, int ROWS>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p) {
+  wait_prior_grids();
+  const int4 item = p.begun[blockIdx.x];
+  const int first = blockIdx.x, last = item.z, lane = threadIdx.x & 31;
+  if (!item.w || last <= first || last >= (int)gridDim.x) return;   // (or a kernel that gave up)
+  Desc d;
+  describe<ROWS>(p, item.x, d);
+  const int kvh = item.y, here = min(ROWS, d.rows - d.row0);
+  for (int r = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5); r < here; r += gridDim.y * (kJoinThreads / 32)) {
+    int b, t, hl;
+    row_token(p, d, d.row0 + r, &b, &t, &hl);
+    Sum<D> s;
+    s.parts(p, ROWS, first, last, r, lane);
+    s.give(p, ((size_t)b * p.H + (size_t)kvh * p.group + hl) * p.T + t, kvh, lane);
+  }
+}
+// every row of a batch with shared prefixes: its prefix's part and its own
+template <int D, int ROWS>
+__global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const PagedParams p) {
+  wait_prior_grids();
+  const long long at = (long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5), all = (long long)p.B * p.H * p.T;
+  const int lane = threadIdx.x & 31;
+  if (at >= all) return;
+  const int t = (int)(at % p.T), h = (int)(at / p.T % p.H), b = (int)(at / p.T / p.H), kvh = h / p.group, hl = h - kvh * p.group;
+  if (t >= tokens_of(p, b)) return;
+  Sum<D> sum;
+  auto take = [&](int x, int row) {
+    Desc d;
+    describe<ROWS>(p, x, d);
+    if (!d.nt) return;
+    const int2 ctas = p.split[split_place<ROWS>(p, d, kvh * d.rts + row / ROWS)];
+    Sum<D> s;
+    const long long w = d.g < 0 ? all + at : at;
+    if (ctas.x < 0) s.one(p.whole + w * D, p.whole_ml[w], lane);
+    else if (ctas.y >= ctas.x && ctas.y < kMostCtas) s.parts(p, ROWS, ctas.x, ctas.y, row % ROWS, lane);
+    sum.add(s);
   };
-  if (fmt == FP4ATTN_FMT_NVFP4) return d == 64 ? go(row_kernel<FP4ATTN_FMT_NVFP4, 64>) : go(row_kernel<FP4ATTN_FMT_NVFP4, 128>);
-  return d == 64 ? go(row_kernel<FP4ATTN_FMT_E4M3, 64>) : go(row_kernel<FP4ATTN_FMT_E4M3, 128>);
+  // the last group that begins here or before
+  int g = 0, end = p.groups;
+  while (end - g > 1) {
+    const int mid = (g + end) / 2;
+    if (load(p.group_start + mid) <= b) g = mid;
+    else end = mid;
+  }
+  const int b0 = load(p.group_start + g);
+  if (b >= b0 && b < load(p.group_start + g + 1)) take(g, ((b - max(0, b0)) * p.T + t) * p.group + hl);
+  take(p.groups + b, t * p.group + hl);
+  sum.give(p, (size_t)at, kvh, lane);
+}
+
+// keys that each tile of rows sees, where first or last say so: a warp a tile
+template <int ROWS>
+__global__ void __launch_bounds__(128) range_kernel(const PagedParams p, int2* ranges) {
+  launch_dependents();
+  wait_prior_grids();
+  const int x = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (x >= p.B * p.row_tiles) return;
+  const int b = x / p.row_tiles, row0 = (x - b * p.row_tiles) * ROWS, n = tokens_of(p, b), ctx = context_of(p, b);
+  int lo = INT_MAX, hi = 0;
+  for (int t = row0 / p.group + lane; t < n && t <= (row0 + ROWS - 1) / p.group; t += 32) {
+    const int from = p.first ? max(0, load(p.first + (size_t)b * p.T + t)) : 0, until = min(p.last ? load(p.last + (size_t)b * p.T + t) : ctx + t + 1, ctx + n);
+    if (from < until) {
+      lo = min(lo, from);
+      hi = max(hi, until);
+    }
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if (lane == 0) ranges[x] = hi ? make_int2(lo, hi) : make_int2(0, 0);
+}
+
+// ---- workspace
+struct Plan {
+  int rt, row_tiles;                       // 128-row halves of an item; items of a sequence's rows
+  size_t ml, begun, ranges, split, whole, whole_ml, total;
+};
+size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
+Plan plan(int B, int H, int kv_heads, int T, int d, int groups) {
+  Plan t;
+  const long long rows = (long long)(H / kv_heads) * T;
+  // 256 rows an item where they come together (a prefix's rows are those of all its members)
+  t.rt = (groups ? rows * B / groups : rows) > 128 ? 2 : 1;
+  const long long R = 128 * t.rt, all = (long long)B * H * T;
+  t.row_tiles = (int)((rows + R - 1) / R);
+  const size_t slots = 2 * (size_t)kMostCtas * R;
+  t.ml = slots * d * 4;
+  t.begun = t.ml + slots * 8;
+  t.ranges = t.begun + kMostCtas * 16;
+  t.split = t.ranges + (groups ? 0 : align16((size_t)B * t.row_tiles * 8));
+  t.whole = t.split + (groups ? align16((size_t)(B * rows / R + groups + 1 + (long long)B * t.row_tiles) * kv_heads * 8) : 0);
+  t.whole_ml = t.whole + (groups ? (size_t)(2 * all) * d * 4 : 0);
+  t.total = t.whole_ml + (groups ? align16((size_t)(2 * all) * 8) : 0);
+  return t;
+}
+
+template <int FMT, int D, int RT, int SCORES>
+int launch_scores(const PagedParams& p, cudaStream_t st) {
+  using C = PagedCfg<FMT, D, RT>;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FP4ATTN_ERR_CUDA;
+  static std::atomic<bool> attr_set[kMaxDevices];
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(paged_kernel<FMT, D, RT, SCORES>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
+    attr_set[dev].store(true, std::memory_order_release);
+  }
+  const int sms = device_sms();
+  if (!sms) return FP4ATTN_ERR_CUDA;
+  const unsigned grid = (unsigned)std::min(sms, kMostCtas);
+  cudaError_t e = cudaSuccess;
+  if (p.ranges)
+    e = launch_overlapped(range_kernel<C::kRows>, dim3((unsigned)((p.B * p.row_tiles + 3) / 4)), 128u, 0, st, p, const_cast<int2*>(p.ranges));
+  if (e == cudaSuccess) e = launch_overlapped(paged_kernel<FMT, D, RT, SCORES>, dim3(grid), C::kThreads, C::kSmem, st, p);
+  const long long rows = (long long)p.B * p.H * p.T;
+  if (e == cudaSuccess)
+    e = p.groups ? launch_overlapped(shared_join_kernel<D, C::kRows>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), kJoinThreads, 0, st, p)
+                 : launch_overlapped(join_kernel<D, C::kRows>, dim3(grid, (unsigned)std::min(8, (std::min(p.group * p.T, C::kRows) + 7) / 8)), kJoinThreads, 0, st, p);
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
+}
+template <int FMT, int D, int RT>
+int launch_rows(const PagedParams& p, cudaStream_t st) {
+  if (p.slopes) return launch_scores<FMT, D, RT, kBiased>(p, st);
+  return p.cap > 0.f ? launch_scores<FMT, D, RT, kCapped>(p, st) : launch_scores<FMT, D, RT, kScaled>(p, st);
+}
+int launch(PagedParams& p, const Plan& t, void* workspace, int fmt, int d, cudaStream_t st) {
+  char* const ws = (char*)workspace;
+  p.row_tiles = t.row_tiles;
+  p.part = (float*)ws;
+  p.part_ml = (float2*)(ws + t.ml);
+  if (p.groups) {
+    p.split = (int2*)(ws + t.split);
+    p.whole = (float*)(ws + t.whole);
+    p.whole_ml = (float2*)(ws + t.whole_ml);
+  } else {
+    p.begun = (int4*)(ws + t.begun);
+    if (p.first || p.last) p.ranges = (const int2*)(ws + t.ranges);
+  }
+  auto rows = [&](auto fmt_c, auto d_c) {
+    return t.rt == 2 ? launch_rows<fmt_c.value, d_c.value, 2>(p, st) : launch_rows<fmt_c.value, d_c.value, 1>(p, st);
+  };
+  using std::integral_constant;
+  if (fmt == FP4ATTN_FMT_NVFP4)
+    return d == 64 ? rows(integral_constant<int, FP4ATTN_FMT_NVFP4>(), integral_constant<int, 64>())
+                   : rows(integral_constant<int, FP4ATTN_FMT_NVFP4>(), integral_constant<int, 128>());
+  return d == 64 ? rows(integral_constant<int, FP4ATTN_FMT_E4M3>(), integral_constant<int, 64>())
+                 : rows(integral_constant<int, FP4ATTN_FMT_E4M3>(), integral_constant<int, 128>());
 }
 
 // what the two calls have in common
@@ -132,13 +1140,14 @@ int check(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, in
           const int* count, float softmax_scale, float soft_cap, const float* slopes, void* O, float* LSE, int* device_status, PagedParams* p) {
   const int rc = check_cache(cache, B, block_table, max_pages, context, count, &p->cache);
   if (rc != FP4ATTN_OK) return rc;
-  if (!q || !q->data || !O || H <= 0 || T <= 0 || !(softmax_scale >= 0.f) || !(soft_cap >= 0.f) || isinf(softmax_scale) || isinf(soft_cap))
+  if (!q || !q->data || !O || H <= 0 || T <= 0 || !(softmax_scale >= 0.f) || isinf(softmax_scale) || !(soft_cap == 0.f || (soft_cap >= 0x1p-60f && soft_cap <= 0x1p60f)))
     return FP4ATTN_ERR_INVALID_ARG;
   if (type != FP4ATTN_TYPE_BF16 && type != FP4ATTN_TYPE_FP16) return FP4ATTN_ERR_INVALID_ARG;
   if (H % cache->kv_heads != 0) return FP4ATTN_ERR_INVALID_ARG;
-  if ((long long)B * H * T >= (1ll << 31)) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;
+  if ((long long)B * H * T >= (1ll << 31) || T >= (1 << 30)) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;
   if (((uintptr_t)q->data & 1) || ((uintptr_t)O & 15) || ((uintptr_t)LSE | (uintptr_t)device_status | (uintptr_t)slopes) & 3) return FP4ATTN_ERR_ALIGNMENT;
   p->q = q->data; p->q_sb = q->stride_b; p->q_sh = q->stride_h; p->q_sn = q->stride_n;
+  p->q_vector = view_vectors(*q, 2);
   p->half = type == FP4ATTN_TYPE_FP16;
   p->context = context; p->count = count; p->slopes = slopes;
   p->out = O; p->lse = LSE; p->status = device_status;
@@ -154,8 +1163,8 @@ int check(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, in
 using namespace fp4attn;
 
 extern "C" size_t fp4attn_paged_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d) {
-  if (B <= 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || T <= 0 || (d != 64 && d != 128) || (long long)B * H * T >= (1ll << 31)) return 0;
-  return 16;
+  if (B <= 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || T <= 0 || (d != 64 && d != 128) || (long long)B * H * T >= (1ll << 31) || T >= (1 << 30)) return 0;
+  return plan(B, H, kv_heads, T, d, 0).total;
 }
 
 extern "C" int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, const int* block_table,
@@ -170,12 +1179,12 @@ extern "C" int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp
   if ((uintptr_t)workspace & 15) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   p.first = first; p.last = last;
-  return launch(p, cache->fmt, cache->d, (cudaStream_t)stream);
+  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, 0), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
 }
 
 extern "C" size_t fp4attn_shared_prefix_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d, int groups) {
   if (groups <= 0 || groups > 65535 || T > FP4ATTN_MOST_TREE_TOKENS) return 0;
-  return fp4attn_paged_attention_workspace_bytes(B, H, kv_heads, T, d);
+  return fp4attn_paged_attention_workspace_bytes(B, H, kv_heads, T, d) ? plan(B, H, kv_heads, T, d, groups).total : 0;
 }
 
 extern "C" int fp4attn_shared_prefix_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, int groups,
@@ -194,5 +1203,5 @@ extern "C" int fp4attn_shared_prefix_attention(const fp4attn_view* q, int type, 
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   p.groups = groups; p.prefix_table = prefix_table; p.prefix_pages = prefix_pages; p.prefix_length = prefix_length; p.group_start = group_start;
   p.mask = tree_mask;
-  return launch(p, cache->fmt, cache->d, (cudaStream_t)stream);
+  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, groups), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
 }
