@@ -72,15 +72,17 @@ struct PagedCfg {
   static constexpr int kStage = kTile * L::kToken;                 // K or V of a tile
   static constexpr int kQ = kRows * D * 2, kOp = kTile * D * 2;    // an operand tile
   static constexpr int kKB = 2, kVB = RT == 2 && D == 128 && !L::kFp4 ? 1 : 2;
+  static constexpr int kJoin = RT == 1 ? 8 * 32 * 16 * 4 : 0;      // sixteen columns of O of all copies
   static constexpr int kRing = 32, kRingC = 4;                     // tiles whose pages, items whose constants are remembered
-  static constexpr int kFixed = kQ + (kKB + kVB) * kOp + 2048 + 4 * kRows * kRingC + 2048 + 4 * kRing + 256 + 64 + 512 + 1024;
+  static constexpr int kFixed = kQ + (kKB + kVB) * kOp + 2048 + 4 * kRows * kRingC + 2048 + 4 * kRing + 256 + 64 + 512 + 1024 + kJoin;
   static constexpr int kStages = (227 * 1024 - kFixed) / kStage < 8 ? (227 * 1024 - kFixed) / kStage : 8;
   static_assert(kStages >= 2, "shared memory");
   static constexpr int kOffQ = 0, kOffK = kOffQ + kQ, kOffV = kOffK + kKB * kOp, kOffStage = kOffV + kVB * kOp;
   static constexpr int kOffVScale = kOffStage + kStages * kStage;  // f16 [4 V warps][2 blocks][128 tokens]
   static constexpr int kOffC = kOffVScale + 2048;                  // float [kRingC][kRows]: score constants of the last items
   static constexpr int kOffML = kOffC + 4 * kRows * kRingC;        // float2 [2][128]
-  static constexpr int kOffValid = kOffML + 2048;                  // u32 [kRing]: pages of a tile that are there
+  static constexpr int kOffJoin = kOffML + 2048;                   // float [8 softmax warps][32][16]
+  static constexpr int kOffValid = kOffJoin + kJoin;                  // u32 [kRing]: pages of a tile that are there
   static constexpr int kOffScan = kOffValid + 4 * kRing;           // i64 [18]
   static constexpr int kOffFind = kOffScan + 256;                  // i64 [5]
   static constexpr int kOffBar = kOffFind + 64;
@@ -271,6 +273,12 @@ __device__ __forceinline__ void row_token(const PagedParams& p, const Desc& d, i
   }
 }
 
+// How often the rows of an item stand among the 128 lanes.  A warp's instructions cost the same for one row as for 32, and it sees only its own 32
+// lanes of tensor memory: few rows are kept twice or four times, and each copy takes a half or a quarter of the keys of a tile, with a reference, a
+// sum and an O of its own, its other probabilities 0.
+template <int ROWS>
+__device__ __forceinline__ int copies_of(int rows) { return ROWS > 128 || rows > 64 ? 1 : rows > 32 ? 2 : 4; }
+
 // bits [a, b) of a word, whatever a and b are
 __device__ __forceinline__ uint32_t bits_between(int a, int b) {
   const uint32_t from = a <= 0 ? 0xFFFFFFFFu : a >= 32 ? 0u : 0xFFFFFFFFu << a, until = b >= 32 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << b) - 1;
@@ -314,8 +322,8 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i) {
-      const bool four = (i < C::K_FREE) || (i >= C::V_FULL && i < C::V_FREE) || i == C::Q_FULL || (i >= C::P_FULL && i < C::PV_DONE) || i >= C::RING_FREE;
-      mbar_init(bar(i), four ? 4 : 1);
+      const bool four = (i < C::K_FREE) || (i >= C::V_FULL && i < C::V_FREE) || (i >= C::P_FULL && i < C::PV_DONE) || i >= C::RING_FREE;
+      mbar_init(bar(i), i == C::Q_FULL ? 8 : four ? 4 : 1);
     }
     *abort_word = 0;
     fence_barrier_init();
@@ -334,6 +342,72 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   const int log_page = p.cache.log_page, P = 1 << log_page, half_record = p.cache.record / 2;
   const uint32_t all_pages = (1u << (kTile >> log_page)) - 1;
 
+  // Q of an item, by the 256 threads that convert K and V.  Rows are scaled by a power of two into f16's range (the largest element to [2^14,
+  // 2^15)): exact for 8-bit significands, and a row's scores are scaled back by its constant.  Rows up to the next 32 are written, since a warp of softmax
+  // threads takes all of its 32 or none; few rows are written as often as their copies are (see copies_of).
+  auto bring_q = [&](int& item, int& q_phase) {
+    wait(C::Q_FREE, q_phase);
+    q_phase ^= 1;
+    constexpr int kParts = D / 16;                                  // threads of a row
+    const int kvh = w.kvh(), here = min(ROWS, w.d.rows - w.row0), copies = copies_of<ROWS>(here), apart = 128 / copies;
+    const float c = __fdiv_rn(p.scale * 1.4426950408889634f, load(p.cache.k_G + kvh));
+    float* const con = reinterpret_cast<float*>(sgen + C::kOffC) + (item & (C::kRingC - 1)) * ROWS;
+    constexpr int kAtOnce = 4;                                      // rows of a thread whose loads are on their way together
+    for (int j0 = threadIdx.x; j0 < ((here + 31) & ~31) * kParts; j0 += 256 * kAtOnce) {
+      uint32_t raw[kAtOnce][8];
+      const int e = (j0 % kParts) * 16;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int r = (j0 + 256 * i) / kParts;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) raw[i][x] = 0u;
+        if (r < here) {
+          int b, tok, hl;
+          row_token(p, w.d, w.row0 + r, &b, &tok, &hl);
+          const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
+          if (p.q_vector) {
+            *reinterpret_cast<uint4*>(raw[i]) = load(reinterpret_cast<const uint4*>(q));
+            *reinterpret_cast<uint4*>(raw[i] + 4) = load(reinterpret_cast<const uint4*>(q) + 1);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) raw[i][x] = (uint32_t)load(q + 2 * x) | (uint32_t)load(q + 2 * x + 1) << 16;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int r = (j0 + 256 * i) / kParts;
+        if (r >= ((here + 31) & ~31)) break;                        // (a warp's rows are a few neighbours: all or none)
+        float v[16], a = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const float2 f = p.half ? unpack16<true>(raw[i][x]) : unpack16<false>(raw[i][x]);
+          v[2 * x] = f.x;
+          v[2 * x + 1] = f.y;
+          a = fmaxf(a, fmaxf(fabsf(f.x), fabsf(f.y)));
+        }
+#pragma unroll
+        for (int x = 1; x < kParts; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
+        const uint32_t up = row_exponent(a);
+        const float f = __uint_as_float(up << 23);
+        uint32_t h[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(v[2 * x] * f, v[2 * x + 1] * f);
+        uint8_t* const panel = sgen + C::kOffQ + (r >> 7) * (128 * D * 2) + (e >> 6) * 16384;
+        for (int k = 0; k < copies; ++k) {
+          const int to = (r & 127) + k * apart;
+          *reinterpret_cast<uint4*>(panel + chunk_at(to, (e & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(panel + chunk_at(to, ((e & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
+        }
+        if (e == 0) con[r] = c * __uint_as_float((254u - up) << 23);
+      }
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(C::Q_FULL));
+    ++item;
+  };
+
   if (warp == C::kProducer) {
     // ===================================================================== pages -> shared memory
     Turn<C::kStages> ring;
@@ -341,6 +415,17 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     int parts = 0;
 #pragma unroll 1
     for (int i = 0; w.left > 0; ++i) {
+      if (rare(w.fresh)) {
+        // Q of an item into L2, while the tiles before it are worked on
+        const int here = min(ROWS, w.d.rows - w.row0), kvh = w.kvh();
+        for (int r = lane; r < here; r += 32) {
+          int b, tok, hl;
+          row_token(p, w.d, w.row0 + r, &b, &tok, &hl);
+          const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn;
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
+          if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
+        }
+      }
       const int first = w.first_key(), pos = first + lane * P;
       int page = -1;
       if (lane < kTile >> log_page && pos < w.d.hi && pos + P > w.d.lo) {
@@ -456,12 +541,12 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   } else if (warp < C::kFirstV) {
     // ===================================================================== K and Q
     const int key = threadIdx.x, slot = key >> log_page, t = key & (P - 1);
-    const float c0 = p.scale * 1.4426950408889634f;
     Turn<C::kStages> ring;
     Turn<C::kKB> kb;
     int item = 0, q_phase = 1;
 #pragma unroll 1
     while (w.left > 0) {
+      if (rare(w.fresh)) bring_q(item, q_phase);
       wait(C::K_FREE + kb.at, kb.phase ^ 1);
       wait(C::RING_FULL + ring.at, ring.phase);
       {
@@ -510,60 +595,6 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       if (lane == 0) mbar_arrive(bar(C::K_FULL + kb.at));
       ring.next(2);
       kb.next();
-      if (rare(w.fresh)) {
-        // Rows scaled by a power of two into f16's range (the largest element to [2^14, 2^15)): exact for 8-bit significands, and a row's scores are
-        // scaled back by its constant.  Rows up to the next 32 are written: a warp of softmax threads takes all of its 32 or none.
-        wait(C::Q_FREE, q_phase);
-        q_phase ^= 1;
-        const int kvh = w.kvh(), here = min(ROWS, w.d.rows - w.row0);
-        const float c = __fdiv_rn(c0, load(p.cache.k_G + kvh));
-        constexpr int kParts = D / 16;                              // threads of a row
-        float* const con = reinterpret_cast<float*>(sgen + C::kOffC) + (item & (C::kRingC - 1)) * ROWS;
-#pragma unroll 2
-        for (int j = key; j < ((here + 31) & ~31) * kParts; j += 128) {
-          const int r = j / kParts, e = (j % kParts) * 16;
-          float v[16];
-#pragma unroll
-          for (int x = 0; x < 16; ++x) v[x] = 0.f;
-          if (r < here) {
-            int b, tok, hl;
-            row_token(p, w.d, w.row0 + r, &b, &tok, &hl);
-            const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
-            uint32_t raw[8];
-            if (p.q_vector) {
-              *reinterpret_cast<uint4*>(raw) = load(reinterpret_cast<const uint4*>(q));
-              *reinterpret_cast<uint4*>(raw + 4) = load(reinterpret_cast<const uint4*>(q) + 1);
-            } else {
-#pragma unroll
-              for (int x = 0; x < 8; ++x) raw[x] = (uint32_t)load(q + 2 * x) | (uint32_t)load(q + 2 * x + 1) << 16;
-            }
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              const float2 f = p.half ? unpack16<true>(raw[x]) : unpack16<false>(raw[x]);
-              v[2 * x] = f.x;
-              v[2 * x + 1] = f.y;
-            }
-          }
-          float a = 0.f;
-#pragma unroll
-          for (int x = 0; x < 16; ++x) a = fmaxf(a, fabsf(v[x]));
-#pragma unroll
-          for (int x = 1; x < kParts; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
-          const uint32_t up = row_exponent(a);
-          const float f = __uint_as_float(up << 23);
-          uint32_t h[8];
-#pragma unroll
-          for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(v[2 * x] * f, v[2 * x + 1] * f);
-          uint8_t* const panel = sgen + C::kOffQ + (r >> 7) * (128 * D * 2) + (e >> 6) * 16384;
-          *reinterpret_cast<uint4*>(panel + chunk_at(r & 127, (e & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(panel + chunk_at(r & 127, ((e & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
-          if (e == 0) con[r] = c * __uint_as_float((254u - up) << 23);
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::Q_FULL));
-        ++item;
-      }
       w.next(p);
     }
   } else if (warp < C::kFirstSoftmax) {
@@ -578,9 +609,11 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     const uint32_t scale0 = (uint32_t)((sc_tok >> log_page) * half_record + P * L::kRow + sc_block * P + (sc_tok & (P - 1)));
     Turn<C::kStages> ring;
     Turn<C::kVB> vb;
+    int item = 0, q_phase = 1;
     ring.next();
 #pragma unroll 1
     for (int i = 0; w.left > 0; ++i) {
+      if (rare(w.fresh)) bring_q(item, q_phase);
       wait(C::V_FREE + vb.at, vb.phase ^ 1);
       wait(C::RING_FULL + ring.at, ring.phase);
       {
@@ -649,15 +682,34 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     int lo = 0, hi = 0, row = 0, ctx = 0, b = 0, t = 0, hl = 0;
     long long done = 0;                                               // tiles of this CTA's run
     float m = -INFINITY, l0 = 0.f, l1 = 0.f, con = 0.f, slope = 0.f;
-    int pos = 0;
+    int pos = 0, copies = 1, row_in = 0, c_first = 0;                 // this thread's row of the item, its first 32 keys of a tile
     unsigned long long mask = 0;
+    auto top_of = [&](int from, int end) {                            // largest of the scores of 32-key pieces
+      float top = -INFINITY;
+#pragma unroll 1
+      for (int k = from; k < end; ++k) {
+        uint32_t a[32];
+        tmem_ld_32x32b_x32(s_at + 32 * k, a);
+        tmem_wait_ld();
+        float t2 = __uint_as_float(a[0]);
+#pragma unroll
+        for (int x = 0; x < 32; x += 4) {
+          top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
+          t2 = max3(t2, __uint_as_float(a[x + 2]), __uint_as_float(a[x + 3]));
+        }
+        top = fmaxf(top, t2);
+      }
+      return top;
+    };
     const float cap_in = p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f;
 #pragma unroll 1
     while (w.left > 0) {
       const bool two = w.two();
       if (rare(w.fresh)) {
-        const int r = (two ? (group ^ par) * 128 : 0) + in_tile;
-        row = w.row0 + r;
+        copies = copies_of<ROWS>(min(ROWS, w.d.rows - w.row0));
+        row_in = two ? (group ^ par) * 128 + in_tile : in_tile & (128 / copies - 1);
+        c_first = two ? 0 : in_tile / (128 / copies) * (4 / copies);
+        row = w.row0 + row_in;
         live = row < w.d.rows;
         part_first = w.tile;
         m = -INFINITY;
@@ -695,41 +747,22 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         wait(C::S_FULL + group, s_phase);
         s_phase ^= 1;
         tc_fence_after();
-        if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + (two ? (group ^ par) * 128 : 0) + in_tile] : 0.f;
+        if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
         if (warp_live) {
           const int first = w.first_key();
           const uint32_t held = valid_ring[done % C::kRing];
           const bool plain = __all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + kTile);
           float top = -INFINITY, c2 = con;
+          const int c_end = c_first + 4 / copies;
           if (SCORES == kScaled && plain) {
-            uint32_t a[32], c[32];
-#pragma unroll
-            for (int k = 0; k < 4; k += 2) {
-              tmem_ld_32x32b_x32(s_at + 32 * k, a);
-              tmem_ld_32x32b_x32(s_at + 32 * k + 32, c);
-              tmem_wait_ld();
-#pragma unroll
-              for (int x = 0; x < 32; x += 2) {
-                top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
-                top = max3(top, __uint_as_float(c[x]), __uint_as_float(c[x + 1]));
-              }
-            }
-            top *= con;
+            top = top_of(c_first, c_end) * con;
           } else if (CAP && plain) {
-            uint32_t a[32];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              tmem_ld_32x32b_x32(s_at + 32 * k, a);
-              tmem_wait_ld();
-#pragma unroll
-              for (int x = 0; x < 32; x += 2) top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
-            }
-            top = cap_score(top * con, cap_in, cap_out);
+            top = cap_score(top_of(c_first, c_end) * con, cap_in, cap_out);
           } else {
             // the scores are changed, masked and put back
             c2 = 1.f;
 #pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
+            for (int k = c_first; k < c_end; ++k) {
               uint32_t a[32];
               tmem_ld_32x32b_x32(s_at + 32 * k, a);
               const int at = first + 32 * k;
@@ -807,15 +840,22 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
             }
             tmem_st_32x32b_x8(s_at + 8 * k, h);                       // (over scores that have been read)
           };
-          tmem_ld_32x32b_x16(s_at, a);
-#pragma unroll
-          for (int k = 0; k < 8; k += 2) {
+          tmem_ld_32x32b_x16(s_at + 32 * c_first, a);
+#pragma unroll 1
+          for (int k = 2 * c_first; k < 2 * c_end; k += 2) {
             tmem_wait_ld();
             tmem_ld_32x32b_x16(s_at + 16 * k + 16, c);
             work(a, k);
             tmem_wait_ld();
-            if (k < 6) tmem_ld_32x32b_x16(s_at + 16 * k + 32, a);
+            if (k + 2 < 2 * c_end) tmem_ld_32x32b_x16(s_at + 16 * k + 32, a);
             work(c, k + 1);
+          }
+          if (ROWS <= 128 && copies > 1) {                            // the other copies' keys
+#pragma unroll
+            for (int x = 0; x < 16; ++x) a[x] = 0u;
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k)
+              if (k < c_first || k >= c_end) tmem_st_32x32b_x16(s_at + 16 * k, a);
           }
           tmem_wait_st();
         }
@@ -832,24 +872,26 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         const int kvh = w.kvh(), slot = 2 * (int)blockIdx.x + (part_first == 0);
         if (have) wait(C::PV_DONE + group, pv_phase);
         float f[2] = {1.f, 1.f}, top = m, sum = l0 + l1;
-        if (!two) {                                                   // both groups have had tiles of these rows
-          ml[group * 128 + in_tile] = make_float2(m, sum);
+        if (!two) {                                                   // both groups, and every copy, have had tiles of these rows
+          ml[group * 128 + in_tile] = make_float2(have ? m : -INFINITY, have ? sum : 0.f);
           bar_sync(1, 256);
-          const float2 other = ml[(group ^ 1) * 128 + in_tile];
-          top = fmaxf(m, other.x);
-          const float mine = !have || m == -INFINITY && sum == 0.f ? 0.f : m == top ? 1.f : exp2_approx(m - top);
-          const float others = other.x == -INFINITY && other.y == 0.f ? 0.f : other.x == top ? 1.f : exp2_approx(other.x - top);
-          f[group] = mine;
-          f[group ^ 1] = others;
-          // (in one order, so that both groups have the same bits)
-          const float s0 = group == 0 ? mine * sum : others * other.y, s1 = group == 0 ? others * other.y : mine * sum;
-          sum = s0 + s1;
+          // (in one order, so that all have the same bits)
+          top = -INFINITY;
+          for (int k = 0; k < 2 * copies; ++k) top = fmaxf(top, ml[(k & 1) * 128 + row_in + (k >> 1) * (128 / copies)].x);
+          auto weight = [&](float2 x) { return x.x == -INFINITY && x.y == 0.f ? 0.f : x.x == top ? 1.f : exp2_approx(x.x - top); };
+          sum = 0.f;
+          for (int k = 0; k < 2 * copies; ++k) {
+            const float2 x = ml[(k & 1) * 128 + row_in + (k >> 1) * (128 / copies)];
+            const float y = weight(x);
+            sum += y == 0.f ? 0.f : y * x.y;
+          }
+          f[0] = weight(ml[in_tile]);
+          f[1] = weight(ml[128 + in_tile]);
         } else if (m == -INFINITY && sum == 0.f) {
           f[group] = 0.f;
         }
         tc_fence_after();
-        const int r = row - w.row0;
-        const bool mine = live && row < w.d.rows;
+        const bool mine = live && row < w.d.rows, tells = two || (group == 0 && in_tile < 128 / copies);
         long long at = 0;                                             // of the row among the outputs
         if (mine) at = ((long long)b * p.H + kvh * p.group + hl) * p.T + t;
         const bool out = whole && !p.groups;
@@ -858,14 +900,63 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
           const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum * load(p.cache.v_G + kvh));          // nothing seen: 0, not 0 / 0
           f[0] = f[0] == 0.f ? 0.f : f[0] * inv;
           f[1] = f[1] == 0.f ? 0.f : f[1] * inv;
-          if (mine && p.lse && (two || group == 0)) p.lse[at] = sum == 0.f ? -INFINITY : (top - kShift + log2f(sum)) * 0.6931471805599453f;
+          if (mine && p.lse && tells) p.lse[at] = sum == 0.f ? -INFINITY : (top - kShift + log2f(sum)) * 0.6931471805599453f;
         } else if (mine) {
           const bool own = w.d.g < 0;
-          dst = whole ? p.whole + (own ? (long long)p.B * p.H * p.T + at : at) * D : p.part + ((size_t)slot * ROWS + r) * D;
-          if (two || group == 0) *(whole ? p.whole_ml + (own ? (long long)p.B * p.H * p.T + at : at) : p.part_ml + (size_t)slot * ROWS + r) = make_float2(top, sum);
+          dst = whole ? p.whole + (own ? (long long)p.B * p.H * p.T + at : at) * D : p.part + ((size_t)slot * ROWS + row_in) * D;
+          if (tells) *(whole ? p.whole_ml + (own ? (long long)p.B * p.H * p.T + at : at) : p.part_ml + (size_t)slot * ROWS + row_in) = make_float2(top, sum);
         }
         __syncwarp();
-        if (warp_live) {
+        auto write = [&](int e, const float* o) {                     // sixteen elements of a row
+          if (out) {
+            uint32_t h[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) h[x] = p.half ? pack_pair<__half>(o[2 * x], o[2 * x + 1]) : pack_pair<__nv_bfloat16>(o[2 * x], o[2 * x + 1]);
+            uint4* const y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at * D + e);
+            y[0] = make_uint4(h[0], h[1], h[2], h[3]);
+            y[1] = make_uint4(h[4], h[5], h[6], h[7]);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 16; x += 4) *reinterpret_cast<float4*>(dst + e + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+          }
+        };
+        if (ROWS <= 128 && copies > 1) {
+          // The copies' O meet in shared memory, sixteen elements at a time; the group's warps of the first copy take the even or the odd
+          // ones of a row from there.  Rows that do not exist are skipped, but for the barriers.
+          float* const join = reinterpret_cast<float*>(sgen + C::kOffJoin);
+          float* const put = join + ((warp - C::kFirstSoftmax) * 32 + lane) * 16;
+#pragma unroll 1
+          for (int e = 0; e < D; e += 16) {
+            if (warp_live) {
+              uint32_t v[16];
+              tmem_ld_32x32b_x16(o_at + e, v);
+              tmem_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 16; x += 4) {
+                const float g = f[group];
+                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (g != 0.f) y = make_float4(__uint_as_float(v[x]) * g, __uint_as_float(v[x + 1]) * g, __uint_as_float(v[x + 2]) * g, __uint_as_float(v[x + 3]) * g);
+                *reinterpret_cast<float4*>(put + (x ^ (lane >> 1 & 3) * 4)) = y;
+              }
+            }
+            bar_sync(1, 256);
+            if (mine && in_tile < 128 / copies && (e >> 4 & 1) == group) {
+              float o[16];
+#pragma unroll
+              for (int x = 0; x < 16; ++x) o[x] = 0.f;
+              for (int k = 0; k < 2 * copies; ++k) {                  // (warp of the copy: of the group k & 1, as many warps on as a copy has)
+                const float* const from = join + (((k & 1) * 4 + (k >> 1) * (4 / copies) + quarter) * 32 + lane) * 16;
+#pragma unroll
+                for (int x = 0; x < 16; x += 4) {
+                  const float4 y = *reinterpret_cast<const float4*>(from + (x ^ (lane >> 1 & 3) * 4));
+                  o[x] += y.x; o[x + 1] += y.y; o[x + 2] += y.z; o[x + 3] += y.w;
+                }
+              }
+              write(e, o);
+            }
+            bar_sync(1, 256);
+          }
+        } else if (warp_live) {
           const int d0 = two ? 0 : group * (D / 2), d1 = two ? D : d0 + D / 2;
 #pragma unroll 1
           for (int e = d0; e < d1; e += 16) {
@@ -885,17 +976,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               for (int x = 0; x < 16; ++x)
                 o[x] = (f[0] == 0.f ? 0.f : __uint_as_float(v[x]) * f[0]) + (f[1] == 0.f ? 0.f : __uint_as_float(v2[x]) * f[1]);
             }
-            if (mine && out) {
-              uint32_t h[8];
-#pragma unroll
-              for (int x = 0; x < 8; ++x) h[x] = p.half ? pack_pair<__half>(o[2 * x], o[2 * x + 1]) : pack_pair<__nv_bfloat16>(o[2 * x], o[2 * x + 1]);
-              uint4* const y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at * D + e);
-              y[0] = make_uint4(h[0], h[1], h[2], h[3]);
-              y[1] = make_uint4(h[4], h[5], h[6], h[7]);
-            } else if (mine) {
-#pragma unroll
-              for (int x = 0; x < 16; x += 4) *reinterpret_cast<float4*>(dst + e + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
-            }
+            if (mine) write(e, o);
             __syncwarp();
           }
         }
@@ -1068,8 +1149,7 @@ size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
 Plan plan(int B, int H, int kv_heads, int T, int d, int groups) {
   Plan t;
   const long long rows = (long long)(H / kv_heads) * T;
-  // 256 rows an item where they come together (a prefix's rows are those of all its members)
-  t.rt = (groups ? rows * B / groups : rows) > 128 ? 2 : 1;
+  t.rt = !groups && rows > 128 ? 2 : 1;
   const long long R = 128 * t.rt, all = (long long)B * H * T;
   t.row_tiles = (int)((rows + R - 1) / R);
   const size_t slots = 2 * (size_t)kMostCtas * R;
