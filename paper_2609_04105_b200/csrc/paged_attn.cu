@@ -59,9 +59,24 @@ struct PagedParams {
   float* whole;                            // shared: [2][B, H, T][D] of whole items
   float2* whole_ml;                        // [2][B, H, T]
   int B, H, T, group, row_tiles;           // row_tiles: of a sequence's rows
+  unsigned long long by_group, by_tokens;  // for divide()
   float scale, cap;
-  bool half, q_vector;
+  bool half, q_vector, out_wide;           // out_wide: O begins at a multiple of 32 bytes
 };
+
+// What a CTA has of an item: written by the producer, read by the other roles
+struct Item {
+  int tiles;                               // of the item here; 0: no item, the end
+  int first;                               // first key of the first of them
+  int lo, hi, ctx;                         // as in Desc
+  int b, g, kvh;
+  int row0, here, v0, h0;                  // its first row, how many it has; token and head of the first
+  int two, copies;                         // more than 128 rows; how often rows are kept (see copies_of)
+  int begins, whole;                       // does it begin here, and does all of it lie here
+  int last_cta, slot;                      // where it ends; place of its partial result
+  long long split;                         // place in p.split
+};
+constexpr int kItems = 32;                 // the producer is some ten tiles, hence items, ahead at most
 
 template <int FMT, int D, int RT>
 struct PagedCfg {
@@ -74,7 +89,8 @@ struct PagedCfg {
   static constexpr int kKB = 2, kVB = RT == 2 && D == 128 && !L::kFp4 ? 1 : 2;
   static constexpr int kJoin = RT == 1 ? 8 * 32 * 16 * 4 : 0;      // sixteen columns of O of all copies
   static constexpr int kRing = 32, kRingC = 4;                     // tiles whose pages, items whose constants are remembered
-  static constexpr int kFixed = kQ + (kKB + kVB) * kOp + 2048 + 4 * kRows * kRingC + 2048 + 4 * kRing + 256 + 64 + 512 + 1024 + kJoin;
+  static constexpr int kItemBytes = kItems * (int)sizeof(Item);
+  static constexpr int kFixed = kQ + (kKB + kVB) * kOp + 2048 + 4 * kRows * kRingC + 2048 + 4 * kRing + 256 + 64 + 1024 + 1024 + kJoin + kItemBytes;
   static constexpr int kStages = (227 * 1024 - kFixed) / kStage < 8 ? (227 * 1024 - kFixed) / kStage : 8;
   static_assert(kStages >= 2, "shared memory");
   static constexpr int kOffQ = 0, kOffK = kOffQ + kQ, kOffV = kOffK + kKB * kOp, kOffStage = kOffV + kVB * kOp;
@@ -83,14 +99,15 @@ struct PagedCfg {
   static constexpr int kOffML = kOffC + 4 * kRows * kRingC;        // float2 [2][128]
   static constexpr int kOffJoin = kOffML + 2048;                   // float [8 softmax warps][32][16]
   static constexpr int kOffValid = kOffJoin + kJoin;                  // u32 [kRing]: pages of a tile that are there
-  static constexpr int kOffScan = kOffValid + 4 * kRing;           // i64 [18]
+  static constexpr int kOffItems = kOffValid + 4 * kRing;
+  static constexpr int kOffScan = kOffItems + kItemBytes;           // i64 [18]
   static constexpr int kOffFind = kOffScan + 256;                  // i64 [5]
   static constexpr int kOffBar = kOffFind + 64;
-  static constexpr int kSmem = kOffBar + 512 + 1024;
+  static constexpr int kSmem = kOffBar + 1024 + 1024;
   static_assert(kSmem <= 227 * 1024 && kOffStage % 1024 == 0 && kStage % 16 == 0, "shared memory");
   enum { K_FULL = 0, K_FREE = K_FULL + kKB, V_FULL = K_FREE + kKB, V_FREE = V_FULL + kVB, Q_FULL = V_FREE + kVB, Q_FREE, S_FULL, P_FULL = S_FULL + 2,
-         PV_DONE = P_FULL + 2, DRAIN = PV_DONE + 2, RING_FULL, RING_FREE = RING_FULL + kStages, kBars = RING_FREE + kStages };
-  static_assert(kBars * 8 + 16 <= 512, "barriers");
+         PV_DONE = P_FULL + 2, DRAIN = PV_DONE + 2, MEET, RING_FULL, RING_FREE = RING_FULL + kStages, ITEM = RING_FREE + kStages, kBars = ITEM + kItems };
+  static_assert(kBars * 8 + 16 <= 1024, "barriers");
   static constexpr int kS = 0, kO = 256;                           // tensor memory: scores (and P) of the two groups, their O
 };
 
@@ -175,44 +192,25 @@ __device__ __forceinline__ size_t split_place(const PagedParams& p, const Desc& 
   const long long at = d.g >= 0 ? d.b * rows / ROWS + d.g + rt : p.B * rows / ROWS + p.groups + 1 + (long long)d.b * p.row_tiles + rt;
   return (size_t)at * p.cache.kv_heads + kvh;
 }
-template <int ROWS>
-struct Walk {
-  Desc d;
-  int x, u;                                // item: u = KV head x row tiles + row tile
-  int tile;                                // of the item
-  int left;                                // of this CTA's run, this one included
-  bool fresh;                              // the item's first tile here
-  int row0;
-  __device__ __forceinline__ int kvh() const { return u / d.rts; }
-  __device__ __forceinline__ int first_key() const { return (d.k0 + tile) * kTile; }
-  __device__ __forceinline__ bool two() const { return ROWS > 128 && d.rows - row0 > 128; }
-  __device__ __forceinline__ bool ends() const { return tile + 1 == d.nt || left == 1; }        // the item here
-  __device__ __forceinline__ void set_rows() { row0 = d.row0 + u % d.rts * ROWS; }
-  __device__ __forceinline__ void next(const PagedParams& p) {
-    fresh = false;
-    --left;
-    if (!rare(++tile == d.nt) || left <= 0) return;
-    tile = 0;
-    fresh = true;
-    if (++u == d.rts * p.cache.kv_heads) {
-      u = 0;
-      do describe<ROWS>(p, ++x, d);
-      while (d.nt == 0);                   // (there is another item: the run goes on)
-    }
-    set_rows();
-  }
-};
+// n / d for n up to 2^24 (d < 2^12) or 2^17 (d < 2^16): m = ceil(2^36 / d), so that n (m d - 2^36) < n d stays below 2^36
+__device__ __forceinline__ int divide(int n, unsigned long long m) { return (int)((unsigned long long)n * m >> 36); }
 
-// This CTA's run of tiles.  find: its first tile's number, all tiles, CTAs.  Barriers of the block.
+// This CTA's run of the list, in units: a tile is one, and an item that many more (bringing Q, writing O), which come before its tiles.  x, the run's
+// first unit among x's, how many, the first one's number in the list, all units, CTAs.  Barriers of the block.
+constexpr int kItemCost = 2;
+struct Run {
+  int x;
+  long long at, tiles, first, total, ctas;
+};
 template <int ROWS, int THREADS>
-__device__ __forceinline__ void find_run(const PagedParams& p, Walk<ROWS>& w, long long* scan, long long* find) {
+__device__ __forceinline__ Run find_run(const PagedParams& p, long long* scan, long long* find) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int X = p.groups ? p.groups + p.B : p.B * p.row_tiles;
   const int per = (X + THREADS - 1) / THREADS, x0 = min(X, (int)threadIdx.x * per), x1 = min(X, x0 + per);
   Desc d;
   auto tiles = [&](int x) {
     describe<ROWS>(p, x, d);
-    return d.nt ? (long long)d.nt * d.rts * p.cache.kv_heads : 0ll;
+    return d.nt ? (long long)(d.nt + kItemCost) * d.rts * p.cache.kv_heads : 0ll;
   };
   long long mine = 0;
 #pragma unroll 1
@@ -225,51 +223,46 @@ __device__ __forceinline__ void find_run(const PagedParams& p, Walk<ROWS>& w, lo
   }
   if (lane == 31) scan[warp] = incl;
   __syncthreads();
-  long long before = 0, total = 0;
+  Run r;
+  long long before = 0;
+  r.total = 0;
 #pragma unroll 1
   for (int i = 0; i < THREADS / 32; ++i) {
     if (i < warp) before += scan[i];
-    total += scan[i];
+    r.total += scan[i];
   }
   before += incl - mine;
-  const long long ctas = min((long long)gridDim.x, total);
-  const long long t0 = blockIdx.x < ctas ? mul_div(blockIdx.x, total, ctas) : total, t1 = blockIdx.x < ctas ? mul_div(blockIdx.x + 1, total, ctas) : total;
-  if (threadIdx.x == 0) {
-    find[2] = t0;
-    find[3] = total;
-    find[4] = ctas;
-  }
-  if (t0 < t1 && before <= t0 && t0 < before + mine) {              // one thread
+  r.ctas = min((long long)gridDim.x, r.total);
+  r.first = blockIdx.x < r.ctas ? mul_div(blockIdx.x, r.total, r.ctas) : r.total;
+  r.tiles = blockIdx.x < r.ctas ? mul_div(blockIdx.x + 1, r.total, r.ctas) - r.first : 0;
+  if (r.tiles && before <= r.first && r.first < before + mine) {    // one thread
     int x = x0;
-    for (;; ++x) {
-      const long long here = tiles(x);
-      if (t0 < before + here) break;
-      before += here;
-    }
+    if (per > 1)
+      for (;; ++x) {
+        const long long here = tiles(x);
+        if (r.first < before + here) break;
+        before += here;
+      }
     find[0] = x;
-    find[1] = t0 - before;
+    find[1] = r.first - before;
   }
   __syncthreads();
-  w.left = (int)min(t1 - t0, (long long)INT_MAX);
-  w.fresh = true;
-  w.x = w.u = w.tile = w.row0 = 0;
-  if (w.left <= 0) return;
-  w.x = (int)find[0];
-  describe<ROWS>(p, w.x, w.d);
-  w.u = (int)mul_div(find[1], 1, w.d.nt);
-  w.tile = (int)(find[1] - (long long)w.u * w.d.nt);
-  w.set_rows();
+  r.x = r.tiles ? (int)find[0] : 0;
+  r.at = r.tiles ? find[1] : 0;
+  return r;
 }
 
-// entry and token of row r of an item
-__device__ __forceinline__ void row_token(const PagedParams& p, const Desc& d, int r, int* b, int* t, int* h) {
-  const int v = r / p.group;
-  *h = r - v * p.group;
-  *b = d.b;
-  *t = v;
-  if (d.g >= 0) {
-    *b = d.b + v / p.T;
-    *t = v % p.T;
+// entry, token and head of row r of an item (or of x: the same with v0 = h0 = 0 where r * group is small)
+template <class I>
+__device__ __forceinline__ void row_token(const PagedParams& p, const I& i, int r, int* b, int* t, int* h) {
+  const int at = i.h0 + r, v = divide(at, p.by_group);
+  *h = at - v * p.group;
+  *b = i.b;
+  *t = i.v0 + v;
+  if (i.g >= 0) {
+    const int e = divide(*t, p.by_tokens);
+    *b = i.b + e;
+    *t -= e * p.T;
   }
 }
 
@@ -293,6 +286,13 @@ __device__ __forceinline__ float rcp_approx(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+// the larger of two magnitudes as row_exponent wants it: a NaN counts as the largest number there is
+__device__ __forceinline__ float finite_max(float a, float b) { return fminf(fmaxf(a, b), 0x1.fffffep127f); }
+// 32 bytes at once, so aligned
+__device__ __forceinline__ void store_32(void* dst, const uint32_t* h) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(dst), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
 }
 // f16 pairs: NaN and infinities of bytes that nobody wrote become numbers, everything that a cache holds stays (E4M3 ends at 448): a probability
 // of 0 times any of them is 0
@@ -322,8 +322,8 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i) {
-      const bool four = (i < C::K_FREE) || (i >= C::V_FULL && i < C::V_FREE) || (i >= C::P_FULL && i < C::PV_DONE) || i >= C::RING_FREE;
-      mbar_init(bar(i), i == C::Q_FULL ? 8 : four ? 4 : 1);
+      const bool four = (i < C::K_FREE) || (i >= C::V_FULL && i < C::V_FREE) || (i >= C::P_FULL && i < C::PV_DONE) || (i >= C::RING_FREE && i < C::ITEM);
+      mbar_init(bar(i), i == C::Q_FULL || i == C::MEET ? 8 : four ? 4 : 1);
     }
     *abort_word = 0;
     fence_barrier_init();
@@ -332,131 +332,193 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   tc_fence_before();
   launch_dependents();                                              // the joining kernel: its launch lies under this one
   wait_prior_grids();
-  Walk<ROWS> w;
-  long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
   if (threadIdx.x == 0 && p.begun) p.begun[blockIdx.x].w = 0;
-  find_run<ROWS, C::kThreads>(p, w, reinterpret_cast<long long*>(sgen + C::kOffScan), find);
+  const Run run = find_run<ROWS, C::kThreads>(p, reinterpret_cast<long long*>(sgen + C::kOffScan), reinterpret_cast<long long*>(sgen + C::kOffFind));
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars + 4);
   uint32_t* const valid_ring = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
+  Item* const items = reinterpret_cast<Item*>(sgen + C::kOffItems);
   const int log_page = p.cache.log_page, P = 1 << log_page, half_record = p.cache.record / 2;
   const uint32_t all_pages = (1u << (kTile >> log_page)) - 1;
+  // item i of this CTA; none (0 tiles) where some wait ran out
+  auto next_item = [&](int i) -> const Item* {
+    wait(C::ITEM + (i & (kItems - 1)), i / kItems & 1);
+    return items + (i & (kItems - 1));
+  };
+  auto none = [&](const Item* it) { return it->tiles == 0 || *abort_word; };
 
   // Q of an item, by the 256 threads that convert K and V.  Rows are scaled by a power of two into f16's range (the largest element to [2^14,
   // 2^15)): exact for 8-bit significands, and a row's scores are scaled back by its constant.  Rows up to the next 32 are written, since a warp of softmax
   // threads takes all of its 32 or none; few rows are written as often as their copies are (see copies_of).
-  auto bring_q = [&](int& item, int& q_phase) {
-    wait(C::Q_FREE, q_phase);
-    q_phase ^= 1;
+  auto bring_q = [&](const Item* it, int item, int& q_phase) {
     constexpr int kParts = D / 16;                                  // threads of a row
-    const int kvh = w.kvh(), here = min(ROWS, w.d.rows - w.row0), copies = copies_of<ROWS>(here), apart = 128 / copies;
+    const int here = it->here, kvh = it->kvh, copies = it->copies, rows32 = (here + 31) & ~31, e = (threadIdx.x % kParts) * 16;
     const float c = __fdiv_rn(p.scale * 1.4426950408889634f, load(p.cache.k_G + kvh));
     float* const con = reinterpret_cast<float*>(sgen + C::kOffC) + (item & (C::kRingC - 1)) * ROWS;
-    constexpr int kAtOnce = 4;                                      // rows of a thread whose loads are on their way together
-    for (int j0 = threadIdx.x; j0 < ((here + 31) & ~31) * kParts; j0 += 256 * kAtOnce) {
-      uint32_t raw[kAtOnce][8];
-      const int e = (j0 % kParts) * 16;
+    bool waited = false;
+    constexpr int kAtOnce = D == 128 ? 4 : 2, kStep = 256 / kParts; // rows of a thread whose loads are on their way together; how far apart
+#pragma unroll 1
+    for (int r0 = threadIdx.x / kParts; r0 < rows32; r0 += kStep * kAtOnce) {
+      uint4 raw[kAtOnce][2];
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
-        const int r = (j0 + 256 * i) / kParts;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) raw[i][x] = 0u;
+        const int r = r0 + kStep * i;
+        raw[i][0] = raw[i][1] = make_uint4(0u, 0u, 0u, 0u);
         if (r < here) {
           int b, tok, hl;
-          row_token(p, w.d, w.row0 + r, &b, &tok, &hl);
+          row_token(p, *it, r, &b, &tok, &hl);
           const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
           if (p.q_vector) {
-            *reinterpret_cast<uint4*>(raw[i]) = load(reinterpret_cast<const uint4*>(q));
-            *reinterpret_cast<uint4*>(raw[i] + 4) = load(reinterpret_cast<const uint4*>(q) + 1);
+            raw[i][0] = load(reinterpret_cast<const uint4*>(q));
+            raw[i][1] = load(reinterpret_cast<const uint4*>(q) + 1);
           } else {
+            uint32_t* const words = reinterpret_cast<uint32_t*>(raw[i]);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) raw[i][x] = (uint32_t)load(q + 2 * x) | (uint32_t)load(q + 2 * x + 1) << 16;
+            for (int x = 0; x < 8; ++x) words[x] = (uint32_t)load(q + 2 * x) | (uint32_t)load(q + 2 * x + 1) << 16;
           }
         }
       }
+      if (!waited) wait(C::Q_FREE, q_phase);                        // (the first loads are on their way while the buffer is waited for)
+      waited = true;
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
-        const int r = (j0 + 256 * i) / kParts;
-        if (r >= ((here + 31) & ~31)) break;                        // (a warp's rows are a few neighbours: all or none)
-        float v[16], a = 0.f;
+        const int r = r0 + kStep * i;
+        if (r < rows32) {                                           // (a warp's rows are a few neighbours: all or none)
+          const uint32_t words[8] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w, raw[i][1].x, raw[i][1].y, raw[i][1].z, raw[i][1].w};
+          // the largest magnitude, of pairs as they are (bits without their sign are in order in either type; NaN and infinity come out on top)
+          uint32_t a2 = 0u;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const float2 f = p.half ? unpack16<true>(raw[i][x]) : unpack16<false>(raw[i][x]);
-          v[2 * x] = f.x;
-          v[2 * x + 1] = f.y;
-          a = fmaxf(a, fmaxf(fabsf(f.x), fabsf(f.y)));
+          for (int x = 0; x < 8; ++x) a2 = __vmaxu2(a2, words[x] & 0x7FFF7FFFu);
+#pragma unroll
+          for (int x = 1; x < kParts; x <<= 1) a2 = __vmaxu2(a2, __shfl_xor_sync(0xffffffffu, a2, x));
+          const float2 two = p.half ? unpack16<true>(a2) : unpack16<false>(a2);
+          const uint32_t up = row_exponent(finite_max(two.x, two.y));
+          const float f = __uint_as_float(up << 23);
+          uint32_t h[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const float2 v = p.half ? unpack16<true>(words[x]) : unpack16<false>(words[x]);
+            h[x] = pack_pair<__half>(v.x * f, v.y * f);
+          }
+          uint8_t* const panel = sgen + C::kOffQ + (r >> 7) * (128 * D * 2) + (e >> 6) * 16384;
+#pragma unroll 1
+          for (int k = 0; k < copies; ++k) {
+            const int to = (r & 127) + k * (128 / copies);
+            *reinterpret_cast<uint4*>(panel + chunk_at(to, (e & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4*>(panel + chunk_at(to, ((e & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
+          }
+          if (e == 0) con[r] = c * __uint_as_float((254u - up) << 23);
         }
-#pragma unroll
-        for (int x = 1; x < kParts; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
-        const uint32_t up = row_exponent(a);
-        const float f = __uint_as_float(up << 23);
-        uint32_t h[8];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(v[2 * x] * f, v[2 * x + 1] * f);
-        uint8_t* const panel = sgen + C::kOffQ + (r >> 7) * (128 * D * 2) + (e >> 6) * 16384;
-        for (int k = 0; k < copies; ++k) {
-          const int to = (r & 127) + k * apart;
-          *reinterpret_cast<uint4*>(panel + chunk_at(to, (e & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(panel + chunk_at(to, ((e & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
-        }
-        if (e == 0) con[r] = c * __uint_as_float((254u - up) << 23);
       }
     }
+    if (!waited) wait(C::Q_FREE, q_phase);                          // (no rows for this thread: its arrival belongs to this item all the same)
+    q_phase ^= 1;
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(C::Q_FULL));
-    ++item;
   };
 
   if (warp == C::kProducer) {
-    // ===================================================================== pages -> shared memory
+    // ===================================================================== items, and pages -> shared memory
     Turn<C::kStages> ring;
     bool lost = false;
-    int parts = 0;
+    int parts = 0, x = run.x, u = 0, i = 0;
+    long long left = run.tiles, number = run.first, at = run.at;      // number: of the first unit of the run, at: its place in the item
+    Desc d;
+    if (left > 0) {
+      describe<ROWS>(p, x, d);
+      u = (int)mul_div(at, 1, d.nt + kItemCost);
+      at -= (long long)u * (d.nt + kItemCost);
+    }
+    int n = 0;                                                        // items
 #pragma unroll 1
-    for (int i = 0; w.left > 0; ++i) {
-      if (rare(w.fresh)) {
-        // Q of an item into L2, while the tiles before it are worked on
-        const int here = min(ROWS, w.d.rows - w.row0), kvh = w.kvh();
-        for (int r = lane; r < here; r += 32) {
-          int b, tok, hl;
-          row_token(p, w.d, w.row0 + r, &b, &tok, &hl);
-          const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn;
-          asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
-          if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
-        }
+    while (left > 0 && !*abort_word) {
+      // units [at, end) of the item; its tiles are those from unit kItemCost on
+      const int from = (int)at, end = (int)min((long long)(d.nt + kItemCost), at + left), tile = max(0, from - kItemCost);
+      const long long item0 = number - from;
+      left -= end - from;
+      number += end - from;
+      at = 0;
+      const int kvh = u / d.rts, rt = u - kvh * d.rts;
+      Item it;
+      it.tiles = max(0, end - kItemCost - tile);
+      it.first = (d.k0 + tile) * kTile;
+      it.lo = d.lo; it.hi = d.hi; it.ctx = d.ctx; it.b = d.b; it.g = d.g; it.kvh = kvh;
+      it.row0 = d.row0 + rt * ROWS;
+      it.here = min(ROWS, d.rows - it.row0);
+      it.v0 = it.row0 / p.group;
+      it.h0 = it.row0 - it.v0 * p.group;
+      it.two = it.here > 128;
+      it.copies = copies_of<ROWS>(it.here);
+      it.begins = tile == 0;
+      it.whole = it.tiles == d.nt;
+      it.last_cta = cta_of(item0 + kItemCost + d.nt - 1, run.total, run.ctas);
+      it.slot = 2 * (int)blockIdx.x + it.begins;
+      it.split = p.groups ? (long long)split_place<ROWS>(p, d, u) : 0;
+      if (lane == 0 && it.tiles) {
+        items[n & (kItems - 1)] = it;
+        if (!p.groups && it.begins && !it.whole) p.begun[blockIdx.x] = make_int4(x, u, it.last_cta, 1);
+        mbar_arrive(bar(C::ITEM + (n & (kItems - 1))));
       }
-      const int first = w.first_key(), pos = first + lane * P;
-      int page = -1;
-      if (lane < kTile >> log_page && pos < w.d.hi && pos + P > w.d.lo) {
-        if (w.d.g >= 0) {
-          const int id = load(p.prefix_table + (size_t)w.d.g * p.prefix_pages + (pos >> log_page));
-          page = id >= 0 && id < p.cache.num_pages ? id : -1;
-        } else {
-          page = p.cache.page_of(w.d.b, pos);
-        }
-        lost |= page < 0 && pos < w.d.need;
-      }
-      lost |= w.d.need > w.d.hi && w.d.nt - w.tile == 1 && (w.d.g >= 0 ? w.d.need > p.prefix_pages << log_page : w.d.need > p.cache.max_pages << log_page);
-      const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
-      const uint8_t* const rec = page >= 0 ? p.cache.rec(page, w.kvh()) : nullptr;
+      __syncwarp();
+      n += it.tiles > 0;
+      // Q into L2, while the tiles before it are worked on
 #pragma unroll 1
-      for (int part = 0; part < 2; ++part) {
-        wait(C::RING_FREE + ring.at, ring.phase ^ 1);
-        if (lane == 0) {
-          if (part == 0) valid_ring[i % C::kRing] = held;
-          mbar_arrive_expect_tx(bar(C::RING_FULL + ring.at), __popc(held) * half_record);
-        }
-        __syncwarp();
-        if (page >= 0)
-          bulk_load_1d(sbase + C::kOffStage + ring.at * C::kStage + lane * half_record, rec + part * half_record, half_record, bar(C::RING_FULL + ring.at));
-        ring.next();
-        ++parts;
+      for (int r = lane; r < it.here && it.tiles; r += 32) {
+        int b, tok, hl;
+        row_token(p, it, r, &b, &tok, &hl);
+        const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
+        if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
       }
-      w.next(p);
+      const int room = (d.g >= 0 ? p.prefix_pages : p.cache.max_pages) << log_page;
+      lost |= it.tiles && d.need > d.hi && d.need > room;
+      const int* const table = d.g >= 0 ? p.prefix_table + (size_t)d.g * p.prefix_pages : p.cache.table + (size_t)d.b * p.cache.max_pages;
+      const uint8_t* const pages = p.cache.pages + (size_t)kvh * p.cache.record;
+      const size_t page_bytes = (size_t)p.cache.kv_heads * p.cache.record;
+      auto page_at = [&](int first) {                                 // of this lane, -1: none, or not needed
+        const int pos = first + lane * P;
+        if (lane >= kTile >> log_page || pos >= d.hi || pos + P <= d.lo) return -1;
+        const int id = load(table + (pos >> log_page));               // (d.hi is inside the table)
+        if (id >= 0 && id < p.cache.num_pages) return id;
+        lost |= pos < d.need;
+        return -1;
+      };
+      int page = page_at(it.first);
+#pragma unroll 1
+      for (int k = 0; k < it.tiles; ++k) {
+        const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
+        const uint8_t* const rec = pages + (size_t)max(page, 0) * page_bytes;
+        const bool mine = page >= 0;
+        if (k + 1 < it.tiles) page = page_at(it.first + (k + 1) * kTile);            // (its entry comes while a stage is waited for)
+#pragma unroll 1
+        for (int part = 0; part < 2; ++part) {
+          wait(C::RING_FREE + ring.at, ring.phase ^ 1);
+          if (lane == 0) {
+            if (part == 0) valid_ring[i % C::kRing] = held;
+            mbar_arrive_expect_tx(bar(C::RING_FULL + ring.at), __popc(held) * half_record);
+          }
+          __syncwarp();
+          if (mine)
+            bulk_load_1d(sbase + C::kOffStage + ring.at * C::kStage + lane * half_record, rec + part * half_record, half_record, bar(C::RING_FULL + ring.at));
+          ring.next();
+          ++parts;
+        }
+        ++i;
+      }
+      if (left > 0 && ++u == d.rts * p.cache.kv_heads) {
+        u = 0;
+        do describe<ROWS>(p, ++x, d);
+        while (d.nt == 0);                                            // (there is another item: the run goes on)
+      }
+    }
+    if (lane == 0) {
+      items[n & (kItems - 1)].tiles = 0;
+      mbar_arrive(bar(C::ITEM + (n & (kItems - 1))));
     }
     if (__any_sync(0xffffffffu, lost) && lane == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
     // the last copies end before this warp does (also where the others have given up on them)
+#pragma unroll 1
     for (int k = 0; k < C::kStages && k < parts; ++k) {
       ring.at = ring.at ? ring.at - 1 : (ring.phase ^= 1, C::kStages - 1);
       wait(C::RING_FULL + ring.at, ring.phase);
@@ -466,210 +528,228 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     // Jobs: a tile of 128 rows and a tile of keys.  Job j is of softmax group j & 1.  S of a group's next job is issued right behind its O: P stands
     // where S did, and products run in the order of their issue.
     constexpr uint32_t kIdescS = make_idesc_f16(128, kTile, false), kIdescO = make_idesc_f16(128, D, false);
-    Walk<ROWS> ws = w, wo = w;
+    struct Cursor {
+      int item = -1, tiles = 0, half = 0, two = 0, group = 0;         // tiles: left of the item
+      bool fresh = false, done = false;
+    } cs, co;
     Turn<C::kKB> kb;
     Turn<C::kVB> vb;
-    int rs = 0, ro = 0, gs = 0, go = 0, q_phase = 0, jobs_in_item = 0;
-    int p_phase[2] = {0, 0};
-    auto issue_scores = [&] {
-      if (rare(ws.left <= 0)) return;
-      const bool two = ws.two();
-      if (rs == 0) {
-        if (rare(ws.fresh)) {
-          wait(C::Q_FULL, q_phase);
-          q_phase ^= 1;
-        }
-        wait(C::K_FULL + kb.at, kb.phase);
+    int q_phase = 0, jobs_in_item = 0;
+    uint32_t p_phases = 0;
+    auto step = [&](Cursor& c) {                                      // before a job
+      c.fresh = false;
+      if (rare(c.tiles == 0) && !c.done) {
+        const Item* const it = next_item(++c.item);
+        c.done = none(it);
+        c.tiles = it->tiles;
+        c.two = it->two;
+        c.fresh = true;
       }
+    };
+    const uint64_t q_desc = make_smem_desc(sbase + C::kOffQ, 16, 1024, kSwz128), k_desc = make_smem_desc(sbase + C::kOffK, 16, 1024, kSwz128),
+                   v_desc = make_smem_desc(sbase + C::kOffV, 16, 1024, kSwz128);    // (an address is a sum in their low bits)
+    auto issue_scores = [&] {
+      step(cs);
+      if (rare(cs.done)) return;
+      if (rare(cs.fresh)) {
+        wait(C::Q_FULL, q_phase);
+        q_phase ^= 1;
+      }
+      if (cs.half == 0) wait(C::K_FULL + kb.at, kb.phase);
       tc_fence_after();
-      const bool last = !two || rs == 1;
+      const bool last = !cs.two || cs.half == 1;
       if (elect_one()) {
-        const uint32_t a = sbase + C::kOffQ + rs * (128 * D * 2), b = sbase + C::kOffK + kb.at * C::kOp;
+        const uint64_t a = q_desc + (uint32_t)(cs.half * (128 * D * 2) >> 4), b = k_desc + (uint32_t)(kb.at * C::kOp >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t at = (k >> 2) * 16384 + (k & 3) * 32;
-          tc_mma_f16(tmem + C::kS + 128 * gs, make_smem_desc(a + at, 16, 1024, kSwz128), make_smem_desc(b + at, 16, 1024, kSwz128), kIdescS, k > 0);
+          constexpr int kPanel = 16384 >> 4;
+          const int at = (k >> 2) * kPanel + (k & 3) * 2;
+          tc_mma_f16(tmem + C::kS + 128 * cs.group, a + at, b + at, kIdescS, k > 0);
         }
-        tc_commit(bar(C::S_FULL + gs));
+        tc_commit(bar(C::S_FULL + cs.group));
         if (last) tc_commit(bar(C::K_FREE + kb.at));
-        if (last && ws.ends()) tc_commit(bar(C::Q_FREE));
+        if (last && cs.tiles == 1) tc_commit(bar(C::Q_FREE));
       }
       __syncwarp();
-      gs ^= 1;
-      rs ^= 1;
+      cs.group ^= 1;
+      cs.half ^= 1;
       if (last) {
-        rs = 0;
+        cs.half = 0;
         kb.next();
-        ws.next(p);
+        --cs.tiles;
       }
     };
     issue_scores();
     issue_scores();
 #pragma unroll 1
-    while (wo.left > 0) {
-      const bool two = wo.two(), last = !two || ro == 1;
-      if (ro == 0) {
-        if (wo.fresh) jobs_in_item = 0;
-        wait(C::V_FULL + vb.at, vb.phase);
-      }
-      wait(C::P_FULL + go, p_phase[go]);
-      p_phase[go] ^= 1;
+    while (true) {
+      step(co);
+      if (rare(co.done)) break;
+      if (rare(co.fresh)) jobs_in_item = 0;
+      const bool last = !co.two || co.half == 1;
+      if (co.half == 0) wait(C::V_FULL + vb.at, vb.phase);
+      wait(C::P_FULL + co.group, p_phases >> co.group & 1);
+      p_phases ^= 1u << co.group;
       tc_fence_after();
       const uint32_t more = jobs_in_item >= 2;                        // not the item's first of this group
       if (elect_one()) {
-        const uint32_t b = sbase + C::kOffV + vb.at * C::kOp;
+        const uint64_t b = v_desc + (uint32_t)(vb.at * C::kOp >> 4);
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
-          tc_mma_f16_ta(tmem + C::kO + D * go, tmem + C::kS + 128 * go + 8 * k, make_smem_desc(b + (k >> 2) * (D * 128) + (k & 3) * 32, 16, 1024, kSwz128), kIdescO,
-                        k > 0 ? 1u : more);
-        tc_commit(bar(C::PV_DONE + go));
+          tc_mma_f16_ta(tmem + C::kO + D * co.group, tmem + C::kS + 128 * co.group + 8 * k, b + ((k >> 2) * (D * 128 >> 4) + (k & 3) * 2), kIdescO, k > 0 ? 1u : more);
+        tc_commit(bar(C::PV_DONE + co.group));
         if (last) tc_commit(bar(C::V_FREE + vb.at));
       }
       __syncwarp();
       ++jobs_in_item;
-      go ^= 1;
-      ro ^= 1;
+      co.group ^= 1;
+      co.half ^= 1;
       if (last) {
-        ro = 0;
+        co.half = 0;
         vb.next();
-        wo.next(p);
+        --co.tiles;
       }
       issue_scores();
     }
     if (elect_one()) tc_commit(bar(C::DRAIN));
     __syncwarp();
-  } else if (warp < C::kFirstV) {
-    // ===================================================================== K and Q
-    const int key = threadIdx.x, slot = key >> log_page, t = key & (P - 1);
-    Turn<C::kStages> ring;
-    Turn<C::kKB> kb;
-    int item = 0, q_phase = 1;
-#pragma unroll 1
-    while (w.left > 0) {
-      if (rare(w.fresh)) bring_q(item, q_phase);
-      wait(C::K_FREE + kb.at, kb.phase ^ 1);
-      wait(C::RING_FULL + ring.at, ring.phase);
-      {
-        const uint8_t* const rec = sgen + C::kOffStage + ring.at * C::kStage + slot * half_record;
-        const uint8_t* codes = rec + t * 16;
-        uint8_t* const dst = sgen + C::kOffK + kb.at * C::kOp;
-        uint2 sw = make_uint2(0u, 0u);
-        if (L::kFp4 && D == 128) sw = *reinterpret_cast<const uint2*>(rec + P * L::kRow + t * L::kScales);
-        if (L::kFp4 && D == 64) sw.x = *reinterpret_cast<const uint32_t*>(rec + P * L::kRow + t * L::kScales);
-#pragma unroll 2
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t h[16];
-          if (L::kFp4) {
-            const uint4 raw = *reinterpret_cast<const uint4*>(codes);
-            codes += P * 16;
-            const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w}, both = cvt_f16x2_e4m3x2(sw.x & 0xFFFFu);
-            sw.x = __funnelshift_r(sw.x, sw.y, 16);
-            sw.y >>= 16;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const uint32_t f = splat_half(both, x >> 1);
-              cvt_f16x2_e2m1x8(words[x], h + 4 * x);
-#pragma unroll
-              for (int y = 0; y < 4; ++y) h[4 * x + y] = mul_half2(h[4 * x + y], f);
-            }
-          } else {
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const uint4 raw = *reinterpret_cast<const uint4*>(codes);
-              codes += P * 16;
-              const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-              for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(words[x], h + 8 * y + 2 * x);
-            }
-          }
-          uint8_t* const panel = dst + (c >> 1) * 16384;
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<uint4*>(panel + chunk_at(key, 4 * (c & 1) + x)) = make_uint4(h[4 * x], h[4 * x + 1], h[4 * x + 2], h[4 * x + 3]);
-        }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::K_FULL + kb.at));
-      ring.next(2);
-      kb.next();
-      w.next(p);
-    }
   } else if (warp < C::kFirstSoftmax) {
-    // ===================================================================== V
-    // D = 128: a thread an index; D = 64: two threads, half of the tokens each
-    const int tid = threadIdx.x - 32 * C::kFirstV, e = D == 128 ? tid : tid & 63, tok0 = D == 128 ? 0 : tid & 64;
+    // ===================================================================== K, V and Q
+    const bool is_v = warp >= C::kFirstV;
+    // K: a thread a key
+    const int tid = threadIdx.x & 127, key = tid, slot = key >> log_page, t = key & (P - 1);
+    const uint32_t mine = (uint32_t)(slot * half_record + t * 16), my_scales = (uint32_t)(slot * half_record + P * L::kRow + t * L::kScales);
+    // V: D = 128: a thread an index; D = 64: two threads, half of the tokens each
+    const int e = D == 128 ? tid : tid & 63, tok0 = D == 128 ? 0 : tid & 64;
     constexpr int kTokens = D == 128 ? 128 : 64;                      // of a thread
-    uint8_t* const scales = sgen + C::kOffVScale + (warp - C::kFirstV) * 512;
+    uint8_t* const scales = sgen + C::kOffVScale + (warp & 3) * 512;
     const uint32_t shift = 4 * (e & 1);
     // eight tokens whose scales of a block of this warp's indices a lane converts
     const int sc_tok = tok0 + 8 * (lane & (kTokens / 8 - 1)), sc_block = (e & ~31) / 16 + lane / (kTokens / 8);
     const uint32_t scale0 = (uint32_t)((sc_tok >> log_page) * half_record + P * L::kRow + sc_block * P + (sc_tok & (P - 1)));
+    const uint8_t* const factors = scales + ((e >> 4) & 1) * (2 * kTokens);
     Turn<C::kStages> ring;
+    Turn<C::kKB> kb;
     Turn<C::kVB> vb;
-    int item = 0, q_phase = 1;
-    ring.next();
+    int q_phase = 1, done = 0;
+    if (is_v) ring.next();
 #pragma unroll 1
-    for (int i = 0; w.left > 0; ++i) {
-      if (rare(w.fresh)) bring_q(item, q_phase);
-      wait(C::V_FREE + vb.at, vb.phase ^ 1);
-      wait(C::RING_FULL + ring.at, ring.phase);
-      {
-        const int first = w.first_key();
-        // is every byte one that some row sees, hence one that was written?
-        const bool clean = valid_ring[i % C::kRing] == all_pages && !p.ranges && first >= w.d.lo && first + kTile <= (p.groups && w.d.g < 0 ? w.d.ctx : w.d.hi);
-        const uint8_t* const stage = sgen + C::kOffStage + ring.at * C::kStage;
-        uint8_t* const dst = sgen + C::kOffV + vb.at * C::kOp;
-        if (L::kFp4) {
-          if (lane < kTokens / 4) {
-            const uint2 sc = *reinterpret_cast<const uint2*>(stage + scale0);
-            uint32_t f[4];
-            cvt_f16x2_e4m3x4(sc.x, f);
-            cvt_f16x2_e4m3x4(sc.y, f + 2);
-            *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(finite(f[0]), finite(f[1]), finite(f[2]), finite(f[3]));
-          }
-          __syncwarp();
-        }
-        const uint8_t* const factors = scales + ((e >> 4) & 1) * (2 * kTokens);
+    for (int item = 0;; ++item) {
+      const Item* const it = next_item(item);
+      if (none(it)) break;
+      const int tiles = it->tiles, lo = it->lo, clean_end = p.ranges ? 0 : p.groups && it->g < 0 ? min(it->ctx, it->hi) : it->hi;
+      int first = it->first;
+      bring_q(it, item, q_phase);
+      if (!is_v) {
+#pragma unroll 1
+        for (int i = 0; i < tiles; ++i) {
+          wait(C::K_FREE + kb.at, kb.phase ^ 1);
+          wait(C::RING_FULL + ring.at, ring.phase);
+          const uint8_t* const stage = sgen + C::kOffStage + ring.at * C::kStage;
+          const uint8_t* codes = stage + mine;
+          uint8_t* const dst = sgen + C::kOffK + kb.at * C::kOp;
+          uint2 sw = make_uint2(0u, 0u);
+          if (L::kFp4 && D == 128) sw = *reinterpret_cast<const uint2*>(stage + my_scales);
+          if (L::kFp4 && D == 64) sw.x = *reinterpret_cast<const uint32_t*>(stage + my_scales);
 #pragma unroll 2
-        for (int j = 0; j < kTokens; j += 16) {                       // sixteen tokens
-          const int tok = tok0 + j;
-          const uint4 raw = *reinterpret_cast<const uint4*>(stage + (tok >> log_page) * half_record + ((tok & (P - 1)) >> 4) * (16 * L::kRow) + (L::kFp4 ? e >> 1 : e) * 16);
-          const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
-          uint32_t h[8];
-          if (L::kFp4) {
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t h[16];
+            if (L::kFp4) {
+              const uint4 raw = *reinterpret_cast<const uint4*>(codes);
+              codes += P * 16;
+              const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w}, both = cvt_f16x2_e4m3x2(sw.x & 0xFFFFu);
+              sw.x = __funnelshift_r(sw.x, sw.y, 16);
+              sw.y >>= 16;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {                             // eight tokens: i and i + 4 in a byte
-              const uint4 f = *reinterpret_cast<const uint4*>(factors + 2 * j + 16 * x);
-              cvt_f16x2_e2m1x8((cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u), h + 4 * x);
-              h[4 * x] = mul_half2(h[4 * x], f.x);
-              h[4 * x + 1] = mul_half2(h[4 * x + 1], f.y);
-              h[4 * x + 2] = mul_half2(h[4 * x + 2], f.z);
-              h[4 * x + 3] = mul_half2(h[4 * x + 3], f.w);
+              for (int x = 0; x < 4; ++x) {
+                const uint32_t f = splat_half(both, x >> 1);
+                cvt_f16x2_e2m1x8(words[x], h + 4 * x);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) h[4 * x + y] = mul_half2(h[4 * x + y], f);
+              }
+            } else {
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const uint4 raw = *reinterpret_cast<const uint4*>(codes);
+                codes += P * 16;
+                const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(words[x], h + 8 * y + 2 * x);
+              }
             }
-          } else {
+            uint8_t* const panel = dst + (c >> 1) * 16384;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(cw[x], h + 2 * x);
-            if (rare(!clean)) {
-#pragma unroll
-              for (int x = 0; x < 8; ++x) h[x] = finite(h[x]);
-            }
+            for (int x = 0; x < 4; ++x)
+              *reinterpret_cast<uint4*>(panel + chunk_at(key, 4 * (c & 1) + x)) = make_uint4(h[4 * x], h[4 * x + 1], h[4 * x + 2], h[4 * x + 3]);
           }
-          uint8_t* const panel = dst + (tok >> 6) * (D * 128);
-          *reinterpret_cast<uint4*>(panel + chunk_at(e, (tok & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(panel + chunk_at(e, ((tok & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar(C::RING_FREE + ring.at));
+            mbar_arrive(bar(C::K_FULL + kb.at));
+          }
+          ring.next(2);
+          kb.next();
+        }
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < tiles; ++i) {
+          wait(C::V_FREE + vb.at, vb.phase ^ 1);
+          wait(C::RING_FULL + ring.at, ring.phase);
+          // is every byte one that some row sees, hence one that was written?
+          const bool clean = L::kFp4 || (valid_ring[done % C::kRing] == all_pages && first >= lo && first + kTile <= clean_end);
+          const uint8_t* const stage = sgen + C::kOffStage + ring.at * C::kStage;
+          uint8_t* const dst = sgen + C::kOffV + vb.at * C::kOp;
+          if (L::kFp4) {
+            if (lane < kTokens / 4) {
+              const uint2 sc = *reinterpret_cast<const uint2*>(stage + scale0);
+              uint32_t f[4];
+              cvt_f16x2_e4m3x4(sc.x, f);
+              cvt_f16x2_e4m3x4(sc.y, f + 2);
+              *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(finite(f[0]), finite(f[1]), finite(f[2]), finite(f[3]));
+            }
+            __syncwarp();
+          }
+#pragma unroll 2
+          for (int j = 0; j < kTokens; j += 16) {                       // sixteen tokens
+            const int tok = tok0 + j;
+            const uint4 raw = *reinterpret_cast<const uint4*>(stage + (tok >> log_page) * half_record + ((tok & (P - 1)) >> 4) * (16 * L::kRow) + (L::kFp4 ? e >> 1 : e) * 16);
+            const uint32_t cw[4] = {raw.x, raw.y, raw.z, raw.w};
+            uint32_t h[8];
+            if (L::kFp4) {
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {                             // eight tokens: i and i + 4 in a byte
+                const uint4 f = *reinterpret_cast<const uint4*>(factors + 2 * j + 16 * x);
+                cvt_f16x2_e2m1x8((cw[2 * x] >> shift & 0x0F0F0F0Fu) | (cw[2 * x + 1] << (4 - shift) & 0xF0F0F0F0u), h + 4 * x);
+                h[4 * x] = mul_half2(h[4 * x], f.x);
+                h[4 * x + 1] = mul_half2(h[4 * x + 1], f.y);
+                h[4 * x + 2] = mul_half2(h[4 * x + 2], f.z);
+                h[4 * x + 3] = mul_half2(h[4 * x + 3], f.w);
+              }
+            } else {
+#pragma unroll
+              for (int x = 0; x < 4; ++x) cvt_f16x2_e4m3x4(cw[x], h + 2 * x);
+              if (rare(!clean)) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) h[x] = finite(h[x]);
+              }
+            }
+            uint8_t* const panel = dst + (tok >> 6) * (D * 128);
+            *reinterpret_cast<uint4*>(panel + chunk_at(e, (tok & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4*>(panel + chunk_at(e, ((tok & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar(C::RING_FREE + ring.at));
+            mbar_arrive(bar(C::V_FULL + vb.at));
+          }
+          ring.next(2);
+          vb.next();
+          first += kTile;
+          ++done;
         }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::RING_FREE + ring.at));
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::V_FULL + vb.at));
-      ring.next(2);
-      vb.next();
-      w.next(p);
     }
   } else {
     // ===================================================================== softmax
@@ -677,286 +757,330 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_at = tmem + lanes + C::kS + 128 * group, o_at = tmem + lanes + C::kO + D * group;
     float2* const ml = reinterpret_cast<float2*>(sgen + C::kOffML);
-    int par = 0, s_phase = 0, pv_phase = 1, item = 0, part_first = 0;
-    bool have = false, warp_live = false, live = false;               // a job of the item so far; a row of this warp, of this thread
-    int lo = 0, hi = 0, row = 0, ctx = 0, b = 0, t = 0, hl = 0;
-    long long done = 0;                                               // tiles of this CTA's run
-    float m = -INFINITY, l0 = 0.f, l1 = 0.f, con = 0.f, slope = 0.f;
-    int pos = 0, copies = 1, row_in = 0, c_first = 0;                 // this thread's row of the item, its first 32 keys of a tile
-    unsigned long long mask = 0;
-    auto top_of = [&](int from, int end) {                            // largest of the scores of 32-key pieces
-      float top = -INFINITY;
-#pragma unroll 1
-      for (int k = from; k < end; ++k) {
-        uint32_t a[32];
-        tmem_ld_32x32b_x32(s_at + 32 * k, a);
-        tmem_wait_ld();
-        float t2 = __uint_as_float(a[0]);
-#pragma unroll
-        for (int x = 0; x < 32; x += 4) {
-          top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
-          t2 = max3(t2, __uint_as_float(a[x + 2]), __uint_as_float(a[x + 3]));
-        }
-        top = fmaxf(top, t2);
-      }
-      return top;
-    };
     const float cap_in = p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f;
+    int par = 0, s_phase = 0, pv_phase = 1, meet_phase = 0, done = 0; // done: tiles of this CTA's run
+    auto meet = [&] {                                                 // both groups (a barrier whose wait ends, unlike that of the hardware's named ones)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::MEET));
+      wait(C::MEET, meet_phase);
+      meet_phase ^= 1;
+    };
 #pragma unroll 1
-    while (w.left > 0) {
-      const bool two = w.two();
-      if (rare(w.fresh)) {
-        copies = copies_of<ROWS>(min(ROWS, w.d.rows - w.row0));
-        row_in = two ? (group ^ par) * 128 + in_tile : in_tile & (128 / copies - 1);
-        c_first = two ? 0 : in_tile / (128 / copies) * (4 / copies);
-        row = w.row0 + row_in;
-        live = row < w.d.rows;
-        part_first = w.tile;
-        m = -INFINITY;
-        l0 = l1 = 0.f;
-        have = false;
-        lo = hi = 0;
-        mask = 0;
-        ctx = w.d.ctx;
-        if (live) {
-          row_token(p, w.d, row, &b, &t, &hl);
-          if (ANY) {
-            slope = p.slopes ? load(p.slopes + w.kvh() * p.group + hl) * 1.4426950408889634f : 0.f;
-            pos = (int)((unsigned)(w.d.g >= 0 ? w.d.hi + context_of(p, b) : ctx) + (unsigned)t);
-          }
-          if (w.d.g >= 0) {
-            live = t < tokens_of(p, b);
-            hi = w.d.hi;
-          } else if (p.groups) {
-            if (p.mask) {
-              mask = load(p.mask + (size_t)b * p.T + t);
-              if (p.T < 64) mask &= (1ull << p.T) - 1;
-              hi = min(ctx, w.d.hi);
-            } else {
-              hi = min(ctx + t + 1, w.d.hi);
-            }
-          } else {
-            lo = p.first ? max(0, load(p.first + (size_t)b * p.T + t)) : 0;
-            hi = max(0, min(p.last ? load(p.last + (size_t)b * p.T + t) : ctx + t + 1, w.d.hi));
-          }
+    for (int item = 0;; ++item) {
+      const Item* const it = next_item(item);
+      if (none(it)) break;
+      const bool two = it->two;
+      const int copies = it->copies, tiles = it->tiles;
+      // this thread's row of the item, its first 32 keys of a tile
+      const int row_in = two ? (group ^ par) * 128 + in_tile : in_tile & (128 / copies - 1);
+      const int c_first = two ? 0 : in_tile / (128 / copies) * (4 / copies), c_end = c_first + 4 / copies;
+      bool live = row_in < it->here;
+      int b = 0, t = 0, hl = 0, lo = 0, hi = 0;
+      float slope = 0.f;
+      int pos = 0;
+      unsigned long long mask = 0;
+      if (live) {
+        row_token(p, *it, row_in, &b, &t, &hl);
+        const int ctx = it->ctx;
+        if (ANY) {
+          slope = p.slopes ? load(p.slopes + it->kvh * p.group + hl) * 1.4426950408889634f : 0.f;
+          pos = (int)((unsigned)(it->g >= 0 ? it->hi + context_of(p, b) : ctx) + (unsigned)t);
         }
-        warp_live = __any_sync(0xffffffffu, live);
-        if (!live) hi = INT_MAX;                                      // (a row of zeros, or one that is not written: never the reason to look at masks)
-      }
-      if (two || par == group) {
-        wait(C::S_FULL + group, s_phase);
-        s_phase ^= 1;
-        tc_fence_after();
-        if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
-        if (warp_live) {
-          const int first = w.first_key();
-          const uint32_t held = valid_ring[done % C::kRing];
-          const bool plain = __all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + kTile);
-          float top = -INFINITY, c2 = con;
-          const int c_end = c_first + 4 / copies;
-          if (SCORES == kScaled && plain) {
-            top = top_of(c_first, c_end) * con;
-          } else if (CAP && plain) {
-            top = cap_score(top_of(c_first, c_end) * con, cap_in, cap_out);
+        if (it->g >= 0) {
+          live = t < tokens_of(p, b);
+          hi = it->hi;
+        } else if (p.groups) {
+          if (p.mask) {
+            mask = load(p.mask + (size_t)b * p.T + t);
+            if (p.T < 64) mask &= (1ull << p.T) - 1;
+            hi = min(ctx, it->hi);
           } else {
-            // the scores are changed, masked and put back
-            c2 = 1.f;
+            hi = min(ctx + t + 1, it->hi);
+          }
+        } else {
+          lo = p.first ? max(0, load(p.first + (size_t)b * p.T + t)) : 0;
+          hi = max(0, min(p.last ? load(p.last + (size_t)b * p.T + t) : ctx + t + 1, it->hi));
+        }
+      }
+      const bool warp_live = __any_sync(0xffffffffu, live);
+      if (!live) hi = INT_MAX;                                        // (a row of zeros, or one that is not written: never the reason to look at masks)
+      const int mask_at = p.mask && it->g < 0 ? it->ctx : INT_MIN;    // where the drafted tokens begin
+      bool have = false;                                              // a job of the item so far
+      float m = -INFINITY, l0 = 0.f, l1 = 0.f, con = 0.f;
+      int first = it->first;
 #pragma unroll 1
-            for (int k = c_first; k < c_end; ++k) {
-              uint32_t a[32];
-              tmem_ld_32x32b_x32(s_at + 32 * k, a);
-              const int at = first + 32 * k;
-              uint32_t seen = bits_between(lo - at, hi - at);
-              const int o = ctx - at;
-              if (p.mask && w.d.g < 0) seen |= o >= 32 || o <= -64 ? 0u : (uint32_t)(o >= 0 ? mask << o : mask >> -o);
-              seen &= held_bits(held, k, log_page);
-              const float far = (float)(pos - at);
-              tmem_wait_ld();
+      for (int i = 0; i < tiles; ++i) {
+        if (two || par == group) {
+          wait(C::S_FULL + group, s_phase);
+          s_phase ^= 1;
+          tc_fence_after();
+          if (warp_live) {
+            if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
+            const uint32_t held = valid_ring[done % C::kRing];
+            const bool plain = __all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + kTile);
+            float top = -INFINITY, c2 = con;
+            if (!ANY && plain) {
+              // the largest score, 64 keys at a time
+              float t2 = -INFINITY;
+#pragma unroll 1
+              for (int k = c_first; k < c_end; k += 2) {
+                uint32_t a[32], c[32];
+                tmem_ld_32x32b_x32(s_at + 32 * k, a);
+                if (copies < 4) tmem_ld_32x32b_x32(s_at + 32 * k + 32, c);
+                tmem_wait_ld();
 #pragma unroll
-              for (int x = 0; x < 32; ++x) {
-                float y = __uint_as_float(a[x]) * con;
-                if (CAP || (ANY && p.cap > 0.f)) y = cap_score(y, cap_in, cap_out);
-                if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
-                y = seen >> x & 1 ? y : -INFINITY;
-                top = fmaxf(top, y);
-                a[x] = __float_as_uint(y);
+                for (int x = 0; x < 32; x += 4) {
+                  top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
+                  t2 = max3(t2, __uint_as_float(a[x + 2]), __uint_as_float(a[x + 3]));
+                }
+                if (copies < 4) {
+#pragma unroll
+                  for (int x = 0; x < 32; x += 4) {
+                    top = max3(top, __uint_as_float(c[x]), __uint_as_float(c[x + 1]));
+                    t2 = max3(t2, __uint_as_float(c[x + 2]), __uint_as_float(c[x + 3]));
+                  }
+                }
               }
-              tmem_st_32x32b_x16(s_at + 32 * k, a);
-              tmem_st_32x32b_x16(s_at + 32 * k + 16, a + 16);
+              top = fmaxf(top, t2) * con;
+              if (CAP) top = cap_score(top, cap_in, cap_out);
+            } else {
+              // the scores are changed, masked and put back
+              c2 = 1.f;
+              float t2 = -INFINITY;
+#pragma unroll 1
+              for (int k = c_first; k < c_end; ++k) {
+                uint32_t a[32];
+                tmem_ld_32x32b_x32(s_at + 32 * k, a);
+                const int at = first + 32 * k;
+                uint32_t seen = bits_between(lo - at, hi - at);
+                if (mask_at >= 0) {
+                  const int o = mask_at - at;
+                  seen |= o >= 32 || o <= -64 ? 0u : (uint32_t)(o >= 0 ? mask << o : mask >> -o);
+                }
+                seen &= held_bits(held, k, log_page);
+                const float far = (float)(pos - at);
+                tmem_wait_ld();
+#pragma unroll
+                for (int x = 0; x < 32; ++x) {
+                  float y = __uint_as_float(a[x]) * con;
+                  if (CAP || (ANY && p.cap > 0.f)) y = cap_score(y, cap_in, cap_out);
+                  if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
+                  y = seen & 1u << x ? y : -INFINITY;
+                  a[x] = __float_as_uint(y);
+                }
+#pragma unroll
+                for (int x = 0; x < 32; x += 4) {
+                  top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
+                  t2 = max3(t2, __uint_as_float(a[x + 2]), __uint_as_float(a[x + 3]));
+                }
+                tmem_st_32x32b_x16(s_at + 32 * k, a);
+                tmem_st_32x32b_x16(s_at + 32 * k + 16, a + 16);
+              }
+              top = fmaxf(top, t2);
+              tmem_wait_st();
+            }
+            if (rare(__any_sync(0xffffffffu, top > m + kLag || m == -INFINITY))) {
+              // the reference moves: to the largest score seen so far
+              const float old = m;
+              m = fmaxf(m, top);
+              const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
+              l0 *= f;
+              l1 *= f;
+              if (have) {                                             // (S_FULL is behind the group's last product on O)
+#pragma unroll 1
+                for (int k = 0; k < D; k += 32) {
+                  uint32_t o[32];
+                  tmem_ld_32x32b_x32(o_at + k, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                  tmem_st_32x32b_x16(o_at + k, o);
+                  tmem_st_32x32b_x16(o_at + k + 16, o + 16);
+                }
+                tmem_wait_st();
+              }
+            }
+            const float shift = m == -INFINITY ? 0.f : kShift - m;
+            uint32_t a[16], c[16];
+            auto work = [&](uint32_t* raw, int k) {                   // sixteen keys
+              uint32_t h[8];
+#pragma unroll
+              for (int y = 0; y < 16; y += 8) {
+                float z[8];
+#pragma unroll
+                for (int x = 0; x < 8; x += 2) {
+                  if (CAP && plain) {
+                    z[x] = cap_score(__uint_as_float(raw[y + x]) * con, cap_in, cap_out) + shift;
+                    z[x + 1] = cap_score(__uint_as_float(raw[y + x + 1]) * con, cap_in, cap_out) + shift;
+                  } else {
+                    const uint32_t cc = __float_as_uint(c2), ss = __float_as_uint(shift);
+                    fma_pair(z[x], z[x + 1], raw[y + x], raw[y + x + 1], cc, cc, ss, ss);
+                  }
+                  z[x] = exp2_approx(z[x]);
+                  z[x + 1] = exp2_approx(z[x + 1]);
+                  add_pair(l0, l1, z[x], z[x + 1]);
+                }
+                if (L::kFp4) {                                        // the order that V's tokens stand in: 0 4 1 5 2 6 3 7
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[x], z[x + 4]);
+                } else {
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[2 * x], z[2 * x + 1]);
+                }
+              }
+              tmem_st_32x32b_x8(s_at + 8 * k, h);                     // (over scores that have been read)
+            };
+            tmem_ld_32x32b_x16(s_at + 32 * c_first, a);
+#pragma unroll 1
+            for (int k = 2 * c_first; k < 2 * c_end; k += 2) {
+              tmem_wait_ld();
+              tmem_ld_32x32b_x16(s_at + 16 * k + 16, c);
+              work(a, k);
+              tmem_wait_ld();
+              if (k + 2 < 2 * c_end) tmem_ld_32x32b_x16(s_at + 16 * k + 32, a);
+              work(c, k + 1);
+            }
+            if (ROWS <= 128 && copies > 1) {                          // the other copies' keys
+#pragma unroll
+              for (int x = 0; x < 16; ++x) a[x] = 0u;
+#pragma unroll 1
+              for (int k = 0; k < 4; ++k)
+                if (k < c_first || k >= c_end) tmem_st_32x32b_x16(s_at + 16 * k, a);
             }
             tmem_wait_st();
           }
-          if (rare(__any_sync(0xffffffffu, top > m + kLag || m == -INFINITY))) {
-            // the reference moves: to the largest score seen so far
-            const float old = m;
-            m = fmaxf(m, top);
-            const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
-            l0 *= f;
-            l1 *= f;
-            if (have) {                                               // (S_FULL is behind the group's last product on O)
-#pragma unroll 1
-              for (int k = 0; k < D; k += 16) {
-                uint32_t o[16];
-                tmem_ld_32x32b_x16(o_at + k, o);
-                tmem_wait_ld();
-#pragma unroll
-                for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
-                tmem_st_32x32b_x16(o_at + k, o);
-              }
-              tmem_wait_st();
-            }
-          }
-          const float shift = m == -INFINITY ? 0.f : kShift - m;
-          uint32_t a[16], c[16];
-          auto work = [&](uint32_t* raw, int k) {                     // sixteen keys
-            uint32_t h[8];
-#pragma unroll
-            for (int y = 0; y < 16; y += 8) {
-              float z[8];
-#pragma unroll
-              for (int x = 0; x < 8; x += 2) {
-                if (CAP) {
-                  if (plain) {
-                    raw[y + x] = __float_as_uint(cap_score(__uint_as_float(raw[y + x]) * con, cap_in, cap_out));
-                    raw[y + x + 1] = __float_as_uint(cap_score(__uint_as_float(raw[y + x + 1]) * con, cap_in, cap_out));
-                  }
-                  z[x] = __uint_as_float(raw[y + x]) + shift;
-                  z[x + 1] = __uint_as_float(raw[y + x + 1]) + shift;
-                } else {
-                  const uint32_t cc = __float_as_uint(c2), ss = __float_as_uint(shift);
-                  fma_pair(z[x], z[x + 1], raw[y + x], raw[y + x + 1], cc, cc, ss, ss);
-                }
-                z[x] = exp2_approx(z[x]);
-                z[x + 1] = exp2_approx(z[x + 1]);
-                add_pair(l0, l1, z[x], z[x + 1]);
-              }
-              if (L::kFp4) {                                          // the order that V's tokens stand in: 0 4 1 5 2 6 3 7
-#pragma unroll
-                for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[x], z[x + 4]);
-              } else {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[2 * x], z[2 * x + 1]);
-              }
-            }
-            tmem_st_32x32b_x8(s_at + 8 * k, h);                       // (over scores that have been read)
-          };
-          tmem_ld_32x32b_x16(s_at + 32 * c_first, a);
-#pragma unroll 1
-          for (int k = 2 * c_first; k < 2 * c_end; k += 2) {
-            tmem_wait_ld();
-            tmem_ld_32x32b_x16(s_at + 16 * k + 16, c);
-            work(a, k);
-            tmem_wait_ld();
-            if (k + 2 < 2 * c_end) tmem_ld_32x32b_x16(s_at + 16 * k + 32, a);
-            work(c, k + 1);
-          }
-          if (ROWS <= 128 && copies > 1) {                            // the other copies' keys
-#pragma unroll
-            for (int x = 0; x < 16; ++x) a[x] = 0u;
-#pragma unroll 1
-            for (int k = 0; k < 4; ++k)
-              if (k < c_first || k >= c_end) tmem_st_32x32b_x16(s_at + 16 * k, a);
-          }
-          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::P_FULL + group));
+          have = true;
+          pv_phase ^= 1;
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::P_FULL + group));
-        have = true;
-        pv_phase ^= 1;
+        if (!two) par ^= 1;
+        first += kTile;
+        ++done;
       }
-      if (!two) par ^= 1;
-      if (rare(w.ends())) {
-        // ---- end of the item, or of this CTA's part of it
-        const bool whole = part_first == 0 && w.tile + 1 == w.d.nt;
-        const int kvh = w.kvh(), slot = 2 * (int)blockIdx.x + (part_first == 0);
-        if (have) wait(C::PV_DONE + group, pv_phase);
-        float f[2] = {1.f, 1.f}, top = m, sum = l0 + l1;
-        if (!two) {                                                   // both groups, and every copy, have had tiles of these rows
-          ml[group * 128 + in_tile] = make_float2(have ? m : -INFINITY, have ? sum : 0.f);
-          bar_sync(1, 256);
-          // (in one order, so that all have the same bits)
-          top = -INFINITY;
-          for (int k = 0; k < 2 * copies; ++k) top = fmaxf(top, ml[(k & 1) * 128 + row_in + (k >> 1) * (128 / copies)].x);
-          auto weight = [&](float2 x) { return x.x == -INFINITY && x.y == 0.f ? 0.f : x.x == top ? 1.f : exp2_approx(x.x - top); };
-          sum = 0.f;
-          for (int k = 0; k < 2 * copies; ++k) {
-            const float2 x = ml[(k & 1) * 128 + row_in + (k >> 1) * (128 / copies)];
-            const float y = weight(x);
-            sum += y == 0.f ? 0.f : y * x.y;
-          }
-          f[0] = weight(ml[in_tile]);
-          f[1] = weight(ml[128 + in_tile]);
-        } else if (m == -INFINITY && sum == 0.f) {
-          f[group] = 0.f;
+      // ---- end of the item, or of this CTA's part of it
+      const int kvh = it->kvh;
+      const bool whole = it->whole;
+      const float v_G = load(p.cache.v_G + kvh);
+      if (have) wait(C::PV_DONE + group, pv_phase);
+      float f[2] = {1.f, 1.f}, top = m, sum = l0 + l1;
+      if (!two) {                                                     // both groups, and every copy, have had tiles of these rows
+        ml[group * 128 + in_tile] = make_float2(m, sum);
+        meet();
+        // (in one order, so that all have the same bits)
+        float2 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x[k] = k < 2 * copies ? ml[(k & 1) * 128 + row_in + (k >> 1) * (128 / copies)] : make_float2(-INFINITY, 0.f);
+          top = fmaxf(top, x[k].x);
         }
-        tc_fence_after();
-        const bool mine = live && row < w.d.rows, tells = two || (group == 0 && in_tile < 128 / copies);
-        long long at = 0;                                             // of the row among the outputs
-        if (mine) at = ((long long)b * p.H + kvh * p.group + hl) * p.T + t;
-        const bool out = whole && !p.groups;
-        float* dst = nullptr;
+        auto weight = [&](float2 y) { return y.x == -INFINITY && y.y == 0.f ? 0.f : y.x == top ? 1.f : exp2_approx(y.x - top); };
+        sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float y = weight(x[k]);
+          sum += y == 0.f ? 0.f : y * x[k].y;
+        }
+        f[0] = weight(ml[in_tile]);
+        f[1] = weight(ml[128 + in_tile]);
+      } else if (m == -INFINITY && sum == 0.f) {
+        f[group] = 0.f;
+      }
+      tc_fence_after();
+      const bool tells = two || (group == 0 && in_tile < 128 / copies);
+      const long long at = ((long long)b * p.H + kvh * p.group + hl) * p.T + t;          // of the row among the outputs
+      const bool out = whole && !p.groups;
+      char* dst = nullptr;                                            // of the row's elements
+      if (out) {
+        const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum * v_G);                  // nothing seen: 0, not 0 / 0
+        f[0] = f[0] == 0.f ? 0.f : f[0] * inv;
+        f[1] = f[1] == 0.f ? 0.f : f[1] * inv;
+        if (live && p.lse && tells) p.lse[at] = sum == 0.f ? -INFINITY : (top - kShift + log2f(sum)) * 0.6931471805599453f;
+        dst = static_cast<char*>(p.out) + at * (2 * D);
+      } else if (live) {
+        const long long place = whole ? (it->g < 0 ? (long long)p.B * p.H * p.T : 0) + at : (long long)it->slot * ROWS + row_in;
+        dst = reinterpret_cast<char*>((whole ? p.whole : p.part) + place * D);
+        if (tells) (whole ? p.whole_ml : p.part_ml)[place] = make_float2(top, sum);
+      }
+      if (p.groups && it->begins && group == 0 && in_tile == 0) p.split[it->split] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, it->last_cta);
+      __syncwarp();
+      auto write = [&](int e, const float* o) {                       // sixteen elements of a row, 32 bytes a store
         if (out) {
-          const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum * load(p.cache.v_G + kvh));          // nothing seen: 0, not 0 / 0
-          f[0] = f[0] == 0.f ? 0.f : f[0] * inv;
-          f[1] = f[1] == 0.f ? 0.f : f[1] * inv;
-          if (mine && p.lse && tells) p.lse[at] = sum == 0.f ? -INFINITY : (top - kShift + log2f(sum)) * 0.6931471805599453f;
-        } else if (mine) {
-          const bool own = w.d.g < 0;
-          dst = whole ? p.whole + (own ? (long long)p.B * p.H * p.T + at : at) * D : p.part + ((size_t)slot * ROWS + row_in) * D;
-          if (tells) *(whole ? p.whole_ml + (own ? (long long)p.B * p.H * p.T + at : at) : p.part_ml + (size_t)slot * ROWS + row_in) = make_float2(top, sum);
-        }
-        __syncwarp();
-        auto write = [&](int e, const float* o) {                     // sixteen elements of a row
-          if (out) {
-            uint32_t h[8];
+          uint32_t h[8];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) h[x] = p.half ? pack_pair<__half>(o[2 * x], o[2 * x + 1]) : pack_pair<__nv_bfloat16>(o[2 * x], o[2 * x + 1]);
-            uint4* const y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at * D + e);
-            y[0] = make_uint4(h[0], h[1], h[2], h[3]);
-            y[1] = make_uint4(h[4], h[5], h[6], h[7]);
+          for (int x = 0; x < 8; ++x) h[x] = p.half ? pack_pair<__half>(o[2 * x], o[2 * x + 1]) : pack_pair<__nv_bfloat16>(o[2 * x], o[2 * x + 1]);
+          if (p.out_wide) {
+            store_32(dst + 2 * e, h);
           } else {
-#pragma unroll
-            for (int x = 0; x < 16; x += 4) *reinterpret_cast<float4*>(dst + e + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+            reinterpret_cast<uint4*>(dst + 2 * e)[0] = make_uint4(h[0], h[1], h[2], h[3]);
+            reinterpret_cast<uint4*>(dst + 2 * e)[1] = make_uint4(h[4], h[5], h[6], h[7]);
           }
-        };
-        if (ROWS <= 128 && copies > 1) {
-          // The copies' O meet in shared memory, sixteen elements at a time; the group's warps of the first copy take the even or the odd
-          // ones of a row from there.  Rows that do not exist are skipped, but for the barriers.
-          float* const join = reinterpret_cast<float*>(sgen + C::kOffJoin);
-          float* const put = join + ((warp - C::kFirstSoftmax) * 32 + lane) * 16;
+        } else {
+          uint32_t h[16];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) h[x] = __float_as_uint(o[x]);
+          store_32(dst + 4 * e, h);
+          store_32(dst + 4 * e + 32, h + 8);
+        }
+      };
+      if (ROWS <= 128 && copies > 1) {
+        // The copies' O meet in shared memory, as many elements at a time as there is room for of the rows that there are; then a thread takes four
+        // elements of a row and adds them up.
+        float* const join = reinterpret_cast<float*>(sgen + C::kOffJoin);
+        const int here = it->here, most = here <= 4 ? 128 : here <= 8 ? 64 : here <= 16 ? 32 : 16, cols = min(D, most), stride = here > 32 ? 32 : here;
+        // of this warp: [rows of the warp][cols]; row of the warp
+        float* const put = join + ((warp - C::kFirstSoftmax) * stride + lane) * cols;
+        const float g = f[group];
+        char* const o_row = reinterpret_cast<char*>(whole ? (p.groups ? (void*)p.whole : p.out) : (void*)p.part);
+        const long long whole0 = p.groups && it->g < 0 ? (long long)p.B * p.H * p.T : 0;
 #pragma unroll 1
-          for (int e = 0; e < D; e += 16) {
-            if (warp_live) {
+        for (int e0 = 0; e0 < D; e0 += cols) {
+          if (warp_live) {
+#pragma unroll 1
+            for (int e = 0; e < cols; e += 16) {
               uint32_t v[16];
-              tmem_ld_32x32b_x16(o_at + e, v);
+              tmem_ld_32x32b_x16(o_at + e0 + e, v);
               tmem_wait_ld();
-#pragma unroll
-              for (int x = 0; x < 16; x += 4) {
-                const float g = f[group];
-                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (g != 0.f) y = make_float4(__uint_as_float(v[x]) * g, __uint_as_float(v[x + 1]) * g, __uint_as_float(v[x + 2]) * g, __uint_as_float(v[x + 3]) * g);
-                *reinterpret_cast<float4*>(put + (x ^ (lane >> 1 & 3) * 4)) = y;
-              }
-            }
-            bar_sync(1, 256);
-            if (mine && in_tile < 128 / copies && (e >> 4 & 1) == group) {
-              float o[16];
-#pragma unroll
-              for (int x = 0; x < 16; ++x) o[x] = 0.f;
-              for (int k = 0; k < 2 * copies; ++k) {                  // (warp of the copy: of the group k & 1, as many warps on as a copy has)
-                const float* const from = join + (((k & 1) * 4 + (k >> 1) * (4 / copies) + quarter) * 32 + lane) * 16;
+              if (live) {
 #pragma unroll
                 for (int x = 0; x < 16; x += 4) {
-                  const float4 y = *reinterpret_cast<const float4*>(from + (x ^ (lane >> 1 & 3) * 4));
-                  o[x] += y.x; o[x + 1] += y.y; o[x + 2] += y.z; o[x + 3] += y.w;
+                  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                  if (g != 0.f) y = make_float4(__uint_as_float(v[x]) * g, __uint_as_float(v[x + 1]) * g, __uint_as_float(v[x + 2]) * g, __uint_as_float(v[x + 3]) * g);
+                  *reinterpret_cast<float4*>(put + ((e + x) ^ (lane & 3) * 4)) = y;
                 }
               }
-              write(e, o);
+              __syncwarp();
             }
-            bar_sync(1, 256);
           }
-        } else if (warp_live) {
+          tc_fence_before();
+          meet();
+          const int quads = cols / 4;
+#pragma unroll 1
+          for (int j = threadIdx.x - 32 * C::kFirstSoftmax; j < here * quads; j += 256) {
+            const int r = j / quads, c = (j - r * quads) * 4;
+            int rb, rt, rh;
+            row_token(p, *it, r, &rb, &rt, &rh);
+            if (it->g >= 0 && rt >= tokens_of(p, rb)) continue;
+            float o[4] = {0.f, 0.f, 0.f, 0.f};
+            const float* const from = join + ((r >> 5) * stride + (r & 31)) * cols + (c ^ (r & 3) * 4);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {                             // (warp of the copy: of the group k & 1, as many warps on as a copy has)
+              if (k >= 2 * copies) break;
+              const float4 y = *reinterpret_cast<const float4*>(from + ((k & 1) * 4 + (k >> 1) * (4 / copies)) * stride * cols);
+              o[0] += y.x; o[1] += y.y; o[2] += y.z; o[3] += y.w;
+            }
+            const long long row = whole ? whole0 + ((long long)rb * p.H + kvh * p.group + rh) * p.T + rt : (long long)it->slot * ROWS + r;
+            if (out)
+              *reinterpret_cast<uint2*>(o_row + (row * D + e0 + c) * 2) = p.half ? make_uint2(pack_pair<__half>(o[0], o[1]), pack_pair<__half>(o[2], o[3]))
+                                                                                 : make_uint2(pack_pair<__nv_bfloat16>(o[0], o[1]), pack_pair<__nv_bfloat16>(o[2], o[3]));
+            else
+              *reinterpret_cast<float4*>(o_row + (row * D + e0 + c) * 4) = make_float4(o[0], o[1], o[2], o[3]);
+          }
+          meet();
+        }
+      } else {
+        if (warp_live) {
           const int d0 = two ? 0 : group * (D / 2), d1 = two ? D : d0 + D / 2;
 #pragma unroll 1
           for (int e = d0; e < d1; e += 16) {
@@ -976,21 +1100,14 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               for (int x = 0; x < 16; ++x)
                 o[x] = (f[0] == 0.f ? 0.f : __uint_as_float(v[x]) * f[0]) + (f[1] == 0.f ? 0.f : __uint_as_float(v2[x]) * f[1]);
             }
-            if (mine) write(e, o);
+            if (live) write(e, o);
             __syncwarp();
           }
         }
-        if (group == 0 && in_tile == 0) {
-          const int last_cta = cta_of(find[2] + done + (w.d.nt - 1 - w.tile), find[3], find[4]);
-          if (p.groups && part_first == 0) p.split[split_place<ROWS>(p, w.d, w.u)] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, last_cta);
-          if (!p.groups && part_first == 0 && !whole) p.begun[blockIdx.x] = make_int4(w.x, w.u, last_cta, 1);
-        }
         tc_fence_before();
-        if (!two) bar_sync(1, 256);                                   // the next item's products may overwrite either O
-        ++item;
+        if (!two) meet();                                   // the next item's products may overwrite either O
       }
-      ++done;
-      w.next(p);
+      tc_fence_before();
     }
   }
   tc_fence_before();
@@ -1078,11 +1195,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p)
   describe<ROWS>(p, item.x, d);
   const int kvh = item.y, here = min(ROWS, d.rows - d.row0);
   for (int r = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5); r < here; r += gridDim.y * (kJoinThreads / 32)) {
-    int b, t, hl;
-    row_token(p, d, d.row0 + r, &b, &t, &hl);
+    const int t = (d.row0 + r) / p.group, hl = d.row0 + r - t * p.group;
     Sum<D> s;
     s.parts(p, ROWS, first, last, r, lane);
-    s.give(p, ((size_t)b * p.H + (size_t)kvh * p.group + hl) * p.T + t, kvh, lane);
+    s.give(p, ((size_t)d.b * p.H + (size_t)kvh * p.group + hl) * p.T + t, kvh, lane);
   }
 }
 // every row of a batch with shared prefixes: its prefix's part and its own
@@ -1145,7 +1261,7 @@ struct Plan {
   int rt, row_tiles;                       // 128-row halves of an item; items of a sequence's rows
   size_t ml, begun, ranges, split, whole, whole_ml, total;
 };
-size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
+size_t align32(size_t x) { return (x + 31) & ~(size_t)31; }
 Plan plan(int B, int H, int kv_heads, int T, int d, int groups) {
   Plan t;
   const long long rows = (long long)(H / kv_heads) * T;
@@ -1156,10 +1272,10 @@ Plan plan(int B, int H, int kv_heads, int T, int d, int groups) {
   t.ml = slots * d * 4;
   t.begun = t.ml + slots * 8;
   t.ranges = t.begun + kMostCtas * 16;
-  t.split = t.ranges + (groups ? 0 : align16((size_t)B * t.row_tiles * 8));
-  t.whole = t.split + (groups ? align16((size_t)(B * rows / R + groups + 1 + (long long)B * t.row_tiles) * kv_heads * 8) : 0);
+  t.split = t.ranges + (groups ? 0 : align32((size_t)B * t.row_tiles * 8));
+  t.whole = t.split + (groups ? align32((size_t)(B * rows / R + groups + 1 + (long long)B * t.row_tiles) * kv_heads * 8) : 0);
   t.whole_ml = t.whole + (groups ? (size_t)(2 * all) * d * 4 : 0);
-  t.total = t.whole_ml + (groups ? align16((size_t)(2 * all) * 8) : 0);
+  t.total = t.whole_ml + (groups ? align32((size_t)(2 * all) * 8) : 0);
   return t;
 }
 
@@ -1194,6 +1310,10 @@ int launch_rows(const PagedParams& p, cudaStream_t st) {
 int launch(PagedParams& p, const Plan& t, void* workspace, int fmt, int d, cudaStream_t st) {
   char* const ws = (char*)workspace;
   p.row_tiles = t.row_tiles;
+  auto reciprocal = [](int n) { return ((1ull << 36) + n - 1) / n; };
+  p.by_group = reciprocal(p.group);
+  p.by_tokens = reciprocal(p.T);
+  p.out_wide = ((uintptr_t)p.out & 31) == 0;
   p.part = (float*)ws;
   p.part_ml = (float2*)(ws + t.ml);
   if (p.groups) {
@@ -1256,7 +1376,7 @@ extern "C" int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp
   if (rc != FP4ATTN_OK) return rc;
   if (((uintptr_t)first | (uintptr_t)last) & 3) return FP4ATTN_ERR_ALIGNMENT;
   if (!workspace || workspace_bytes < fp4attn_paged_attention_workspace_bytes(B, H, cache->kv_heads, T, cache->d)) return FP4ATTN_ERR_WORKSPACE;
-  if ((uintptr_t)workspace & 15) return FP4ATTN_ERR_ALIGNMENT;
+  if ((uintptr_t)workspace & 31) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   p.first = first; p.last = last;
   return launch(p, plan(B, H, cache->kv_heads, T, cache->d, 0), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
@@ -1279,7 +1399,7 @@ extern "C" int fp4attn_shared_prefix_attention(const fp4attn_view* q, int type, 
   if (groups > 65535 || T > FP4ATTN_MOST_TREE_TOKENS || (long long)prefix_pages * cache->page_size >= (1ll << 30)) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;
   if (((uintptr_t)prefix_table | (uintptr_t)prefix_length | (uintptr_t)group_start) & 3 || ((uintptr_t)tree_mask & 7)) return FP4ATTN_ERR_ALIGNMENT;
   if (!workspace || workspace_bytes < fp4attn_shared_prefix_attention_workspace_bytes(B, H, cache->kv_heads, T, cache->d, groups)) return FP4ATTN_ERR_WORKSPACE;
-  if ((uintptr_t)workspace & 15) return FP4ATTN_ERR_ALIGNMENT;
+  if ((uintptr_t)workspace & 31) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   p.groups = groups; p.prefix_table = prefix_table; p.prefix_pages = prefix_pages; p.prefix_length = prefix_length; p.group_start = group_start;
   p.mask = tree_mask;
