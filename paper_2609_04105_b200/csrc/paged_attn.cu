@@ -105,8 +105,8 @@ struct PagedCfg {
   static constexpr int kOffBar = kOffFind + 64;
   static constexpr int kSmem = kOffBar + 1024 + 1024;
   static_assert(kSmem <= 227 * 1024 && kOffStage % 1024 == 0 && kStage % 16 == 0, "shared memory");
-  enum { K_FULL = 0, K_FREE = K_FULL + kKB, V_FULL = K_FREE + kKB, V_FREE = V_FULL + kVB, Q_FULL = V_FREE + kVB, Q_FREE, S_FULL, P_FULL = S_FULL + 2,
-         PV_DONE = P_FULL + 2, DRAIN = PV_DONE + 2, MEET, RING_FULL, RING_FREE = RING_FULL + kStages, ITEM = RING_FREE + kStages, kBars = ITEM + kItems };
+  enum { K_FULL = 0, K_FREE = K_FULL + kKB, V_FULL = K_FREE + kKB, V_FREE = V_FULL + kVB, Q_FULL = V_FREE + kVB, Q_FREE, S_FULL, P_FULL = S_FULL + 4,
+         PV_DONE = P_FULL + 4, DRAIN = PV_DONE + 4, MEET, RING_FULL, RING_FREE = RING_FULL + kStages, ITEM = RING_FREE + kStages, kBars = ITEM + kItems };
   static_assert(kBars * 8 + 16 <= 1024, "barriers");
   static constexpr int kS = 0, kO = 256;                           // tensor memory: scores (and P) of the two groups, their O
 };
@@ -276,11 +276,6 @@ __device__ __forceinline__ int copies_of(int rows) { return ROWS > 128 || rows >
 __device__ __forceinline__ uint32_t bits_between(int a, int b) {
   const uint32_t from = a <= 0 ? 0xFFFFFFFFu : a >= 32 ? 0u : 0xFFFFFFFFu << a, until = b >= 32 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << b) - 1;
   return from & until;
-}
-// of 32 keys from place `c` x 32 of a tile on, those whose pages are there
-__device__ __forceinline__ uint32_t held_bits(uint32_t held, int c, int log_page) {
-  if (log_page >= 5) return held >> (32 * c >> log_page) & 1 ? 0xFFFFFFFFu : 0u;
-  return (held >> (2 * c) & 1 ? 0xFFFFu : 0u) | (held >> (2 * c + 1) & 1 ? 0xFFFF0000u : 0u);
 }
 __device__ __forceinline__ float rcp_approx(float x) {
   float r;
@@ -525,17 +520,20 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     }
   } else if (warp == C::kIssuer) {
     // ===================================================================== products
-    // Jobs: a tile of 128 rows and a tile of keys.  Job j is of softmax group j & 1.  S of a group's next job is issued right behind its O: P stands
-    // where S did, and products run in the order of their issue.
-    constexpr uint32_t kIdescS = make_idesc_f16(128, kTile, false), kIdescO = make_idesc_f16(128, D, false);
+    // Jobs: 128 rows and 64 keys, of the softmax groups in turn.  A tile has four (both halves of the rows, both of the keys) or, with up to 128 rows,
+    // two (a group has a half of the keys).  A group has two places for its scores, so that those of its next job are there when it comes to them; S of
+    // its job after the next is issued right behind O of this one: P stands where S did, and products run in the order of their issue.
+    constexpr uint32_t kIdescS = make_idesc_f16(128, 64, false), kIdescO = make_idesc_f16(128, D, false);
     struct Cursor {
-      int item = -1, tiles = 0, half = 0, two = 0, group = 0;         // tiles: left of the item
+      int item = -1, tiles = 0, job = 0, two = 0;                     // tiles: left of the item; job: of the tile
+      uint32_t n = 0;                                                 // jobs so far
       bool fresh = false, done = false;
+      __device__ __forceinline__ bool last() const { return job == (two ? 3 : 1); }
+      __device__ __forceinline__ int keys() const { return two ? job >> 1 : job; }       // which half of the tile
     } cs, co;
     Turn<C::kKB> kb;
     Turn<C::kVB> vb;
     int q_phase = 0, jobs_in_item = 0;
-    uint32_t p_phases = 0;
     auto step = [&](Cursor& c) {                                      // before a job
       c.fresh = false;
       if (rare(c.tiles == 0) && !c.done) {
@@ -544,6 +542,15 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         c.tiles = it->tiles;
         c.two = it->two;
         c.fresh = true;
+      }
+    };
+    auto advance = [&](Cursor& c) {
+      ++c.n;
+      if (c.last()) {
+        c.job = 0;
+        --c.tiles;
+      } else {
+        ++c.job;
       }
     };
     const uint64_t q_desc = make_smem_desc(sbase + C::kOffQ, 16, 1024, kSwz128), k_desc = make_smem_desc(sbase + C::kOffK, 16, 1024, kSwz128),
@@ -555,61 +562,52 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         wait(C::Q_FULL, q_phase);
         q_phase ^= 1;
       }
-      if (cs.half == 0) wait(C::K_FULL + kb.at, kb.phase);
+      if (cs.job == 0) wait(C::K_FULL + kb.at, kb.phase);
       tc_fence_after();
-      const bool last = !cs.two || cs.half == 1;
+      const bool last = cs.last();
+      const uint32_t group = cs.n & 1, place = cs.n >> 1 & 1;
       if (elect_one()) {
-        const uint64_t a = q_desc + (uint32_t)(cs.half * (128 * D * 2) >> 4), b = k_desc + (uint32_t)(kb.at * C::kOp >> 4);
+        const uint64_t a = q_desc + (cs.two ? group * (128 * D * 2 >> 4) : 0u), b = k_desc + (uint32_t)(kb.at * C::kOp + cs.keys() * 8192 >> 4);
+        const uint32_t to = tmem + C::kS + 128 * group + 64 * place;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          constexpr int kPanel = 16384 >> 4;
-          const int at = (k >> 2) * kPanel + (k & 3) * 2;
-          tc_mma_f16(tmem + C::kS + 128 * cs.group, a + at, b + at, kIdescS, k > 0);
+          const int at = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
+          tc_mma_f16(to, a + at, b + at, kIdescS, k > 0);
         }
-        tc_commit(bar(C::S_FULL + cs.group));
+        tc_commit(bar(C::S_FULL + 2 * group + place));
         if (last) tc_commit(bar(C::K_FREE + kb.at));
         if (last && cs.tiles == 1) tc_commit(bar(C::Q_FREE));
       }
       __syncwarp();
-      cs.group ^= 1;
-      cs.half ^= 1;
-      if (last) {
-        cs.half = 0;
-        kb.next();
-        --cs.tiles;
-      }
+      if (last) kb.next();
+      advance(cs);
     };
-    issue_scores();
-    issue_scores();
+#pragma unroll 1
+    for (int i = 0; i < 3; ++i) issue_scores();
 #pragma unroll 1
     while (true) {
+      issue_scores();
       step(co);
       if (rare(co.done)) break;
       if (rare(co.fresh)) jobs_in_item = 0;
-      const bool last = !co.two || co.half == 1;
-      if (co.half == 0) wait(C::V_FULL + vb.at, vb.phase);
-      wait(C::P_FULL + co.group, p_phases >> co.group & 1);
-      p_phases ^= 1u << co.group;
+      const bool last = co.last();
+      const uint32_t group = co.n & 1, place = co.n >> 1 & 1;
+      if (co.job == 0) wait(C::V_FULL + vb.at, vb.phase);
+      wait(C::P_FULL + 2 * group + place, co.n >> 2 & 1);
       tc_fence_after();
       const uint32_t more = jobs_in_item >= 2;                        // not the item's first of this group
       if (elect_one()) {
-        const uint64_t b = v_desc + (uint32_t)(vb.at * C::kOp >> 4);
+        const uint64_t b = v_desc + (uint32_t)(vb.at * C::kOp + co.keys() * (D * 128) >> 4);
+        const uint32_t p_at = tmem + C::kS + 128 * group + 64 * place;
 #pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          tc_mma_f16_ta(tmem + C::kO + D * co.group, tmem + C::kS + 128 * co.group + 8 * k, b + ((k >> 2) * (D * 128 >> 4) + (k & 3) * 2), kIdescO, k > 0 ? 1u : more);
-        tc_commit(bar(C::PV_DONE + co.group));
+        for (int k = 0; k < 4; ++k) tc_mma_f16_ta(tmem + C::kO + D * group, p_at + 8 * k, b + 2 * k, kIdescO, k > 0 ? 1u : more);
+        tc_commit(bar(C::PV_DONE + 2 * group + place));
         if (last) tc_commit(bar(C::V_FREE + vb.at));
       }
       __syncwarp();
       ++jobs_in_item;
-      co.group ^= 1;
-      co.half ^= 1;
-      if (last) {
-        co.half = 0;
-        vb.next();
-        --co.tiles;
-      }
-      issue_scores();
+      if (last) vb.next();
+      advance(co);
     }
     if (elect_one()) tc_commit(bar(C::DRAIN));
     __syncwarp();
@@ -758,7 +756,11 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     const uint32_t s_at = tmem + lanes + C::kS + 128 * group, o_at = tmem + lanes + C::kO + D * group;
     float2* const ml = reinterpret_cast<float2*>(sgen + C::kOffML);
     const float cap_in = p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f;
-    int par = 0, s_phase = 0, pv_phase = 1, meet_phase = 0, done = 0; // done: tiles of this CTA's run
+    int meet_phase = 0, done = 0;                                     // done: tiles of this CTA's run
+    uint32_t n = 0;                                                   // jobs of this group
+    // the group's last product on O.  (A barrier for each place: scores of a job say that the product before the last is done, so the last one is the
+    // only one that this wait can be in doubt about.)
+    auto o_done = [&] { wait(C::PV_DONE + 2 * group + (n - 1 & 1), (n - 1) >> 1 & 1); };
     auto meet = [&] {                                                 // both groups (a barrier whose wait ends, unlike that of the hardware's named ones)
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::MEET));
@@ -771,8 +773,8 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       if (none(it)) break;
       const bool two = it->two;
       const int copies = it->copies, tiles = it->tiles;
-      // this thread's row of the item, its first 32 keys of a tile
-      const int row_in = two ? (group ^ par) * 128 + in_tile : in_tile & (128 / copies - 1);
+      // this thread's row of the item; of a job's four times sixteen keys, those of its copy
+      const int row_in = two ? group * 128 + in_tile : in_tile & (128 / copies - 1);
       const int c_first = two ? 0 : in_tile / (128 / copies) * (4 / copies), c_end = c_first + 4 / copies;
       bool live = row_in < it->here;
       int b = 0, t = 0, hl = 0, lo = 0, hi = 0;
@@ -807,163 +809,161 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       const int mask_at = p.mask && it->g < 0 ? it->ctx : INT_MIN;    // where the drafted tokens begin
       bool have = false;                                              // a job of the item so far
       float m = -INFINITY, l0 = 0.f, l1 = 0.f, con = 0.f;
-      int first = it->first;
+      int first = it->first + (two ? 0 : 64 * group);                 // first key of the job
+      const int jobs = two ? 2 * tiles : tiles;
 #pragma unroll 1
-      for (int i = 0; i < tiles; ++i) {
-        if (two || par == group) {
-          wait(C::S_FULL + group, s_phase);
-          s_phase ^= 1;
-          tc_fence_after();
-          if (warp_live) {
-            if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
-            const uint32_t held = valid_ring[done % C::kRing];
-            const bool plain = __all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + kTile);
-            float top = -INFINITY, c2 = con;
-            if (!ANY && plain) {
-              // the largest score, 64 keys at a time
-              float t2 = -INFINITY;
+      for (int i = 0; i < jobs; ++i) {
+        const uint32_t place = n & 1;
+        wait(C::S_FULL + 2 * group + place, n >> 1 & 1);
+        tc_fence_after();
+        if (warp_live) {
+          const uint32_t s_job = s_at + 64 * place, held = valid_ring[done % C::kRing];
+          if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
+          const bool plain = __all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + 64);
+          float top = -INFINITY, t2 = -INFINITY, c2 = con;
+          if (rare(ANY || !plain)) {
+            // the scores are changed, masked and put back
+            c2 = 1.f;
+            const int in_tile0 = two ? 64 * (i & 1) : 64 * group;
 #pragma unroll 1
-              for (int k = c_first; k < c_end; k += 2) {
-                uint32_t a[32], c[32];
-                tmem_ld_32x32b_x32(s_at + 32 * k, a);
-                if (copies < 4) tmem_ld_32x32b_x32(s_at + 32 * k + 32, c);
-                tmem_wait_ld();
-#pragma unroll
-                for (int x = 0; x < 32; x += 4) {
-                  top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
-                  t2 = max3(t2, __uint_as_float(a[x + 2]), __uint_as_float(a[x + 3]));
-                }
-                if (copies < 4) {
-#pragma unroll
-                  for (int x = 0; x < 32; x += 4) {
-                    top = max3(top, __uint_as_float(c[x]), __uint_as_float(c[x + 1]));
-                    t2 = max3(t2, __uint_as_float(c[x + 2]), __uint_as_float(c[x + 3]));
-                  }
-                }
+            for (int k = c_first; k < c_end; ++k) {
+              uint32_t a[16];
+              tmem_ld_32x32b_x16(s_job + 16 * k, a);
+              const int at = first + 16 * k;
+              uint32_t seen = bits_between(lo - at, hi - at);
+              if (mask_at >= 0) {
+                const int o = mask_at - at;
+                seen |= o >= 32 || o <= -64 ? 0u : (uint32_t)(o >= 0 ? mask << o : mask >> -o);
               }
-              top = fmaxf(top, t2) * con;
-              if (CAP) top = cap_score(top, cap_in, cap_out);
-            } else {
-              // the scores are changed, masked and put back
-              c2 = 1.f;
-              float t2 = -INFINITY;
-#pragma unroll 1
-              for (int k = c_first; k < c_end; ++k) {
-                uint32_t a[32];
-                tmem_ld_32x32b_x32(s_at + 32 * k, a);
-                const int at = first + 32 * k;
-                uint32_t seen = bits_between(lo - at, hi - at);
-                if (mask_at >= 0) {
-                  const int o = mask_at - at;
-                  seen |= o >= 32 || o <= -64 ? 0u : (uint32_t)(o >= 0 ? mask << o : mask >> -o);
-                }
-                seen &= held_bits(held, k, log_page);
-                const float far = (float)(pos - at);
-                tmem_wait_ld();
+              seen = held >> ((in_tile0 + 16 * k) >> log_page) & 1 ? seen : 0u;
+              const float far = (float)(pos - at);
+              tmem_wait_ld();
 #pragma unroll
-                for (int x = 0; x < 32; ++x) {
-                  float y = __uint_as_float(a[x]) * con;
-                  if (CAP || (ANY && p.cap > 0.f)) y = cap_score(y, cap_in, cap_out);
-                  if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
-                  y = seen & 1u << x ? y : -INFINITY;
-                  a[x] = __float_as_uint(y);
-                }
-#pragma unroll
-                for (int x = 0; x < 32; x += 4) {
-                  top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
-                  t2 = max3(t2, __uint_as_float(a[x + 2]), __uint_as_float(a[x + 3]));
-                }
-                tmem_st_32x32b_x16(s_at + 32 * k, a);
-                tmem_st_32x32b_x16(s_at + 32 * k + 16, a + 16);
+              for (int x = 0; x < 16; ++x) {
+                float y = __uint_as_float(a[x]) * con;
+                if (CAP || (ANY && p.cap > 0.f)) y = cap_score(y, cap_in, cap_out);
+                if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
+                a[x] = seen & 1u << x ? __float_as_uint(y) : 0xFF800000u;
               }
-              top = fmaxf(top, t2);
-              tmem_wait_st();
+              tmem_st_32x32b_x16(s_job + 16 * k, a);
             }
+            tmem_wait_st();
+          }
+          // the reference moves: to the largest score seen so far
+          auto refer = [&] {
             if (rare(__any_sync(0xffffffffu, top > m + kLag || m == -INFINITY))) {
-              // the reference moves: to the largest score seen so far
               const float old = m;
               m = fmaxf(m, top);
               const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
               l0 *= f;
               l1 *= f;
-              if (have) {                                             // (S_FULL is behind the group's last product on O)
+              if (have) {
+                o_done();
+                tc_fence_after();
 #pragma unroll 1
-                for (int k = 0; k < D; k += 32) {
-                  uint32_t o[32];
-                  tmem_ld_32x32b_x32(o_at + k, o);
+                for (int k = 0; k < D; k += 16) {
+                  uint32_t o[16];
+                  tmem_ld_32x32b_x16(o_at + k, o);
                   tmem_wait_ld();
 #pragma unroll
-                  for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                  for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
                   tmem_st_32x32b_x16(o_at + k, o);
-                  tmem_st_32x32b_x16(o_at + k + 16, o + 16);
                 }
                 tmem_wait_st();
               }
             }
-            const float shift = m == -INFINITY ? 0.f : kShift - m;
-            uint32_t a[16], c[16];
-            auto work = [&](uint32_t* raw, int k) {                   // sixteen keys
-              uint32_t h[8];
+            return m == -INFINITY ? 0.f : kShift - m;
+          };
+          // probabilities of eight keys: four words
+          auto eight = [&](const uint32_t* raw, float shift, uint32_t* h) {
+            float z[8];
 #pragma unroll
-              for (int y = 0; y < 16; y += 8) {
-                float z[8];
-#pragma unroll
-                for (int x = 0; x < 8; x += 2) {
-                  if (CAP && plain) {
-                    z[x] = cap_score(__uint_as_float(raw[y + x]) * con, cap_in, cap_out) + shift;
-                    z[x + 1] = cap_score(__uint_as_float(raw[y + x + 1]) * con, cap_in, cap_out) + shift;
-                  } else {
-                    const uint32_t cc = __float_as_uint(c2), ss = __float_as_uint(shift);
-                    fma_pair(z[x], z[x + 1], raw[y + x], raw[y + x + 1], cc, cc, ss, ss);
-                  }
-                  z[x] = exp2_approx(z[x]);
-                  z[x + 1] = exp2_approx(z[x + 1]);
-                  add_pair(l0, l1, z[x], z[x + 1]);
-                }
-                if (L::kFp4) {                                        // the order that V's tokens stand in: 0 4 1 5 2 6 3 7
-#pragma unroll
-                  for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[x], z[x + 4]);
-                } else {
-#pragma unroll
-                  for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[2 * x], z[2 * x + 1]);
-                }
+            for (int x = 0; x < 8; x += 2) {
+              if (CAP && plain) {
+                z[x] = cap_score(__uint_as_float(raw[x]) * con, cap_in, cap_out) + shift;
+                z[x + 1] = cap_score(__uint_as_float(raw[x + 1]) * con, cap_in, cap_out) + shift;
+              } else {
+                const uint32_t cc = __float_as_uint(c2), ss = __float_as_uint(shift);
+                fma_pair(z[x], z[x + 1], raw[x], raw[x + 1], cc, cc, ss, ss);
               }
-              tmem_st_32x32b_x8(s_at + 8 * k, h);                     // (over scores that have been read)
-            };
-            tmem_ld_32x32b_x16(s_at + 32 * c_first, a);
-#pragma unroll 1
-            for (int k = 2 * c_first; k < 2 * c_end; k += 2) {
-              tmem_wait_ld();
-              tmem_ld_32x32b_x16(s_at + 16 * k + 16, c);
-              work(a, k);
-              tmem_wait_ld();
-              if (k + 2 < 2 * c_end) tmem_ld_32x32b_x16(s_at + 16 * k + 32, a);
-              work(c, k + 1);
+              z[x] = exp2_approx(z[x]);
+              z[x + 1] = exp2_approx(z[x + 1]);
+              add_pair(l0, l1, z[x], z[x + 1]);
             }
-            if (ROWS <= 128 && copies > 1) {                          // the other copies' keys
+            if (L::kFp4) {                                            // the order that V's tokens stand in: 0 4 1 5 2 6 3 7
 #pragma unroll
-              for (int x = 0; x < 16; ++x) a[x] = 0u;
-#pragma unroll 1
-              for (int k = 0; k < 4; ++k)
-                if (k < c_first || k >= c_end) tmem_st_32x32b_x16(s_at + 16 * k, a);
+              for (int x = 0; x < 4; ++x) h[x] = pack_pair<__half>(z[x], z[x + 4]);
+            } else {
+#pragma unroll
+              for (int x = 0; x < 4; ++x) h[x] = pack_pair<__half>(z[2 * x], z[2 * x + 1]);
             }
-            tmem_wait_st();
+          };
+          auto top_of = [&](const uint32_t* raw, int count) {
+#pragma unroll
+            for (int x = 0; x < count; x += 4) {
+              top = max3(top, __uint_as_float(raw[x]), __uint_as_float(raw[x + 1]));
+              t2 = max3(t2, __uint_as_float(raw[x + 2]), __uint_as_float(raw[x + 3]));
+            }
+          };
+          auto scaled_top = [&] {
+            top = fmaxf(top, t2) * c2;
+            if (CAP && plain) top = cap_score(top, cap_in, cap_out);
+          };
+          if (ROWS > 128 || copies == 1) {
+            uint32_t raw[64];
+            tmem_ld_32x32b_x32(s_job, raw);
+            tmem_ld_32x32b_x32(s_job + 32, raw + 32);
+            tmem_wait_ld();
+            top_of(raw, 64);
+            scaled_top();
+            const float shift = refer();
+#pragma unroll
+            for (int x = 0; x < 64; x += 16) {
+              uint32_t h[8];
+              eight(raw + x, shift, h);
+              eight(raw + x + 8, shift, h + 4);
+              tmem_st_32x32b_x8(s_job + x / 2, h);                    // (over scores that have been read)
+            }
+          } else {
+            uint32_t raw[16], h[8];
+#pragma unroll 1
+            for (int k = c_first; k < c_end; ++k) {
+              tmem_ld_32x32b_x16(s_job + 16 * k, raw);
+              tmem_wait_ld();
+              top_of(raw, 16);
+            }
+            scaled_top();
+            const float shift = refer();
+#pragma unroll 1
+            for (int k = c_first; k < c_end; ++k) {
+              tmem_ld_32x32b_x16(s_job + 16 * k, raw);
+              tmem_wait_ld();
+              eight(raw, shift, h);
+              eight(raw + 8, shift, h + 4);
+              tmem_st_32x32b_x8(s_job + 8 * k, h);
+            }
+#pragma unroll
+            for (int x = 0; x < 8; ++x) h[x] = 0u;
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k)                               // the other copies' keys
+              if (k < c_first || k >= c_end) tmem_st_32x32b_x8(s_job + 8 * k, h);
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(C::P_FULL + group));
-          have = true;
-          pv_phase ^= 1;
+          tmem_wait_st();
         }
-        if (!two) par ^= 1;
-        first += kTile;
-        ++done;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::P_FULL + 2 * group + place));
+        have = true;
+        ++n;
+        const bool tile_done = !two || (i & 1);
+        first += two ? 64 : kTile;
+        done += tile_done;
       }
       // ---- end of the item, or of this CTA's part of it
       const int kvh = it->kvh;
       const bool whole = it->whole;
       const float v_G = load(p.cache.v_G + kvh);
-      if (have) wait(C::PV_DONE + group, pv_phase);
+      o_done();
       float f[2] = {1.f, 1.f}, top = m, sum = l0 + l1;
       if (!two) {                                                     // both groups, and every copy, have had tiles of these rows
         ml[group * 128 + in_tile] = make_float2(m, sum);
