@@ -10,7 +10,7 @@
 //   producer   pages of a tile of 128 keys -> a ring of stages, K and V by themselves: one bulk copy a page
 //   K          codes -> f16 (exact) -> shared memory, a key a row; Q of an item, a power of two per row, -> f16 -> shared memory
 //   V          codes -> f16 (exact) -> shared memory, V^T: an index of the head dimension a row
-//   issuer     S of the next tile, O of this one, of two softmax groups in turn
+//   issuers    of S and of O, of two softmax groups in turn
 //   softmax    two groups of 128 threads, a thread a row: scores -> P, f16, over its own scores in tensor memory, where the product reads it
 //
 // Two groups because a tile is one long chain (scores - maximum - exp2 - P - product): while one waits for its products the other has the
@@ -83,7 +83,7 @@ struct PagedCfg {
   using L = RecordLayout<FMT, D>;
   static constexpr int kRows = 128 * RT;                           // of an item
   // warps
-  static constexpr int kFirstV = 4, kFirstSoftmax = 8, kProducer = 16, kIssuer = 17, kThreads = 32 * 18;
+  static constexpr int kFirstV = 4, kFirstSoftmax = 8, kProducer = 16, kIssuerS = 17, kIssuerO = 18, kThreads = 32 * 19;
   static constexpr int kStage = kTile * L::kToken;                 // K or V of a tile
   static constexpr int kQ = kRows * D * 2, kOp = kTile * D * 2;    // an operand tile
   static constexpr int kKB = 2, kVB = RT == 2 && D == 128 && !L::kFp4 ? 1 : 2;
@@ -106,7 +106,7 @@ struct PagedCfg {
   static constexpr int kSmem = kOffBar + 1024 + 1024;
   static_assert(kSmem <= 227 * 1024 && kOffStage % 1024 == 0 && kStage % 16 == 0, "shared memory");
   enum { K_FULL = 0, K_FREE = K_FULL + kKB, V_FULL = K_FREE + kKB, V_FREE = V_FULL + kVB, Q_FULL = V_FREE + kVB, Q_FREE, S_FULL, P_FULL = S_FULL + 4,
-         PV_DONE = P_FULL + 4, DRAIN = PV_DONE + 4, MEET, RING_FULL, RING_FREE = RING_FULL + kStages, ITEM = RING_FREE + kStages, kBars = ITEM + kItems };
+         PV_DONE = P_FULL + 4, DRAIN = PV_DONE + 4, MEET = DRAIN + 2, RING_FULL, RING_FREE = RING_FULL + kStages, ITEM = RING_FREE + kStages, kBars = ITEM + kItems };
   static_assert(kBars * 8 + 16 <= 1024, "barriers");
   static constexpr int kS = 0, kO = 256;                           // tensor memory: scores (and P) of the two groups, their O
 };
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     *abort_word = 0;
     fence_barrier_init();
   }
-  if (warp == C::kIssuer) { tmem_alloc(tslot, 512); tmem_relinquish(); }
+  if (warp == C::kIssuerS) { tmem_alloc(tslot, 512); tmem_relinquish(); }
   tc_fence_before();
   launch_dependents();                                              // the joining kernel: its launch lies under this one
   wait_prior_grids();
@@ -518,98 +518,92 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       ring.at = ring.at ? ring.at - 1 : (ring.phase ^= 1, C::kStages - 1);
       wait(C::RING_FULL + ring.at, ring.phase);
     }
-  } else if (warp == C::kIssuer) {
+  } else if (warp == C::kIssuerS || warp == C::kIssuerO) {
     // ===================================================================== products
     // Jobs: 128 rows and 64 keys, of the softmax groups in turn.  A tile has four (both halves of the rows, both of the keys) or, with up to 128 rows,
-    // two (a group has a half of the keys).  A group has two places for its scores, so that those of its next job are there when it comes to them; S of
-    // its job after the next is issued right behind O of this one: P stands where S did, and products run in the order of their issue.
-    constexpr uint32_t kIdescS = make_idesc_f16(128, 64, false), kIdescO = make_idesc_f16(128, D, false);
-    struct Cursor {
-      int item = -1, tiles = 0, job = 0, two = 0;                     // tiles: left of the item; job: of the tile
-      uint32_t n = 0;                                                 // jobs so far
-      bool fresh = false, done = false;
-      __device__ __forceinline__ bool last() const { return job == (two ? 3 : 1); }
-      __device__ __forceinline__ int keys() const { return two ? job >> 1 : job; }       // which half of the tile
-    } cs, co;
-    Turn<C::kKB> kb;
-    Turn<C::kVB> vb;
-    int q_phase = 0, jobs_in_item = 0;
-    auto step = [&](Cursor& c) {                                      // before a job
-      c.fresh = false;
-      if (rare(c.tiles == 0) && !c.done) {
-        const Item* const it = next_item(++c.item);
-        c.done = none(it);
-        c.tiles = it->tiles;
-        c.two = it->two;
-        c.fresh = true;
+    // two (a group has a half of the keys).  A group has two places for its scores, so that those of its next job are there when it comes to them; P
+    // stands where S did.  A warp each for S and O: what an issuer executes besides products is one chain of instructions, which shares its scheduler with five
+    // other warps; in one warp it took twice the time of the products.
+    int item = -1, tiles = 0, two = 0, in_item = 0;                   // tiles: left of the item; in_item: jobs of the item so far
+    int job = 0;                                                      // of the tile
+    uint32_t n = 0;                                                   // jobs so far
+    auto another = [&] {                                              // before a job: is there one?
+      if (rare(tiles == 0)) {
+        const Item* const it = next_item(++item);
+        if (none(it)) return false;
+        tiles = it->tiles;
+        two = it->two;
+        in_item = 0;
+      }
+      return true;
+    };
+    auto next = [&](bool last) {
+      ++n;
+      ++in_item;
+      ++job;
+      if (last) {
+        job = 0;
+        --tiles;
       }
     };
-    auto advance = [&](Cursor& c) {
-      ++c.n;
-      if (c.last()) {
-        c.job = 0;
-        --c.tiles;
-      } else {
-        ++c.job;
-      }
-    };
-    const uint64_t q_desc = make_smem_desc(sbase + C::kOffQ, 16, 1024, kSwz128), k_desc = make_smem_desc(sbase + C::kOffK, 16, 1024, kSwz128),
-                   v_desc = make_smem_desc(sbase + C::kOffV, 16, 1024, kSwz128);    // (an address is a sum in their low bits)
-    auto issue_scores = [&] {
-      step(cs);
-      if (rare(cs.done)) return;
-      if (rare(cs.fresh)) {
-        wait(C::Q_FULL, q_phase);
-        q_phase ^= 1;
-      }
-      if (cs.job == 0) wait(C::K_FULL + kb.at, kb.phase);
-      tc_fence_after();
-      const bool last = cs.last();
-      const uint32_t group = cs.n & 1, place = cs.n >> 1 & 1;
-      if (elect_one()) {
-        const uint64_t a = q_desc + (cs.two ? group * (128 * D * 2 >> 4) : 0u), b = k_desc + (uint32_t)(kb.at * C::kOp + cs.keys() * 8192 >> 4);
-        const uint32_t to = tmem + C::kS + 128 * group + 64 * place;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const int at = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
-          tc_mma_f16(to, a + at, b + at, kIdescS, k > 0);
+    if (warp == C::kIssuerS) {
+      constexpr uint32_t kIdesc = make_idesc_f16(128, 64, false);
+      const uint64_t q_desc = make_smem_desc(sbase + C::kOffQ, 16, 1024, kSwz128), k_desc = make_smem_desc(sbase + C::kOffK, 16, 1024, kSwz128);
+      Turn<C::kKB> kb;
+      int q_phase = 0;
+#pragma unroll 1
+      while (another()) {
+        const bool last = job == (two ? 3 : 1);
+        const uint32_t group = n & 1, place = n >> 1 & 1;
+        if (rare(in_item == 0)) {
+          wait(C::Q_FULL, q_phase);
+          q_phase ^= 1;
         }
-        tc_commit(bar(C::S_FULL + 2 * group + place));
-        if (last) tc_commit(bar(C::K_FREE + kb.at));
-        if (last && cs.tiles == 1) tc_commit(bar(C::Q_FREE));
-      }
-      __syncwarp();
-      if (last) kb.next();
-      advance(cs);
-    };
-#pragma unroll 1
-    for (int i = 0; i < 3; ++i) issue_scores();
-#pragma unroll 1
-    while (true) {
-      issue_scores();
-      step(co);
-      if (rare(co.done)) break;
-      if (rare(co.fresh)) jobs_in_item = 0;
-      const bool last = co.last();
-      const uint32_t group = co.n & 1, place = co.n >> 1 & 1;
-      if (co.job == 0) wait(C::V_FULL + vb.at, vb.phase);
-      wait(C::P_FULL + 2 * group + place, co.n >> 2 & 1);
-      tc_fence_after();
-      const uint32_t more = jobs_in_item >= 2;                        // not the item's first of this group
-      if (elect_one()) {
-        const uint64_t b = v_desc + (uint32_t)(vb.at * C::kOp + co.keys() * (D * 128) >> 4);
-        const uint32_t p_at = tmem + C::kS + 128 * group + 64 * place;
+        if (job == 0) wait(C::K_FULL + kb.at, kb.phase);
+        wait(C::PV_DONE + 2 * group + place, (n >> 2 & 1) ^ 1);       // what stood in this place has been read
+        tc_fence_after();
+        // (an address is a sum in a descriptor's low bits)
+        const uint64_t a = q_desc + (two ? group * (128 * D * 2 >> 4) : 0u), b = k_desc + (uint32_t)(kb.at * C::kOp + (two ? job >> 1 : job) * 8192 >> 4);
+        const uint32_t to = tmem + C::kS + 128 * group + 64 * place;
+        if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tc_mma_f16_ta(tmem + C::kO + D * group, p_at + 8 * k, b + 2 * k, kIdescO, k > 0 ? 1u : more);
-        tc_commit(bar(C::PV_DONE + 2 * group + place));
-        if (last) tc_commit(bar(C::V_FREE + vb.at));
+          for (int k = 0; k < D / 16; ++k) {
+            const int at = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
+            tc_mma_f16(to, a + at, b + at, kIdesc, k > 0);
+          }
+          tc_commit(bar(C::S_FULL + 2 * group + place));
+          if (last) tc_commit(bar(C::K_FREE + kb.at));
+          if (last && tiles == 1) tc_commit(bar(C::Q_FREE));
+        }
+        __syncwarp();
+        if (last) kb.next();
+        next(last);
       }
-      __syncwarp();
-      ++jobs_in_item;
-      if (last) vb.next();
-      advance(co);
+    } else {
+      constexpr uint32_t kIdesc = make_idesc_f16(128, D, false);
+      const uint64_t v_desc = make_smem_desc(sbase + C::kOffV, 16, 1024, kSwz128);
+      Turn<C::kVB> vb;
+#pragma unroll 1
+      while (another()) {
+        const bool last = job == (two ? 3 : 1);
+        const uint32_t group = n & 1, place = n >> 1 & 1;
+        if (job == 0) wait(C::V_FULL + vb.at, vb.phase);
+        const uint64_t b = v_desc + (uint32_t)(vb.at * C::kOp + (two ? job >> 1 : job) * (D * 128) >> 4);
+        const uint32_t p_at = tmem + C::kS + 128 * group + 64 * place, more = in_item >= 2;         // not the item's first of this group
+        wait(C::P_FULL + 2 * group + place, n >> 2 & 1);
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tc_mma_f16_ta(tmem + C::kO + D * group, p_at + 8 * k, b + 2 * k, kIdesc, k > 0 ? 1u : more);
+          tc_commit(bar(C::PV_DONE + 2 * group + place));
+          if (last) tc_commit(bar(C::V_FREE + vb.at));
+        }
+        __syncwarp();
+        if (last) vb.next();
+        next(last);
+      }
     }
-    if (elect_one()) tc_commit(bar(C::DRAIN));
+    if (elect_one()) tc_commit(bar(C::DRAIN + (warp == C::kIssuerO)));
     __syncwarp();
   } else if (warp < C::kFirstSoftmax) {
     // ===================================================================== K, V and Q
@@ -1113,9 +1107,10 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   tc_fence_before();
   __syncthreads();
   if (*abort_word && threadIdx.x == 0 && p.status) *p.status = FP4ATTN_ERR_TIMEOUT;
-  if (warp == C::kIssuer) {
+  if (warp == C::kIssuerS) {
     if (*abort_word && lane == 0)                                   // given up: the products in flight end before tensor memory does
-      for (int spin = 0; spin < (1 << 14) && !mbar_try_wait(bar(C::DRAIN), 0); ++spin) {}
+      for (int k = 0; k < 2; ++k)
+        for (int spin = 0; spin < (1 << 14) && !mbar_try_wait(bar(C::DRAIN + k), 0); ++spin) {}
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, 512);
