@@ -814,38 +814,48 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
           const uint32_t s_job = s_at + 64 * place, held = valid_ring[done % C::kRing];
           if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
           const bool plain = __all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + 64);
-          float top = -INFINITY, t2 = -INFINITY, c2 = con;
-          if (rare(ANY || !plain)) {
-            // the scores are changed, masked and put back
-            c2 = 1.f;
+          const bool change = ANY || !plain;
+          const float c2 = change ? 1.f : con;
+          // The reference moves to the largest score seen so far, which is looked for first: changed and masked scores are put back where they were.
+          auto refer = [&] {
+            float top = -INFINITY;
             const int in_tile0 = two ? 64 * (i & 1) : 64 * group;
 #pragma unroll 1
             for (int k = c_first; k < c_end; ++k) {
               uint32_t a[16];
               tmem_ld_32x32b_x16(s_job + 16 * k, a);
-              const int at = first + 16 * k;
-              uint32_t seen = bits_between(lo - at, hi - at);
-              if (mask_at >= 0) {
-                const int o = mask_at - at;
-                seen |= o >= 32 || o <= -64 ? 0u : (uint32_t)(o >= 0 ? mask << o : mask >> -o);
-              }
-              seen = held >> ((in_tile0 + 16 * k) >> log_page) & 1 ? seen : 0u;
-              const float far = (float)(pos - at);
-              tmem_wait_ld();
+              if (change) {
+                const int at = first + 16 * k;
+                uint32_t seen = bits_between(lo - at, hi - at);
+                if (mask_at >= 0) {
+                  const int o = mask_at - at;
+                  seen |= o >= 32 || o <= -64 ? 0u : (uint32_t)(o >= 0 ? mask << o : mask >> -o);
+                }
+                seen = held >> ((in_tile0 + 16 * k) >> log_page) & 1 ? seen : 0u;
+                const float far = (float)(pos - at);
+                tmem_wait_ld();
 #pragma unroll
-              for (int x = 0; x < 16; ++x) {
-                float y = __uint_as_float(a[x]) * con;
-                if (CAP || (ANY && p.cap > 0.f)) y = cap_score(y, cap_in, cap_out);
-                if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
-                a[x] = seen & 1u << x ? __float_as_uint(y) : 0xFF800000u;
+                for (int x = 0; x < 16; ++x) {
+                  float y = __uint_as_float(a[x]) * con;
+                  if (CAP || (ANY && p.cap > 0.f)) y = cap_score(y, cap_in, cap_out);
+                  if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
+                  a[x] = seen & 1u << x ? __float_as_uint(y) : 0xFF800000u;
+                }
+                tmem_st_32x32b_x16(s_job + 16 * k, a);
               }
-              tmem_st_32x32b_x16(s_job + 16 * k, a);
+              tmem_wait_ld();
+              float t2 = -INFINITY;
+#pragma unroll
+              for (int x = 0; x < 16; x += 4) {
+                top = max3(top, __uint_as_float(a[x]), __uint_as_float(a[x + 1]));
+                t2 = max3(t2, __uint_as_float(a[x + 2]), __uint_as_float(a[x + 3]));
+              }
+              top = fmaxf(top, t2);
             }
-            tmem_wait_st();
-          }
-          // the reference moves: to the largest score seen so far
-          auto refer = [&] {
-            if (rare(__any_sync(0xffffffffu, top > m + kLag || m == -INFINITY))) {
+            top *= c2;
+            if (CAP && plain) top = cap_score(top, cap_in, cap_out);
+            if (change) tmem_wait_st();
+            if (__any_sync(0xffffffffu, top > m + kLag || m == -INFINITY)) {
               const float old = m;
               m = fmaxf(m, top);
               const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
@@ -866,82 +876,96 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
                 tmem_wait_st();
               }
             }
-            return m == -INFINITY ? 0.f : kShift - m;
           };
-          // probabilities of eight keys: four words
-          auto eight = [&](const uint32_t* raw, float shift, uint32_t* h) {
-            float z[8];
+          // probabilities of sixteen keys: eight words; the largest score above the reference (+ kShift), the sum
+          float over, s0, s1, shift;
+          auto sixteen = [&](const uint32_t* raw, uint32_t* h) {
 #pragma unroll
-            for (int x = 0; x < 8; x += 2) {
-              if (CAP && plain) {
-                z[x] = cap_score(__uint_as_float(raw[x]) * con, cap_in, cap_out) + shift;
-                z[x + 1] = cap_score(__uint_as_float(raw[x + 1]) * con, cap_in, cap_out) + shift;
-              } else {
-                const uint32_t cc = __float_as_uint(c2), ss = __float_as_uint(shift);
-                fma_pair(z[x], z[x + 1], raw[x], raw[x + 1], cc, cc, ss, ss);
+            for (int y = 0; y < 16; y += 8) {
+              float z[8];
+#pragma unroll
+              for (int x = 0; x < 8; x += 2) {
+                if (CAP && plain) {
+                  z[x] = cap_score(__uint_as_float(raw[y + x]) * con, cap_in, cap_out) + shift;
+                  z[x + 1] = cap_score(__uint_as_float(raw[y + x + 1]) * con, cap_in, cap_out) + shift;
+                } else {
+                  const uint32_t cc = __float_as_uint(c2), ss = __float_as_uint(shift);
+                  fma_pair(z[x], z[x + 1], raw[y + x], raw[y + x + 1], cc, cc, ss, ss);
+                }
+                over = max3(over, z[x], z[x + 1]);
+                z[x] = exp2_approx(z[x]);
+                z[x + 1] = exp2_approx(z[x + 1]);
+                add_pair(s0, s1, z[x], z[x + 1]);
               }
-              z[x] = exp2_approx(z[x]);
-              z[x + 1] = exp2_approx(z[x + 1]);
-              add_pair(l0, l1, z[x], z[x + 1]);
-            }
-            if (L::kFp4) {                                            // the order that V's tokens stand in: 0 4 1 5 2 6 3 7
+              if (L::kFp4) {                                          // the order that V's tokens stand in: 0 4 1 5 2 6 3 7
 #pragma unroll
-              for (int x = 0; x < 4; ++x) h[x] = pack_pair<__half>(z[x], z[x + 4]);
-            } else {
+                for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[x], z[x + 4]);
+              } else {
 #pragma unroll
-              for (int x = 0; x < 4; ++x) h[x] = pack_pair<__half>(z[2 * x], z[2 * x + 1]);
+                for (int x = 0; x < 4; ++x) h[y / 2 + x] = pack_pair<__half>(z[2 * x], z[2 * x + 1]);
+              }
             }
           };
-          auto top_of = [&](const uint32_t* raw, int count) {
-#pragma unroll
-            for (int x = 0; x < count; x += 4) {
-              top = max3(top, __uint_as_float(raw[x]), __uint_as_float(raw[x + 1]));
-              t2 = max3(t2, __uint_as_float(raw[x + 2]), __uint_as_float(raw[x + 3]));
-            }
-          };
-          auto scaled_top = [&] {
-            top = fmaxf(top, t2) * c2;
-            if (CAP && plain) top = cap_score(top, cap_in, cap_out);
-          };
+          // Scores rarely exceed their reference: it is looked for first where there is none yet or scores change, and in all other jobs only
+          // when they have turned out to; then the job is done again.
+          bool sure = change || __any_sync(0xffffffffu, m == -INFINITY);
           if (ROWS > 128 || copies == 1) {
-            uint32_t raw[64];
-            tmem_ld_32x32b_x32(s_job, raw);
-            tmem_ld_32x32b_x32(s_job + 32, raw + 32);
-            tmem_wait_ld();
-            top_of(raw, 64);
-            scaled_top();
-            const float shift = refer();
-#pragma unroll
-            for (int x = 0; x < 64; x += 16) {
-              uint32_t h[8];
-              eight(raw + x, shift, h);
-              eight(raw + x + 8, shift, h + 4);
-              tmem_st_32x32b_x8(s_job + x / 2, h);                    // (over scores that have been read)
+            uint32_t h[32];
+#pragma unroll 1
+            while (true) {
+              if (rare(sure)) refer();
+              shift = m == -INFINITY ? 0.f : kShift - m;
+              over = -INFINITY;
+              s0 = s1 = 0.f;
+              uint32_t a[16], c[16];
+              tmem_ld_32x32b_x16(s_job, a);
+              tmem_wait_ld();
+              tmem_ld_32x32b_x16(s_job + 16, c);
+              sixteen(a, h);
+              tmem_wait_ld();
+              tmem_ld_32x32b_x16(s_job + 32, a);
+              sixteen(c, h + 8);
+              tmem_wait_ld();
+              tmem_ld_32x32b_x16(s_job + 48, c);
+              sixteen(a, h + 16);
+              tmem_wait_ld();
+              sixteen(c, h + 24);
+              if (sure || !rare(__any_sync(0xffffffffu, over > kLag + kShift))) break;
+              sure = true;
             }
+            tmem_st_32x32b_x16(s_job, h);                             // (over scores that have been read)
+            tmem_st_32x32b_x16(s_job + 16, h + 16);
           } else {
-            uint32_t raw[16], h[8];
+            // (two pieces at most: what the one before the last has to store waits)
+            uint32_t h[16];
 #pragma unroll 1
-            for (int k = c_first; k < c_end; ++k) {
-              tmem_ld_32x32b_x16(s_job + 16 * k, raw);
+            while (true) {
+              if (rare(sure)) refer();
+              shift = m == -INFINITY ? 0.f : kShift - m;
+              over = -INFINITY;
+              s0 = s1 = 0.f;
+              uint32_t a[16];
+              tmem_ld_32x32b_x16(s_job + 16 * c_first, a);
               tmem_wait_ld();
-              top_of(raw, 16);
+              sixteen(a, h);
+              if (copies == 2) {
+                tmem_ld_32x32b_x16(s_job + 16 * c_first + 16, a);
+                tmem_wait_ld();
+                sixteen(a, h + 8);
+              }
+              if (sure || !rare(__any_sync(0xffffffffu, over > kLag + kShift))) break;
+              sure = true;
             }
-            scaled_top();
-            const float shift = refer();
-#pragma unroll 1
-            for (int k = c_first; k < c_end; ++k) {
-              tmem_ld_32x32b_x16(s_job + 16 * k, raw);
-              tmem_wait_ld();
-              eight(raw, shift, h);
-              eight(raw + 8, shift, h + 4);
-              tmem_st_32x32b_x8(s_job + 8 * k, h);
-            }
+            tmem_st_32x32b_x8(s_job + 8 * c_first, h);
+            if (copies == 2) tmem_st_32x32b_x8(s_job + 8 * c_first + 8, h + 8);
 #pragma unroll
             for (int x = 0; x < 8; ++x) h[x] = 0u;
 #pragma unroll 1
             for (int k = 0; k < 4; ++k)                               // the other copies' keys
               if (k < c_first || k >= c_end) tmem_st_32x32b_x8(s_job + 8 * k, h);
           }
+          l0 += s0;
+          l1 += s1;
           tmem_wait_st();
         }
         tc_fence_before();
