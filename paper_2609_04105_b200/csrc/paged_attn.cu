@@ -345,69 +345,80 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   // Q of an item, by the 256 threads that convert K and V.  Rows are scaled by a power of two into f16's range (the largest element to [2^14,
   // 2^15)): exact for 8-bit significands, and a row's scores are scaled back by its constant.  Rows up to the next 32 are written, since a warp of softmax
   // threads takes all of its 32 or none; few rows are written as often as their copies are (see copies_of).
+  // All of an item's rows are in these threads' registers, converted, before the buffer is free: then only stores stand between the last scores of an item
+  // and the first of the next.
   auto bring_q = [&](const Item* it, int item, int& q_phase) {
-    constexpr int kParts = D / 16;                                  // threads of a row
-    const int here = it->here, kvh = it->kvh, copies = it->copies, rows32 = (here + 31) & ~31, e = (threadIdx.x % kParts) * 16;
+    constexpr int kParts = D / 16, kStep = 256 / kParts, kMost = ROWS / kStep;       // threads of a row; how far apart a thread's rows are; how many
+    const int here = it->here, kvh = it->kvh, copies = it->copies, rows32 = (here + 31) & ~31, e = (threadIdx.x % kParts) * 16, r0 = threadIdx.x / kParts;
     const float c = __fdiv_rn(p.scale * 1.4426950408889634f, load(p.cache.k_G + kvh));
-    float* const con = reinterpret_cast<float*>(sgen + C::kOffC) + (item & (C::kRingC - 1)) * ROWS;
-    bool waited = false;
-    constexpr int kAtOnce = D == 128 ? 4 : 2, kStep = 256 / kParts; // rows of a thread whose loads are on their way together; how far apart
+    uint32_t words[kMost][8];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      const int r = r0 + kStep * i;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) words[i][x] = 0u;
+      if (r < here) {
+        int b, tok, hl;
+        row_token(p, *it, r, &b, &tok, &hl);
+        const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
+        if (p.q_vector) {
+          *reinterpret_cast<uint4*>(words[i]) = load(reinterpret_cast<const uint4*>(q));
+          *reinterpret_cast<uint4*>(words[i] + 4) = load(reinterpret_cast<const uint4*>(q) + 1);
+        } else {
 #pragma unroll 1
-    for (int r0 = threadIdx.x / kParts; r0 < rows32; r0 += kStep * kAtOnce) {
-      uint4 raw[kAtOnce][2];
+          for (int x = 0; x < 8; ++x) {                               // (shifted in, so that no register is named by a variable)
+            const uint32_t w = (uint32_t)load(q + 2 * x) | (uint32_t)load(q + 2 * x + 1) << 16;
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int r = r0 + kStep * i;
-        raw[i][0] = raw[i][1] = make_uint4(0u, 0u, 0u, 0u);
-        if (r < here) {
-          int b, tok, hl;
-          row_token(p, *it, r, &b, &tok, &hl);
-          const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn + e;
-          if (p.q_vector) {
-            raw[i][0] = load(reinterpret_cast<const uint4*>(q));
-            raw[i][1] = load(reinterpret_cast<const uint4*>(q) + 1);
-          } else {
-            uint32_t* const words = reinterpret_cast<uint32_t*>(raw[i]);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) words[x] = (uint32_t)load(q + 2 * x) | (uint32_t)load(q + 2 * x + 1) << 16;
+            for (int y = 0; y < 7; ++y) words[i][y] = words[i][y + 1];
+            words[i][7] = w;
           }
-        }
-      }
-      if (!waited) wait(C::Q_FREE, q_phase);                        // (the first loads are on their way while the buffer is waited for)
-      waited = true;
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int r = r0 + kStep * i;
-        if (r < rows32) {                                           // (a warp's rows are a few neighbours: all or none)
-          const uint32_t words[8] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w, raw[i][1].x, raw[i][1].y, raw[i][1].z, raw[i][1].w};
-          // the largest magnitude, of pairs as they are (bits without their sign are in order in either type; NaN and infinity come out on top)
-          uint32_t a2 = 0u;
-#pragma unroll
-          for (int x = 0; x < 8; ++x) a2 = __vmaxu2(a2, words[x] & 0x7FFF7FFFu);
-#pragma unroll
-          for (int x = 1; x < kParts; x <<= 1) a2 = __vmaxu2(a2, __shfl_xor_sync(0xffffffffu, a2, x));
-          const float2 two = p.half ? unpack16<true>(a2) : unpack16<false>(a2);
-          const uint32_t up = row_exponent(finite_max(two.x, two.y));
-          const float f = __uint_as_float(up << 23);
-          uint32_t h[8];
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const float2 v = p.half ? unpack16<true>(words[x]) : unpack16<false>(words[x]);
-            h[x] = pack_pair<__half>(v.x * f, v.y * f);
-          }
-          uint8_t* const panel = sgen + C::kOffQ + (r >> 7) * (128 * D * 2) + (e >> 6) * 16384;
-#pragma unroll 1
-          for (int k = 0; k < copies; ++k) {
-            const int to = (r & 127) + k * (128 / copies);
-            *reinterpret_cast<uint4*>(panel + chunk_at(to, (e & 63) >> 3)) = make_uint4(h[0], h[1], h[2], h[3]);
-            *reinterpret_cast<uint4*>(panel + chunk_at(to, ((e & 63) >> 3) + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
-          }
-          if (e == 0) con[r] = c * __uint_as_float((254u - up) << 23);
         }
       }
     }
-    if (!waited) wait(C::Q_FREE, q_phase);                          // (no rows for this thread: its arrival belongs to this item all the same)
+    uint32_t ups[(kMost + 3) / 4];                                    // exponents of the rows' factors, a byte each
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      if (r0 + kStep * i >= rows32) break;                            // (a warp's rows are a few neighbours: all or none)
+      // the largest magnitude, of pairs as they are (bits without their sign are in order in either type; NaN and infinity come out on top)
+      uint32_t a2 = 0u;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) a2 = __vmaxu2(a2, words[i][x] & 0x7FFF7FFFu);
+#pragma unroll
+      for (int x = 1; x < kParts; x <<= 1) a2 = __vmaxu2(a2, __shfl_xor_sync(0xffffffffu, a2, x));
+      const float2 both = p.half ? unpack16<true>(a2) : unpack16<false>(a2);
+      const uint32_t up = row_exponent(finite_max(both.x, both.y));
+      const float f = __uint_as_float(up << 23);
+      if (p.half) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const float2 v = unpack16<true>(words[i][x]);
+          words[i][x] = pack_pair<__half>(v.x * f, v.y * f);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const float2 v = unpack16<false>(words[i][x]);
+          words[i][x] = pack_pair<__half>(v.x * f, v.y * f);
+        }
+      }
+      ups[i / 4] = i % 4 ? ups[i / 4] | up << (8 * (i % 4)) : up;
+    }
+    wait(C::Q_FREE, q_phase);
     q_phase ^= 1;
+    float* const con = reinterpret_cast<float*>(sgen + C::kOffC) + (item & (C::kRingC - 1)) * ROWS;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      const int r = r0 + kStep * i;
+      if (r >= rows32) break;
+      uint8_t* const panel = sgen + C::kOffQ + (r >> 7) * (128 * D * 2) + (e >> 6) * 16384;
+#pragma unroll 1
+      for (int k = 0; k < copies; ++k) {
+        const int to = (r & 127) + k * (128 / copies);
+        *reinterpret_cast<uint4*>(panel + chunk_at(to, (e & 63) >> 3)) = *reinterpret_cast<const uint4*>(words[i]);
+        *reinterpret_cast<uint4*>(panel + chunk_at(to, ((e & 63) >> 3) + 1)) = *reinterpret_cast<const uint4*>(words[i] + 4);
+      }
+      if (e == 0) con[r] = c * __uint_as_float((254u - (ups[i / 4] >> (8 * (i % 4)) & 255u)) << 23);
+    }
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(C::Q_FULL));
