@@ -5,6 +5,21 @@
 
 namespace fp4attn {
 
+// Attention of few rows per KV head with the masks and scores of fp4attn_paged_attention (tree_attn.cu): does a call have few, the workspace, the launch.
+struct FewRows {
+  const fp4attn_view* q;
+  CacheRef cache;
+  const int *context, *count, *first, *last;
+  const float* slopes;
+  void* out;
+  float* lse;
+  int* status;
+  int type, fmt, d, B, H, T;
+  float scale, cap;
+};
+bool few_rows(int rows, int fmt, int d);
+size_t few_rows_workspace(int B, int H, int kv_heads, int T, int d, int fmt);
+int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st);
 int check_cache(const fp4attn_cache* c, int B, const int* block_table, int max_pages, const int* start, const int* count, CacheRef* ref);
 
 namespace {
@@ -87,6 +102,25 @@ __device__ __forceinline__ float exp2_approx(float x) {
 // bits of scores that are nothing beside any others)
 __device__ __forceinline__ uint32_t row_exponent(float a) { return a == 0.f ? 127u : min(268u - (__float_as_uint(a) >> 23), 227u); }
 
+// bits [a, b) of a word, whatever a and b are
+__device__ __forceinline__ uint32_t bits_between(int a, int b) {
+  const uint32_t from = a <= 0 ? 0xFFFFFFFFu : a >= 32 ? 0u : 0xFFFFFFFFu << a, until = b >= 32 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << b) - 1;
+  return from & until;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// f16 pairs: NaN and infinities of bytes that nobody wrote become numbers, everything that a cache holds stays (E4M3 ends at 448): a probability
+// of 0 times any of them is 0
+__device__ __forceinline__ uint32_t finite(uint32_t h2) {
+  const __half2 most = __float2half2_rn(448.f), r = __hmin2(*reinterpret_cast<const __half2*>(&h2), most);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// a score in octaves (of e^s), capped: cap tanh(s / cap) = cap - 2 cap / (1 + e^(2 s / cap)); in = 2 / cap, out = cap log2 e.  Off by no more than
+// 2^-21 of the cap: the exponential and the reciprocal by 2^-22 of themselves.  (The tanh of the special-function unit is off by 2^-11.)
+__device__ __forceinline__ float cap_score(float y, float in, float out) { return fmaf(-2.f * out, rcp_approx(1.f + exp2_approx(y * in)), out); }
 // floor(a * b / c), floor((a + 1) * b / c), ... of tile numbers: in 32 bits where they are enough (64-bit divisions took 0.5 us of the
 // smallest calls)
 __device__ __forceinline__ constexpr long long div_short(long long a, long long c) {

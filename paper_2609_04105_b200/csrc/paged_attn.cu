@@ -272,16 +272,6 @@ __device__ __forceinline__ void row_token(const PagedParams& p, const I& i, int 
 template <int ROWS>
 __device__ __forceinline__ int copies_of(int rows) { return ROWS > 128 || rows > 64 ? 1 : rows > 32 ? 2 : 4; }
 
-// bits [a, b) of a word, whatever a and b are
-__device__ __forceinline__ uint32_t bits_between(int a, int b) {
-  const uint32_t from = a <= 0 ? 0xFFFFFFFFu : a >= 32 ? 0u : 0xFFFFFFFFu << a, until = b >= 32 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << b) - 1;
-  return from & until;
-}
-__device__ __forceinline__ float rcp_approx(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 // the larger of two magnitudes as row_exponent wants it: a NaN counts as the largest number there is
 __device__ __forceinline__ float finite_max(float a, float b) { return fminf(fmaxf(a, b), 0x1.fffffep127f); }
 // 32 bytes at once, so aligned
@@ -289,15 +279,6 @@ __device__ __forceinline__ void store_32(void* dst, const uint32_t* h) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"l"(dst), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
 }
-// f16 pairs: NaN and infinities of bytes that nobody wrote become numbers, everything that a cache holds stays (E4M3 ends at 448): a probability
-// of 0 times any of them is 0
-__device__ __forceinline__ uint32_t finite(uint32_t h2) {
-  const __half2 most = __float2half2_rn(448.f), r = __hmin2(*reinterpret_cast<const __half2*>(&h2), most);
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-// a score in octaves (of e^s), capped: cap tanh(s / cap) = cap - 2 cap / (1 + e^(2 s / cap)); in = 2 / cap, out = cap log2 e.  Off by no more than
-// 2^-21 of the cap: the exponential and the reciprocal by 2^-22 of themselves.  (The tanh of the special-function unit is off by 2^-11.)
-__device__ __forceinline__ float cap_score(float y, float in, float out) { return fmaf(-2.f * out, rcp_approx(1.f + exp2_approx(y * in)), out); }
 // place of 16-byte chunk c of a row of 128 bytes in a swizzled operand
 __device__ __forceinline__ uint32_t chunk_at(int row, int c) { return (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4)); }
 
@@ -1392,9 +1373,19 @@ int check(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, in
 
 using namespace fp4attn;
 
+namespace {
+// what a call needs, whatever its cache's format
+size_t paged_workspace(int B, int H, int kv_heads, int T, int d) {
+  size_t most = plan(B, H, kv_heads, T, d, 0).total;
+  for (int fmt : {FP4ATTN_FMT_NVFP4, FP4ATTN_FMT_E4M3})
+    if (few_rows(H / kv_heads * T, fmt, d)) most = std::max(most, few_rows_workspace(B, H, kv_heads, T, d, fmt));
+  return most;
+}
+}  // namespace
+
 extern "C" size_t fp4attn_paged_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d) {
   if (B <= 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || T <= 0 || (d != 64 && d != 128) || (long long)B * H * T >= (1ll << 31) || T >= (1 << 30)) return 0;
-  return plan(B, H, kv_heads, T, d, 0).total;
+  return paged_workspace(B, H, kv_heads, T, d);
 }
 
 extern "C" int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, const int* block_table,
@@ -1408,6 +1399,10 @@ extern "C" int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp
   if (!workspace || workspace_bytes < fp4attn_paged_attention_workspace_bytes(B, H, cache->kv_heads, T, cache->d)) return FP4ATTN_ERR_WORKSPACE;
   if ((uintptr_t)workspace & 31) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
+  if (few_rows(H / cache->kv_heads * T, cache->fmt, cache->d)) {
+    const FewRows a = {q, p.cache, context, count, first, last, slopes, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, p.cap};
+    return launch_few_rows(a, workspace, (cudaStream_t)stream);
+  }
   p.first = first; p.last = last;
   return launch(p, plan(B, H, cache->kv_heads, T, cache->d, 0), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
 }

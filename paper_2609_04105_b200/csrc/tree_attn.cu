@@ -59,6 +59,10 @@ struct TreeParams {
   int B, H, T, group, rows, row_tiles;     // rows = group * T of a KV head
   float scale;
   bool half, q_vector;
+  // of fp4attn_paged_attention (PAGED instances)
+  const int *seen_from, *seen_until;       // [B, T] or null
+  const float* slopes;
+  float cap;
 };
 
 // ---- what a CTA walks: tiles of items, in order.  The roles of a scheduler run in turn and each is one chain of instructions, so a tile
@@ -68,30 +72,56 @@ struct Walk {
   int first, left;                         // first key of the tile, tiles of the item from here on
   int ctx, len;                            // context, keys (context and drafted tokens) that the table has room for
   int need;                                // keys that are there: a page that the table does not have among them is reported
+  int begin, lowest;                       // PAGED: first tile of keys that rows see, first key
 };
 // drafted tokens that entry b has
 __device__ __forceinline__ int drafted(const TreeParams& p, int b) { return p.count ? max(0, min(load(p.count + b), p.T)) : p.T; }
 // tiles of an item: one at least, of no keys, where an entry has no rows
+// PAGED: keys that some row sees lie between begin and len; ctx is the context all the same
+template <bool PAGED = false>
 __device__ __forceinline__ int load_entry(Walk& w, const TreeParams& p) {
+  if (PAGED) {
+    const int room = p.cache.max_pages << p.cache.log_page, n = drafted(p, w.b);
+    w.ctx = max(0, min(load(p.context + w.b), (1 << 30) - 1));
+    int lo = INT_MAX, hi = 0;
+#pragma unroll 1
+    for (int t = 0; t < n; ++t) {
+      const int from = p.seen_from ? max(0, load(p.seen_from + (size_t)w.b * p.T + t)) : 0;
+      const int until = min(p.seen_until ? load(p.seen_until + (size_t)w.b * p.T + t) : w.ctx + t + 1, w.ctx + n);
+      if (from < until) {
+        lo = min(lo, from);
+        hi = max(hi, until);
+      }
+    }
+    w.need = hi;
+    w.len = min(hi, room);
+    w.begin = lo < w.len ? lo / kTile * kTile : 0;
+    w.lowest = lo;
+    if (lo >= w.len) w.len = 0;
+    return max(1, (w.len - w.begin + kTile - 1) / kTile);
+  }
   const int room = p.cache.max_pages << p.cache.log_page, n = drafted(p, w.b), c = n ? max(0, load(p.context + w.b)) : 0;
   w.ctx = min(c, room);
   w.need = (int)min((long long)c + n, (long long)INT_MAX);
   w.len = n ? (int)min((long long)c + (p.mask ? p.T : n), (long long)room) : 0;        // (a mask may look behind the count)
   return max(1, (w.len + kTile - 1) / kTile);
 }
+template <bool PAGED = false>
 __device__ __forceinline__ void next_item(Walk& w, const TreeParams& p, int units) {
   w.first = 0;
   if (++w.u == units) {
     w.u = 0;
     ++w.b;
   }
-  if (w.b < p.B) w.left = load_entry(w, p);
+  if (w.b < p.B) w.left = load_entry<PAGED>(w, p);
+  if (PAGED) w.first = w.begin;
 }
 // to the next tile; was this one the last of its item?
+template <bool PAGED = false>
 __device__ __forceinline__ bool advance(Walk& w, const TreeParams& p, int units) {
   w.first += kTile;
   if (!rare(--w.left == 0)) return false;
-  next_item(w, p, units);
+  next_item<PAGED>(w, p, units);
   return true;
 }
 // n tiles on; how many items ended on the way, and whether the tile is the first of its item
@@ -205,7 +235,7 @@ __device__ __forceinline__ uint32_t valid_eight(const Walk& w, unsigned long lon
 
 // This CTA's run of tiles: how many, and where it starts.  find: entry and place of the first tile, its number in the list, all tiles,
 // CTAs.  A barrier of the block (two for a batch of more than 32): everything that the block wrote to shared memory before is visible after it.
-template <int THREADS>
+template <int THREADS, bool PAGED = false>
 __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0, long long* scan, long long* find) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   Walk w;
@@ -223,7 +253,7 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
   long long at;                                                     // of the first tile among its entry's
   if (p.B <= 32) {                                                  // every warp for itself
     w.b = lane;
-    const int nt = lane < p.B ? load_entry(w, p) : 0;
+    const int nt = lane < p.B ? load_entry<PAGED>(w, p) : 0;
     const long long mine = (long long)nt * units;
     long long incl = mine;
 #pragma unroll
@@ -239,6 +269,10 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
     w0.ctx = __shfl_sync(0xffffffffu, w.ctx, b);
     w0.len = __shfl_sync(0xffffffffu, w.len, b);
     w0.need = __shfl_sync(0xffffffffu, w.need, b);
+    if (PAGED) {
+      w0.begin = __shfl_sync(0xffffffffu, w.begin, b);
+      w0.lowest = __shfl_sync(0xffffffffu, w.lowest, b);
+    }
     w0.left = __shfl_sync(0xffffffffu, nt, b);
     at = t0 < t1 ? t0 - __shfl_sync(0xffffffffu, incl - mine, b) : 0;
     __syncthreads();
@@ -246,7 +280,7 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
     const int per = (p.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, b1 = min(p.B, b0 + per);
     long long mine = 0;
 #pragma unroll 1
-    for (w.b = b0; w.b < b1; ++w.b) mine += (long long)load_entry(w, p) * units;
+    for (w.b = b0; w.b < b1; ++w.b) mine += (long long)load_entry<PAGED>(w, p) * units;
     long long incl = mine;
 #pragma unroll 1
     for (int s = 1; s < 32; s <<= 1) {
@@ -266,7 +300,7 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
     run();
     if (t0 < t1 && before <= t0 && t0 < before + mine) {            // one thread
       for (w.b = b0;; ++w.b) {
-        const long long here = (long long)load_entry(w, p) * units;
+        const long long here = (long long)load_entry<PAGED>(w, p) * units;
         if (t0 < before + here) break;
         before += here;
       }
@@ -275,19 +309,19 @@ __device__ __forceinline__ int find_run(const TreeParams& p, int units, Walk& w0
     }
     __syncthreads();
     w0.b = t0 < t1 ? (int)find[0] : 0;
-    w0.left = load_entry(w0, p);
+    w0.left = load_entry<PAGED>(w0, p);
     at = t0 < t1 ? find[1] : 0;
   }
   w0.u = (int)mul_div(at, 1, w0.left);
   const int kt = (int)(at - (long long)w0.u * w0.left);
-  w0.first = kt * kTile;
+  w0.first = kt * kTile + (PAGED ? w0.begin : 0);
   w0.left -= kt;
   return (int)min(t1 - t0, (long long)INT_MAX);
 }
 
 // Brings the pages of tiles into a ring of stages, one bulk copy each; a whole warp.  RING: stages for which `valid` remembers which of the
 // pages exist.  PARTS = 2: K and V by themselves, each in a stage of its own.
-template <int STAGES, int STAGE, int RING, int PARTS, bool CALL>
+template <int STAGES, int STAGE, int RING, int PARTS, bool CALL, bool PAGED = false>
 struct Pages {
   Walk w;
   Turn<STAGES> ring;
@@ -297,11 +331,11 @@ struct Pages {
   __device__ __forceinline__ void find(const TreeParams& p) {
     const int lane = threadIdx.x & 31, P = 1 << p.cache.log_page, slots = kTile >> p.cache.log_page;       // pages of a tile: 1 to 8
     page = -1;
-    if (lane < slots && w.first + lane * P < w.len) {
+    if (lane < slots && w.first + lane * P < w.len && (!PAGED || w.first + lane * P + P > w.lowest)) {
       page = p.cache.page_of(w.b, w.first + lane * P);
       lost |= page < 0 && w.first + lane * P < w.need;
     }
-    lost |= w.need > w.len;                                         // the table has no room for the last tokens
+    lost |= w.need > (PAGED ? p.cache.max_pages << p.cache.log_page : w.len);        // the table has no room for the last tokens
   }
   __device__ __forceinline__ void bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
     const int lane = threadIdx.x & 31;
@@ -320,7 +354,7 @@ struct Pages {
   __device__ __forceinline__ void skip(const TreeParams& p, int units, int n) {
 #pragma unroll 1
     for (int k = 0; k < n; ++k) {
-      if (PARTS == 1 || (i & 1)) advance(w, p, units);
+      if (PARTS == 1 || (i & 1)) advance<PAGED>(w, p, units);
       ring.next();
       ++i;
     }
@@ -966,7 +1000,8 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   return r;
 }
 
-template <int FMT, int D, int NT>
+// PAGED: rows see intervals of keys, and scores may be capped or biased (fp4attn_paged_attention)
+template <int FMT, int D, int NT, bool PAGED>
 __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D, NT>::kCtas) tree_warp_kernel(const TreeParams p) {
   using C = WarpCfg<FMT, D, NT>;
   using L = typename C::L;
@@ -990,14 +1025,14 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
   wait_prior_grids();
   Walk w0;
   long long* const find = reinterpret_cast<long long*>(sgen + C::kOffFind);
-  const int n_tiles = find_run<C::kThreads>(p, units, w0, reinterpret_cast<long long*>(sgen + C::kOffScan), find);
+  const int n_tiles = find_run<C::kThreads, PAGED>(p, units, w0, reinterpret_cast<long long*>(sgen + C::kOffScan), find);
   uint32_t* const valid = reinterpret_cast<uint32_t*>(sgen + C::kOffValid);
   const int P = 1 << p.cache.log_page;
 
   // K and V of the first tiles; then the warps take turns, each bringing what takes the place of the K or V before the one they have just
   // been through (of that one the other warps may not be through yet).  A warp that fills a stage has itself been through what stood there
   // before: the stage's barrier cannot be further back than a wait by parity can tell.
-  Pages<C::kStages, C::kStage, C::kStages, 2, true> pages;
+  Pages<C::kStages, C::kStage, C::kStages, 2, true, PAGED> pages;
   pages.w = w0;
   const int n_parts = n_tiles > INT_MAX / 2 ? INT_MAX : 2 * n_tiles;
   if (warp == 0) {
@@ -1044,12 +1079,16 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
     float* const o_smem = reinterpret_cast<float*>(sgen + C::kOffO);
     float2* const ml_smem = reinterpret_cast<float2*>(sgen + C::kOffML);
 
+    const bool changed = PAGED && (p.cap > 0.f || p.slopes);
     Walk w = w0;
     Turn<C::kStages> ring;
     bool fresh = true;
     int part_first = 0, b_of = -1, n_drafted = 0, kvh = 0, row0 = 0;
     unsigned long long seen = 0;
     uint32_t qf[NT][kSteps][2];                                     // Q^T: rows 8n + lane / 4
+    int from[NT][2], until[NT][2], at[NT][2], plain_from = 0, plain_until = 0;     // PAGED: keys that rows 8n + 2c, + 1 see, where they stand; that all rows see
+    float slope[NT][2];
+    const float cap_in = PAGED && p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f;
     float con[NT][2], ref[NT][2], l[NT][2];                         // of rows 8n + 2c, + 1: score constant, kShift minus the reference, sum
     float o[kSteps][NT][4];
 #pragma unroll 1
@@ -1060,12 +1099,33 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
         if (w.b != b_of) {
           b_of = w.b;
           n_drafted = drafted(p, w.b);
-          seen = row_mask(p, w.b, lane, n_drafted) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n_drafted) : 0ull);
-          seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
+          if (!PAGED) {
+            seen = row_mask(p, w.b, lane, n_drafted) | (lane + 32 < p.T ? row_mask(p, w.b, lane + 32, n_drafted) : 0ull);
+            seen = (unsigned long long)__reduce_or_sync(0xffffffffu, (uint32_t)(seen >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)seen);
+          }
         }
         kvh = w.u / p.row_tiles;
         row0 = (w.u - kvh * p.row_tiles) * R;
         const float c0 = __fdiv_rn(p.scale * 1.4426950408889634f, load(p.cache.k_G + kvh));
+        if (PAGED) {
+          plain_from = 0;
+          plain_until = INT_MAX;
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const int row = row0 + 8 * n + 2 * c + y, hl = row / p.T, tok = row - hl * p.T;
+              const bool is = row < p.rows && tok < n_drafted;
+              from[n][y] = is && p.seen_from ? max(0, load(p.seen_from + (size_t)w.b * p.T + tok)) : 0;
+              until[n][y] = !is ? INT_MAX : max(0, min(p.seen_until ? load(p.seen_until + (size_t)w.b * p.T + tok) : w.ctx + tok + 1, w.len));
+              at[n][y] = w.ctx + tok;
+              slope[n][y] = is && p.slopes ? load(p.slopes + kvh * p.group + hl) * 1.4426950408889634f : 0.f;
+              plain_from = max(plain_from, from[n][y]);
+              plain_until = min(plain_until, until[n][y]);
+            }
+          plain_from = __reduce_max_sync(0xffffffffu, plain_from);
+          plain_until = __reduce_min_sync(0xffffffffu, plain_until);
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           // Q scaled by a power of two per row, as above
@@ -1122,10 +1182,11 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
         wait_phase<true>(full + 8 * ring.at, ring.phase, abort_at);
         const uint8_t* stage = sgen + ring.at * C::kStage;
         const uint32_t held = valid[ring.at];
-        const bool plain = w.first + kTile <= w.ctx && held == (1u << (kTile >> p.cache.log_page)) - 1;
+        const bool plain = (PAGED ? w.first >= plain_from && w.first + kTile <= plain_until : w.first + kTile <= w.ctx) &&
+                           held == (1u << (kTile >> p.cache.log_page)) - 1;
         const bool v_here = held >> ((tok0 + 8 * c) >> p.cache.log_page) & 1;
         uint32_t v_mask = 0xFFu;                                    // of tokens 8c .., those that count
-        if (rare(!plain)) v_mask = v_here ? valid_eight(w, seen, w.first + tok0 + 8 * c) : 0u;
+        if (!PAGED && rare(!plain)) v_mask = v_here ? valid_eight(w, seen, w.first + tok0 + 8 * c) : 0u;
         // ---- scores
         float s[NT][8];
 #pragma unroll
@@ -1176,7 +1237,29 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
         // ---- probabilities: octaves above the rows' references (+ kShift); what is not seen goes to -infinity
         float x[NT][8], top = -INFINITY;
         uint32_t hidden = 0;                                        // bit 8n + y: s[n][y] is not seen
-        if (rare(!plain)) {
+        if (PAGED) {
+          if (rare(!plain)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int y = 0; y < 8; ++y) {
+                const int tok = tok_k + kSecondStep * (y >> 2) + kSecondRow * (y >> 1 & 1), pos = w.first + tok0 + tok;
+                const bool here = held >> ((tok0 + tok) >> p.cache.log_page) & 1;
+                hidden |= (here && pos >= from[n][y & 1] && pos < until[n][y & 1] ? 0u : 1u) << (8 * n + y);
+              }
+          }
+          if (changed) {                            // scores in octaves, changed; their constants are spent
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int y = 0; y < 8; ++y) {
+                const int tok = tok_k + kSecondStep * (y >> 2) + kSecondRow * (y >> 1 & 1), pos = w.first + tok0 + tok;
+                float z = s[n][y] * con[n][y & 1];
+                if (p.cap > 0.f) z = cap_score(z, cap_in, cap_out);
+                s[n][y] = fmaf(-slope[n][y & 1], fabsf((float)(at[n][y & 1] - pos)), z);
+              }
+          }
+        } else if (rare(!plain)) {
 #pragma unroll 1
           for (int n = 0; n < NT; ++n) {
             unsigned long long mask[2];                             // drafted tokens that the rows see
@@ -1198,7 +1281,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int y = 0; y < 8; ++y) x[n][y] = fmaf(s[n][y], con[n][y & 1], ref[n][y & 1]);
+            for (int y = 0; y < 8; ++y) x[n][y] = fmaf(s[n][y], PAGED && changed ? 1.f : con[n][y & 1], ref[n][y & 1]);
           if (rare(hidden != 0)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -1220,7 +1303,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
               float m = -INFINITY;                                  // the largest seen; max leaves NaN out
 #pragma unroll
               for (int z = 0; z < 8; z += 2)
-                if (!(hidden >> (8 * n + y + z) & 1)) m = fmaxf(m, s[n][y + z] * con[n][y]);
+                if (!(hidden >> (8 * n + y + z) & 1)) m = fmaxf(m, s[n][y + z] * (PAGED && changed ? 1.f : con[n][y]));
               for (int z = 4; z < 32; z <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, z));
               const float old = kShift - ref[n][y];                 // -infinity: none yet
               m = fmaxf(m, old);
@@ -1249,7 +1332,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
         // ---- scales of V: f16, by block and token
         if (L::kFp4 && lane < D / 4) {
           uint2 sc = *reinterpret_cast<const uint2*>(stage + vs_at);
-          if (rare(!plain)) {
+          if (!PAGED && rare(!plain)) {
             const uint32_t v = permute_eight(v_mask);
             sc.x &= byte_mask(v);
             sc.y &= byte_mask(v >> 4);
@@ -1257,6 +1340,10 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
           uint32_t f[4];
           cvt_f16x2_e4m3x4(sc.x, f);
           cvt_f16x2_e4m3x4(sc.y, f + 2);
+          if (PAGED) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) f[y] = finite(f[y]);        // (what nobody sees has a probability of 0)
+          }
           *reinterpret_cast<uint4*>(scales + lane * 16) = make_uint4(f[0], f[1], f[2], f[3]);
         }
         __syncwarp();
@@ -1277,7 +1364,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             }
           } else {
             uint2 e = *reinterpret_cast<const uint2*>(stage + v_at + z * 256), d = *reinterpret_cast<const uint2*>(stage + v_at + z * 256 + 16);
-            if (rare(!plain)) {
+            if (!PAGED && rare(!plain)) {
               const uint32_t lo = byte_mask(v_mask), hi = byte_mask(v_mask >> 4);
               e.x &= lo; e.y &= hi; d.x &= lo; d.y &= hi;
             }
@@ -1285,6 +1372,13 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             cvt_f16x2_e4m3x4(e.y, even + 2);
             cvt_f16x2_e4m3x4(d.x, odd);
             cvt_f16x2_e4m3x4(d.y, odd + 2);
+            if (PAGED && rare(!plain)) {
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                even[y] = finite(even[y]);
+                odd[y] = finite(odd[y]);
+              }
+            }
           }
 #pragma unroll
           for (int q = 0; q < 2; ++q)
@@ -1298,9 +1392,9 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
       }
       // ---- end of the item, or of this CTA's part of it: the warps together
       if (rare(w.left == 1 || i + 1 == n_tiles)) {
-        const bool whole = part_first == 0 && w.left == 1;
+        const bool begins = part_first == (PAGED ? w.begin : 0), whole = begins && w.left == 1;
         const long long out0 = ((long long)w.b * p.H + (long long)kvh * p.group) * p.T;
-        const int slot_of = 2 * (int)blockIdx.x + (part_first == 0);
+        const int slot_of = 2 * (int)blockIdx.x + begins;
 #pragma unroll
         for (int n = 0; n < NT; ++n)                                // eight rows and half the elements at a time
 #pragma unroll
@@ -1346,12 +1440,12 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
             }
             __syncthreads();
           }
-        if (threadIdx.x == 0 && part_first == 0)
+        if (threadIdx.x == 0 && begins)
           p.split[(size_t)w.b * units + w.u] =
               whole ? make_int2(-1, -1) : make_int2(blockIdx.x, cta_of(find[2] + i + w.left - 1, find[3], find[4]));
         fresh = true;
       }
-      advance(w, p, units);
+      advance<PAGED>(w, p, units);
     }
     pages.tell(p);
   }
@@ -1465,21 +1559,21 @@ int launch_tree(const TreeParams& p, cudaStream_t st) {
     e = launch_overlapped(tree_join_kernel<D, R>, dim3((unsigned)(p.B * units), (unsigned)(std::min(R, p.rows) + 3) / 4), 128u, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
-template <int FMT, int D, int NT>
+template <int FMT, int D, int NT, bool PAGED = false>
 int launch_warps(const TreeParams& p, cudaStream_t st) {
   using C = WarpCfg<FMT, D, NT>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FP4ATTN_ERR_CUDA;
   static std::atomic<bool> attr_set[kMaxDevices];
   if (!attr_set[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(tree_warp_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
+    if (cudaFuncSetAttribute(tree_warp_kernel<FMT, D, NT, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) return FP4ATTN_ERR_CUDA;
     attr_set[dev].store(true, std::memory_order_release);
   }
   const int sms = device_sms();
   if (!sms) return FP4ATTN_ERR_CUDA;
   const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * p.cache.kv_heads * p.row_tiles;
   const unsigned grid = (unsigned)std::min<long long>(std::min(C::kCtas * sms, kMostCtas<C::R>), most_tiles);
-  cudaError_t e = launch_overlapped(tree_warp_kernel<FMT, D, NT>, dim3(grid), C::kThreads, C::kSmem, st, p);
+  cudaError_t e = launch_overlapped(tree_warp_kernel<FMT, D, NT, PAGED>, dim3(grid), C::kThreads, C::kSmem, st, p);
   if (e == cudaSuccess)
     e = launch_overlapped(tree_join_kernel<D, C::R>, dim3((unsigned)(p.B * p.cache.kv_heads * p.row_tiles), (unsigned)(std::min(p.rows, C::R) + 3) / 4), 128u, 0,
                           st, p);
@@ -1493,7 +1587,39 @@ int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
   return R == 32 ? launch_tree<FMT, D, 32>(p, st) : launch_tree<FMT, D, 64>(p, st);
 }
 
+template <int FMT, int D>
+int launch_few(const TreeParams& p, int R, bool changed, cudaStream_t st) {
+  if (R == 8) return changed ? launch_warps<FMT, D, 1, true>(p, st) : launch_warps<FMT, D, 1>(p, st);
+  if constexpr (!(FMT == FP4ATTN_FMT_NVFP4 && D == 128)) return changed ? launch_warps<FMT, D, 2, true>(p, st) : launch_warps<FMT, D, 2>(p, st);
+  return FP4ATTN_ERR_UNSUPPORTED_SHAPE;                             // (not few)
+}
+
 }  // namespace
+
+bool few_rows(int rows, int fmt, int d) { return rows_of_tile(rows, fmt, d) <= 16; }
+size_t few_rows_workspace(int B, int H, int kv_heads, int T, int d, int fmt) { return plan(B, H, kv_heads, T, d, fmt).total; }
+int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st) {
+  const TreePlan t = plan(a.B, a.H, a.cache.kv_heads, a.T, a.d, a.fmt);
+  TreeParams p = {};
+  p.q = a.q->data; p.q_sb = a.q->stride_b; p.q_sh = a.q->stride_h; p.q_sn = a.q->stride_n;
+  p.q_vector = view_vectors(*a.q, 2);
+  p.half = a.type == FP4ATTN_TYPE_FP16;
+  p.cache = a.cache;
+  p.context = a.context; p.count = a.count;
+  p.out = a.out; p.lse = a.lse; p.status = a.status;
+  p.B = a.B; p.H = a.H; p.T = a.T; p.group = a.H / a.cache.kv_heads;
+  p.rows = p.group * a.T;
+  p.row_tiles = t.row_tiles;
+  p.scale = a.scale;
+  p.seen_from = a.first; p.seen_until = a.last; p.slopes = a.slopes; p.cap = a.cap;
+  p.part = (float*)workspace;
+  p.part_ml = (float2*)((char*)workspace + t.ml);
+  p.split = (int2*)((char*)workspace + t.split);
+  const bool changed = a.first || a.last || a.slopes || a.cap > 0.f;        // (else it is attention over a tree in which every token sees those before it)
+  if (a.fmt == FP4ATTN_FMT_NVFP4) return a.d == 64 ? launch_few<FP4ATTN_FMT_NVFP4, 64>(p, t.R, changed, st) : launch_few<FP4ATTN_FMT_NVFP4, 128>(p, t.R, changed, st);
+  return a.d == 64 ? launch_few<FP4ATTN_FMT_E4M3, 64>(p, t.R, changed, st) : launch_few<FP4ATTN_FMT_E4M3, 128>(p, t.R, changed, st);
+}
+
 }  // namespace fp4attn
 
 using namespace fp4attn;
