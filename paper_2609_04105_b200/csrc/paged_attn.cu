@@ -61,6 +61,8 @@ struct PagedParams {
   int B, H, T, group, row_tiles;           // row_tiles: of a sequence's rows
   unsigned long long by_group, by_tokens;  // for divide()
   float scale, cap;
+  OwnParts own;                            // shared, of sequences by themselves, where they are not items of this kernel
+  bool own_items;                          // shared: are they?
   bool half, q_vector, out_wide;           // out_wide: O begins at a multiple of 32 bytes
 };
 
@@ -205,7 +207,7 @@ struct Run {
 template <int ROWS, int THREADS>
 __device__ __forceinline__ Run find_run(const PagedParams& p, long long* scan, long long* find) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int X = p.groups ? p.groups + p.B : p.B * p.row_tiles;
+  const int X = p.groups ? p.groups + (p.own_items ? p.B : 0) : p.B * p.row_tiles;
   const int per = (X + THREADS - 1) / THREADS, x0 = min(X, (int)threadIdx.x * per), x1 = min(X, x0 + per);
   Desc d;
   auto tiles = [&](int x) {
@@ -1148,14 +1150,14 @@ struct Sum {
     else *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(src + lane * E);
   }
   // row r of the parts that an item left in CTAs first .. last
-  __device__ __forceinline__ void parts(const PagedParams& p, int rows, int first, int last, int r, int lane) {
+  __device__ __forceinline__ void parts(const float* part_of, const float2* ml_of, int rows, int first, int last, int r, int lane) {
     const int n = last - first + 1;
     auto at = [&](int i) { return (size_t)(i ? 2 * (first + i) : 2 * first + 1) * rows + r; };
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, p.part_ml[at(i)].x);
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, ml_of[at(i)].x);
     m = warp_max(m);
     for (int i0 = 0; i0 < n; i0 += 32) {
       const int i = i0 + lane;
-      const float2 ml = i < n ? p.part_ml[at(i)] : make_float2(-INFINITY, 0.f);
+      const float2 ml = i < n ? ml_of[at(i)] : make_float2(-INFINITY, 0.f);
       const float mine = m == -INFINITY || i >= n ? 0.f : exp2_approx(ml.x - m);
       const float weighted = ml.x == -INFINITY ? ml.y : mine * ml.y;
       constexpr int kAtOnce = 8;                                    // loads on their way together
@@ -1165,7 +1167,7 @@ struct Sum {
         for (int k = 0; k < kAtOnce; ++k) {
 #pragma unroll
           for (int x = 0; x < E; ++x) part[k][x] = 0.f;
-          if (i0 + k0 + k < n) fetch(p.part + at(i0 + k0 + k) * D, lane, part[k]);
+          if (i0 + k0 + k < n) fetch(part_of + at(i0 + k0 + k) * D, lane, part[k]);
         }
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {                         // (behind the last part: weights and parts of 0)
@@ -1208,7 +1210,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedParams p)
   for (int r = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5); r < here; r += gridDim.y * (kJoinThreads / 32)) {
     const int t = (d.row0 + r) / p.group, hl = d.row0 + r - t * p.group;
     Sum<D> s;
-    s.parts(p, ROWS, first, last, r, lane);
+    s.parts(p.part, p.part_ml, ROWS, first, last, r, lane);
     s.give(p, ((size_t)d.b * p.H + (size_t)kvh * p.group + hl) * p.T + t, kvh, lane);
   }
 }
@@ -1230,7 +1232,7 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const PagedPa
     Sum<D> s;
     const long long w = d.g < 0 ? all + at : at;
     if (ctas.x < 0) s.one(p.whole + w * D, p.whole_ml[w], lane);
-    else if (ctas.y >= ctas.x && ctas.y < kMostCtas) s.parts(p, ROWS, ctas.x, ctas.y, row % ROWS, lane);
+    else if (ctas.y >= ctas.x && ctas.y < kMostCtas) s.parts(p.part, p.part_ml, ROWS, ctas.x, ctas.y, row % ROWS, lane);
     sum.add(s);
   };
   // the last group that begins here or before
@@ -1242,7 +1244,16 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const PagedPa
   }
   const int b0 = load(p.group_start + g);
   if (b >= b0 && b < load(p.group_start + g + 1)) take(g, ((b - max(0, b0)) * p.T + t) * p.group + hl);
-  take(p.groups + b, t * p.group + hl);
+  if (p.own_items) {
+    take(p.groups + b, t * p.group + hl);
+  } else {
+    const int row = hl * p.T + t;                                   // (heads first)
+    const int2 ctas = p.own.split[((size_t)b * p.cache.kv_heads + kvh) * p.own.row_tiles + row / p.own.rows];
+    Sum<D> s;
+    if (ctas.x < 0) s.one(p.whole + (all + at) * D, p.whole_ml[all + at], lane);
+    else if (ctas.y >= ctas.x && ctas.y < p.own.most_ctas) s.parts(p.own.part, p.own.part_ml, p.own.rows, ctas.x, ctas.y, row % p.own.rows, lane);
+    sum.add(s);
+  }
   sum.give(p, (size_t)at, kvh, lane);
 }
 
@@ -1270,13 +1281,13 @@ __global__ void __launch_bounds__(128) range_kernel(const PagedParams p, int2* r
 // ---- workspace
 struct Plan {
   int rt, row_tiles;                       // 128-row halves of an item; items of a sequence's rows
-  size_t ml, begun, ranges, split, whole, whole_ml, total;
+  size_t ml, begun, ranges, split, whole, whole_ml, own, total;
 };
 size_t align32(size_t x) { return (x + 31) & ~(size_t)31; }
-Plan plan(int B, int H, int kv_heads, int T, int d, int groups) {
+Plan plan(int B, int H, int kv_heads, int T, int d, int groups, bool own_items = false) {
   Plan t;
   const long long rows = (long long)(H / kv_heads) * T;
-  t.rt = !groups && rows > 128 ? 2 : 1;
+  t.rt = (!groups ? rows : own_items ? 0 : rows * B / groups) > 128 ? 2 : 1;
   const long long R = 128 * t.rt, all = (long long)B * H * T;
   t.row_tiles = (int)((rows + R - 1) / R);
   const size_t slots = 2 * (size_t)kMostCtas * R;
@@ -1286,12 +1297,12 @@ Plan plan(int B, int H, int kv_heads, int T, int d, int groups) {
   t.split = t.ranges + (groups ? 0 : align32((size_t)B * t.row_tiles * 8));
   t.whole = t.split + (groups ? align32((size_t)(B * rows / R + groups + 1 + (long long)B * t.row_tiles) * kv_heads * 8) : 0);
   t.whole_ml = t.whole + (groups ? (size_t)(2 * all) * d * 4 : 0);
-  t.total = t.whole_ml + (groups ? align32((size_t)(2 * all) * 8) : 0);
+  t.own = t.total = t.whole_ml + (groups ? align32((size_t)(2 * all) * 8) : 0);
   return t;
 }
 
 template <int FMT, int D, int RT, int SCORES>
-int launch_scores(const PagedParams& p, cudaStream_t st) {
+int launch_scores(const PagedParams& p, const FewRows* own, void* own_workspace, cudaStream_t st) {
   using C = PagedCfg<FMT, D, RT>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FP4ATTN_ERR_CUDA;
@@ -1307,18 +1318,25 @@ int launch_scores(const PagedParams& p, cudaStream_t st) {
   if (p.ranges)
     e = launch_overlapped(range_kernel<C::kRows>, dim3((unsigned)((p.B * p.row_tiles + 3) / 4)), 128u, 0, st, p, const_cast<int2*>(p.ranges));
   if (e == cudaSuccess) e = launch_overlapped(paged_kernel<FMT, D, RT, SCORES>, dim3(grid), C::kThreads, C::kSmem, st, p);
+  if (e != cudaSuccess) return FP4ATTN_ERR_CUDA;
+  PagedParams joined = p;
+  if (own) {
+    const int rc = launch_own_rows(*own, own_workspace, p.whole + (size_t)p.B * p.H * p.T * D, p.whole_ml + (size_t)p.B * p.H * p.T, &joined.own, st);
+    if (rc != FP4ATTN_OK) return rc;
+  }
   const long long rows = (long long)p.B * p.H * p.T;
   if (e == cudaSuccess)
-    e = p.groups ? launch_overlapped(shared_join_kernel<D, C::kRows>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), kJoinThreads, 0, st, p)
+    e = p.groups ? launch_overlapped(shared_join_kernel<D, C::kRows>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), kJoinThreads, 0, st, joined)
                  : launch_overlapped(join_kernel<D, C::kRows>, dim3(grid, (unsigned)std::min(8, (std::min(p.group * p.T, C::kRows) + 7) / 8)), kJoinThreads, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
 template <int FMT, int D, int RT>
-int launch_rows(const PagedParams& p, cudaStream_t st) {
-  if (p.slopes) return launch_scores<FMT, D, RT, kBiased>(p, st);
-  return p.cap > 0.f ? launch_scores<FMT, D, RT, kCapped>(p, st) : launch_scores<FMT, D, RT, kScaled>(p, st);
+int launch_rows(const PagedParams& p, const FewRows* own, void* own_workspace, cudaStream_t st) {
+  if (p.slopes) return launch_scores<FMT, D, RT, kBiased>(p, own, own_workspace, st);
+  return p.cap > 0.f ? launch_scores<FMT, D, RT, kCapped>(p, own, own_workspace, st) : launch_scores<FMT, D, RT, kScaled>(p, own, own_workspace, st);
 }
-int launch(PagedParams& p, const Plan& t, void* workspace, int fmt, int d, cudaStream_t st) {
+// own: shared prefixes, sequences by themselves in a kernel of their own
+int launch(PagedParams& p, const Plan& t, const FewRows* own, void* workspace, int fmt, int d, cudaStream_t st) {
   char* const ws = (char*)workspace;
   p.row_tiles = t.row_tiles;
   auto reciprocal = [](int n) { return ((1ull << 36) + n - 1) / n; };
@@ -1336,7 +1354,7 @@ int launch(PagedParams& p, const Plan& t, void* workspace, int fmt, int d, cudaS
     if (p.first || p.last) p.ranges = (const int2*)(ws + t.ranges);
   }
   auto rows = [&](auto fmt_c, auto d_c) {
-    return t.rt == 2 ? launch_rows<fmt_c.value, d_c.value, 2>(p, st) : launch_rows<fmt_c.value, d_c.value, 1>(p, st);
+    return t.rt == 2 ? launch_rows<fmt_c.value, d_c.value, 2>(p, own, ws + t.own, st) : launch_rows<fmt_c.value, d_c.value, 1>(p, own, ws + t.own, st);
   };
   using std::integral_constant;
   if (fmt == FP4ATTN_FMT_NVFP4)
@@ -1400,16 +1418,19 @@ extern "C" int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp
   if ((uintptr_t)workspace & 31) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   if (few_rows(H / cache->kv_heads * T, cache->fmt, cache->d)) {
-    const FewRows a = {q, p.cache, context, count, first, last, slopes, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, p.cap};
+    const FewRows a = {q, p.cache, context, count, first, last, nullptr, slopes, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, p.cap};
     return launch_few_rows(a, workspace, (cudaStream_t)stream);
   }
   p.first = first; p.last = last;
-  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, 0), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
+  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, 0), nullptr, workspace, cache->fmt, cache->d, (cudaStream_t)stream);
 }
 
 extern "C" size_t fp4attn_shared_prefix_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d, int groups) {
   if (groups <= 0 || groups > 65535 || T > FP4ATTN_MOST_TREE_TOKENS) return 0;
-  return fp4attn_paged_attention_workspace_bytes(B, H, kv_heads, T, d) ? plan(B, H, kv_heads, T, d, groups).total : 0;
+  if (!fp4attn_paged_attention_workspace_bytes(B, H, kv_heads, T, d)) return 0;
+  // (the size does not depend on which way a call goes)
+  return std::max(plan(B, H, kv_heads, T, d, groups).total + fp4attn_tree_attention_workspace_bytes(B, H, kv_heads, T, d),
+                  plan(B, H, kv_heads, T, d, groups, true).total);
 }
 
 extern "C" int fp4attn_shared_prefix_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, int groups,
@@ -1428,5 +1449,9 @@ extern "C" int fp4attn_shared_prefix_attention(const fp4attn_view* q, int type, 
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   p.groups = groups; p.prefix_table = prefix_table; p.prefix_pages = prefix_pages; p.prefix_length = prefix_length; p.group_start = group_start;
   p.mask = tree_mask;
-  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, groups), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
+  // Sequences by themselves have few rows each, which the kernels of attention over a tree are made for: 48 sequences of up to 900 tokens behind one of
+  // 16000 OLDNEW us.  Those know no caps and biases: then they are items like the prefixes.
+  p.own_items = slopes || soft_cap > 0.f;
+  const FewRows own = {q, p.cache, context, count, nullptr, nullptr, tree_mask, nullptr, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, 0.f};
+  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, groups, p.own_items), p.own_items ? nullptr : &own, workspace, cache->fmt, cache->d, (cudaStream_t)stream);
 }
