@@ -93,6 +93,14 @@ __device__ __forceinline__ void fma_pair(float& x0, float& x1, uint32_t a0, uint
       "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
       : "=f"(x0), "=f"(x1) : "r"(a0), "r"(a1), "r"(b0), "r"(b1), "r"(c0), "r"(c1));
 }
+// x = a * b
+__device__ __forceinline__ void mul_pair(float& x0, float& x1, float a0, float a1, float b0, float b1) {
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(x0), "=f"(x1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void fma_pair(float& x0, float& x1, float a0, float a1, float b0, float b1, float c0, float c1) {
+  fma_pair(x0, x1, __float_as_uint(a0), __float_as_uint(a1), __float_as_uint(b0), __float_as_uint(b1), __float_as_uint(c0), __float_as_uint(c1));
+}
 __device__ __forceinline__ void add_pair(float& l0, float& l1, float a0, float a1) {
   asm("{\n\t.reg .b64 a, l;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 l, {%0, %1};\n\tadd.rn.f32x2 l, l, a;\n\tmov.b64 {%0, %1}, l;\n\t}"
       : "+f"(l0), "+f"(l1) : "f"(a0), "f"(a1));

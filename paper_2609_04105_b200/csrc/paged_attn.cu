@@ -17,6 +17,9 @@
 // exponential unit.  Items of more than 128 rows give each group half of the rows; those of fewer give the groups tiles in turn, with references,
 // sums and an O each, joined at the item's end.
 //
+// A row's keys are walked from its last to its first: what a mask cuts off comes where a reference has to be looked for anyway, and a bias by distance falls
+// from there on, so that references do not move.
+//
 // All tiles of all items stand in one list of which every CTA takes an equal run; what an item leaves in several CTAs (maximum, sum, O) is joined by a
 // second kernel in the order of its keys, so results repeat bit by bit.  With shared prefixes an item is a prefix's rows of all members of its group, or
 // a sequence's rows over its own tokens; every row is joined from both.
@@ -69,7 +72,7 @@ struct PagedParams {
 // What a CTA has of an item: written by the producer, read by the other roles
 struct Item {
   int tiles;                               // of the item here; 0: no item, the end
-  int first;                               // first key of the first of them
+  int first;                               // first key of the first of them; tiles go from the last keys to the first (see below)
   int lo, hi, ctx;                         // as in Desc
   int b, g, kvh;
   int row0, here, v0, h0;                  // its first row, how many it has; token and head of the first
@@ -103,7 +106,7 @@ struct PagedCfg {
   static constexpr int kOffValid = kOffJoin + kJoin;                  // u32 [kRing]: pages of a tile that are there
   static constexpr int kOffItems = kOffValid + 4 * kRing;
   static constexpr int kOffScan = kOffItems + kItemBytes;           // i64 [18]
-  static constexpr int kOffFind = kOffScan + 256;                  // i64 [5]
+  static constexpr int kOffFind = kOffScan + 256;                  // i64 [2], Desc
   static constexpr int kOffBar = kOffFind + 64;
   static constexpr int kSmem = kOffBar + 1024 + 1024;
   static_assert(kSmem <= 227 * 1024 && kOffStage % 1024 == 0 && kStage % 16 == 0, "shared memory");
@@ -228,10 +231,11 @@ __device__ __forceinline__ Run find_run(const PagedParams& p, long long* scan, l
   Run r;
   long long before = 0;
   r.total = 0;
-#pragma unroll 1
+#pragma unroll
   for (int i = 0; i < THREADS / 32; ++i) {
-    if (i < warp) before += scan[i];
-    r.total += scan[i];
+    const long long here = scan[i];
+    before += i < warp ? here : 0;
+    r.total += here;
   }
   before += incl - mine;
   r.ctas = min((long long)gridDim.x, r.total);
@@ -247,6 +251,7 @@ __device__ __forceinline__ Run find_run(const PagedParams& p, long long* scan, l
       }
     find[0] = x;
     find[1] = r.first - before;
+    *reinterpret_cast<Desc*>(find + 2) = d;                         // (of x: the one described last)
   }
   __syncthreads();
   r.x = r.tiles ? (int)find[0] : 0;
@@ -415,7 +420,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     long long left = run.tiles, number = run.first, at = run.at;      // number: of the first unit of the run, at: its place in the item
     Desc d;
     if (left > 0) {
-      describe<ROWS>(p, x, d);
+      d = *reinterpret_cast<const Desc*>(sgen + C::kOffFind + 16);
       u = (int)mul_div(at, 1, d.nt + kItemCost);
       at -= (long long)u * (d.nt + kItemCost);
     }
@@ -431,7 +436,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       const int kvh = u / d.rts, rt = u - kvh * d.rts;
       Item it;
       it.tiles = max(0, end - kItemCost - tile);
-      it.first = (d.k0 + tile) * kTile;
+      it.first = (d.k0 + d.nt - 1 - tile) * kTile;
       it.lo = d.lo; it.hi = d.hi; it.ctx = d.ctx; it.b = d.b; it.g = d.g; it.kvh = kvh;
       it.row0 = d.row0 + rt * ROWS;
       it.here = min(ROWS, d.rows - it.row0);
@@ -479,7 +484,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
         const uint8_t* const rec = pages + (size_t)max(page, 0) * page_bytes;
         const bool mine = page >= 0;
-        if (k + 1 < it.tiles) page = page_at(it.first + (k + 1) * kTile);            // (its entry comes while a stage is waited for)
+        if (k + 1 < it.tiles) page = page_at(it.first - (k + 1) * kTile);            // (its entry comes while a stage is waited for)
 #pragma unroll 1
         for (int part = 0; part < 2; ++part) {
           wait(C::RING_FREE + ring.at, ring.phase ^ 1);
@@ -557,7 +562,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         wait(C::PV_DONE + 2 * group + place, (n >> 2 & 1) ^ 1);       // what stood in this place has been read
         tc_fence_after();
         // (an address is a sum in a descriptor's low bits)
-        const uint64_t a = q_desc + (two ? group * (128 * D * 2 >> 4) : 0u), b = k_desc + (uint32_t)(kb.at * C::kOp + (two ? job >> 1 : job) * 8192 >> 4);
+        const uint64_t a = q_desc + (two ? group * (128 * D * 2 >> 4) : 0u), b = k_desc + (uint32_t)(kb.at * C::kOp + (two ? 1 - (job >> 1) : job) * 8192 >> 4);
         const uint32_t to = tmem + C::kS + 128 * group + 64 * place;
         if (elect_one()) {
 #pragma unroll
@@ -582,7 +587,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         const bool last = job == (two ? 3 : 1);
         const uint32_t group = n & 1, place = n >> 1 & 1;
         if (job == 0) wait(C::V_FULL + vb.at, vb.phase);
-        const uint64_t b = v_desc + (uint32_t)(vb.at * C::kOp + (two ? job >> 1 : job) * (D * 128) >> 4);
+        const uint64_t b = v_desc + (uint32_t)(vb.at * C::kOp + (two ? 1 - (job >> 1) : job) * (D * 128) >> 4);
         const uint32_t p_at = tmem + C::kS + 128 * group + 64 * place, more = in_item >= 2;         // not the item's first of this group
         wait(C::P_FULL + 2 * group + place, n >> 2 & 1);
         tc_fence_after();
@@ -732,7 +737,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
           }
           ring.next(2);
           vb.next();
-          first += kTile;
+          first -= kTile;
           ++done;
         }
       }
@@ -743,7 +748,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_at = tmem + lanes + C::kS + 128 * group, o_at = tmem + lanes + C::kO + D * group;
     float2* const ml = reinterpret_cast<float2*>(sgen + C::kOffML);
-    const float cap_in = p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f;
+    const float cap_in = p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f, cap_inverse = p.cap > 0.f ? __fdiv_rn(1.f, cap_out) : 0.f;
     int meet_phase = 0, done = 0;                                     // done: tiles of this CTA's run
     uint32_t n = 0;                                                   // jobs of this group
     // the group's last product on O.  (A barrier for each place: scores of a job say that the product before the last is done, so the last one is the
@@ -797,7 +802,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       const int mask_at = p.mask && it->g < 0 ? it->ctx : INT_MIN;    // where the drafted tokens begin
       bool have = false;                                              // a job of the item so far
       float m = -INFINITY, l0 = 0.f, l1 = 0.f, con = 0.f;
-      int first = it->first + (two ? 0 : 64 * group);                 // first key of the job
+      int first = it->first + (two ? 64 : 64 * group);                // first key of the job
       const int jobs = two ? 2 * tiles : tiles;
 #pragma unroll 1
       for (int i = 0; i < jobs; ++i) {
@@ -807,27 +812,32 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         if (warp_live) {
           const uint32_t s_job = s_at + 64 * place, held = valid_ring[done % C::kRing];
           if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
-          const bool plain = __all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + 64);
-          const bool change = ANY || !plain;
-          const float c2 = change ? 1.f : con;
-          // The reference moves to the largest score seen so far, which is looked for first: changed and masked scores are put back where they were.
+          // Does every row see every key (with a bias: of those before it)?  Otherwise scores are changed, masked and put back before anything else; so are capped
+          // scores beyond the polynomial's range.
+          bool change = !__all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + 64 && (!ANY || pos >= first + 63)) || (ANY && p.cap > 0.f);
+          // (by no row of the warp any of them: documents, the tile on the diagonal)
+          const bool unseen = rare(change) && mask_at < 0 && __all_sync(0xffffffffu, hi <= first || lo >= first + 64);
+          // The reference moves to the largest score seen so far.
           auto refer = [&] {
             float top = -INFINITY;
-            const int in_tile0 = two ? 64 * (i & 1) : 64 * group;
+            const int in_tile0 = two ? 64 - 64 * (i & 1) : 64 * group;
 #pragma unroll 1
             for (int k = c_first; k < c_end; ++k) {
               uint32_t a[16];
               tmem_ld_32x32b_x16(s_job + 16 * k, a);
+              const int at = first + 16 * k;
+              const float far = (float)(pos - at);
+              uint32_t seen = 0xFFFFu;
               if (change) {
-                const int at = first + 16 * k;
-                uint32_t seen = bits_between(lo - at, hi - at);
+                seen = bits_between(lo - at, hi - at);
                 if (mask_at >= 0) {
                   const int o = mask_at - at;
                   seen |= o >= 32 || o <= -64 ? 0u : (uint32_t)(o >= 0 ? mask << o : mask >> -o);
                 }
                 seen = held >> ((in_tile0 + 16 * k) >> log_page) & 1 ? seen : 0u;
-                const float far = (float)(pos - at);
-                tmem_wait_ld();
+              }
+              tmem_wait_ld();
+              if (ANY || change) {
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
                   float y = __uint_as_float(a[x]) * con;
@@ -835,9 +845,8 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
                   if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
                   a[x] = seen & 1u << x ? __float_as_uint(y) : 0xFF800000u;
                 }
-                tmem_st_32x32b_x16(s_job + 16 * k, a);
+                if (change) tmem_st_32x32b_x16(s_job + 16 * k, a);
               }
-              tmem_wait_ld();
               float t2 = -INFINITY;
 #pragma unroll
               for (int x = 0; x < 16; x += 4) {
@@ -846,10 +855,13 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               }
               top = fmaxf(top, t2);
             }
-            top *= c2;
-            if (CAP && plain) top = cap_score(top, cap_in, cap_out);
+            if (!ANY && !change) {
+              top *= con;
+              if (CAP) top = cap_score(top, cap_in, cap_out);
+            }
             if (change) tmem_wait_st();
-            if (__any_sync(0xffffffffu, top > m + kLag || m == -INFINITY)) {
+            if (m == -INFINITY) m = top;                              // (so far nothing: its sum and O are 0)
+            if (__any_sync(0xffffffffu, top > m + kLag)) {
               const float old = m;
               m = fmaxf(m, top);
               const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
@@ -871,20 +883,38 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               }
             }
           };
-          // probabilities of sixteen keys: eight words; the largest score above the reference (+ kShift), the sum
-          float over, s0, s1, shift;
-          auto sixteen = [&](const uint32_t* raw, uint32_t* h) {
+          // Probabilities of sixteen keys, eight words; the largest score above the reference (+ kShift), the sum.  HOW: scores times a constant; capped; with a
+          // bias that falls along the keys.
+          float over, wide, s0, s1, shift, c2;
+          auto sixteen = [&](auto how, const uint32_t* raw, int k, uint32_t* h) {
+            constexpr int HOW = decltype(how)::value;
 #pragma unroll
             for (int y = 0; y < 16; y += 8) {
               float z[8];
 #pragma unroll
               for (int x = 0; x < 8; x += 2) {
-                if (CAP && plain) {
-                  z[x] = cap_score(__uint_as_float(raw[y + x]) * con, cap_in, cap_out) + shift;
-                  z[x + 1] = cap_score(__uint_as_float(raw[y + x + 1]) * con, cap_in, cap_out) + shift;
+                const float r0 = __uint_as_float(raw[y + x]), r1 = __uint_as_float(raw[y + x + 1]);
+                if (HOW == kCapped) {
+                  // tanh u = u P(u^2) to 2^-21 for |u| up to 1.25 (P: least maximum error, by Lawson's weights): nine multiply-adds for two scores,
+                  // where an exponential and a reciprocal each are 32 clocks of the special-function unit for a warp, as much again as exp2 twice over
+                  float u0, u1, w0, w1, t0, t1;
+                  mul_pair(u0, u1, r0, r1, c2, c2);
+                  mul_pair(w0, w1, u0, u1, u0, u1);
+                  wide = max3(wide, w0, w1);
+                  fma_pair(t0, t1, w0, w1, 5.25480427e-4f, 5.25480427e-4f, -4.32547880e-3f, -4.32547880e-3f);
+                  fma_pair(t0, t1, t0, t1, w0, w1, 1.76362153e-2f, 1.76362153e-2f);
+                  fma_pair(t0, t1, t0, t1, w0, w1, -5.16446717e-2f, -5.16446717e-2f);
+                  fma_pair(t0, t1, t0, t1, w0, w1, 1.32648021e-1f, 1.32648021e-1f);
+                  fma_pair(t0, t1, t0, t1, w0, w1, -3.33242148e-1f, -3.33242148e-1f);
+                  fma_pair(t0, t1, t0, t1, w0, w1, 9.99996483e-1f, 9.99996483e-1f);
+                  mul_pair(u0, u1, u0, u1, cap_out, cap_out);
+                  fma_pair(z[x], z[x + 1], t0, t1, u0, u1, shift, shift);
+                } else if (HOW == kBiased) {
+                  float b0, b1;
+                  fma_pair(b0, b1, slope, slope, (float)(16 * k + y + x), (float)(16 * k + y + x + 1), shift, shift);
+                  fma_pair(z[x], z[x + 1], r0, r1, c2, c2, b0, b1);
                 } else {
-                  const uint32_t cc = __float_as_uint(c2), ss = __float_as_uint(shift);
-                  fma_pair(z[x], z[x + 1], raw[y + x], raw[y + x + 1], cc, cc, ss, ss);
+                  fma_pair(z[x], z[x + 1], r0, r1, c2, c2, shift, shift);
                 }
                 over = max3(over, z[x], z[x + 1]);
                 z[x] = exp2_approx(z[x]);
@@ -900,56 +930,72 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               }
             }
           };
-          // Scores rarely exceed their reference: it is looked for first where there is none yet or scores change, and in all other jobs only
-          // when they have turned out to; then the job is done again.
+          // Scores rarely exceed their reference: the largest is looked for first where there is none yet or scores have to be changed, and in all other
+          // jobs only when they have turned out to; then the job is done again.
           bool sure = change || __any_sync(0xffffffffu, m == -INFINITY);
-          if (ROWS > 128 || copies == 1) {
-            uint32_t h[32];
+          s0 = s1 = 0.f;
+          auto attempt = [&](auto pass) {
 #pragma unroll 1
             while (true) {
               if (rare(sure)) refer();
               shift = m == -INFINITY ? 0.f : kShift - m;
               over = -INFINITY;
-              s0 = s1 = 0.f;
+              s0 = s1 = wide = 0.f;
+              if (SCORES == kScaled || rare(change)) {
+                c2 = change ? 1.f : con;
+                pass(std::integral_constant<int, kScaled>());
+              } else {
+                c2 = CAP ? con * cap_inverse : con;
+                if (ANY) shift -= slope * (float)(pos - first);
+                pass(std::integral_constant<int, SCORES>());
+                if (CAP && rare(__any_sync(0xffffffffu, wide > 1.25f * 1.25f))) {
+                  change = sure = true;
+                  continue;
+                }
+              }
+              if (sure || !rare(__any_sync(0xffffffffu, over > kLag + kShift))) break;
+              sure = true;
+            }
+          };
+          if (unseen) {
+            uint32_t h[16];
+#pragma unroll
+            for (int x = 0; x < 16; ++x) h[x] = 0u;
+            tmem_st_32x32b_x16(s_job, h);
+            tmem_st_32x32b_x16(s_job + 16, h);
+          } else if (ROWS > 128 || copies == 1) {
+            uint32_t h[32];
+            attempt([&](auto how) {
               uint32_t a[16], c[16];
               tmem_ld_32x32b_x16(s_job, a);
               tmem_wait_ld();
               tmem_ld_32x32b_x16(s_job + 16, c);
-              sixteen(a, h);
+              sixteen(how, a, 0, h);
               tmem_wait_ld();
               tmem_ld_32x32b_x16(s_job + 32, a);
-              sixteen(c, h + 8);
+              sixteen(how, c, 1, h + 8);
               tmem_wait_ld();
               tmem_ld_32x32b_x16(s_job + 48, c);
-              sixteen(a, h + 16);
+              sixteen(how, a, 2, h + 16);
               tmem_wait_ld();
-              sixteen(c, h + 24);
-              if (sure || !rare(__any_sync(0xffffffffu, over > kLag + kShift))) break;
-              sure = true;
-            }
+              sixteen(how, c, 3, h + 24);
+            });
             tmem_st_32x32b_x16(s_job, h);                             // (over scores that have been read)
             tmem_st_32x32b_x16(s_job + 16, h + 16);
           } else {
             // (two pieces at most: what the one before the last has to store waits)
             uint32_t h[16];
-#pragma unroll 1
-            while (true) {
-              if (rare(sure)) refer();
-              shift = m == -INFINITY ? 0.f : kShift - m;
-              over = -INFINITY;
-              s0 = s1 = 0.f;
+            attempt([&](auto how) {
               uint32_t a[16];
               tmem_ld_32x32b_x16(s_job + 16 * c_first, a);
               tmem_wait_ld();
-              sixteen(a, h);
+              sixteen(how, a, c_first, h);
               if (copies == 2) {
                 tmem_ld_32x32b_x16(s_job + 16 * c_first + 16, a);
                 tmem_wait_ld();
-                sixteen(a, h + 8);
+                sixteen(how, a, c_first + 1, h + 8);
               }
-              if (sure || !rare(__any_sync(0xffffffffu, over > kLag + kShift))) break;
-              sure = true;
-            }
+            });
             tmem_st_32x32b_x8(s_job + 8 * c_first, h);
             if (copies == 2) tmem_st_32x32b_x8(s_job + 8 * c_first + 8, h + 8);
 #pragma unroll
@@ -968,7 +1014,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         have = true;
         ++n;
         const bool tile_done = !two || (i & 1);
-        first += two ? 64 : kTile;
+        first -= two ? 64 : kTile;
         done += tile_done;
       }
       // ---- end of the item, or of this CTA's part of it
@@ -1327,7 +1373,7 @@ int launch_scores(const PagedParams& p, const FewRows* own, void* own_workspace,
   const long long rows = (long long)p.B * p.H * p.T;
   if (e == cudaSuccess)
     e = p.groups ? launch_overlapped(shared_join_kernel<D, C::kRows>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), kJoinThreads, 0, st, joined)
-                 : launch_overlapped(join_kernel<D, C::kRows>, dim3(grid, (unsigned)std::min(8, (std::min(p.group * p.T, C::kRows) + 7) / 8)), kJoinThreads, 0, st, p);
+                 : launch_overlapped(join_kernel<D, C::kRows>, dim3(grid, (unsigned)(std::min(p.group * p.T, C::kRows) + 7) / 8), kJoinThreads, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
 template <int FMT, int D, int RT>
