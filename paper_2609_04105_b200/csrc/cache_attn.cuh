@@ -10,7 +10,6 @@ struct FewRows {
   const fp4attn_view* q;
   CacheRef cache;
   const int *context, *count, *first, *last;
-  const unsigned long long* mask;
   const float* slopes;
   void* out;
   float* lse;
@@ -21,14 +20,6 @@ struct FewRows {
 bool few_rows(int rows, int fmt, int d);
 size_t few_rows_workspace(int B, int H, int kv_heads, int T, int d, int fmt);
 int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st);
-// Rows of a tree (any number of them) whose results are to be joined with others': whole items in raw and raw_ml ([B, H, T]), items in parts as `own` says.
-struct OwnParts {
-  const float* part;                   // [2 * CTAs][rows][d]
-  const float2* part_ml;               // [2 * CTAs][rows]: reference, sum
-  const int2* split;                   // [B, KV heads, row tiles]: first and last CTA of an item; first = -1: whole
-  int rows, row_tiles, most_ctas;      // rows of a tile
-};
-int launch_own_rows(const FewRows& a, void* workspace, float* raw, float2* raw_ml, OwnParts* own, cudaStream_t st);
 int check_cache(const fp4attn_cache* c, int B, const int* block_table, int max_pages, const int* start, const int* count, CacheRef* ref);
 
 namespace {

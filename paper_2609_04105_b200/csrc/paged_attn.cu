@@ -64,8 +64,6 @@ struct PagedParams {
   int B, H, T, group, row_tiles;           // row_tiles: of a sequence's rows
   unsigned long long by_group, by_tokens;  // for divide()
   float scale, cap;
-  OwnParts own;                            // shared, of sequences by themselves, where they are not items of this kernel
-  bool own_items;                          // shared: are they?
   bool half, q_vector, out_wide;           // out_wide: O begins at a multiple of 32 bytes
 };
 
@@ -114,6 +112,8 @@ struct PagedCfg {
          PV_DONE = P_FULL + 4, DRAIN = PV_DONE + 4, MEET = DRAIN + 2, RING_FULL, RING_FREE = RING_FULL + kStages, ITEM = RING_FREE + kStages, kBars = ITEM + kItems };
   static_assert(kBars * 8 + 16 <= 1024, "barriers");
   static constexpr int kS = 0, kO = 256;                           // tensor memory: scores (and P) of the two groups, their O
+  // a group's two places for scores; with the same rows for both, those of a tile are neighbours
+  __device__ static constexpr uint32_t scores_at(uint32_t group, uint32_t place) { return kS + (RT == 1 ? 128 * place + 64 * group : 128 * group + 64 * place); }
 };
 
 // tokens that entry b has
@@ -202,7 +202,7 @@ __device__ __forceinline__ int divide(int n, unsigned long long m) { return (int
 
 // This CTA's run of the list, in units: a tile is one, and an item that many more (bringing Q, writing O), which come before its tiles.  x, the run's
 // first unit among x's, how many, the first one's number in the list, all units, CTAs.  Barriers of the block.
-constexpr int kItemCost = 2;
+constexpr int kItemCost = 4;
 struct Run {
   int x;
   long long at, tiles, first, total, ctas;
@@ -210,7 +210,7 @@ struct Run {
 template <int ROWS, int THREADS>
 __device__ __forceinline__ Run find_run(const PagedParams& p, long long* scan, long long* find) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int X = p.groups ? p.groups + (p.own_items ? p.B : 0) : p.B * p.row_tiles;
+  const int X = p.groups ? p.groups + p.B : p.B * p.row_tiles;
   const int per = (X + THREADS - 1) / THREADS, x0 = min(X, (int)threadIdx.x * per), x1 = min(X, x0 + per);
   Desc d;
   auto tiles = [&](int x) {
@@ -545,7 +545,42 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         --tiles;
       }
     };
-    if (warp == C::kIssuerS) {
+    if (warp == C::kIssuerS && RT == 1) {
+      // Both groups have the same rows and a half of the keys each: one product of N = 128 for both (eight of 64 clocks instead of sixteen, which take more to
+      // issue than to compute: a tile of few rows 2800 -> SMALLTILE clocks)
+      constexpr uint32_t kIdesc = make_idesc_f16(128, kTile, false);
+      const uint64_t q_desc = make_smem_desc(sbase + C::kOffQ, 16, 1024, kSwz128), k_desc = make_smem_desc(sbase + C::kOffK, 16, 1024, kSwz128);
+      Turn<C::kKB> kb;
+      int q_phase = 0;
+#pragma unroll 1
+      while (another()) {
+        const uint32_t place = n & 1;
+        if (rare(in_item == 0)) {
+          wait(C::Q_FULL, q_phase);
+          q_phase ^= 1;
+        }
+        wait(C::K_FULL + kb.at, kb.phase);
+        wait(C::PV_DONE + place, (n >> 1 & 1) ^ 1);                   // what stood in this place has been read
+        wait(C::PV_DONE + 2 + place, (n >> 1 & 1) ^ 1);
+        tc_fence_after();
+        const uint64_t b = k_desc + (uint32_t)(kb.at * C::kOp >> 4);
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const int at = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
+            tc_mma_f16(tmem + C::kS + 128 * place, q_desc + at, b + at, kIdesc, k > 0);
+          }
+          tc_commit(bar(C::S_FULL + place));
+          tc_commit(bar(C::K_FREE + kb.at));
+          if (tiles == 1) tc_commit(bar(C::Q_FREE));
+        }
+        __syncwarp();
+        kb.next();
+        ++n;
+        in_item = 1;
+        --tiles;
+      }
+    } else if (warp == C::kIssuerS) {
       constexpr uint32_t kIdesc = make_idesc_f16(128, 64, false);
       const uint64_t q_desc = make_smem_desc(sbase + C::kOffQ, 16, 1024, kSwz128), k_desc = make_smem_desc(sbase + C::kOffK, 16, 1024, kSwz128);
       Turn<C::kKB> kb;
@@ -563,7 +598,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         tc_fence_after();
         // (an address is a sum in a descriptor's low bits)
         const uint64_t a = q_desc + (two ? group * (128 * D * 2 >> 4) : 0u), b = k_desc + (uint32_t)(kb.at * C::kOp + (two ? 1 - (job >> 1) : job) * 8192 >> 4);
-        const uint32_t to = tmem + C::kS + 128 * group + 64 * place;
+        const uint32_t to = tmem + C::scores_at(group, place);
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
@@ -588,7 +623,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         const uint32_t group = n & 1, place = n >> 1 & 1;
         if (job == 0) wait(C::V_FULL + vb.at, vb.phase);
         const uint64_t b = v_desc + (uint32_t)(vb.at * C::kOp + (two ? 1 - (job >> 1) : job) * (D * 128) >> 4);
-        const uint32_t p_at = tmem + C::kS + 128 * group + 64 * place, more = in_item >= 2;         // not the item's first of this group
+        const uint32_t p_at = tmem + C::scores_at(group, place), more = in_item >= 2;         // not the item's first of this group
         wait(C::P_FULL + 2 * group + place, n >> 2 & 1);
         tc_fence_after();
         if (elect_one()) {
@@ -746,7 +781,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     // ===================================================================== softmax
     const int group = (warp - C::kFirstSoftmax) >> 2, quarter = warp & 3, in_tile = quarter * 32 + lane;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const uint32_t s_at = tmem + lanes + C::kS + 128 * group, o_at = tmem + lanes + C::kO + D * group;
+    const uint32_t o_at = tmem + lanes + C::kO + D * group;
     float2* const ml = reinterpret_cast<float2*>(sgen + C::kOffML);
     const float cap_in = p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f, cap_inverse = p.cap > 0.f ? __fdiv_rn(1.f, cap_out) : 0.f;
     int meet_phase = 0, done = 0;                                     // done: tiles of this CTA's run
@@ -807,10 +842,10 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
 #pragma unroll 1
       for (int i = 0; i < jobs; ++i) {
         const uint32_t place = n & 1;
-        wait(C::S_FULL + 2 * group + place, n >> 1 & 1);
+        wait(C::S_FULL + (RT == 1 ? 0 : 2 * group) + place, n >> 1 & 1);
         tc_fence_after();
         if (warp_live) {
-          const uint32_t s_job = s_at + 64 * place, held = valid_ring[done % C::kRing];
+          const uint32_t s_job = tmem + lanes + C::scores_at(group, place), held = valid_ring[done % C::kRing];
           if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
           // Does every row see every key (with a bias: of those before it)?  Otherwise scores are changed, masked and put back before anything else; so are capped
           // scores beyond the polynomial's range.
@@ -1290,16 +1325,7 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const PagedPa
   }
   const int b0 = load(p.group_start + g);
   if (b >= b0 && b < load(p.group_start + g + 1)) take(g, ((b - max(0, b0)) * p.T + t) * p.group + hl);
-  if (p.own_items) {
-    take(p.groups + b, t * p.group + hl);
-  } else {
-    const int row = hl * p.T + t;                                   // (heads first)
-    const int2 ctas = p.own.split[((size_t)b * p.cache.kv_heads + kvh) * p.own.row_tiles + row / p.own.rows];
-    Sum<D> s;
-    if (ctas.x < 0) s.one(p.whole + (all + at) * D, p.whole_ml[all + at], lane);
-    else if (ctas.y >= ctas.x && ctas.y < p.own.most_ctas) s.parts(p.own.part, p.own.part_ml, p.own.rows, ctas.x, ctas.y, row % p.own.rows, lane);
-    sum.add(s);
-  }
+  take(p.groups + b, t * p.group + hl);
   sum.give(p, (size_t)at, kvh, lane);
 }
 
@@ -1327,13 +1353,15 @@ __global__ void __launch_bounds__(128) range_kernel(const PagedParams p, int2* r
 // ---- workspace
 struct Plan {
   int rt, row_tiles;                       // 128-row halves of an item; items of a sequence's rows
-  size_t ml, begun, ranges, split, whole, whole_ml, own, total;
+  size_t ml, begun, ranges, split, whole, whole_ml, total;
 };
 size_t align32(size_t x) { return (x + 31) & ~(size_t)31; }
-Plan plan(int B, int H, int kv_heads, int T, int d, int groups, bool own_items = false) {
+Plan plan(int B, int H, int kv_heads, int T, int d, int groups) {
   Plan t;
   const long long rows = (long long)(H / kv_heads) * T;
-  t.rt = (!groups ? rows : own_items ? 0 : rows * B / groups) > 128 ? 2 : 1;
+  // (a sequence by itself has few rows, and instances for those keep copies of them: prefixes go along.  shared_batch, whose prefix has 192 rows: 80 us with
+  // 256 rows an item, LESS with 128)
+  t.rt = !groups && rows > 128 ? 2 : 1;
   const long long R = 128 * t.rt, all = (long long)B * H * T;
   t.row_tiles = (int)((rows + R - 1) / R);
   const size_t slots = 2 * (size_t)kMostCtas * R;
@@ -1343,12 +1371,12 @@ Plan plan(int B, int H, int kv_heads, int T, int d, int groups, bool own_items =
   t.split = t.ranges + (groups ? 0 : align32((size_t)B * t.row_tiles * 8));
   t.whole = t.split + (groups ? align32((size_t)(B * rows / R + groups + 1 + (long long)B * t.row_tiles) * kv_heads * 8) : 0);
   t.whole_ml = t.whole + (groups ? (size_t)(2 * all) * d * 4 : 0);
-  t.own = t.total = t.whole_ml + (groups ? align32((size_t)(2 * all) * 8) : 0);
+  t.total = t.whole_ml + (groups ? align32((size_t)(2 * all) * 8) : 0);
   return t;
 }
 
 template <int FMT, int D, int RT, int SCORES>
-int launch_scores(const PagedParams& p, const FewRows* own, void* own_workspace, cudaStream_t st) {
+int launch_scores(const PagedParams& p, cudaStream_t st) {
   using C = PagedCfg<FMT, D, RT>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FP4ATTN_ERR_CUDA;
@@ -1364,25 +1392,18 @@ int launch_scores(const PagedParams& p, const FewRows* own, void* own_workspace,
   if (p.ranges)
     e = launch_overlapped(range_kernel<C::kRows>, dim3((unsigned)((p.B * p.row_tiles + 3) / 4)), 128u, 0, st, p, const_cast<int2*>(p.ranges));
   if (e == cudaSuccess) e = launch_overlapped(paged_kernel<FMT, D, RT, SCORES>, dim3(grid), C::kThreads, C::kSmem, st, p);
-  if (e != cudaSuccess) return FP4ATTN_ERR_CUDA;
-  PagedParams joined = p;
-  if (own) {
-    const int rc = launch_own_rows(*own, own_workspace, p.whole + (size_t)p.B * p.H * p.T * D, p.whole_ml + (size_t)p.B * p.H * p.T, &joined.own, st);
-    if (rc != FP4ATTN_OK) return rc;
-  }
   const long long rows = (long long)p.B * p.H * p.T;
   if (e == cudaSuccess)
-    e = p.groups ? launch_overlapped(shared_join_kernel<D, C::kRows>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), kJoinThreads, 0, st, joined)
+    e = p.groups ? launch_overlapped(shared_join_kernel<D, C::kRows>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), kJoinThreads, 0, st, p)
                  : launch_overlapped(join_kernel<D, C::kRows>, dim3(grid, (unsigned)(std::min(p.group * p.T, C::kRows) + 7) / 8), kJoinThreads, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
 template <int FMT, int D, int RT>
-int launch_rows(const PagedParams& p, const FewRows* own, void* own_workspace, cudaStream_t st) {
-  if (p.slopes) return launch_scores<FMT, D, RT, kBiased>(p, own, own_workspace, st);
-  return p.cap > 0.f ? launch_scores<FMT, D, RT, kCapped>(p, own, own_workspace, st) : launch_scores<FMT, D, RT, kScaled>(p, own, own_workspace, st);
+int launch_rows(const PagedParams& p, cudaStream_t st) {
+  if (p.slopes) return launch_scores<FMT, D, RT, kBiased>(p, st);
+  return p.cap > 0.f ? launch_scores<FMT, D, RT, kCapped>(p, st) : launch_scores<FMT, D, RT, kScaled>(p, st);
 }
-// own: shared prefixes, sequences by themselves in a kernel of their own
-int launch(PagedParams& p, const Plan& t, const FewRows* own, void* workspace, int fmt, int d, cudaStream_t st) {
+int launch(PagedParams& p, const Plan& t, void* workspace, int fmt, int d, cudaStream_t st) {
   char* const ws = (char*)workspace;
   p.row_tiles = t.row_tiles;
   auto reciprocal = [](int n) { return ((1ull << 36) + n - 1) / n; };
@@ -1400,7 +1421,7 @@ int launch(PagedParams& p, const Plan& t, const FewRows* own, void* workspace, i
     if (p.first || p.last) p.ranges = (const int2*)(ws + t.ranges);
   }
   auto rows = [&](auto fmt_c, auto d_c) {
-    return t.rt == 2 ? launch_rows<fmt_c.value, d_c.value, 2>(p, own, ws + t.own, st) : launch_rows<fmt_c.value, d_c.value, 1>(p, own, ws + t.own, st);
+    return t.rt == 2 ? launch_rows<fmt_c.value, d_c.value, 2>(p, st) : launch_rows<fmt_c.value, d_c.value, 1>(p, st);
   };
   using std::integral_constant;
   if (fmt == FP4ATTN_FMT_NVFP4)
@@ -1464,19 +1485,16 @@ extern "C" int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp
   if ((uintptr_t)workspace & 31) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   if (few_rows(H / cache->kv_heads * T, cache->fmt, cache->d)) {
-    const FewRows a = {q, p.cache, context, count, first, last, nullptr, slopes, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, p.cap};
+    const FewRows a = {q, p.cache, context, count, first, last, slopes, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, p.cap};
     return launch_few_rows(a, workspace, (cudaStream_t)stream);
   }
   p.first = first; p.last = last;
-  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, 0), nullptr, workspace, cache->fmt, cache->d, (cudaStream_t)stream);
+  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, 0), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
 }
 
 extern "C" size_t fp4attn_shared_prefix_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d, int groups) {
   if (groups <= 0 || groups > 65535 || T > FP4ATTN_MOST_TREE_TOKENS) return 0;
-  if (!fp4attn_paged_attention_workspace_bytes(B, H, kv_heads, T, d)) return 0;
-  // (the size does not depend on which way a call goes)
-  return std::max(plan(B, H, kv_heads, T, d, groups).total + fp4attn_tree_attention_workspace_bytes(B, H, kv_heads, T, d),
-                  plan(B, H, kv_heads, T, d, groups, true).total);
+  return fp4attn_paged_attention_workspace_bytes(B, H, kv_heads, T, d) ? plan(B, H, kv_heads, T, d, groups).total : 0;
 }
 
 extern "C" int fp4attn_shared_prefix_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, int groups,
@@ -1495,9 +1513,5 @@ extern "C" int fp4attn_shared_prefix_attention(const fp4attn_view* q, int type, 
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
   p.groups = groups; p.prefix_table = prefix_table; p.prefix_pages = prefix_pages; p.prefix_length = prefix_length; p.group_start = group_start;
   p.mask = tree_mask;
-  // Sequences by themselves have few rows each, which the kernels of attention over a tree are made for: 48 sequences of up to 900 tokens behind one of
-  // 16000 OLDNEW us.  Those know no caps and biases: then they are items like the prefixes.
-  p.own_items = slopes || soft_cap > 0.f;
-  const FewRows own = {q, p.cache, context, count, nullptr, nullptr, tree_mask, nullptr, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, 0.f};
-  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, groups, p.own_items), p.own_items ? nullptr : &own, workspace, cache->fmt, cache->d, (cudaStream_t)stream);
+  return launch(p, plan(B, H, cache->kv_heads, T, cache->d, groups), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
 }

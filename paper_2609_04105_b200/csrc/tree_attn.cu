@@ -63,9 +63,6 @@ struct TreeParams {
   const int *seen_from, *seen_until;       // [B, T] or null
   const float* slopes;
   float cap;
-  // of fp4attn_shared_prefix_attention: whole items are left as partial results, and nothing is joined
-  float* raw;                              // [B, H, T, d] or null
-  float2* raw_ml;                          // [B, H, T]
 };
 
 // ---- what a CTA walks: tiles of items, in order.  The roles of a scheduler run in turn and each is one chain of instructions, so a tile
@@ -888,9 +885,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
           }
           const int row = row0 + key;
           float inv = 1.f;
-          if (whole && p.raw) {
-            if (row < p.rows && row % p.T < n) p.raw_ml[out0 + row] = make_float2(top, total_l);
-          } else if (whole) {
+          if (whole) {
             inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * load(p.cache.v_G + kvh));     // nothing seen: 0, not 0 / 0
             if (p.lse && row < p.rows && row % p.T < n)
               p.lse[out0 + row] = total_l == 0.f ? -INFINITY : (top - kShift + log2f(total_l)) * 0.6931471805599453f;
@@ -928,12 +923,7 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
         if (C::kSets > 1) bar_sync(id_all, 128 * C::kSets);         // the next item's products may overwrite either O
         const uint32_t keep = __ballot_sync(0xffffffffu, lane < M && row0 + r0 + lane < p.rows && (row0 + r0 + lane) % p.T < n);
         if (key < D) {
-          if (whole && p.raw) {
-            float* const dst = p.raw + (size_t)(out0 + row0 + r0) * D + key;
-#pragma unroll
-            for (int r = 0; r < M; ++r)
-              if (keep >> r & 1) dst[r * D] = o[r];
-          } else if (whole) {
+          if (whole) {
             uint16_t* const dst = static_cast<uint16_t*>(p.out) + (size_t)(out0 + row0 + r0) * D + key;
 #pragma unroll
             for (int r = 0; r < M; ++r) {
@@ -1435,12 +1425,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
                 total_l += f * ml.y;
                 y[0] = fmaf(f, v.x, y[0]); y[1] = fmaf(f, v.y, y[1]); y[2] = fmaf(f, v.z, y[2]); y[3] = fmaf(f, v.w, y[3]);
               }
-              if (whole && p.raw) {
-                if (row % p.T < n_drafted) {
-                  *reinterpret_cast<float4*>(p.raw + (size_t)(out0 + row) * D + e) = make_float4(y[0], y[1], y[2], y[3]);
-                  if (e == 0) p.raw_ml[out0 + row] = make_float2(top_m, total_l);
-                }
-              } else if (whole) {
+              if (whole) {
                 if (row % p.T < n_drafted) {
                   const float inv = total_l == 0.f ? 0.f : __fdiv_rn(1.f, total_l * load(p.cache.v_G + kvh));     // nothing seen: 0
                   const uint2 h = p.half ? make_uint2(pack_pair<__half>(y[0] * inv, y[1] * inv), pack_pair<__half>(y[2] * inv, y[3] * inv))
@@ -1570,7 +1555,7 @@ int launch_tree(const TreeParams& p, cudaStream_t st) {
   const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * units;
   const unsigned grid = (unsigned)std::min<long long>(std::min(sms, kMostCtas<R>), most_tiles);
   cudaError_t e = launch_overlapped(tree_kernel<FMT, D, R>, dim3(grid), C::kThreads, C::kSmem, st, p);
-  if (e == cudaSuccess && !p.raw)
+  if (e == cudaSuccess)
     e = launch_overlapped(tree_join_kernel<D, R>, dim3((unsigned)(p.B * units), (unsigned)(std::min(R, p.rows) + 3) / 4), 128u, 0, st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
@@ -1589,7 +1574,7 @@ int launch_warps(const TreeParams& p, cudaStream_t st) {
   const long long most_tiles = (((long long)p.cache.max_pages << p.cache.log_page) + kTile - 1) / kTile * p.B * p.cache.kv_heads * p.row_tiles;
   const unsigned grid = (unsigned)std::min<long long>(std::min(C::kCtas * sms, kMostCtas<C::R>), most_tiles);
   cudaError_t e = launch_overlapped(tree_warp_kernel<FMT, D, NT, PAGED>, dim3(grid), C::kThreads, C::kSmem, st, p);
-  if (e == cudaSuccess && !p.raw)
+  if (e == cudaSuccess)
     e = launch_overlapped(tree_join_kernel<D, C::R>, dim3((unsigned)(p.B * p.cache.kv_heads * p.row_tiles), (unsigned)(std::min(p.rows, C::R) + 3) / 4), 128u, 0,
                           st, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
@@ -1613,14 +1598,14 @@ int launch_few(const TreeParams& p, int R, bool changed, cudaStream_t st) {
 
 bool few_rows(int rows, int fmt, int d) { return rows_of_tile(rows, fmt, d) <= 16; }
 size_t few_rows_workspace(int B, int H, int kv_heads, int T, int d, int fmt) { return plan(B, H, kv_heads, T, d, fmt).total; }
-namespace {
-TreeParams params_of(const FewRows& a, const TreePlan& t, void* workspace) {
+int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st) {
+  const TreePlan t = plan(a.B, a.H, a.cache.kv_heads, a.T, a.d, a.fmt);
   TreeParams p = {};
   p.q = a.q->data; p.q_sb = a.q->stride_b; p.q_sh = a.q->stride_h; p.q_sn = a.q->stride_n;
   p.q_vector = view_vectors(*a.q, 2);
   p.half = a.type == FP4ATTN_TYPE_FP16;
   p.cache = a.cache;
-  p.context = a.context; p.count = a.count; p.mask = a.mask;
+  p.context = a.context; p.count = a.count;
   p.out = a.out; p.lse = a.lse; p.status = a.status;
   p.B = a.B; p.H = a.H; p.T = a.T; p.group = a.H / a.cache.kv_heads;
   p.rows = p.group * a.T;
@@ -1630,26 +1615,10 @@ TreeParams params_of(const FewRows& a, const TreePlan& t, void* workspace) {
   p.part = (float*)workspace;
   p.part_ml = (float2*)((char*)workspace + t.ml);
   p.split = (int2*)((char*)workspace + t.split);
-  return p;
-}
-}  // namespace
-int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st) {
-  const TreePlan t = plan(a.B, a.H, a.cache.kv_heads, a.T, a.d, a.fmt);
-  const TreeParams p = params_of(a, t, workspace);
   const bool changed = a.first || a.last || a.slopes || a.cap > 0.f;        // (else it is attention over a tree in which every token sees those before it)
   if (a.fmt == FP4ATTN_FMT_NVFP4) return a.d == 64 ? launch_few<FP4ATTN_FMT_NVFP4, 64>(p, t.R, changed, st) : launch_few<FP4ATTN_FMT_NVFP4, 128>(p, t.R, changed, st);
   return a.d == 64 ? launch_few<FP4ATTN_FMT_E4M3, 64>(p, t.R, changed, st) : launch_few<FP4ATTN_FMT_E4M3, 128>(p, t.R, changed, st);
 }
-int launch_own_rows(const FewRows& a, void* workspace, float* raw, float2* raw_ml, OwnParts* own, cudaStream_t st) {
-  const TreePlan t = plan(a.B, a.H, a.cache.kv_heads, a.T, a.d, a.fmt);
-  TreeParams p = params_of(a, t, workspace);
-  p.raw = raw;
-  p.raw_ml = raw_ml;
-  *own = {p.part, p.part_ml, p.split, t.R, t.row_tiles, t.R <= 16 ? kMostWarpCtas : kMostRoleCtas};
-  if (a.fmt == FP4ATTN_FMT_NVFP4) return a.d == 64 ? launch_rows<FP4ATTN_FMT_NVFP4, 64>(p, t.R, st) : launch_rows<FP4ATTN_FMT_NVFP4, 128>(p, t.R, st);
-  return a.d == 64 ? launch_rows<FP4ATTN_FMT_E4M3, 64>(p, t.R, st) : launch_rows<FP4ATTN_FMT_E4M3, 128>(p, t.R, st);
-}
-
 }  // namespace fp4attn
 
 using namespace fp4attn;
