@@ -3,19 +3,27 @@
 // Row (b, h, t) at position p sees keys [first, last), clipped to the keys that are there.  With s the scaled product of q and a key,
 //     x = cap tanh(s / cap) (if capped) - slope_h |p - j|,   O = sum_j e^(x_j - m) v_j / sum_j e^(x_j - m),   LSE = m + ln sum_j e^(x_j - m).
 //
-// Rows are in lanes: S = Q K^T (128 rows x 128 keys), O += P V (128 rows x d), both on the fifth-generation tensor core with fp32 sums in tensor
+// Rows are in lanes: S = Q K^T (128 rows x 64 or 128 keys), O += P V (128 rows x d), both on the fifth-generation tensor core with fp32 sums in tensor
 // memory.  The rows that read one KV head (tokens x heads of its group, tokens first) are an item's, 256 at a time or, where there are no more,
 // 128.  A row's maximum and sum then belong to one thread, and a key is converted once for all rows of the item:
 //
-//   producer   pages of a tile of 128 keys -> a ring of stages, K and V by themselves: one bulk copy a page
-//   K          codes -> f16 (exact) -> shared memory, a key a row; Q of an item, a power of two per row, -> f16 -> shared memory
+//   producer   items, and the pages of a tile of 128 keys -> a ring of stages, K and V by themselves: one bulk copy a page
+//   K          codes -> f16 (exact) -> shared memory, a key a row
 //   V          codes -> f16 (exact) -> shared memory, V^T: an index of the head dimension a row
-//   issuers    of S and of O, of two softmax groups in turn
+//              both: Q of an item, times a power of two per row, -> f16 -> shared memory
+//   issuers    of S and of O
 //   softmax    two groups of 128 threads, a thread a row: scores -> P, f16, over its own scores in tensor memory, where the product reads it
 //
-// Two groups because a tile is one long chain (scores - maximum - exp2 - P - product): while one waits for its products the other has the
-// exponential unit.  Items of more than 128 rows give each group half of the rows; those of fewer give the groups tiles in turn, with references,
-// sums and an O each, joined at the item's end.
+// A job of a softmax group is 64 keys, and it has two places for their scores, so that those of the next job are there when it comes to them (with one place of
+// 128 it stood still for two products in between: a chunk of 2048 tokens 1229 us instead of 1112).  Items of more than 128 rows give each group half of the
+// rows; those of fewer give it half of the keys of a tile, with a reference, a sum and an O of its own, joined at the item's end.
+//
+// Few rows (up to 16 a KV head; up to 8 in NVFP4 with d = 128) go to the kernel of warps in tree_attn.cu, but for shared prefixes.
+//
+// What bounds it: instructions.  A softmax warp executes one about every five clocks (waits, branches and instruction fetches among them), a job of 64
+// keys is some 250, and an item costs as much as three or four tiles (bringing Q, the first references, writing O).  2048 tokens of 32 heads over 8 behind 30720, d = 128,
+// NVFP4: 1.05 to 1.12 ms, 960 to 1020 TFLOP/s (power: 1780 MHz); two prompts of 4096: 366 us, 750 TFLOP/s.  Beside the products of N = 64, whose operands
+// come from shared memory (48 clocks instead of 32) and which take longer to issue than to compute (90), exponentials do not count: without them nothing changes.
 //
 // A row's keys are walked from its last to its first: what a mask cuts off comes where a reference has to be looked for anyway, and a bias by distance falls
 // from there on, so that references do not move.
@@ -202,7 +210,7 @@ __device__ __forceinline__ int divide(int n, unsigned long long m) { return (int
 
 // This CTA's run of the list, in units: a tile is one, and an item that many more (bringing Q, writing O), which come before its tiles.  x, the run's
 // first unit among x's, how many, the first one's number in the list, all units, CTAs.  Barriers of the block.
-constexpr int kItemCost = 4;
+constexpr int kItemCost = 3;
 struct Run {
   int x;
   long long at, tiles, first, total, ctas;
@@ -547,7 +555,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     };
     if (warp == C::kIssuerS && RT == 1) {
       // Both groups have the same rows and a half of the keys each: one product of N = 128 for both (eight of 64 clocks instead of sixteen, which take more to
-      // issue than to compute: a tile of few rows 2800 -> SMALLTILE clocks)
+      // issue than to compute: 40 sequences of 5 drafted tokens behind six prefixes 43 -> 38 us)
       constexpr uint32_t kIdesc = make_idesc_f16(128, kTile, false);
       const uint64_t q_desc = make_smem_desc(sbase + C::kOffQ, 16, 1024, kSwz128), k_desc = make_smem_desc(sbase + C::kOffK, 16, 1024, kSwz128);
       Turn<C::kKB> kb;
@@ -897,9 +905,10 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
             if (change) tmem_wait_st();
             if (m == -INFINITY) m = top;                              // (so far nothing: its sum and O are 0)
             if (__any_sync(0xffffffffu, top > m + kLag)) {
+              // (of all rows of the warp: if only those moved that need it, some row would in many more jobs: prompt 371 -> 439 us)
               const float old = m;
               m = fmaxf(m, top);
-              const float f = m == -INFINITY ? 1.f : exp2_approx(old - m);
+              const float f = m == old ? 1.f : exp2_approx(old - m);
               l0 *= f;
               l1 *= f;
               if (have) {
@@ -1359,8 +1368,8 @@ size_t align32(size_t x) { return (x + 31) & ~(size_t)31; }
 Plan plan(int B, int H, int kv_heads, int T, int d, int groups) {
   Plan t;
   const long long rows = (long long)(H / kv_heads) * T;
-  // (a sequence by itself has few rows, and instances for those keep copies of them: prefixes go along.  shared_batch, whose prefix has 192 rows: 80 us with
-  // 256 rows an item, LESS with 128)
+  // (a sequence by itself has few rows, and instances for those keep copies of them: prefixes go along.  48 sequences of 4 rows behind
+  // a prefix of 16000 tokens, 192 rows: 80 us with 256 rows an item, 71 with 128)
   t.rt = !groups && rows > 128 ? 2 : 1;
   const long long R = 128 * t.rt, all = (long long)B * H * T;
   t.row_tiles = (int)((rows + R - 1) / R);

@@ -170,37 +170,37 @@ struct ReleaseParams {
 __device__ __forceinline__ int2 range_of(const ReleaseParams& p, int b) {
   return make_int2(p.keep ? pages_of(load(p.keep + b), p.log_page) : 0, min(pages_of(load(p.length + b), p.log_page), p.max_pages));
 }
-constexpr int kReleaseThreads = 128;
-__global__ void __launch_bounds__(kReleaseThreads) release_count_kernel(const ReleaseParams p) {
+constexpr int kMostReleaseThreads = 512;                            // of a block: 128, or as many for long tables
+__global__ void __launch_bounds__(kMostReleaseThreads) release_count_kernel(const ReleaseParams p) {
   launch_dependents();
   wait_prior_grids();
-  const int b = blockIdx.x;
+  const int b = blockIdx.x, threads = blockDim.x;
   const int2 r = range_of(p, b);
   int mine = 0;
-  for (int i = r.x + threadIdx.x; i < r.y; i += kReleaseThreads) {
+  for (int i = r.x + threadIdx.x; i < r.y; i += threads) {
     const int page = load(p.table + (size_t)b * p.max_pages + i);
     mine += page >= 0 && page < p.num_pages;
   }
-  __shared__ int warps[kReleaseThreads / 32];
+  __shared__ int warps[kMostReleaseThreads / 32];
   mine = __reduce_add_sync(0xffffffffu, mine);
   if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = mine;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int i = 1; i < kReleaseThreads / 32; ++i) mine += warps[i];
+    for (int i = 1; i < threads / 32; ++i) mine += warps[i];
     p.counts[b] = mine;
     if (b == 0) p.counts[p.B] = max(0, min(load(p.left), p.num_pages));
   }
 }
-__global__ void __launch_bounds__(kReleaseThreads) release_push_kernel(const ReleaseParams p) {
-  __shared__ int warps[kReleaseThreads / 32];
-  __shared__ long long sums[2 * (kReleaseThreads / 32)];
+__global__ void __launch_bounds__(kMostReleaseThreads) release_push_kernel(const ReleaseParams p) {
+  __shared__ int warps[kMostReleaseThreads / 32];
+  __shared__ long long sums[2 * (kMostReleaseThreads / 32)];
   launch_dependents();
   wait_prior_grids();
-  const int b = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int b = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, threads = blockDim.x;
   const int2 r = range_of(p, b);
   if (b != 0 && r.x >= r.y) return;
   long long before = 0, total = 0;
-  for (int i = threadIdx.x; i < p.B; i += kReleaseThreads) {
+  for (int i = threadIdx.x; i < p.B; i += threads) {
     const int c = load(p.counts + i);
     total += c;
     before += i < b ? c : 0;
@@ -216,14 +216,14 @@ __global__ void __launch_bounds__(kReleaseThreads) release_push_kernel(const Rel
   }
   __syncthreads();
   before = total = 0;
-  for (int i = 0; i < kReleaseThreads / 32; ++i) {
+  for (int i = 0; i < threads / 32; ++i) {
     before += sums[2 * i];
     total += sums[2 * i + 1];
   }
   const long long left = load(p.counts + p.B);
   bool lost = left + total > p.num_pages;
   if (b == 0 && threadIdx.x == 0) *p.left = (int)min(left + total, (long long)p.num_pages);
-  for (int i0 = r.x; i0 < r.y; i0 += kReleaseThreads) {
+  for (int i0 = r.x; i0 < r.y; i0 += threads) {
     const int i = i0 + threadIdx.x;
     int* const at = p.table + (size_t)b * p.max_pages + i;
     const int page = i < r.y ? load(at) : -1;
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kReleaseThreads) release_push_kernel(const Rel
     if (lane == 0) warps[warp] = __popc(votes);
     __syncthreads();
     long long rank = before + __popc(votes & ((1u << lane) - 1));
-    for (int k = 0; k < kReleaseThreads / 32; ++k) {
+    for (int k = 0; k < threads / 32; ++k) {
       if (k < warp) rank += warps[k];
       before += warps[k];
     }
@@ -298,7 +298,8 @@ extern "C" int fp4attn_pages_release(const fp4attn_page_pool* pool, int B, int* 
   p.table = block_table; p.max_pages = max_pages;
   p.length = length; p.keep = keep; p.counts = (int*)workspace; p.status = device_status;
   p.B = B;
-  cudaError_t e = launch_overlapped(release_count_kernel, dim3((unsigned)B), kReleaseThreads, 0, (cudaStream_t)stream, p);
-  if (e == cudaSuccess) e = launch_overlapped(release_push_kernel, dim3((unsigned)B), kReleaseThreads, 0, (cudaStream_t)stream, p);
+  const unsigned threads = max_pages > 256 ? kMostReleaseThreads : 128;
+  cudaError_t e = launch_overlapped(release_count_kernel, dim3((unsigned)B), threads, 0, (cudaStream_t)stream, p);
+  if (e == cudaSuccess) e = launch_overlapped(release_push_kernel, dim3((unsigned)B), threads, 0, (cudaStream_t)stream, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? FP4ATTN_OK : FP4ATTN_ERR_CUDA;
 }
