@@ -1096,8 +1096,8 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       char* dst = nullptr;                                            // of the row's elements
       if (out) {
         const float inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum * v_G);                  // nothing seen: 0, not 0 / 0
-        f[0] = f[0] == 0.f ? 0.f : f[0] * inv;
-        f[1] = f[1] == 0.f ? 0.f : f[1] * inv;
+        f[0] *= inv;
+        f[1] *= inv;
         if (live && p.lse && tells) p.lse[at] = sum == 0.f ? -INFINITY : (top - kShift + log2f(sum)) * 0.6931471805599453f;
         dst = static_cast<char*>(p.out) + at * (2 * D);
       } else if (live) {
@@ -1107,11 +1107,17 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       }
       if (p.groups && it->begins && group == 0 && in_tile == 0) p.split[it->split] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, it->last_cta);
       __syncwarp();
+      // (Every group has had a job of the item, so what stands in O is a sum: 0 where nothing was seen, as P was 0 and V is finite.)
       auto write = [&](int e, const float* o) {                       // sixteen elements of a row, 32 bytes a store
         if (out) {
           uint32_t h[8];
+          if (p.half) {
 #pragma unroll
-          for (int x = 0; x < 8; ++x) h[x] = p.half ? pack_pair<__half>(o[2 * x], o[2 * x + 1]) : pack_pair<__nv_bfloat16>(o[2 * x], o[2 * x + 1]);
+            for (int x = 0; x < 8; ++x) h[x] = pack_pair<__half>(o[2 * x], o[2 * x + 1]);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) h[x] = pack_pair<__nv_bfloat16>(o[2 * x], o[2 * x + 1]);
+          }
           if (p.out_wide) {
             store_32(dst + 2 * e, h);
           } else {
@@ -1146,11 +1152,9 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               tmem_wait_ld();
               if (live) {
 #pragma unroll
-                for (int x = 0; x < 16; x += 4) {
-                  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-                  if (g != 0.f) y = make_float4(__uint_as_float(v[x]) * g, __uint_as_float(v[x + 1]) * g, __uint_as_float(v[x + 2]) * g, __uint_as_float(v[x + 3]) * g);
-                  *reinterpret_cast<float4*>(put + ((e + x) ^ (lane & 3) * 4)) = y;
-                }
+                for (int x = 0; x < 16; x += 4)
+                  *reinterpret_cast<float4*>(put + ((e + x) ^ (lane & 3) * 4)) =
+                      make_float4(__uint_as_float(v[x]) * g, __uint_as_float(v[x + 1]) * g, __uint_as_float(v[x + 2]) * g, __uint_as_float(v[x + 3]) * g);
               }
               __syncwarp();
             }
@@ -1192,15 +1196,14 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               tmem_ld_32x32b_x16(o_at + e, v);
               tmem_wait_ld();
 #pragma unroll
-              for (int x = 0; x < 16; ++x) o[x] = f[group] == 0.f ? 0.f : __uint_as_float(v[x]) * f[group];
+              for (int x = 0; x < 16; ++x) o[x] = __uint_as_float(v[x]) * f[group];
             } else {
               uint32_t v2[16];
               tmem_ld_32x32b_x16(tmem + lanes + C::kO + e, v);
               tmem_ld_32x32b_x16(tmem + lanes + C::kO + D + e, v2);
               tmem_wait_ld();
 #pragma unroll
-              for (int x = 0; x < 16; ++x)
-                o[x] = (f[0] == 0.f ? 0.f : __uint_as_float(v[x]) * f[0]) + (f[1] == 0.f ? 0.f : __uint_as_float(v2[x]) * f[1]);
+              for (int x = 0; x < 16; ++x) o[x] = __uint_as_float(v[x]) * f[0] + __uint_as_float(v2[x]) * f[1];
             }
             if (live) write(e, o);
             __syncwarp();

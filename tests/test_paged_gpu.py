@@ -198,6 +198,34 @@ def test_paged_attention_masks_caps_and_biases(B, H, kv, T, d, P, context, kind,
     _check_paged(got, q, cache, table, context, first=first, last=last, cap=cap, slopes=slopes)
 
 
+@pytest.mark.parametrize("fmt,d", [("nvfp4", 128), ("e4m3", 64), ("e4m3", 128)])
+@pytest.mark.parametrize("T", [1, 2, 9])
+def test_paged_attention_steps_far_into_contexts(T, fmt, d):
+    """Few rows, with windows and documents that begin anywhere in contexts of up to 20000 tokens, capped, with a bias, and both."""
+    Bd, g, rng = _bd(), _gen(d + T), np.random.default_rng(T)
+    B, H, kv, P = 3, 4, 2, 32
+    context = [20000, 127, 4096]
+    cache, table = _filled(Bd, g, fmt, B, kv, P, d, 20000 + T)
+    q = _randn(g, B, H, T, d, scale=2.0)
+    slopes = torch.tensor([0.01, 0.0, 2.0, -0.001], device="cuda")
+    p = np.array(context)[:, None] + np.arange(T)[None]
+    for first in (None, np.maximum(0, p + 1 - 100), np.maximum(0, p - 5000), rng.integers(0, np.array(context)[:, None] + 1, (B, T))):
+        for kw in (dict(), dict(cap=20.0), dict(slopes=slopes), dict(cap=1.5, slopes=slopes)):
+            got = Bd.fp4attn_paged_attention(q, cache, table, _i32(context), first=None if first is None else _i32(first.tolist()), soft_cap=kw.get("cap", 0.0),
+                                             slopes=kw.get("slopes"))
+            _check_paged(got, q, cache, table, context, first=first, **kw)
+
+
+def test_paged_attention_many_items():
+    """More items than a block remembers, of one tile each."""
+    Bd, g = _bd(), _gen(81)
+    B, H, kv, T, d, P = 620, 16, 8, 66, 64, 16
+    context = [(i * 7) % 40 for i in range(B)]
+    cache, table = _filled(Bd, g, "e4m3", B, kv, P, d, 40 + T)
+    q = _randn(g, B, H, T, d)
+    _check_paged(Bd.fp4attn_paged_attention(q, cache, table, _i32(context)), q, cache, table, context)
+
+
 @pytest.mark.parametrize("T", [5, 200])
 @pytest.mark.parametrize("fmt", FMTS)
 def test_paged_attention_what_nobody_sees(fmt, T):
@@ -365,6 +393,7 @@ SHARED = [  # H, kv, T, d, P, prefixes, group_start, contexts, counts
     (40, 1, 2, 128, 16, [2000, 77], [0, 9, 11], [i * 13 for i in range(11)], None),
     (2, 1, 1, 64, 16, [260], [0, 300], [i % 23 for i in range(300)], None),
     (4, 4, 1, 128, 64, [9000], [0, 4], [5, 2, 0, 600], None),
+    (8, 8, 1, 64, 16, [3, 200], [0, 500, 700], [i % 37 for i in range(700)], None),         # more items than a block remembers
 ]
 
 
