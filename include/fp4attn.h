@@ -1,6 +1,6 @@
 /*
  * fp4attn — full-FP4 attention forward with Direct-P for NVIDIA B200 (sm_100a), and what serving needs around a quantized cache
- * of K and V: rotary positions, the cache, attention of a token or of a tree of drafted tokens over it (last section).
+ * of K and V: rotary positions, the cache and its pages, attention of tokens, drafted trees, prompts and shared prefixes over it (last section).
  *
  * C ABI.  Unless an argument says otherwise every pointer is a DEVICE pointer owned by the
  * caller; the library allocates no device memory.  State kept between calls: cached kernel attributes and
