@@ -843,7 +843,9 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       const bool warp_live = __any_sync(0xffffffffu, live);
       if (!live) hi = INT_MAX;                                        // (a row of zeros, or one that is not written: never the reason to look at masks)
       const int mask_at = p.mask && it->g < 0 ? it->ctx : INT_MIN;    // where the drafted tokens begin
-      bool have = false;                                              // a job of the item so far
+      // keys that every row of the warp sees
+      const int plain_lo = __reduce_max_sync(0xffffffffu, lo), plain_hi = __reduce_min_sync(0xffffffffu, hi);
+      bool have = false, settled = false;                             // a job of the item so far; a reference for every row
       float m = -INFINITY, l0 = 0.f, l1 = 0.f, con = 0.f;
       int first = it->first + (two ? 64 : 64 * group);                // first key of the job
       const int jobs = two ? 2 * tiles : tiles;
@@ -857,7 +859,10 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
           if (rare(!have)) con = live ? reinterpret_cast<const float*>(sgen + C::kOffC)[(item & (C::kRingC - 1)) * ROWS + row_in] : 0.f;
           // Does every row see every key (with a bias: of those before it)?  Otherwise scores are changed, masked and put back before anything else; so are capped
           // scores beyond the polynomial's range.
-          bool change = !__all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + 64 && (!ANY || pos >= first + 63)) || (ANY && p.cap > 0.f);
+          // (Scaled scores only: two votes fewer a job are 8 % of the time.  The others are as fast without, and have no registers for the bounds.)
+          bool change = (SCORES == kScaled ? held != all_pages || first < plain_lo || first + 64 > plain_hi
+                                           : !__all_sync(0xffffffffu, held == all_pages && lo <= first && hi >= first + 64 && (!ANY || pos >= first + 63))) ||
+                        (ANY && p.cap > 0.f);
           // (by no row of the warp any of them: documents, the tile on the diagonal)
           const bool unseen = rare(change) && mask_at < 0 && __all_sync(0xffffffffu, hi <= first || lo >= first + 64);
           // The reference moves to the largest score seen so far.
@@ -926,6 +931,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
                 tmem_wait_st();
               }
             }
+            settled = !__any_sync(0xffffffffu, m == -INFINITY);
           };
           // Probabilities of sixteen keys, eight words; the largest score above the reference (+ kShift), the sum.  HOW: scores times a constant; capped; with a
           // bias that falls along the keys.
@@ -976,7 +982,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
           };
           // Scores rarely exceed their reference: the largest is looked for first where there is none yet or scores have to be changed, and in all other
           // jobs only when they have turned out to; then the job is done again.
-          bool sure = change || __any_sync(0xffffffffu, m == -INFINITY);
+          bool sure = change || (SCORES == kScaled ? !settled : __any_sync(0xffffffffu, m == -INFINITY));
           s0 = s1 = 0.f;
           auto attempt = [&](auto pass) {
 #pragma unroll 1
