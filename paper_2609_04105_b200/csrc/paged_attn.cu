@@ -87,6 +87,7 @@ struct Item {
   int last_cta, slot;                      // where it ends; place of its partial result
   long long split;                         // place in p.split
 };
+constexpr float kMostSum = 32768.f;        // of a job's probabilities: none of them is beyond f16 then
 constexpr int kItems = 32;                 // the producer is some ten tiles, hence items, ahead at most
 
 template <int FMT, int D, int RT>
@@ -865,6 +866,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
                         (ANY && p.cap > 0.f);
           // (by no row of the warp any of them: documents, the tile on the diagonal)
           const bool unseen = rare(change) && mask_at < 0 && __all_sync(0xffffffffu, hi <= first || lo >= first + 64);
+          float lag = kLag;
           // The reference moves to the largest score seen so far.
           auto refer = [&] {
             float top = -INFINITY;
@@ -909,7 +911,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
             }
             if (change) tmem_wait_st();
             if (m == -INFINITY) m = top;                              // (so far nothing: its sum and O are 0)
-            if (__any_sync(0xffffffffu, top > m + kLag)) {
+            if (__any_sync(0xffffffffu, top > m + lag)) {
               // (of all rows of the warp: if only those moved that need it, some row would in many more jobs: prompt 371 -> 439 us)
               const float old = m;
               m = fmaxf(m, top);
@@ -933,9 +935,9 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
             }
             settled = !__any_sync(0xffffffffu, m == -INFINITY);
           };
-          // Probabilities of sixteen keys, eight words; the largest score above the reference (+ kShift), the sum.  HOW: scores times a constant; capped; with a
+          // Probabilities of sixteen keys, eight words, and their sum.  HOW: scores times a constant; capped; with a
           // bias that falls along the keys.
-          float over, wide, s0, s1, shift, c2;
+          float wide, s0, s1, shift, c2;
           auto sixteen = [&](auto how, const uint32_t* raw, int k, uint32_t* h) {
             constexpr int HOW = decltype(how)::value;
 #pragma unroll
@@ -966,7 +968,6 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
                 } else {
                   fma_pair(z[x], z[x + 1], r0, r1, c2, c2, shift, shift);
                 }
-                over = max3(over, z[x], z[x + 1]);
                 z[x] = exp2_approx(z[x]);
                 z[x + 1] = exp2_approx(z[x + 1]);
                 add_pair(s0, s1, z[x], z[x + 1]);
@@ -980,8 +981,8 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               }
             }
           };
-          // Scores rarely exceed their reference: the largest is looked for first where there is none yet or scores have to be changed, and in all other
-          // jobs only when they have turned out to; then the job is done again.
+          // Scores rarely exceed their reference by much: the largest is looked for first where there is none yet or scores have to be changed, and in all other
+          // jobs only when their sum has turned out to be more than f16 is sure to hold of one of them; then the job is done again.
           bool sure = change || (SCORES == kScaled ? !settled : __any_sync(0xffffffffu, m == -INFINITY));
           s0 = s1 = 0.f;
           auto attempt = [&](auto pass) {
@@ -989,7 +990,6 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
             while (true) {
               if (rare(sure)) refer();
               shift = m == -INFINITY ? 0.f : kShift - m;
-              over = -INFINITY;
               s0 = s1 = wide = 0.f;
               if (SCORES == kScaled || rare(change)) {
                 c2 = change ? 1.f : con;
@@ -1003,8 +1003,9 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
                   continue;
                 }
               }
-              if (sure || !rare(__any_sync(0xffffffffu, over > kLag + kShift))) break;
+              if (sure || !rare(__any_sync(0xffffffffu, s0 + s1 > kMostSum))) break;
               sure = true;
+              lag = 1.f;                                              // (64 keys of that sum: one is 2^9 or more, two octaves above the reference's 2^7)
             }
           };
           if (unseen) {
