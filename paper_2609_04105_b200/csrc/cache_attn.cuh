@@ -16,8 +16,9 @@ struct FewRows {
   int* status;
   int type, fmt, d, B, H, T;
   float scale, cap;
+  bool changed() const { return first || last || slopes || cap > 0.f; }       // else: attention over a tree in which every token sees those before it
 };
-bool few_rows(int rows, int fmt, int d);
+bool few_rows(int rows, int fmt, int d, bool changed);
 size_t few_rows_workspace(int B, int H, int kv_heads, int T, int d, int fmt);
 int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st);
 int check_cache(const fp4attn_cache* c, int B, const int* block_table, int max_pages, const int* start, const int* count, CacheRef* ref);

@@ -18,11 +18,12 @@
 // 128 it stood still for two products in between: a chunk of 2048 tokens 1229 us instead of 1112).  Items of more than 128 rows give each group half of the
 // rows; those of fewer give it half of the keys of a tile, with a reference, a sum and an O of its own, joined at the item's end.
 //
-// Few rows (up to 16 a KV head; up to 8 in NVFP4 with d = 128) go to the kernel of warps in tree_attn.cu, but for shared prefixes.
+// Few rows (up to 16 a KV head; up to 8 in NVFP4 with d = 128) go to the kernel of warps in tree_attn.cu, and up to 32 with neither mask nor cap nor bias to its
+// roles, but for shared prefixes.
 //
 // What bounds it: instructions.  A softmax warp executes one about every five clocks (waits, branches and instruction fetches among them), a job of 64
 // keys is some 250, and an item costs as much as three or four tiles (bringing Q, the first references, writing O).  2048 tokens of 32 heads over 8 behind 30720, d = 128,
-// NVFP4: 1.05 to 1.12 ms, 960 to 1020 TFLOP/s (power: 1780 MHz); two prompts of 4096: 366 us, 750 TFLOP/s.  Beside the products of N = 64, whose operands
+// NVFP4: 0.98 to 1.05 ms, 1020 to 1090 TFLOP/s (power: 1780 MHz); two prompts of 4096: 344 us, 800 TFLOP/s.  Beside the products of N = 64, whose operands
 // come from shared memory (48 clocks instead of 32) and which take longer to issue than to compute (90), exponentials do not count: without them nothing changes.
 //
 // A row's keys are walked from its last to its first: what a mask cuts off comes where a reference has to be looked for anyway, and a bias by distance falls
@@ -1482,7 +1483,7 @@ namespace {
 size_t paged_workspace(int B, int H, int kv_heads, int T, int d) {
   size_t most = plan(B, H, kv_heads, T, d, 0).total;
   for (int fmt : {FP4ATTN_FMT_NVFP4, FP4ATTN_FMT_E4M3})
-    if (few_rows(H / kv_heads * T, fmt, d)) most = std::max(most, few_rows_workspace(B, H, kv_heads, T, d, fmt));
+    if (few_rows(H / kv_heads * T, fmt, d, false)) most = std::max(most, few_rows_workspace(B, H, kv_heads, T, d, fmt));
   return most;
 }
 }  // namespace
@@ -1503,10 +1504,8 @@ extern "C" int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp
   if (!workspace || workspace_bytes < fp4attn_paged_attention_workspace_bytes(B, H, cache->kv_heads, T, cache->d)) return FP4ATTN_ERR_WORKSPACE;
   if ((uintptr_t)workspace & 31) return FP4ATTN_ERR_ALIGNMENT;
   if ((rc = check_device_sm100()) != FP4ATTN_OK) return rc;
-  if (few_rows(H / cache->kv_heads * T, cache->fmt, cache->d)) {
-    const FewRows a = {q, p.cache, context, count, first, last, slopes, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, p.cap};
-    return launch_few_rows(a, workspace, (cudaStream_t)stream);
-  }
+  const FewRows few = {q, p.cache, context, count, first, last, slopes, O, LSE, device_status, type, cache->fmt, cache->d, B, H, T, p.scale, p.cap};
+  if (few_rows(H / cache->kv_heads * T, cache->fmt, cache->d, few.changed())) return launch_few_rows(few, workspace, (cudaStream_t)stream);
   p.first = first; p.last = last;
   return launch(p, plan(B, H, cache->kv_heads, T, cache->d, 0), workspace, cache->fmt, cache->d, (cudaStream_t)stream);
 }

@@ -1590,13 +1590,20 @@ int launch_rows(const TreeParams& p, int R, cudaStream_t st) {
 template <int FMT, int D>
 int launch_few(const TreeParams& p, int R, bool changed, cudaStream_t st) {
   if (R == 8) return changed ? launch_warps<FMT, D, 1, true>(p, st) : launch_warps<FMT, D, 1>(p, st);
-  if constexpr (!(FMT == FP4ATTN_FMT_NVFP4 && D == 128)) return changed ? launch_warps<FMT, D, 2, true>(p, st) : launch_warps<FMT, D, 2>(p, st);
-  return FP4ATTN_ERR_UNSUPPORTED_SHAPE;                             // (not few)
+  if constexpr (!(FMT == FP4ATTN_FMT_NVFP4 && D == 128))
+    if (R == 16) return changed ? launch_warps<FMT, D, 2, true>(p, st) : launch_warps<FMT, D, 2>(p, st);
+  return R == 32 && !changed ? launch_tree<FMT, D, 32>(p, st) : FP4ATTN_ERR_UNSUPPORTED_SHAPE;      // (not few)
 }
 
 }  // namespace
 
-bool few_rows(int rows, int fmt, int d) { return rows_of_tile(rows, fmt, d) <= 16; }
+// With no mask, cap or bias the roles of 32 rows against 128 rows in lanes (paged_attn.cu), us:
+//   32 rows, 8 KV heads     1 x 1000      8 x 4096      16 x 16000
+//     NVFP4, d = 128      13.5 | 22.4   35.2 | 43.8   123 | 151
+//     E4M3, d = 128       13.6 | 22.1   35.5 | 44.3   122 | 208
+//     NVFP4, d = 64       12.3 | 17.4   32.3 | 33.9   112 | 121        (E4M3 alike)
+//   64 rows, NVFP4, d = 128: 15.7 | 22.6, 43.5 | 45.6, 185 | 160: left to the other, as is all that is masked, which has no roles of its own
+bool few_rows(int rows, int fmt, int d, bool changed) { return rows_of_tile(rows, fmt, d) <= (changed ? 16 : 32); }
 size_t few_rows_workspace(int B, int H, int kv_heads, int T, int d, int fmt) { return plan(B, H, kv_heads, T, d, fmt).total; }
 int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st) {
   const TreePlan t = plan(a.B, a.H, a.cache.kv_heads, a.T, a.d, a.fmt);
@@ -1615,7 +1622,7 @@ int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st) {
   p.part = (float*)workspace;
   p.part_ml = (float2*)((char*)workspace + t.ml);
   p.split = (int2*)((char*)workspace + t.split);
-  const bool changed = a.first || a.last || a.slopes || a.cap > 0.f;        // (else it is attention over a tree in which every token sees those before it)
+  const bool changed = a.changed();
   if (a.fmt == FP4ATTN_FMT_NVFP4) return a.d == 64 ? launch_few<FP4ATTN_FMT_NVFP4, 64>(p, t.R, changed, st) : launch_few<FP4ATTN_FMT_NVFP4, 128>(p, t.R, changed, st);
   return a.d == 64 ? launch_few<FP4ATTN_FMT_E4M3, 64>(p, t.R, changed, st) : launch_few<FP4ATTN_FMT_E4M3, 128>(p, t.R, changed, st);
 }

@@ -165,6 +165,26 @@ def test_paged_attention(B, H, kv, T, d, P, context, counts, fmt, dtype):
             assert not got[0][b, :, n:].any() and torch.isneginf(got[1][b, :, n:]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,kv,T,context,counts", [(4, 2, 8, [300, 0, 1], None), (9, 1, 3, [127, 4000, 128], [3, 0, 2]), (8, 2, 8, [1001, 5, 77], [1, 8, 7]),
+                                                   (16, 2, 4, [0, 640, 2500], None), (1, 1, 32, [95, 96, 97], [32, 31, 0]), (11, 1, 3, [500, 31, 0], None)])
+def test_some_rows_of_a_kv_head(H, kv, T, context, counts, d, fmt, dtype):
+    """16 to 33 of them, on either side of where another kernel takes over: none of it shows, nor does a mask that hides nothing."""
+    Bd, g = _bd(), _gen(H * T + d)
+    cache, table = _filled(Bd, g, fmt, 3, kv, 32, d, max(context) + T)
+    q = _randn(g, 3, T, H, d, dtype=dtype, scale=2.0).transpose(1, 2)
+    count = None if counts is None else _i32(counts)
+    got = Bd.fp4attn_paged_attention(q, cache, table, _i32(context), count=count)
+    _check_paged(got, q, cache, table, context, counts)
+    first = torch.zeros(3, T, dtype=torch.int32, device="cuda")
+    masked = Bd.fp4attn_paged_attention(q, cache, table, _i32(context), count=count, first=first)
+    _check_paged(masked, q, cache, table, context, counts)
+    again = Bd.fp4attn_paged_attention(q, cache, table, _i32(context), count=count)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
 def _masks(rng, B, T, context, kind):
     """first, last of some kinds; None where a kind leaves one out."""
     p = np.array(context)[:, None] + np.arange(T)[None]
