@@ -514,7 +514,7 @@ int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4attn_cache*
 /*
  * Attention of T query tokens of every sequence over its cache, T of any size: a step, a chunk of a prompt, a whole prompt.  q [B, H, T, d] (bf16
  * or fp16), O [B, H, T, d] of that type, contiguous, LSE fp32 [B, H, T] (may be NULL), natural logarithm.  Head h reads KV head
- * h / (H / kv_heads).
+ * h / (H / kv_heads); up to 65535 heads read one.
  *
  * The T tokens stand in the cache already, token t at position p = context[b] + t; of entry b there are n = count[b] (NULL: T), and rows
  * t >= n are not written.  Row t sees positions j with first[b, t] <= j < last[b, t] and j < context[b] + n (int32 [B, T], device; first NULL: 0,

@@ -46,6 +46,7 @@ namespace fp4attn {
 namespace {
 
 constexpr int kMostCtas = 160;             // one an SM; each may leave two partial results
+constexpr int kMostGroup = (1 << 16) - 1;  // query heads of a KV head: see divide()
 
 // how a product becomes a score: scaled; scaled and capped; with a bias, and perhaps capped
 enum { kScaled, kCapped, kBiased };
@@ -207,7 +208,8 @@ __device__ __forceinline__ size_t split_place(const PagedParams& p, const Desc& 
   const long long at = d.g >= 0 ? d.b * rows / ROWS + d.g + rt : p.B * rows / ROWS + p.groups + 1 + (long long)d.b * p.row_tiles + rt;
   return (size_t)at * p.cache.kv_heads + kvh;
 }
-// n / d for n up to 2^24 (d < 2^12) or 2^17 (d < 2^16): m = ceil(2^36 / d), so that n (m d - 2^36) < n d stays below 2^36
+// n / d for n up to 2^24 (d < 2^12) or 2^17 (d < 2^16): m = ceil(2^36 / d), so that n (m d - 2^36) < n d stays below 2^36.  d is a KV head's query heads (n
+// less than 256 more) or a call's tokens (n those of a group): more heads than that are refused.
 __device__ __forceinline__ int divide(int n, unsigned long long m) { return (int)((unsigned long long)n * m >> 36); }
 
 // This CTA's run of the list, in units: a tile is one, and an item that many more (bringing Q, writing O), which come before its tiles.  x, the run's
@@ -1460,7 +1462,7 @@ int check(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, in
     return FP4ATTN_ERR_INVALID_ARG;
   if (type != FP4ATTN_TYPE_BF16 && type != FP4ATTN_TYPE_FP16) return FP4ATTN_ERR_INVALID_ARG;
   if (H % cache->kv_heads != 0) return FP4ATTN_ERR_INVALID_ARG;
-  if ((long long)B * H * T >= (1ll << 31) || T >= (1 << 30)) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;
+  if ((long long)B * H * T >= (1ll << 31) || T >= (1 << 30) || H / cache->kv_heads > kMostGroup) return FP4ATTN_ERR_UNSUPPORTED_SHAPE;
   if (((uintptr_t)q->data & 1) || ((uintptr_t)O & 15) || ((uintptr_t)LSE | (uintptr_t)device_status | (uintptr_t)slopes) & 3) return FP4ATTN_ERR_ALIGNMENT;
   p->q = q->data; p->q_sb = q->stride_b; p->q_sh = q->stride_h; p->q_sn = q->stride_n;
   p->q_vector = view_vectors(*q, 2);
@@ -1489,7 +1491,8 @@ size_t paged_workspace(int B, int H, int kv_heads, int T, int d) {
 }  // namespace
 
 extern "C" size_t fp4attn_paged_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d) {
-  if (B <= 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || T <= 0 || (d != 64 && d != 128) || (long long)B * H * T >= (1ll << 31) || T >= (1 << 30)) return 0;
+  if (B <= 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || T <= 0 || (d != 64 && d != 128) || (long long)B * H * T >= (1ll << 31) || T >= (1 << 30) || H / kv_heads > kMostGroup)
+    return 0;
   return paged_workspace(B, H, kv_heads, T, d);
 }
 
