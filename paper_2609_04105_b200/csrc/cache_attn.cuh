@@ -31,17 +31,19 @@ constexpr float kLag = 8.f;                // octaves by which a score may excee
 constexpr float kShift = 7.f;              // a probability of 1 is 2^7: with the lag just inside f16, whose subnormals then begin at 2^-21
 
 __device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
-// Waits for a barrier's phase; the whole warp goes on together.  A wait that runs out, or sees that another one did, sets the abort word
-// and returns as if the phase had come: what the roles then read and multiply means nothing, but stays in bounds, and every wait of
-// theirs ends at once, so that they run out of tiles.  The phase has come at the first look, or while that look was suspended, in nearly
+// Waits for a barrier's phase; the whole warp goes on together.  A wait that runs out sets the abort word, and one that sees it set returns at once.
+// The answer, a thread's own: has the phase come?  Those who compute need not ask: what they then read and multiply means nothing, but stays in bounds, and
+// every wait of theirs ends at once, so that they run out of tiles.  Who brings copies must: a barrier that still expects bytes takes no second
+// arrival, and no copy may go where another is under way.  The phase has come at the first look, or while that look was suspended, in nearly
 // every wait.  CALL: the loop behind it is a function of its own: inlined at each wait it took up to 12 % of the time, in instruction
 // fetches.  (Code that shares out registers by setmaxnreg may not call.)
-__device__ __forceinline__ void poll_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
+__device__ __forceinline__ bool poll_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
   uint32_t since = 0;
   for (uint32_t n = 1;; ++n) {
     uint32_t gone;
     asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(gone) : "r"(abort_at) : "memory");
-    if (gone || mbar_try_wait(bar, parity)) return;
+    if (gone) return false;
+    if (mbar_try_wait(bar, parity)) return true;
     if (n % kPolls) continue;
     uint32_t now;
     asm volatile("mov.u32 %0, %%clock;" : "=r"(now));
@@ -49,15 +51,15 @@ __device__ __forceinline__ void poll_phase(uint32_t bar, uint32_t parity, uint32
     if (now - since >= kWaitClocks) break;
   }
   asm volatile("st.volatile.shared.u32 [%0], 1;" ::"r"(abort_at) : "memory");
+  return false;
 }
-__device__ __noinline__ void wait_longer(uint32_t bar, uint32_t parity, uint32_t abort_at) { poll_phase(bar, parity, abort_at); }
+__device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity, uint32_t abort_at) { return poll_phase(bar, parity, abort_at); }
 template <bool CALL>
-__device__ __forceinline__ void wait_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
-  if (rare(!mbar_try_wait(bar, parity))) {
-    if (CALL) wait_longer(bar, parity, abort_at);
-    else poll_phase(bar, parity, abort_at);
-  }
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
+  bool come = true;
+  if (rare(!mbar_try_wait(bar, parity))) come = CALL ? wait_longer(bar, parity, abort_at) : poll_phase(bar, parity, abort_at);
   __syncwarp();
+  return come;
 }
 // which of N buffers, and the phase of its barriers
 template <int N>
@@ -70,6 +72,18 @@ struct Turn {
     }
   }
 };
+
+// The last copies into a ring of STAGES end before the warp that brought `parts` does, also where the others have given up on them: whatever the abort word says,
+// but no longer than some tens of milliseconds.  ring: behind the last part.
+template <int STAGES>
+__device__ __forceinline__ void drain(Turn<STAGES> ring, uint32_t full, int parts) {
+#pragma unroll 1
+  for (int k = 0; k < STAGES && k < parts; ++k) {
+    ring.at = ring.at ? ring.at - 1 : (ring.phase ^= 1, STAGES - 1);
+    for (int spin = 0; spin < (1 << 13) && !mbar_try_wait(full + 8 * ring.at, (uint32_t)ring.phase); ++spin) {}
+  }
+  __syncwarp();
+}
 
 template <bool HALF>
 __device__ __forceinline__ float2 unpack16(uint32_t w) { return HALF ? unpack2<__half>(w) : unpack2<__nv_bfloat16>(w); }

@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   const uint32_t abort_at = sbase + C::kOffBar + 8 * C::kBars, tslot = abort_at + 4;
   volatile uint32_t* const abort_word = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars);
   auto bar = [&](int i) { return sbase + C::kOffBar + 8u * i; };
-  auto wait = [&](int b, int phase) { wait_phase<true>(bar(b), (uint32_t)phase, abort_at); };
+  auto wait = [&](int b, int phase) { return wait_phase<true>(bar(b), (uint32_t)phase, abort_at); };
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i) {
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   if (warp == C::kProducer) {
     // ===================================================================== items, and pages -> shared memory
     Turn<C::kStages> ring;
-    bool lost = false;
+    bool lost = false, going = true;                                  // going: every stage waited for has become free
     int parts = 0, x = run.x, u = 0, i = 0;
     long long left = run.tiles, number = run.first, at = run.at;      // number: of the first unit of the run, at: its place in the item
     Desc d;
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     }
     int n = 0;                                                        // items
 #pragma unroll 1
-    while (left > 0 && !*abort_word) {
+    while (left > 0 && going && !*abort_word) {
       // units [at, end) of the item; its tiles are those from unit kItemCost on
       const int from = (int)at, end = (int)min((long long)(d.nt + kItemCost), at + left), tile = max(0, from - kItemCost);
       const long long item0 = number - from;
@@ -492,14 +492,15 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       };
       int page = page_at(it.first);
 #pragma unroll 1
-      for (int k = 0; k < it.tiles; ++k) {
+      for (int k = 0; k < it.tiles && going; ++k) {
         const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
         const uint8_t* const rec = pages + (size_t)max(page, 0) * page_bytes;
         const bool mine = page >= 0;
         if (k + 1 < it.tiles) page = page_at(it.first - (k + 1) * kTile);            // (its entry comes while a stage is waited for)
 #pragma unroll 1
         for (int part = 0; part < 2; ++part) {
-          wait(C::RING_FREE + ring.at, ring.phase ^ 1);
+          going = __all_sync(0xffffffffu, wait(C::RING_FREE + ring.at, ring.phase ^ 1));
+          if (rare(!going)) break;
           if (lane == 0) {
             if (part == 0) valid_ring[i % C::kRing] = held;
             mbar_arrive_expect_tx(bar(C::RING_FULL + ring.at), __popc(held) * half_record);
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         }
         ++i;
       }
-      if (left > 0 && ++u == d.rts * p.cache.kv_heads) {
+      if (left > 0 && going && ++u == d.rts * p.cache.kv_heads) {
         u = 0;
         do describe<ROWS>(p, ++x, d);
         while (d.nt == 0);                                            // (there is another item: the run goes on)
@@ -523,12 +524,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       mbar_arrive(bar(C::ITEM + (n & (kItems - 1))));
     }
     if (__any_sync(0xffffffffu, lost) && lane == 0 && p.status) *p.status = FP4ATTN_ERR_PAGE;
-    // the last copies end before this warp does (also where the others have given up on them)
-#pragma unroll 1
-    for (int k = 0; k < C::kStages && k < parts; ++k) {
-      ring.at = ring.at ? ring.at - 1 : (ring.phase ^= 1, C::kStages - 1);
-      wait(C::RING_FULL + ring.at, ring.phase);
-    }
+    drain(ring, bar(C::RING_FULL), parts);
   } else if (warp == C::kIssuerS || warp == C::kIssuerO) {
     // ===================================================================== products
     // Jobs: 128 rows and 64 keys, of the softmax groups in turn.  A tile has four (both halves of the rows, both of the keys) or, with up to 128 rows,

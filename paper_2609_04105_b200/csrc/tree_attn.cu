@@ -337,10 +337,11 @@ struct Pages {
     }
     lost |= w.need > (PAGED ? p.cache.max_pages << p.cache.log_page : w.len);        // the table has no room for the last tokens
   }
-  __device__ __forceinline__ void bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
+  // false: the stage has not become free, some wait has run out; nothing was begun, and nothing more must be
+  __device__ __forceinline__ bool bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
     const int lane = threadIdx.x & 31;
     const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
-    wait_phase<CALL>(free + 8 * ring.at, ring.phase ^ 1, abort_at);
+    if (rare(!__all_sync(0xffffffffu, wait_phase<CALL>(free + 8 * ring.at, ring.phase ^ 1, abort_at)))) return false;
     const int bytes = p.cache.record / PARTS;
     if (lane == 0) {
       valid[i % RING] = held;
@@ -350,6 +351,7 @@ struct Pages {
     if (page >= 0)
       bulk_load_1d(stages + ring.at * STAGE + lane * bytes, p.cache.rec(page, w.u / p.row_tiles) + (PARTS == 2 ? (i & 1) * bytes : 0), bytes,
                    full + 8 * ring.at);
+    return true;
   }
   __device__ __forceinline__ void skip(const TreeParams& p, int units, int n) {
 #pragma unroll 1
@@ -421,16 +423,12 @@ __global__ void __launch_bounds__(TreeCfg<FMT, D, R>::kThreads, 1) tree_kernel(c
       pages.w = w0;
       if (n_tiles > 0) pages.find(p);
       while (pages.i < n_tiles) {
-        pages.bring(p, sbase + C::kOffStage, bar(C::RING_FULL), bar(C::RING_FREE), abort_at, valid_ring);
+        if (rare(!pages.bring(p, sbase + C::kOffStage, bar(C::RING_FULL), bar(C::RING_FREE), abort_at, valid_ring))) break;
         pages.skip(p, units, 1);
         if (pages.i < n_tiles) pages.find(p);                         // the table's entries come while the stage is waited for
       }
       pages.tell(p);
-      // the last copies end before this warp does (also where the others have given up on them)
-      for (int k = 0; k < C::kStages && k < n_tiles; ++k) {
-        pages.ring.at = pages.ring.at ? pages.ring.at - 1 : (pages.ring.phase ^= 1, C::kStages - 1);
-        wait(C::RING_FULL + pages.ring.at, pages.ring.phase);
-      }
+      drain(pages.ring, bar(C::RING_FULL), pages.i);
     } else if (warp == C::kIssuerS) {
       // ===================================================================== S^T = K Q^T
       // Q: K-major, core matrices of 8 rows x 16 bytes, those along d neighbours.  A product takes 45 clocks or more whatever its N up to 64,
@@ -1038,7 +1036,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
   if (warp == 0) {
     while (pages.i < C::kStages && pages.i < n_parts) {
       pages.find(p);
-      pages.bring(p, sbase, full, free, abort_at, valid);
+      if (rare(!pages.bring(p, sbase, full, free, abort_at, valid))) break;             // (they are free: no wait can have run out yet)
       pages.skip(p, units, 1);
     }
   } else if (C::kStages + warp < n_parts) {
@@ -1049,8 +1047,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
   if (pages.i < n_parts) pages.find(p);
   auto next_pages = [&](int part) {                                 // this warp's turn?
     if (pages.i == part - 1 + C::kStages && pages.i < n_parts) {
-      pages.bring(p, sbase, full, free, abort_at, valid);
-      if (pages.i >= n_parts - C::kWarps) {
+      if (rare(!pages.bring(p, sbase, full, free, abort_at, valid)) || pages.i >= n_parts - C::kWarps) {
         pages.i = n_parts;
       } else {
         pages.skip(p, units, C::kWarps);

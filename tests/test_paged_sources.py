@@ -1,0 +1,36 @@
+"""Rules of the sources of attention over a cache that no healthy run can show to hold, checked on the CPU."""
+import re
+
+import pytest
+
+from test_serving_sources import _code
+
+
+@pytest.mark.parametrize("name", ["tree_attn.cu", "paged_attn.cu"])
+def test_nothing_is_brought_into_a_stage_that_has_not_become_free(name):
+    """A wait that sees the abort word returns although its phase has not come.  An arrival at a barrier that still expects bytes is one too many, and a
+    copy into its stage would lie over one under way: between a wait for a stage and the arrival that announces a copy, the wait's answer ends the
+    bringing, for the whole warp alike."""
+    code = _code(name)
+    places = [m.start() for m in re.finditer(r"\bmbar_arrive_expect_tx\(", code)]
+    assert places
+    for at in places:
+        wait = list(re.finditer(r"\bwait(_phase)?\b[^;]*;", code[:at]))[-1]
+        statement = code[code.rfind(";", 0, wait.start()) + 1:at]
+        assert "__all_sync(0xffffffffu, wait" in statement and re.search(r"\b(break|return false);", statement), statement
+    # nobody goes on as if a part had been brought
+    for m in re.finditer(r"[^;{}]*\bpages\.bring\(", code):
+        assert "!pages.bring(" in m.group(), m.group()
+
+
+def test_the_last_copies_are_waited_for_whatever_the_abort_word_says():
+    """A block whose copies are still under way must not end: after a wait has run out, too, and for a limited time."""
+    shared = _code("cache_attn.cuh")
+    body = re.search(r"\bvoid drain\(.*?\n}", shared, re.S).group()
+    assert "spin < (1 << 13) && !mbar_try_wait(" in body and "abort" not in body and "wait_phase" not in body
+    for name, kernels in (("tree_attn.cu", 2), ("paged_attn.cu", 1)):
+        code = _code(name)
+        # by the warp that has brought them, or, where every warp brings some, by the block when it has given up
+        drains = len(re.findall(r"\bdrain\([^;]*RING_FULL\), (?:pages\.i|parts)\);", code))
+        drains += len(re.findall(r"if \(threadIdx\.x < 2 \* C::kStages\)\s*for \(int spin = 0; spin < \(1 << 10\) && !mbar_try_wait\(full", code))
+        assert drains == kernels
