@@ -525,8 +525,8 @@ int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4attn_cache*
  * Positions without a page are seen by no row; FP4ATTN_ERR_PAGE reports those that a row would see, and may report those that lie between
  * positions that rows see.
  *
- * Precision as fp4attn_tree_attention (16-bit probabilities, fp32 scores, maxima, sums and O); a capped score is off by no more than 2^-20 of
- * soft_cap, a bias by no more than 2^-21 of its slope times the largest distance.  soft_cap is 0 or between 2^-60 and 2^60.  workspace: device memory
+ * Precision as fp4attn_tree_attention (16-bit probabilities, fp32 scores, maxima, sums and O); a capped score is off by no more than 2^-19 of
+ * itself, whatever the cap, a bias by no more than 2^-21 of its slope times the largest distance.  soft_cap is 0 or between 2^-60 and 2^60.  workspace: device memory
  * of the queried size, 32-byte aligned, for this call alone until it has run.  Two calls with the same arguments give the same bits.
  */
 size_t fp4attn_paged_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d);

@@ -141,9 +141,42 @@ __device__ __forceinline__ uint32_t finite(uint32_t h2) {
   const __half2 most = __float2half2_rn(448.f), r = __hmin2(*reinterpret_cast<const __half2*>(&h2), most);
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-// a score in octaves (of e^s), capped: cap tanh(s / cap) = cap - 2 cap / (1 + e^(2 s / cap)); in = 2 / cap, out = cap log2 e.  Off by no more than
-// 2^-21 of the cap: the exponential and the reciprocal by 2^-22 of themselves.  (The tanh of the special-function unit is off by 2^-11.)
-__device__ __forceinline__ float cap_score(float y, float in, float out) { return fmaf(-2.f * out, rcp_approx(1.f + exp2_approx(y * in)), out); }
+// Capped scores, cap tanh u with u = s / cap, are off by no more than 2^-20 of themselves, in every kernel and every job alike (roundings of u beside it):
+//   |u| <= 1.25   cap u P(u^2), P of least largest relative error (2^-20.6; by Lawson's weights), seven multiply-adds, two scores at a time
+//   beyond        cap - 2 cap / (1 + e^(2|u|)) with the sign of u: the second term, off by 2^-21 of itself, is less than a fifth of the result
+// The second form alone is off by 2^-21 of the cap: near 0 it is a difference of two numbers as large as the cap (scores of 10 under a cap of 1e7 were 9.7,
+// under 1e9 nothing).  The special-function unit's own tanh is off by 2^-11.
+constexpr float kTanhReach = 1.25f * 1.25f;                         // of u^2
+__device__ __forceinline__ void tanh_pair(float& t0, float& t1, float w0, float w1) {               // P(w)
+  fma_pair(t0, t1, w0, w1, 5.84494090e-4f, 5.84494090e-4f, -4.62690555e-3f, -4.62690555e-3f);
+  fma_pair(t0, t1, t0, t1, w0, w1, 1.82291232e-2f, 1.82291232e-2f);
+  fma_pair(t0, t1, t0, t1, w0, w1, -5.22054434e-2f, -5.22054434e-2f);
+  fma_pair(t0, t1, t0, t1, w0, w1, 1.32906482e-1f, 1.32906482e-1f);
+  fma_pair(t0, t1, t0, t1, w0, w1, -3.33293408e-1f, -3.33293408e-1f);
+  fma_pair(t0, t1, t0, t1, w0, w1, 9.99999404e-1f, 9.99999404e-1f);
+}
+// N scores in octaves (of e^s) from their u; out = cap log2 e.  (One look for all of them: with a branch for each pair prompts of 4095 and 1774 tokens with capped
+// documents took 254 us instead of 235, and of 4 x 2047 with a bias, which is the same code, 296 instead of 251.)
+template <int N>
+__device__ __forceinline__ void cap_scores(float (&x)[N], const float (&u)[N], float out) {
+  float wide = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    float w0, w1, t0, t1;
+    mul_pair(w0, w1, u[i], u[i + 1], u[i], u[i + 1]);
+    wide = max3(wide, w0, w1);
+    tanh_pair(t0, t1, w0, w1);
+    mul_pair(x[i], x[i + 1], u[i], u[i + 1], out, out);
+    mul_pair(x[i], x[i + 1], t0, t1, x[i], x[i + 1]);
+  }
+  if (rare(wide > kTanhReach)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (u[i] * u[i] > kTanhReach) x[i] = copysignf(fmaf(-2.f * out, rcp_approx(1.f + exp2_approx(fabsf(u[i]) * 2.885390082f)), out), u[i]);
+  }
+}
+// u of a product is it times this, of a row's constant and 1 / out: a number, so that a product of 0 stays 0
+__device__ __forceinline__ float cap_constant(float con, float inverse) { return fminf(con * inverse, 0x1.fffffep127f); }
 // floor(a * b / c), floor((a + 1) * b / c), ... of tile numbers: in 32 bits where they are enough (64-bit divisions took 0.5 us of the
 // smallest calls)
 __device__ __forceinline__ constexpr long long div_short(long long a, long long c) {

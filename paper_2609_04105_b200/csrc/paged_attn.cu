@@ -791,7 +791,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t o_at = tmem + lanes + C::kO + D * group;
     float2* const ml = reinterpret_cast<float2*>(sgen + C::kOffML);
-    const float cap_in = p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f, cap_inverse = p.cap > 0.f ? __fdiv_rn(1.f, cap_out) : 0.f;
+    const float cap_out = p.cap * 1.4426950408889634f, cap_inverse = p.cap > 0.f ? __fdiv_rn(1.f, cap_out) : 0.f;
     int meet_phase = 0, done = 0;                                     // done: tiles of this CTA's run
     uint32_t n = 0;                                                   // jobs of this group
     // the group's last product on O.  (A barrier for each place: scores of a job say that the product before the last is done, so the last one is the
@@ -870,6 +870,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
           auto refer = [&] {
             float top = -INFINITY;
             const int in_tile0 = two ? 64 - 64 * (i & 1) : 64 * group;
+            const float c = CAP || (ANY && p.cap > 0.f) ? cap_constant(con, cap_inverse) : con;
 #pragma unroll 1
             for (int k = c_first; k < c_end; ++k) {
               uint32_t a[16];
@@ -887,12 +888,19 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               }
               tmem_wait_ld();
               if (ANY || change) {
+                float y[16];
+#pragma unroll
+                for (int x = 0; x < 16; ++x) y[x] = __uint_as_float(a[x]) * c;
+                if (CAP || (ANY && p.cap > 0.f)) {
+                  float u[16];
+#pragma unroll
+                  for (int x = 0; x < 16; ++x) u[x] = y[x];
+                  cap_scores(y, u, cap_out);
+                }
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
-                  float y = __uint_as_float(a[x]) * con;
-                  if (CAP || (ANY && p.cap > 0.f)) y = cap_score(y, cap_in, cap_out);
-                  if (ANY) y = fmaf(-slope, fabsf(far - (float)x), y);
-                  a[x] = seen & 1u << x ? __float_as_uint(y) : 0xFF800000u;
+                  if (ANY) y[x] = fmaf(-slope, fabsf(far - (float)x), y[x]);
+                  a[x] = seen & 1u << x ? __float_as_uint(y[x]) : 0xFF800000u;
                 }
                 if (change) tmem_st_32x32b_x16(s_job + 16 * k, a);
               }
@@ -905,8 +913,13 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               top = fmaxf(top, t2);
             }
             if (!ANY && !change) {
-              top *= con;
-              if (CAP) top = cap_score(top, cap_in, cap_out);
+              top *= c;
+              if (CAP) {
+                float x[2];
+                const float u[2] = {top, 0.f};
+                cap_scores(x, u, cap_out);
+                top = x[0];
+              }
             }
             if (change) tmem_wait_st();
             if (m == -INFINITY) m = top;                              // (so far nothing: its sum and O are 0)
@@ -946,18 +959,13 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
               for (int x = 0; x < 8; x += 2) {
                 const float r0 = __uint_as_float(raw[y + x]), r1 = __uint_as_float(raw[y + x + 1]);
                 if (HOW == kCapped) {
-                  // tanh u = u P(u^2) to 2^-21 for |u| up to 1.25 (P: least maximum error, by Lawson's weights): nine multiply-adds for two scores,
-                  // where an exponential and a reciprocal each are 32 clocks of the special-function unit for a warp, as much again as exp2 twice over
+                  // (ten instructions for two scores, where an exponential and a reciprocal each are 32 clocks of the special-function unit for a warp, as much
+                  // again as exp2 twice over)
                   float u0, u1, w0, w1, t0, t1;
                   mul_pair(u0, u1, r0, r1, c2, c2);
                   mul_pair(w0, w1, u0, u1, u0, u1);
                   wide = max3(wide, w0, w1);
-                  fma_pair(t0, t1, w0, w1, 5.25480427e-4f, 5.25480427e-4f, -4.32547880e-3f, -4.32547880e-3f);
-                  fma_pair(t0, t1, t0, t1, w0, w1, 1.76362153e-2f, 1.76362153e-2f);
-                  fma_pair(t0, t1, t0, t1, w0, w1, -5.16446717e-2f, -5.16446717e-2f);
-                  fma_pair(t0, t1, t0, t1, w0, w1, 1.32648021e-1f, 1.32648021e-1f);
-                  fma_pair(t0, t1, t0, t1, w0, w1, -3.33242148e-1f, -3.33242148e-1f);
-                  fma_pair(t0, t1, t0, t1, w0, w1, 9.99996483e-1f, 9.99996483e-1f);
+                  tanh_pair(t0, t1, w0, w1);
                   mul_pair(u0, u1, u0, u1, cap_out, cap_out);
                   fma_pair(z[x], z[x + 1], t0, t1, u0, u1, shift, shift);
                 } else if (HOW == kBiased) {
@@ -994,10 +1002,10 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
                 c2 = change ? 1.f : con;
                 pass(std::integral_constant<int, kScaled>());
               } else {
-                c2 = CAP ? con * cap_inverse : con;
+                c2 = CAP ? cap_constant(con, cap_inverse) : con;
                 if (ANY) shift -= slope * (float)(pos - first);
                 pass(std::integral_constant<int, SCORES>());
-                if (CAP && rare(__any_sync(0xffffffffu, wide > 1.25f * 1.25f))) {
+                if (CAP && rare(__any_sync(0xffffffffu, wide > kTanhReach))) {
                   change = sure = true;
                   continue;
                 }

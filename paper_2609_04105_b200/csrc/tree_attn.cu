@@ -1085,7 +1085,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
     uint32_t qf[NT][kSteps][2];                                     // Q^T: rows 8n + lane / 4
     int from[NT][2], until[NT][2], at[NT][2], plain_from = 0, plain_until = 0;     // PAGED: keys that rows 8n + 2c, + 1 see, where they stand; that all rows see
     float slope[NT][2];
-    const float cap_in = PAGED && p.cap > 0.f ? __fdiv_rn(2.f, p.cap) : 0.f, cap_out = p.cap * 1.4426950408889634f;
+    const float cap_out = p.cap * 1.4426950408889634f, cap_inverse = PAGED && p.cap > 0.f ? __fdiv_rn(1.f, cap_out) : 0.f;
     float con[NT][2], ref[NT][2], l[NT][2];                         // of rows 8n + 2c, + 1: score constant, kShift minus the reference, sum
     float o[kSteps][NT][4];
 #pragma unroll 1
@@ -1166,6 +1166,7 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             con[n][y] = __shfl_sync(0xffffffffu, mine, (2 * c + y) * 4);
+            if (PAGED && p.cap > 0.f) con[n][y] = cap_constant(con[n][y], cap_inverse);
             ref[n][y] = INFINITY;
             l[n][y] = 0.f;
           }
@@ -1249,12 +1250,20 @@ __global__ void __launch_bounds__(WarpCfg<FMT, D, NT>::kThreads, WarpCfg<FMT, D,
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
+              for (int y = 0; y < 8; ++y) s[n][y] *= con[n][y & 1];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              if (p.cap > 0.f) {
+                cap_scores(x[n], s[n], cap_out);
+#pragma unroll
+                for (int y = 0; y < 8; ++y) s[n][y] = x[n][y];
+              }
+#pragma unroll
               for (int y = 0; y < 8; ++y) {
                 const int tok = tok_k + kSecondStep * (y >> 2) + kSecondRow * (y >> 1 & 1), pos = w.first + tok0 + tok;
-                float z = s[n][y] * con[n][y & 1];
-                if (p.cap > 0.f) z = cap_score(z, cap_in, cap_out);
-                s[n][y] = fmaf(-slope[n][y & 1], fabsf((float)(at[n][y & 1] - pos)), z);
+                s[n][y] = fmaf(-slope[n][y & 1], fabsf((float)(at[n][y & 1] - pos)), s[n][y]);
               }
+            }
           }
         } else if (rare(!plain)) {
 #pragma unroll 1
