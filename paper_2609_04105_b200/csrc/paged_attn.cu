@@ -468,7 +468,8 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
       }
       __syncwarp();
       n += it.tiles > 0;
-      // Q into L2, while the tiles before it are worked on
+      // Q into L2, while the tiles before it are worked on.  (Of a prefix's members some may have no tokens: what only those would see is nobody's loss.)
+      bool missing = false, someone = it.g < 0;
 #pragma unroll 1
       for (int r = lane; r < it.here && it.tiles; r += 32) {
         int b, tok, hl;
@@ -476,9 +477,10 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         const uint16_t* q = static_cast<const uint16_t*>(p.q) + b * p.q_sb + (long long)(kvh * p.group + hl) * p.q_sh + tok * p.q_sn;
         asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
         if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
+        if (it.g >= 0) someone |= tok < tokens_of(p, b);
       }
       const int room = (d.g >= 0 ? p.prefix_pages : p.cache.max_pages) << log_page;
-      lost |= it.tiles && d.need > d.hi && d.need > room;
+      missing |= it.tiles && d.need > d.hi && d.need > room;
       const int* const table = d.g >= 0 ? p.prefix_table + (size_t)d.g * p.prefix_pages : p.cache.table + (size_t)d.b * p.cache.max_pages;
       const uint8_t* const pages = p.cache.pages + (size_t)kvh * p.cache.record;
       const size_t page_bytes = (size_t)p.cache.kv_heads * p.cache.record;
@@ -487,7 +489,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         if (lane >= kTile >> log_page || pos >= d.hi || pos + P <= d.lo) return -1;
         const int id = load(table + (pos >> log_page));               // (d.hi is inside the table)
         if (id >= 0 && id < p.cache.num_pages) return id;
-        lost |= pos < d.need;
+        missing |= pos < d.need;
         return -1;
       };
       int page = page_at(it.first);
@@ -513,6 +515,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         }
         ++i;
       }
+      lost |= __any_sync(0xffffffffu, missing) && __any_sync(0xffffffffu, someone);
       if (left > 0 && going && ++u == d.rts * p.cache.kv_heads) {
         u = 0;
         do describe<ROWS>(p, ++x, d);
