@@ -526,8 +526,9 @@ int fp4attn_tree_attention(const fp4attn_view* q, int type, const fp4attn_cache*
  * positions that rows see.
  *
  * Precision as fp4attn_tree_attention (16-bit probabilities, fp32 scores, maxima, sums and O); a capped score is off by no more than 2^-19 of
- * itself, whatever the cap, a bias by no more than 2^-21 of its slope times the largest distance.  soft_cap is 0 or between 2^-60 and 2^60.  workspace: device memory
- * of the queried size, 32-byte aligned, for this call alone until it has run.  Two calls with the same arguments give the same bits.
+ * itself, whatever the cap, a bias by no more than 2^-21 of its slope times the largest distance.  soft_cap is 0 or between 2^-60 and 2^60.  O may be
+ * q itself (the same view); otherwise q, O and LSE must not overlap.  workspace: device memory of the queried size, 32-byte aligned, for this call
+ * alone until it has run.  Two calls with the same arguments give the same bits.
  */
 size_t fp4attn_paged_attention_workspace_bytes(int B, int H, int kv_heads, int T, int d);
 int fp4attn_paged_attention(const fp4attn_view* q, int type, const fp4attn_cache* cache, int B, int H, int T, const int* block_table,

@@ -382,7 +382,8 @@ def fp4attn_paged_attention(q: torch.Tensor, cache: QuantizedCache, block_table:
     fp16) -> (O of q's type [B,H,T,d], LSE fp32 [B,H,T]).  The tokens are in the cache, token t at position p = context[b] + t (int32 [B]);
     row t sees positions first[b,t] <= j < last[b,t] of those that are there (int32 [B,T]; None: from 0, up to p) - a document, a window, a prefix
     that sees itself whole.  Scores are soft_cap * tanh(score / soft_cap) (0: as they are) - slopes[h] * |p - j| (fp32 [H]; None: no bias).  A row
-    that sees nothing is 0, its LSE -infinity.  Rows t >= count[b] are left as they were (0 and -infinity in tensors that this call made)."""
+    that sees nothing is 0, its LSE -infinity.  Rows t >= count[b] are left as they were (0 and -infinity in tensors that this call made).
+    out may be q itself; otherwise q, out and lse must not overlap."""
     return (_native_module or _native()).paged_attention(q, cache, block_table, context, count, first, last, softmax_scale, soft_cap, slopes,
                                                          out, lse, status)
 

@@ -750,6 +750,7 @@ struct Attention {
     if (!plain(out_o, q.t->scalar_type(), rows * q.d, cache.device, true, &out_ptr) || !shaped(out_o, {q.B, q.H, q.N, q.d}) ||
         !plain(lse_o, at::kFloat, rows, cache.device, true, &lse_ptr) || !shaped(lse_o, {q.B, q.H, q.N}))
       return "out [B, H, T, d] of q's type and lse [B, H, T] float32 must be contiguous CUDA tensors on the cache's device";
+    if (overlaps(out_o, lse_o, rows)) return "out may be q, the same view of it; otherwise out, lse and q must not overlap";
     if (c10::GradMode::is_enabled() && (q.t->requires_grad() || (slopes && THPVariable_Unpack(slopes_o).requires_grad())))
       return "attention over a quantized cache takes no gradient: detach the inputs, or call under torch.no_grad()";
     return nullptr;
@@ -777,6 +778,20 @@ struct Attention {
   }
   void* workspace() const { return nw ? ws.data_ptr() : nullptr; }
   PyObject* give() { return Py_BuildValue("(NN)", out.release(), lse.release()); }
+
+ private:
+  // Tensors of the caller's over one another.  A row's Q has been read when its O is written, so O may lie where Q does; nothing else may: other
+  // rows' Q, or both outputs of a row, in one place.  (Of a q with gaps only the beginning is looked at: what lies in the gaps is not q.)
+  bool overlaps(PyObject* out_o, PyObject* lse_o, int64_t rows) const {
+    const auto meet = [](const void* a, int64_t na, const void* b, int64_t nb) {
+      return a && b && (const char*)a < (const char*)b + nb && (const char*)b < (const char*)a + na;
+    };
+    const int64_t out_bytes = rows * q.d * 2, q_bytes = q.t->is_non_overlapping_and_dense() ? out_bytes : 1;
+    Strided o;
+    const bool in_place = out_ptr && o.take(out_o, false) && o.same_view(q);
+    return meet(out_ptr, out_bytes, lse_ptr, rows * 4) || meet(lse_ptr, rows * 4, q.view.data, q_bytes) ||
+           (!in_place && meet(out_ptr, out_bytes, q.view.data, q_bytes));
+  }
 };
 
 // paged_attention(q, cache, block_table, context, count, first, last, softmax_scale, soft_cap, slopes, out, lse, status) -> (out, lse)

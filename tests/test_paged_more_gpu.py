@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from test_paged_gpu import _check_shared, _shared
-from test_serving_gpu import _bd, _gen, _i32, _randn
+from test_serving_gpu import _bd, _filled, _gen, _i32, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,54 @@ def test_a_prefix_of_sequences_without_tokens_is_nobodys_loss(members):
             Bd.fp4attn_shared_prefix_attention(q, cache, gone, _i32(lengths), _i32(starts), table, _i32(context), count=_i32(counts), status=status)
             assert status.item() == Bd.ERR_PAGE
             status.zero_()
+
+
+def _both(Bd, g, H, kv, T, d=64, P=16):
+    """Calls of either operator that take q and the tensors of the caller's, of 2 sequences whose items fall to several blocks."""
+    context = [700, 90]
+    cache, table = _filled(Bd, g, "e4m3", 2, kv, P, d, max(context) + T)
+    paged = lambda q, **kw: Bd.fp4attn_paged_attention(q, cache, table, _i32(context), **kw)
+    capped = lambda q, **kw: Bd.fp4attn_paged_attention(q, cache, table, _i32(context), soft_cap=20.0, **kw)
+    shared = lambda q, **kw: Bd.fp4attn_shared_prefix_attention(q, cache, table[:1], _i32([300]), _i32([0, 2]), table, _i32(context), **kw)
+    return (paged, capped) + ((shared,) if T <= 64 else ())
+
+
+def test_outputs_over_one_another():
+    """Both outputs in one place, LSE over q, O over q in another order or shifted: rows would be overwritten that others have still to read, or twice."""
+    Bd, g = _bd(), _gen(91)
+    H, kv, T, d = 4, 2, 3, 64
+    room = _randn(g, 4 * 2 * H * T * d)
+    n = 2 * H * T * d
+    q = room[:n].view(2, H, T, d)
+    kept = room.clone()
+    for call in _both(Bd, g, H, kv, T):
+        lse = lambda at: room[at:at + 4 * H * T].view(torch.float32).view(2, H, T)
+        for kw in (dict(out=room[8:n + 8].view(2, H, T, d)), dict(out=room[n - 8:2 * n - 8].view(2, H, T, d)), dict(lse=lse(0)), dict(lse=lse(n - 8)),
+                   dict(out=room[n:2 * n].view(2, H, T, d), lse=lse(n)), dict(out=room[n:2 * n].view(2, H, T, d), lse=lse(2 * n - 8))):
+            with pytest.raises(AssertionError, match="overlap"):
+                call(q, **kw)
+        with pytest.raises(AssertionError, match="overlap"):
+            call(room[:n].view(2, T, H, d).transpose(1, 2), out=q)
+        with pytest.raises(AssertionError, match="overlap"):
+            call(q[:1].expand(2, H, T, d), out=q)
+        assert torch.equal(room, kept)
+        # side by side, and in the gaps of one another, nothing overlaps
+        want = call(q)
+        got = call(q, out=room[n:2 * n].view(2, H, T, d), lse=lse(2 * n))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        wide = torch.zeros(2, 3 * H * T * d, dtype=q.dtype, device="cuda")
+        apart = wide[:, :H * T * d].unflatten(1, (H, T, d))
+        apart.copy_(q)
+        inside = wide[0, H * T * d:].view(2, H, T, d)
+        assert torch.equal(call(apart, out=inside)[0], want[0])
+        room.copy_(kept)
+
+
+@pytest.mark.parametrize("T", [1, 7, 40, 200])
+def test_outputs_over_the_queries_themselves(T):
+    Bd, g = _bd(), _gen(T)
+    for call in _both(Bd, g, 8, 2, T):
+        q = _randn(g, 2, 8, T, 64)
+        want = call(q)
+        got = call(q, out=q)
+        assert got[0] is q and torch.equal(q, want[0]) and torch.equal(got[1], want[1])
