@@ -577,8 +577,10 @@ int fp4attn_pages_assign(const fp4attn_page_pool* pool, int B, int N, int* block
 /*
  * Pages back onto the stack: of entry b, whose length[b] tokens hold ceil(length[b] / page_size) pages, those behind the first keep[b] tokens'
  * (int32 [B]; NULL: 0, all of them).  Their places in the table become -1; places that hold no page of the pool are passed over.  The last page of
- * the last entry goes down first, so that a release of what one assign gave leaves the stack as it was.  More pages than the pool has (one
- * released twice) are dropped and reported (FP4ATTN_ERR_PAGE).  workspace: device memory, 4-byte aligned.
+ * the last entry goes down first, so that a release of what one assign gave leaves the stack as it was.  What goes back must have been taken, once:
+ * pages are not looked for among the free ones, and one that is released twice (by two entries whose tables share it, or in two calls) is free twice,
+ * so that two entries get it later.  Only what the stack has no room for is dropped and reported (FP4ATTN_ERR_PAGE).  workspace: device memory of
+ * the queried size, 4-byte aligned.
  */
 size_t fp4attn_pages_release_workspace_bytes(int B);
 int fp4attn_pages_release(const fp4attn_page_pool* pool, int B, int* block_table, int max_pages, const int* length, const int* keep,

@@ -434,7 +434,8 @@ def fp4attn_pages_assign(pool: PagePool, block_table: torch.Tensor, start: torch
 def fp4attn_pages_release(pool: PagePool, block_table: torch.Tensor, length: torch.Tensor, keep: Optional[torch.Tensor] = None,
                           status: Optional[torch.Tensor] = None) -> None:
     """The pages of sequences of length[b] tokens (int32 [B]) back into the pool, but those of the first keep[b] tokens (int32 [B]; None: 0);
-    their places in block_table become -1.  Undoes an assign exactly: keep what there was before it."""
+    their places in block_table become -1.  Undoes an assign exactly: keep what there was before it.  A page must go back once: one that two tables
+    share is released by one of them.  (Released twice it is free twice, without an error unless the pool overflows, and two sequences get it later.)"""
     (_native_module or _native()).pages_release(pool, block_table, length, keep, status)
 
 

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from oracle import serving as S
 from test_paged_gpu import _check_shared, _shared
 from test_serving_gpu import _bd, _filled, _gen, _i32, _randn
 
@@ -82,3 +83,28 @@ def test_outputs_over_the_queries_themselves(T):
         want = call(q)
         got = call(q, out=q)
         assert got[0] is q and torch.equal(q, want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_page_released_twice_is_free_twice():
+    """As documented: while other pages are held nobody notices, and two sequences get the page.  Of a page that two tables share, one lets go: the other
+    keeps its first 16 tokens' pages."""
+    Bd, P = _bd(), 16
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def shared():
+        pool, table = Bd.fp4attn_pages_create(12, P), torch.full((3, 4), -1, dtype=torch.int32, device="cuda")
+        Bd.fp4attn_pages_assign(pool, table, _i32([0, 16, 0]), _i32([48, 16, 64]))
+        table[1, 0] = table[0, 0]
+        return pool, table
+
+    for keep, left in (([0, 0, 64], 9), ([0, 16, 64], 8)):
+        pool, table = shared()
+        free, want = pool.free.tolist(), table.tolist()
+        assert pool.count.item() == 4 and want == [[0, 1, 2, -1], [0, 3, -1, -1], [4, 5, 6, 7]]
+        Bd.fp4attn_pages_release(pool, table, _i32([48, 32, 64]), keep=_i32(keep), status=status)
+        assert S.pages_release(free, 4, want, [48, 32, 64], keep, P) == (left, True)
+        assert status.item() == 0 and pool.count.item() == left and pool.free.tolist() == free and table.tolist() == want
+        assert free[:left].count(0) == (2 if left == 9 else 1)
+    # twice in two calls, with too little room on the stack for all of them: the ones that have none are reported
+    Bd.fp4attn_pages_release(pool, table, _i32([0, 16, 64]), status=status)
+    assert status.item() == Bd.ERR_PAGE and pool.count.item() == 12
