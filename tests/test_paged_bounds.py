@@ -27,3 +27,17 @@ def test_token_and_head_by_a_multiplication():
     for d in range(1, 65):                                          # tokens of a call; of a group
         n = np.arange(65535 * d + 256, dtype=np.uint64)[:: 1 if d < 4 else 61]
         assert np.array_equal(n * np.uint64(-(-2 ** 36 // d)) >> np.uint64(36), n // np.uint64(d))
+
+
+@pytest.mark.parametrize("B,kv", [(1, 1), (32, 8), (5, 3)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_workspace_of_a_step_is_that_of_the_kernel_that_runs(lib, d, B, kv):  # noqa: F811
+    """Rows of a KV head that go to the kernel of warps whatever the format and the masks: two partial results (O, maximum, sum) of its row tile per block."""
+    for group, T in ((1, 1), (4, 1), (8, 1), (4, 2), (1, 7)) + (((16, 1), (9, 1), (4, 3)) if d == 64 else ()):
+        R = 8 if group * T <= 8 else 16
+        n = lib.fp4attn_paged_attention_workspace_bytes(B, group * kv, kv, T, d)
+        assert 0 < n <= 2 * 640 * R * (4 * d + 8) + 8 * B * kv + 32
+    # with more of them no call may ask for less than 128 rows in lanes leave
+    for rows in (17, 33, 64, 200):
+        assert lib.fp4attn_paged_attention_workspace_bytes(B, kv, kv, rows, d) >= 2 * 148 * 128 * (4 * d + 8)
+    assert lib.fp4attn_paged_attention_workspace_bytes(B, 9 * kv, kv, 1, 128) >= 2 * 148 * 128 * (4 * 128 + 8)          # NVFP4 with a mask
