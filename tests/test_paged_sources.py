@@ -34,3 +34,9 @@ def test_the_last_copies_are_waited_for_whatever_the_abort_word_says():
         drains = len(re.findall(r"\bdrain\([^;]*RING_FULL\), (?:pages\.i|parts)\);", code))
         drains += len(re.findall(r"if \(threadIdx\.x < 2 \* C::kStages\)\s*for \(int spin = 0; spin < \(1 << 10\) && !mbar_try_wait\(full", code))
         assert drains == kernels
+
+
+@pytest.mark.parametrize("name", ["cache_attn.cuh", "paged_attn.cu", "pages.cu"])
+def test_no_pointer_is_said_to_be_the_only_one(name):
+    """As of the other serving kernels: a load through `const T* __restrict__` may become one that is not coherent."""
+    assert "__restrict__" not in _code(name)
