@@ -148,11 +148,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         if (++s == C::NST) { s = 0; ph ^= 1; st = sbase + C::OFF_STAGE; }
       }
     }
-    if (*abortf && lane == 0) {
-      // bounded drain: give copies still in flight time to land before the CTA retires
-      for (int r = 0; r < C::NST; ++r)
-        for (int spin = 0; spin < (1 << 12) && !mbar_try_wait(bar_full(r), 0) && !mbar_try_wait(bar_full(r), 1); ++spin) {}
-    }
+    if (*abortf) let_copies_land();                               // before the CTA retires
     __syncwarp();
   } else if (warp == 1) {
     // ===================================================================== QK issuer: S = Q K^T, one stage per issue

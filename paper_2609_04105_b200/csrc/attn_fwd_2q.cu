@@ -161,10 +161,7 @@ attn_fwd_2q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (++s == C::NST) { s = 0; ph ^= 1; st = sbase + C2::OFF_STAGE; }
       }
     }
-    if (*abortf && lane == 0) {
-      for (int r = 0; r < C::NST; ++r)
-        for (int spin = 0; spin < (1 << 12) && !mbar_try_wait(bar_full(r), 0) && !mbar_try_wait(bar_full(r), 1); ++spin) {}
-    }
+    if (*abortf) let_copies_land();                               // before the CTA retires
     __syncwarp();
   } else if (warp == 1) {
     // ===================================================================== QK issuer: per stage S_q = Q_q K^T for q = 0, 1

@@ -233,12 +233,7 @@ attn_fwd_fp8pv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         }
       }
     }
-    if (*abortf && lane == 0) {
-      for (int r = 0; r < C8::KST; ++r)
-        for (int spin = 0; spin < (1 << 12) && !mbar_try_wait(k_full(r), 0) && !mbar_try_wait(k_full(r), 1); ++spin) {}
-      for (int r = 0; r < C8::VST; ++r)
-        for (int spin = 0; spin < (1 << 12) && !mbar_try_wait(v_full(r), 0) && !mbar_try_wait(v_full(r), 1); ++spin) {}
-    }
+    if (*abortf) let_copies_land();                               // before the CTA retires
     __syncwarp();
   } else if (warp == 1 || warp == kFirstSoftmaxWarp + 4 * kTeams) {
     // ===================================================================== QK issuers (both sweeps), one for the steps of either team pair

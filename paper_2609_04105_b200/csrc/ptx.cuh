@@ -96,6 +96,15 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
   return __all_sync(0xffffffffu, mbar_wait_thread(bar, parity, abort_at, limit));
 }
 
+// After a wait has run out: half a millisecond, in which copies that are under way, of some microseconds, land.  (By the clock: of a barrier's two parities
+// one has always come, so a look at both tells nothing, and which one the last copies have is known only inside the loop that issues them.)
+__device__ __forceinline__ void let_copies_land() {
+  uint32_t since, now;
+  asm volatile("mov.u32 %0, %%clock;" : "=r"(since));
+  do asm volatile("mov.u32 %0, %%clock;" : "=r"(now));
+  while (now - since < (1u << 20));
+}
+
 __device__ __forceinline__ void fence_barrier_init() {
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
