@@ -19,11 +19,12 @@
 // rows; those of fewer give it half of the keys of a tile, with a reference, a sum and an O of its own, joined at the item's end.
 //
 // Few rows (up to 16 a KV head; up to 8 in NVFP4 with d = 128) go to the kernel of warps in tree_attn.cu, and up to 32 with neither mask nor cap nor bias to its
-// roles, but for shared prefixes.
+// roles, but for shared prefixes.  (Rule and measurements: at few_rows there.)
 //
 // What bounds it: instructions.  A softmax warp executes one about every five clocks (waits, branches and instruction fetches among them), a job of 64
-// keys is some 250, and an item costs as much as three or four tiles (bringing Q, the first references, writing O).  2048 tokens of 32 heads over 8 behind 30720, d = 128,
-// NVFP4: 0.98 to 1.05 ms, 1020 to 1090 TFLOP/s (power: 1780 MHz); two prompts of 4096: 344 us, 800 TFLOP/s.  Beside the products of N = 64, whose operands
+// keys is some 250, and an item costs as much as three or four tiles (bringing Q, the first references, writing O).  All 19 warps have 96 registers, so that every instance
+// spills, 8 to 96 bytes of stores and 4 to 128 of loads a thread.  2048 tokens of 32 heads over 8 behind 30720, d = 128, NVFP4: 1.04 to 1.07 ms, 1000 to 1025
+// TFLOP/s (power: 1780 MHz); two prompts of 4096: 345 to 361 us, 760 to 800 TFLOP/s.  Beside the products of N = 64, whose operands
 // come from shared memory (48 clocks instead of 32) and which take longer to issue than to compute (90), exponentials do not count: without them nothing changes.
 //
 // A row's keys are walked from its last to its first: what a mask cuts off comes where a reference has to be looked for anyway, and a bias by distance falls

@@ -6,7 +6,9 @@
 // release  pages ceil(keep / P) .. ceil(length / P) - 1 of an entry's table go back, the call's last one first: what an assign took lies on the
 //          stack afterwards as it lay before.  Tables may have holes, so the pages are counted by a kernel of their own first.
 //
-// Bound by launches and by dependent loads (start - page - slot); a prompt's slots by writing them: 48 sequences of up to 16384 tokens are 9 MB.
+// Bound by launches and by dependent loads (start - page - slot); a prompt's slots by writing them: 48 sequences of up to 16384 tokens are 9 MB.  Every block
+// sums over all entries for itself (release: a block an entry), which is little up to some thousands of them and quadratic beyond: one token each, assigned and
+// released, 12 us for 1024 entries, 59 for 8192, 2.1 ms for 65535, the most there may be (of which the assign is 40 us).
 #include "kv_cache.cuh"
 
 namespace fp4attn {

@@ -1603,12 +1603,20 @@ int launch_few(const TreeParams& p, int R, bool changed, cudaStream_t st) {
 
 }  // namespace
 
-// With no mask, cap or bias the roles of 32 rows against 128 rows in lanes (paged_attn.cu), us:
-//   32 rows, 8 KV heads     1 x 1000      8 x 4096      16 x 16000
-//     NVFP4, d = 128      13.5 | 22.4   35.2 | 43.8   123 | 151
-//     E4M3, d = 128       13.6 | 22.1   35.5 | 44.3   122 | 208
-//     NVFP4, d = 64       12.3 | 17.4   32.3 | 33.9   112 | 121        (E4M3 alike)
-//   64 rows, NVFP4, d = 128: 15.7 | 22.6, 43.5 | 45.6, 185 | 160: left to the other, as is all that is masked, which has no roles of its own
+// The warps take up to 16 rows whatever the masks (8 where rows_of_tile says so); the roles, which know no masks, caps or biases, up to 32.  The roles of 32 or 64 rows
+// against 128 rows in lanes (paged_attn.cu), without any, 8 KV heads, us:
+//                       1 x 1000       8 x 4096       16 x 16000
+//   32 rows
+//     NVFP4, d = 128   13.5 | 22.4    35.2 | 43.8     123 | 151
+//     E4M3,  d = 128   13.6 | 22.1    35.5 | 44.3     122 | 208
+//     NVFP4, d = 64    12.3 | 17.4    32.3 | 33.9     112 | 121       (E4M3 alike)
+//   64 rows
+//     NVFP4, d = 128   15.4 | 22.3    44.0 | 45.2     196 | 159
+//     E4M3,  d = 128   16.2 | 22.6    45.3 | 46.6     189 | 211
+//     NVFP4, d = 64    12.6 | 17.4    36.9 | 35.3     178 | 136
+//     E4M3,  d = 64    13.5 | 17.3    38.2 | 35.0     179 | 133
+// One limit for every format and length: with 64 rows the lanes win where much is read in three of the four formats, by a fifth to a quarter, and lose 4 to 7 us on
+// short calls and a tenth in E4M3 with d = 128.  32 rows with a mask, cap or bias take the lanes for want of roles that know them: 24, 45 and 152 us (E4M3: 218).
 bool few_rows(int rows, int fmt, int d, bool changed) { return rows_of_tile(rows, fmt, d) <= (changed ? 16 : 32); }
 size_t few_rows_workspace(int B, int H, int kv_heads, int T, int d, int fmt) { return plan(B, H, kv_heads, T, d, fmt).total; }
 int launch_few_rows(const FewRows& a, void* workspace, cudaStream_t st) {
