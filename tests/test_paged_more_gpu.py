@@ -1,10 +1,11 @@
 """Attention of prompts and of shared prefixes over a paged cache: calls that padded and partly empty batches make, tensors that lie over one another."""
+import numpy as np
 import pytest
 import torch
 
 from oracle import serving as S
 from test_paged_gpu import _check_shared, _shared
-from test_serving_gpu import _bd, _filled, _gen, _i32, _randn
+from test_serving_gpu import _bd, _filled, _gen, _i32, _randn, _tree_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -108,3 +109,40 @@ def test_a_page_released_twice_is_free_twice():
     # twice in two calls, with too little room on the stack for all of them: the ones that have none are reported
     Bd.fp4attn_pages_release(pool, table, _i32([0, 16, 64]), status=status)
     assert status.item() == Bd.ERR_PAGE and pool.count.item() == 12
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(soft_cap=9.0), dict(slopes=True), dict(soft_cap=9.0, slopes=True)], ids=["scaled", "capped", "biased", "both"])
+@pytest.mark.parametrize("fmt", ["nvfp4", "e4m3"])
+@pytest.mark.parametrize("T,P", [(1, 64), (6, 16), (33, 128)])
+def test_shared_prefixes_what_nobody_sees(T, P, fmt, kw):
+    """Bytes of every token that no row sees are 0xFF, NaN as an E4M3 code or scale: behind a prefix's and a sequence's last token, drafted tokens that no mask
+    names, sequences without tokens, pages of nobody.  The same bits as with a cache that was written whole."""
+    Bd, g, rng = _bd(), _gen(T + P), np.random.default_rng(T)
+    H, kv, d = 4, 2, 64
+    prefixes, starts, context = [333, 61, 0], [0, 3, 5, 6], [130, 0, 7, 64, 31, 5, 200]
+    B, counts = len(context), [T, T, max(1, T - 2), T, 0, T, T]
+    cache, prefix_table, table = _shared(Bd, g, fmt, kv, P, d, prefixes, context, T)
+    q = _randn(g, B, H, T, d)
+    if kw.get("slopes"):
+        kw = dict(kw, slopes=torch.tensor([0.5, 0.0, -0.01, 0.1], device="cuda"))
+    for bits in (None, _tree_bits(rng, B, T) & torch.as_tensor(rng.integers(0, 2 ** 62, (B, 1)) | 1, device="cuda")):
+        call = lambda c: Bd.fp4attn_shared_prefix_attention(q, c, prefix_table, _i32(prefixes), _i32(starts), table, _i32(context), tree_mask=bits, count=_i32(counts), **kw)
+        want = call(cache)
+        held = np.zeros((len(cache.pages), P), bool)                # tokens that some row sees
+        for g_, n in enumerate(prefixes):
+            for pos in range(n):
+                held[int(prefix_table[g_, pos // P]), pos % P] = True
+        for b in range(B):
+            seen = set(range(context[b])) if counts[b] else set()
+            for t in range(counts[b]):
+                seen |= {context[b] + j for j in range(T) if (j <= t if bits is None else int(bits[b, t]) >> j & 1)}
+            for pos in seen:
+                held[int(table[b, pos // P]), pos % P] = True
+        kc, ks, vc, vs, _ = S.places(fmt, P, d)
+        raw = cache.pages.cpu().numpy().copy()
+        for page, t in zip(*np.nonzero(~held)):
+            for a in ([kc[t], vc[t]] if ks is None else [kc[t], ks[t], vs[t]]):
+                raw[page][:, a] = 255
+        got = call(Bd.QuantizedCache(torch.as_tensor(raw, device="cuda"), cache.k_G, cache.v_G, cache.fmt, P, d))
+        assert torch.isfinite(want[0]).all()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
