@@ -31,19 +31,17 @@ constexpr float kLag = 8.f;                // octaves by which a score may excee
 constexpr float kShift = 7.f;              // a probability of 1 is 2^7: with the lag just inside f16, whose subnormals then begin at 2^-21
 
 __device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
-// Waits for a barrier's phase; the whole warp goes on together.  A wait that runs out sets the abort word, and one that sees it set returns at once.
-// The answer, a thread's own: has the phase come?  Those who compute need not ask: what they then read and multiply means nothing, but stays in bounds, and
-// every wait of theirs ends at once, so that they run out of tiles.  Who brings copies must: a barrier that still expects bytes takes no second
-// arrival, and no copy may go where another is under way.  The phase has come at the first look, or while that look was suspended, in nearly
-// every wait.  CALL: the loop behind it is a function of its own: inlined at each wait it took up to 12 % of the time, in instruction
-// fetches.  (Code that shares out registers by setmaxnreg may not call.)
-__device__ __forceinline__ bool poll_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
+// Waits for a barrier's phase; the whole warp goes on together.  A wait that runs out, or sees that another one did, sets the abort word
+// and returns as if the phase had come: what the roles then read and multiply means nothing, but stays in bounds, and every wait of
+// theirs ends at once, so that they run out of tiles.  (Who brings copies asks given_up() behind it.)  The phase has come at the first look,
+// or while that look was suspended, in nearly every wait.  CALL: the loop behind it is a function of its own: inlined at each wait it took
+// up to 12 % of the time, in instruction fetches.  (Code that shares out registers by setmaxnreg may not call.)
+__device__ __forceinline__ void poll_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
   uint32_t since = 0;
   for (uint32_t n = 1;; ++n) {
     uint32_t gone;
     asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(gone) : "r"(abort_at) : "memory");
-    if (gone) return false;
-    if (mbar_try_wait(bar, parity)) return true;
+    if (gone || mbar_try_wait(bar, parity)) return;
     if (n % kPolls) continue;
     uint32_t now;
     asm volatile("mov.u32 %0, %%clock;" : "=r"(now));
@@ -51,15 +49,24 @@ __device__ __forceinline__ bool poll_phase(uint32_t bar, uint32_t parity, uint32
     if (now - since >= kWaitClocks) break;
   }
   asm volatile("st.volatile.shared.u32 [%0], 1;" ::"r"(abort_at) : "memory");
-  return false;
 }
-__device__ __noinline__ bool wait_longer(uint32_t bar, uint32_t parity, uint32_t abort_at) { return poll_phase(bar, parity, abort_at); }
+__device__ __noinline__ void wait_longer(uint32_t bar, uint32_t parity, uint32_t abort_at) { poll_phase(bar, parity, abort_at); }
 template <bool CALL>
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
-  bool come = true;
-  if (rare(!mbar_try_wait(bar, parity))) come = CALL ? wait_longer(bar, parity, abort_at) : poll_phase(bar, parity, abort_at);
+__device__ __forceinline__ void wait_phase(uint32_t bar, uint32_t parity, uint32_t abort_at) {
+  if (rare(!mbar_try_wait(bar, parity))) {
+    if (CALL) wait_longer(bar, parity, abort_at);
+    else poll_phase(bar, parity, abort_at);
+  }
   __syncwarp();
-  return come;
+}
+// Behind a wait for a stage, before anything is brought into it: has some wait run out?  Then those who read stages no longer wait for what
+// they read, so that the stage may seem free while its last copies are still under way: a barrier that still expects bytes takes no second
+// arrival, and no copy may go where another is.  (One who gives up sets the word before it arrives anywhere, so an arrival that is seen shows
+// it.  By a shuffle: a vote, or the wait's own answer voted on, made attention over trees of 64 tokens 2 to 3 % slower.)
+__device__ __forceinline__ bool given_up(uint32_t abort_at) {
+  uint32_t gone;
+  asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(gone) : "r"(abort_at) : "memory");
+  return __shfl_sync(0xffffffffu, gone, 0) != 0;
 }
 // which of N buffers, and the phase of its barriers
 template <int N>

@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
   const uint32_t abort_at = sbase + C::kOffBar + 8 * C::kBars, tslot = abort_at + 4;
   volatile uint32_t* const abort_word = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 8 * C::kBars);
   auto bar = [&](int i) { return sbase + C::kOffBar + 8u * i; };
-  auto wait = [&](int b, int phase) { return wait_phase<true>(bar(b), (uint32_t)phase, abort_at); };
+  auto wait = [&](int b, int phase) { wait_phase<true>(bar(b), (uint32_t)phase, abort_at); };
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i) {
@@ -502,7 +502,8 @@ __global__ void __launch_bounds__(PagedCfg<FMT, D, RT>::kThreads, 1) paged_kerne
         if (k + 1 < it.tiles) page = page_at(it.first - (k + 1) * kTile);            // (its entry comes while a stage is waited for)
 #pragma unroll 1
         for (int part = 0; part < 2; ++part) {
-          going = __all_sync(0xffffffffu, wait(C::RING_FREE + ring.at, ring.phase ^ 1));
+          wait(C::RING_FREE + ring.at, ring.phase ^ 1);
+          going = !given_up(abort_at);
           if (rare(!going)) break;
           if (lane == 0) {
             if (part == 0) valid_ring[i % C::kRing] = held;

@@ -341,7 +341,8 @@ struct Pages {
   __device__ __forceinline__ bool bring(const TreeParams& p, uint32_t stages, uint32_t full, uint32_t free, uint32_t abort_at, uint32_t* valid) {
     const int lane = threadIdx.x & 31;
     const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
-    if (rare(!__all_sync(0xffffffffu, wait_phase<CALL>(free + 8 * ring.at, ring.phase ^ 1, abort_at)))) return false;
+    wait_phase<CALL>(free + 8 * ring.at, ring.phase ^ 1, abort_at);
+    if (rare(given_up(abort_at))) return false;
     const int bytes = p.cache.record / PARTS;
     if (lane == 0) {
       valid[i % RING] = held;

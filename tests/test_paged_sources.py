@@ -8,19 +8,21 @@ from test_serving_sources import _code
 
 @pytest.mark.parametrize("name", ["tree_attn.cu", "paged_attn.cu"])
 def test_nothing_is_brought_into_a_stage_that_has_not_become_free(name):
-    """A wait that sees the abort word returns although its phase has not come.  An arrival at a barrier that still expects bytes is one too many, and a
-    copy into its stage would lie over one under way: between a wait for a stage and the arrival that announces a copy, the wait's answer ends the
-    bringing, for the whole warp alike."""
+    """A wait that sees the abort word returns although its phase has not come, and after that those who read stages free them unread.  An arrival at a barrier
+    that still expects bytes is one too many, and a copy into its stage would lie over one under way: between a wait for a stage and the arrival that
+    announces a copy, the abort word is looked at and ends the bringing, for the whole warp alike."""
     code = _code(name)
     places = [m.start() for m in re.finditer(r"\bmbar_arrive_expect_tx\(", code)]
     assert places
     for at in places:
-        wait = list(re.finditer(r"\bwait(_phase)?\b[^;]*;", code[:at]))[-1]
-        statement = code[code.rfind(";", 0, wait.start()) + 1:at]
-        assert "__all_sync(0xffffffffu, wait" in statement and re.search(r"\b(break|return false);", statement), statement
+        wait = list(re.finditer(r"\bwait(_phase<CALL>)?\([^;]*;", code[:at]))[-1]
+        between = code[wait.end():at]
+        assert re.search(r"given_up\(abort_at\)", between) and re.search(r"\b(break|return false);", between), between
     # nobody goes on as if a part had been brought
     for m in re.finditer(r"[^;{}]*\bpages\.bring\(", code):
         assert "!pages.bring(" in m.group(), m.group()
+    body = re.search(r"\bbool given_up\(.*?\n}", _code("cache_attn.cuh"), re.S).group()
+    assert "ld.volatile.shared" in body and "return __shfl_sync(0xffffffffu, gone, 0)" in body          # the word itself, one answer for the warp
 
 
 def test_the_last_copies_are_waited_for_whatever_the_abort_word_says():
